@@ -363,6 +363,113 @@ cc_status cc_compact_rows(const cc_problem* p, void* rows, int32_t row_bytes,
                           void* out_rows, void* workspace, size_t workspace_bytes,
                           void* stream);
 
+/* ------------------------------------------------------------------ cache in 8 bits */
+
+/* A KV cache in 8 bits: OCP E4M3 codes, and for each block of scale_block consecutive
+ * entries of one (sequence, layer, KV head) one power-of-two scale, stored as the exponent
+ * byte x of the scale 2^(x-127) (E8M0; 0 and 255 are never written and read as 2^-127 and
+ * 2^127).  An entry's element is code * scale.
+ * `codes` has the fields of a cc_kv, its elements being bytes (strides in bytes, multiples
+ * of 16).  The scale of token t is at
+ *   CONTIGUOUS: k_scale + b*scale_seq_stride + l*scale_layer_stride + h*scale_head_stride
+ *               + t/scale_block
+ *   PAGED:      k_scale + l*scale_layer_stride + page*scale_page_stride
+ *               + h*scale_head_stride + slot/scale_block
+ * (v_scale alike).  scale_block: a power of two from 16 to 128, at most page_size. */
+typedef struct cc_kv8 {
+  cc_kv codes;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int64_t scale_seq_stride;    /* CONTIGUOUS only */
+  int64_t scale_layer_stride;
+  int64_t scale_head_stride;
+  int64_t scale_page_stride;   /* PAGED only */
+  int32_t scale_block;
+} cc_kv8;
+
+/* ------------------------------------------------------------------ appending */
+
+/* Rows of new tokens: element (layer l, token i, head h, e) is at
+ * base + l*layer_stride + i*tok_stride + h*head_stride + e (strides in elements; rows of
+ * head_dim elements are contiguous and 16-byte aligned).  Slices of one fused projection
+ * output are such views. */
+typedef struct cc_rows {
+  const void* base;
+  int64_t layer_stride, tok_stride, head_stride;
+} cc_rows;
+
+/* What is appended.  The problem's cu_seqlens count the NEW tokens of each sequence (0 is
+ * valid), M = cu_seqlens[n_seqs] in all; cached[b] entries are in the cache before. */
+typedef struct cc_append {
+  cc_rows k, v;                /* [n_layers][M][Hkv][head_dim] in p->dtype */
+  cc_rows q;                   /* base NULL: none; [M][Hq][head_dim], n_layers = 1 only */
+  void* q_out;                 /* with q: [M][Hq][head_dim] packed, in p->dtype; may be q
+                                  itself where q is packed like that */
+  const int32_t* cached;       /* device [n_seqs] */
+  const int32_t* pos_ids;      /* device [M] original positions, NULL -> cached[b] + i */
+  int64_t capacity;            /* entries that a sequence's place in the cache holds.  Paged:
+                                  0 selects max_pages * page_size, which is also the limit */
+  int32_t layer;               /* first cache layer written */
+  int32_t n_layers;            /* layers written, >= 1 */
+  int32_t rotate;              /* 1: k and q are rotated (elements e and e + head_dim/2 by
+                                  position * rope_theta^(-2e/head_dim)); 0: they are already */
+} cc_append;
+
+/* Appends the new tokens' keys and values to a cache in p->dtype, at entries cached[b],
+ * cached[b] + 1, ... of each sequence, rotating keys on the way (angles in fp64, the
+ * rotation in fp32, one rounding to the cache's type); rotates q into q_out alike.  Tokens
+ * at or past the capacity, and those whose page id is negative, are not written.  `cached`
+ * is read on the device, so a captured call follows lengths that advance between replays.
+ * No other entry is touched.  Sequences must not share pages that are written. */
+cc_status cc_append_kv(const cc_problem* p, const cc_append* a, const cc_kv* kv, void* stream);
+
+/* The same into a cache in 8 bits (p->dtype: the type of k, v and q; fp32 values are
+ * rounded once).  A block that held no entry gets the smallest scale s = 2^e, e >= -100, with
+ * max |x| <= 448 s over its new elements; a block that held some keeps the larger of that
+ * and its scale, its entries' codes being rounded again where the scale grows (exact but for
+ * elements below 2^-6 of the new scale).  Codes are E4M3(x / s), nearest even; NaN and infinities
+ * become NaN codes and do not count for the scale. */
+cc_status cc_append_kv8(const cc_problem* p, const cc_append* a, const cc_kv8* kv, void* stream);
+
+/* ------------------------------------------------------------------ compaction in 8 bits */
+
+/* cc_compact_kv on a cache in 8 bits: the kept entries move to the front of their planes.
+ * A destination block gets the smallest scale s = 2^e, e >= -100, with max |x| <= 448 s over the
+ * kept elements in it (NaN not counted), and their codes are rounded again (exact but for
+ * elements below 2^-6 of the new scale; NaN codes stay).  keep_idx, k_h, per_head,
+ * token_ids and pos_ids as in cc_compact_kv; `out` NULL compacts in place, else a cache of
+ * the same layout, layers and scale_block that does not overlap kv.  Codes past entry k_b
+ * and scales past its block are left untouched.  Needs no workspace. */
+cc_status cc_compact_kv8(const cc_problem* p, const cc_kv8* kv, const int32_t* keep_idx,
+                         const int32_t* k_h, int32_t per_head, int32_t* token_ids,
+                         int32_t* pos_ids, const cc_kv8* out, void* stream);
+
+/* ------------------------------------------------------------------ attention in 8 bits */
+
+/* Which entries a query attends to.  With n_b = kv_lens[b] entries in the cache and m_b
+ * queries in the call, query i of a sequence stands at entry n_b - m_b + i (the queries are
+ * the last entries).  CAUSAL: entries up to and including its own.  COUNTER_CAUSAL: those
+ * after its own (p->diag STRICT) or from its own on (INCLUSIVE).  A query with no entry to
+ * attend to (one that stands before the first, too) has a zero output. */
+typedef enum cc_mask { CC_MASK_CAUSAL = 0, CC_MASK_COUNTER_CAUSAL = 1 } cc_mask;
+
+/* Workspace for cc_attention_kv8 (partial results of rows whose entries are shared out). */
+cc_status cc_attention_kv8_workspace(const cc_problem* p, int32_t mask, int32_t max_kv_len,
+                                     size_t* bytes);
+
+/* Attention over layer `layer` of a cache in 8 bits: o[i][h][:] = sum_j softmax_j(scale *
+ * q[i][h] . k[j][c]) v[j][c], c = h / g, over the entries that `mask` allows.  The problem's
+ * cu_seqlens count the QUERIES of each sequence; q, o: [N][Hq][head_dim] bf16, packed, not
+ * overlapping.  kv_lens: device [n_seqs] entries in the cache (the queries' own among them),
+ * read on the device; max_kv_len: host, at least every kv_lens[b] (longer ones are cut there, negative
+ * ones are 0), sizes the launch and the workspace.  Entries past kv_lens[b] are not
+ * read, and one that a query may not attend to does not reach it, whatever it holds; a NaN
+ * code in one that it attends to gives NaN.  Sums, maxima and outputs are kept in
+ * fp32 until the last rounding; the probabilities enter the second product in bf16. */
+cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv, int32_t layer,
+                           int32_t mask, const int32_t* kv_lens, int32_t max_kv_len, void* o,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,6 +26,7 @@ CC_F32, CC_BF16 = 0, 1
 CC_DIAG_STRICT, CC_DIAG_INCLUSIVE = 0, 1
 CC_MODE_LAST_LAYER, CC_MODE_FULL, CC_MODE_LAST_LAYER_H, CC_MODE_LAST_LAYER_FUSED = 0, 1, 2, 3
 CC_KV_CONTIGUOUS, CC_KV_PAGED = 0, 1
+CC_MASK_CAUSAL, CC_MASK_COUNTER_CAUSAL = 0, 1
 
 EXPORTED = [
     "cc_status_str", "cc_version", "cc_score_workspace", "cc_score", "cc_attention_workspace",
@@ -34,7 +35,8 @@ EXPORTED = [
     "cc_compact_rows_workspace", "cc_compact_rows", "cc_fuse_wo_lmhead_workspace",
     "cc_fuse_wo_lmhead", "cc_quantize_fp8_workspace", "cc_quantize_fp8",
     "cc_lmhead_fp8_workspace", "cc_lmhead_score_fp8", "cc_pack_lmhead_bytes", "cc_pack_lmhead",
-    "cc_lmhead_score_packed", "cc_lmhead_score_noalloc",
+    "cc_lmhead_score_packed", "cc_lmhead_score_noalloc", "cc_append_kv", "cc_append_kv8",
+    "cc_compact_kv8", "cc_attention_kv8_workspace", "cc_attention_kv8",
 ]
 
 _c_void_p = ctypes.c_void_p
@@ -69,6 +71,23 @@ class c_inputs(ctypes.Structure):
                 ("w_o", _c_void_p), ("w_lm", _c_void_p), ("embed", _c_void_p),
                 ("layers_h", ctypes.POINTER(c_layer_weights)), ("final_norm", _c_void_p),
                 ("h_last", _c_void_p), ("w_lm_packed", _c_void_p)]
+
+
+class c_kv8(ctypes.Structure):
+    _fields_ = [("codes", c_kv), ("k_scale", _c_void_p), ("v_scale", _c_void_p),
+                ("scale_seq_stride", _i64), ("scale_layer_stride", _i64),
+                ("scale_head_stride", _i64), ("scale_page_stride", _i64), ("scale_block", _i32)]
+
+
+class c_rows(ctypes.Structure):
+    _fields_ = [("base", _c_void_p), ("layer_stride", _i64), ("tok_stride", _i64),
+                ("head_stride", _i64)]
+
+
+class c_append(ctypes.Structure):
+    _fields_ = [("k", c_rows), ("v", c_rows), ("q", c_rows), ("q_out", _c_void_p),
+                ("cached", _c_void_p), ("pos_ids", _c_void_p), ("capacity", _i64),
+                ("layer", _i32), ("n_layers", _i32), ("rotate", _i32)]
 
 
 def _load():
@@ -117,6 +136,13 @@ def _load():
         "cc_compact_rows_workspace": (st, [P(c_problem), _i32, _i32, sz]),
         "cc_compact_rows": (st, [P(c_problem), _c_void_p, _i32, _c_void_p, P(_i32), _i32,
                                  _c_void_p, _c_void_p, ctypes.c_size_t, _c_void_p]),
+        "cc_append_kv": (st, [P(c_problem), P(c_append), P(c_kv), _c_void_p]),
+        "cc_append_kv8": (st, [P(c_problem), P(c_append), P(c_kv8), _c_void_p]),
+        "cc_compact_kv8": (st, [P(c_problem), P(c_kv8), _c_void_p, P(_i32), _i32, _c_void_p,
+                                _c_void_p, P(c_kv8), _c_void_p]),
+        "cc_attention_kv8_workspace": (st, [P(c_problem), _i32, _i32, sz]),
+        "cc_attention_kv8": (st, [P(c_problem), _c_void_p, P(c_kv8), _i32, _i32, _c_void_p, _i32,
+                                  _c_void_p, _c_void_p, ctypes.c_size_t, _c_void_p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -164,6 +190,9 @@ def _stream(stream=None):
 
 def _workspace(nbytes: int, device) -> torch.Tensor:
     return torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=device)
+
+
+_DTYPES = {CC_F32: torch.float32, CC_BF16: torch.bfloat16}
 
 
 # ---------------------------------------------------------------- descriptors
@@ -514,3 +543,149 @@ def cc_compact_rows(p: Problem, rows: torch.Tensor, keep_idx: torch.Tensor, k: S
     _check(_lib.cc_compact_rows(ctypes.byref(p.struct), _ptr(rows), row_bytes, _ptr(keep_idx), kk,
                                 per_head, _ptr(out), _ptr(workspace), workspace.numel(),
                                 _stream(stream)), "cc_compact_rows")
+
+
+# ---------------------------------------------------------------- cache in 8 bits
+
+@dataclass
+class KV8:
+    """A cc_kv8 view (E4M3 codes, E8M0 scales) plus the tensors it points at."""
+    struct: c_kv8
+    keep: list = field(default_factory=list)
+
+
+def _kv8(codes: KV, k_scale: torch.Tensor, v_scale: torch.Tensor, scale_block: int, seq: int,
+         layer: int, head: int, page: int) -> KV8:
+    for t in (*codes.keep[:2], k_scale, v_scale):
+        if t.element_size() != 1:
+            raise ValueError(f"codes and scales are bytes, got {t.dtype}")
+    s = c_kv8()
+    s.codes = codes.struct
+    s.k_scale, s.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+    s.scale_seq_stride, s.scale_layer_stride, s.scale_head_stride, s.scale_page_stride = seq, layer, head, page
+    s.scale_block = scale_block
+    return KV8(s, [codes, k_scale, v_scale])
+
+
+def kv8_contiguous(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, *,
+                   n_layers: int, layer_stride: int, head_stride: int, tok_stride: int, scale_block: int,
+                   scale_layer_stride: int, scale_head_stride: int, seq_stride: int = 0,
+                   scale_seq_stride: int = 0) -> KV8:
+    """k, v: E4M3 codes, one byte an element (uint8 or float8_e4m3fn); scales: exponent bytes."""
+    return _kv8(kv_contiguous(k, v, n_layers=n_layers, layer_stride=layer_stride, head_stride=head_stride,
+                              tok_stride=tok_stride, seq_stride=seq_stride),
+                k_scale, v_scale, scale_block, scale_seq_stride, scale_layer_stride, scale_head_stride, 0)
+
+
+def kv8_paged(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+              block_table: torch.Tensor, *, n_layers: int, layer_stride: int, page_stride: int,
+              head_stride: int, tok_stride: int, page_size: int, scale_block: int,
+              scale_layer_stride: int, scale_page_stride: int, scale_head_stride: int) -> KV8:
+    return _kv8(kv_paged(k, v, block_table, n_layers=n_layers, layer_stride=layer_stride,
+                         page_stride=page_stride, head_stride=head_stride, tok_stride=tok_stride,
+                         page_size=page_size),
+                k_scale, v_scale, scale_block, 0, scale_layer_stride, scale_head_stride, scale_page_stride)
+
+
+def _rows(t: Optional[torch.Tensor], p: Problem, what: str, heads: int, layers: int) -> c_rows:
+    """The view of [M][heads][head_dim] (or [layers][M][heads][head_dim]) rows of any strides."""
+    r = c_rows()
+    if t is None:
+        return r
+    if t.dtype != _DTYPES[p.struct.dtype]:
+        raise ValueError(f"{what} is {t.dtype}, the problem {_DTYPES[p.struct.dtype]}")
+    if t.dim() == 3 and layers == 1:
+        t = t.unsqueeze(0)
+    want = (layers, p.n_tokens, heads, p.struct.head_dim)
+    if tuple(t.shape) != want:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {want}")
+    if t.stride(3) != 1 and t.shape[3] > 1:
+        raise ValueError(f"rows of {what} must be contiguous")
+    r.base = t.data_ptr()
+    r.layer_stride, r.tok_stride, r.head_stride = t.stride(0), t.stride(1), t.stride(2)
+    return r
+
+
+def _int32(t: Optional[torch.Tensor], n: int, what: str) -> None:
+    if t is not None and (t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{what} must be {n} contiguous int32 values")
+
+
+def _append(fn, p: Problem, kv, k, v, cached, capacity, layer, n_layers, pos_ids, q, q_out, rotate, stream):
+    s = p.struct
+    _int32(cached, s.n_seqs, "cached")
+    _int32(pos_ids, p.n_tokens, "pos_ids")
+    a = c_append()
+    a.k = _rows(k, p, "k", s.n_heads_kv, n_layers)
+    a.v = _rows(v, p, "v", s.n_heads_kv, n_layers)
+    if q is not None:
+        a.q = _rows(q, p, "q", s.n_heads_q, n_layers)
+        if q_out is None:
+            q_out = torch.empty((p.n_tokens, s.n_heads_q, s.head_dim), dtype=q.dtype, device=q.device)
+        elif q_out.dtype != q.dtype or q_out.numel() != p.n_tokens * s.n_heads_q * s.head_dim or not q_out.is_contiguous():
+            raise ValueError("q_out must be contiguous rows of q's type and size")
+        a.q_out = q_out.data_ptr()
+    a.cached = cached.data_ptr()
+    a.pos_ids = pos_ids.data_ptr() if pos_ids is not None else None
+    a.capacity, a.layer, a.n_layers, a.rotate = capacity, layer, n_layers, int(rotate)
+    _check(fn(ctypes.byref(s), ctypes.byref(a), ctypes.byref(kv.struct), _stream(stream)), fn.__name__)
+    return q_out
+
+
+def cc_append_kv(p: Problem, kv: KV, k: torch.Tensor, v: torch.Tensor, cached: torch.Tensor, *, capacity: int = 0,
+                 layer: int = 0, n_layers: int = 1, pos_ids: Optional[torch.Tensor] = None,
+                 q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, rotate: bool = True,
+                 stream=None) -> Optional[torch.Tensor]:
+    """Appends k, v [M][Hkv][d] (with n_layers > 1: [n_layers][M][Hkv][d]; any token and head strides) behind
+    cached[b] entries of each sequence; p.cu_seqlens count the new tokens.  Returns the rotated queries
+    where q [M][Hq][d] is given."""
+    return _append(_lib.cc_append_kv, p, kv, k, v, cached, capacity, layer, n_layers, pos_ids, q, q_out, rotate, stream)
+
+
+def cc_append_kv8(p: Problem, kv: KV8, k: torch.Tensor, v: torch.Tensor, cached: torch.Tensor, *, capacity: int = 0,
+                  layer: int = 0, n_layers: int = 1, pos_ids: Optional[torch.Tensor] = None,
+                  q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, rotate: bool = True,
+                  stream=None) -> Optional[torch.Tensor]:
+    """cc_append_kv into a cache in 8 bits."""
+    return _append(_lib.cc_append_kv8, p, kv, k, v, cached, capacity, layer, n_layers, pos_ids, q, q_out, rotate, stream)
+
+
+def cc_compact_kv8(p: Problem, kv: KV8, keep_idx: torch.Tensor, k: Sequence[int], per_head: int,
+                   token_ids: Optional[torch.Tensor] = None, pos_ids: Optional[torch.Tensor] = None,
+                   out: Optional[KV8] = None, stream=None) -> None:
+    """cc_compact_kv on a cache in 8 bits (in place unless `out` is given)."""
+    kk, n = _host_array(k, np.int32, _i32)
+    if n != p.struct.n_seqs * (p.struct.n_heads_kv if per_head else 1):
+        raise ValueError(f"{n} budgets for {p.struct.n_seqs} sequences")
+    _check(_lib.cc_compact_kv8(ctypes.byref(p.struct), ctypes.byref(kv.struct), _ptr(keep_idx), kk, per_head,
+                               _ptr(token_ids), _ptr(pos_ids),
+                               ctypes.byref(out.struct) if out is not None else None, _stream(stream)),
+           "cc_compact_kv8")
+
+
+_MASKS = {"causal": CC_MASK_CAUSAL, "counter": CC_MASK_COUNTER_CAUSAL}
+
+
+def cc_attention_kv8_workspace(p: Problem, mask: str, max_kv_len: int) -> int:
+    return _query(_lib.cc_attention_kv8_workspace, ctypes.byref(p.struct), _MASKS[mask], max_kv_len)
+
+
+def cc_attention_kv8(p: Problem, q: torch.Tensor, kv: KV8, layer: int, kv_lens: torch.Tensor, max_kv_len: int,
+                     o: Optional[torch.Tensor] = None, *, mask: str = "causal",
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of the queries q [N][Hq][d] (p.cu_seqlens count them) over a cache in 8 bits that holds
+    kv_lens[b] entries of each sequence, the queries' own last; mask "causal" or "counter"."""
+    s = p.struct
+    _int32(kv_lens, s.n_seqs, "kv_lens")
+    if q.dtype != torch.bfloat16 or q.numel() != p.n_tokens * s.n_heads_q * s.head_dim or not q.is_contiguous():
+        raise ValueError("q must be contiguous bf16 rows [N][Hq][head_dim]")
+    if o is None:
+        o = torch.empty_like(q)
+    elif o.dtype != q.dtype or o.numel() != q.numel() or not o.is_contiguous():
+        raise ValueError("o must be contiguous and of q's type and size")
+    if workspace is None:
+        workspace = _workspace(cc_attention_kv8_workspace(p, mask, max_kv_len), p.device)
+    _check(_lib.cc_attention_kv8(ctypes.byref(s), _ptr(q), ctypes.byref(kv.struct), layer, _MASKS[mask],
+                                 _ptr(kv_lens), max_kv_len, _ptr(o), _ptr(workspace), workspace.numel(),
+                                 _stream(stream)), "cc_attention_kv8")
+    return o

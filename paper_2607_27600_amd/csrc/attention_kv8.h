@@ -1,0 +1,33 @@
+// What the kernels of the attention over a cache in 8 bits share with each other and with the planner.
+#pragma once
+
+#include "cc_internal.h"
+
+namespace cc {
+
+constexpr int FEW_ROWS = 64;     // rows (queries times heads of a group) up to which a sequence counts as few
+constexpr int FEW_NT = 256;
+constexpr int KV8_LIST = 64;     // sequences of a launch listed by value
+constexpr int MANY_ROWS = 128;   // rows of a block of the kernel for many
+constexpr int MANY_KEYS = 64;    // entries of its tiles
+
+// One class of sequences (few or many rows) of a call.
+struct Kv8Args {
+  const u16* q;
+  u16* o;
+  Kv8View k, v;                  // alike but for base and scale
+  const int32_t *cu, *lens;
+  int layer, mask, inclusive, max_len;
+  int hq, hkv, g, head_dim;
+  float c2;                      // scale * log2(e)
+  int R;                         // most rows of a sequence of the class
+  int piece, splits;             // entries of a piece, pieces of the longest sequence
+  float* part;                   // splits > 1: [splits][n_list][Hkv][R][head_dim] outputs
+  float2* part_ml;               // and [splits][n_list][Hkv][R] (maximum, sum)
+  int n_list, listed;            // sequences walked: list[0..n_list), or (listed = 0) all
+  int32_t list[KV8_LIST];
+};
+hipError_t launch_attention_kv8(const Kv8Args& a, bool few, hipStream_t s);
+hipError_t launch_attn_many(const Kv8Args& a, hipStream_t s);
+
+}  // namespace cc

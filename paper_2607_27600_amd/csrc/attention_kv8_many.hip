@@ -1,0 +1,451 @@
+// Attention over a cache in 8 bits, many rows of a sequence and KV head: chunks of a prompt (causal) and
+// the scoring pass (counter-causal).  The sums, roundings and masks are those of attention_kv8.hip.
+//
+// One workgroup of 4 waves takes 128 rows (32 a wave), a row being a (query, query head of the group)
+// pair, and walks tiles of 64 entries.  S^T = K Q^T and O^T = V^T P^T on 32x32x16 MFMA: a lane owns one
+// row, its softmax stays in its registers, and its P feeds the second product from them.
+//
+// A tile's codes are loaded 16 bytes a lane a whole tile ahead, and turned into bf16 once for the
+// four waves, on the way into LDS: 32 conversions, 8 LDS writes a wave and tile.  (Turning them into
+// operands in every wave instead would cost each wave 128.)  In LDS a tile is bf16 rows whose 16-byte
+// chunks are swizzled by bits of the row so that fragment reads hit every bank once; V^T is read
+// with transpose reads.  Two K and two V buffers, one barrier a tile.  Matrix work of one tile is
+// interleaved with the exponentials of the tile before.
+#include <type_traits>
+
+#include "attention_kv8.h"
+
+namespace cc {
+namespace {
+
+constexpr int BN = MANY_KEYS;
+constexpr int ROWS_W = 32;
+constexpr int NWAVES = 4;
+constexpr float kRescale = 8.f;
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef short v8i16 __attribute__((ext_vector_type(8)));
+
+template <int HD>
+struct Shape {
+  static constexpr int TILE = BN * HD;
+  static constexpr int ROWB = HD * 2;        // bytes of a tile row in LDS
+  static constexpr int CPR = HD / 16;        // 16-code pieces of a row
+  static constexpr int RPW = 64 / CPR;       // rows a wave's load covers
+  static constexpr int NI = BN / (NWAVES * RPW);   // loads of a wave and tile
+  static constexpr int NKS = HD / 16;
+  static constexpr int NDB = HD / 32;
+  static constexpr int NS = 2 * NKS;
+  static constexpr int NPV = 4 * NDB;
+  __device__ static constexpr int kswz(int r) { return HD == 128 ? (r & 15) : ((r >> 1) & 7); }
+  __device__ static constexpr int vswz(int r) { return HD == 128 ? ((r & 3) << 2) : (((r >> 1) & 1) << 2); }
+};
+
+__device__ __forceinline__ v4i16 ds_read_tr(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16*)(p));
+}
+
+// Sixteen codes times the scale, in bf16: exact.
+__device__ __forceinline__ void widen16(const uint4& w, float scale, uint4& lo, uint4& hi) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  uint32_t y[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(x[i]), scale, false));
+    y[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(x[i]), scale, true));
+  }
+  lo = make_uint4(y[0], y[1], y[2], y[3]);
+  hi = make_uint4(y[4], y[5], y[6], y[7]);
+}
+
+template <int HD>
+__global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
+  using SH = Shape<HD>;
+  constexpr int TILE = SH::TILE, ROWB = SH::ROWB, CPR = SH::CPR, NI = SH::NI;
+  constexpr int NKS = SH::NKS, NDB = SH::NDB, NS = SH::NS, NPV = SH::NPV;
+  __shared__ __attribute__((aligned(1024))) u16 kb0[TILE];
+  __shared__ __attribute__((aligned(1024))) u16 kb1[TILE];
+  __shared__ __attribute__((aligned(1024))) u16 vb0[TILE];
+  __shared__ __attribute__((aligned(1024))) u16 vb1[TILE];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hi = lane >> 5, col = lane & 31;
+  const bool causal = a.mask == CC_MASK_CAUSAL;
+
+  // Heaviest blocks first: the last rows of a causal sequence, the first of a counter-causal one.
+  int x = blockIdx.x;
+  const int split = x % a.splits;
+  x /= a.splits;
+  const int kvh = x % a.hkv;
+  x /= a.hkv;
+  const int j = x % a.n_list, nth = x / a.n_list;
+  const int b = a.listed ? a.list[j] : j;
+  const int q0 = a.cu[b], m = a.cu[b + 1] - q0;
+  const int rows = m * a.g;
+  const int blocks = (rows + MANY_ROWS - 1) / MANY_ROWS;
+  if (rows <= FEW_ROWS || nth >= blocks) return;
+  const int rb = causal ? blocks - 1 - nth : nth;
+  const int len = min(max(a.lens[b], 0), a.max_len);
+  const int c0 = split * a.piece, c1 = min(len, c0 + a.piece);
+  if (split > 0 && c0 >= len) return;
+  const int shift = len - m;     // cache position of query 0
+
+  const int row0 = rb * MANY_ROWS;
+  const int row = row0 + wave * ROWS_W + col;
+  const bool valid = row < rows;
+  const int i_row = (valid ? row : rows - 1) / a.g;
+  const int hq = kvh * a.g + (valid ? row : rows - 1) % a.g;
+  const int after = a.inclusive ? 0 : 1;
+  // entries [lo, hi_) are seen by the row
+  const int lo = causal ? 0 : max(0, shift + i_row + after);
+  const int past = causal ? max(0, shift + i_row + 1) : len;
+
+  bf16x8 qf[NKS];
+  {
+    const u16* qp = a.q + (int64_t(q0 + i_row) * a.hq + hq) * HD + hi * 8;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) qf[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qp + ks * 16));
+  }
+
+  const int i_lo = row0 / a.g, i_hi = (min(row0 + MANY_ROWS, rows) - 1) / a.g;   // the block's queries
+  const int see0 = max(c0, causal ? 0 : max(0, shift + i_lo + after));   // entries some row sees
+  const int see1 = min(c1, causal ? max(0, shift + i_hi + 1) : len);
+  const int full0 = causal ? 0 : max(0, shift + i_hi + after);           // entries every row sees
+  const int full1 = causal ? max(0, shift + i_lo + 1) : len;
+  const int tb = see0 / BN, te = (see1 + BN - 1) / BN;
+  const int stop = min(c1, len);      // (c1 is a multiple of the tile or the sequence's end)
+
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16 acc[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) acc[db] = f32x16{};
+
+  if (see0 < see1) {
+    const int64_t cplane = int64_t(a.layer) * a.k.codes.layer_stride + int64_t(kvh) * a.k.codes.head_stride +
+                           (a.k.paged ? 0 : int64_t(b) * a.k.codes.seq_stride);
+    const int64_t splane = int64_t(a.layer) * a.k.s_layer + int64_t(kvh) * a.k.s_head +
+                           (a.k.paged ? 0 : int64_t(b) * a.k.s_seq);
+    const char* kplane = static_cast<const char*>(a.k.codes.base) + cplane;
+    const char* vplane = static_cast<const char*>(a.v.codes.base) + cplane;
+    const uint8_t* kscale = a.k.scale + splane;
+    const uint8_t* vscale = a.v.scale + splane;
+    const int32_t* table = a.k.paged ? a.k.codes.block_table + int64_t(b) * a.k.codes.max_pages : nullptr;
+    const int last = len - 1;
+
+    // Row of the tile and 16-code piece of this lane's load i: rows of one load lie in one 16-entry
+    // group, i.e. one page and one scale block.
+    const int lrow = (lane / CPR) + wave * SH::RPW;      // + i * NWAVES * RPW
+    const int piece = lane % CPR;
+    constexpr int RSTEP = NWAVES * SH::RPW;
+    // LDS places of the two bf16 chunks: rows i * RSTEP further have the same swizzles
+    uint32_t kst[2], vst[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      kst[h] = lrow * ROWB + (((2 * piece + h) ^ SH::kswz(lrow)) * 16);
+      vst[h] = lrow * ROWB + (((2 * piece + h) ^ SH::vswz(lrow)) * 16);
+    }
+
+    // Pages of the 16-entry groups a lane each, 64 groups (16 tiles) at a time, and their scales.
+    const int gfirst = tb * 4, glast = last >> 4;
+    int gbase = gfirst;
+    auto pages_at = [&](int base) { return a.k.paged ? table[min(base + lane, glast) >> (a.k.codes.page_shift - 4)] : 0; };
+    auto scales_at = [&](int base, int pg) {
+      const int gg = min(base + lane, glast);
+      const int slot = a.k.paged ? (gg << 4) & a.k.codes.page_mask : gg << 4;
+      const int64_t o = int64_t(pg) * a.k.s_page + (slot >> a.k.block_shift);
+      return uint32_t(kscale[o]) | (uint32_t(vscale[o]) << 8);
+    };
+    int page = pages_at(gbase);
+    uint32_t scale = scales_at(gbase, page);
+    int page_n = page;
+    uint32_t scale_n = scale;
+    // group of load i of tile t, and the lane that holds it
+    auto group_of = [&](int t, int i) {
+      return min(t * 4 + __builtin_amdgcn_readfirstlane((wave * SH::RPW + i * RSTEP) >> 4), glast);
+    };
+    auto held = [&](int cur, int nxt, int gg) {
+      const int at = gg - gbase;
+      return at < 64 ? __builtin_amdgcn_readlane(cur, at) : __builtin_amdgcn_readlane(nxt, min(at - 64, 63));
+    };
+    auto load = [&](const char* plane, int t, uint4 (&w)[NI]) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int gg = group_of(t, i);
+        const int pg = held(page, page_n, gg);
+        const int slot = a.k.paged ? (gg << 4) & a.k.codes.page_mask : gg << 4;
+        const char* base = plane + int64_t(pg) * a.k.codes.page_stride + int64_t(slot) * a.k.codes.tok_stride;
+        const int r = min((lrow + i * RSTEP) & 15, last - (gg << 4));
+        w[i] = *reinterpret_cast<const uint4*>(base + int64_t(r) * a.k.codes.tok_stride + piece * 16);
+      }
+    };
+    auto put = [&](u16* dst, const uint32_t (&at)[2], int t, int which, const uint4 (&w)[NI]) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const uint32_t sc = uint32_t(held(int(scale), int(scale_n), group_of(t, i)));
+        uint4 y[2], z = w[i];
+        if (which && t * BN + BN > len && t * BN + lrow + i * RSTEP >= len) z = make_uint4(0, 0, 0, 0);
+        widen16(z, e8m0_scale((sc >> (8 * which)) & 255u), y[0], y[1]);
+        char* d = reinterpret_cast<char*>(dst) + i * RSTEP * ROWB;
+        *reinterpret_cast<uint4*>(d + at[0]) = y[0];
+        *reinterpret_cast<uint4*>(d + at[1]) = y[1];
+      }
+    };
+
+    uint32_t koff[NKS];
+#pragma unroll
+    for (int jj = 0; jj < NKS; ++jj) koff[jj] = col * ROWB + 16 * ((2 * jj + hi) ^ SH::kswz(col));
+    uint32_t voff[NDB];
+    {
+      const int G = lane >> 4, L = lane & 15, y = L >> 2;
+      const int r = 4 * (G >> 1) + y;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+        if constexpr (HD == 128)
+          voff[db] = r * ROWB + 64 * (db ^ y) + 32 * (G & 1) + 8 * (L & 3);
+        else
+          voff[db] = r * ROWB + 16 * ((4 * db + 2 * (G & 1) + ((L & 3) >> 1)) ^ SH::vswz(r)) + 8 * (L & 1);
+      }
+    }
+    auto kfrag = [&](const u16* Kl, int q) {
+      return as_bf16x8(*reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(Kl) + koff[q >> 1] +
+                                                       (q & 1) * (32 * ROWB)));
+    };
+    auto vfrag = [&](const u16* Vl, int q) {
+      const char* p = reinterpret_cast<const char*>(Vl) + voff[q % NDB] + (q / NDB) * (16 * ROWB);
+      const v4i16 l4 = ds_read_tr(p), h4 = ds_read_tr(p + 8 * ROWB);
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(l4, h4, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto half_max = [](float v) {
+      auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+      return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    };
+    auto row_max = [&](const f32x16(&s)[2]) {
+      float v = -INFINITY;
+#pragma unroll
+      for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v = fmaxf(v, s[mb][e]);
+      return half_max(v);
+    };
+    auto seen = [&](int t, int mb, int e) {
+      const int key = t * BN + mb * 32 + (e >> 2) * 8 + hi * 4 + (e & 3);
+      return key >= lo && key < past;
+    };
+
+    uint4 kr[NI], vr[NI];
+    load(kplane, tb, kr);
+    load(vplane, tb, vr);
+    put(kb0, kst, tb, 0, kr);
+    put(vb0, vst, tb, 1, vr);
+    if (tb + 1 < te) {
+      load(kplane, tb + 1, kr);
+      put(kb1, kst, tb + 1, 0, kr);
+    }
+    __syncthreads();
+    f32x16 sa[2], sb[2];
+    sa[0] = f32x16{};
+    sa[1] = f32x16{};
+#pragma unroll
+    for (int q = 0; q < NS; ++q) sa[q & 1] = mfma32(kfrag(kb0, q), qf[q >> 1], sa[q & 1]);
+    if (tb + 2 < te) __syncthreads();   // every wave has read K(tb) before its buffer is refilled
+    float mx = row_max(sa);
+
+    // Tile t with parity P: S(t) in sc, its unmasked row maximum in mx; K(t+1) and V(t) in LDS.  The codes
+    // of K(t+2) and V(t+1) are loaded at the start and written at the end, into buffers that the tile
+    // before has freed.
+    auto step = [&](int t, auto par) {
+      constexpr int P = decltype(par)::value;
+      f32x16(&sc)[2] = P ? sb : sa;
+      f32x16(&sn)[2] = P ? sa : sb;
+      const u16* Kn = P ? kb0 : kb1;
+      u16* Kfree = P ? kb1 : kb0;
+      const u16* Vc = P ? vb1 : vb0;
+      u16* Vfree = P ? vb0 : vb1;
+      if (t + 2 < te) load(kplane, t + 2, kr);
+      if (t + 1 < te) load(vplane, t + 1, vr);
+      const bool masked = t * BN < full0 || t * BN + BN > min(full1, stop);
+      bf16x8 kf[4];
+      kf[0] = kfrag(Kn, 0);
+      kf[1] = kfrag(Kn, 1);
+      kf[2] = kfrag(Kn, 2);
+      if (masked) {
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[mb][e] = seen(t, mb, e) ? sc[mb][e] : -INFINITY;
+        mx = row_max(sc);
+      }
+      const bool up = mx > m_run + kRescale / a.c2;
+      const float corr = up ? fast_exp2((m_run - mx) * a.c2) : 1.f;
+      m_run = up ? mx : m_run;
+      const float mc = (m_run == -INFINITY ? 0.f : m_run) * a.c2;
+      sn[0] = f32x16{};
+      sn[1] = f32x16{};
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+      constexpr int EPM = 32 / NS;
+#pragma unroll
+      for (int q = 0; q < NS; ++q) {
+        if (q + 3 < NS) kf[(q + 3) & 3] = kfrag(Kn, q + 3);
+        sn[q & 1] = mfma32(kf[q & 3], qf[q >> 1], sn[q & 1]);
+#pragma unroll
+        for (int u = 0; u < EPM; ++u) {
+          const int f = EPM * q + u, mb = f >> 4, e = f & 15;
+          const float p = fast_exp2(fmaf(sc[mb][e], a.c2, -mc));
+          asm volatile("" ::"v"(p));
+          sc[mb][e] = p;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (__any(corr != 1.f)) {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) acc[db] *= corr;
+      }
+      bf16x8 pf[4];
+      auto pack = [&](int kk) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pf[kk][e] = (__bf16)sc[kk >> 1][(kk & 1) * 8 + e];
+      };
+      __builtin_amdgcn_s_setprio(0);
+      float ls0 = 0.f, ls1 = 0.f, m0 = -INFINITY, m1 = -INFINITY;
+      if (masked) {
+        // NaN codes of values, taken out and counted by the rows that see them
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          pack(kk);
+          bf16x8 see;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            see[e] = (__bf16)(seen(t, kk >> 1, (kk & 1) * 8 + e) ? 1.f : 0.f);
+            ls0 += sc[kk >> 1][(kk & 1) * 8 + e];
+          }
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) {
+            const bf16x8 v = vfrag(Vc, kk * NDB + db);
+            v8i16 w = __builtin_bit_cast(v8i16, v), one;
+            bool nan = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const bool n = (w[e] & 0x7fff) > 0x7f80;
+              nan |= n;
+              one[e] = n ? 0x3f80 : 0;
+              w[e] = n ? 0 : w[e];
+            }
+            acc[db] = mfma32(__builtin_bit_cast(bf16x8, w), pf[kk], acc[db]);
+            if (__any(nan)) {
+              const f32x16 hits = mfma32(__builtin_bit_cast(bf16x8, one), see, f32x16{});
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (hits[e] > 0.f) acc[db][e] = __uint_as_float(0x7fc00000u);
+            }
+          }
+        }
+        m0 = row_max(sn);
+      } else {
+        bf16x8 vf[4];
+        vf[0] = vfrag(Vc, 0);
+        vf[1] = vfrag(Vc, 1);
+        vf[2] = vfrag(Vc, 2);
+        pack(0);
+        constexpr int SPM = 32 / NPV;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 0; q < NPV; ++q) {
+          if (q + 3 < NPV) vf[(q + 3) & 3] = vfrag(Vc, q + 3);
+          acc[q % NDB] = mfma32(vf[q & 3], pf[q / NDB], acc[q % NDB]);
+          if (q % NDB == NDB - 1 && q < NPV - 1) pack(q / NDB + 1);
+#pragma unroll
+          for (int u = 0; u < SPM; u += 2) {
+            ls0 += sc[(SPM * q + u) >> 4][(SPM * q + u) & 15];
+            ls1 += sc[(SPM * q + u + 1) >> 4][(SPM * q + u + 1) & 15];
+          }
+          asm volatile("" : "+v"(ls0), "+v"(ls1));
+          // the row maximum of S(t+1): 32 entries over the later slots
+          constexpr int PER = (32 + NPV - 3) / (NPV - 2);
+          if (q >= 2) {
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+              const int f = PER * (q - 2) + u;
+              if (f < 16) m0 = fmaxf(m0, sn[0][f]);
+              else if (f < 32) m1 = fmaxf(m1, sn[1][f - 16]);
+            }
+            asm volatile("" : "+v"(m0), "+v"(m1));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      l_run = l_run * corr + (ls0 + ls1);
+      mx = half_max(fmaxf(m0, m1));
+      if (t + 2 < te) put(Kfree, kst, t + 2, 0, kr);
+      if (t + 1 < te) put(Vfree, vst, t + 1, 1, vr);
+      // the next 64 groups: pages in the middle of these, scales behind them
+      const int at = t + 1 - gbase / 4;
+      if (at == 4) page_n = pages_at(gbase + 64);
+      if (at == 8) scale_n = scales_at(gbase + 64, page_n);
+      if (at == 16) {
+        gbase += 64;
+        page = page_n;
+        scale = scale_n;
+      }
+      __syncthreads();
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    for (int t = tb; t < te; t += 2) {
+      step(t, I0{});
+      if (t + 1 < te) step(t + 1, I1{});
+    }
+  }
+
+  const float l_all = l_run + __shfl_xor(l_run, 32);
+  if (a.splits > 1) {
+    if (valid) {
+      const int64_t prow = (int64_t(split) * a.n_list * a.hkv + int64_t(j) * a.hkv + kvh) * a.R + row;
+      float* po = a.part + prow * HD + 4 * hi;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<float4*>(po + db * 32 + q * 8) =
+              make_float4(acc[db][q * 4], acc[db][q * 4 + 1], acc[db][q * 4 + 2], acc[db][q * 4 + 3]);
+      if (hi == 0) a.part_ml[prow] = make_float2(m_run, l_all);
+    }
+    return;
+  }
+  const float inv = l_all == 0.f ? 0.f : 1.f / l_all;   // an empty row gives 0, a NaN sum NaN
+  // The outputs go out through LDS as whole rows (the K buffers are free), 16 bytes a lane.
+  char* stg = reinterpret_cast<char*>(wave < 2 ? kb0 : kb1) + (wave & 1) * (ROWS_W * ROWB);
+  constexpr int OCPR = HD / 8;
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      bf16x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[db][q * 4 + e] * inv);
+      *reinterpret_cast<bf16x4*>(stg + col * ROWB + (((db * 4 + q) ^ SH::kswz(col)) * 16) + hi * 8) = o;
+    }
+#pragma unroll
+  for (int i = 0; i < ROWS_W * OCPR / 64; ++i) {
+    const int r = (64 / OCPR) * i + lane / OCPR, c = lane % OCPR;
+    const uint4 v = *reinterpret_cast<const uint4*>(stg + r * ROWB + ((c ^ SH::kswz(r)) * 16));
+    const int orow = row0 + wave * ROWS_W + r;
+    if (orow < rows)
+      *reinterpret_cast<uint4*>(a.o + (int64_t(q0 + orow / a.g) * a.hq + kvh * a.g + orow % a.g) * HD + c * 8) = v;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attn_many(const Kv8Args& a, hipStream_t s) {
+  const int64_t grid = int64_t((a.R + MANY_ROWS - 1) / MANY_ROWS) * a.n_list * a.hkv * a.splits;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  if (a.head_dim == 128)
+    hipLaunchKernelGGL(attn_many<128>, dim3(unsigned(grid)), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL(attn_many<64>, dim3(unsigned(grid)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace cc

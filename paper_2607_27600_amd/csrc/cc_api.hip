@@ -7,6 +7,7 @@
 #include <mutex>
 #include <vector>
 
+#include "attention_kv8.h"
 #include "cc_internal.h"
 
 using namespace cc;
@@ -70,13 +71,15 @@ int max_len(const cc_problem* p) {
   return m;
 }
 
-cc_status check_kv(const cc_problem* p, const cc_kv* kv, int min_layers) {
+// es: bytes of a cache element; longest: entries that a sequence's block-table row must reach (-1: the
+// problem's longest sequence).
+cc_status check_kv(const cc_problem* p, const cc_kv* kv, int min_layers, int es = 0, int longest = -1) {
   if (!kv || !kv->k || !kv->v) return CC_ERR_ARG;
   if (kv->layout != CC_KV_CONTIGUOUS && kv->layout != CC_KV_PAGED) return CC_ERR_ARG;
   if (kv->n_layers < min_layers) return CC_ERR_SHAPE;
   if (kv->layer_stride < 0 || kv->head_stride < 0 || kv->tok_stride < p->head_dim)
     return CC_ERR_SHAPE;
-  const int es = esize(p->dtype);
+  if (es == 0) es = esize(p->dtype);
   if (!aligned16(kv->k) || !aligned16(kv->v)) return CC_ERR_ARG;
   auto str_ok = [&](int64_t s) { return (s * es) % 16 == 0; };
   if (!str_ok(kv->layer_stride) || !str_ok(kv->head_stride) || !str_ok(kv->tok_stride))
@@ -88,8 +91,8 @@ cc_status check_kv(const cc_problem* p, const cc_kv* kv, int min_layers) {
     constexpr int64_t kPageLimit = int64_t(1) << 32;
     if (kv->page_stride * es >= kPageLimit || int64_t(kv->page_size) * kv->tok_stride * es >= kPageLimit)
       return CC_ERR_UNSUPPORTED;
-    const int need = (max_len(p) + kv->page_size - 1) / kv->page_size;
-    if (kv->max_pages < need) return CC_ERR_SHAPE;
+    const int64_t len = longest >= 0 ? longest : max_len(p);
+    if (kv->max_pages < (len + kv->page_size - 1) / kv->page_size) return CC_ERR_SHAPE;
   } else {
     if (kv->seq_stride < 0 || !str_ok(kv->seq_stride)) return CC_ERR_UNSUPPORTED;
   }
@@ -936,6 +939,279 @@ cc_status cc_compact_rows(const cc_problem* p, void* rows, int32_t row_bytes,
   c.ids[0] = c.ids[1] = nullptr;
   c.cu_d = p->cu_seqlens_d;
   return compact_run(c, lists, ws, s);
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ cache in 8 bits
+
+namespace {
+
+cc_status check_kv8(const cc_problem* p, const cc_kv8* kv, int min_layers, int longest) {
+  if (!kv) return CC_ERR_ARG;
+  CC_TRY(check_kv(p, &kv->codes, min_layers, 1, longest));
+  if (!kv->k_scale || !kv->v_scale) return CC_ERR_ARG;
+  if (!is_pow2(kv->scale_block) || kv->scale_block < 16 || kv->scale_block > 128) return CC_ERR_UNSUPPORTED;
+  if (kv->scale_layer_stride < 0 || kv->scale_head_stride < 0) return CC_ERR_SHAPE;
+  if (kv->codes.layout == CC_KV_PAGED) {
+    if (kv->scale_page_stride < 0 || kv->scale_block > kv->codes.page_size) return CC_ERR_SHAPE;
+  } else if (kv->scale_seq_stride < 0) {
+    return CC_ERR_SHAPE;
+  }
+  return CC_OK;
+}
+
+Kv8View make_view8(const cc_kv8* kv, const void* base, uint8_t* scale) {
+  Kv8View v;
+  v.codes = make_view(&kv->codes, base, 1);
+  v.scale = scale;
+  v.s_seq = kv->scale_seq_stride;
+  v.s_layer = kv->scale_layer_stride;
+  v.s_head = kv->scale_head_stride;
+  v.s_page = kv->scale_page_stride;
+  v.block_shift = 0;
+  while ((1 << v.block_shift) < kv->scale_block) ++v.block_shift;
+  v.paged = kv->codes.layout == CC_KV_PAGED;
+  return v;
+}
+
+cc_status check_rows(const cc_problem* p, const cc_rows& r) {
+  const int es = esize(p->dtype);
+  if (!r.base || !aligned16(r.base)) return CC_ERR_ARG;
+  if (r.layer_stride < 0 || r.tok_stride < 0 || r.head_stride < 0) return CC_ERR_SHAPE;
+  if (r.layer_stride * es % 16 || r.tok_stride * es % 16 || r.head_stride * es % 16) return CC_ERR_UNSUPPORTED;
+  return CC_OK;
+}
+
+// The checks of both appends but the cache's own, and the launch's sizes.
+cc_status plan_append(const cc_problem* p, const cc_append* a, const cc_kv* kv, AppendLaunch& l) {
+  if (a->n_layers < 1 || a->layer < 0 || a->layer > kv->n_layers - a->n_layers) return CC_ERR_SHAPE;
+  if (a->rotate != 0 && a->rotate != 1) return CC_ERR_ARG;
+  if (a->rotate && !(p->rope_theta > 0.f && std::isfinite(p->rope_theta))) return CC_ERR_ARG;
+  if (a->capacity < 0) return CC_ERR_SHAPE;
+  const int64_t room = kv->layout == CC_KV_PAGED ? int64_t(kv->max_pages) * kv->page_size : INT32_MAX;
+  if (a->capacity == 0 && kv->layout != CC_KV_PAGED) return CC_ERR_ARG;
+  l.capacity = int(std::min<int64_t>({a->capacity ? a->capacity : room, room, INT32_MAX - 128}));
+  if (n_tokens(p) > 0) {
+    CC_TRY(check_rows(p, a->k));
+    CC_TRY(check_rows(p, a->v));
+    if (!a->cached) return CC_ERR_ARG;
+    if (a->q.base) {
+      if (a->n_layers != 1) return CC_ERR_UNSUPPORTED;
+      CC_TRY(check_rows(p, a->q));
+      if (!a->q_out || !aligned16(a->q_out)) return CC_ERR_ARG;
+    }
+  }
+  l.dtype = p->dtype;
+  l.k = a->k;
+  l.v = a->v;
+  l.q = a->q;
+  l.q_out = a->q_out;
+  l.cached = a->cached;
+  l.pos = a->pos_ids;
+  l.cu_d = p->cu_seqlens_d;
+  l.cu_h = p->cu_seqlens_h;
+  l.n_seqs = p->n_seqs;
+  l.layer = a->layer;
+  l.n_layers = a->n_layers;
+  l.n_heads_q = p->n_heads_q;
+  l.n_heads_kv = p->n_heads_kv;
+  l.head_dim = p->head_dim;
+  l.rotate = a->rotate;
+  l.theta = p->rope_theta;
+  return CC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cc_status cc_append_kv(const cc_problem* p, const cc_append* a, const cc_kv* kv, void* stream) {
+  CC_TRY(check_problem(p));
+  if (!a) return CC_ERR_ARG;
+  CC_TRY(check_kv(p, kv, 1));
+  AppendLaunch l;
+  CC_TRY(plan_append(p, a, kv, l));
+  const int es = esize(p->dtype);
+  l.f8 = false;
+  l.kc = Kv8View{};
+  l.kc.codes = make_view(kv, kv->k, es);
+  l.kc.paged = kv->layout == CC_KV_PAGED;
+  l.vc = l.kc;
+  l.vc.codes = make_view(kv, kv->v, es);
+  CC_HIP(launch_append(l, static_cast<hipStream_t>(stream)));
+  return CC_OK;
+}
+
+cc_status cc_append_kv8(const cc_problem* p, const cc_append* a, const cc_kv8* kv, void* stream) {
+  CC_TRY(check_problem(p));
+  if (!a) return CC_ERR_ARG;
+  CC_TRY(check_kv8(p, kv, 1, -1));
+  AppendLaunch l;
+  CC_TRY(plan_append(p, a, &kv->codes, l));
+  l.f8 = true;
+  l.kc = make_view8(kv, kv->codes.k, kv->k_scale);
+  l.vc = make_view8(kv, kv->codes.v, kv->v_scale);
+  CC_HIP(launch_append(l, static_cast<hipStream_t>(stream)));
+  return CC_OK;
+}
+
+cc_status cc_compact_kv8(const cc_problem* p, const cc_kv8* kv, const int32_t* keep_idx,
+                         const int32_t* k_h, int32_t per_head, int32_t* token_ids,
+                         int32_t* pos_ids, const cc_kv8* out, void* stream) {
+  CC_TRY(check_problem(p));
+  CC_TRY(check_kv8(p, kv, 1, -1));
+  if (per_head != 0 && per_head != 1) return CC_ERR_ARG;
+  if (!k_h) return CC_ERR_ARG;
+  if (out) {
+    CC_TRY(check_kv8(p, out, kv->codes.n_layers, -1));
+    if (out->codes.layout != kv->codes.layout || out->scale_block != kv->scale_block) return CC_ERR_ARG;
+  }
+  const int hkv = p->n_heads_kv, per = per_head ? hkv : 1;
+  if (per > 64) return CC_ERR_UNSUPPORTED;   // the lists of a sequence travel with one launch
+  std::vector<CompactList> lists;
+  int max_k = 0;
+  int64_t off = 0;
+  CC_TRY(compact_lists(p, k_h, per, per, false, lists, max_k, off));
+  if (off > 0 && !keep_idx) return CC_ERR_ARG;
+  if (max_k == 0) return CC_OK;
+  const cc_kv8* dst = out ? out : kv;
+  Compact8Launch c;
+  c.src[0] = make_view8(kv, kv->codes.k, kv->k_scale);
+  c.src[1] = make_view8(kv, kv->codes.v, kv->v_scale);
+  c.dst[0] = make_view8(dst, dst->codes.k, dst->k_scale);
+  c.dst[1] = make_view8(dst, dst->codes.v, dst->v_scale);
+  c.keep = keep_idx;
+  c.lists = lists.data();
+  c.n_lists = int(lists.size());
+  c.n_layers = kv->codes.n_layers;
+  c.n_heads = hkv;
+  c.per_head = per_head;
+  c.head_dim = p->head_dim;
+  c.max_k = max_k;
+  c.in_place = out == nullptr;
+  c.ids[0] = token_ids;
+  c.ids[1] = pos_ids;
+  c.cu_d = p->cu_seqlens_d;
+  CC_HIP(launch_compact8(c, static_cast<hipStream_t>(stream)));
+  return CC_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// One class of sequences of a call, few or many rows: which they are, and how their entries are cut.
+// Sizes only, so that the workspace query and the call agree.
+struct Kv8Class {
+  int n = 0;               // sequences of the class
+  int n_list = 0, listed = 0;
+  int32_t list[KV8_LIST];
+  int R = 0, piece = 0, splits = 1;
+  size_t part = 0, total = 0;   // workspace: (maximum, sum) pairs behind the outputs
+};
+
+constexpr int kCus = 256;
+
+Kv8Class kv8_class(const cc_problem* p, int max_len, bool few) {
+  Kv8Class c;
+  const int g = p->n_heads_q / p->n_heads_kv;
+  int64_t blocks = 0;
+  for (int b = 0; b < p->n_seqs; ++b) {
+    const int64_t rows = int64_t(p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) * g;
+    if (rows == 0 || (rows <= FEW_ROWS) != few) continue;
+    if (c.n < KV8_LIST) c.list[c.n] = b;
+    ++c.n;
+    c.R = int(std::max<int64_t>(c.R, rows));
+    blocks += few ? 1 : (rows + MANY_ROWS - 1) / MANY_ROWS;
+  }
+  if (c.n == 0) return c;
+  c.listed = c.n <= KV8_LIST;
+  c.n_list = c.listed ? c.n : p->n_seqs;
+  const int64_t items = blocks * p->n_heads_kv;   // workgroups without a cut
+  int64_t want;
+  if (few) {
+    // pieces until there are eight workgroups a CU, of 256 entries (64 a wave) at the least
+    want = std::min<int64_t>((8 * kCus + items - 1) / items, (int64_t(max_len) + 255) / 256);
+  } else {
+    // pieces until there are two workgroups a CU (what is resident), of 512 entries at the least
+    want = std::min<int64_t>((2 * kCus + items - 1) / items, (int64_t(max_len) + 511) / 512);
+  }
+  want = std::max<int64_t>(want, 1);
+  c.piece = int(((int64_t(max_len) + want - 1) / want + MANY_KEYS - 1) / MANY_KEYS * MANY_KEYS);
+  c.piece = std::max(c.piece, MANY_KEYS);
+  c.splits = std::max(1, int((int64_t(max_len) + c.piece - 1) / c.piece));
+  if (c.splits > 1) {
+    const size_t rows = size_t(c.splits) * c.n_list * p->n_heads_kv * c.R;
+    c.part = align_up(rows * p->head_dim * sizeof(float));
+    c.total = c.part + align_up(rows * sizeof(float2));
+  }
+  return c;
+}
+
+cc_status check_attention8(const cc_problem* p, int32_t mask, int32_t max_len) {
+  CC_TRY(check_problem(p));
+  if (mask != CC_MASK_CAUSAL && mask != CC_MASK_COUNTER_CAUSAL) return CC_ERR_ARG;
+  if (max_len < 0 || max_len > INT32_MAX - 4096) return CC_ERR_SHAPE;
+  if (p->dtype != CC_BF16) return CC_ERR_UNSUPPORTED;
+  if (int64_t(n_tokens(p)) * (p->n_heads_q / p->n_heads_kv) > INT32_MAX) return CC_ERR_UNSUPPORTED;
+  return CC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cc_status cc_attention_kv8_workspace(const cc_problem* p, int32_t mask, int32_t max_kv_len, size_t* bytes) {
+  if (!bytes) return CC_ERR_ARG;
+  CC_TRY(check_attention8(p, mask, max_kv_len));
+  *bytes = kv8_class(p, max_kv_len, true).total + kv8_class(p, max_kv_len, false).total;
+  return CC_OK;
+}
+
+cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv, int32_t layer, int32_t mask,
+                           const int32_t* kv_lens, int32_t max_kv_len, void* o, void* ws, size_t ws_bytes,
+                           void* stream) {
+  CC_TRY(check_attention8(p, mask, max_kv_len));
+  CC_TRY(check_kv8(p, kv, 1, max_kv_len));
+  if (layer < 0 || layer >= kv->codes.n_layers) return CC_ERR_ARG;
+  const int N = n_tokens(p);
+  if (N > 0 && (!q || !o || !kv_lens || !aligned16(q) || !aligned16(o))) return CC_ERR_ARG;
+  const Kv8Class classes[2] = {kv8_class(p, max_kv_len, true), kv8_class(p, max_kv_len, false)};
+  CC_TRY(check_ws(ws, ws_bytes, classes[0].total + classes[1].total));
+  if (N == 0) return CC_OK;
+  size_t off = 0;
+  for (int i = 0; i < 2; ++i) {
+    const Kv8Class& c = classes[i];
+    if (c.n == 0) continue;
+    Kv8Args a;
+    a.q = static_cast<const u16*>(q);
+    a.o = static_cast<u16*>(o);
+    a.k = make_view8(kv, kv->codes.k, kv->k_scale);
+    a.v = make_view8(kv, kv->codes.v, kv->v_scale);
+    a.cu = p->cu_seqlens_d;
+    a.lens = kv_lens;
+    a.layer = layer;
+    a.mask = mask;
+    a.inclusive = p->diag == CC_DIAG_INCLUSIVE;
+    a.max_len = max_kv_len;
+    a.hq = p->n_heads_q;
+    a.hkv = p->n_heads_kv;
+    a.g = p->n_heads_q / p->n_heads_kv;
+    a.head_dim = p->head_dim;
+    a.c2 = softmax_scale(p) * kLog2e;
+    a.R = c.R;
+    a.piece = c.piece;
+    a.splits = c.splits;
+    a.part = c.splits > 1 ? reinterpret_cast<float*>(at(ws, off)) : nullptr;
+    a.part_ml = c.splits > 1 ? reinterpret_cast<float2*>(at(ws, off + c.part)) : nullptr;
+    a.n_list = c.n_list;
+    a.listed = c.listed;
+    std::copy_n(c.list, c.listed ? c.n : 0, a.list);
+    CC_HIP(launch_attention_kv8(a, i == 0, static_cast<hipStream_t>(stream)));
+    off += c.total;
+  }
+  return CC_OK;
 }
 
 }  // extern "C"

@@ -283,4 +283,62 @@ hipError_t launch_enter(const void* embed, const int32_t* ids, const int32_t* po
 // part[S-1] (each [N][D]) when part is not null.
 hipError_t launch_residual_rmsnorm(const float* part, int S, float* h, const void* gamma, void* y,
                                    int N, int D, float eps, hipStream_t s);
+
+// ------------------------------------------------------------------ cache in 8 bits
+// One tensor (keys or values) of a cache in 8 bits: E4M3 codes (strides in bytes) and the scales'
+// exponent bytes.
+struct Kv8View {
+  KvView codes;
+  uint8_t* scale;
+  int64_t s_seq, s_layer, s_head, s_page;
+  int32_t block_shift;   // log2 of the entries a scale covers
+  int32_t paged;
+};
+
+// The smallest scale a block is given: 2^-100.  Codes of it stay clear of fp32's subnormal numbers.
+constexpr uint32_t kScaleLow = 27;
+
+// Exponent byte of the smallest power of two s with m <= 448 s (448 = 1.75 * 2^8), from the bits of
+// m >= 0 (finite).
+__device__ __forceinline__ uint32_t e8m0_of(uint32_t m_bits) {
+  const int e = int(m_bits >> 23) - 8 + ((m_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return e < int(kScaleLow) ? kScaleLow : uint32_t(e);
+}
+// The scale 2^(x - 127) and, for x >= kScaleLow, its inverse.
+__device__ __forceinline__ float e8m0_scale(uint32_t x) {
+  return __uint_as_float(x == 0 ? 0x00400000u : min(x, 254u) << 23);
+}
+__device__ __forceinline__ float e8m0_inverse(uint32_t x) { return __uint_as_float((254u - x) << 23); }
+
+// Four floats -> four E4M3 codes, round to nearest even (NaN: the NaN code).
+__device__ __forceinline__ uint32_t e4m3_pack(float a, float b, float c, float d) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
+}
+
+struct AppendLaunch {
+  int dtype;                 // of k, v, q
+  bool f8;                   // the cache is in 8 bits
+  cc_rows k, v, q;
+  void* q_out;
+  const int32_t *cached, *pos, *cu_d;
+  const int32_t* cu_h;
+  Kv8View kc, vc;            // 16/32-bit caches: codes alone, strides in bytes
+  int n_seqs, layer, n_layers, n_heads_q, n_heads_kv, head_dim, capacity, rotate;
+  double theta;
+};
+hipError_t launch_append(const AppendLaunch& a, hipStream_t s);
+
+// Compaction of a cache in 8 bits.
+struct Compact8Launch {
+  Kv8View src[2], dst[2];    // keys, values
+  const int32_t* keep;
+  const CompactList* lists;  // host, sorted by falling budget
+  int n_lists;
+  int n_layers, n_heads, per_head, head_dim, max_k;
+  bool in_place;
+  int32_t* ids[2];
+  const int32_t* cu_d;
+};
+hipError_t launch_compact8(const Compact8Launch& a, hipStream_t s);
 }  // namespace cc

@@ -1,0 +1,249 @@
+// Compaction of a cache in 8 bits: the kept entries of every cache layer and KV head move to the front
+// of their plane, dst[j] = src[keep[j]], and every destination block of entries gets a scale of its
+// own.  The entries of a destination block come from several source blocks with scales of their own, so
+// its scale is taken from the values that they stand for, and codes whose scale changes are rounded
+// again; both scales are powers of two, so only codes that leave the normal range lose bits, and an
+// entry whose source has the block's scale is a bit copy.
+//
+// A workgroup moves chunks of 128 (head_dim 64: 256) rows, whole blocks: rows in registers, 16 codes a
+// lane; a block's largest magnitude by an LDS maximum of fp32 bits (order-free); one barrier; the
+// codes.  Out of place every chunk is a workgroup.  In place one workgroup walks its plane's chunks in
+// rising order: keep is ascending, so the sources of chunk c + 1 lie at or past its first row, beyond
+// everything chunk c writes (codes and scales), and are loaded before chunk c is written; the
+// barrier of chunk c orders its own reads before its writes.  Bound by memory at many planes, by the
+// chain of chunks (a round trip for keep indices, pages and rows) at few.
+#include <algorithm>
+
+#include "cc_internal.h"
+
+namespace cc {
+namespace {
+
+constexpr int NT = 256;
+constexpr int U = 4;           // 16-byte row pieces of a thread in a chunk
+constexpr int LISTS = 64;      // lists of a launch, by value
+
+struct Args {
+  Kv8View src[2], dst[2];
+  const int32_t* keep;
+  int n_lists, n_layers, n_heads, per_head;
+  int chunks;                  // workgroups of a plane (in place: 1)
+  int id_blocks;
+  int32_t* ids[2];
+  const int32_t* cu;
+  CompactList lists[LISTS];
+};
+
+struct Piece {
+  uint4 w[U];
+  uint32_t sc[U];
+};
+
+// ids[cu_b + j] = ids[cu_b + keep[j]], in place: a chunk's reads precede its writes, and later chunks
+// read at or past their own first row.
+__device__ __forceinline__ void move_ids(const Args& a, const CompactList& L) {
+  const int32_t* keep = a.keep + L.keep_off;
+  const int base = a.cu[L.seq];
+  for (int j0 = 0; j0 < L.k; j0 += NT * 4) {
+    int32_t x[2][4] = {};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int s = base + keep[min(j0 + u * NT + int(threadIdx.x), L.k - 1)];
+      if (a.ids[0]) x[0][u] = a.ids[0][s];
+      if (a.ids[1]) x[1][u] = a.ids[1][s];
+    }
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int j = j0 + u * NT + threadIdx.x;
+      if (j < L.k) {
+        if (a.ids[0]) a.ids[0][base + j] = x[0][u];
+        if (a.ids[1]) a.ids[1][base + j] = x[1][u];
+      }
+    }
+  }
+}
+
+// Largest magnitude of 16 codes times their scale, as fp32 bits.  Codes without their sign rise with
+// the magnitudes; 0x7f is NaN and does not count.
+__device__ __forceinline__ uint32_t top_of(const uint4& w, uint32_t sc) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int s = 0; s < 32; s += 8) {
+      const uint32_t c = (x[i] >> s) & 0x7fu;
+      m = max(m, c == 0x7fu ? 0u : c);
+    }
+  const auto f = __builtin_amdgcn_cvt_pk_f32_fp8(int(m), false);
+  return __float_as_uint(f[0] * e8m0_scale(sc));
+}
+
+__device__ __forceinline__ uint4 rescale(const uint4& w, float f) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(x[i]), false);
+    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(x[i]), true);
+    y[i] = e4m3_pack(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
+  }
+  return make_uint4(y[0], y[1], y[2], y[3]);
+}
+
+template <int HD, bool INPLACE>
+__global__ __launch_bounds__(NT) void compact8_kernel(Args a) {
+  constexpr int LPR = HD / 16, ROWS = NT / LPR, CHUNK = ROWS * U;
+  __shared__ uint32_t tops[2][CHUNK / 16];
+  const int tid = threadIdx.x;
+  if (int(blockIdx.x) < a.id_blocks) {
+    move_ids(a, a.lists[a.per_head ? blockIdx.x * a.n_heads : blockIdx.x]);
+    return;
+  }
+  int i = blockIdx.x - a.id_blocks;
+  int c = 0;
+  if constexpr (!INPLACE) {
+    c = i % a.chunks;
+    i /= a.chunks;
+  }
+  const int which = i & 1;
+  i >>= 1;
+  int head = 0;
+  int list = 0;
+  head = i % a.n_heads;
+  i /= a.n_heads;
+  const int layer = i % a.n_layers;
+  i /= a.n_layers;
+  list = a.per_head ? i * a.n_heads + head : i;
+  const CompactList L = a.lists[list];
+  const int k = L.k;
+  const int nch = (k + CHUNK - 1) / CHUNK;
+  if (c >= nch) return;
+  const Kv8View sv = which ? a.src[1] : a.src[0], dv = which ? a.dst[1] : a.dst[0];
+  const int32_t* keep = a.keep + L.keep_off;
+  const int g = tid / LPR, col = (tid % LPR) * 16;
+  const int shift = sv.block_shift;
+  const char* sb = static_cast<const char*>(sv.codes.base) + int64_t(layer) * sv.codes.layer_stride +
+                   int64_t(head) * sv.codes.head_stride + (sv.paged ? 0 : int64_t(L.seq) * sv.codes.seq_stride) + col;
+  const uint8_t* ss = sv.scale + int64_t(layer) * sv.s_layer + int64_t(head) * sv.s_head +
+                      (sv.paged ? 0 : int64_t(L.seq) * sv.s_seq);
+  char* db = static_cast<char*>(const_cast<void*>(dv.codes.base)) + int64_t(layer) * dv.codes.layer_stride +
+             int64_t(head) * dv.codes.head_stride + (dv.paged ? 0 : int64_t(L.seq) * dv.codes.seq_stride) + col;
+  uint8_t* ds = dv.scale + int64_t(layer) * dv.s_layer + int64_t(head) * dv.s_head +
+                (dv.paged ? 0 : int64_t(L.seq) * dv.s_seq);
+  const int32_t* sbt = sv.paged ? sv.codes.block_table + int64_t(L.seq) * sv.codes.max_pages : nullptr;
+  const int32_t* dbt = dv.paged ? dv.codes.block_table + int64_t(L.seq) * dv.codes.max_pages : nullptr;
+  // rows past the list's end repeat its last one; they are neither counted nor written
+  auto index = [&](int ch, int (&id)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = keep[min(ch * CHUNK + u * ROWS + g, k - 1)];
+  };
+  auto load = [&](const int (&id)[U], Piece& p) {
+    int page[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) page[u] = sv.paged ? sbt[id[u] >> sv.codes.page_shift] : 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int slot = sv.paged ? id[u] & sv.codes.page_mask : id[u];
+      p.w[u] = *reinterpret_cast<const uint4*>(sb + int64_t(page[u]) * sv.codes.page_stride +
+                                               int64_t(slot) * sv.codes.tok_stride);
+      p.sc[u] = ss[int64_t(page[u]) * sv.s_page + (slot >> shift)];
+    }
+  };
+  int id[U];
+  Piece now, next;
+  index(c, id);
+  load(id, now);
+  if (INPLACE && c + 1 < nch) index(c + 1, id);
+  if (tid < 2 * (CHUNK / 16)) (&tops[0][0])[tid] = 0;
+  __syncthreads();
+  const int last = INPLACE ? nch : c + 1;
+  for (; c < last; ++c) {
+    uint32_t* top = tops[c & 1];
+    uint32_t* other = tops[(c & 1) ^ 1];
+    int dpage[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = min(c * CHUNK + u * ROWS + g, k - 1);
+      dpage[u] = dv.paged ? dbt[j >> dv.codes.page_shift] : 0;
+    }
+    if (INPLACE && c + 1 < nch) {
+      load(id, next);
+      if (c + 2 < nch) index(c + 2, id);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t m = top_of(now.w[u], now.sc[u]);
+#pragma unroll
+      for (int off = 1; off < LPR; off <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), off)));
+      const int r = u * ROWS + g;
+      if (col == 0 && c * CHUNK + r < k) atomicMax(&top[r >> shift], m);
+    }
+    __syncthreads();   // maxima whole; this chunk's rows and scales have all been read
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = u * ROWS + g, j = c * CHUNK + r;
+      if (j < k) {
+        const uint32_t e = e8m0_of(top[r >> shift]);
+        uint4 w = now.w[u];
+        if (e != now.sc[u]) w = rescale(w, e8m0_scale(now.sc[u]) * e8m0_inverse(e));
+        const int slot = dv.paged ? j & dv.codes.page_mask : j;
+        *reinterpret_cast<uint4*>(db + int64_t(dpage[u]) * dv.codes.page_stride + int64_t(slot) * dv.codes.tok_stride) = w;
+        if (col == 0 && (r & ((1 << shift) - 1)) == 0) ds[int64_t(dpage[u]) * dv.s_page + (slot >> shift)] = uint8_t(e);
+      }
+    }
+    if constexpr (INPLACE) {
+      // the other half's maxima were last read before this chunk's barrier; the next chunk's start
+      // behind the barrier below
+      if (tid < CHUNK / 16) other[tid] = 0;
+      __syncthreads();
+      now = next;
+    }
+  }
+}
+
+template <int HD>
+hipError_t launch_dim(const Compact8Launch& l, hipStream_t s) {
+  constexpr int CHUNK = NT / (HD / 16) * U;
+  const int per = l.per_head ? l.n_heads : 1;
+  const int per_launch = LISTS / per * per;
+  for (int lo = 0; lo < l.n_lists; lo += per_launch) {
+    Args a;
+    for (int t = 0; t < 2; ++t) {
+      a.src[t] = l.src[t];
+      a.dst[t] = l.dst[t];
+      a.ids[t] = l.ids[t];
+    }
+    a.keep = l.keep;
+    a.n_lists = std::min(per_launch, l.n_lists - lo);
+    std::copy_n(l.lists + lo, a.n_lists, a.lists);
+    int most = 0;
+    for (int i = 0; i < a.n_lists; ++i) most = std::max(most, a.lists[i].k);
+    if (most == 0) continue;
+    a.n_layers = l.n_layers;
+    a.n_heads = l.n_heads;
+    a.per_head = l.per_head;
+    a.cu = l.cu_d;
+    a.id_blocks = l.ids[0] || l.ids[1] ? a.n_lists / per : 0;
+    a.chunks = l.in_place ? 1 : (most + CHUNK - 1) / CHUNK;
+    const int64_t grid = a.id_blocks + int64_t(a.n_lists / per) * l.n_heads * l.n_layers * 2 * a.chunks;
+    if (grid > INT32_MAX) return hipErrorInvalidValue;
+    if (l.in_place)
+      hipLaunchKernelGGL((compact8_kernel<HD, true>), dim3(unsigned(grid)), dim3(NT), 0, s, a);
+    else
+      hipLaunchKernelGGL((compact8_kernel<HD, false>), dim3(unsigned(grid)), dim3(NT), 0, s, a);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_compact8(const Compact8Launch& l, hipStream_t s) {
+  return l.head_dim == 128 ? launch_dim<128>(l, s) : launch_dim<64>(l, s);
+}
+
+}  // namespace cc

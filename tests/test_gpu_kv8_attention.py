@@ -1,0 +1,194 @@
+"""Attention over a cache in 8 bits against fp64: few and many rows, both masks, ragged batches, every
+layout and scale block, pieces that are joined, rows that see nothing, NaN where a row may not look."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv8_oracle as O8
+from tests.gpu_util import assert_attention_close, f64
+from tests.kv8_util import Cache8, cu_of, i32
+
+pytestmark = pytest.mark.gpu
+
+
+def _problem(cc, new, hq, hkv, d, **kw):
+    return cc.problem(dtype="bf16", cu_seqlens=cu_of(new), n_heads_q=hq, n_heads_kv=hkv, head_dim=d, hidden=64, vocab=1, **kw)
+
+
+def _oracle(cache, q, new, lens, hq, hkv, mask, inclusive=False, layer=0, scale=None):
+    g, out, at = hq // hkv, [], 0
+    qh = f64(q)
+    for b, m in enumerate(new):
+        o = np.zeros((m, hq, cache.d))
+        for c in range(hkv):
+            k, v = (cache.values(layer, b, c, t, lens[b]) for t in ("k", "v"))
+            for h in range(c * g, (c + 1) * g):
+                o[:, h] = O8.attention(qh[at:at + m, h], k, v, mask, inclusive, scale)
+        out.append(o)
+        at += m
+    return np.concatenate(out)
+
+
+def _run(cc, cache, q, new, lens, hq, hkv, mask, layer=0, longest=None, **kw):
+    p = _problem(cc, new, hq, hkv, cache.d, **kw)
+    o = torch.full_like(q, 7.0)
+    cc.cc_attention_kv8(p, q, cache.view(cc), layer, i32(lens), max(lens) if longest is None else longest, o, mask=mask)
+    torch.cuda.synchronize()
+    return o
+
+
+def _q(new, hq, d, seed):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(sum(new), hq, d, generator=g).to(torch.bfloat16).cuda()
+
+
+CASES = [
+    # new, lens, hq, hkv, d, page, block
+    ([1], [1], 4, 2, 128, 0, 16),
+    ([1], [17], 8, 1, 128, 0, 16),
+    ([1, 1, 1, 1], [1, 64, 65, 333], 28, 4, 128, 16, 16),
+    ([1, 1], [1500, 40], 32, 8, 128, 64, 64),
+    ([1, 3, 0, 8], [100, 3, 9, 257], 16, 4, 64, 16, 16),
+    ([5], [700], 20, 2, 128, 32, 16),          # 50 rows of a KV head: four row blocks
+    ([7], [130], 12, 4, 64, 128, 128),         # 21: two
+    ([20, 2], [20, 300], 8, 2, 128, 16, 16),   # many beside few
+    ([64], [1000], 4, 4, 128, 64, 32),
+    ([130, 33], [130, 500], 14, 2, 128, 16, 16),
+    ([200], [321], 8, 8, 64, 0, 64),
+    ([257], [257], 4, 2, 64, 32, 32),
+]
+
+
+@pytest.mark.parametrize("mask", ["causal", "counter", "counter_inclusive"])
+@pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
+def test_attention(case, mask):
+    from paper_2607_27600_amd import cc
+    new, lens, hq, hkv, d, page, block = case
+    print(f"[attn8] {case} {mask}", flush=True)
+    cache = Cache8(lens, hkv, d, layers=2, page=page, block=block, seed=21, fill=0x7f)
+    q = _q(new, hq, d, 22)
+    kw = dict(diag="inclusive") if mask == "counter_inclusive" else {}
+    name = mask.split("_")[0]
+    o = _run(cc, cache, q, new, lens, hq, hkv, name, layer=1, **kw)
+    assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, name, bool(kw), layer=1), f"{case} {mask}")
+
+
+@pytest.mark.parametrize("new,lens,hq,hkv,d", [([1], [9000], 4, 1, 128), ([1, 1], [5001, 37], 4, 2, 64),
+                                               ([70], [4100], 2, 1, 128), ([300, 1], [3000, 2500], 2, 2, 64)])
+def test_attention_in_pieces(new, lens, hq, hkv, d):
+    """Long caches of few heads are cut into pieces and joined; the plan may reach beyond the longest."""
+    from paper_2607_27600_amd import cc
+    print(f"[attn8 pieces] {new} {lens} {hq} {hkv} {d}", flush=True)
+    cache = Cache8(lens, hkv, d, page=16, block=16, seed=23, fill=0x7f, room=5000)
+    q = _q(new, hq, d, 24)
+    want = _oracle(cache, q, new, lens, hq, hkv, "causal")
+    for longest in (max(lens), max(lens) + 4321):
+        o = _run(cc, cache, q, new, lens, hq, hkv, "causal", longest=longest)
+        assert_attention_close(f64(o), want, f"{longest}")
+    again = _run(cc, cache, q, new, lens, hq, hkv, "causal", longest=max(lens))
+    assert torch.equal(again, _run(cc, cache, q, new, lens, hq, hkv, "causal", longest=max(lens)))
+
+
+@pytest.mark.parametrize("new,d", [([3, 5, 2], 128), ([100, 5, 70], 128), ([100, 90, 2], 64)])
+def test_rows_that_see_nothing(new, d):
+    """More queries than entries: those that stand before the first see nothing (causal); an empty sequence."""
+    from paper_2607_27600_amd import cc
+    hq, hkv = 4, 2
+    lens = [2, 0, 1]
+    cache = Cache8([max(x, 1) for x in lens], hkv, d, page=16, block=16, seed=25, fill=0x7f, room=64)
+    q = _q(new, hq, d, 26)
+    for mask in ("causal", "counter"):
+        o = _run(cc, cache, q, new, lens, hq, hkv, mask, longest=90)
+        want = _oracle(cache, q, new, lens, hq, hkv, mask)
+        assert_attention_close(f64(o), want, mask)
+        assert np.all(f64(o)[(want == 0).all(-1)] == 0)
+
+
+@pytest.mark.parametrize("new,n", [([4], 100), ([40], 200), ([150], 150)])
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("mask", ["causal", "counter"])
+def test_nan_reaches_only_rows_that_see_it(new, n, d, mask):
+    from paper_2607_27600_amd import cc
+    hq, hkv, m = 4, 2, new[0]
+    print(f"[attn8 nan] {new} {n} {d} {mask}", flush=True)
+    cache = Cache8([n], hkv, d, page=16, block=16, seed=27, fill=0x7f, room=64)
+    # a NaN value in one dim, and a NaN key, in entries that only some of the queries see
+    tv, tk = n - 2, n - 1 - m // 2
+    for c, t, e, which in ((0, tv, 5, "v"), (1, tk, 9, "k")):
+        codes, sc = cache.plane(0, 0, c, which, n=n)
+        codes[t, e] = 0xff
+        cache.put(0, 0, c, which, codes, sc)
+        cache.t[which].copy_(torch.from_numpy(cache.host[which]))
+    q = _q(new, hq, d, 28)
+    o = f64(_run(cc, cache, q, new, [n], hq, hkv, mask))
+    want = _oracle(cache, q, new, [n], hq, hkv, mask)
+    at = np.arange(m) + n - m
+    sees = (lambda t: at >= t) if mask == "causal" else (lambda t: at < t)
+    nan = np.zeros_like(want, dtype=bool)
+    nan[np.ix_(sees(tv), [0, 1], [5])] = True
+    nan[np.ix_(sees(tk), [2, 3])] = True
+    np.testing.assert_array_equal(np.isnan(want), nan)
+    np.testing.assert_array_equal(np.isnan(o), nan)
+    assert_attention_close(np.where(nan, 0, o), np.where(nan, 0, want))
+
+
+@pytest.mark.parametrize("new,n", [([1], 300), ([90], 300)])
+def test_scales_far_apart_and_peaked_rows(new, n):
+    """Blocks whose scales differ by 2^60, and logits so large that one entry takes all."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d = 4, 1, 128
+    cache = Cache8([n], hkv, d, block=16, seed=29)
+    codes, sc = cache.plane(0, 0, 0, "v", n=n)
+    sc[:] = np.random.default_rng(30).integers(97, 157, len(sc))
+    cache.put(0, 0, 0, "v", codes, sc)
+    codes, sc = cache.plane(0, 0, 0, "k", n=n)
+    sc[::3] += 4
+    cache.put(0, 0, 0, "k", codes, sc)
+    for t in ("k", "v", "ks", "vs"):
+        cache.t[t].copy_(torch.from_numpy(cache.host[t]))
+    q = _q(new, hq, d, 31)
+    want = _oracle(cache, q, new, [n], hq, hkv, "causal")
+    o = f64(_run(cc, cache, q, new, [n], hq, hkv, "causal"))
+    # Relative to the row's probability-weighted magnitudes: the probabilities and the output are
+    # rounded to bf16 (2^-8 each); logits reach some hundreds here, and fp32 sums of 128 products leave
+    # up to 2^-17 of that, 1e-3 of a probability.
+    k, v = cache.values(0, 0, 0, "k", n), np.abs(cache.values(0, 0, 0, "v", n))
+    size = np.stack([O8.attention(f64(q)[:, h], k, v, "causal") for h in range(hq)], 1)
+    assert np.all(np.abs(o - want) <= (2.0 ** -8 + 1e-3) * size + 2.0 ** -8 * np.abs(want))
+
+
+def test_lengths_on_the_device_in_a_graph():
+    """A captured call follows kv_lens; lengths beyond the plan are cut to it, negative ones are empty."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d, new = 8, 2, 128, [1, 1, 2]
+    cache = Cache8([600, 300, 77], hkv, d, page=16, block=16, seed=32, room=200)
+    q = _q(new, hq, d, 33)
+    p = _problem(cc, new, hq, hkv, d)
+    kv, lens = cache.view(cc), i32([1, 1, 2])
+    o = torch.empty_like(q)
+    ws = torch.empty(max(1, cc.cc_attention_kv8_workspace(p, "causal", 600)), dtype=torch.uint8, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    cc.cc_attention_kv8(p, q, kv, 0, lens, 600, o, workspace=ws)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        cc.cc_attention_kv8(p, q, kv, 0, lens, 600, o, workspace=ws)
+    for now in ([600, 300, 77], [1, 17, 2], [599, 0, 40], [10**6, -5, 77]):
+        lens.copy_(i32(now))
+        o.fill_(3.0)
+        g.replay()
+        torch.cuda.synchronize()
+        real = [min(max(x, 0), 600) for x in now]
+        assert_attention_close(f64(o), _oracle(cache, q, new, real, hq, hkv, "causal"), str(now))
+
+
+def test_sequences_beyond_the_listed_ones():
+    """More sequences of both classes than a launch lists."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d = 4, 2, 64
+    r = np.random.default_rng(34)
+    new = [int(x) for x in r.choice([0, 1, 1, 2, 40], 150)]
+    lens = [m + int(x) for m, x in zip(new, r.integers(1, 60, 150))]
+    cache = Cache8(lens, hkv, d, page=16, block=16, seed=35, fill=0x7f)
+    q = _q(new, hq, d, 36)
+    o = _run(cc, cache, q, new, lens, hq, hkv, "causal")
+    assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, "causal"))

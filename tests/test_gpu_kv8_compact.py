@@ -1,0 +1,112 @@
+"""Compaction of a cache in 8 bits: codes, scales, ids and positions bit for bit as the oracle's, in place
+and out of place, contiguous and paged, one list or one per head; other bytes untouched."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv8_oracle as O8
+from tests.kv8_util import Cache8, cu_of, i32
+
+pytestmark = pytest.mark.gpu
+
+CASES = [
+    # lens, kept, hkv, d, layers, page, block, per_head
+    ([1], [1], 1, 64, 1, 0, 16, 0),
+    ([40], [0], 2, 128, 1, 0, 16, 0),
+    ([768], [512], 4, 128, 2, 0, 16, 0),
+    ([300, 5, 130], [77, 5, 1], 2, 128, 2, 16, 16, 0),
+    ([1000, 257], [1000, 129], 2, 128, 1, 64, 64, 0),
+    ([513], [400], 2, 64, 1, 128, 128, 0),
+    ([700, 90], [513, 17], 2, 64, 1, 32, 32, 1),
+    ([260], [131], 3, 128, 1, 128, 128, 1),
+]
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
+def test_compact(case, in_place):
+    from paper_2607_27600_amd import cc
+    lens, kept, hkv, d, layers, page, block, per_head = case
+    print(f"[compact8] {case} in_place={in_place}", flush=True)
+    r = np.random.default_rng(11)
+    c = Cache8(lens, hkv, d, layers=layers, page=page, block=block, seed=12)
+    dst = c if in_place else Cache8(lens, hkv, d, layers=layers, page=page, block=block, seed=13)
+    per = hkv if per_head else 1
+    budgets = [max(0, min(n, k + (h if k else 0))) for n, k in zip(lens, kept) for h in range(per)]
+    lists = [np.sort(r.permutation(lens[i // per])[:k]).astype(np.int32) for i, k in enumerate(budgets)]
+    N = sum(lens)
+    ids = r.integers(0, 1000, N).astype(np.int32)
+    pos = r.integers(0, 1 << 20, N).astype(np.int32)
+    idd, posd = torch.from_numpy(ids.copy()).cuda(), torch.from_numpy(pos.copy()).cuda()
+    keep = torch.from_numpy(np.concatenate(lists + [np.zeros(1, np.int32)])).cuda()
+    p = cc.problem(dtype="bf16", cu_seqlens=cu_of(lens), n_heads_q=hkv, n_heads_kv=hkv, head_dim=d, hidden=64, vocab=1)
+    cc.cc_compact_kv8(p, c.view(cc), keep, budgets, per_head, idd, posd, out=None if in_place else dst.view(cc))
+    torch.cuda.synchronize()
+    after = dst.read()
+    want = {k: v.copy() for k, v in dst.host.items()}
+    cu = cu_of(lens)
+    for b in range(len(lens)):
+        for h in range(hkv):
+            kl = lists[b * per + (h if per_head else 0)]
+            for l in range(layers):
+                for t in ("k", "v"):
+                    codes, sc = O8.compact(*c.plane(l, b, h, t, n=lens[b]), kl, block)
+                    e = np.arange(len(kl))
+                    pg, sl = dst._where(b, e)
+                    want[t][l, pg, h, sl, :d] = codes
+                    e = np.arange(0, len(kl), block)
+                    pg, sl = dst._where(b, e)
+                    want[t + "s"][l, pg, h, sl // block] = sc
+        first = lists[b * per]
+        ids[cu[b]:cu[b] + len(first)] = ids[cu[b] + first]
+        pos[cu[b]:cu[b] + len(first)] = pos[cu[b] + first]
+    for k in want:
+        np.testing.assert_array_equal(after[k], want[k], err_msg=k)
+    if not in_place:
+        for k, v in c.read().items():
+            np.testing.assert_array_equal(v, c.host[k])
+    np.testing.assert_array_equal(idd.cpu().numpy(), ids)
+    np.testing.assert_array_equal(posd.cpu().numpy(), pos)
+
+
+def test_many_sequences_take_several_launches():
+    from paper_2607_27600_amd import cc
+    r = np.random.default_rng(15)
+    lens = r.integers(0, 90, 150).tolist()
+    lens[0] = 90
+    kept = [int(x) for x in (np.array(lens) * r.uniform(0, 1, 150)).astype(int)]
+    c = Cache8(lens, 1, 64, page=16, block=16, seed=16)
+    lists = [np.sort(r.permutation(n)[:k]).astype(np.int32) for n, k in zip(lens, kept)]
+    keep = torch.from_numpy(np.concatenate(lists)).cuda()
+    p = cc.problem(dtype="bf16", cu_seqlens=cu_of(lens), n_heads_q=1, n_heads_kv=1, head_dim=64, hidden=64, vocab=1)
+    cc.cc_compact_kv8(p, c.view(cc), keep, kept, 0)
+    torch.cuda.synchronize()
+    after = c.read()
+    for b, kl in enumerate(lists):
+        for t in ("k", "v"):
+            codes, sc = O8.compact(*c.plane(0, b, 0, t, n=max(lens[b], 1)), kl, 16)
+            gc, gs = c.plane(0, b, 0, t, src=after, n=max(len(kl), 1))
+            np.testing.assert_array_equal(gc[: len(kl)], codes)
+            np.testing.assert_array_equal(gs[: len(sc)], sc)
+
+
+def test_nan_codes_and_extreme_scales():
+    """NaN codes stay NaN and do not count; scales far apart in one block."""
+    from paper_2607_27600_amd import cc
+    c = Cache8([64], 1, 128, block=16, seed=17)
+    codes, sc = c.plane(0, 0, 0, "k", n=64)
+    sc[:] = [27, 120, 60, 200]
+    codes[1, 3], codes[33, 4], codes[50] = 0x7f, 0xff, 0
+    c.put(0, 0, 0, "k", codes, sc)
+    c.t["k"].copy_(torch.from_numpy(c.host["k"]))
+    c.t["ks"].copy_(torch.from_numpy(c.host["ks"]))
+    kl = np.array([0, 1, 2, 17, 20, 33, 40, 47, 48, 49, 50, 63], np.int32)
+    p = cc.problem(dtype="bf16", cu_seqlens=[0, 64], n_heads_q=1, n_heads_kv=1, head_dim=128, hidden=64, vocab=1)
+    cc.cc_compact_kv8(p, c.view(cc), torch.from_numpy(kl).cuda(), [len(kl)], 0)
+    torch.cuda.synchronize()
+    want, ws = O8.compact(codes, sc, kl, 16)
+    gc, gs = c.plane(0, 0, 0, "k", src=c.read(), n=len(kl))
+    nan = (want & 0x7f) == 0x7f
+    np.testing.assert_array_equal((gc & 0x7f) == 0x7f, nan)
+    np.testing.assert_array_equal(gc[~nan], want[~nan])
+    np.testing.assert_array_equal(gs, ws)
