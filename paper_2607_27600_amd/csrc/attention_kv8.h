@@ -5,7 +5,10 @@
 
 namespace cc {
 
-constexpr int FEW_ROWS = 64;     // rows (queries times heads of a group) up to which a sequence counts as few
+// Rows (queries times heads of a group) up to which a sequence counts as few.  Four row blocks of the
+// kernel for few against the one for many, 8000 entries and 8 KV heads of 128: 64 rows 41.5 us and (68
+// rows) 31.6, sixteen such sequences 328 and 122; two row blocks, 32 rows: 26.4 and 31, sixteen 128 and 122.
+constexpr int FEW_ROWS = 32;
 constexpr int FEW_NT = 256;
 constexpr int KV8_LIST = 64;     // sequences of a launch listed by value
 constexpr int MANY_ROWS = 128;   // rows of a block of the kernel for many

@@ -475,7 +475,7 @@ template <int HD>
 hipError_t launch_dim(const Kv8Args& a, bool few, hipStream_t s) {
   hipError_t e;
   if (few)
-    e = a.R <= 16 ? few_rows<HD, 1>(a, s) : a.R <= 32 ? few_rows<HD, 2>(a, s) : few_rows<HD, 4>(a, s);
+    e = a.R <= 16 ? few_rows<HD, 1>(a, s) : few_rows<HD, 2>(a, s);
   else
     e = launch_attn_many(a, s);
   if (e != hipSuccess || a.splits == 1) return e;

@@ -5,12 +5,18 @@
 // pair, and walks tiles of 64 entries.  S^T = K Q^T and O^T = V^T P^T on 32x32x16 MFMA: a lane owns one
 // row, its softmax stays in its registers, and its P feeds the second product from them.
 //
-// A tile's codes are loaded 16 bytes a lane a whole tile ahead, and turned into bf16 once for the
-// four waves, on the way into LDS: 32 conversions, 8 LDS writes a wave and tile.  (Turning them into
-// operands in every wave instead would cost each wave 128.)  In LDS a tile is bf16 rows whose 16-byte
-// chunks are swizzled by bits of the row so that fragment reads hit every bank once; V^T is read
-// with transpose reads.  Two K and two V buffers, one barrier a tile.  Matrix work of one tile is
-// interleaved with the exponentials of the tile before.
+// A tile's codes go from memory straight into LDS while the tile before is worked on (each lane reads
+// back what its own load brought, so they need no barrier, and no registers for a whole step: with the
+// codes held in registers instead the kernel spilled 376 bytes a lane and ran at a sixth of its
+// speed), and are turned into bf16 once for the four waves: 32 conversions, 8 LDS writes a wave and
+// tile.  (Turning them into operands in every wave would cost each 128.)  In LDS a tile is bf16 rows
+// whose 16-byte chunks are swizzled by bits of the row so that fragment reads hit every bank once; V^T
+// is read with transpose reads.  Two K and two V buffers, one barrier a tile.  Matrix work of one tile
+// is interleaved with the exponentials of the tile before.
+//
+// A NaN value in a tile that some rows see in part becomes the least bf16 number, 2^-133: nothing beside
+// fp32 sums, and told from every other value by its last bit (E4M3 values end in zeros).  A tile that
+// holds one sends its rows through a loop over its codes, which sets NaN where a row sees it.
 #include <type_traits>
 
 #include "attention_kv8.h"
@@ -46,6 +52,23 @@ __device__ __forceinline__ v4i16 ds_read_tr(const char* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16*)(p));
 }
 
+// 16 bytes a lane from sbase + voff into LDS at lds + 16 * lane, by the wave.  The loads are waited for
+// where their bytes are read.
+__device__ __forceinline__ void dma16(const char* sbase, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds)
+               : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(p)));
+}
+// A wave-uniform pointer in scalar registers.
+__device__ __forceinline__ const char* uniform_ptr(const char* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(u));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(u >> 32));
+  return reinterpret_cast<const char*>((uint64_t(hi) << 32) | lo);
+}
+
 // Sixteen codes times the scale, in bf16: exact.
 __device__ __forceinline__ void widen16(const uint4& w, float scale, uint4& lo, uint4& hi) {
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};
@@ -68,6 +91,9 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
   __shared__ __attribute__((aligned(1024))) u16 kb1[TILE];
   __shared__ __attribute__((aligned(1024))) u16 vb0[TILE];
   __shared__ __attribute__((aligned(1024))) u16 vb1[TILE];
+  // codes on their way: [load][wave][lane][16]
+  __shared__ __attribute__((aligned(1024))) char kraw[BN * HD];
+  __shared__ __attribute__((aligned(1024))) char vraw[BN * HD];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hi = lane >> 5, col = lane & 31;
@@ -168,29 +194,54 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
       const int at = gg - gbase;
       return at < 64 ? __builtin_amdgcn_readlane(cur, at) : __builtin_amdgcn_readlane(nxt, min(at - 64, 63));
     };
-    auto load = [&](const char* plane, int t, uint4 (&w)[NI]) {
+    const uint32_t ts = uint32_t(a.k.codes.tok_stride);
+    auto load = [&](char* raw, const char* plane, int t) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int gg = group_of(t, i);
         const int pg = held(page, page_n, gg);
         const int slot = a.k.paged ? (gg << 4) & a.k.codes.page_mask : gg << 4;
-        const char* base = plane + int64_t(pg) * a.k.codes.page_stride + int64_t(slot) * a.k.codes.tok_stride;
-        const int r = min((lrow + i * RSTEP) & 15, last - (gg << 4));
-        w[i] = *reinterpret_cast<const uint4*>(base + int64_t(r) * a.k.codes.tok_stride + piece * 16);
+        const char* base =
+            uniform_ptr(plane + (int64_t(pg) * a.k.codes.page_stride + int64_t(slot) * a.k.codes.tok_stride));
+        const int r = min((lrow + i * RSTEP) & 15, last - (gg << 4));   // past the end: the last entry again
+        dma16(base, uint32_t(r) * ts + piece * 16, lds_addr(raw + (i * NWAVES + wave) * 1024));
       }
     };
-    auto put = [&](u16* dst, const uint32_t (&at)[2], int t, int which, const uint4 (&w)[NI]) {
+    auto is_masked = [&](int t) { return t * BN < full0 || t * BN + BN > min(full1, stop); };
+    auto put = [&](u16* dst, const char* raw, const uint32_t (&at)[2], int t, auto values) {
+      constexpr bool V = decltype(values)::value;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const uint32_t sc = uint32_t(held(int(scale), int(scale_n), group_of(t, i)));
-        uint4 y[2], z = w[i];
-        if (which && t * BN + BN > len && t * BN + lrow + i * RSTEP >= len) z = make_uint4(0, 0, 0, 0);
-        widen16(z, e8m0_scale((sc >> (8 * which)) & 255u), y[0], y[1]);
+        uint4 y[2], z = *reinterpret_cast<const uint4*>(raw + (i * NWAVES + wave) * 1024 + lane * 16);
+        const float f = e8m0_scale((sc >> (V ? 8 : 0)) & 255u);
+        if (V && is_masked(t)) {
+          uint32_t w[4] = {z.x, z.y, z.z, z.w}, n[4];
+          const bool out = t * BN + lrow + i * RSTEP >= len;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            n[k] = out ? 0 : ((w[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // 0x80 at a NaN code
+            w[k] = out ? 0 : w[k] & ~((n[k] >> 7) * 0xffu);
+          }
+          widen16(make_uint4(w[0], w[1], w[2], w[3]), f, y[0], y[1]);
+          auto tag = [](uint32_t& lo, uint32_t& hi, uint32_t m) {
+            lo |= ((m >> 7) & 1u) | ((m << 1) & 0x10000u);
+            hi |= ((m >> 23) & 1u) | ((m >> 15) & 0x10000u);
+          };
+          tag(y[0].x, y[0].y, n[0]);
+          tag(y[0].z, y[0].w, n[1]);
+          tag(y[1].x, y[1].y, n[2]);
+          tag(y[1].z, y[1].w, n[3]);
+        } else {
+          widen16(z, f, y[0], y[1]);
+        }
         char* d = reinterpret_cast<char*>(dst) + i * RSTEP * ROWB;
         *reinterpret_cast<uint4*>(d + at[0]) = y[0];
         *reinterpret_cast<uint4*>(d + at[1]) = y[1];
       }
     };
+    // the codes that this wave asked for have arrived
+    auto arrived = [] { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
 
     uint32_t koff[NKS];
 #pragma unroll
@@ -233,14 +284,18 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
       return key >= lo && key < past;
     };
 
-    uint4 kr[NI], vr[NI];
-    load(kplane, tb, kr);
-    load(vplane, tb, vr);
-    put(kb0, kst, tb, 0, kr);
-    put(vb0, vst, tb, 1, vr);
+    using Keys = std::false_type;
+    using Values = std::true_type;
+    load(kraw, kplane, tb);
+    load(vraw, vplane, tb);
+    arrived();
+    put(kb0, kraw, kst, tb, Keys{});
+    put(vb0, vraw, vst, tb, Values{});
     if (tb + 1 < te) {
-      load(kplane, tb + 1, kr);
-      put(kb1, kst, tb + 1, 0, kr);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the codes have been read back
+      load(kraw, kplane, tb + 1);
+      arrived();
+      put(kb1, kraw, kst, tb + 1, Keys{});
     }
     __syncthreads();
     f32x16 sa[2], sb[2];
@@ -250,6 +305,26 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
     for (int q = 0; q < NS; ++q) sa[q & 1] = mfma32(kfrag(kb0, q), qf[q >> 1], sa[q & 1]);
     if (tb + 2 < te) __syncthreads();   // every wave has read K(tb) before its buffer is refilled
     float mx = row_max(sa);
+
+    // NaN into the outputs of rows that see a NaN value in tile t.
+    auto poison = [&](int t) {
+#pragma unroll 1
+      for (int key = max(t * BN, lo); key < min(t * BN + BN, past); ++key) {
+        const int gg = key >> 4;
+        const int pg = a.k.paged ? table[gg >> (a.k.codes.page_shift - 4)] : 0;
+        const int slot = a.k.paged ? key & a.k.codes.page_mask : key;
+        const char* v = vplane + int64_t(pg) * a.k.codes.page_stride + int64_t(slot) * a.k.codes.tok_stride + 4 * hi;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(v + db * 32 + q * 8);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (((w >> (8 * e)) & 0x7fu) == 0x7fu) acc[db][q * 4 + e] = __uint_as_float(0x7fc00000u);
+          }
+      }
+    };
 
     // Tile t with parity P: S(t) in sc, its unmasked row maximum in mx; K(t+1) and V(t) in LDS.  The codes
     // of K(t+2) and V(t+1) are loaded at the start and written at the end, into buffers that the tile
@@ -262,9 +337,9 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
       u16* Kfree = P ? kb1 : kb0;
       const u16* Vc = P ? vb1 : vb0;
       u16* Vfree = P ? vb0 : vb1;
-      if (t + 2 < te) load(kplane, t + 2, kr);
-      if (t + 1 < te) load(vplane, t + 1, vr);
-      const bool masked = t * BN < full0 || t * BN + BN > min(full1, stop);
+      if (t + 2 < te) load(kraw, kplane, t + 2);
+      if (t + 1 < te) load(vraw, vplane, t + 1);
+      const bool masked = is_masked(t);
       bf16x8 kf[4];
       kf[0] = kfrag(Kn, 0);
       kf[1] = kfrag(Kn, 1);
@@ -302,6 +377,16 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
 #pragma unroll
         for (int db = 0; db < NDB; ++db) acc[db] *= corr;
       }
+      bool tagged = false;
+      if (masked) {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int q = 0; q < NPV; ++q) {
+          const uint4 w = __builtin_bit_cast(uint4, vfrag(Vc, q));
+          bits |= w.x | w.y | w.z | w.w;
+        }
+        tagged = __any((bits & 0x00010001u) != 0);
+      }
       bf16x8 pf[4];
       auto pack = [&](int kk) {
 #pragma unroll
@@ -309,76 +394,43 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
       };
       __builtin_amdgcn_s_setprio(0);
       float ls0 = 0.f, ls1 = 0.f, m0 = -INFINITY, m1 = -INFINITY;
-      if (masked) {
-        // NaN codes of values, taken out and counted by the rows that see them
+      bf16x8 vf[4];
+      vf[0] = vfrag(Vc, 0);
+      vf[1] = vfrag(Vc, 1);
+      vf[2] = vfrag(Vc, 2);
+      pack(0);
+      constexpr int SPM = 32 / NPV;
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          pack(kk);
-          bf16x8 see;
+      for (int q = 0; q < NPV; ++q) {
+        if (q + 3 < NPV) vf[(q + 3) & 3] = vfrag(Vc, q + 3);
+        acc[q % NDB] = mfma32(vf[q & 3], pf[q / NDB], acc[q % NDB]);
+        if (q % NDB == NDB - 1 && q < NPV - 1) pack(q / NDB + 1);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            see[e] = (__bf16)(seen(t, kk >> 1, (kk & 1) * 8 + e) ? 1.f : 0.f);
-            ls0 += sc[kk >> 1][(kk & 1) * 8 + e];
-          }
-#pragma unroll
-          for (int db = 0; db < NDB; ++db) {
-            const bf16x8 v = vfrag(Vc, kk * NDB + db);
-            v8i16 w = __builtin_bit_cast(v8i16, v), one;
-            bool nan = false;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const bool n = (w[e] & 0x7fff) > 0x7f80;
-              nan |= n;
-              one[e] = n ? 0x3f80 : 0;
-              w[e] = n ? 0 : w[e];
-            }
-            acc[db] = mfma32(__builtin_bit_cast(bf16x8, w), pf[kk], acc[db]);
-            if (__any(nan)) {
-              const f32x16 hits = mfma32(__builtin_bit_cast(bf16x8, one), see, f32x16{});
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (hits[e] > 0.f) acc[db][e] = __uint_as_float(0x7fc00000u);
-            }
-          }
+        for (int u = 0; u < SPM; u += 2) {
+          ls0 += sc[(SPM * q + u) >> 4][(SPM * q + u) & 15];
+          ls1 += sc[(SPM * q + u + 1) >> 4][(SPM * q + u + 1) & 15];
         }
-        m0 = row_max(sn);
-      } else {
-        bf16x8 vf[4];
-        vf[0] = vfrag(Vc, 0);
-        vf[1] = vfrag(Vc, 1);
-        vf[2] = vfrag(Vc, 2);
-        pack(0);
-        constexpr int SPM = 32 / NPV;
+        asm volatile("" : "+v"(ls0), "+v"(ls1));
+        // the row maximum of S(t+1): 32 entries over the later slots
+        constexpr int PER = (32 + NPV - 3) / (NPV - 2);
+        if (q >= 2) {
+#pragma unroll
+          for (int u = 0; u < PER; ++u) {
+            const int f = PER * (q - 2) + u;
+            if (f < 16) m0 = fmaxf(m0, sn[0][f]);
+            else if (f < 32) m1 = fmaxf(m1, sn[1][f - 16]);
+          }
+          asm volatile("" : "+v"(m0), "+v"(m1));
+        }
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int q = 0; q < NPV; ++q) {
-          if (q + 3 < NPV) vf[(q + 3) & 3] = vfrag(Vc, q + 3);
-          acc[q % NDB] = mfma32(vf[q & 3], pf[q / NDB], acc[q % NDB]);
-          if (q % NDB == NDB - 1 && q < NPV - 1) pack(q / NDB + 1);
-#pragma unroll
-          for (int u = 0; u < SPM; u += 2) {
-            ls0 += sc[(SPM * q + u) >> 4][(SPM * q + u) & 15];
-            ls1 += sc[(SPM * q + u + 1) >> 4][(SPM * q + u + 1) & 15];
-          }
-          asm volatile("" : "+v"(ls0), "+v"(ls1));
-          // the row maximum of S(t+1): 32 entries over the later slots
-          constexpr int PER = (32 + NPV - 3) / (NPV - 2);
-          if (q >= 2) {
-#pragma unroll
-            for (int u = 0; u < PER; ++u) {
-              const int f = PER * (q - 2) + u;
-              if (f < 16) m0 = fmaxf(m0, sn[0][f]);
-              else if (f < 32) m1 = fmaxf(m1, sn[1][f - 16]);
-            }
-            asm volatile("" : "+v"(m0), "+v"(m1));
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        }
       }
+      if (masked && tagged) poison(t);
       l_run = l_run * corr + (ls0 + ls1);
       mx = half_max(fmaxf(m0, m1));
-      if (t + 2 < te) put(Kfree, kst, t + 2, 0, kr);
-      if (t + 1 < te) put(Vfree, vst, t + 1, 1, vr);
+      arrived();
+      if (t + 2 < te) put(Kfree, kraw, kst, t + 2, Keys{});
+      if (t + 1 < te) put(Vfree, vraw, vst, t + 1, Values{});
       // the next 64 groups: pages in the middle of these, scales behind them
       const int at = t + 1 - gbase / 4;
       if (at == 4) page_n = pages_at(gbase + 64);
