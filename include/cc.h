@@ -470,6 +470,29 @@ cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv,
                            int32_t mask, const int32_t* kv_lens, int32_t max_kv_len, void* o,
                            void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------ log-probabilities */
+
+/* Most alternatives per row of cc_lmhead_logprobs. */
+#define CC_LOGPROBS_MAX_TOP 32
+
+/* Workspace for cc_lmhead_logprobs. */
+cc_status cc_lmhead_logprobs_workspace(int32_t dtype, int32_t n, int32_t vocab, int32_t hidden,
+                                       int32_t top, size_t* bytes);
+
+/* Log-probabilities of the LM head's distribution, row by row: with z = W_lm u_i,
+ *   logprob[i] = z[ids[i]] - logsumexp(z),   entropy[i] = -sum_v p_v log p_v,
+ *   top_ids[i][0..top) the words of the largest logits, falling (ties: the lower id first),
+ *   top_logprob[i][r] = z[top_ids[i][r]] - logsumexp(z).
+ * u [n][hidden] and w_lm [vocab][hidden] bf16 (packed = 1: w_lm in the layout of
+ * cc_pack_lmhead), hidden a multiple of 64, fp32 accumulation.  0 <= top <= min(vocab,
+ * CC_LOGPROBS_MAX_TOP).  logprob and ids (both or neither), entropy, and with top = 0 the top
+ * arrays may be NULL.  The [n][vocab] logits are never materialised.  A NaN logit ranks below every
+ * other (the row's log-probabilities and entropy are then NaN). */
+cc_status cc_lmhead_logprobs(int32_t dtype, const void* u, const void* w_lm, int32_t packed, int32_t n,
+                             int32_t vocab, int32_t hidden, const int32_t* ids, int32_t top,
+                             float* logprob, float* entropy, int32_t* top_ids, float* top_logprob,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

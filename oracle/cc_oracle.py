@@ -133,6 +133,17 @@ def surprise(u, w_lm, ids, spread: bool = False) -> tuple:
     return lse - zt, lse, zt
 
 
+def logprobs(u, w_lm, ids, k: int) -> dict:
+    """log P of ids, entropy and the k most probable words (ties: the lower id) of each row of
+    softmax(u W_lm^T)."""
+    z = lm_head_logits(u, w_lm)
+    lp = z - logsumexp_rows(z)[:, None]
+    order = np.argsort(-z, axis=1, kind="stable")[:, :k]
+    return {"logprob": None if ids is None else lp[np.arange(len(z)), np.asarray(ids, dtype=np.int64)],
+            "entropy": -(np.exp(lp) * lp).sum(1), "top_ids": order,
+            "top_logprob": np.take_along_axis(lp, order, 1), "logits": z}
+
+
 def edge_rows(cu_seqlens, n_frozen: int = 0) -> np.ndarray:
     """Boolean mask over all N rows: True where the score is +inf by rule (the last
     entry of each sequence, and the first n_frozen entries of each sequence)."""

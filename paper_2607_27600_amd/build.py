@@ -16,7 +16,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["attention.hip", "attention_f32.hip", "lmhead.hip", "gemm_f32.hip", "projections.hip", "select.hip", "compact.hip", "fullpass.hip",
-           "append.hip", "compact8.hip", "attention_kv8.hip", "attention_kv8_many.hip", "cc_api.hip"]
+           "append.hip", "compact8.hip", "attention_kv8.hip", "attention_kv8_many.hip",
+           "logprobs.hip", "cc_api.hip"]
 
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}",

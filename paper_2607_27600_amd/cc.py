@@ -27,6 +27,7 @@ CC_DIAG_STRICT, CC_DIAG_INCLUSIVE = 0, 1
 CC_MODE_LAST_LAYER, CC_MODE_FULL, CC_MODE_LAST_LAYER_H, CC_MODE_LAST_LAYER_FUSED = 0, 1, 2, 3
 CC_KV_CONTIGUOUS, CC_KV_PAGED = 0, 1
 CC_MASK_CAUSAL, CC_MASK_COUNTER_CAUSAL = 0, 1
+CC_LOGPROBS_MAX_TOP = 32
 
 EXPORTED = [
     "cc_status_str", "cc_version", "cc_score_workspace", "cc_score", "cc_attention_workspace",
@@ -37,6 +38,7 @@ EXPORTED = [
     "cc_lmhead_fp8_workspace", "cc_lmhead_score_fp8", "cc_pack_lmhead_bytes", "cc_pack_lmhead",
     "cc_lmhead_score_packed", "cc_lmhead_score_noalloc", "cc_append_kv", "cc_append_kv8",
     "cc_compact_kv8", "cc_attention_kv8_workspace", "cc_attention_kv8",
+    "cc_lmhead_logprobs_workspace", "cc_lmhead_logprobs",
 ]
 
 _c_void_p = ctypes.c_void_p
@@ -143,6 +145,10 @@ def _load():
         "cc_attention_kv8_workspace": (st, [P(c_problem), _i32, _i32, sz]),
         "cc_attention_kv8": (st, [P(c_problem), _c_void_p, P(c_kv8), _i32, _i32, _c_void_p, _i32,
                                   _c_void_p, _c_void_p, ctypes.c_size_t, _c_void_p]),
+        "cc_lmhead_logprobs_workspace": (st, [_i32, _i32, _i32, _i32, _i32, sz]),
+        "cc_lmhead_logprobs": (st, [_i32, _c_void_p, _c_void_p, _i32, _i32, _i32, _i32, _c_void_p,
+                                    _i32, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
+                                    ctypes.c_size_t, _c_void_p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -689,3 +695,49 @@ def cc_attention_kv8(p: Problem, q: torch.Tensor, kv: KV8, layer: int, kv_lens: 
                                  _ptr(kv_lens), max_kv_len, _ptr(o), _ptr(workspace), workspace.numel(),
                                  _stream(stream)), "cc_attention_kv8")
     return o
+
+# ---------------------------------------------------------------- log-probabilities
+
+@dataclass
+class Logprobs:
+    """Outputs of cc_lmhead_logprobs: [n], [n], [n][top], [n][top]."""
+    logprob: torch.Tensor
+    entropy: torch.Tensor
+    top_ids: torch.Tensor
+    top_logprob: torch.Tensor
+
+
+def logprobs_out(n: int, top: int, device="cuda") -> Logprobs:
+    f = lambda *s: torch.empty(s, dtype=torch.float32, device=device)
+    return Logprobs(f(n), f(n), torch.empty((n, top), dtype=torch.int32, device=device), f(n, top))
+
+
+def cc_lmhead_logprobs_workspace(dtype: str, n: int, vocab: int, hidden: int, top: int) -> int:
+    return _query(_lib.cc_lmhead_logprobs_workspace, {"f32": CC_F32, "bf16": CC_BF16}[dtype], n, vocab, hidden, top)
+
+
+def cc_lmhead_logprobs(dtype: str, u: torch.Tensor, w_lm: torch.Tensor, vocab: int, ids: Optional[torch.Tensor],
+                       top: int, out: Optional[Logprobs] = None, *, packed: bool = False,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> Logprobs:
+    """Log-probabilities of ids [n] (None: not taken), entropies and `top` alternatives of each hidden row u
+    [n][hidden] under the LM head w_lm [vocab][hidden] (packed: in the layout of cc_pack_lmhead)."""
+    n, hidden = u.shape
+    _int32(ids, n, "ids")
+    if not u.is_contiguous() or not w_lm.is_contiguous():
+        raise ValueError("u and w_lm must be contiguous")
+    if not packed and tuple(w_lm.shape) != (vocab, hidden):
+        raise ValueError(f"w_lm has shape {tuple(w_lm.shape)}, expected {(vocab, hidden)}")
+    if packed and w_lm.numel() * w_lm.element_size() < cc_pack_lmhead_bytes(vocab, hidden):
+        raise ValueError("w_lm holds less than a packed weight of that size")
+    if out is None:
+        out = logprobs_out(n, top, u.device)
+    if out.top_ids.numel() < n * top or out.top_logprob.numel() < n * top:
+        raise ValueError(f"out has no room for {top} alternatives of {n} rows")
+    if workspace is None:
+        workspace = _workspace(cc_lmhead_logprobs_workspace(dtype, n, vocab, hidden, top), u.device)
+    _check(_lib.cc_lmhead_logprobs({"f32": CC_F32, "bf16": CC_BF16}[dtype], _ptr(u), _ptr(w_lm), int(packed), n,
+                                   vocab, hidden, _ptr(ids), top, _ptr(out.logprob) if ids is not None else None,
+                                   _ptr(out.entropy), _ptr(out.top_ids) if top else None,
+                                   _ptr(out.top_logprob) if top else None, _ptr(workspace), workspace.numel(),
+                                   _stream(stream)), "cc_lmhead_logprobs")
+    return out

@@ -1215,3 +1215,57 @@ cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv,
 }
 
 }  // extern "C"
+
+// ------------------------------------------------------------------ log-probabilities
+
+namespace {
+cc_status check_logprobs(int32_t dtype, int32_t n, int32_t vocab, int32_t hidden, int32_t top) {
+  if (dtype != CC_F32 && dtype != CC_BF16) return CC_ERR_DTYPE;
+  if (dtype != CC_BF16) return CC_ERR_UNSUPPORTED;
+  if (n < 0 || vocab < 1 || hidden < 1) return CC_ERR_SHAPE;
+  if (top < 0 || top > vocab || top > CC_LOGPROBS_MAX_TOP) return CC_ERR_ARG;
+  if (hidden % 64 != 0) return CC_ERR_UNSUPPORTED;
+  return CC_OK;
+}
+}  // namespace
+
+extern "C" {
+
+cc_status cc_lmhead_logprobs_workspace(int32_t dtype, int32_t n, int32_t vocab, int32_t hidden, int32_t top,
+                                       size_t* bytes) {
+  if (!bytes) return CC_ERR_ARG;
+  CC_TRY(check_logprobs(dtype, n, vocab, hidden, top));
+  *bytes = logprobs_ws_bytes(n, vocab, top);
+  return CC_OK;
+}
+
+cc_status cc_lmhead_logprobs(int32_t dtype, const void* u, const void* w_lm, int32_t packed, int32_t n,
+                             int32_t vocab, int32_t hidden, const int32_t* ids, int32_t top, float* logprob,
+                             float* entropy, int32_t* top_ids, float* top_logprob, void* ws, size_t ws_bytes,
+                             void* stream) {
+  CC_TRY(check_logprobs(dtype, n, vocab, hidden, top));
+  if (packed != 0 && packed != 1) return CC_ERR_ARG;
+  if ((ids == nullptr) != (logprob == nullptr) && n > 0) return CC_ERR_ARG;
+  if (n > 0 && (!u || !w_lm || !aligned16(u) || !aligned16(w_lm))) return CC_ERR_ARG;
+  if (n > 0 && top > 0 && (!top_ids || !top_logprob)) return CC_ERR_ARG;
+  CC_TRY(check_ws(ws, ws_bytes, logprobs_ws_bytes(n, vocab, top)));
+  if (n == 0) return CC_OK;
+  LogprobsLaunch a;
+  a.u = static_cast<const u16*>(u);
+  a.w = w_lm;
+  a.packed = packed != 0;
+  a.ids = ids;
+  a.N = n;
+  a.D = hidden;
+  a.V = vocab;
+  a.top = top;
+  a.logprob = logprob;
+  a.entropy = entropy;
+  a.top_ids = top_ids;
+  a.top_logprob = top_logprob;
+  a.ws = ws;
+  CC_HIP(launch_logprobs(a, static_cast<hipStream_t>(stream)));
+  return CC_OK;
+}
+
+}  // extern "C"

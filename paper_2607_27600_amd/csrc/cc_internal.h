@@ -181,6 +181,24 @@ hipError_t launch_linear_f32(const float* x, const float* w, float* y, int M, in
 hipError_t launch_lmhead_f32(const LmHeadLaunch& a, hipStream_t s);
 int lmhead_f32_vocab_tile();
 
+// Width of the bf16 LM head's tiles in 64 entries (1 to 4).
+int lmhead_tile_width(int V, int N, int K);
+
+// Log-probabilities, entropies and alternatives from the LM head (bf16).  Rows are taken in slabs.
+struct LogprobsLaunch {
+  const u16* u;          // [N][D]
+  const void* w;         // [V][D], or packed
+  bool packed;
+  const int32_t* ids;    // [N] or null
+  int N, D, V, top;
+  float *logprob, *entropy;
+  int32_t* top_ids;
+  float* top_logprob;
+  void* ws;
+};
+size_t logprobs_ws_bytes(int N, int V, int top);
+hipError_t launch_logprobs(const LogprobsLaunch& a, hipStream_t s);
+
 // FP8 LM head: u (dtype) quantized per row into uq / su, then the E4M3 GEMM with the LSE
 // epilogue on the scaled logits, the target logits and the combine.
 struct LmHeadFp8Launch {

@@ -415,7 +415,6 @@ hipError_t launch_pack_rows(const void* x, int64_t rows, int cols, int64_t ldx, 
   return hipGetLastError();
 }
 
-namespace {
 // Tile width by estimated time: rounds of 256 workgroups, each its k-tiles (us below, bound by loads
 // at 64 entries and by matrix work at 256; the same for bf16 and E4M3), the first loads and the
 // epilogue; a last round that leaves CUs idle runs up to 30% quicker.  Over 1026 timings of
@@ -424,7 +423,7 @@ namespace {
 // entries, without regard to rounds, is 8% and up to 80% (4000 x 1024 at 256 entries: 26 us in
 // one column of 16 tiles, 15 in four; 16000 x 2048 at 770: 71 us in five columns of 315 tiles, 59 in
 // four of 252).
-int lmhead_nb(int V, int N, int K) {
+int lmhead_tile_width(int V, int N, int K) {
   const double us[4] = {0.66, 0.88, 1.15, 1.47};
   const int64_t tiles_m = (int64_t(V) + VT - 1) / VT;
   int best = 4;
@@ -442,6 +441,7 @@ int lmhead_nb(int V, int N, int K) {
   return best;
 }
 
+namespace {
 template <int AM>
 hipError_t launch_lmhead_gemm(const void* w, const void* u, int V, int N, int K, float2* partial,
                               float* target, const int32_t* ids, const float* su, const float* sw,
@@ -454,7 +454,7 @@ hipError_t launch_lmhead_gemm(const void* w, const void* u, int V, int N, int K,
   g.K = K;
   if (K >= kWideRow)
     return launch_tile<8, 3, 3, 2, AM, true>(g, EpiLse<3>{partial, target, ids, su, sw}, 1, s);
-  switch (lmhead_nb(V, N, K)) {
+  switch (lmhead_tile_width(V, N, K)) {
     case 1: return launch_tile<8, 1, 4, 4, AM>(g, EpiLse<1>{partial, target, ids, su, sw}, 1, s);
     case 2: return launch_tile<8, 2, 3, 3, AM>(g, EpiLse<2>{partial, target, ids, su, sw}, 1, s);
     case 3: return launch_tile<8, 3, 3, 2, AM>(g, EpiLse<3>{partial, target, ids, su, sw}, 1, s);

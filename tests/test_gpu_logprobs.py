@@ -1,0 +1,154 @@
+"""Log-probabilities, entropies and alternatives of the LM head against fp64."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cc_oracle as O
+from tests.gpu_util import f64
+
+pytestmark = pytest.mark.gpu
+
+# The inputs lie on a grid (u in steps of 1/16, w of 2^-11), so that every logit is exact in fp32 in
+# any order and the order of the alternatives, ties included, belongs to the inputs.  What remains:
+# a term's exponent z log2(e) - m is rounded at 2^-24 of up to 64 (4e-6 of the term), its
+# exponential and the fp32 sums at some 2^-23, the logarithm and the last difference at 2^-23 of up to 64:
+# under 2e-5; an entropy weighs its terms with up to 20 nats: five times that.
+TOL, TOL_H = 2e-5, 1e-4
+
+
+def _grid(n, D, V, seed, wide=1.0):
+    g = torch.Generator().manual_seed(seed)
+    u = (torch.randn(n, D, generator=g) * 16 * wide).round().clamp(-255, 255) / 16
+    w = (torch.randn(V, D, generator=g) * 41).round().clamp(-255, 255) / 2048
+    ids = torch.randint(0, V, (n,), generator=g, dtype=torch.int32)
+    return u.to(torch.bfloat16), w.to(torch.bfloat16), ids
+
+
+def _call(cc, u, w, ids, top, packed=False, out=None):
+    V = w.shape[0]
+    wd = w.cuda()
+    if packed:
+        wd = cc.cc_pack_lmhead(wd)
+    r = cc.cc_lmhead_logprobs("bf16", u.cuda(), wd, V, None if ids is None else ids.cuda(), top, out, packed=packed)
+    torch.cuda.synchronize()
+    return r
+
+
+def _check(r, u, w, ids, top):
+    want = O.logprobs(f64(u), f64(w), None if ids is None else ids.numpy(), top)
+    if ids is not None:
+        np.testing.assert_allclose(f64(r.logprob), want["logprob"], rtol=0, atol=TOL)
+        assert np.all(f64(r.logprob) <= 0)
+    np.testing.assert_allclose(f64(r.entropy), want["entropy"], rtol=0, atol=TOL_H)
+    assert np.all(f64(r.entropy) >= 0)
+    if top:
+        np.testing.assert_array_equal(r.top_ids.cpu().numpy()[:, :top], want["top_ids"])
+        np.testing.assert_allclose(f64(r.top_logprob), want["top_logprob"], rtol=0, atol=TOL)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("n,D,V,top", [(1, 64, 1, 1), (1, 64, 5, 5), (3, 128, 1000, 0), (17, 256, 1000, 1), (64, 192, 4099, 8),
+                                       (65, 512, 257, 32), (200, 128, 20000, 5), (257, 64, 300, 20), (1000, 64, 2500, 3)])
+def test_logprobs(n, D, V, top, packed):
+    from paper_2607_27600_amd import cc
+    print(f"[logprobs] {n} {D} {V} {top} packed={packed}", flush=True)
+    u, w, ids = _grid(n, D, V, n + V)
+    _check(_call(cc, u, w, ids, top, packed), u, w, ids, top)
+
+
+def test_rows_beyond_a_slab():
+    from paper_2607_27600_amd import cc
+    u, w, ids = _grid(4500, 64, 700, 3)
+    _check(_call(cc, u, w, ids, 4), u, w, ids, 4)
+
+
+def test_no_ids_and_peaked_rows():
+    from paper_2607_27600_amd import cc
+    u, w, _ = _grid(70, 256, 3001, 4, wide=8.0)
+    r = _call(cc, u, w, None, 6)
+    _check(r, u, w, None, 6)
+
+
+@pytest.mark.parametrize("order", ["equal", "falling", "rising", "few"])
+def test_ties_and_orders(order):
+    """All logits equal (the lowest ids first), rising or falling with the id, a handful of values."""
+    from paper_2607_27600_amd import cc
+    V, D, n, top = 3000, 64, 33, 32
+    w = torch.zeros(V, D)
+    v = torch.arange(V)
+    if order == "falling":
+        w[:, 0], w[:, 1] = -(v // 64).float(), -(v % 64).float() / 64
+    elif order == "rising":
+        w[:, 0], w[:, 1] = (v // 64).float(), (v % 64).float() / 64
+    elif order == "few":
+        w[:, 0] = (v % 7 == 3).float() - (v % 5 == 0).float()
+    u = torch.zeros(n, D)
+    u[:, 0] = u[:, 1] = 1
+    u[1::2] *= -1
+    u, w = u.to(torch.bfloat16), w.to(torch.bfloat16)
+    ids = torch.arange(n, dtype=torch.int32) * 90
+    _check(_call(cc, u, w, ids, top), u, w, ids, top)
+
+
+def test_random_inputs_and_the_score():
+    """Inputs off the grid; logprob is minus the score of cc_lmhead_score on the same rows."""
+    from paper_2607_27600_amd import cc
+    n, D, V, top = 128, 1024, 9000, 10
+    g = torch.Generator().manual_seed(9)
+    u, w = torch.randn(n, D, generator=g).to(torch.bfloat16), (torch.randn(V, D, generator=g) * 0.02).to(torch.bfloat16)
+    ids = torch.randint(0, V, (n,), generator=g, dtype=torch.int32)
+    r = _call(cc, u, w, ids, top)
+    want = O.logprobs(f64(u), f64(w), ids.numpy(), top)
+    # 1024 products of size up to 0.1 in fp32: under 1e-5 beside the bounds above
+    np.testing.assert_allclose(f64(r.logprob), want["logprob"], rtol=0, atol=TOL + 1e-5)
+    np.testing.assert_allclose(f64(r.top_logprob), want["top_logprob"], rtol=0, atol=TOL + 1e-5)
+    got = np.take_along_axis(want["logits"], r.top_ids.cpu().numpy().astype(np.int64), 1)
+    np.testing.assert_allclose(got, np.take_along_axis(want["logits"], want["top_ids"], 1), rtol=0, atol=1e-5)
+    p = cc.problem(dtype="bf16", cu_seqlens=[0, n], n_heads_q=1, n_heads_kv=1, head_dim=64, hidden=D, vocab=V)
+    s = torch.empty(n, device="cuda")
+    cc.cc_lmhead_score(p, u.cuda(), w.cuda(), ids.cuda(), s)
+    np.testing.assert_allclose(f64(s)[:-1], -f64(r.logprob)[:-1], rtol=0, atol=1e-5)
+
+
+def test_nan_and_infinite_logits():
+    """A NaN logit makes its row's numbers NaN and ranks last; other rows are untouched; a word of logit
+    -inf has probability 0."""
+    from paper_2607_27600_amd import cc
+    u, w, ids = _grid(40, 64, 900, 11)
+    clean = _call(cc, u, w, ids, 5)
+    u2 = u.clone()
+    u2[7, 3] = float("nan")
+    r = _call(cc, u2, w, ids, 5)
+    rows = np.arange(40) != 7
+    for a, b in zip((r.logprob, r.entropy, r.top_logprob), (clean.logprob, clean.entropy, clean.top_logprob)):
+        assert torch.equal(a[rows], b[rows]) and torch.isnan(a[7]).all()
+    assert torch.equal(r.top_ids[rows], clean.top_ids[rows])
+    assert sorted(r.top_ids[7].tolist()) == [0, 1, 2, 3, 4]
+    u3, w3 = torch.ones(2, 64), torch.zeros(300, 64)
+    w3[5:, 0] = -float("inf")
+    u3[:, 1:] = 0
+    r = _call(cc, u3.to(torch.bfloat16), w3.to(torch.bfloat16), torch.tensor([2, 7], dtype=torch.int32), 7)
+    np.testing.assert_allclose(f64(r.entropy), np.log(5), atol=TOL_H)
+    assert r.top_ids.cpu().tolist() == [[0, 1, 2, 3, 4, 5, 6]] * 2
+    np.testing.assert_allclose(f64(r.logprob), [-np.log(5), -np.inf], atol=TOL)
+
+
+def test_repeats_bit_for_bit_and_in_a_graph():
+    from paper_2607_27600_amd import cc
+    u, w, ids = _grid(300, 256, 30000, 12)
+    ud, wd, idd = u.cuda(), w.cuda(), ids.cuda()
+    ws = torch.empty(cc.cc_lmhead_logprobs_workspace("bf16", 300, 30000, 256, 8), dtype=torch.uint8, device="cuda")
+    a, b = (cc.logprobs_out(300, 8) for _ in range(2))
+    cc.cc_lmhead_logprobs("bf16", ud, wd, 30000, idd, 8, a, workspace=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cc.cc_lmhead_logprobs("bf16", ud, wd, 30000, idd, 8, b, workspace=ws)
+    for i in range(4):
+        for t in (b.logprob, b.entropy, b.top_logprob):
+            t.zero_()
+        ws.fill_(i * 85)      # whatever a workspace holds
+        g.replay()
+        torch.cuda.synchronize()
+        for x, y in zip((a.logprob, a.entropy, a.top_ids, a.top_logprob), (b.logprob, b.entropy, b.top_ids, b.top_logprob)):
+            assert torch.equal(x, y)
