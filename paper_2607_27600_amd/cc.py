@@ -593,23 +593,28 @@ def kv8_paged(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: 
                 k_scale, v_scale, scale_block, 0, scale_layer_stride, scale_head_stride, scale_page_stride)
 
 
-def _rows(t: Optional[torch.Tensor], p: Problem, what: str, heads: int, layers: int) -> c_rows:
-    """The view of [M][heads][head_dim] (or [layers][M][heads][head_dim]) rows of any strides."""
-    r = c_rows()
-    if t is None:
-        return r
-    if t.dtype != _DTYPES[p.struct.dtype]:
-        raise ValueError(f"{what} is {t.dtype}, the problem {_DTYPES[p.struct.dtype]}")
-    if t.dim() == 3 and layers == 1:
-        t = t.unsqueeze(0)
-    want = (layers, p.n_tokens, heads, p.struct.head_dim)
-    if tuple(t.shape) != want:
+def _rows(r: c_rows, t: torch.Tensor, dtype: torch.dtype, what: str, want: tuple) -> None:
+    """The view of rows t, of shape `want` ([M][heads][head_dim], or with layers in front), in any strides."""
+    if t.dtype != dtype:
+        raise ValueError(f"{what} is {t.dtype}, the problem {dtype}")
+    if t.shape != want:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {want}")
-    if t.stride(3) != 1 and t.shape[3] > 1:
+    st = t.stride()
+    if st[-1] != 1:
         raise ValueError(f"rows of {what} must be contiguous")
     r.base = t.data_ptr()
-    r.layer_stride, r.tok_stride, r.head_stride = t.stride(0), t.stride(1), t.stride(2)
-    return r
+    r.tok_stride, r.head_stride = st[-3], st[-2]
+    r.layer_stride = st[0] if len(st) == 4 else 0
+
+
+def _on_gpu(*tensors) -> None:
+    """Kernels run on the current device: tensors elsewhere would be read there by address."""
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError(f"tensors must be on the GPU, got one on {t.device}")
+    t = next(x for x in tensors if x is not None)
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
 def _int32(t: Optional[torch.Tensor], n: int, what: str) -> None:
@@ -619,20 +624,28 @@ def _int32(t: Optional[torch.Tensor], n: int, what: str) -> None:
 
 def _append(fn, p: Problem, kv, k, v, cached, capacity, layer, n_layers, pos_ids, q, q_out, rotate, stream):
     s = p.struct
-    _int32(cached, s.n_seqs, "cached")
-    _int32(pos_ids, p.n_tokens, "pos_ids")
+    n_seqs, d, hkv = s.n_seqs, s.head_dim, s.n_heads_kv
+    M = s.cu_seqlens_h[n_seqs]
+    dtype = _DTYPES[s.dtype]
+    _int32(cached, n_seqs, "cached")
+    _int32(pos_ids, M, "pos_ids")
     a = c_append()
-    a.k = _rows(k, p, "k", s.n_heads_kv, n_layers)
-    a.v = _rows(v, p, "v", s.n_heads_kv, n_layers)
+    # one layer may come without its dimension
+    want = (n_layers, M, hkv, d) if n_layers != 1 or k.dim() == 4 else (M, hkv, d)
+    _rows(a.k, k, dtype, "k", want)
+    _rows(a.v, v, dtype, "v", want)
     if q is not None:
-        a.q = _rows(q, p, "q", s.n_heads_q, n_layers)
+        hq = s.n_heads_q
+        _rows(a.q, q, dtype, "q", (M, hq, d))
         if q_out is None:
-            q_out = torch.empty((p.n_tokens, s.n_heads_q, s.head_dim), dtype=q.dtype, device=q.device)
-        elif q_out.dtype != q.dtype or q_out.numel() != p.n_tokens * s.n_heads_q * s.head_dim or not q_out.is_contiguous():
+            q_out = torch.empty((M, hq, d), dtype=dtype, device=q.device)
+        elif q_out.dtype != dtype or q_out.numel() != M * hq * d or not q_out.is_contiguous():
             raise ValueError("q_out must be contiguous rows of q's type and size")
         a.q_out = q_out.data_ptr()
+    _on_gpu(k, v, q, q_out, cached, pos_ids)
     a.cached = cached.data_ptr()
-    a.pos_ids = pos_ids.data_ptr() if pos_ids is not None else None
+    if pos_ids is not None:
+        a.pos_ids = pos_ids.data_ptr()
     a.capacity, a.layer, a.n_layers, a.rotate = capacity, layer, n_layers, int(rotate)
     _check(fn(ctypes.byref(s), ctypes.byref(a), ctypes.byref(kv.struct), _stream(stream)), fn.__name__)
     return q_out
@@ -663,6 +676,7 @@ def cc_compact_kv8(p: Problem, kv: KV8, keep_idx: torch.Tensor, k: Sequence[int]
     kk, n = _host_array(k, np.int32, _i32)
     if n != p.struct.n_seqs * (p.struct.n_heads_kv if per_head else 1):
         raise ValueError(f"{n} budgets for {p.struct.n_seqs} sequences")
+    _on_gpu(keep_idx, token_ids, pos_ids)
     _check(_lib.cc_compact_kv8(ctypes.byref(p.struct), ctypes.byref(kv.struct), _ptr(keep_idx), kk, per_head,
                                _ptr(token_ids), _ptr(pos_ids),
                                ctypes.byref(out.struct) if out is not None else None, _stream(stream)),
@@ -682,13 +696,16 @@ def cc_attention_kv8(p: Problem, q: torch.Tensor, kv: KV8, layer: int, kv_lens: 
     """Attention of the queries q [N][Hq][d] (p.cu_seqlens count them) over a cache in 8 bits that holds
     kv_lens[b] entries of each sequence, the queries' own last; mask "causal" or "counter"."""
     s = p.struct
-    _int32(kv_lens, s.n_seqs, "kv_lens")
-    if q.dtype != torch.bfloat16 or q.numel() != p.n_tokens * s.n_heads_q * s.head_dim or not q.is_contiguous():
+    n_seqs = s.n_seqs
+    _int32(kv_lens, n_seqs, "kv_lens")
+    if (q.dtype != torch.bfloat16 or q.numel() != s.cu_seqlens_h[n_seqs] * s.n_heads_q * s.head_dim
+            or not q.is_contiguous()):
         raise ValueError("q must be contiguous bf16 rows [N][Hq][head_dim]")
     if o is None:
         o = torch.empty_like(q)
     elif o.dtype != q.dtype or o.numel() != q.numel() or not o.is_contiguous():
         raise ValueError("o must be contiguous and of q's type and size")
+    _on_gpu(q, o, kv_lens, workspace)
     if workspace is None:
         workspace = _workspace(cc_attention_kv8_workspace(p, mask, max_kv_len), p.device)
     _check(_lib.cc_attention_kv8(ctypes.byref(s), _ptr(q), ctypes.byref(kv.struct), layer, _MASKS[mask],
@@ -733,6 +750,7 @@ def cc_lmhead_logprobs(dtype: str, u: torch.Tensor, w_lm: torch.Tensor, vocab: i
         out = logprobs_out(n, top, u.device)
     if out.top_ids.numel() < n * top or out.top_logprob.numel() < n * top:
         raise ValueError(f"out has no room for {top} alternatives of {n} rows")
+    _on_gpu(u, w_lm, ids, out.entropy, workspace)
     if workspace is None:
         workspace = _workspace(cc_lmhead_logprobs_workspace(dtype, n, vocab, hidden, top), u.device)
     _check(_lib.cc_lmhead_logprobs({"f32": CC_F32, "bf16": CC_BF16}[dtype], _ptr(u), _ptr(w_lm), int(packed), n,

@@ -421,36 +421,83 @@ __global__ __launch_bounds__(FEW_NT) void attn_few(Kv8Args a) {
 
 // ------------------------------------------------------------------ joining pieces
 
-// One row of a few lanes: out = sum_s o_s 2^((m_s - M) c2) / sum_s l_s 2^((m_s - M) c2).
-template <int HD>
+// out = sum_s o_s 2^((m_s - M) c2) / sum_s l_s 2^((m_s - M) c2), M = max m_s.  HD / 4 lanes take a row, G
+// groups of them its pieces in turn, four in flight; the groups meet in LDS.  G = 8 from 8 pieces on
+// (128 rows of 64 pieces: 35 us with G = 1, a chain of loads in 16 workgroups).
+template <int HD, int G>
 __global__ __launch_bounds__(256) void attn_join(Kv8Args a, int few) {
-  constexpr int LPR = HD / 4, PER = 256 / LPR;
-  const int row_in = blockIdx.x * PER + threadIdx.x / LPR;
-  const int d = (threadIdx.x % LPR) * 4;
-  if (row_in >= a.n_list * a.hkv * a.R) return;
-  const int r = row_in % a.R, jh = row_in / a.R;
+  constexpr int LPR = HD / 4, PER = 256 / (LPR * G);
+  __shared__ float4 po[G > 1 ? 256 : 1];
+  __shared__ float2 pm[G > 1 ? 256 : 1];
+  const int tid = threadIdx.x;
+  const int gi = tid / LPR % G, lane = tid % LPR;
+  const int row_in = blockIdx.x * PER + tid / (LPR * G);
+  const int d = lane * 4;
+  const int64_t step = int64_t(a.n_list) * a.hkv * a.R;
+  bool on = row_in < step;
+  const int r = row_in % a.R, jh = on ? row_in / a.R : 0;
   const int kvh = jh % a.hkv;
   const Seq s = seq_of(a, jh / a.hkv);
   const int rows = s.m * a.g;
-  if (r >= rows || (rows <= FEW_ROWS) != (few != 0)) return;
+  on = on && r < rows && (rows <= FEW_ROWS) == (few != 0);
   const int n = min(a.splits, max(1, (s.len + a.piece - 1) / a.piece));
-  const int64_t step = int64_t(a.n_list) * a.hkv * a.R;
-  float M = -INFINITY;
-  for (int i = 0; i < n; ++i) M = fmaxf(M, a.part_ml[i * step + row_in].x);
-  const float ref = M == -INFINITY ? 0.f : M;
-  float L = 0.f;
+  float M = -INFINITY, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const float2 p = a.part_ml[i * step + row_in];
-    const float4 x = *reinterpret_cast<const float4*>(a.part + (i * step + row_in) * HD + d);
-    const float f = fast_exp2((p.x - ref) * a.c2);
-    L += p.y * f;
-    o.x += x.x * f;
-    o.y += x.y * f;
-    o.z += x.z * f;
-    o.w += x.w * f;
+  if (on) {
+    for (int i0 = gi; i0 < n; i0 += 4 * G) {
+      float2 p[4];
+      float4 x[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t at = min(i0 + q * G, n - 1) * step + row_in;
+        p[q] = a.part_ml[at];
+        x[q] = *reinterpret_cast<const float4*>(a.part + at * HD + d);
+      }
+      float t = M;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (i0 + q * G < n) t = fmaxf(t, p[q].x);
+      const float ref = t == -INFINITY ? 0.f : t;
+      const float c = fast_exp2((M - ref) * a.c2);
+      M = t;
+      L *= c;
+      o = make_float4(o.x * c, o.y * c, o.z * c, o.w * c);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (i0 + q * G >= n) continue;
+        const float f = fast_exp2((p[q].x - ref) * a.c2);
+        L += p[q].y * f;
+        o.x += x[q].x * f;
+        o.y += x[q].y * f;
+        o.z += x[q].z * f;
+        o.w += x[q].w * f;
+      }
+    }
   }
+  if constexpr (G > 1) {
+    po[tid] = o;
+    pm[tid] = make_float2(M, L);
+    __syncthreads();
+    if (gi != 0) return;
+    M = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < G; ++q) M = fmaxf(M, pm[tid + q * LPR].x);
+    const float ref = M == -INFINITY ? 0.f : M;
+    L = 0.f;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int q = 0; q < G; ++q) {
+      const float2 p = pm[tid + q * LPR];
+      const float4 x = po[tid + q * LPR];
+      const float f = fast_exp2((p.x - ref) * a.c2);
+      L += p.y * f;
+      o.x += x.x * f;
+      o.y += x.y * f;
+      o.z += x.z * f;
+      o.w += x.w * f;
+    }
+  }
+  if (!on) return;
   const float inv = L == 0.f ? 0.f : 1.f / L;
   u16* out = a.o + (int64_t(s.q0 + r / a.g) * a.hq + kvh * a.g + r % a.g) * HD + d;
   *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf2(o.x * inv, o.y * inv), pack_bf2(o.z * inv, o.w * inv));
@@ -479,9 +526,14 @@ hipError_t launch_dim(const Kv8Args& a, bool few, hipStream_t s) {
   else
     e = launch_attn_many(a, s);
   if (e != hipSuccess || a.splits == 1) return e;
-  constexpr int PER = 256 / (HD / 4);
   const int64_t rows = int64_t(a.n_list) * a.hkv * a.R;
-  hipLaunchKernelGGL(attn_join<HD>, dim3(unsigned((rows + PER - 1) / PER)), dim3(256), 0, s, a, few ? 1 : 0);
+  if (a.splits >= 8) {
+    constexpr int PER = 256 / (HD / 4 * 8);
+    hipLaunchKernelGGL((attn_join<HD, 8>), dim3(unsigned((rows + PER - 1) / PER)), dim3(256), 0, s, a, few ? 1 : 0);
+  } else {
+    constexpr int PER = 256 / (HD / 4);
+    hipLaunchKernelGGL((attn_join<HD, 1>), dim3(unsigned((rows + PER - 1) / PER)), dim3(256), 0, s, a, few ? 1 : 0);
+  }
   return hipGetLastError();
 }
 

@@ -66,18 +66,26 @@ __device__ __forceinline__ void move_ids(const Args& a, const CompactList& L) {
 }
 
 // Largest magnitude of 16 codes times their scale, as fp32 bits.  Codes without their sign rise with
-// the magnitudes; 0x7f is NaN and does not count.
+// the magnitudes, two to a 32-bit word by packed 16-bit maxima; 0x7f is NaN and does not count.
 __device__ __forceinline__ uint32_t top_of(const uint4& w, uint32_t sc) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-  uint32_t m = 0;
+  u16x2 m = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int s = 0; s < 32; s += 8) {
-      const uint32_t c = (x[i] >> s) & 0x7fu;
-      m = max(m, c == 0x7fu ? 0u : c);
+  for (int i = 0; i < 4; ++i) {
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[i] & 0x007f007fu));
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, (x[i] >> 8) & 0x007f007fu));
+  }
+  uint32_t c = max(uint32_t(m[0]), uint32_t(m[1]));
+  if (c == 0x7fu) {
+    c = 0;
+#pragma unroll 1
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t b = ((i < 4 ? w.x : i < 8 ? w.y : i < 12 ? w.z : w.w) >> (8 * (i & 3))) & 0x7fu;
+      c = max(c, b == 0x7fu ? 0u : b);
     }
-  const auto f = __builtin_amdgcn_cvt_pk_f32_fp8(int(m), false);
+  }
+  const auto f = __builtin_amdgcn_cvt_pk_f32_fp8(int(c), false);
   return __float_as_uint(f[0] * e8m0_scale(sc));
 }
 
@@ -86,9 +94,9 @@ __device__ __forceinline__ uint4 rescale(const uint4& w, float f) {
   uint32_t y[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(x[i]), false);
-    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(x[i]), true);
-    y[i] = e4m3_pack(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
+    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(int(x[i]), f, false);
+    const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(int(x[i]), f, true);
+    y[i] = e4m3_pack(lo[0], lo[1], hi[0], hi[1]);
   }
   return make_uint4(y[0], y[1], y[2], y[3]);
 }
