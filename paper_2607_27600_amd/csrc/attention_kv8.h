@@ -9,6 +9,10 @@ namespace cc {
 // kernel for few against the one for many, 8000 entries and 8 KV heads of 128: 64 rows 41.5 us and (68
 // rows) 31.6, sixteen such sequences 328 and 122; two row blocks, 32 rows: 26.4 and 31, sixteen 128 and 122.
 constexpr int FEW_ROWS = 32;
+// Few rows: the longest cache of which each (sequence, head) is one workgroup's, with nothing to join
+// (64 sequences of 1000 entries, 4 heads: 17 us against 27 shared out; one of 1024, 8 heads: 13.4
+// against 14; there a CU's own loads, some 40 GB/s, are the bound).
+constexpr int KV8_DIRECT = 1024;
 constexpr int FEW_NT = 256;
 constexpr int KV8_LIST = 64;     // sequences of a launch listed by value
 constexpr int MANY_ROWS = 128;   // rows of a block of the kernel for many
@@ -24,9 +28,12 @@ struct Kv8Args {
   int hq, hkv, g, head_dim;
   float c2;                      // scale * log2(e)
   int R;                         // most rows of a sequence of the class
-  int piece, splits;             // entries of a piece, pieces of the longest sequence
-  float* part;                   // splits > 1: [splits][n_list][Hkv][R][head_dim] outputs
-  float2* part_ml;               // and [splits][n_list][Hkv][R] (maximum, sum)
+  int piece, splits;             // many rows: entries of a piece, pieces of the longest sequence
+  int direct, parts;             // few rows: a workgroup for each (sequence, head); else workgroups to share it all
+  // Results to be joined (null: none), outputs and (maximum, sum): many rows
+  // [splits][n_list][Hkv][R], few rows [parts + n_list * Hkv][R].
+  float* part;
+  float2* part_ml;
   int n_list, listed;            // sequences walked: list[0..n_list), or (listed = 0) all
   int32_t list[KV8_LIST];
 };

@@ -55,7 +55,7 @@ __device__ __forceinline__ bf16x8 widen44(uint32_t lo, uint32_t hi, float slo, f
 
 // Bytes 0x80 where a byte of x is a NaN code (0x7f or 0xff).
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-// x without its NaN codes; ones (code 0x38) in their places.
+// Bytes 0xff there.
 __device__ __forceinline__ uint32_t nan_mask(uint32_t x) { return (nan_bytes(x) >> 7) * 0xffu; }
 
 // 4 x 4 bytes transposed: word i of the result holds byte i of w[0..3].
@@ -69,6 +69,14 @@ __device__ __forceinline__ void transpose4(const uint32_t (&w)[4], uint32_t (&t)
   t[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
   t[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
   t[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
+// A wave-uniform pointer in scalar registers.
+__device__ __forceinline__ const char* uniform_ptr(const char* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(u));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(u >> 32));
+  return reinterpret_cast<const char*>((uint64_t(hi) << 32) | lo);
 }
 
 // Maximum over the four lanes l % 16 + 16 k.
@@ -137,6 +145,142 @@ __device__ __forceinline__ int past_of(const Kv8Args& a, const Seq& s, int i) {
   return a.mask == CC_MASK_CAUSAL ? max(0, s.shift + i + 1) : s.len;
 }
 
+// Shares of the work of the kernel for few rows.  Lengths are known on the device alone, so every
+// workgroup works out its own.  The work is a line of units of 128 entries: the sequences in order, of
+// each its KV heads in order, of each its entries.
+//   Much work: each of `parts` workgroups takes an equal part of the line, so that a ragged batch keeps
+//     every CU busy to the end (64 sequences of 31 to 15987 entries, 4 heads: equal pieces of 2048
+//     entries 118 us, of 680 entries 84, shares 78).  A part may hold the end of one (sequence, head),
+//     whole ones and the start of another.  Every item takes HEAD units more, without entries, for what
+//     it costs to begin one (without them a part of many short sequences is the last: 88 us).
+//   Little work (up to LITTLE units for each of two workgroups a CU): the time is that of one chain of
+//     round trips, and a second item in a part would double it, so the units become pieces of q units
+//     that no two items share, a workgroup each (32 rows, 8 heads, 8000 entries: 22 us, shares 27).
+//   A short longest sequence (`direct`): a workgroup for each (sequence, head), nothing to join.
+// An item that is whole in one part is final there; other results are joined.  A result's place is the
+// workgroup's index plus that of the (sequence, head): both rise along the line, so no two meet.
+constexpr int UNIT = 128;
+constexpr int LITTLE = 8;
+constexpr int HEAD = 2;
+struct Shares {
+  int64_t total;     // units of q * 128 entries
+  int parts;         // workgroups that have some
+  int q;
+  int head;          // units without entries at an item's start
+  int mine;          // of the lane's sequence, if the list has up to 64: units of 128 entries
+  __device__ __forceinline__ int64_t begin(int w) const { return total * w / parts; }
+  // the workgroup whose part unit x is in
+  __device__ __forceinline__ int part_of(int64_t x) const { return int(((x + 1) * parts - 1) / total); }
+};
+__device__ __forceinline__ int entry_units(const Kv8Args& a, int j) {   // of one KV head, 128 entries each
+  if (j >= a.n_list) return 0;
+  const Seq s = seq_of(a, j);
+  const int64_t rows = int64_t(s.m) * a.g;
+  return rows == 0 || rows > FEW_ROWS ? 0 : max(1, (s.len + UNIT - 1) / UNIT);
+}
+__device__ __forceinline__ int units_of(const Kv8Args& a, const Shares& sh, int j) {
+  const int u = a.n_list <= 64 ? sh.mine : entry_units(a, j);   // (there, j is the lane)
+  return u == 0 ? 0 : (u + sh.q - 1) / sh.q + sh.head;
+}
+// Inclusive sums over the wave (64 sequences of 2^31 entries have fewer than 2^31 units).
+__device__ __forceinline__ int wave_scan(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int o = __shfl_up(v, off);
+    if (lane >= off) v += o;
+  }
+  return v;
+}
+__device__ __forceinline__ int64_t units_in_all(const Kv8Args& a, const Shares& sh) {
+  if (a.n_list == 1) return int64_t(units_of(a, sh, 0)) * a.hkv;
+  int64_t n = 0;
+  for (int b = 0; b < a.n_list; b += 64)
+    n += __builtin_amdgcn_readlane(wave_scan(units_of(a, sh, b + int(threadIdx.x & 63))), 63);
+  return n * a.hkv;
+}
+__device__ __forceinline__ Shares shares_of(const Kv8Args& a) {
+  Shares s;
+  s.q = 1;
+  s.head = 0;
+  if (a.direct) {   // a (sequence, head) a workgroup
+    s.mine = 1;
+    s.total = s.parts = a.n_list * a.hkv;
+    return s;
+  }
+  // (one sequence: its length by scalar loads, no sums over the wave; 2 us less of 15)
+  s.mine = a.n_list == 1 ? entry_units(a, 0) : a.n_list <= 64 ? entry_units(a, threadIdx.x & 63) : 0;
+  s.total = units_in_all(a, s);
+  const int items = a.n_list * a.hkv;
+  if (items < a.parts) {
+    const int64_t q = max(int64_t(2), (s.total + a.parts - items - 1) / (a.parts - items));
+    if (q <= LITTLE) {   // at most total / q + items <= parts pieces
+      s.q = int(q);
+      s.total = units_in_all(a, s);
+      s.parts = int(s.total);
+      return s;
+    }
+  }
+  s.head = HEAD;
+  s.total = units_in_all(a, s);
+  s.parts = int(min(int64_t(a.parts), s.total));
+  return s;
+}
+struct Item {
+  int j, kvh, unit, units;   // sequence of the list, head, unit of its units
+};
+__device__ __forceinline__ Item item_at(const Kv8Args& a, const Shares& sh, int64_t x) {
+  Item it;
+  if (a.direct) {
+    it.j = int(x) / a.hkv;
+    it.kvh = int(x) % a.hkv;
+    it.unit = 0;
+    it.units = 1;
+    return it;
+  }
+  if (a.n_list == 1) {
+    it.j = 0;
+    it.units = units_of(a, sh, 0);
+    it.kvh = int(x / it.units);
+    it.unit = int(x - int64_t(it.kvh) * it.units);
+    return it;
+  }
+  int64_t start = 0;
+  for (int b = 0;; b += 64) {
+    const int u = units_of(a, sh, b + int(threadIdx.x & 63));
+    const int sum = wave_scan(u);
+    const uint64_t past = __ballot(start + int64_t(sum) * a.hkv > x);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      it.units = __builtin_amdgcn_readlane(u, l);
+      it.j = b + l;
+      const int y = int(x - start - int64_t(__builtin_amdgcn_readlane(sum, l) - it.units) * a.hkv);
+      it.kvh = y / it.units;
+      it.unit = y - it.kvh * it.units;
+      return it;
+    }
+    start += int64_t(__builtin_amdgcn_readlane(sum, 63)) * a.hkv;
+  }
+}
+// First unit of a head of the j-th sequence, and how many it has.
+__device__ __forceinline__ void item_of(const Kv8Args& a, const Shares& sh, int j, int64_t& start, int& units) {
+  start = 0;
+  if (a.n_list == 1) {
+    units = units_of(a, sh, 0);
+    return;
+  }
+  for (int b = 0;; b += 64) {
+    const int u = units_of(a, sh, b + int(threadIdx.x & 63));
+    const int sum = wave_scan(u);
+    if (j < b + 64) {
+      units = __builtin_amdgcn_readlane(u, j - b);
+      start += int64_t(__builtin_amdgcn_readlane(sum, j - b) - units) * a.hkv;
+      return;
+    }
+    start += int64_t(__builtin_amdgcn_readlane(sum, 63)) * a.hkv;
+  }
+}
+
 // ------------------------------------------------------------------ few rows
 //
 // S^T = K Q^T on 16x16x32 MFMA, entries as its rows, so that a lane holds four entries of one row of
@@ -147,7 +291,7 @@ __device__ __forceinline__ int past_of(const Kv8Args& a, const Seq& s, int i) {
 // covering the row, and turns 4 x 4 bytes with eight byte permutations; dim 8 (l % 16) + i is then row
 // l % 16 of output block i.
 template <int HD, int NR>
-__global__ __launch_bounds__(FEW_NT) void attn_few(Kv8Args a) {
+__global__ __launch_bounds__(FEW_NT, 2) void attn_few(Kv8Args a) {
   constexpr int NKS = HD / 32;          // k-steps of the first product
   constexpr int NK = HD / 64;           // 16-byte pieces of a lane's entry
   constexpr int NDB = HD / 16;          // 16-dim blocks of the output: also a lane's bytes of a V row
@@ -155,267 +299,308 @@ __global__ __launch_bounds__(FEW_NT) void attn_few(Kv8Args a) {
   constexpr int ROWS = 16 * NR;
   extern __shared__ float lds[];        // [NW][ROWS][HD] outputs, then [NW][ROWS] (max, sum)
   float2* ml = reinterpret_cast<float2*>(lds + NW * ROWS * HD);
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int grp = lane >> 4, r16 = lane & 15;
-  int x = blockIdx.x;
-  const int kvh = x % a.hkv;
-  x /= a.hkv;
-  const int split = x % a.splits, j = x / a.splits;
-  const Seq s = seq_of(a, j);
-  const int rows = s.m * a.g;
-  if (rows == 0 || rows > FEW_ROWS) return;
-  const int c0 = split * a.piece, c1 = min(s.len, c0 + a.piece);
-  if (split > 0 && c0 >= s.len) return;   // the join does not read this piece
+  const Shares sh = shares_of(a);
+  if (int(blockIdx.x) >= sh.parts) return;
+  int64_t x = sh.begin(blockIdx.x);
+  const int64_t x1 = sh.begin(blockIdx.x + 1);
+  while (x < x1) {
+    int lane = tid & 63;
+    asm volatile("" : "+v"(lane));   // what follows from it is made anew for each item, not kept over the loop
+    const int grp = lane >> 4, r16 = lane & 15;
+    const Item it = item_at(a, sh, x);
+    const int j = it.j, kvh = it.kvh;
+    const Seq s = seq_of(a, j);
+    const int rows = s.m * a.g;
+    const int past = it.unit + int(min(int64_t(it.units - it.unit), x1 - x));   // of the item's units
+    x += past - it.unit;
+    const int u0 = max(0, it.unit - sh.head), u1 = past - sh.head;   // those with entries
+    const bool whole = u0 == 0 && past == it.units;
+    const int unit = sh.q * UNIT;
+    const int c0 = u0 * unit, c1 = a.direct ? s.len : int(min(int64_t(s.len), int64_t(u1) * unit));
+    // (another class is met only where every item is a workgroup)
+    if (u1 <= u0 || rows == 0 || rows > FEW_ROWS) continue;
 
-  bf16x8 qf[NR][NKS];
-  int lo[NR], hi[NR];
+    bf16x8 qf[NR][NKS];
+    int lo[NR], hi[NR];
 #pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const int r = min(n * 16 + r16, rows - 1), i = r / a.g;
-    lo[n] = first_of(a, s, i);
-    hi[n] = past_of(a, s, i);
-    const u16* q = a.q + (int64_t(s.q0 + i) * a.hq + kvh * a.g + r % a.g) * HD;
+    for (int n = 0; n < NR; ++n) {
+      const int r = min(n * 16 + r16, rows - 1), i = r / a.g;
+      lo[n] = first_of(a, s, i);
+      hi[n] = past_of(a, s, i);
+      const u16* q = a.q + (int64_t(s.q0 + i) * a.hq + kvh * a.g + r % a.g) * HD;
 #pragma unroll
-    for (int k = 0; k < NKS; ++k)
-      qf[n][k] = as_bf16x8(*reinterpret_cast<const uint4*>(q + 64 * (k >> 1) + 16 * grp + 8 * (k & 1)));
-  }
-  // entries [full0, full1) are seen by every row
-  const int full0 = first_of(a, s, s.m - 1), full1 = past_of(a, s, 0);
-  // this wave's 16-entry groups: the piece's, in NW runs of whole steps of two
-  const int g0 = c0 >> 4, g1 = (c1 + 15) >> 4;
-  const int per = ((g1 - g0 + NW - 1) / NW + 1) & ~1;
-  int lo_all = first_of(a, s, 0) >> 4, hi_all = (past_of(a, s, s.m - 1) + 15) >> 4;   // nothing to see outside
-  int gb = g0 + wave * per, ge = min(g1, gb + per);
-  gb = max(gb, lo_all & ~1);
-  ge = min(ge, hi_all);
-  const Plane P = plane_of(a, s.b, kvh);
-  const int last = s.len - 1;
+      for (int k = 0; k < NKS; ++k)
+        qf[n][k] = as_bf16x8(*reinterpret_cast<const uint4*>(q + 64 * (k >> 1) + 16 * grp + 8 * (k & 1)));
+    }
+    // entries [full0, full1) are seen by every row
+    const int full0 = first_of(a, s, s.m - 1), full1 = past_of(a, s, 0);
+    // this wave's 16-entry groups: the piece's, in NW runs of whole steps of two
+    const int g0 = c0 >> 4, g1 = (c1 + 15) >> 4;
+    const int per = ((g1 - g0 + NW - 1) / NW + 1) & ~1;
+    int lo_all = first_of(a, s, 0) >> 4, hi_all = (past_of(a, s, s.m - 1) + 15) >> 4;   // nothing to see outside
+    int gb = g0 + wave * per, ge = min(g1, gb + per);
+    gb = max(gb, lo_all & ~1);
+    ge = min(ge, hi_all);
+    const Plane P = plane_of(a, s.b, kvh);
+    const int last = s.len - 1;
 
-  float m_run[NR], l_run[NR];
-  f32x4 acc[NR][NDB];
+    float m_run[NR], l_run[NR];
+    f32x4 acc[NR][NDB];
 #pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    m_run[n] = -INFINITY;
-    l_run[n] = 0.f;
+    for (int n = 0; n < NR; ++n) {
+      m_run[n] = -INFINITY;
+      l_run[n] = 0.f;
 #pragma unroll
-    for (int d = 0; d < NDB; ++d) acc[n][d] = f32x4{};
-  }
+      for (int d = 0; d < NDB; ++d) acc[n][d] = f32x4{};
+    }
 
-  struct Step {
-    uint4 k[2][NK];
-    uint32_t v[8][NDB / 4];
-  };
-  // Pages and scales of 64 groups at a time, a lane each.
-  for (int sb = gb; sb < ge; sb += 64) {
-    const int se = min(ge, sb + 64);
-    const int mine = min(sb + lane, se - 1);
-    const int page = group_page(a, P, mine);
-    const int64_t so = group_scale(a, page, mine);
-    const uint32_t sc = uint32_t(P.ks[so]) | (uint32_t(P.vs[so]) << 8);
-    auto load = [&](int gr, Step& st) {   // groups gr and gr + 1 (past the end: the last one again)
+    // a lane's places in a whole group: its K row, its four V rows
+    const uint32_t ts = uint32_t(a.k.codes.tok_stride);
+    const uint32_t ko0 = r16 * ts + 16 * grp;
+    const uint32_t vo0[4] = {(4 * grp) * ts + NDB * r16, (4 * grp + 1) * ts + NDB * r16, (4 * grp + 2) * ts + NDB * r16,
+                             (4 * grp + 3) * ts + NDB * r16};
+    struct Step {
+      uint4 k[2][NK];
+      uint32_t v[8][NDB / 4];
+    };
+    // Pages and scales of 64 groups at a time, a lane each.
+    for (int sb = gb; sb < ge; sb += 64) {
+      const int se = min(ge, sb + 64);
+      const int mine = min(sb + lane, se - 1);
+      const int page = group_page(a, P, mine);
+      const int64_t so = group_scale(a, page, mine);
+      const uint32_t sc = uint32_t(P.ks[so]) | (uint32_t(P.vs[so]) << 8);
+      auto load = [&](int gr, Step& st) {   // groups gr and gr + 1 (past the end: the last one again)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int gg = min(gr + t, se - 1);
-        const int64_t off = group_codes(a, __builtin_amdgcn_readlane(page, gg - sb), gg);
-        const int e0 = gg << 4;
-        {
-          const char* p = P.k + off + int64_t(min(r16, last - e0)) * a.k.codes.tok_stride + 16 * grp;
+        for (int t = 0; t < 2; ++t) {
+          const int gg = min(gr + t, se - 1);
+          const int64_t off = group_codes(a, __builtin_amdgcn_readlane(page, gg - sb), gg);
+          const char* kp = uniform_ptr(P.k + off);
+          const char* vp = uniform_ptr(P.v + off);
+          uint32_t ko = ko0, vo[4] = {vo0[0], vo0[1], vo0[2], vo0[3]};
+          const int have = last - (gg << 4);   // the group's last entry; past it: that one again
+          if (have < 15) {
+            ko = uint32_t(min(r16, have)) * ts + 16 * grp;
 #pragma unroll
-          for (int k = 0; k < NK; ++k) st.k[t][k] = *reinterpret_cast<const uint4*>(p + 64 * k);
-        }
+            for (int e = 0; e < 4; ++e) vo[e] = uint32_t(min(4 * grp + e, have)) * ts + NDB * r16;
+          }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const char* p = P.v + off + int64_t(min(4 * grp + e, last - e0)) * a.v.codes.tok_stride + NDB * r16;
-          if constexpr (NDB == 8) {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-            st.v[4 * t + e][0] = w[0];
-            st.v[4 * t + e][NDB / 4 - 1] = w[1];
-          } else {
-            st.v[4 * t + e][0] = *reinterpret_cast<const uint32_t*>(p);
+          for (int k = 0; k < NK; ++k) st.k[t][k] = *reinterpret_cast<const uint4*>(kp + ko + 64 * k);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (NDB == 8) {
+              const u32x2 w = *reinterpret_cast<const u32x2*>(vp + vo[e]);
+              st.v[4 * t + e][0] = w[0];
+              st.v[4 * t + e][NDB / 4 - 1] = w[1];
+            } else {
+              st.v[4 * t + e][0] = *reinterpret_cast<const uint32_t*>(vp + vo[e]);
+            }
           }
         }
-      }
-    };
-    auto compute = [&](int gr, Step& st) {
-      const uint32_t s0 = __builtin_amdgcn_readlane(sc, gr - sb);
-      const uint32_t s1 = __builtin_amdgcn_readlane(sc, min(gr + 1, se - 1) - sb);
-      const float ks[2] = {e8m0_scale(s0 & 255u), e8m0_scale(s1 & 255u)};
-      const float vs[2] = {e8m0_scale(s0 >> 8), e8m0_scale(s1 >> 8)};
-      f32x4 z[NR][2];
+      };
+      auto compute = [&](int gr, Step& st) {
+        const uint32_t s0 = __builtin_amdgcn_readlane(sc, gr - sb);
+        const uint32_t s1 = __builtin_amdgcn_readlane(sc, min(gr + 1, se - 1) - sb);
+        const float ks[2] = {e8m0_scale(s0 & 255u), e8m0_scale(s1 & 255u)};
+        const float vs[2] = {e8m0_scale(s0 >> 8), e8m0_scale(s1 >> 8)};
+        f32x4 z[NR][2];
 #pragma unroll
-      for (int n = 0; n < NR; ++n) z[n][0] = z[n][1] = f32x4{};
+        for (int n = 0; n < NR; ++n) z[n][0] = z[n][1] = f32x4{};
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int k = 0; k < NKS; ++k) {
-          const uint4 w = st.k[t][k >> 1];
-          const bf16x8 kf = (k & 1) ? widen8(w.z, w.w, ks[t]) : widen8(w.x, w.y, ks[t]);
+          for (int k = 0; k < NKS; ++k) {
+            const uint4 w = st.k[t][k >> 1];
+            const bf16x8 kf = (k & 1) ? widen8(w.z, w.w, ks[t]) : widen8(w.x, w.y, ks[t]);
 #pragma unroll
-          for (int n = 0; n < NR; ++n) z[n][t] = mfma16(kf, qf[n][k], z[n][t]);
-        }
-      const int e0 = gr << 4;
-      // past the wave's own groups counts as masked: the last group stands there a second time
-      const int stop = min(full1, ge << 4);
-      const bool masked = e0 < full0 || e0 + 32 > stop;
-      bool nans = false;
-      if (masked) {
+            for (int n = 0; n < NR; ++n) z[n][t] = mfma16(kf, qf[n][k], z[n][t]);
+          }
+        const int e0 = gr << 4;
+        // past the wave's own groups counts as masked: the last group stands there a second time
+        const int stop = min(full1, ge << 4);
+        const bool masked = e0 < full0 || e0 + 32 > stop;
+        bool nans = false;
+        uint32_t hit[NR];
+        if (masked) {
 #pragma unroll
-        for (int n = 0; n < NR; ++n)
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int key = e0 + 16 * t + 4 * grp + e;
+                if (key < lo[n] || key >= min(hi[n], ge << 4)) z[n][t][e] = -INFINITY;
+              }
+          // values of entries that the sequence does not have
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int key = e0 + 16 * t + 4 * grp + e;
-              if (key < lo[n] || key >= min(hi[n], ge << 4)) z[n][t][e] = -INFINITY;
+              const bool in = e0 + 16 * t + 4 * grp + e < min(s.len, ge << 4);
+#pragma unroll
+              for (int i = 0; i < NDB / 4; ++i) {
+                if (!in) st.v[4 * t + e][i] = 0;
+                nans |= nan_bytes(st.v[4 * t + e][i]) != 0;
+              }
             }
-        // values of entries that the sequence does not have
+          nans = __any(nans);
+          if (nans) {
+            // which outputs of this lane a NaN value reaches: a product of indicators
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+            for (int n = 0; n < NR; ++n) hit[n] = 0;
+            bf16x8 see[NR];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bool in = e0 + 16 * t + 4 * grp + e < min(s.len, ge << 4);
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int key = e0 + 16 * (e >> 2) + 4 * grp + (e & 3);
+                see[n][e] = (__bf16)(key >= lo[n] && key < min(hi[n], ge << 4) ? 1.f : 0.f);
+              }
 #pragma unroll
             for (int i = 0; i < NDB / 4; ++i) {
-              if (!in) st.v[4 * t + e][i] = 0;
-              nans |= nan_bytes(st.v[4 * t + e][i]) != 0;
+              uint32_t wa[4], wb[4], ta[4], tb[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                wa[e] = nan_mask(st.v[e][i]);
+                wb[e] = nan_mask(st.v[4 + e][i]);
+                st.v[e][i] &= ~wa[e];
+                st.v[4 + e][i] &= ~wb[e];
+              }
+              transpose4(wa, ta);
+              transpose4(wb, tb);
+#pragma unroll
+              for (int d = 0; d < 4; ++d) {
+                const bf16x8 one = widen44(ta[d] & 0x38383838u, tb[d] & 0x38383838u, 1.f, 1.f);   // code 0x38: 1
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                  const f32x4 h = mfma16(one, see[n], f32x4{});
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) hit[n] |= h[e] > 0.f ? 1u << (16 * i + 4 * d + e) : 0u;
+                }
+              }
             }
           }
-        nans = __any(nans);
-      }
-      bf16x8 pf[NR];
-      bool moved = false;
-      float mx[NR];
-#pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        float t = fmaxf(fmaxf(fmaxf(z[n][0][0], z[n][0][1]), fmaxf(z[n][0][2], z[n][0][3])),
-                        fmaxf(fmaxf(z[n][1][0], z[n][1][1]), fmaxf(z[n][1][2], z[n][1][3])));
-        mx[n] = quad_max(t);
-        moved |= mx[n] > m_run[n] + kRescale / a.c2;
-      }
-      if (__any(moved)) {
+        }
+        bf16x8 pf[NR];
+        bool moved = false;
+        float mx[NR];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-          const bool up = mx[n] > m_run[n] + kRescale / a.c2;
-          const float corr = up ? fast_exp2((m_run[n] - mx[n]) * a.c2) : 1.f;   // 0 from -inf
-          if (up) m_run[n] = mx[n];
-          l_run[n] *= corr;
-#pragma unroll
-          for (int d = 0; d < NDB; ++d) acc[n][d] *= corr;
+          float t = fmaxf(fmaxf(fmaxf(z[n][0][0], z[n][0][1]), fmaxf(z[n][0][2], z[n][0][3])),
+                          fmaxf(fmaxf(z[n][1][0], z[n][1][1]), fmaxf(z[n][1][2], z[n][1][3])));
+          mx[n] = quad_max(t);
+          moved |= mx[n] > m_run[n] + kRescale / a.c2;
         }
-      }
+        if (__any(moved)) {
 #pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        const float mc = m_run[n] == -INFINITY ? 0.f : m_run[n] * a.c2;
-        float p[8], sum = 0.f;
+          for (int n = 0; n < NR; ++n) {
+            const bool up = mx[n] > m_run[n] + kRescale / a.c2;
+            const float corr = up ? fast_exp2((m_run[n] - mx[n]) * a.c2) : 1.f;   // 0 from -inf
+            if (up) m_run[n] = mx[n];
+            l_run[n] *= corr;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            p[4 * t + e] = fast_exp2(fmaf(z[n][t][e], a.c2, -mc));
-            sum += p[4 * t + e];
+            for (int d = 0; d < NDB; ++d) acc[n][d] *= corr;
           }
-        l_run[n] += sum;
-        pf[n] = bf16x8{(__bf16)p[0], (__bf16)p[1], (__bf16)p[2], (__bf16)p[3],
-                       (__bf16)p[4], (__bf16)p[5], (__bf16)p[6], (__bf16)p[7]};
-      }
+        }
 #pragma unroll
-      for (int i = 0; i < NDB / 4; ++i) {
-        uint32_t ta[4], tb[4];
-        const uint32_t wa[4] = {st.v[0][i], st.v[1][i], st.v[2][i], st.v[3][i]};
-        const uint32_t wb[4] = {st.v[4][i], st.v[5][i], st.v[6][i], st.v[7][i]};
-        transpose4(wa, ta);
-        transpose4(wb, tb);
-        if (!nans) {
+        for (int n = 0; n < NR; ++n) {
+          const float mc = m_run[n] == -INFINITY ? 0.f : m_run[n] * a.c2;
+          float p[8], sum = 0.f;
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              p[4 * t + e] = fast_exp2(fmaf(z[n][t][e], a.c2, -mc));
+              sum += p[4 * t + e];
+            }
+          l_run[n] += sum;
+          pf[n] = bf16x8{(__bf16)p[0], (__bf16)p[1], (__bf16)p[2], (__bf16)p[3],
+                         (__bf16)p[4], (__bf16)p[5], (__bf16)p[6], (__bf16)p[7]};
+        }
+#pragma unroll
+        for (int i = 0; i < NDB / 4; ++i) {
+          uint32_t ta[4], tb[4];
+          const uint32_t wa[4] = {st.v[0][i], st.v[1][i], st.v[2][i], st.v[3][i]};
+          const uint32_t wb[4] = {st.v[4][i], st.v[5][i], st.v[6][i], st.v[7][i]};
+          transpose4(wa, ta);
+          transpose4(wb, tb);
 #pragma unroll
           for (int d = 0; d < 4; ++d) {
             const bf16x8 vf = widen44(ta[d], tb[d], vs[0], vs[1]);
 #pragma unroll
             for (int n = 0; n < NR; ++n) acc[n][4 * i + d] = mfma16(vf, pf[n], acc[n][4 * i + d]);
           }
-        } else {
+        }
+        if (nans) {
 #pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const uint32_t na = nan_mask(ta[d]), nb = nan_mask(tb[d]);
-            const bf16x8 vf = widen44(ta[d] & ~na, tb[d] & ~nb, vs[0], vs[1]);
-            const bf16x8 one = widen44(na & 0x38383838u, nb & 0x38383838u, 1.f, 1.f);
+          for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int n = 0; n < NR; ++n) {
-              bf16x8 see;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const int key = e0 + 16 * (e >> 2) + 4 * grp + (e & 3);
-                see[e] = (__bf16)(key >= lo[n] && key < min(hi[n], ge << 4) ? 1.f : 0.f);
-              }
-              const f32x4 hits = mfma16(one, see, f32x4{});
-              f32x4 o = mfma16(vf, pf[n], acc[n][4 * i + d]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (hits[e] > 0.f) o[e] = __uint_as_float(0x7fc00000u);
-              acc[n][4 * i + d] = o;
-            }
-          }
+            for (int i = 0; i < NDB * 4; ++i)
+              if (hit[n] >> i & 1u) acc[n][i >> 2][i & 3] = __uint_as_float(0x7fc00000u);
+        }
+      };
+      Step st[2];
+      load(sb, st[0]);
+      for (int gr = sb; gr < se; gr += 4) {
+        if (gr + 2 < se) load(gr + 2, st[1]);
+        compute(gr, st[0]);
+        if (gr + 2 < se) {
+          if (gr + 4 < se) load(gr + 4, st[0]);
+          compute(gr + 2, st[1]);
         }
       }
-    };
-    Step st[2];
-    load(sb, st[0]);
-    for (int gr = sb; gr < se; gr += 4) {
-      if (gr + 2 < se) load(gr + 2, st[1]);
-      compute(gr, st[0]);
-      if (gr + 2 < se) {
-        if (gr + 4 < se) load(gr + 4, st[0]);
-        compute(gr + 2, st[1]);
+    }
+
+    // The waves' results meet in LDS.
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const float l = quad_sum(l_run[n]);
+      const int row = wave * ROWS + n * 16 + r16;
+      if (grp == 0) ml[row] = make_float2(m_run[n], l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float* o = lds + row * HD + NDB * (4 * grp + e);
+#pragma unroll
+        for (int d = 0; d < NDB; d += 4)
+          *reinterpret_cast<float4*>(o + d) =
+              make_float4(acc[n][d][e], acc[n][d + 1][e], acc[n][d + 2][e], acc[n][d + 3][e]);
       }
     }
-  }
-
-  // The waves' results meet in LDS.
+    __syncthreads();
+    constexpr int LPR = HD / 8;   // lanes of a row
+    for (int r = tid / LPR; r < rows; r += FEW_NT / LPR) {
+      const int d = (tid % LPR) * 8;
+      float M = -INFINITY;
 #pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const float l = quad_sum(l_run[n]);
-    const int row = wave * ROWS + n * 16 + r16;
-    if (grp == 0) ml[row] = make_float2(m_run[n], l);
+      for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w * ROWS + r].x);
+      const float ref = M == -INFINITY ? 0.f : M;
+      float L = 0.f, o[8] = {};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float* o = lds + row * HD + NDB * (4 * grp + e);
+      for (int w = 0; w < NW; ++w) {
+        const float2 p = ml[w * ROWS + r];
+        const float f = fast_exp2((p.x - ref) * a.c2);
+        L += p.y * f;
+        const float* src = lds + (w * ROWS + r) * HD + d;
 #pragma unroll
-      for (int d = 0; d < NDB; d += 4)
-        *reinterpret_cast<float4*>(o + d) =
-            make_float4(acc[n][d][e], acc[n][d + 1][e], acc[n][d + 2][e], acc[n][d + 3][e]);
+        for (int e = 0; e < 8; ++e) o[e] += src[e] * f;
+      }
+      if (!whole) {
+        const int64_t row = (int64_t(blockIdx.x) + int64_t(j) * a.hkv + kvh) * a.R + r;
+        float* po = a.part + row * HD + d;
+        *reinterpret_cast<float4*>(po) = make_float4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<float4*>(po + 4) = make_float4(o[4], o[5], o[6], o[7]);
+        if (d == 0) a.part_ml[row] = make_float2(M, L);
+      } else {
+        // an empty row has L = 0 and outputs 0; a NaN sum stays NaN
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        u16* out = a.o + (int64_t(s.q0 + r / a.g) * a.hq + kvh * a.g + r % a.g) * HD + d;
+        *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf2(o[0] * inv, o[1] * inv), pack_bf2(o[2] * inv, o[3] * inv),
+                                                    pack_bf2(o[4] * inv, o[5] * inv), pack_bf2(o[6] * inv, o[7] * inv));
+      }
     }
-  }
-  __syncthreads();
-  constexpr int LPR = HD / 8;   // lanes of a row
-  for (int r = tid / LPR; r < rows; r += FEW_NT / LPR) {
-    const int d = (tid % LPR) * 8;
-    float M = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w * ROWS + r].x);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float L = 0.f, o[8] = {};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float2 p = ml[w * ROWS + r];
-      const float f = fast_exp2((p.x - ref) * a.c2);
-      L += p.y * f;
-      const float* src = lds + (w * ROWS + r) * HD + d;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] += src[e] * f;
-    }
-    if (a.splits > 1) {
-      const int64_t row = (int64_t(split) * a.n_list * a.hkv + int64_t(j) * a.hkv + kvh) * a.R + r;
-      float* po = a.part + row * HD + d;
-      *reinterpret_cast<float4*>(po) = make_float4(o[0], o[1], o[2], o[3]);
-      *reinterpret_cast<float4*>(po + 4) = make_float4(o[4], o[5], o[6], o[7]);
-      if (d == 0) a.part_ml[row] = make_float2(M, L);
-    } else {
-      // an empty row has L = 0 and outputs 0; a NaN sum stays NaN
-      const float inv = L == 0.f ? 0.f : 1.f / L;
-      u16* out = a.o + (int64_t(s.q0 + r / a.g) * a.hq + kvh * a.g + r % a.g) * HD + d;
-      *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf2(o[0] * inv, o[1] * inv), pack_bf2(o[2] * inv, o[3] * inv),
-                                                  pack_bf2(o[4] * inv, o[5] * inv), pack_bf2(o[6] * inv, o[7] * inv));
-    }
+    __syncthreads();   // the LDS results have been read
   }
 }
 
@@ -424,8 +609,9 @@ __global__ __launch_bounds__(FEW_NT) void attn_few(Kv8Args a) {
 // out = sum_s o_s 2^((m_s - M) c2) / sum_s l_s 2^((m_s - M) c2), M = max m_s.  HD / 4 lanes take a row, G
 // groups of them its pieces in turn, four in flight; the groups meet in LDS.  G = 8 from 8 pieces on
 // (128 rows of 64 pieces: 35 us with G = 1, a chain of loads in 16 workgroups).
-template <int HD, int G>
-__global__ __launch_bounds__(256) void attn_join(Kv8Args a, int few) {
+// FEW: the pieces are shares of the kernel for few rows, else those of the kernel for many.
+template <int HD, int G, bool FEW>
+__global__ __launch_bounds__(256) void attn_join(Kv8Args a) {
   constexpr int LPR = HD / 4, PER = 256 / (LPR * G);
   __shared__ float4 po[G > 1 ? 256 : 1];
   __shared__ float2 pm[G > 1 ? 256 : 1];
@@ -433,14 +619,45 @@ __global__ __launch_bounds__(256) void attn_join(Kv8Args a, int few) {
   const int gi = tid / LPR % G, lane = tid % LPR;
   const int row_in = blockIdx.x * PER + tid / (LPR * G);
   const int d = lane * 4;
-  const int64_t step = int64_t(a.n_list) * a.hkv * a.R;
-  bool on = row_in < step;
-  const int r = row_in % a.R, jh = on ? row_in / a.R : 0;
-  const int kvh = jh % a.hkv;
-  const Seq s = seq_of(a, jh / a.hkv);
+  const int64_t all = int64_t(a.n_list) * a.hkv * a.R;
+  const int r = row_in % a.R, jh = min(row_in / a.R, a.n_list * a.hkv - 1);
+  const int kvh = jh % a.hkv, j = jh / a.hkv;
+  const Seq s = seq_of(a, j);
   const int rows = s.m * a.g;
-  on = on && r < rows && (rows <= FEW_ROWS) == (few != 0);
-  const int n = min(a.splits, max(1, (s.len + a.piece - 1) / a.piece));
+  bool on = row_in < all && r < rows && (rows <= FEW_ROWS) == FEW;
+  // piece i of the row is at slot + i * step
+  int64_t slot, step;
+  int n;
+  if constexpr (FEW) {
+    // the rows of a workgroup lie in one (sequence, head), or the search runs for each in turn
+    const Shares sh = shares_of(a);
+    const int j0 = __builtin_amdgcn_readfirstlane(j);
+    int64_t start;
+    int units;
+    item_of(a, sh, j0, start, units);
+    uint64_t other = __ballot(j != j0);
+    while (other) {
+      const int jn = __builtin_amdgcn_readlane(j, __builtin_ctzll(other));
+      int64_t st;
+      int un;
+      item_of(a, sh, jn, st, un);
+      if (j == jn) {
+        start = st;
+        units = un;
+      }
+      other &= ~__ballot(j == jn);
+    }
+    const int64_t x = start + int64_t(kvh) * units;
+    const int wa = sh.part_of(x + sh.head), wb = sh.part_of(x + max(units, 1) - 1);
+    n = wb - wa + 1;
+    on = on && n > 1;   // a whole one is final
+    slot = (int64_t(wa) + jh) * a.R + r;
+    step = a.R;
+  } else {
+    n = min(a.splits, max(1, (s.len + a.piece - 1) / a.piece));
+    slot = row_in;
+    step = all;
+  }
   float M = -INFINITY, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   if (on) {
@@ -449,7 +666,7 @@ __global__ __launch_bounds__(256) void attn_join(Kv8Args a, int few) {
       float4 x[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int64_t at = min(i0 + q * G, n - 1) * step + row_in;
+        const int64_t at = slot + min(i0 + q * G, n - 1) * step;
         p[q] = a.part_ml[at];
         x[q] = *reinterpret_cast<const float4*>(a.part + at * HD + d);
       }
@@ -512,8 +729,7 @@ hipError_t few_rows(const Kv8Args& a, hipStream_t s) {
                                              hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
     if (e != hipSuccess) return e;
   }
-  const int64_t grid = int64_t(a.n_list) * a.splits * a.hkv;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  const int grid = a.direct ? a.n_list * a.hkv : a.parts;
   hipLaunchKernelGGL((attn_few<HD, NR>), dim3(unsigned(grid)), dim3(FEW_NT), lds, s, a);
   return hipGetLastError();
 }
@@ -525,15 +741,15 @@ hipError_t launch_dim(const Kv8Args& a, bool few, hipStream_t s) {
     e = a.R <= 16 ? few_rows<HD, 1>(a, s) : few_rows<HD, 2>(a, s);
   else
     e = launch_attn_many(a, s);
-  if (e != hipSuccess || a.splits == 1) return e;
+  if (e != hipSuccess || !a.part) return e;
   const int64_t rows = int64_t(a.n_list) * a.hkv * a.R;
-  if (a.splits >= 8) {
-    constexpr int PER = 256 / (HD / 4 * 8);
-    hipLaunchKernelGGL((attn_join<HD, 8>), dim3(unsigned((rows + PER - 1) / PER)), dim3(256), 0, s, a, few ? 1 : 0);
-  } else {
-    constexpr int PER = 256 / (HD / 4);
-    hipLaunchKernelGGL((attn_join<HD, 1>), dim3(unsigned((rows + PER - 1) / PER)), dim3(256), 0, s, a, few ? 1 : 0);
-  }
+  constexpr int P1 = 256 / (HD / 4), P8 = P1 / 8 ? P1 / 8 : 1;
+  if (few)
+    hipLaunchKernelGGL((attn_join<HD, 8, true>), dim3(unsigned((rows + P8 - 1) / P8)), dim3(256), 0, s, a);
+  else if (a.splits >= 8)
+    hipLaunchKernelGGL((attn_join<HD, 8, false>), dim3(unsigned((rows + P8 - 1) / P8)), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((attn_join<HD, 1, false>), dim3(unsigned((rows + P1 - 1) / P1)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

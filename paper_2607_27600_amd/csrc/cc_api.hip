@@ -1107,7 +1107,7 @@ struct Kv8Class {
   int n = 0;               // sequences of the class
   int n_list = 0, listed = 0;
   int32_t list[KV8_LIST];
-  int R = 0, piece = 0, splits = 1;
+  int R = 0, piece = 0, splits = 1, direct = 0, parts = 0;
   size_t part = 0, total = 0;   // workspace: (maximum, sum) pairs behind the outputs
 };
 
@@ -1129,20 +1129,23 @@ Kv8Class kv8_class(const cc_problem* p, int max_len, bool few) {
   c.listed = c.n <= KV8_LIST;
   c.n_list = c.listed ? c.n : p->n_seqs;
   const int64_t items = blocks * p->n_heads_kv;   // workgroups without a cut
-  int64_t want;
+  size_t rows = 0;                                // partial results
   if (few) {
-    // pieces until there are eight workgroups a CU, of 256 entries (64 a wave) at the least
-    want = std::min<int64_t>((8 * kCus + items - 1) / items, (int64_t(max_len) + 255) / 256);
+    // Short caches: a workgroup for each (sequence, head), nothing to join.  Else the work is shared
+    // out among two workgroups a CU, or one for each (sequence, head) up to eight a CU.
+    c.direct = max_len <= KV8_DIRECT;
+    c.parts = int(std::min<int64_t>(8 * kCus, std::max<int64_t>(2 * kCus, items)));
+    if (!c.direct) rows = (size_t(c.parts) + size_t(c.n_list) * p->n_heads_kv) * c.R;
   } else {
     // pieces until there are two workgroups a CU (what is resident), of 512 entries at the least
-    want = std::min<int64_t>((2 * kCus + items - 1) / items, (int64_t(max_len) + 511) / 512);
+    const int64_t want = std::max<int64_t>(
+        1, std::min<int64_t>((2 * kCus + items - 1) / items, (int64_t(max_len) + 511) / 512));
+    c.piece = int(((int64_t(max_len) + want - 1) / want + MANY_KEYS - 1) / MANY_KEYS * MANY_KEYS);
+    c.piece = std::max(c.piece, MANY_KEYS);
+    c.splits = std::max(1, int((int64_t(max_len) + c.piece - 1) / c.piece));
+    if (c.splits > 1) rows = size_t(c.splits) * c.n_list * p->n_heads_kv * c.R;
   }
-  want = std::max<int64_t>(want, 1);
-  c.piece = int(((int64_t(max_len) + want - 1) / want + MANY_KEYS - 1) / MANY_KEYS * MANY_KEYS);
-  c.piece = std::max(c.piece, MANY_KEYS);
-  c.splits = std::max(1, int((int64_t(max_len) + c.piece - 1) / c.piece));
-  if (c.splits > 1) {
-    const size_t rows = size_t(c.splits) * c.n_list * p->n_heads_kv * c.R;
+  if (rows) {
     c.part = align_up(rows * p->head_dim * sizeof(float));
     c.total = c.part + align_up(rows * sizeof(float2));
   }
@@ -1203,8 +1206,10 @@ cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv,
     a.R = c.R;
     a.piece = c.piece;
     a.splits = c.splits;
-    a.part = c.splits > 1 ? reinterpret_cast<float*>(at(ws, off)) : nullptr;
-    a.part_ml = c.splits > 1 ? reinterpret_cast<float2*>(at(ws, off + c.part)) : nullptr;
+    a.direct = c.direct;
+    a.parts = c.parts;
+    a.part = c.total ? reinterpret_cast<float*>(at(ws, off)) : nullptr;
+    a.part_ml = c.total ? reinterpret_cast<float2*>(at(ws, off + c.part)) : nullptr;
     a.n_list = c.n_list;
     a.listed = c.listed;
     std::copy_n(c.list, c.listed ? c.n : 0, a.list);
