@@ -12,6 +12,11 @@ the end of the prompt (prefill-end mode).
 
 Everything here is orchestration on the caller's stream; every step of the pass runs in
 libcc.  Entries keep the absolute positions they were appended with.
+
+The cache holds bf16, or 8 bits (cache="e4m3": E4M3 codes with a power-of-two scale for each
+block of entries and head, half the bytes): the same cycle on cc_append_kv8, cc_attention_kv8
+and cc_compact_kv8.  An 8-bit cache scores the given-query fast variants, and `attend` runs
+the inference cycle's own attention over it.
 """
 from __future__ import annotations
 
@@ -53,25 +58,43 @@ class RefreshLoop:
     """One sequence's cache under counter-causal memory management."""
 
     def __init__(self, model: Model, J: int, h: int, device="cuda",
-                 capacity: Optional[int] = None):
+                 capacity: Optional[int] = None, cache: str = "bf16", scale_block: int = 16):
+        """cache: "bf16" or "e4m3" (scale_block entries a scale: a power of two from 16 to 128)."""
         if model.mode not in ("last_layer", "last_layer_fused", "last_layer_h"):
             raise ValueError("mode must be last_layer, last_layer_fused or last_layer_h")
         if J < 1 or h < 1:
             raise ValueError("J and h must be positive")
+        if cache not in ("bf16", "e4m3"):
+            raise ValueError("cache must be bf16 or e4m3")
+        if cache == "e4m3" and model.mode == "last_layer_h":
+            raise ValueError("an 8-bit cache scores given queries (last_layer or last_layer_fused)")
+        if cache == "e4m3" and scale_block not in (16, 32, 64, 128):
+            raise ValueError("scale_block must be 16, 32, 64 or 128")
         self.m, self.J, self.h = model, J, h
+        self.cache = cache
         self.device = torch.device(device)
         cap = capacity if capacity is not None else J + h   # chunked mode needs J + h
         self.cap = cap
         L, hkv, d = model.n_layers, model.n_heads_kv, model.head_dim
         bf = torch.bfloat16
-        self.k = torch.zeros((L, hkv, cap, d), dtype=bf, device=self.device)
+        self.k = torch.zeros((L, hkv, cap, d), dtype=torch.uint8 if cache == "e4m3" else bf, device=self.device)
         self.v = torch.zeros_like(self.k)
         self.ids = torch.zeros(cap, dtype=torch.int32, device=self.device)
         self.pos = torch.zeros(cap, dtype=torch.int32, device=self.device)
         self.rows = torch.zeros((cap, model.row_width), dtype=bf, device=self.device)
         self.n = 0
-        self.kv = cc.kv_contiguous(self.k, self.v, n_layers=L, layer_stride=hkv * cap * d,
-                                   head_stride=cap * d, tok_stride=d)
+        if cache == "e4m3":
+            blocks = -(-cap // scale_block)
+            self.k_scale = torch.zeros((L, hkv, blocks), dtype=torch.uint8, device=self.device)
+            self.v_scale = torch.zeros_like(self.k_scale)
+            self.cached = torch.zeros(1, dtype=torch.int32, device=self.device)   # n, for appending
+            self.kv = cc.kv8_contiguous(self.k, self.v, self.k_scale, self.v_scale, n_layers=L,
+                                        layer_stride=hkv * cap * d, head_stride=cap * d, tok_stride=d,
+                                        scale_block=scale_block, scale_layer_stride=hkv * blocks,
+                                        scale_head_stride=blocks)
+        else:
+            self.kv = cc.kv_contiguous(self.k, self.v, n_layers=L, layer_stride=hkv * cap * d,
+                                       head_stride=cap * d, tok_stride=d)
         self.refreshes = 0
 
     # ---------------------------------------------------------------- inference side
@@ -82,28 +105,62 @@ class RefreshLoop:
         if self.n + m > self.cap:
             raise ValueError(f"cache holds {self.n} of {self.cap}; refresh before appending {m}")
         sl = slice(self.n, self.n + m)
-        self.k[:, :, sl].copy_(k)
-        self.v[:, :, sl].copy_(v)
+        if self.cache == "e4m3":
+            if m == 0:
+                return
+            # (lengths written by the stream, as in _queued_problem)
+            self.cached.fill_(self.n)
+            cc.cc_append_kv8(self._queued_problem(m), self.kv, k.transpose(1, 2), v.transpose(1, 2), self.cached,
+                             capacity=self.cap, n_layers=self.m.n_layers, rotate=False)
+        else:
+            self.k[:, :, sl].copy_(k)
+            self.v[:, :, sl].copy_(v)
         self.ids[sl].copy_(ids)
         self.pos[sl].copy_(pos)
         self.rows[sl].copy_(rows)
         self.n += m
 
     # ---------------------------------------------------------------- refresh cycle
-    def problem(self, cu_device: Optional[torch.Tensor] = None) -> cc.Problem:
+    def problem(self, cu_device: Optional[torch.Tensor] = None, n: Optional[int] = None) -> cc.Problem:
         m = self.m
-        return cc.problem(dtype="bf16", cu_seqlens=[0, self.n], n_heads_q=m.n_heads_q,
+        return cc.problem(dtype="bf16", cu_seqlens=[0, self.n if n is None else n], n_heads_q=m.n_heads_q,
                           n_heads_kv=m.n_heads_kv, head_dim=m.head_dim, hidden=m.hidden,
                           vocab=m.vocab, device=self.device, mode=m.mode, ffn=m.ffn,
                           rope_theta=m.rope_theta, rms_eps=m.rms_eps,
                           lmhead_packed=m.w_lm_packed is not None, cu_device=cu_device)
 
-    def _queued_problem(self) -> cc.Problem:
+    def _queued_problem(self, n: Optional[int] = None) -> cc.Problem:
         """problem(), its device lengths written by the current stream: no wait for a copy
         (2% of a pass of 768 entries when passes follow each other)."""
         cu = torch.zeros(2, dtype=torch.int32, device=self.device)
-        cu[1:].fill_(self.n)
-        return self.problem(cu)
+        cu[1:].fill_(self.n if n is None else n)
+        return self.problem(cu, n)
+
+    def attend(self, layer: int, q: torch.Tensor) -> torch.Tensor:
+        """Causal attention of the last m entries' queries q [m][Hq][head_dim] (rotated) over cache
+        layer `layer` (8-bit caches): the inference cycle's attention after its append."""
+        if self.cache != "e4m3":
+            raise ValueError("attend runs on 8-bit caches")
+        m = int(q.shape[0])
+        if m > self.n:
+            raise ValueError(f"{m} queries for {self.n} entries")
+        lens = torch.full((1,), self.n, dtype=torch.int32, device=self.device)
+        return cc.cc_attention_kv8(self._queued_problem(m), q, self.kv, layer, lens, self.n)
+
+    def _scores8(self) -> torch.Tensor:
+        """scores() on an 8-bit cache, step by step: attention, W_o, LM head."""
+        m, n = self.m, self.n
+        p = self._queued_problem()
+        q = self.rows[:n].view(n, m.n_heads_q, m.head_dim)
+        u = cc.cc_attention_kv8(p, q, self.kv, m.n_layers - 1, p.cu_d[1:], n, mask="counter").view(n, m.row_width)
+        if m.mode == "last_layer":
+            u = cc.cc_linear("bf16", u, m.w_o, torch.empty((n, m.hidden), dtype=u.dtype, device=u.device))
+        else:   # the LM head's input is as wide as the queries
+            p.struct.hidden = m.row_width
+        s = torch.empty(n, dtype=torch.float32, device=self.device)
+        if m.w_lm_packed is not None:
+            return cc.cc_lmhead_score_packed(p, u, m.w_lm_packed, self.ids, s)
+        return cc.cc_lmhead_score(p, u, m.w_lm, self.ids, s)
 
     def inputs(self) -> cc.Inputs:
         m, n = self.m, self.n
@@ -116,6 +173,8 @@ class RefreshLoop:
 
     def scores(self) -> torch.Tensor:
         """Counter-causal surprise of every cached entry (the last one is +inf)."""
+        if self.cache == "e4m3":
+            return self._scores8()
         s = torch.empty(self.n, dtype=torch.float32, device=self.device)
         cc.cc_score(self._queued_problem(), self.inputs(), s)
         return s
@@ -131,7 +190,8 @@ class RefreshLoop:
         cc.cc_select_keep(s, [0], [self.n], [self.J], keep)
         if hook is not None:
             hook(s, keep)
-        cc.cc_compact_kv(p, self.kv, keep, [self.J], 0, token_ids=self.ids, pos_ids=self.pos)
+        compact = cc.cc_compact_kv8 if self.cache == "e4m3" else cc.cc_compact_kv
+        compact(p, self.kv, keep, [self.J], 0, token_ids=self.ids, pos_ids=self.pos)
         cc.cc_compact_rows(p, self.rows, keep, [self.J], 0)
         self.n = self.J
         self.refreshes += 1
