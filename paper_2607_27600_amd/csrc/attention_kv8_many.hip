@@ -7,12 +7,17 @@
 //
 // A tile's codes go from memory straight into LDS while the tile before is worked on (each lane reads
 // back what its own load brought, so they need no barrier, and no registers for a whole step: with the
-// codes held in registers instead the kernel spilled 376 bytes a lane and ran at a sixth of its
+// codes held in registers instead the kernel spilled 376 bytes a lane and ran at a fifth of its
 // speed), and are turned into bf16 once for the four waves: 32 conversions, 8 LDS writes a wave and
-// tile.  (Turning them into operands in every wave would cost each 128.)  In LDS a tile is bf16 rows
-// whose 16-byte chunks are swizzled by bits of the row so that fragment reads hit every bank once; V^T
-// is read with transpose reads.  Two K and two V buffers, one barrier a tile.  Matrix work of one tile
-// is interleaved with the exponentials of the tile before.
+// tile, between the matrix instructions.  (At the end of a step, behind the loads' arrival: 677 us in
+// place of 605, 8192 entries scored by 32 heads on 8.)  In LDS a tile is bf16 rows whose 16-byte chunks
+// are swizzled by bits of the row so that fragment reads hit every bank once; V^T is read with transpose
+// reads.  Two K and two V buffers, one barrier a tile.  Matrix work of one tile is interleaved with the
+// exponentials of the tile before.
+//
+// Bound by the issue of a wave's instructions, matrix ones and exponentials first: 4096 entries scored by
+// 32 heads on 8 in 166 us (830 TFLOP/s), against 144 us of cc_attention_cc on bf16 entries, which has 29
+// vector instructions where this has 39 and 8 scalar ones where this has 24.
 //
 // A NaN value in a tile that some rows see in part becomes the least bf16 number, 2^-133: nothing beside
 // fp32 sums, and told from every other value by its last bit (E4M3 values end in zeros).  A tile that
@@ -164,17 +169,27 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
     const int lrow = (lane / CPR) + wave * SH::RPW;      // + i * NWAVES * RPW
     const int piece = lane % CPR;
     constexpr int RSTEP = NWAVES * SH::RPW;
-    // LDS places of the two bf16 chunks: rows i * RSTEP further have the same swizzles
+    // LDS places of the two bf16 chunks: rows i * RSTEP further have the same swizzles.  A write takes eight
+    // lanes at a time, and in rows of 256 bytes these should meet eight different chunks modulo 128: half of them
+    // write their second chunk first, and read their codes back in that order (0.8%; nothing in rows of 128).
+    const int second = HD == 128 ? piece >> 2 : 0;
     uint32_t kst[2], vst[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      kst[h] = lrow * ROWB + (((2 * piece + h) ^ SH::kswz(lrow)) * 16);
-      vst[h] = lrow * ROWB + (((2 * piece + h) ^ SH::vswz(lrow)) * 16);
+      kst[h] = lrow * ROWB + (((2 * piece + (h ^ second)) ^ SH::kswz(lrow)) * 16);
+      vst[h] = lrow * ROWB + (((2 * piece + (h ^ second)) ^ SH::vswz(lrow)) * 16);
     }
+    const uint32_t raw_off = lane * 16 + second * 8;
 
-    // Pages of the 16-entry groups a lane each, 64 groups (16 tiles) at a time, and their scales.
-    const int gfirst = tb * 4, glast = last >> 4;
-    int gbase = gfirst;
+    // Where a tile's codes lie and their scales (K in byte 0, V in byte 1), for this wave's loads.  Pages
+    // and scales are fetched a group a lane, 64 groups (16 tiles) at a time, the next ones in two steps
+    // while these are used up.
+    struct At {
+      int64_t off[NI];
+      uint32_t sc[NI];
+    };
+    const int glast = last >> 4;
+    int gbase = tb * 4;
     auto pages_at = [&](int base) { return a.k.paged ? table[min(base + lane, glast) >> (a.k.codes.page_shift - 4)] : 0; };
     auto scales_at = [&](int base, int pg) {
       const int gg = min(base + lane, glast);
@@ -182,66 +197,77 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
       const int64_t o = int64_t(pg) * a.k.s_page + (slot >> a.k.block_shift);
       return uint32_t(kscale[o]) | (uint32_t(vscale[o]) << 8);
     };
-    int page = pages_at(gbase);
-    uint32_t scale = scales_at(gbase, page);
-    int page_n = page;
-    uint32_t scale_n = scale;
-    // group of load i of tile t, and the lane that holds it
-    auto group_of = [&](int t, int i) {
-      return min(t * 4 + __builtin_amdgcn_readfirstlane((wave * SH::RPW + i * RSTEP) >> 4), glast);
-    };
-    auto held = [&](int cur, int nxt, int gg) {
-      const int at = gg - gbase;
-      return at < 64 ? __builtin_amdgcn_readlane(cur, at) : __builtin_amdgcn_readlane(nxt, min(at - 64, 63));
-    };
-    const uint32_t ts = uint32_t(a.k.codes.tok_stride);
-    auto load = [&](char* raw, const char* plane, int t) {
+    int page = pages_at(gbase), page_n = page;
+    uint32_t scale = scales_at(gbase, page), scale_n = scale;
+    auto look = [&](int t, At& at) {   // every tile once, in order
+      const int nth = (t - tb) & 15;
+      if (nth == 0 && t > tb) {
+        gbase += 64;
+        page = page_n;
+        scale = scale_n;
+      }
+      if (nth == 6) page_n = pages_at(gbase + 64);
+      if (nth == 11) scale_n = scales_at(gbase + 64, page_n);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int gg = group_of(t, i);
-        const int pg = held(page, page_n, gg);
+        const int gg = min(t * 4 + ((wave * SH::RPW + i * RSTEP) >> 4), glast);
         const int slot = a.k.paged ? (gg << 4) & a.k.codes.page_mask : gg << 4;
-        const char* base =
-            uniform_ptr(plane + (int64_t(pg) * a.k.codes.page_stride + int64_t(slot) * a.k.codes.tok_stride));
-        const int r = min((lrow + i * RSTEP) & 15, last - (gg << 4));   // past the end: the last entry again
-        dma16(base, uint32_t(r) * ts + piece * 16, lds_addr(raw + (i * NWAVES + wave) * 1024));
+        at.off[i] = int64_t(__builtin_amdgcn_readlane(page, gg - gbase)) * a.k.codes.page_stride +
+                    int64_t(slot) * a.k.codes.tok_stride;
+        at.sc[i] = __builtin_amdgcn_readlane(scale, gg - gbase);
+      }
+    };
+    const uint32_t ts = uint32_t(a.k.codes.tok_stride);
+    const uint32_t lane_off = (lrow & 15) * ts + piece * 16;   // (i * RSTEP is a multiple of 16)
+    auto load = [&](char* raw, const char* plane, int t, const At& at) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        uint32_t off = lane_off;
+        if (t * BN + BN > len) {   // past the end: the last entry again
+          const int g0 = min(t * 4 + ((wave * SH::RPW + i * RSTEP) >> 4), glast) << 4;
+          off = uint32_t(min(lrow & 15, last - g0)) * ts + piece * 16;
+        }
+        dma16(uniform_ptr(plane + at.off[i]), off, lds_addr(raw + (i * NWAVES + wave) * 1024));
       }
     };
     auto is_masked = [&](int t) { return t * BN < full0 || t * BN + BN > min(full1, stop); };
-    auto put = [&](u16* dst, const char* raw, const uint32_t (&at)[2], int t, auto values) {
-      constexpr bool V = decltype(values)::value;
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const uint32_t sc = uint32_t(held(int(scale), int(scale_n), group_of(t, i)));
-        uint4 y[2], z = *reinterpret_cast<const uint4*>(raw + (i * NWAVES + wave) * 1024 + lane * 16);
-        const float f = e8m0_scale((sc >> (V ? 8 : 0)) & 255u);
-        if (V && is_masked(t)) {
-          uint32_t w[4] = {z.x, z.y, z.z, z.w}, n[4];
-          const bool out = t * BN + lrow + i * RSTEP >= len;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            n[k] = out ? 0 : ((w[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // 0x80 at a NaN code
-            w[k] = out ? 0 : w[k] & ~((n[k] >> 7) * 0xffu);
-          }
-          widen16(make_uint4(w[0], w[1], w[2], w[3]), f, y[0], y[1]);
-          auto tag = [](uint32_t& lo, uint32_t& hi, uint32_t m) {
-            lo |= ((m >> 7) & 1u) | ((m << 1) & 0x10000u);
-            hi |= ((m >> 23) & 1u) | ((m >> 15) & 0x10000u);
-          };
-          tag(y[0].x, y[0].y, n[0]);
-          tag(y[0].z, y[0].w, n[1]);
-          tag(y[1].x, y[1].y, n[2]);
-          tag(y[1].z, y[1].w, n[3]);
-        } else {
-          widen16(z, f, y[0], y[1]);
-        }
-        char* d = reinterpret_cast<char*>(dst) + i * RSTEP * ROWB;
-        *reinterpret_cast<uint4*>(d + at[0]) = y[0];
-        *reinterpret_cast<uint4*>(d + at[1]) = y[1];
-      }
+    auto fetch = [&](const char* raw, int i) {
+      const char* p = raw + (i * NWAVES + wave) * 1024;
+      const uint2 a8 = *reinterpret_cast<const uint2*>(p + raw_off), b8 = *reinterpret_cast<const uint2*>(p + (raw_off ^ 8));
+      return make_uint4(a8.x, a8.y, b8.x, b8.y);
     };
-    // the codes that this wave asked for have arrived
+    auto put = [&](u16* dst, int i, const uint4& z, int t, const At& at, auto values) {
+      constexpr bool V = decltype(values)::value;
+      const float f = e8m0_scale((at.sc[i] >> (V ? 8 : 0)) & 255u);
+      uint4 y[2];
+      if (V && is_masked(t)) {
+        uint32_t w[4] = {z.x, z.y, z.z, z.w}, n[4];
+        const bool out = t * BN + lrow + i * RSTEP >= len;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          n[k] = out ? 0 : ((w[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // 0x80 at a NaN code
+          w[k] = out ? 0 : w[k] & ~((n[k] >> 7) * 0xffu);
+        }
+        widen16(make_uint4(w[0], w[1], w[2], w[3]), f, y[0], y[1]);
+        auto tag = [](uint32_t& lo, uint32_t& hi, uint32_t m) {
+          lo |= ((m >> 7) & 1u) | ((m << 1) & 0x10000u);
+          hi |= ((m >> 23) & 1u) | ((m >> 15) & 0x10000u);
+        };
+        tag(y[0].x, y[0].y, n[0]);
+        tag(y[0].z, y[0].w, n[1]);
+        tag(y[1].x, y[1].y, n[2]);
+        tag(y[1].z, y[1].w, n[3]);
+      } else {
+        widen16(z, f, y[0], y[1]);
+      }
+      char* d = reinterpret_cast<char*>(dst) + i * RSTEP * ROWB;
+      *reinterpret_cast<uint4*>(d + (V ? vst : kst)[0]) = y[0];
+      *reinterpret_cast<uint4*>(d + (V ? vst : kst)[1]) = y[1];
+    };
+    // the codes that this wave asked for have arrived; but for its latest loads of one tensor
     auto arrived = [] { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
+    auto arrived_but = [] { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NI) : "memory"); };
+    auto read_back = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
 
     uint32_t koff[NKS];
 #pragma unroll
@@ -286,16 +312,31 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
 
     using Keys = std::false_type;
     using Values = std::true_type;
-    load(kraw, kplane, tb);
-    load(vraw, vplane, tb);
+    At at1, at2, at3;   // tiles t + 1, t + 2, t + 3
+    look(tb, at1);
+    load(kraw, kplane, tb, at1);
+    load(vraw, vplane, tb, at1);
     arrived();
-    put(kb0, kraw, kst, tb, Keys{});
-    put(vb0, vraw, vst, tb, Values{});
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      put(kb0, i, fetch(kraw, i), tb, at1, Keys{});
+      put(vb0, i, fetch(vraw, i), tb, at1, Values{});
+    }
+    at2 = at3 = at1;
     if (tb + 1 < te) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the codes have been read back
-      load(kraw, kplane, tb + 1);
+      look(tb + 1, at1);
+      read_back();
+      load(kraw, kplane, tb + 1, at1);
       arrived();
-      put(kb1, kraw, kst, tb + 1, Keys{});
+#pragma unroll
+      for (int i = 0; i < NI; ++i) put(kb1, i, fetch(kraw, i), tb + 1, at1, Keys{});
+      read_back();
+      if (tb + 2 < te) {
+        look(tb + 2, at2);
+        load(kraw, kplane, tb + 2, at2);
+      }
+      load(vraw, vplane, tb + 1, at1);
+      if (tb + 3 < te) look(tb + 3, at3);
     }
     __syncthreads();
     f32x16 sa[2], sb[2];
@@ -326,9 +367,10 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
       }
     };
 
-    // Tile t with parity P: S(t) in sc, its unmasked row maximum in mx; K(t+1) and V(t) in LDS.  The codes
-    // of K(t+2) and V(t+1) are loaded at the start and written at the end, into buffers that the tile
-    // before has freed.
+    // Tile t with parity P: S(t) in sc, its unmasked row maximum in mx; K(t+1) and V(t) in LDS; the codes
+    // of K(t+2) and V(t+1) on their way since the step before.  K(t+2) is turned into bf16 between the
+    // matrix instructions of S(t+1), V(t+1) between those of P V, into buffers that the tile before has freed,
+    // and the codes of the next tile are asked for right behind.
     auto step = [&](int t, auto par) {
       constexpr int P = decltype(par)::value;
       f32x16(&sc)[2] = P ? sb : sa;
@@ -337,8 +379,7 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
       u16* Kfree = P ? kb1 : kb0;
       const u16* Vc = P ? vb1 : vb0;
       u16* Vfree = P ? vb0 : vb1;
-      if (t + 2 < te) load(kraw, kplane, t + 2);
-      if (t + 1 < te) load(vraw, vplane, t + 1);
+      const bool more_k = t + 2 < te, more_v = t + 1 < te;
       const bool masked = is_masked(t);
       bf16x8 kf[4];
       kf[0] = kfrag(Kn, 0);
@@ -357,11 +398,18 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
       const float mc = (m_run == -INFINITY ? 0.f : m_run) * a.c2;
       sn[0] = f32x16{};
       sn[1] = f32x16{};
+      if (more_k) arrived_but();   // (V(t+1) was asked for behind K(t+2))
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(1);
       constexpr int EPM = 32 / NS;
+      uint4 raw[NI];
 #pragma unroll
       for (int q = 0; q < NS; ++q) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          if (q == 1 + 6 * i && more_k) raw[i] = fetch(kraw, i);
+          if (q == 5 + 6 * i && more_k) put(Kfree, i, raw[i], t + 2, at2, Keys{});
+        }
         if (q + 3 < NS) kf[(q + 3) & 3] = kfrag(Kn, q + 3);
         sn[q & 1] = mfma32(kf[q & 3], qf[q >> 1], sn[q & 1]);
 #pragma unroll
@@ -373,6 +421,7 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
         }
         __builtin_amdgcn_sched_barrier(0);
       }
+      if (t + 3 < te) load(kraw, kplane, t + 3, at3);
       if (__any(corr != 1.f)) {
 #pragma unroll
         for (int db = 0; db < NDB; ++db) acc[db] *= corr;
@@ -400,9 +449,20 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
       vf[2] = vfrag(Vc, 2);
       pack(0);
       constexpr int SPM = 32 / NPV;
+      if (more_v) {
+        if (t + 3 < te)
+          arrived_but();
+        else
+          arrived();
+      }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int q = 0; q < NPV; ++q) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          if (q == 1 + 6 * i && more_v) raw[i] = fetch(vraw, i);
+          if (q == 5 + 6 * i && more_v) put(Vfree, i, raw[i], t + 1, at1, Values{});
+        }
         if (q + 3 < NPV) vf[(q + 3) & 3] = vfrag(Vc, q + 3);
         acc[q % NDB] = mfma32(vf[q & 3], pf[q / NDB], acc[q % NDB]);
         if (q % NDB == NDB - 1 && q < NPV - 1) pack(q / NDB + 1);
@@ -428,18 +488,10 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
       if (masked && tagged) poison(t);
       l_run = l_run * corr + (ls0 + ls1);
       mx = half_max(fmaxf(m0, m1));
-      arrived();
-      if (t + 2 < te) put(Kfree, kraw, kst, t + 2, Keys{});
-      if (t + 1 < te) put(Vfree, vraw, vst, t + 1, Values{});
-      // the next 64 groups: pages in the middle of these, scales behind them
-      const int at = t + 1 - gbase / 4;
-      if (at == 4) page_n = pages_at(gbase + 64);
-      if (at == 8) scale_n = scales_at(gbase + 64, page_n);
-      if (at == 16) {
-        gbase += 64;
-        page = page_n;
-        scale = scale_n;
-      }
+      if (more_k) load(vraw, vplane, t + 2, at2);
+      at1 = at2;
+      at2 = at3;
+      if (t + 4 < te) look(t + 4, at3);
       __syncthreads();
     };
     using I0 = std::integral_constant<int, 0>;

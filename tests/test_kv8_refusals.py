@@ -1,0 +1,271 @@
+"""What the operators of the inference cycle refuse, on the host: every bad call ends with its status
+before anything is enqueued (no GPU is needed), and the binding's own checks."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2607_27600_amd import cc
+
+P = 0x100000   # an address that is checked, never read
+
+
+def _problem(cu=(0, 3, 8), **kw):
+    c = (ctypes.c_int32 * len(cu))(*cu)
+    p = cc.c_problem()
+    p.dtype, p.n_seqs = cc.CC_BF16, len(cu) - 1
+    p.cu_seqlens_h = ctypes.cast(c, ctypes.POINTER(ctypes.c_int32))
+    p.cu_seqlens_d = P
+    p.n_heads_q, p.n_heads_kv, p.head_dim, p.hidden, p.vocab, p.rope_theta = 8, 2, 128, 64, 1, 1e4
+    for k, v in kw.items():
+        setattr(p, k, v)
+    p._keep = c
+    return p
+
+
+def _kv(paged=True, es=1, **kw):
+    s = cc.c_kv()
+    s.layout, s.n_layers = (cc.CC_KV_PAGED if paged else cc.CC_KV_CONTIGUOUS), 2
+    s.k, s.v = P, P
+    s.layer_stride, s.head_stride, s.tok_stride, s.seq_stride = 1 << 20, 1 << 14, 128, 1 << 16
+    s.page_stride, s.block_table, s.page_size, s.max_pages = 1 << 15, P, 16, 64
+    for k, v in kw.items():
+        setattr(s, k, v)
+    return s
+
+
+def _kv8(paged=True, **kw):
+    s = cc.c_kv8()
+    codes = {k: v for k, v in kw.items() if k in dict(cc.c_kv._fields_)}
+    s.codes = _kv(paged, **codes)
+    s.k_scale, s.v_scale, s.scale_block = P, P, 16
+    s.scale_layer_stride, s.scale_head_stride, s.scale_page_stride, s.scale_seq_stride = 64, 8, 16, 128
+    for k, v in kw.items():
+        if k not in codes:
+            setattr(s, k, v)
+    return s
+
+
+def _rows(**kw):
+    r = cc.c_rows()
+    r.base, r.layer_stride, r.tok_stride, r.head_stride = P, 8192, 1024, 128
+    for k, v in kw.items():
+        setattr(r, k, v)
+    return r
+
+
+def _append(**kw):
+    a = cc.c_append()
+    a.k, a.v, a.q, a.q_out, a.cached = _rows(), _rows(), _rows(), P, P
+    a.capacity, a.layer, a.n_layers, a.rotate = 0, 0, 1, 1
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+BAD_APPEND = [
+    (dict(), dict(n_layers=0), {}, cc.CC_ERR_SHAPE),
+    (dict(), dict(layer=-1), {}, cc.CC_ERR_SHAPE),
+    (dict(), dict(layer=2), {}, cc.CC_ERR_SHAPE),
+    (dict(), dict(layer=1, n_layers=2, q=cc.c_rows()), {}, cc.CC_ERR_SHAPE),
+    (dict(), dict(n_layers=2), {}, cc.CC_ERR_UNSUPPORTED),            # queries belong to one layer
+    (dict(), dict(rotate=2), {}, cc.CC_ERR_ARG),
+    (dict(rope_theta=0.0), dict(), {}, cc.CC_ERR_ARG),
+    (dict(rope_theta=float("inf")), dict(), {}, cc.CC_ERR_ARG),
+    (dict(rope_theta=float("nan")), dict(), {}, cc.CC_ERR_ARG),
+    (dict(), dict(capacity=-1), {}, cc.CC_ERR_SHAPE),
+    (dict(), dict(cached=None), {}, cc.CC_ERR_ARG),
+    (dict(), dict(k=_rows(base=None)), {}, cc.CC_ERR_ARG),
+    (dict(), dict(v=_rows(base=P + 8)), {}, cc.CC_ERR_ARG),
+    (dict(), dict(k=_rows(tok_stride=1020)), {}, cc.CC_ERR_UNSUPPORTED),
+    (dict(), dict(k=_rows(head_stride=-128)), {}, cc.CC_ERR_SHAPE),
+    (dict(), dict(q=_rows(tok_stride=4)), {}, cc.CC_ERR_UNSUPPORTED),
+    (dict(), dict(q_out=None), {}, cc.CC_ERR_ARG),
+    (dict(), dict(q_out=P + 4), {}, cc.CC_ERR_ARG),
+    (dict(head_dim=96), dict(), {}, cc.CC_ERR_UNSUPPORTED),
+    (dict(n_heads_kv=3), dict(), {}, cc.CC_ERR_SHAPE),
+    (dict(dtype=9), dict(), {}, cc.CC_ERR_DTYPE),
+    (dict(), dict(), dict(page_size=24), cc.CC_ERR_ARG),
+    (dict(), dict(), dict(page_size=8), cc.CC_ERR_ARG),
+    (dict(), dict(), dict(block_table=None), cc.CC_ERR_ARG),
+    (dict(), dict(), dict(tok_stride=64), cc.CC_ERR_SHAPE),
+    (dict(), dict(), dict(k=P + 1), cc.CC_ERR_ARG),
+    (dict(), dict(), dict(max_pages=0), cc.CC_ERR_SHAPE),
+]
+BAD_KV8 = [
+    (dict(k_scale=None), cc.CC_ERR_ARG),
+    (dict(scale_block=8), cc.CC_ERR_UNSUPPORTED),
+    (dict(scale_block=48), cc.CC_ERR_UNSUPPORTED),
+    (dict(scale_block=256), cc.CC_ERR_UNSUPPORTED),
+    (dict(scale_block=32), cc.CC_ERR_SHAPE),          # longer than a page of 16
+    (dict(scale_page_stride=-1), cc.CC_ERR_SHAPE),
+    (dict(scale_head_stride=-1), cc.CC_ERR_SHAPE),
+    (dict(tok_stride=136), cc.CC_ERR_UNSUPPORTED),    # rows 16 bytes aligned
+    (dict(page_stride=1 << 32), cc.CC_ERR_UNSUPPORTED),
+]
+
+
+def _ref(x):
+    return ctypes.byref(x)
+
+
+@pytest.mark.parametrize("n", range(len(BAD_APPEND)))
+def test_append_refuses(n):
+    pk, ak, kk, want = BAD_APPEND[n]
+    a, p = _append(**ak), _problem(**pk)
+    assert cc._lib.cc_append_kv8(_ref(p), _ref(a), _ref(_kv8(**kk)), None) == want
+    if "tok_stride" not in kk:
+        kv = _kv(**{**dict(tok_stride=128), **kk})
+        assert cc._lib.cc_append_kv(_ref(p), _ref(a), _ref(kv), None) == want
+
+
+def test_append_refuses_more():
+    f8, f16 = cc._lib.cc_append_kv8, cc._lib.cc_append_kv
+    p, a = _problem(), _append()
+    assert f8(None, _ref(a), _ref(_kv8()), None) == cc.CC_ERR_ARG
+    assert f8(_ref(p), None, _ref(_kv8()), None) == cc.CC_ERR_ARG
+    assert f8(_ref(p), _ref(a), None, None) == cc.CC_ERR_ARG
+    assert f16(_ref(p), _ref(a), None, None) == cc.CC_ERR_ARG
+    # a contiguous cache needs its capacity said
+    assert f8(_ref(p), _ref(a), _ref(_kv8(paged=False)), None) == cc.CC_ERR_ARG
+    assert f16(_ref(p), _ref(a), _ref(_kv(paged=False)), None) == cc.CC_ERR_ARG
+    # nothing to append: fine, whatever the rows
+    empty = _problem((0, 0, 0))
+    assert f8(_ref(empty), _ref(_append(k=cc.c_rows(), cached=None)), _ref(_kv8()), None) == cc.CC_OK
+
+
+@pytest.mark.parametrize("n", range(len(BAD_KV8)))
+def test_bad_8bit_caches(n):
+    kw, want = BAD_KV8[n]
+    kv, p, size = _kv8(**kw), _problem(), ctypes.c_size_t()
+    assert cc._lib.cc_append_kv8(_ref(p), _ref(_append()), _ref(kv), None) == want
+    k = (ctypes.c_int32 * 2)(1, 1)
+    assert cc._lib.cc_compact_kv8(_ref(p), _ref(kv), P, k, 0, None, None, None, None) == want
+    assert cc._lib.cc_compact_kv8(_ref(p), _ref(_kv8()), P, k, 0, None, None, _ref(kv), None) == want
+    assert cc._lib.cc_attention_kv8(_ref(p), P, _ref(kv), 0, 0, P, 100, P, P, 1 << 30, None) == want
+
+
+def test_compact_refuses():
+    f, p = cc._lib.cc_compact_kv8, _problem()
+    k = lambda *x: (ctypes.c_int32 * len(x))(*x)
+    kv = _kv8()
+    assert f(_ref(p), _ref(kv), P, None, 0, None, None, None, None) == cc.CC_ERR_ARG
+    assert f(_ref(p), _ref(kv), P, k(1, 1), 2, None, None, None, None) == cc.CC_ERR_ARG
+    assert f(_ref(p), _ref(kv), P, k(4, 1), 0, None, None, None, None) == cc.CC_ERR_SHAPE      # of 3
+    assert f(_ref(p), _ref(kv), P, k(-1, 1), 0, None, None, None, None) == cc.CC_ERR_SHAPE
+    assert f(_ref(p), _ref(kv), None, k(1, 1), 0, None, None, None, None) == cc.CC_ERR_ARG
+    assert f(_ref(p), _ref(kv), P, k(1, 1), 0, None, None, _ref(_kv8(paged=False)), None) == cc.CC_ERR_ARG
+    assert f(_ref(p), _ref(_kv8(page_size=32)), P, k(1, 1), 0, None, None, _ref(_kv8(page_size=32, scale_block=32)), None) == cc.CC_ERR_ARG
+    assert f(_ref(p), _ref(kv), P, k(1, 1), 0, None, None, _ref(_kv8(n_layers=1)), None) == cc.CC_ERR_SHAPE
+    assert f(_ref(p), _ref(_kv8(max_pages=0)), P, k(1, 1), 0, None, None, None, None) == cc.CC_ERR_SHAPE
+    many = _problem(n_heads_q=130, n_heads_kv=65)
+    assert f(_ref(many), _ref(kv), P, k(*[1] * 130), 1, None, None, None, None) == cc.CC_ERR_UNSUPPORTED
+    assert f(_ref(p), _ref(kv), None, k(0, 0), 0, None, None, None, None) == cc.CC_OK
+
+
+def test_attention_refuses():
+    f, q = cc._lib.cc_attention_kv8, cc._lib.cc_attention_kv8_workspace
+    p, kv, n = _problem(), _kv8(), ctypes.c_size_t()
+    ok = [_ref(p), P, _ref(kv), 0, 0, P, 1000, P, P, 1 << 30, None]
+
+    def call(i, x):
+        return f(*[x if j == i else y for j, y in enumerate(ok)])
+
+    assert call(1, None) == call(5, None) == call(7, None) == call(1, P + 8) == call(7, P + 2) == cc.CC_ERR_ARG
+    assert call(3, -1) == call(3, 2) == call(4, 2) == call(4, -1) == cc.CC_ERR_ARG
+    assert call(6, -1) == cc.CC_ERR_SHAPE
+    assert call(6, 1025) == cc.CC_ERR_SHAPE            # 64 pages of 16
+    assert call(6, 2 ** 31 - 1) == cc.CC_ERR_SHAPE
+    assert call(0, _ref(_problem(dtype=cc.CC_F32))) == cc.CC_ERR_UNSUPPORTED
+    assert call(0, _ref(_problem(head_dim=256))) == cc.CC_ERR_UNSUPPORTED
+    wide = _kv8(max_pages=1 << 20)
+    assert q(_ref(p), 0, 100000, _ref(n)) == cc.CC_OK and n.value > 0
+    assert f(_ref(p), P, _ref(wide), 0, 0, P, 100000, P, P, n.value - 1, None) == cc.CC_ERR_WORKSPACE
+    assert f(_ref(p), P, _ref(wide), 0, 0, P, 100000, P, None, n.value, None) == cc.CC_ERR_ARG
+    assert f(_ref(p), P, _ref(wide), 0, 0, P, 100000, P, P + 16, n.value, None) == cc.CC_ERR_ARG
+    assert q(_ref(p), 0, 100, None) == cc.CC_ERR_ARG
+    assert q(_ref(p), 5, 100, _ref(n)) == cc.CC_ERR_ARG
+    assert q(_ref(p), 0, -1, _ref(n)) == cc.CC_ERR_SHAPE
+    empty = _problem((0, 0))
+    assert f(_ref(empty), None, _ref(kv), 0, 0, None, 0, None, None, 0, None) == cc.CC_OK
+
+
+def test_workspace_is_bounded():
+    """Partial results do not grow with the product of lengths and sequences."""
+    n = ctypes.c_size_t()
+    big = _problem([0] + list(range(1, 4097)), n_heads_q=32, n_heads_kv=8)
+    assert cc._lib.cc_attention_kv8_workspace(_ref(big), 0, 1 << 20, _ref(n)) == cc.CC_OK
+    assert n.value < 1 << 28
+    long = _problem([0, 1 << 20], n_heads_q=32, n_heads_kv=8)
+    assert cc._lib.cc_attention_kv8_workspace(_ref(long), 0, 1 << 20, _ref(n)) == cc.CC_OK and n.value == 0
+
+
+def test_logprobs_refuses():
+    f, q, n = cc._lib.cc_lmhead_logprobs, cc._lib.cc_lmhead_logprobs_workspace, ctypes.c_size_t()
+    ok = [cc.CC_BF16, P, P, 0, 4, 1000, 128, P, 5, P, P, P, P, P, 1 << 30, None]
+
+    def call(i, x):
+        return f(*[x if j == i else y for j, y in enumerate(ok)])
+
+    assert call(0, cc.CC_F32) == cc.CC_ERR_UNSUPPORTED and call(0, 7) == cc.CC_ERR_DTYPE
+    assert call(1, None) == call(2, None) == call(1, P + 2) == call(2, P + 8) == cc.CC_ERR_ARG
+    assert call(3, 2) == cc.CC_ERR_ARG
+    assert call(4, -1) == call(5, 0) == call(6, 0) == cc.CC_ERR_SHAPE
+    assert call(6, 100) == cc.CC_ERR_UNSUPPORTED
+    assert call(7, None) == call(9, None) == cc.CC_ERR_ARG     # ids and logprob go together
+    assert call(8, -1) == call(8, 33) == cc.CC_ERR_ARG
+    assert f(*[3 if j == 5 else y for j, y in enumerate(ok)]) == cc.CC_ERR_ARG   # 5 of 3 words
+    assert call(11, None) == call(12, None) == cc.CC_ERR_ARG
+    assert call(14, 16) == cc.CC_ERR_WORKSPACE
+    assert call(13, None) == call(13, P + 64) == cc.CC_ERR_ARG
+    assert f(*[0 if j == 4 else y for j, y in enumerate(ok)]) == cc.CC_OK
+    assert q(cc.CC_BF16, 4, 1000, 128, 5, None) == cc.CC_ERR_ARG
+    assert q(cc.CC_BF16, 100000, 128256, 4096, 32, _ref(n)) == cc.CC_OK
+    assert n.value < 3 << 30          # rows are taken in slabs
+
+
+def test_binding_refuses():
+    p = cc.problem(dtype="bf16", cu_seqlens=[0, 2], n_heads_q=4, n_heads_kv=2, head_dim=64, hidden=64, vocab=1, rope_theta=1e4,
+                   device="cpu")
+    z = lambda *s, t=torch.bfloat16: torch.zeros(*s, dtype=t)
+    codes, sc = z(1, 2, 32, 64, t=torch.uint8), z(1, 2, 2, t=torch.uint8)
+    kw = dict(n_layers=1, layer_stride=4096, head_stride=2048, tok_stride=64, scale_block=16, scale_layer_stride=4,
+              scale_head_stride=2)
+    kv = cc.kv8_contiguous(codes, codes, sc, sc, **kw)
+    with pytest.raises(ValueError, match="bytes"):
+        cc.kv8_contiguous(z(1, 2, 32, 64), codes, sc, sc, **kw)
+    k, lens = z(2, 2, 64), torch.zeros(1, dtype=torch.int32)
+    ok = dict(capacity=32)
+    with pytest.raises(ValueError, match="GPU"):
+        cc.cc_append_kv8(p, kv, k, k, lens, **ok)
+    with pytest.raises(ValueError, match="shape"):
+        cc.cc_append_kv8(p, kv, z(3, 2, 64), k, lens, **ok)
+    with pytest.raises(ValueError, match="float32"):
+        cc.cc_append_kv8(p, kv, k, z(2, 2, 64, t=torch.float32), lens, **ok)
+    with pytest.raises(ValueError, match="contiguous"):
+        cc.cc_append_kv8(p, kv, z(2, 64, 2).transpose(1, 2), k, lens, **ok)
+    with pytest.raises(ValueError, match="cached"):
+        cc.cc_append_kv8(p, kv, k, k, lens.long(), **ok)
+    with pytest.raises(ValueError, match="pos_ids"):
+        cc.cc_append_kv8(p, kv, k, k, lens, pos_ids=torch.zeros(3, dtype=torch.int32), **ok)
+    with pytest.raises(ValueError, match="q_out"):
+        cc.cc_append_kv8(p, kv, k, k, lens, q=z(2, 4, 64), q_out=z(2, 4, 32), **ok)
+    with pytest.raises(ValueError, match="kv_lens"):
+        cc.cc_attention_kv8(p, z(2, 4, 64), kv, 0, torch.zeros(2, dtype=torch.int32), 10)
+    with pytest.raises(ValueError, match="q must"):
+        cc.cc_attention_kv8(p, z(3, 4, 64), kv, 0, lens, 10)
+    with pytest.raises(ValueError, match="GPU"):
+        cc.cc_attention_kv8(p, z(2, 4, 64), kv, 0, lens, 10)
+    with pytest.raises(KeyError):
+        cc.cc_attention_kv8_workspace(p, "both", 10)
+    with pytest.raises(ValueError, match="budgets"):
+        cc.cc_compact_kv8(p, kv, lens, [1, 1], 0)
+    u, w = z(2, 64), z(10, 64)
+    with pytest.raises(ValueError, match="w_lm"):
+        cc.cc_lmhead_logprobs("bf16", u, w, 11, None, 1)
+    with pytest.raises(ValueError, match="ids"):
+        cc.cc_lmhead_logprobs("bf16", u, w, 10, torch.zeros(3, dtype=torch.int32), 1)
+    with pytest.raises(ValueError, match="room"):
+        cc.cc_lmhead_logprobs("bf16", u, w, 10, None, 3, cc.logprobs_out(2, 1, "cpu"))
+    with pytest.raises(ValueError, match="packed"):
+        cc.cc_lmhead_logprobs("bf16", u, w, 1000, None, 1, packed=True)
