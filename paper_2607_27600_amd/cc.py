@@ -609,12 +609,16 @@ def _rows(r: c_rows, t: torch.Tensor, dtype: torch.dtype, what: str, want: tuple
 
 def _on_gpu(*tensors) -> None:
     """Kernels run on the current device: tensors elsewhere would be read there by address."""
+    here = None
     for t in tensors:
-        if t is not None and not t.is_cuda:
-            raise ValueError(f"tensors must be on the GPU, got one on {t.device}")
-    t = next(x for x in tensors if x is not None)
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+        if t is not None:
+            if not t.is_cuda:
+                raise ValueError(f"tensors must be on the GPU, got one on {t.device}")
+            if here is not None and t.get_device() != here:
+                raise ValueError("tensors on different devices")
+            here = t.get_device()
+    if here != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors are on cuda:{here}, the current device is cuda:{torch._C._cuda_getDevice()}")
 
 
 def _int32(t: Optional[torch.Tensor], n: int, what: str) -> None:

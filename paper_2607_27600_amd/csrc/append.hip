@@ -13,8 +13,10 @@
 // so a block whose scale grows with a later token keeps its entries exactly, but for codes that
 // fall below the normal range, and products with scales are exact wherever they are taken.
 //
-// Bound by memory for chunks of a prompt and by two dependent round trips (lengths, then rows) for
-// single tokens; a row is read 16 bytes a lane, 16 elements a lane (e .. e + 7 and their partners).
+// Bound by memory for chunks of a prompt (8192 tokens, 32 heads on 8, into 8 bits: 185 MB in 44 us, 4.2 TB/s;
+// 3166 ragged tokens into bf16 pages: 78 MB in 15.8 us, 4.9 TB/s, what a large copy reaches) and by the
+// round trips to lengths, then rows, for single tokens (eight: 6.2 us); a row is read 16 elements a lane
+// (e .. e + 7 and their partners), 16 bytes a load.
 #include <cmath>
 
 #include "cc_internal.h"
@@ -335,8 +337,10 @@ hipError_t launch_typed(const AppendLaunch& l, hipStream_t s) {
   a.units_kv = int(kv);
   a.units_q = int(q);
   a.units = int(kv + q);
-  if (l.rotate)
-    for (int e = 0; e < HD / 2; ++e) a.freq[e] = std::exp(-2.0 * e / HD * std::log(l.theta)) / 6.283185307179586476925;
+  if (l.rotate) {
+    const double step = -2.0 / HD * std::log(l.theta);
+    for (int e = 0; e < HD / 2; ++e) a.freq[e] = std::exp(e * step) / 6.283185307179586476925;
+  }
   const int most = a.each >= 0 ? std::min(B, a.each) : B;
   const size_t lds = l.rotate ? size_t(std::max(most, QT)) * (HD / 2) * sizeof(float2) : 0;
   hipLaunchKernelGGL((append_kernel<T, HD, F8>), dim3(unsigned(a.units * l.n_layers)), dim3(NT), lds, s, a);
