@@ -607,6 +607,15 @@ def _rows(r: c_rows, t: torch.Tensor, dtype: torch.dtype, what: str, want: tuple
     r.layer_stride = st[0] if len(st) == 4 else 0
 
 
+def _empty(shape, dtype: torch.dtype, device, stream=None) -> torch.Tensor:
+    """torch.empty for a call on `stream`: the memory is that stream's, so neither what the current stream
+    still does with a block it has freed nor what it is given after this one's release can meet the call."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _on_gpu(*tensors) -> None:
     """Kernels run on the current device: tensors elsewhere would be read there by address."""
     here = None
@@ -617,7 +626,7 @@ def _on_gpu(*tensors) -> None:
             if here is not None and t.get_device() != here:
                 raise ValueError("tensors on different devices")
             here = t.get_device()
-    if here != torch._C._cuda_getDevice():
+    if here is not None and here != torch._C._cuda_getDevice():
         raise ValueError(f"tensors are on cuda:{here}, the current device is cuda:{torch._C._cuda_getDevice()}")
 
 
@@ -642,7 +651,7 @@ def _append(fn, p: Problem, kv, k, v, cached, capacity, layer, n_layers, pos_ids
         hq = s.n_heads_q
         _rows(a.q, q, dtype, "q", (M, hq, d))
         if q_out is None:
-            q_out = torch.empty((M, hq, d), dtype=dtype, device=q.device)
+            q_out = _empty((M, hq, d), dtype, q.device, stream)
         elif q_out.dtype != dtype or q_out.numel() != M * hq * d or not q_out.is_contiguous():
             raise ValueError("q_out must be contiguous rows of q's type and size")
         a.q_out = q_out.data_ptr()
@@ -706,12 +715,12 @@ def cc_attention_kv8(p: Problem, q: torch.Tensor, kv: KV8, layer: int, kv_lens: 
             or not q.is_contiguous()):
         raise ValueError("q must be contiguous bf16 rows [N][Hq][head_dim]")
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty(q.shape, q.dtype, q.device, stream)
     elif o.dtype != q.dtype or o.numel() != q.numel() or not o.is_contiguous():
         raise ValueError("o must be contiguous and of q's type and size")
     _on_gpu(q, o, kv_lens, workspace)
     if workspace is None:
-        workspace = _workspace(cc_attention_kv8_workspace(p, mask, max_kv_len), p.device)
+        workspace = _empty(max(1, cc_attention_kv8_workspace(p, mask, max_kv_len)), torch.uint8, q.device, stream)
     _check(_lib.cc_attention_kv8(ctypes.byref(s), _ptr(q), ctypes.byref(kv.struct), layer, _MASKS[mask],
                                  _ptr(kv_lens), max_kv_len, _ptr(o), _ptr(workspace), workspace.numel(),
                                  _stream(stream)), "cc_attention_kv8")
@@ -728,9 +737,9 @@ class Logprobs:
     top_logprob: torch.Tensor
 
 
-def logprobs_out(n: int, top: int, device="cuda") -> Logprobs:
-    f = lambda *s: torch.empty(s, dtype=torch.float32, device=device)
-    return Logprobs(f(n), f(n), torch.empty((n, top), dtype=torch.int32, device=device), f(n, top))
+def logprobs_out(n: int, top: int, device="cuda", stream=None) -> Logprobs:
+    f = lambda *s: _empty(s, torch.float32, device, stream)
+    return Logprobs(f(n), f(n), _empty((n, top), torch.int32, device, stream), f(n, top))
 
 
 def cc_lmhead_logprobs_workspace(dtype: str, n: int, vocab: int, hidden: int, top: int) -> int:
@@ -746,17 +755,19 @@ def cc_lmhead_logprobs(dtype: str, u: torch.Tensor, w_lm: torch.Tensor, vocab: i
     _int32(ids, n, "ids")
     if not u.is_contiguous() or not w_lm.is_contiguous():
         raise ValueError("u and w_lm must be contiguous")
+    if u.dtype != torch.bfloat16 or (not packed and w_lm.dtype != torch.bfloat16):
+        raise ValueError("u and w_lm must be bf16")
     if not packed and tuple(w_lm.shape) != (vocab, hidden):
         raise ValueError(f"w_lm has shape {tuple(w_lm.shape)}, expected {(vocab, hidden)}")
     if packed and w_lm.numel() * w_lm.element_size() < cc_pack_lmhead_bytes(vocab, hidden):
         raise ValueError("w_lm holds less than a packed weight of that size")
     if out is None:
-        out = logprobs_out(n, top, u.device)
+        out = logprobs_out(n, top, u.device, stream)
     if out.top_ids.numel() < n * top or out.top_logprob.numel() < n * top:
         raise ValueError(f"out has no room for {top} alternatives of {n} rows")
     _on_gpu(u, w_lm, ids, out.entropy, workspace)
     if workspace is None:
-        workspace = _workspace(cc_lmhead_logprobs_workspace(dtype, n, vocab, hidden, top), u.device)
+        workspace = _empty(max(1, cc_lmhead_logprobs_workspace(dtype, n, vocab, hidden, top)), torch.uint8, u.device, stream)
     _check(_lib.cc_lmhead_logprobs({"f32": CC_F32, "bf16": CC_BF16}[dtype], _ptr(u), _ptr(w_lm), int(packed), n,
                                    vocab, hidden, _ptr(ids), top, _ptr(out.logprob) if ids is not None else None,
                                    _ptr(out.entropy), _ptr(out.top_ids) if top else None,

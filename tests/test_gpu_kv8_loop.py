@@ -200,3 +200,33 @@ def test_decode_step_of_a_batch_in_a_graph():
         lp = O.logprobs(f64(u), f64(w_lm), np.arange(B), 5)
         np.testing.assert_allclose(f64(out.logprob), lp["logprob"], rtol=0, atol=3e-5)
         np.testing.assert_allclose(f64(out.top_logprob), lp["top_logprob"], rtol=0, atol=3e-5)
+
+
+def test_calls_on_another_stream():
+    """Every operator on a stream that is not the current one, with memory that the call allocates."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d, new, cached = 4, 2, 128, [3, 40], [20, 9]
+    caches = [Cache8(cached, hkv, d, page=16, block=16, seed=51, room=50) for _ in range(2)]
+    g = torch.Generator().manual_seed(52)
+    qkv = torch.randn(43, hq + 2 * hkv, d, generator=g).to(torch.bfloat16).cuda()
+    u, w = torch.randn(70, 128, generator=g).to(torch.bfloat16).cuda(), torch.randn(20000, 128, generator=g).to(torch.bfloat16).cuda()
+    ids = torch.arange(70, dtype=torch.int32, device="cuda")
+    p = cc.problem(dtype="bf16", cu_seqlens=cu_of(new), n_heads_q=hq, n_heads_kv=hkv, head_dim=d, hidden=64, vocab=1,
+                   rope_theta=1e4)
+    whole = cc.problem(dtype="bf16", cu_seqlens=cu_of([23, 49]), n_heads_q=hq, n_heads_kv=hkv, head_dim=d, hidden=64, vocab=1)
+    lens, after = i32(cached), i32([23, 49])
+    keep = i32([0, 5, 22, 1, 2, 48])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for cache, stream in zip(caches, (None, side)):
+        kv = cache.view(cc)
+        q, k, v = qkv.split([hq, hkv, hkv], 1)
+        q2 = cc.cc_append_kv8(p, kv, k, v, lens, q=q, stream=stream)
+        o = cc.cc_attention_kv8(p, q2, kv, 0, after, 60, stream=stream)
+        lp = cc.cc_lmhead_logprobs("bf16", u, w, 20000, ids, 7, stream=stream)
+        cc.cc_compact_kv8(whole, kv, keep, [3, 3], 0, stream=stream)
+        torch.cuda.synchronize()
+        got.append((q2, o, lp.logprob, lp.entropy, lp.top_ids, lp.top_logprob, *cache.t.values()))
+    for a, b in zip(*got):
+        assert torch.equal(a.view(torch.uint8) if a.dtype == torch.bfloat16 else a, b.view(torch.uint8) if b.dtype == torch.bfloat16 else b)

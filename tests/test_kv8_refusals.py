@@ -269,3 +269,22 @@ def test_binding_refuses():
         cc.cc_lmhead_logprobs("bf16", u, w, 10, None, 3, cc.logprobs_out(2, 1, "cpu"))
     with pytest.raises(ValueError, match="packed"):
         cc.cc_lmhead_logprobs("bf16", u, w, 1000, None, 1, packed=True)
+
+
+def test_struct_layouts_match_the_header(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    classes = {"cc_kv8": cc.c_kv8, "cc_rows": cc.c_rows, "cc_append": cc.c_append}
+    lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "cc.h"', "int main(void){"]
+    for n, c in classes.items():
+        lines.append(f'printf("%zu\\n", sizeof({n}));')
+        lines += [f'printf("%zu\\n", offsetof({n}, {f[0]}));' for f in c._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text("\n".join(lines + ["return 0;}"]))
+    subprocess.run(["gcc", "-I", os.path.join(root, "include"), str(src), "-o", str(tmp_path / "layout")], check=True)
+    got = subprocess.run([str(tmp_path / "layout")], capture_output=True, text=True, check=True).stdout.split()
+    want = []
+    for c in classes.values():
+        want += [ctypes.sizeof(c)] + [getattr(c, f[0]).offset for f in c._fields_]
+    assert [int(x) for x in got] == want
