@@ -199,7 +199,9 @@ __global__ __launch_bounds__(NT) void compact8_kernel(Args a) {
       if (j < k) {
         const uint32_t e = e8m0_of(top[r >> shift]);
         uint4 w = now.w[u];
-        if (e != now.sc[u]) w = rescale(w, e8m0_scale(now.sc[u]) * e8m0_inverse(e));
+        // (a scale more than 2^18 larger than the block's belongs to zeros and NaN alone; up to 2^220 it may be,
+        // past fp32, and infinity is no scale)
+        if (e != now.sc[u]) w = rescale(w, fminf(e8m0_scale(now.sc[u]) * e8m0_inverse(e), 0x1p100f));
         const int slot = dv.paged ? j & dv.codes.page_mask : j;
         *reinterpret_cast<uint4*>(db + int64_t(dpage[u]) * dv.codes.page_stride + int64_t(slot) * dv.codes.tok_stride) = w;
         if (col == 0 && (r & ((1 << shift) - 1)) == 0) ds[int64_t(dpage[u]) * dv.s_page + (slot >> shift)] = uint8_t(e);

@@ -110,3 +110,62 @@ def test_nan_codes_and_extreme_scales():
     np.testing.assert_array_equal((gc & 0x7f) == 0x7f, nan)
     np.testing.assert_array_equal(gc[~nan], want[~nan])
     np.testing.assert_array_equal(gs, ws)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_zeros_kept_from_blocks_of_large_scales(d):
+    """All that stays of blocks with scales up to 2^120 are zeros and NaN: the new scale is the smallest,
+    2^220 below, and zeros stay zeros."""
+    from paper_2607_27600_amd import cc
+    c = Cache8([64], 1, d, block=16, seed=18)
+    codes, sc = c.plane(0, 0, 0, "v", n=64)
+    sc[:] = [247, 160, 230, 155]
+    codes[0:64:2] = 0
+    codes[6], codes[34, 5] = 0x80, 0x7f
+    c.put(0, 0, 0, "v", codes, sc)
+    c.t["v"].copy_(torch.from_numpy(c.host["v"]))
+    c.t["vs"].copy_(torch.from_numpy(c.host["vs"]))
+    kl = np.arange(0, 64, 2, dtype=np.int32)
+    p = cc.problem(dtype="bf16", cu_seqlens=[0, 64], n_heads_q=1, n_heads_kv=1, head_dim=d, hidden=64, vocab=1)
+    cc.cc_compact_kv8(p, c.view(cc), torch.from_numpy(kl).cuda(), [len(kl)], 0)
+    torch.cuda.synchronize()
+    gc, gs = c.plane(0, 0, 0, "v", src=c.read(), n=len(kl))
+    np.testing.assert_array_equal(gs, [27, 27])
+    nan = np.zeros(gc.shape, bool)
+    nan[17, 5] = True
+    np.testing.assert_array_equal((gc & 0x7f) == 0x7f, nan)
+    assert np.all((gc[~nan] & 0x7f) == 0)
+
+
+def test_two_graphs_and_an_eager_call_in_turn():
+    """Calls captured in two graphs, replayed in turn with an eager call between them."""
+    from paper_2607_27600_amd import cc
+    r = np.random.default_rng(21)
+    lens, kept, hkv, d = [300, 70], [120, 41], 2, 128
+    c = Cache8(lens, hkv, d, layers=2, page=16, block=16, seed=22)
+    outs = [Cache8(lens, hkv, d, layers=2, page=16, block=16, seed=23) for _ in range(3)]
+    p = cc.problem(dtype="bf16", cu_seqlens=cu_of(lens), n_heads_q=hkv, n_heads_kv=hkv, head_dim=d, hidden=64, vocab=1)
+    lists = [[np.sort(r.permutation(n)[:k]).astype(np.int32) for n, k in zip(lens, kept)] for _ in range(2)]
+    keeps = [torch.from_numpy(np.concatenate(x)).cuda() for x in lists]
+    src = c.view(cc)
+    graphs = []
+    for keep, out in zip(keeps, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            cc.cc_compact_kv8(p, src, keep, kept, 0, out=out.view(cc))
+        graphs.append(g)
+    for _ in range(3):
+        for o in outs:
+            for t in ("k", "v", "ks", "vs"):
+                o.t[t].copy_(torch.from_numpy(o.host[t]))
+        graphs[0].replay()
+        cc.cc_compact_kv8(p, src, keeps[1], kept, 0, out=outs[2].view(cc))
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for o, ll in zip(outs, (lists[0], lists[1], lists[1])):
+            after = o.read()
+            for b, kl in enumerate(ll):
+                codes, sc = O8.compact(*c.plane(1, b, 1, "v", n=lens[b]), kl, 16)
+                gc, gs = o.plane(1, b, 1, "v", src=after, n=len(kl))
+                np.testing.assert_array_equal(gc, codes)
+                np.testing.assert_array_equal(gs, sc)
