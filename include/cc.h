@@ -486,7 +486,8 @@ cc_status cc_lmhead_logprobs_workspace(int32_t dtype, int32_t n, int32_t vocab, 
  * u [n][hidden] and w_lm [vocab][hidden] bf16 (packed = 1: w_lm in the layout of
  * cc_pack_lmhead), hidden a multiple of 64, fp32 accumulation.  0 <= top <= min(vocab,
  * CC_LOGPROBS_MAX_TOP).  logprob and ids (both or neither), entropy, and with top = 0 the top
- * arrays may be NULL.  The [n][vocab] logits are never materialised.  A NaN logit ranks below every
+ * arrays may be NULL.  An id outside [0, vocab), as in the rows that pad a batch, gives a NaN
+ * log-probability.  The [n][vocab] logits are never materialised.  A NaN logit ranks below every
  * other (the row's log-probabilities and entropy are then NaN). */
 cc_status cc_lmhead_logprobs(int32_t dtype, const void* u, const void* w_lm, int32_t packed, int32_t n,
                              int32_t vocab, int32_t hidden, const int32_t* ids, int32_t top,

@@ -141,7 +141,7 @@ struct EpiLogprobs {
     for (int b = 0; b < NB; ++b)   // read ahead of the sums, which hide it
       bound[b] = tb.bound ? load_shared(tb.bound + min(n0w + b * 16 + c16, g.N - 1)) : 0u;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) rt[b] = ids ? ids[min(n0w + b * 16 + c16, g.N - 1)] - m0w : -1;
+    for (int b = 0; b < NB; ++b) rt[b] = ids ? int(uint32_t(ids[min(n0w + b * 16 + c16, g.N - 1)]) - uint32_t(m0w)) : -1;
     float mx[NB], sm[NB], tt[NB], zmax[NB];
     if (rows >= 16 * MB)
       sums<false>(acc, rows, grp, mx, sm, tt, zmax);
@@ -292,6 +292,8 @@ __global__ __launch_bounds__(256) void clear_kernel(uint32_t* p, int n) {
 
 struct JoinArgs {
   Tables tb;
+  const int32_t* ids;
+  int V;
   int tiles, top;
   int falling;       // candidates are listed the largest first
   float *logprob, *entropy, *top_logprob;
@@ -322,7 +324,9 @@ __global__ __launch_bounds__(64) void logprobs_join(JoinArgs a) {
   if (lane == 0) {
     // log P <= 0 and entropy >= 0: rounding may take either a few ulps past
     if (a.logprob) {
-      const float d = tb.target[n] - lse;
+      // (no tile has written the logit of a word that is not there)
+      const bool there = uint32_t(a.ids[n]) < uint32_t(a.V);
+      const float d = there ? tb.target[n] - lse : __uint_as_float(0x7fc00000u);
       a.logprob[n] = d > 0.f ? 0.f : d;
     }
     if (a.entropy) {
@@ -467,6 +471,8 @@ hipError_t launch_logprobs(const LogprobsLaunch& l, hipStream_t s) {
     if (err != hipSuccess) return err;
     JoinArgs j;
     j.tb = tb;
+    j.ids = ids;
+    j.V = l.V;
     j.tiles = tiles;
     j.top = l.top;
     j.falling = !bound;

@@ -152,3 +152,53 @@ def test_repeats_bit_for_bit_and_in_a_graph():
         torch.cuda.synchronize()
         for x, y in zip((a.logprob, a.entropy, a.top_ids, a.top_logprob), (b.logprob, b.entropy, b.top_ids, b.top_logprob)):
             assert torch.equal(x, y)
+
+
+def test_ids_outside_the_vocabulary():
+    """Rows of a padded batch (ids below 0 or at and past the vocabulary): NaN, whatever the workspace
+    holds; their entropy and alternatives and the other rows stand."""
+    from paper_2607_27600_amd import cc
+    n, D, V = 70, 64, 1001
+    u, w, ids = _grid(n, D, V, 14)
+    bad = {0: -1, 5: -100, 17: V, 30: V + 1, 44: 1023, 51: 1024, 63: 2**31 - 1, 69: -2**31}
+    for i, x in bad.items():
+        ids[i] = x
+    ws = torch.zeros(cc.cc_lmhead_logprobs_workspace("bf16", n, V, D, 3), dtype=torch.uint8, device="cuda")
+    r = cc.cc_lmhead_logprobs("bf16", u.cuda(), w.cuda(), V, ids.cuda(), 3, workspace=ws)
+    torch.cuda.synchronize()
+    inside = [i for i in range(n) if i not in bad]
+    clean = ids.clone()
+    clean[list(bad)] = 0
+    want = O.logprobs(f64(u), f64(w), clean.numpy(), 3)
+    assert torch.isnan(r.logprob[list(bad)]).all()
+    np.testing.assert_allclose(f64(r.logprob)[inside], want["logprob"][inside], rtol=0, atol=TOL)
+    np.testing.assert_allclose(f64(r.entropy), want["entropy"], rtol=0, atol=TOL_H)
+    np.testing.assert_array_equal(r.top_ids.cpu().numpy(), want["top_ids"])
+
+
+def test_two_graphs_share_a_workspace():
+    """Calls captured in two graphs that use one workspace in turn, with an eager call between them."""
+    from paper_2607_27600_amd import cc
+    n, D, V, top = 150, 128, 70000, 6
+    sets = [tuple(x.cuda() for x in _grid(n, D, V, s)) for s in (15, 16)]
+    want = [cc.cc_lmhead_logprobs("bf16", u, w, V, ids, top) for u, w, ids in sets]
+    ws = torch.empty(cc.cc_lmhead_logprobs_workspace("bf16", n, V, D, top), dtype=torch.uint8, device="cuda")
+    outs = [cc.logprobs_out(n, top) for _ in range(3)]
+    torch.cuda.synchronize()
+    graphs = []
+    for (u, w, ids), out in zip(sets, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            cc.cc_lmhead_logprobs("bf16", u, w, V, ids, top, out, workspace=ws)
+        graphs.append(g)
+    for _ in range(3):
+        for o in outs:
+            for t in (o.logprob, o.entropy, o.top_ids, o.top_logprob):
+                t.zero_()
+        graphs[0].replay()
+        cc.cc_lmhead_logprobs("bf16", *sets[1][:2], V, sets[1][2], top, outs[2], workspace=ws)
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for o, x in zip(outs, (want[0], want[1], want[1])):
+            for t in ("logprob", "entropy", "top_ids", "top_logprob"):
+                assert torch.equal(getattr(o, t), getattr(x, t)), t
