@@ -192,3 +192,95 @@ def test_sequences_beyond_the_listed_ones():
     q = _q(new, hq, d, 36)
     o = _run(cc, cache, q, new, lens, hq, hkv, "causal")
     assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, "causal"))
+
+
+def test_two_graphs_share_a_workspace():
+    """Calls of both kernels captured in two graphs that use one workspace in turn, an eager call between."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d, lens = 8, 2, 128, [3000, 1500]
+    cache = Cache8(lens, hkv, d, page=64, block=32, seed=41)
+    kv, ld = cache.view(cc), i32(lens)
+    calls = []
+    for new in ([1, 2], [3, 40]):
+        calls.append((_problem(cc, new, hq, hkv, d), _q(new, hq, d, 42 + new[0])))
+    size = max(cc.cc_attention_kv8_workspace(p, "causal", 3000) for p, _ in calls)
+    assert size > 0
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    want = [cc.cc_attention_kv8(p, q, kv, 0, ld, 3000) for p, q in calls]
+    outs = [torch.empty_like(q) for _, q in (*calls, calls[1])]
+    torch.cuda.synchronize()
+    graphs = []
+    for (p, q), o in zip(calls, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            cc.cc_attention_kv8(p, q, kv, 0, ld, 3000, o, workspace=ws)
+        graphs.append(g)
+    for i in range(3):
+        for o in outs:
+            o.fill_(5.0)
+        ws.fill_(0x7f + i)
+        graphs[0].replay()
+        cc.cc_attention_kv8(*calls[1], kv, 0, ld, 3000, outs[2], workspace=ws)
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for o, x in zip(outs, (want[0], want[1], want[1])):
+            assert torch.equal(o, x)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_offsets_past_32_bits(new):
+    """Entries 64 KiB apart: appended, attended to and compacted beyond 4 GiB of their plane."""
+    from paper_2607_27600_amd import cc
+    from tests.kv8_util import quantize
+    n, d, hq, block, tok = 70000, 64, 4, 16, 1 << 16
+    free, _ = torch.cuda.mem_get_info()
+    if free < (12 << 30):
+        pytest.skip("needs 12 GiB of device memory")
+    r = np.random.default_rng(44)
+    pools = {t: torch.zeros(n * tok, dtype=torch.uint8, device="cuda") for t in ("k", "v")}
+    scales = {t: torch.full((-(-n // block),), 27, dtype=torch.uint8, device="cuda") for t in ("k", "v")}
+    rows = {t: x.view(n, tok)[:, :d] for t, x in pools.items()}
+    kv = cc.kv8_contiguous(pools["k"], pools["v"], scales["k"], scales["v"], n_layers=1, layer_stride=0, head_stride=0,
+                           tok_stride=tok, scale_block=block, scale_layer_stride=0, scale_head_stride=0)
+    # entries that count lie at both ends; keys of the rest are so far from the queries that they weigh nothing
+    head, tail = 48, 500
+    q = torch.randn(new, hq, d, generator=torch.Generator().manual_seed(45)).abs().to(torch.bfloat16).cuda()
+    far = np.full((n - head - tail, d), -300.0)
+    vals = {"k": np.concatenate([r.normal(0, 1, (head, d)), far]), "v": r.normal(0, 1, (n - tail, d))}
+    want = {}
+    for t, x in vals.items():
+        codes, sc = quantize(x[:head], block)
+        c2, s2 = quantize(x[head:1024], block)
+        if t == "k":
+            codes, sc = np.concatenate([codes, np.broadcast_to(c2[-1], (n - tail - head, d))]), np.concatenate(
+                [sc, np.full(-(-(n - tail) // block) - head // block, s2[-1])])
+        else:
+            codes, sc = quantize(x, block)
+        rows[t][: n - tail].copy_(torch.from_numpy(np.ascontiguousarray(codes)))
+        scales[t][: len(sc)].copy_(torch.from_numpy(sc.astype(np.uint8)))
+    p = cc.problem(dtype="bf16", cu_seqlens=[0, tail], n_heads_q=hq, n_heads_kv=1, head_dim=d, hidden=64, vocab=1)
+    g = torch.Generator().manual_seed(46)
+    add = {t: torch.randn(tail, 1, d, generator=g).to(torch.bfloat16).cuda() for t in ("k", "v")}
+    cc.cc_append_kv8(p, kv, add["k"], add["v"], i32([n - tail]), capacity=n, rotate=False)
+    torch.cuda.synchronize()
+
+    def values(t, e):   # what the cache holds
+        sv = O8.scale_value(scales[t].cpu().numpy())
+        e = np.asarray(e)
+        return O8.e4m3_decode(rows[t][torch.from_numpy(e).cuda()].cpu().numpy()) * sv[e // block][:, None]
+
+    ends = np.concatenate([np.arange(head), np.arange(n - tail, n)])
+    assert np.all(np.abs(values("k", ends[head:]) - f64(add["k"])[:, 0]) <= 2.0 ** -4 * np.abs(f64(add["k"])[:, 0]) + 2.0 ** -9)
+    pq = _problem(cc, [new], hq, 1, d)
+    o = cc.cc_attention_kv8(pq, q, kv, 0, i32([n]), n)
+    torch.cuda.synchronize()
+    k, v, qh = values("k", ends), values("v", ends), f64(q)
+    # (the last `new` entries of `ends` are the queries' own, as in the whole cache)
+    ref = np.stack([O8.attention(qh[:, h], k, v, "causal") for h in range(hq)], 1)
+    assert_attention_close(f64(o), ref)
+    keep = torch.arange(n - 64, n, dtype=torch.int32, device="cuda")
+    moved = values("v", np.arange(n - 64, n))
+    pc = cc.problem(dtype="bf16", cu_seqlens=[0, n], n_heads_q=1, n_heads_kv=1, head_dim=d, hidden=64, vocab=1)
+    cc.cc_compact_kv8(pc, kv, keep, [64], 0)
+    torch.cuda.synchronize()
+    np.testing.assert_allclose(values("v", np.arange(64)), moved, rtol=2.0 ** -4, atol=2.0 ** -9)
