@@ -1178,6 +1178,7 @@ cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv,
   CC_TRY(check_attention8(p, mask, max_kv_len));
   CC_TRY(check_kv8(p, kv, 1, max_kv_len));
   if (layer < 0 || layer >= kv->codes.n_layers) return CC_ERR_ARG;
+  if (kv->codes.tok_stride >= int64_t(1) << 28) return CC_ERR_UNSUPPORTED;   // 16 entries by 32-bit offsets
   const int N = n_tokens(p);
   if (N > 0 && (!q || !o || !kv_lens || !aligned16(q) || !aligned16(o))) return CC_ERR_ARG;
   const Kv8Class classes[2] = {kv8_class(p, max_kv_len, true), kv8_class(p, max_kv_len, false)};

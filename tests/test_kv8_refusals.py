@@ -288,3 +288,11 @@ def test_struct_layouts_match_the_header(tmp_path):
     for c in classes.values():
         want += [ctypes.sizeof(c)] + [getattr(c, f[0]).offset for f in c._fields_]
     assert [int(x) for x in got] == want
+
+
+def test_attention_refuses_rows_whose_offsets_in_a_group_pass_32_bits():
+    """Sixteen entries are addressed from one place by 32-bit offsets."""
+    f = cc._lib.cc_attention_kv8
+    lens = (P, 100, P, P, 1 << 30, None)
+    assert f(_ref(_problem()), P, _ref(_kv8(paged=False, tok_stride=1 << 28)), 0, 0, *lens) == cc.CC_ERR_UNSUPPORTED
+    assert f(_ref(_problem()), P, _ref(_kv8(paged=False, tok_stride=(1 << 40) + 128)), 0, 0, *lens) == cc.CC_ERR_UNSUPPORTED
