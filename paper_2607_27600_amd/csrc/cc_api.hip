@@ -1068,13 +1068,15 @@ cc_status cc_compact_kv8(const cc_problem* p, const cc_kv8* kv, const int32_t* k
     if (out->codes.layout != kv->codes.layout || out->scale_block != kv->scale_block) return CC_ERR_ARG;
   }
   const int hkv = p->n_heads_kv, per = per_head ? hkv : 1;
-  if (per > 64) return CC_ERR_UNSUPPORTED;   // the lists of a sequence travel with one launch
-  std::vector<CompactList> lists;
-  int max_k = 0;
+  if (per > COMPACT_INLINE) return CC_ERR_UNSUPPORTED;   // the lists of a sequence travel with one launch
   int64_t off = 0;
-  CC_TRY(compact_lists(p, k_h, per, per, false, lists, max_k, off));
-  if (off > 0 && !keep_idx) return CC_ERR_ARG;
-  if (max_k == 0) return CC_OK;
+  for (int64_t i = 0; i < int64_t(p->n_seqs) * per; ++i) {
+    const int b = int(i / per);
+    if (k_h[i] < 0 || k_h[i] > p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) return CC_ERR_SHAPE;
+    off += k_h[i];
+  }
+  if (off == 0) return CC_OK;
+  if (!keep_idx) return CC_ERR_ARG;
   const cc_kv8* dst = out ? out : kv;
   Compact8Launch c;
   c.src[0] = make_view8(kv, kv->codes.k, kv->k_scale);
@@ -1082,13 +1084,12 @@ cc_status cc_compact_kv8(const cc_problem* p, const cc_kv8* kv, const int32_t* k
   c.dst[0] = make_view8(dst, dst->codes.k, dst->k_scale);
   c.dst[1] = make_view8(dst, dst->codes.v, dst->v_scale);
   c.keep = keep_idx;
-  c.lists = lists.data();
-  c.n_lists = int(lists.size());
+  c.k_h = k_h;
+  c.n_seqs = p->n_seqs;
   c.n_layers = kv->codes.n_layers;
   c.n_heads = hkv;
   c.per_head = per_head;
   c.head_dim = p->head_dim;
-  c.max_k = max_k;
   c.in_place = out == nullptr;
   c.ids[0] = token_ids;
   c.ids[1] = pos_ids;

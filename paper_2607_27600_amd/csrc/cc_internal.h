@@ -351,9 +351,8 @@ hipError_t launch_append(const AppendLaunch& a, hipStream_t s);
 struct Compact8Launch {
   Kv8View src[2], dst[2];    // keys, values
   const int32_t* keep;
-  const CompactList* lists;  // host, sorted by falling budget
-  int n_lists;
-  int n_layers, n_heads, per_head, head_dim, max_k;
+  const int32_t* k_h;        // host: budgets of each sequence, or of each of its heads
+  int n_seqs, n_layers, n_heads, per_head, head_dim;
   bool in_place;
   int32_t* ids[2];
   const int32_t* cu_d;

@@ -23,12 +23,12 @@ namespace cc {
 namespace {
 
 constexpr int U = 4;           // 16-byte row pieces of a thread in a chunk
-constexpr int LISTS = 64;      // lists of a launch, by value
+constexpr int LISTS = COMPACT_INLINE;   // lists of a launch, by value
 
 struct Args {
   Kv8View src[2], dst[2];
   const int32_t* keep;
-  int n_lists, n_layers, n_heads, per_head;
+  int n_layers, n_heads, per_head;
   int chunks;                  // workgroups of a plane (in place: 1)
   int id_blocks;
   int32_t* ids[2];
@@ -221,8 +221,9 @@ template <int HD>
 hipError_t launch_dim(const Compact8Launch& l, hipStream_t s) {
   constexpr int NT = 256, NT_IN = 1024, CHUNK = NT / (HD / 16) * U;
   const int per = l.per_head ? l.n_heads : 1;
-  const int per_launch = LISTS / per * per;
-  for (int lo = 0; lo < l.n_lists; lo += per_launch) {
+  const int per_launch = LISTS / per;   // sequences
+  int64_t off = 0;
+  for (int lo = 0; lo < l.n_seqs; lo += per_launch) {
     Args a;
     for (int t = 0; t < 2; ++t) {
       a.src[t] = l.src[t];
@@ -230,18 +231,35 @@ hipError_t launch_dim(const Compact8Launch& l, hipStream_t s) {
       a.ids[t] = l.ids[t];
     }
     a.keep = l.keep;
-    a.n_lists = std::min(per_launch, l.n_lists - lo);
-    std::copy_n(l.lists + lo, a.n_lists, a.lists);
-    int most = 0;
-    for (int i = 0; i < a.n_lists; ++i) most = std::max(most, a.lists[i].k);
+    // the longest lists first: in place a list is one workgroup's, and the last to start should be short
+    const int n = std::min(per_launch, l.n_seqs - lo);
+    const int32_t* k_h = l.k_h + int64_t(lo) * per;
+    int order[LISTS], longest[LISTS];
+    int64_t first[LISTS];
+    for (int b = 0; b < n; ++b) {
+      order[b] = b;
+      first[b] = off;
+      longest[b] = *std::max_element(k_h + b * per, k_h + (b + 1) * per);
+      for (int h = 0; h < per; ++h) off += k_h[b * per + h];
+    }
+    std::sort(order, order + n, [&](int x, int y) { return longest[x] != longest[y] ? longest[x] > longest[y] : x < y; });
+    const int most = longest[order[0]];
     if (most == 0) continue;
+    for (int i = 0; i < n; ++i) {
+      int64_t at = first[order[i]];
+      for (int h = 0; h < per; ++h) {
+        const int k = k_h[order[i] * per + h];
+        a.lists[i * per + h] = CompactList{at, 0, k, lo + order[i]};
+        at += k;
+      }
+    }
     a.n_layers = l.n_layers;
     a.n_heads = l.n_heads;
     a.per_head = l.per_head;
     a.cu = l.cu_d;
-    a.id_blocks = l.ids[0] || l.ids[1] ? a.n_lists / per : 0;
+    a.id_blocks = l.ids[0] || l.ids[1] ? n : 0;
     a.chunks = l.in_place ? 1 : (most + CHUNK - 1) / CHUNK;
-    const int64_t grid = a.id_blocks + int64_t(a.n_lists / per) * l.n_heads * l.n_layers * 2 * a.chunks;
+    const int64_t grid = a.id_blocks + int64_t(n) * l.n_heads * l.n_layers * 2 * a.chunks;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
     if (l.in_place)
       hipLaunchKernelGGL((compact8_kernel<HD, true, NT_IN>), dim3(unsigned(grid)), dim3(NT_IN), 0, s, a);
