@@ -603,8 +603,10 @@ def _rows(r: c_rows, t: torch.Tensor, dtype: torch.dtype, what: str, want: tuple
     if st[-1] != 1:
         raise ValueError(f"rows of {what} must be contiguous")
     r.base = t.data_ptr()
-    r.tok_stride, r.head_stride = st[-3], st[-2]
-    r.layer_stride = st[0] if len(st) == 4 else 0
+    # (what strides lead over a single element says nothing)
+    r.tok_stride = st[-3] if want[-3] > 1 else 0
+    r.head_stride = st[-2] if want[-2] > 1 else 0
+    r.layer_stride = st[0] if len(st) == 4 and want[0] > 1 else 0
 
 
 def _empty(shape, dtype: torch.dtype, device, stream=None) -> torch.Tensor:
@@ -689,6 +691,8 @@ def cc_compact_kv8(p: Problem, kv: KV8, keep_idx: torch.Tensor, k: Sequence[int]
     kk, n = _host_array(k, np.int32, _i32)
     if n != p.struct.n_seqs * (p.struct.n_heads_kv if per_head else 1):
         raise ValueError(f"{n} budgets for {p.struct.n_seqs} sequences")
+    if keep_idx is not None and (keep_idx.dtype != torch.int32 or keep_idx.numel() < sum(k) or not keep_idx.is_contiguous()):
+        raise ValueError(f"keep_idx must be {sum(k)} contiguous int32 values")
     _on_gpu(keep_idx, token_ids, pos_ids)
     _check(_lib.cc_compact_kv8(ctypes.byref(p.struct), ctypes.byref(kv.struct), _ptr(keep_idx), kk, per_head,
                                _ptr(token_ids), _ptr(pos_ids),
@@ -764,8 +768,14 @@ def cc_lmhead_logprobs(dtype: str, u: torch.Tensor, w_lm: torch.Tensor, vocab: i
     if out is None:
         out = logprobs_out(n, top, u.device, stream)
     if out.top_ids.numel() < n * top or out.top_logprob.numel() < n * top:
-        raise ValueError(f"out has no room for {top} alternatives of {n} rows")
-    _on_gpu(u, w_lm, ids, out.entropy, workspace)
+        raise ValueError(f"out has no room for {top} alternatives of {n} rows (top_ids, top_logprob)")
+    f32 = torch.float32
+    for what, t, m, want in (("logprob", out.logprob, n, f32), ("entropy", out.entropy, n, f32),
+                             ("top_ids", out.top_ids, n * top, torch.int32),
+                             ("top_logprob", out.top_logprob, n * top, f32)):
+        if t.dtype != want or t.numel() < m or not t.is_contiguous():
+            raise ValueError(f"{what} must be at least {m} contiguous {want} values")
+    _on_gpu(u, w_lm, ids, out.logprob, out.entropy, out.top_ids, out.top_logprob, workspace)
     if workspace is None:
         workspace = _empty(max(1, cc_lmhead_logprobs_workspace(dtype, n, vocab, hidden, top)), torch.uint8, u.device, stream)
     _check(_lib.cc_lmhead_logprobs({"f32": CC_F32, "bf16": CC_BF16}[dtype], _ptr(u), _ptr(w_lm), int(packed), n,

@@ -296,3 +296,34 @@ def test_attention_refuses_rows_whose_offsets_in_a_group_pass_32_bits():
     lens = (P, 100, P, P, 1 << 30, None)
     assert f(_ref(_problem()), P, _ref(_kv8(paged=False, tok_stride=1 << 28)), 0, 0, *lens) == cc.CC_ERR_UNSUPPORTED
     assert f(_ref(_problem()), P, _ref(_kv8(paged=False, tok_stride=(1 << 40) + 128)), 0, 0, *lens) == cc.CC_ERR_UNSUPPORTED
+
+
+def test_logprobs_out_of_wrong_sizes(monkeypatch):
+    u, w = torch.zeros(3, 64, dtype=torch.bfloat16), torch.zeros(5, 64, dtype=torch.bfloat16)
+    monkeypatch.setattr(cc, "_on_gpu", lambda *t: None)
+    ids = torch.zeros(3, dtype=torch.int32)
+    good = cc.logprobs_out(3, 2, "cpu")
+    for name, bad in (("logprob", torch.zeros(2)), ("logprob", torch.zeros(3, dtype=torch.float64)), ("entropy", torch.zeros(2)),
+                      ("entropy", torch.zeros(6)[::2]), ("top_ids", torch.zeros(3, 2)),
+                      ("top_ids", torch.zeros(2, 2, dtype=torch.int32)), ("top_logprob", torch.zeros(3, 1))):
+        out = cc.Logprobs(**{**good.__dict__, name: bad})
+        with pytest.raises(ValueError, match=name):
+            cc.cc_lmhead_logprobs("bf16", u, w, 5, ids, 2, out)
+
+
+def test_strides_of_single_rows_do_not_matter():
+    """A dimension of one element may have any stride."""
+    r = cc.c_rows()
+    t = torch.zeros(64, dtype=torch.bfloat16).as_strided((1, 1, 64), (3, 5, 1))
+    cc._rows(r, t, torch.bfloat16, "k", (1, 1, 64))
+    assert (r.layer_stride, r.tok_stride, r.head_stride) == (0, 0, 0)
+    cc._rows(r, t[None], torch.bfloat16, "k", (1, 1, 1, 64))
+    assert (r.layer_stride, r.tok_stride, r.head_stride) == (0, 0, 0)
+
+
+def test_compaction_refuses_lists_of_another_type(monkeypatch):
+    monkeypatch.setattr(cc, "_on_gpu", lambda *t: None)
+    p, kv = cc.Problem(_problem(), None, None, []), cc.KV8(_kv8())
+    for keep in (torch.zeros(3, dtype=torch.int64), torch.zeros(2, dtype=torch.int32), torch.zeros(6, dtype=torch.int32)[::2]):
+        with pytest.raises(ValueError, match="keep_idx"):
+            cc.cc_compact_kv8(p, kv, keep, [1, 2], 0)
