@@ -9,10 +9,15 @@ namespace cc {
 // kernel for few against the one for many, 8000 entries and 8 KV heads of 128: 64 rows 41.5 us and (68
 // rows) 31.6, sixteen such sequences 328 and 122; two row blocks, 32 rows: 26.4 and 31, sixteen 128 and 122.
 constexpr int FEW_ROWS = 32;
-// Few rows: the longest cache of which each (sequence, head) is one workgroup's, with nothing to join
-// (64 sequences of 1000 entries, 4 heads: 17 us against 27 shared out; one of 1024, 8 heads: 13.4
-// against 14; there a CU's own loads, some 40 GB/s, are the bound).
-constexpr int KV8_DIRECT = 1024;
+// Few rows: the longest cache of which each (sequence, head) is one workgroup's, with nothing to join.  A
+// CU's own loads, some 40 GB/s, are the bound there, so it grows with the workgroups there are, up to where a
+// batch of one long sequence among short ones would wait for it.  One token each, heads of 128, that
+// against shares of the work:
+//   1024: 64 sequences of 1000, 4 heads: 17 us and 27; one of 1024, 8 heads: 13.4 and 14 (of 2048: 19 and 14);
+//   2048 from 128 (sequence, head)s: 300 sequences of 1500, 8 heads: 170 and 208; 16 of 2048: 23 and 27 (8 of
+//     them 22 and 21; 16, of which four have 2000 entries and the others 20: 22 and 18);
+//   not 4096 from 512: 64 sequences, 8 heads: 99 and 107, but 53 and 27 where eight have them and the others 20.
+inline int kv8_direct(int64_t items) { return items >= 128 ? 2048 : 1024; }
 constexpr int FEW_NT = 256;
 constexpr int KV8_LIST = 64;     // sequences of a launch listed by value
 constexpr int MANY_ROWS = 128;   // rows of a block of the kernel for many

@@ -167,10 +167,14 @@ struct Shares {
   int parts;         // workgroups that have some
   int q;
   int head;          // units without entries at an item's start
-  int mine;          // of the lane's sequence, if the list has up to 64: units of 128 entries
+  int per;           // sequences of a lane, in order: lane l has [l * per, (l + 1) * per) of the list
+  int mine;          // units of one KV head of these
   __device__ __forceinline__ int64_t begin(int w) const { return total * w / parts; }
   // the workgroup whose part unit x is in
   __device__ __forceinline__ int part_of(int64_t x) const { return int(((x + 1) * parts - 1) / total); }
+  __device__ __forceinline__ int of(int entry_units) const {
+    return entry_units == 0 ? 0 : (entry_units + q - 1) / q + head;
+  }
 };
 __device__ __forceinline__ int entry_units(const Kv8Args& a, int j) {   // of one KV head, 128 entries each
   if (j >= a.n_list) return 0;
@@ -178,11 +182,7 @@ __device__ __forceinline__ int entry_units(const Kv8Args& a, int j) {   // of on
   const int64_t rows = int64_t(s.m) * a.g;
   return rows == 0 || rows > FEW_ROWS ? 0 : max(1, (s.len + UNIT - 1) / UNIT);
 }
-__device__ __forceinline__ int units_of(const Kv8Args& a, const Shares& sh, int j) {
-  const int u = a.n_list <= 64 ? sh.mine : entry_units(a, j);   // (there, j is the lane)
-  return u == 0 ? 0 : (u + sh.q - 1) / sh.q + sh.head;
-}
-// Inclusive sums over the wave (64 sequences of 2^31 entries have fewer than 2^31 units).
+// Inclusive sums over the wave (what fits a card's memory has fewer than 2^31 units).
 __device__ __forceinline__ int wave_scan(int v) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -192,37 +192,49 @@ __device__ __forceinline__ int wave_scan(int v) {
   }
   return v;
 }
-__device__ __forceinline__ int64_t units_in_all(const Kv8Args& a, const Shares& sh) {
-  if (a.n_list == 1) return int64_t(units_of(a, sh, 0)) * a.hkv;
-  int64_t n = 0;
-  for (int b = 0; b < a.n_list; b += 64)
-    n += __builtin_amdgcn_readlane(wave_scan(units_of(a, sh, b + int(threadIdx.x & 63))), 63);
-  return n * a.hkv;
+__device__ __forceinline__ int64_t units_in_all(const Kv8Args& a, int mine) {
+  return int64_t(a.n_list == 1 ? mine : __builtin_amdgcn_readlane(wave_scan(mine), 63)) * a.hkv;
 }
 __device__ __forceinline__ Shares shares_of(const Kv8Args& a) {
   Shares s;
-  s.q = 1;
+  s.q = s.per = 1;
   s.head = 0;
   if (a.direct) {   // a (sequence, head) a workgroup
     s.mine = 1;
     s.total = s.parts = a.n_list * a.hkv;
     return s;
   }
+  s.per = (a.n_list + 63) >> 6;
+  const int lane = threadIdx.x & 63;
+  auto sum = [&](int& n) {
+    int v = 0;
+    n = 0;
+#pragma unroll 4
+    for (int c = 0; c < s.per; ++c) {
+      const int u = entry_units(a, lane * s.per + c);
+      v += s.of(u);
+      n += u != 0;
+    }
+    return v;
+  };
   // (one sequence: its length by scalar loads, no sums over the wave; 2 us less of 15)
-  s.mine = a.n_list == 1 ? entry_units(a, 0) : a.n_list <= 64 ? entry_units(a, threadIdx.x & 63) : 0;
-  s.total = units_in_all(a, s);
+  int n = 1;
+  const int raw = a.n_list == 1 ? entry_units(a, 0) : sum(n);
+  s.total = units_in_all(a, raw);
   const int items = a.n_list * a.hkv;
   if (items < a.parts) {
     const int64_t q = max(int64_t(2), (s.total + a.parts - items - 1) / (a.parts - items));
     if (q <= LITTLE) {   // at most total / q + items <= parts pieces
       s.q = int(q);
-      s.total = units_in_all(a, s);
+      s.mine = s.per == 1 ? s.of(raw) : sum(n);
+      s.total = units_in_all(a, s.mine);
       s.parts = int(s.total);
       return s;
     }
   }
   s.head = HEAD;
-  s.total = units_in_all(a, s);
+  s.mine = raw + n * HEAD;
+  s.total = units_in_all(a, s.mine);
   s.parts = int(min(int64_t(a.parts), s.total));
   return s;
 }
@@ -240,41 +252,58 @@ __device__ __forceinline__ Item item_at(const Kv8Args& a, const Shares& sh, int6
   }
   if (a.n_list == 1) {
     it.j = 0;
-    it.units = units_of(a, sh, 0);
+    it.units = sh.mine;
     it.kvh = int(x / it.units);
     it.unit = int(x - int64_t(it.kvh) * it.units);
     return it;
   }
-  int64_t start = 0;
-  for (int b = 0;; b += 64) {
-    const int u = units_of(a, sh, b + int(threadIdx.x & 63));
-    const int sum = wave_scan(u);
-    const uint64_t past = __ballot(start + int64_t(sum) * a.hkv > x);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      it.units = __builtin_amdgcn_readlane(u, l);
-      it.j = b + l;
-      const int y = int(x - start - int64_t(__builtin_amdgcn_readlane(sum, l) - it.units) * a.hkv);
-      it.kvh = y / it.units;
-      it.unit = y - it.kvh * it.units;
-      return it;
+  // the lane that has it, then the sequence among the lane's, 64 at a time
+  int u = sh.mine, sum = wave_scan(u);
+  int l = __builtin_ctzll(__ballot(int64_t(sum) * a.hkv > x));
+  it.j = l;
+  it.units = __builtin_amdgcn_readlane(u, l);
+  int64_t start = int64_t(__builtin_amdgcn_readlane(sum, l) - it.units) * a.hkv;
+  if (sh.per > 1) {
+    const int j0 = l * sh.per;
+    for (int c = 0;; c += 64) {
+      const int mine = c + int(threadIdx.x & 63);
+      u = mine < sh.per ? sh.of(entry_units(a, j0 + mine)) : 0;
+      sum = wave_scan(u);
+      const uint64_t past = __ballot(start + int64_t(sum) * a.hkv > x);
+      if (past) {
+        l = __builtin_ctzll(past);
+        it.j = j0 + c + l;
+        it.units = __builtin_amdgcn_readlane(u, l);
+        start += int64_t(__builtin_amdgcn_readlane(sum, l) - it.units) * a.hkv;
+        break;
+      }
+      start += int64_t(__builtin_amdgcn_readlane(sum, 63)) * a.hkv;
     }
-    start += int64_t(__builtin_amdgcn_readlane(sum, 63)) * a.hkv;
   }
+  const int y = int(x - start);
+  it.kvh = y / it.units;
+  it.unit = y - it.kvh * it.units;
+  return it;
 }
 // First unit of a head of the j-th sequence, and how many it has.
 __device__ __forceinline__ void item_of(const Kv8Args& a, const Shares& sh, int j, int64_t& start, int& units) {
   start = 0;
-  if (a.n_list == 1) {
-    units = units_of(a, sh, 0);
-    return;
-  }
-  for (int b = 0;; b += 64) {
-    const int u = units_of(a, sh, b + int(threadIdx.x & 63));
-    const int sum = wave_scan(u);
-    if (j < b + 64) {
-      units = __builtin_amdgcn_readlane(u, j - b);
-      start += int64_t(__builtin_amdgcn_readlane(sum, j - b) - units) * a.hkv;
+  units = sh.mine;
+  if (a.n_list == 1) return;
+  int l = j / sh.per;
+  int u = sh.mine, sum = wave_scan(u);
+  units = __builtin_amdgcn_readlane(u, l);
+  start = int64_t(__builtin_amdgcn_readlane(sum, l) - units) * a.hkv;
+  if (sh.per == 1) return;
+  const int j0 = l * sh.per;
+  for (int c = 0;; c += 64) {
+    const int mine = c + int(threadIdx.x & 63);
+    u = mine < sh.per ? sh.of(entry_units(a, j0 + mine)) : 0;
+    sum = wave_scan(u);
+    if (j < j0 + c + 64) {
+      l = j - j0 - c;
+      units = __builtin_amdgcn_readlane(u, l);
+      start += int64_t(__builtin_amdgcn_readlane(sum, l) - units) * a.hkv;
       return;
     }
     start += int64_t(__builtin_amdgcn_readlane(sum, 63)) * a.hkv;
@@ -606,21 +635,53 @@ __global__ __launch_bounds__(FEW_NT, 2) void attn_few(Kv8Args a) {
 
 // ------------------------------------------------------------------ joining pieces
 
-// out = sum_s o_s 2^((m_s - M) c2) / sum_s l_s 2^((m_s - M) c2), M = max m_s.  HD / 4 lanes take a row, G
-// groups of them its pieces in turn, four in flight; the groups meet in LDS.  G = 8 from 8 pieces on
-// (128 rows of 64 pieces: 35 us with G = 1, a chain of loads in 16 workgroups).
-// FEW: the pieces are shares of the kernel for few rows, else those of the kernel for many.
-template <int HD, int G, bool FEW>
-__global__ __launch_bounds__(256) void attn_join(Kv8Args a) {
-  constexpr int LPR = HD / 4, PER = 256 / (LPR * G);
-  __shared__ float4 po[G > 1 ? 256 : 1];
-  __shared__ float2 pm[G > 1 ? 256 : 1];
+// out = sum_s o_s 2^((m_s - M) c2) / sum_s l_s 2^((m_s - M) c2), M = max m_s.  HD / 4 lanes hold a row.
+struct Joined {
+  float M, L;
+  float4 o;
+  // N parts at once, those with in[q] set
+  template <int N, class F>
+  __device__ __forceinline__ void add(const float2 (&p)[N], F x, const bool (&in)[N], float c2) {
+    float t = M;
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+      if (in[q]) t = fmaxf(t, p[q].x);
+    const float ref = t == -INFINITY ? 0.f : t, c = fast_exp2((M - ref) * c2);
+    M = t;
+    L *= c;
+    o = make_float4(o.x * c, o.y * c, o.z * c, o.w * c);
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      if (!in[q]) continue;
+      const float f = fast_exp2((p[q].x - ref) * c2);
+      const float4 y = x(q);
+      L += p[q].y * f;
+      o = make_float4(o.x + y.x * f, o.y + y.y * f, o.z + y.z * f, o.w + y.w * f);
+    }
+  }
+};
+
+// FEW: the pieces are shares of the kernel for few rows, else those of the kernel for many.  A workgroup is
+// 256 / (HD / 4) groups of lanes.  With `one`, for up to JOIN_ONE rows in all, it has one row, whose pieces
+// the groups share out (128 rows of 64 pieces by a group each, a chain of loads in 16 workgroups: 35 us);
+// else a row for each group, and those of more than JOIN_ALONE pieces are shared out one after another.
+// (Finding a row's pieces is half of the work: 1023 sequences, 8 heads of 4 rows, 352 us with a
+// workgroup for each row.)
+constexpr int JOIN_ALONE = 8;
+constexpr int JOIN_ONE = 1024;
+template <int HD, bool FEW>
+__global__ __launch_bounds__(256) void attn_join(Kv8Args a, int one) {
+  constexpr int LPR = HD / 4, NG = 256 / LPR;
+  __shared__ float4 po[256];
+  __shared__ float2 pm[256];
+  __shared__ int sn[NG];
+  __shared__ int64_t sslot[NG];
   const int tid = threadIdx.x;
-  const int gi = tid / LPR % G, lane = tid % LPR;
-  const int row_in = blockIdx.x * PER + tid / (LPR * G);
-  const int d = lane * 4;
+  const int gi = tid / LPR, lane = tid % LPR;
   const int64_t all = int64_t(a.n_list) * a.hkv * a.R;
-  const int r = row_in % a.R, jh = min(row_in / a.R, a.n_list * a.hkv - 1);
+  const int64_t row_in = one ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * NG + gi;
+  const int d = lane * 4;
+  const int r = int(row_in % a.R), jh = int(min(row_in / a.R, int64_t(a.n_list) * a.hkv - 1));
   const int kvh = jh % a.hkv, j = jh / a.hkv;
   const Seq s = seq_of(a, j);
   const int rows = s.m * a.g;
@@ -629,7 +690,7 @@ __global__ __launch_bounds__(256) void attn_join(Kv8Args a) {
   int64_t slot, step;
   int n;
   if constexpr (FEW) {
-    // the rows of a workgroup lie in one (sequence, head), or the search runs for each in turn
+    // the rows of a wave lie in one (sequence, head), or the search runs for each in turn
     const Shares sh = shares_of(a);
     const int j0 = __builtin_amdgcn_readfirstlane(j);
     int64_t start;
@@ -658,66 +719,65 @@ __global__ __launch_bounds__(256) void attn_join(Kv8Args a) {
     slot = row_in;
     step = all;
   }
-  float M = -INFINITY, L = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (on) {
-    for (int i0 = gi; i0 < n; i0 += 4 * G) {
+  // pieces first, first + by, ..., four in flight
+  auto some = [&](int64_t from, int n, int first, int by) {
+    Joined g{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    for (int i0 = first; i0 < n; i0 += 4 * by) {
       float2 p[4];
       float4 x[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int64_t at = slot + min(i0 + q * G, n - 1) * step;
+        const int64_t at = from + min(i0 + q * by, n - 1) * step;
         p[q] = a.part_ml[at];
         x[q] = *reinterpret_cast<const float4*>(a.part + at * HD + d);
       }
-      float t = M;
+      bool in[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (i0 + q * G < n) t = fmaxf(t, p[q].x);
-      const float ref = t == -INFINITY ? 0.f : t;
-      const float c = fast_exp2((M - ref) * a.c2);
-      M = t;
-      L *= c;
-      o = make_float4(o.x * c, o.y * c, o.z * c, o.w * c);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (i0 + q * G >= n) continue;
-        const float f = fast_exp2((p[q].x - ref) * a.c2);
-        L += p[q].y * f;
-        o.x += x[q].x * f;
-        o.y += x[q].y * f;
-        o.z += x[q].z * f;
-        o.w += x[q].w * f;
-      }
+      for (int q = 0; q < 4; ++q) in[q] = i0 + q * by < n;
+      g.add(p, [&](int q) { return x[q]; }, in, a.c2);
     }
-  }
-  if constexpr (G > 1) {
-    po[tid] = o;
-    pm[tid] = make_float2(M, L);
+    return g;
+  };
+  auto finish = [&](const Joined& g) {
+    const float inv = g.L == 0.f ? 0.f : 1.f / g.L;
+    u16* out = a.o + (int64_t(s.q0 + r / a.g) * a.hq + kvh * a.g + r % a.g) * HD + d;
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf2(g.o.x * inv, g.o.y * inv), pack_bf2(g.o.z * inv, g.o.w * inv));
+  };
+  auto shared_out = [&](int64_t from, int n, int owner) {
+    const Joined mine = some(from, n, gi, NG);
+    po[tid] = mine.o;
+    pm[tid] = make_float2(mine.M, mine.L);
     __syncthreads();
-    if (gi != 0) return;
-    M = -INFINITY;
+    if (gi == owner) {
+      Joined g{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+      float2 p[NG];
+      bool in[NG];
 #pragma unroll
-    for (int q = 0; q < G; ++q) M = fmaxf(M, pm[tid + q * LPR].x);
-    const float ref = M == -INFINITY ? 0.f : M;
-    L = 0.f;
-    o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int q = 0; q < G; ++q) {
-      const float2 p = pm[tid + q * LPR];
-      const float4 x = po[tid + q * LPR];
-      const float f = fast_exp2((p.x - ref) * a.c2);
-      L += p.y * f;
-      o.x += x.x * f;
-      o.y += x.y * f;
-      o.z += x.z * f;
-      o.w += x.w * f;
+      for (int q = 0; q < NG; ++q) {
+        p[q] = pm[lane + q * LPR];
+        in[q] = true;
+      }
+      g.add(p, [&](int q) { return po[lane + q * LPR]; }, in, a.c2);
+      finish(g);
     }
+  };
+  if (one) {
+    if (on) shared_out(slot, n, 0);   // (alike in the whole workgroup)
+    return;
   }
-  if (!on) return;
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  u16* out = a.o + (int64_t(s.q0 + r / a.g) * a.hq + kvh * a.g + r % a.g) * HD + d;
-  *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf2(o.x * inv, o.y * inv), pack_bf2(o.z * inv, o.w * inv));
+  const bool alone = n <= JOIN_ALONE;
+  if (on && alone) finish(some(slot, n, 0, 1));
+  if (!__syncthreads_or(on && !alone)) return;
+  if (lane == 0) {
+    sn[gi] = on && !alone ? n : 0;
+    sslot[gi] = slot;
+  }
+  __syncthreads();
+  for (int q = 0; q < NG; ++q) {
+    if (sn[q] == 0) continue;
+    shared_out(sslot[q], sn[q], q);
+    __syncthreads();
+  }
 }
 
 template <int HD, int NR>
@@ -743,13 +803,14 @@ hipError_t launch_dim(const Kv8Args& a, bool few, hipStream_t s) {
     e = launch_attn_many(a, s);
   if (e != hipSuccess || !a.part) return e;
   const int64_t rows = int64_t(a.n_list) * a.hkv * a.R;
-  constexpr int P1 = 256 / (HD / 4), P8 = P1 / 8 ? P1 / 8 : 1;
+  constexpr int NG = 256 / (HD / 4);
+  const int one = rows <= JOIN_ONE;
+  const int64_t grid = one ? rows : (rows + NG - 1) / NG;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
   if (few)
-    hipLaunchKernelGGL((attn_join<HD, 8, true>), dim3(unsigned((rows + P8 - 1) / P8)), dim3(256), 0, s, a);
-  else if (a.splits >= 8)
-    hipLaunchKernelGGL((attn_join<HD, 8, false>), dim3(unsigned((rows + P8 - 1) / P8)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attn_join<HD, true>), dim3(unsigned(grid)), dim3(256), 0, s, a, one);
   else
-    hipLaunchKernelGGL((attn_join<HD, 1, false>), dim3(unsigned((rows + P1 - 1) / P1)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attn_join<HD, false>), dim3(unsigned(grid)), dim3(256), 0, s, a, one);
   return hipGetLastError();
 }
 

@@ -1134,7 +1134,7 @@ Kv8Class kv8_class(const cc_problem* p, int max_len, bool few) {
   if (few) {
     // Short caches: a workgroup for each (sequence, head), nothing to join.  Else the work is shared
     // out among two workgroups a CU, or one for each (sequence, head) up to eight a CU.
-    c.direct = max_len <= KV8_DIRECT;
+    c.direct = max_len <= kv8_direct(items);
     c.parts = int(std::min<int64_t>(8 * kCus, std::max<int64_t>(2 * kCus, items)));
     if (!c.direct) rows = (size_t(c.parts) + size_t(c.n_list) * p->n_heads_kv) * c.R;
   } else {

@@ -284,3 +284,19 @@ def test_offsets_past_32_bits(new):
     cc.cc_compact_kv8(pc, kv, keep, [64], 0)
     torch.cuda.synchronize()
     np.testing.assert_allclose(values("v", np.arange(64)), moved, rtol=2.0 ** -4, atol=2.0 ** -9)
+
+
+@pytest.mark.parametrize("n,most,longest,hkv", [(150, 5000, 5000, 2), (4200, 40, 3000, 1), (700, 60, 3000, 3)])
+def test_shares_of_many_sequences(n, most, longest, hkv):
+    """Work shared out over more sequences than a wave has lanes, up to more than 64 for each lane; rows
+    whose entries lie in one share, in a few and in many."""
+    from paper_2607_27600_amd import cc
+    d, hq = 64, 2 * hkv
+    r = np.random.default_rng(n)
+    new = [int(x) for x in r.choice([0, 1, 1, 3], n)]
+    lens = [m + int(x) for m, x in zip(new, r.integers(0, 30, n))]
+    lens[n // 3], lens[n - 1], new[n // 3], new[n - 1] = most, most - 1, 1, 2
+    cache = Cache8(lens, hkv, d, page=16 if n == 150 else 0, block=16, seed=n + 1, fill=0x7f)
+    q = _q(new, hq, d, n + 2)
+    o = _run(cc, cache, q, new, lens, hq, hkv, "causal", longest=longest)
+    assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, "causal"))
