@@ -15,7 +15,7 @@
 //
 // Bound by memory for chunks of a prompt (8192 tokens, 32 heads on 8, into 8 bits: 185 MB in 44 us, 4.2 TB/s;
 // 3166 ragged tokens into bf16 pages: 78 MB in 15.8 us, 4.9 TB/s, what a large copy reaches) and by the
-// round trips to lengths, then rows, for single tokens (eight: 6.2 us); a row is read 16 elements a lane
+// round trips to lengths, then rows, for single tokens (eight: 4.9 us); a row is read 16 elements a lane
 // (e .. e + 7 and their partners), 16 bytes a load.
 #include <cmath>
 
@@ -25,7 +25,9 @@ namespace cc {
 namespace {
 
 constexpr int NT = 256;
-constexpr int QT = 4;          // tokens of a query unit
+// Tokens of a query unit (1, 4 and 16: 8192 tokens of 32 heads 48.6, 44.9 and 54.5 us, one token each of 256
+// sequences 6.7, 8.3 and 15.8, 64 of them 5.3, 5.5 and 12.9).
+constexpr int QT = 4;
 constexpr int PLAIN_SHIFT = 4; // tokens of a unit of a 16/32-bit cache: 16
 
 template <int HD>
@@ -327,8 +329,11 @@ hipError_t launch_typed(const AppendLaunch& l, hipStream_t s) {
   for (int b = 1; b < l.n_seqs && a.each >= 0; ++b)
     if (l.cu_h[b + 1] - l.cu_h[b] != a.each) a.each = -1;
   const int64_t blocks = a.each >= 0 ? int64_t(l.n_seqs) * ((a.each + 2 * B - 2) / B) : a.M / B + 2 * int64_t(l.n_seqs);
-  // Heads are shared out until there are some four workgroups a CU, one head each at the most.
-  a.splits = int(std::min<int64_t>(a.hkv, std::max<int64_t>(1, 1024 / (2 * blocks * l.n_layers))));
+  // Heads are shared out until there are some 640 workgroups, one head each at the most.  (8 heads of 128,
+  // up to 256, 640 and 1024 workgroups: two sequences' chunks of 500 8.7, 7.4 and 7.4 us, one of 2000 10.6,
+  // 10.0 and 13.8, one token each of 256 sequences 5.8, 5.8 and 8.3; 8192 tokens in blocks of 64
+  // 51.7, 43.9 and 45.0.)
+  a.splits = int(std::min<int64_t>(a.hkv, std::max<int64_t>(1, 640 / (2 * blocks * l.n_layers))));
   a.splits = std::max(a.splits, (a.hkv + 63) / 64);
   a.heads = (a.hkv + a.splits - 1) / a.splits;
   a.splits = (a.hkv + a.heads - 1) / a.heads;
