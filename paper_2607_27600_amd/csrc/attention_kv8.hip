@@ -13,13 +13,14 @@
 // Numbers.  E4M3 has 4 significant bits and the scales are powers of two, so entries become bf16
 // exactly (one conversion instruction for two codes, scale included); products accumulate in
 // fp32; a row's maximum and sum are fp32, the reference maximum moving only when it is passed by 2^8
-// (numerator and sum share it).  The probabilities are rounded to bf16 for the second product (off
-// by 2^-9 each, independently), the sum takes them unrounded.
+// (numerator and sum share it).  The probabilities are rounded to bf16 for the second product (each by
+// up to 2^-8 of itself, independently: what the output's own rounding costs), the sum takes them unrounded.
 //
 // Masked entries.  Scores are replaced, not added to, so what a masked key holds is lost.  A masked
 // value meets a probability of 0, and 0 * NaN would reach the output: values past the sequence are
 // zeroed as they are read, and in tiles that some row sees in part, NaN codes are zeroed too and
-// counted by a second product of indicators, by the rows that may see them.
+// counted by a second product of indicators, by the rows that may see them (the kernel for many marks
+// them instead).
 #include <algorithm>
 
 #include "attention_kv8.h"
@@ -150,12 +151,12 @@ __device__ __forceinline__ int past_of(const Kv8Args& a, const Seq& s, int i) {
 // each its KV heads in order, of each its entries.
 //   Much work: each of `parts` workgroups takes an equal part of the line, so that a ragged batch keeps
 //     every CU busy to the end (64 sequences of 31 to 15987 entries, 4 heads: equal pieces of 2048
-//     entries 118 us, of 680 entries 84, shares 78).  A part may hold the end of one (sequence, head),
+//     entries 118 us, of 680 entries 84, shares 76).  A part may hold the end of one (sequence, head),
 //     whole ones and the start of another.  Every item takes HEAD units more, without entries, for what
-//     it costs to begin one (without them a part of many short sequences is the last: 88 us).
+//     it costs to begin one (without them a part of many short sequences is the last: 84 us).
 //   Little work (up to LITTLE units for each of two workgroups a CU): the time is that of one chain of
 //     round trips, and a second item in a part would double it, so the units become pieces of q units
-//     that no two items share, a workgroup each (32 rows, 8 heads, 8000 entries: 22 us, shares 27).
+//     that no two items share, a workgroup each (32 rows, 8 heads, 8000 entries: 23 us, shares 28).
 //   A short longest sequence (`direct`): a workgroup for each (sequence, head), nothing to join.
 // An item that is whole in one part is final there; other results are joined.  A result's place is the
 // workgroup's index plus that of the (sequence, head): both rise along the line, so no two meet.
@@ -664,10 +665,11 @@ struct Joined {
 // FEW: the pieces are shares of the kernel for few rows, else those of the kernel for many.  A workgroup is
 // 256 / (HD / 4) groups of lanes.  With `one`, for up to JOIN_ONE rows in all, it has one row, whose pieces
 // the groups share out (128 rows of 64 pieces by a group each, a chain of loads in 16 workgroups: 35 us);
-// else a row for each group, and those of more than JOIN_ALONE pieces are shared out one after another.
-// (Finding a row's pieces is half of the work: 1023 sequences, 8 heads of 4 rows, 352 us with a
-// workgroup for each row.)
-constexpr int JOIN_ALONE = 8;
+// else a row for each group (finding a row's pieces is half of the work: 1023 sequences, 8 heads of 4
+// rows, 352 us with a workgroup for each row), and those of more than JOIN_ALONE pieces are shared out one after
+// another (with 8 and with 32: 64 queries of 32 heads on 8, nine pieces, 30 us and 23; one sequence of 131072
+// entries among 99 of 20 125 and 118).
+constexpr int JOIN_ALONE = 32;
 constexpr int JOIN_ONE = 1024;
 template <int HD, bool FEW>
 __global__ __launch_bounds__(256) void attn_join(Kv8Args a, int one) {

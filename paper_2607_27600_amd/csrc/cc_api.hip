@@ -1132,15 +1132,18 @@ Kv8Class kv8_class(const cc_problem* p, int max_len, bool few) {
   const int64_t items = blocks * p->n_heads_kv;   // workgroups without a cut
   size_t rows = 0;                                // partial results
   if (few) {
-    // Short caches: a workgroup for each (sequence, head), nothing to join.  Else the work is shared
-    // out among two workgroups a CU, or one for each (sequence, head) up to eight a CU.
+    // Short caches: a workgroup for each (sequence, head), nothing to join.  Else the work is shared out
+    // among two workgroups a CU, all that fit at a time (eight a CU where there are as many (sequence,
+    // head)s: 1023 sequences of 200 to 4000 entries 683 us, with two 652; 600 of 50 to 9000 503 and 466).
     c.direct = max_len <= kv8_direct(items);
-    c.parts = int(std::min<int64_t>(8 * kCus, std::max<int64_t>(2 * kCus, items)));
+    c.parts = 2 * kCus;
     if (!c.direct) rows = (size_t(c.parts) + size_t(c.n_list) * p->n_heads_kv) * c.R;
   } else {
-    // pieces until there are two workgroups a CU (what is resident), of 512 entries at the least
+    // pieces until there are two workgroups a CU (what is resident; 512 queries of 32 heads on 8 at 8000
+    // entries 110 us, with one 142, with four 125), of 256 entries at the least (128 queries of 8 heads on one at
+    // 4000 21 us, of 512 27, of 128 24)
     const int64_t want = std::max<int64_t>(
-        1, std::min<int64_t>((2 * kCus + items - 1) / items, (int64_t(max_len) + 511) / 512));
+        1, std::min<int64_t>((2 * kCus + items - 1) / items, (int64_t(max_len) + 255) / 256));
     c.piece = int(((int64_t(max_len) + want - 1) / want + MANY_KEYS - 1) / MANY_KEYS * MANY_KEYS);
     c.piece = std::max(c.piece, MANY_KEYS);
     c.splits = std::max(1, int((int64_t(max_len) + c.piece - 1) / c.piece));

@@ -8,8 +8,8 @@
 // A workgroup moves chunks of rows, whole blocks: rows in registers, 16 codes a lane; a block's largest
 // magnitude by an LDS maximum of fp32 bits (order-free); one barrier; the codes.
 //   Out of place a chunk of 128 rows (head_dim 64: 256) is a workgroup of 256 threads.  Bound by memory: of
-//   four sequences a quarter kept, 8 paged layers, 115 MB in 46 us (2.5 TB/s; rows of 128 bytes from
-//   anywhere: 94% kept reach 4.2, and a mere copy of the codes takes as long).
+//   four sequences a quarter kept, 8 paged layers, 115 MB in 40 to 49 us (2.9 to 2.3 TB/s; rows of 128 bytes
+//   from anywhere: 94% kept reach 4.2, and a mere copy of the codes takes as long).
 //   In place one workgroup walks its plane's chunks in rising order: keep is ascending, so the sources of
 //   chunk c + 1 lie at or past its first row, beyond everything chunk c writes (codes and scales), and are
 //   loaded before chunk c is written; the barrier of chunk c orders its own reads before its writes.

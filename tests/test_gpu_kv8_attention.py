@@ -300,3 +300,17 @@ def test_shares_of_many_sequences(n, most, longest, hkv):
     q = _q(new, hq, d, n + 2)
     o = _run(cc, cache, q, new, lens, hq, hkv, "causal", longest=longest)
     assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, "causal"))
+
+
+@pytest.mark.parametrize("new,n,hq,hkv,d", [([64], 9100, 12, 3, 64), ([300], 9100, 4, 4, 128), ([90, 70], 9000, 4, 2, 128),
+                                            ([40], 300, 4, 2, 128)])
+@pytest.mark.parametrize("mask", ["causal", "counter"])
+def test_many_rows_in_pieces(new, n, hq, hkv, d, mask):
+    """Rows in few and in more pieces than one group of lanes joins alone, and sequences shorter than the
+    plan's, which have fewer."""
+    from paper_2607_27600_amd import cc
+    lens = [max(m, n // (b + 1) - 17 * b) for b, m in enumerate(new)]
+    cache = Cache8(lens, hkv, d, page=64, block=32, seed=n + d, fill=0x7f)
+    q = _q(new, hq, d, n + 1)
+    o = _run(cc, cache, q, new, lens, hq, hkv, mask)
+    assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, mask))
