@@ -27,7 +27,7 @@ constexpr int VT = 256;          // words of a tile (MB = 8)
 constexpr int SLAB = 2048;       // rows worked on at a time: bounds the workspace
 
 // Tables of one slab.  A row's numbers lie together for the wave that joins them: 16 rows side by side, as
-// the tiles write them, let every load of the join touch 64 lines (64 rows 30 us; now 10 in all).
+// the tiles write them, let every load of the join touch 64 lines (64 rows 30 us; now 15, some ten round trips).
 struct Tables {
   float4* part;      // [row][tile]: (max, S, T, -) in log2 units
   uint8_t* count;    // [row][half tile]: candidates
