@@ -623,13 +623,21 @@ def _on_gpu(*tensors) -> None:
     here = None
     for t in tensors:
         if t is not None:
-            if not t.is_cuda:
-                raise ValueError(f"tensors must be on the GPU, got one on {t.device}")
-            if here is not None and t.get_device() != here:
-                raise ValueError("tensors on different devices")
-            here = t.get_device()
+            d = t.get_device()   # negative: not on a GPU
+            if d != here:
+                if d < 0:
+                    raise ValueError(f"tensors must be on the GPU, got one on {t.device}")
+                if here is not None:
+                    raise ValueError("tensors on different devices")
+                here = d
     if here is not None and here != torch._C._cuda_getDevice():
         raise ValueError(f"tensors are on cuda:{here}, the current device is cuda:{torch._C._cuda_getDevice()}")
+
+
+def _codes(kv) -> Optional[torch.Tensor]:
+    """The keys of a cache view, which say where it lies."""
+    codes = kv.keep[0] if kv.keep else None
+    return codes.keep[0] if isinstance(codes, KV) else codes
 
 
 def _int32(t: Optional[torch.Tensor], n: int, what: str) -> None:
@@ -657,7 +665,7 @@ def _append(fn, p: Problem, kv, k, v, cached, capacity, layer, n_layers, pos_ids
         elif q_out.dtype != dtype or q_out.numel() != M * hq * d or not q_out.is_contiguous():
             raise ValueError("q_out must be contiguous rows of q's type and size")
         a.q_out = q_out.data_ptr()
-    _on_gpu(k, v, q, q_out, cached, pos_ids)
+    _on_gpu(k, v, q, q_out, cached, pos_ids, _codes(kv))
     a.cached = cached.data_ptr()
     if pos_ids is not None:
         a.pos_ids = pos_ids.data_ptr()
@@ -693,7 +701,7 @@ def cc_compact_kv8(p: Problem, kv: KV8, keep_idx: torch.Tensor, k: Sequence[int]
         raise ValueError(f"{n} budgets for {p.struct.n_seqs} sequences")
     if keep_idx is not None and (keep_idx.dtype != torch.int32 or keep_idx.numel() < sum(k) or not keep_idx.is_contiguous()):
         raise ValueError(f"keep_idx must be {sum(k)} contiguous int32 values")
-    _on_gpu(keep_idx, token_ids, pos_ids)
+    _on_gpu(keep_idx, token_ids, pos_ids, _codes(kv), _codes(out) if out is not None else None)
     _check(_lib.cc_compact_kv8(ctypes.byref(p.struct), ctypes.byref(kv.struct), _ptr(keep_idx), kk, per_head,
                                _ptr(token_ids), _ptr(pos_ids),
                                ctypes.byref(out.struct) if out is not None else None, _stream(stream)),
@@ -722,7 +730,7 @@ def cc_attention_kv8(p: Problem, q: torch.Tensor, kv: KV8, layer: int, kv_lens: 
         o = _empty(q.shape, q.dtype, q.device, stream)
     elif o.dtype != q.dtype or o.numel() != q.numel() or not o.is_contiguous():
         raise ValueError("o must be contiguous and of q's type and size")
-    _on_gpu(q, o, kv_lens, workspace)
+    _on_gpu(q, o, kv_lens, workspace, _codes(kv))
     if workspace is None:
         workspace = _empty(max(1, cc_attention_kv8_workspace(p, mask, max_kv_len)), torch.uint8, q.device, stream)
     _check(_lib.cc_attention_kv8(ctypes.byref(s), _ptr(q), ctypes.byref(kv.struct), layer, _MASKS[mask],

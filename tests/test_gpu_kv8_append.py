@@ -92,6 +92,14 @@ CASES = [
 ]
 
 
+MORE_HEADS = [([3, 1], [14, 0], 66, 66, 64, 16, 16, "bf16", 1), ([40], [7], 130, 65, 64, 0, 32, "bf16", 2)]
+
+
+@pytest.mark.parametrize("case", MORE_HEADS, ids=["66", "65"])
+def test_more_heads_than_a_workgroup_takes(case):
+    test_append_8bit(case, False)
+
+
 @pytest.mark.parametrize("pos_given", [True, False])
 @pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
 def test_append_8bit(case, pos_given):

@@ -314,3 +314,24 @@ def test_many_rows_in_pieces(new, n, hq, hkv, d, mask):
     q = _q(new, hq, d, n + 1)
     o = _run(cc, cache, q, new, lens, hq, hkv, mask)
     assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, mask))
+
+
+@pytest.mark.parametrize("new,lens,hq,hkv,d", [([1], [50], 64, 1, 128), ([2, 1], [300, 1], 96, 2, 64), ([1, 1], [2500, 3], 40, 1, 128)])
+def test_many_heads_of_a_group(new, lens, hq, hkv, d):
+    """A single query of a group of more heads than count as few rows."""
+    from paper_2607_27600_amd import cc
+    cache = Cache8(lens, hkv, d, page=16, block=16, seed=hq, fill=0x7f)
+    q = _q(new, hq, d, hq + 1)
+    for mask in ("causal", "counter"):
+        o = _run(cc, cache, q, new, lens, hq, hkv, mask)
+        assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, mask))
+
+
+def test_a_plan_for_no_entries():
+    """max_kv_len 0: every length is cut to it, every output is zero and no page is looked up."""
+    from paper_2607_27600_amd import cc
+    new, hq, hkv, d = [1, 40, 2], 4, 2, 128
+    cache = Cache8([9, 40, 2], hkv, d, page=16, block=16, seed=61)
+    cache.bt.fill_(-1)
+    o = _run(cc, cache, _q(new, hq, d, 62), new, [9, 40, 2], hq, hkv, "causal", longest=0)
+    assert torch.count_nonzero(o) == 0

@@ -169,3 +169,25 @@ def test_two_graphs_and_an_eager_call_in_turn():
                 gc, gs = o.plane(1, b, 1, "v", src=after, n=len(kl))
                 np.testing.assert_array_equal(gc, codes)
                 np.testing.assert_array_equal(gs, sc)
+
+
+@pytest.mark.parametrize("page,page2", [(16, 64), (128, 32)])
+def test_pages_of_another_size(page, page2):
+    """Out of place between pools whose pages differ."""
+    from paper_2607_27600_amd import cc
+    r = np.random.default_rng(31)
+    lens, kept, hkv, d = [400, 130], [333, 100], 2, 128
+    c = Cache8(lens, hkv, d, page=page, block=16, seed=32)
+    dst = Cache8([333, 100], hkv, d, page=page2, block=16, room=70, seed=33)
+    lists = [np.sort(r.permutation(n)[:k]).astype(np.int32) for n, k in zip(lens, kept)]
+    p = cc.problem(dtype="bf16", cu_seqlens=cu_of(lens), n_heads_q=hkv, n_heads_kv=hkv, head_dim=d, hidden=64, vocab=1)
+    cc.cc_compact_kv8(p, c.view(cc), torch.from_numpy(np.concatenate(lists)).cuda(), kept, 0, out=dst.view(cc))
+    torch.cuda.synchronize()
+    after = dst.read()
+    for b, kl in enumerate(lists):
+        for h in range(hkv):
+            for t in ("k", "v"):
+                codes, sc = O8.compact(*c.plane(0, b, h, t, n=lens[b]), kl, 16)
+                gc, gs = dst.plane(0, b, h, t, src=after, n=len(kl))
+                np.testing.assert_array_equal(gc, codes)
+                np.testing.assert_array_equal(gs, sc)

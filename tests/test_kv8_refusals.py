@@ -327,3 +327,23 @@ def test_compaction_refuses_lists_of_another_type(monkeypatch):
     for keep in (torch.zeros(3, dtype=torch.int64), torch.zeros(2, dtype=torch.int32), torch.zeros(6, dtype=torch.int32)[::2]):
         with pytest.raises(ValueError, match="keep_idx"):
             cc.cc_compact_kv8(p, kv, keep, [1, 2], 0)
+
+
+def test_tensors_elsewhere(monkeypatch):
+    """Tensors of one call lie on one GPU, the current one."""
+    class T:
+        def __init__(self, d):
+            self.d, self.device = d, f"cuda:{d}"
+
+        def get_device(self):
+            return self.d
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    cc._on_gpu(T(0), None, T(0))
+    for bad, what in (((T(0), T(1)), "different"), ((T(1), T(1)), "current device"), ((T(0), torch.zeros(1)), "must be on the GPU")):
+        with pytest.raises(ValueError, match=what):
+            cc._on_gpu(*bad)
+    k = torch.zeros(16, dtype=torch.uint8)
+    kv = cc.kv_contiguous(k, k, n_layers=1, layer_stride=0, head_stride=0, tok_stride=16)
+    kv8 = cc.kv8_contiguous(k, k, k, k, n_layers=1, layer_stride=0, head_stride=0, tok_stride=16, scale_block=16,
+                            scale_layer_stride=0, scale_head_stride=0)
+    assert cc._codes(kv) is k and cc._codes(kv8) is k
