@@ -410,9 +410,9 @@ struct Layout {
 };
 // The first round of workgroups knows no bound, so it is kept from two rounds of 256-row tiles on (it costs
 // a launch that clears it).  1000 rows of 2048, 40000 words, three rounds, 5 and 20 alternatives: 221 and
-// 364 us without, 204 and 265 with it; 300 rows of 4096, 128256 words, 398 and 546, 389 and 477.  A tile of up to 64 rows is soon looked
-// through, and waiting for a bound never paid: 64 rows of 3584, 152064 words, 5 and 20 alternatives, with it 250 and
-// 318 us, without 240 and 288; of 2048, 300000 words, 268 and 336, 269 and 341.
+// 364 us without, 204 and 265 with it; 300 rows of 4096, 128256 words, 398 and 546, 389 and 477.  A tile of up
+// to 64 rows is soon looked through, and waiting for a bound never paid: 64 rows of 3584, 152064 words, 5 and 20
+// alternatives, with it 250 and 318 us, without 240 and 288; of 2048, 300000 words, 268 and 336, 269 and 341.
 bool bounded(int N, int V, int top) {
   return top > 0 && N > 64 && (int64_t(V) + VT - 1) / VT * ((std::min(N, SLAB) + 255) / 256) >= 2 * 256;
 }
