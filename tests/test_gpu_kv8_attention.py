@@ -335,3 +335,24 @@ def test_a_plan_for_no_entries():
     cache.bt.fill_(-1)
     o = _run(cc, cache, _q(new, hq, d, 62), new, [9, 40, 2], hq, hkv, "causal", longest=0)
     assert torch.count_nonzero(o) == 0
+
+
+@pytest.mark.parametrize("new,hq,hkv,d", [([8], 16, 4, 128), ([8, 5], 16, 4, 64), ([40], 8, 2, 128)])
+def test_drafts_in_a_graph(new, hq, hkv, d):
+    """Two row blocks, and the kernel for many, captured and replayed as the lengths grow."""
+    from paper_2607_27600_amd import cc
+    cache = Cache8([3000] * len(new), hkv, d, page=16, block=16, seed=71)
+    q, kv, lens = _q(new, hq, d, 72), cache.view(cc), i32([2000] * len(new))
+    p = _problem(cc, new, hq, hkv, d)
+    o = torch.empty_like(q)
+    ws = torch.empty(max(1, cc.cc_attention_kv8_workspace(p, "causal", 3000)), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cc.cc_attention_kv8(p, q, kv, 0, lens, 3000, o, workspace=ws)
+    for n in (2000, 2999, 45):
+        lens.fill_(n)
+        o.fill_(9.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert_attention_close(f64(o), _oracle(cache, q, new, [n] * len(new), hq, hkv, "causal"), str(n))
