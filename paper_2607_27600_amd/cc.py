@@ -652,6 +652,9 @@ def _append(fn, p: Problem, kv, k, v, cached, capacity, layer, n_layers, pos_ids
     dtype = _DTYPES[s.dtype]
     _int32(cached, n_seqs, "cached")
     _int32(pos_ids, M, "pos_ids")
+    codes = _codes(kv)   # (8-bit views are of bytes already)
+    if isinstance(kv, KV) and codes is not None and any(t.dtype != dtype for t in kv.keep[:2]):
+        raise ValueError(f"the cache holds {codes.dtype}, the problem {dtype}")
     a = c_append()
     # one layer may come without its dimension
     want = (n_layers, M, hkv, d) if n_layers != 1 or k.dim() == 4 else (M, hkv, d)
@@ -665,7 +668,7 @@ def _append(fn, p: Problem, kv, k, v, cached, capacity, layer, n_layers, pos_ids
         elif q_out.dtype != dtype or q_out.numel() != M * hq * d or not q_out.is_contiguous():
             raise ValueError("q_out must be contiguous rows of q's type and size")
         a.q_out = q_out.data_ptr()
-    _on_gpu(k, v, q, q_out, cached, pos_ids, _codes(kv))
+    _on_gpu(k, v, q, q_out, cached, pos_ids, codes)
     a.cached = cached.data_ptr()
     if pos_ids is not None:
         a.pos_ids = pos_ids.data_ptr()

@@ -347,3 +347,24 @@ def test_tensors_elsewhere(monkeypatch):
     kv8 = cc.kv8_contiguous(k, k, k, k, n_layers=1, layer_stride=0, head_stride=0, tok_stride=16, scale_block=16,
                             scale_layer_stride=0, scale_head_stride=0)
     assert cc._codes(kv) is k and cc._codes(kv8) is k
+
+
+def test_append_refuses_a_cache_of_another_type(monkeypatch):
+    """Rows of four bytes into a cache of two would be written past its end."""
+    monkeypatch.setattr(cc, "_on_gpu", lambda *t: None)
+    monkeypatch.setattr(cc, "_stream", lambda s=None: None)
+    lens = torch.zeros(1, dtype=torch.int32)
+    for dtype, T, other in (("f32", torch.float32, torch.bfloat16), ("bf16", torch.bfloat16, torch.float32),
+                            ("bf16", torch.bfloat16, torch.float16), ("bf16", torch.bfloat16, torch.uint8)):
+        p = cc.problem(dtype=dtype, cu_seqlens=[0, 2], n_heads_q=4, n_heads_kv=2, head_dim=64, hidden=64, vocab=1, rope_theta=1e4,
+                       device="cpu")
+        k = torch.zeros(2, 2, 64, dtype=T)
+        for pool in ((other, other), (T, other), (other, T)):
+            pools = [torch.zeros(2, 32, 64, dtype=t) for t in pool]
+            kw = dict(n_layers=1, layer_stride=4096, head_stride=2048, tok_stride=64)
+            caches = [cc.kv_contiguous(*pools, **kw),
+                      cc.kv_paged(*pools, torch.zeros(1, 2, dtype=torch.int32), page_stride=4096, page_size=32, **kw)]
+            for kv in caches:
+                # (layer 1 of one: the library refuses the call, so that nothing is launched where the binding does not)
+                with pytest.raises(ValueError, match="the cache holds"):
+                    cc.cc_append_kv(p, kv, k, k, lens, capacity=32, layer=1)
