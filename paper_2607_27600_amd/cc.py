@@ -704,6 +704,10 @@ def cc_compact_kv8(p: Problem, kv: KV8, keep_idx: torch.Tensor, k: Sequence[int]
         raise ValueError(f"{n} budgets for {p.struct.n_seqs} sequences")
     if keep_idx is not None and (keep_idx.dtype != torch.int32 or keep_idx.numel() < sum(k) or not keep_idx.is_contiguous()):
         raise ValueError(f"keep_idx must be {sum(k)} contiguous int32 values")
+    N = p.struct.cu_seqlens_h[p.struct.n_seqs]
+    for what, t in (("token_ids", token_ids), ("pos_ids", pos_ids)):
+        if t is not None and (t.dtype != torch.int32 or t.numel() < N or not t.is_contiguous()):
+            raise ValueError(f"{what} must be at least {N} contiguous int32 values")
     _on_gpu(keep_idx, token_ids, pos_ids, _codes(kv), _codes(out) if out is not None else None)
     _check(_lib.cc_compact_kv8(ctypes.byref(p.struct), ctypes.byref(kv.struct), _ptr(keep_idx), kk, per_head,
                                _ptr(token_ids), _ptr(pos_ids),

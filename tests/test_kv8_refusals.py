@@ -368,3 +368,21 @@ def test_append_refuses_a_cache_of_another_type(monkeypatch):
                 # (layer 1 of one: the library refuses the call, so that nothing is launched where the binding does not)
                 with pytest.raises(ValueError, match="the cache holds"):
                     cc.cc_append_kv(p, kv, k, k, lens, capacity=32, layer=1)
+
+
+@pytest.mark.parametrize("which", ["token_ids", "pos_ids"])
+def test_compaction_refuses_ids_of_another_type_or_too_few(monkeypatch, which):
+    """int64 ids would be moved as pairs of words, a short tensor read and written past its end; a longer one
+    (a buffer of the cache's capacity) is fine."""
+    monkeypatch.setattr(cc, "_on_gpu", lambda *t: None)
+    monkeypatch.setattr(cc, "_stream", lambda s=None: None)
+    p, keep = cc.Problem(_problem(), None, None, []), torch.zeros(2, dtype=torch.int32)
+    # (the library refuses the scale block, so that nothing is launched where the binding does not)
+    kv = cc.KV8(_kv8(scale_block=8))
+    for ids in (torch.zeros(8, dtype=torch.int64), torch.zeros(7, dtype=torch.int32), torch.zeros(16, dtype=torch.int32)[::2],
+                torch.zeros(8)):
+        with pytest.raises(ValueError, match=which):
+            cc.cc_compact_kv8(p, kv, keep, [1, 1], 0, **{which: ids})
+    for n in (8, 11):
+        with pytest.raises(cc.CCError):
+            cc.cc_compact_kv8(p, kv, keep, [1, 1], 0, **{which: torch.zeros(n, dtype=torch.int32)})
