@@ -640,6 +640,13 @@ def _codes(kv) -> Optional[torch.Tensor]:
     return codes.keep[0] if isinstance(codes, KV) else codes
 
 
+def _parts(kv) -> tuple:
+    """Every tensor of a cache view: keys, values, block table, scales."""
+    if kv is None:
+        return ()
+    return tuple(x for t in kv.keep for x in (t.keep if isinstance(t, KV) else (t,)))
+
+
 def _int32(t: Optional[torch.Tensor], n: int, what: str) -> None:
     if t is not None and (t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous()):
         raise ValueError(f"{what} must be {n} contiguous int32 values")
@@ -668,7 +675,7 @@ def _append(fn, p: Problem, kv, k, v, cached, capacity, layer, n_layers, pos_ids
         elif q_out.dtype != dtype or q_out.numel() != M * hq * d or not q_out.is_contiguous():
             raise ValueError("q_out must be contiguous rows of q's type and size")
         a.q_out = q_out.data_ptr()
-    _on_gpu(k, v, q, q_out, cached, pos_ids, codes)
+    _on_gpu(k, v, q, q_out, cached, pos_ids, p.cu_d, *_parts(kv))
     a.cached = cached.data_ptr()
     if pos_ids is not None:
         a.pos_ids = pos_ids.data_ptr()
@@ -708,7 +715,7 @@ def cc_compact_kv8(p: Problem, kv: KV8, keep_idx: torch.Tensor, k: Sequence[int]
     for what, t in (("token_ids", token_ids), ("pos_ids", pos_ids)):
         if t is not None and (t.dtype != torch.int32 or t.numel() < N or not t.is_contiguous()):
             raise ValueError(f"{what} must be at least {N} contiguous int32 values")
-    _on_gpu(keep_idx, token_ids, pos_ids, _codes(kv), _codes(out) if out is not None else None)
+    _on_gpu(keep_idx, token_ids, pos_ids, p.cu_d, *_parts(kv), *_parts(out))
     _check(_lib.cc_compact_kv8(ctypes.byref(p.struct), ctypes.byref(kv.struct), _ptr(keep_idx), kk, per_head,
                                _ptr(token_ids), _ptr(pos_ids),
                                ctypes.byref(out.struct) if out is not None else None, _stream(stream)),
@@ -737,7 +744,7 @@ def cc_attention_kv8(p: Problem, q: torch.Tensor, kv: KV8, layer: int, kv_lens: 
         o = _empty(q.shape, q.dtype, q.device, stream)
     elif o.dtype != q.dtype or o.numel() != q.numel() or not o.is_contiguous():
         raise ValueError("o must be contiguous and of q's type and size")
-    _on_gpu(q, o, kv_lens, workspace, _codes(kv))
+    _on_gpu(q, o, kv_lens, workspace, p.cu_d, *_parts(kv))
     if workspace is None:
         workspace = _empty(max(1, cc_attention_kv8_workspace(p, mask, max_kv_len)), torch.uint8, q.device, stream)
     _check(_lib.cc_attention_kv8(ctypes.byref(s), _ptr(q), ctypes.byref(kv.struct), layer, _MASKS[mask],

@@ -386,3 +386,39 @@ def test_compaction_refuses_ids_of_another_type_or_too_few(monkeypatch, which):
     for n in (8, 11):
         with pytest.raises(cc.CCError):
             cc.cc_compact_kv8(p, kv, keep, [1, 1], 0, **{which: torch.zeros(n, dtype=torch.int32)})
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_every_tensor_of_a_cache_and_a_problem_is_looked_at(monkeypatch, paged):
+    """Values, scales, the block table and the problem's lengths count as much as the keys."""
+    seen = []
+    monkeypatch.setattr(cc, "_on_gpu", lambda *t: seen.append([id(x) for x in t if x is not None]))
+    monkeypatch.setattr(cc, "_stream", lambda s=None: None)
+    z = lambda *s, t=torch.uint8: torch.zeros(*s, dtype=t)
+    # (the library refuses layer 1 of one and a scale block of 8: nothing is launched)
+    kw = dict(n_layers=1, layer_stride=4096, head_stride=2048, tok_stride=64)
+    kw8 = dict(scale_block=8, scale_layer_stride=4, scale_head_stride=2)
+
+    def cache(eight):
+        pools = [z(2, 32, 64, t=torch.uint8 if eight else torch.bfloat16) for _ in range(2)]
+        scales = [z(2, 2) for _ in range(2)] if eight else []
+        table = [z(1, 2, t=torch.int32)] if paged else []
+        if eight:
+            kv = (cc.kv8_paged(*pools, *scales, *table, page_stride=4096, page_size=32, scale_page_stride=4, **kw, **kw8) if paged
+                  else cc.kv8_contiguous(*pools, *scales, **kw, **kw8))
+        else:
+            kv = cc.kv_paged(*pools, *table, page_stride=4096, page_size=32, **kw) if paged else cc.kv_contiguous(*pools, **kw)
+        return kv, pools + scales + table
+
+    p = cc.problem(dtype="bf16", cu_seqlens=[0, 2], n_heads_q=4, n_heads_kv=2, head_dim=64, hidden=64, vocab=1, rope_theta=1e4,
+                   device="cpu")
+    k, lens = z(2, 2, 64, t=torch.bfloat16), z(1, t=torch.int32)
+    (a, ta), (b, tb), (c, tc) = cache(False), cache(True), cache(True)
+    for call, parts in ((lambda: cc.cc_append_kv(p, a, k, k, lens, capacity=32, layer=1), ta),
+                        (lambda: cc.cc_append_kv8(p, b, k, k, lens, capacity=32), tb),
+                        (lambda: cc.cc_compact_kv8(p, b, lens, [1], 0, out=c), tb + tc),
+                        (lambda: cc.cc_attention_kv8(p, z(2, 4, 64, t=torch.bfloat16), b, 0, lens, 10, workspace=z(1 << 16)), tb)):
+        with pytest.raises(cc.CCError):
+            call()
+        missing = {id(x) for x in parts + [p.cu_d]} - set(seen[-1])
+        assert not missing
