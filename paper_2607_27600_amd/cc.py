@@ -756,16 +756,17 @@ def cc_attention_kv8(p: Problem, q: torch.Tensor, kv: KV8, layer: int, kv_lens: 
 
 @dataclass
 class Logprobs:
-    """Outputs of cc_lmhead_logprobs: [n], [n], [n][top], [n][top]."""
-    logprob: torch.Tensor
+    """Outputs of cc_lmhead_logprobs: [n] (None where no ids were given), [n], [n][top], [n][top]."""
+    logprob: Optional[torch.Tensor]
     entropy: torch.Tensor
     top_ids: torch.Tensor
     top_logprob: torch.Tensor
 
 
-def logprobs_out(n: int, top: int, device="cuda", stream=None) -> Logprobs:
+def logprobs_out(n: int, top: int, device="cuda", stream=None, ids: bool = True) -> Logprobs:
+    """Tensors for a call of n rows; ids: False for one that is given no words."""
     f = lambda *s: _empty(s, torch.float32, device, stream)
-    return Logprobs(f(n), f(n), _empty((n, top), torch.int32, device, stream), f(n, top))
+    return Logprobs(f(n) if ids else None, f(n), _empty((n, top), torch.int32, device, stream), f(n, top))
 
 
 def cc_lmhead_logprobs_workspace(dtype: str, n: int, vocab: int, hidden: int, top: int) -> int:
@@ -775,8 +776,9 @@ def cc_lmhead_logprobs_workspace(dtype: str, n: int, vocab: int, hidden: int, to
 def cc_lmhead_logprobs(dtype: str, u: torch.Tensor, w_lm: torch.Tensor, vocab: int, ids: Optional[torch.Tensor],
                        top: int, out: Optional[Logprobs] = None, *, packed: bool = False,
                        workspace: Optional[torch.Tensor] = None, stream=None) -> Logprobs:
-    """Log-probabilities of ids [n] (None: not taken), entropies and `top` alternatives of each hidden row u
-    [n][hidden] under the LM head w_lm [vocab][hidden] (packed: in the layout of cc_pack_lmhead)."""
+    """Log-probabilities of ids [n] (None: not taken, the result has none and out.logprob is left as it is),
+    entropies and `top` alternatives of each hidden row u [n][hidden] under the LM head w_lm [vocab][hidden]
+    (packed: in the layout of cc_pack_lmhead)."""
     n, hidden = u.shape
     _int32(ids, n, "ids")
     if not u.is_contiguous() or not w_lm.is_contiguous():
@@ -788,20 +790,24 @@ def cc_lmhead_logprobs(dtype: str, u: torch.Tensor, w_lm: torch.Tensor, vocab: i
     if packed and w_lm.numel() * w_lm.element_size() < cc_pack_lmhead_bytes(vocab, hidden):
         raise ValueError("w_lm holds less than a packed weight of that size")
     if out is None:
-        out = logprobs_out(n, top, u.device, stream)
+        out = logprobs_out(n, top, u.device, stream, ids is not None)
+    elif ids is None:
+        out = Logprobs(None, out.entropy, out.top_ids, out.top_logprob)
     if out.top_ids.numel() < n * top or out.top_logprob.numel() < n * top:
         raise ValueError(f"out has no room for {top} alternatives of {n} rows (top_ids, top_logprob)")
     f32 = torch.float32
     for what, t, m, want in (("logprob", out.logprob, n, f32), ("entropy", out.entropy, n, f32),
                              ("top_ids", out.top_ids, n * top, torch.int32),
                              ("top_logprob", out.top_logprob, n * top, f32)):
-        if t.dtype != want or t.numel() < m or not t.is_contiguous():
+        if what == "logprob" and ids is None:
+            continue
+        if t is None or t.dtype != want or t.numel() < m or not t.is_contiguous():
             raise ValueError(f"{what} must be at least {m} contiguous {want} values")
     _on_gpu(u, w_lm, ids, out.logprob, out.entropy, out.top_ids, out.top_logprob, workspace)
     if workspace is None:
         workspace = _empty(max(1, cc_lmhead_logprobs_workspace(dtype, n, vocab, hidden, top)), torch.uint8, u.device, stream)
     _check(_lib.cc_lmhead_logprobs({"f32": CC_F32, "bf16": CC_BF16}[dtype], _ptr(u), _ptr(w_lm), int(packed), n,
-                                   vocab, hidden, _ptr(ids), top, _ptr(out.logprob) if ids is not None else None,
+                                   vocab, hidden, _ptr(ids), top, _ptr(out.logprob),
                                    _ptr(out.entropy), _ptr(out.top_ids) if top else None,
                                    _ptr(out.top_logprob) if top else None, _ptr(workspace), workspace.numel(),
                                    _stream(stream)), "cc_lmhead_logprobs")

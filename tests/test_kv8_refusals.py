@@ -422,3 +422,25 @@ def test_every_tensor_of_a_cache_and_a_problem_is_looked_at(monkeypatch, paged):
             call()
         missing = {id(x) for x in parts + [p.cu_d]} - set(seen[-1])
         assert not missing
+
+
+def test_logprobs_without_ids_have_no_logprob(monkeypatch):
+    """No words given: none of the result is memory that nothing wrote."""
+    calls = []
+    monkeypatch.setattr(cc, "_on_gpu", lambda *t: None)
+    monkeypatch.setattr(cc, "_stream", lambda s=None: None)
+    monkeypatch.setattr(cc._lib, "cc_lmhead_logprobs", lambda *a: calls.append(a) or cc.CC_OK)
+    u, w = torch.zeros(3, 64, dtype=torch.bfloat16), torch.zeros(5, 64, dtype=torch.bfloat16)
+    r = cc.cc_lmhead_logprobs("bf16", u, w, 5, None, 2)
+    assert r.logprob is None and r.entropy.shape == (3,) and r.top_ids.shape == (3, 2)
+    out = cc.logprobs_out(3, 2, "cpu")
+    out.logprob.fill_(7)
+    r = cc.cc_lmhead_logprobs("bf16", u, w, 5, None, 2, out)
+    assert r.logprob is None and r.entropy is out.entropy and torch.equal(out.logprob, torch.full((3,), 7.0))
+    r = cc.cc_lmhead_logprobs("bf16", u, w, 5, None, 2, cc.logprobs_out(3, 2, "cpu", ids=False))
+    assert r.logprob is None
+    assert all(a[7] is None and a[9] is None for a in calls)   # ids and logprob
+    with pytest.raises(ValueError, match="logprob"):
+        cc.cc_lmhead_logprobs("bf16", u, w, 5, torch.zeros(3, dtype=torch.int32), 2, cc.logprobs_out(3, 2, "cpu", ids=False))
+    r = cc.cc_lmhead_logprobs("bf16", u, w, 5, torch.zeros(3, dtype=torch.int32), 2, out)
+    assert r is out and calls[-1][9].value == out.logprob.data_ptr()
