@@ -322,11 +322,13 @@ __device__ __forceinline__ uint32_t e8m0_of(uint32_t m_bits) {
   const int e = int(m_bits >> 23) - 8 + ((m_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
   return e < int(kScaleLow) ? kScaleLow : uint32_t(e);
 }
-// The scale 2^(x - 127) and, for x >= kScaleLow, its inverse.
+// The scale 2^(x - 127) and, for x >= kScaleLow, its inverse (of 2^127 a subnormal number).
 __device__ __forceinline__ float e8m0_scale(uint32_t x) {
   return __uint_as_float(x == 0 ? 0x00400000u : min(x, 254u) << 23);
 }
-__device__ __forceinline__ float e8m0_inverse(uint32_t x) { return __uint_as_float((254u - x) << 23); }
+__device__ __forceinline__ float e8m0_inverse(uint32_t x) {
+  return __uint_as_float(x >= 254u ? 0x00400000u : (254u - x) << 23);
+}
 
 // Four floats -> four E4M3 codes, round to nearest even (NaN: the NaN code).
 __device__ __forceinline__ uint32_t e4m3_pack(float a, float b, float c, float d) {

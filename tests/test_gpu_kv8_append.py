@@ -256,3 +256,40 @@ def test_append_token_by_token_follows_device_lengths_in_a_graph():
     for t in a:
         np.testing.assert_array_equal(a[t], b[t])
     assert lens2.tolist() == [35, 49, 66]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_to_a_block_of_the_largest_scale(d, dtype):
+    """A held block of scale byte 254, 2^127: new elements of up to 2^128 are rounded in it, not lost; byte 255
+    reads as 254."""
+    from paper_2607_27600_amd import cc
+    cache = Cache8([5, 3], 2, d, block=16, room=32, seed=61)
+    T = torch.bfloat16 if dtype == "bf16" else torch.float32
+    for t in ("k", "v"):
+        for b, n in ((0, 5), (1, 3)):
+            for hh in range(2):
+                codes, sc = cache.plane(0, b, hh, t, n=n)
+                sc[:] = 254 + (b == 1)
+                cache.put(0, b, hh, t, codes, sc)
+        cache.t[t + "s"].copy_(torch.from_numpy(cache.host[t + "s"]))
+    # magnitudes 2^119 to 2^128, in steps that the type holds: in units of the scale from 2^-8 to 2
+    g = torch.Generator().manual_seed(62)
+    x = (torch.randint(128, 256, (6, 6, d), generator=g).float() * torch.exp2(torch.randint(112, 121, (6, 6, 1), generator=g).float())
+         * torch.where(torch.rand(6, 6, d, generator=g) < 0.5, -1.0, 1.0)).to(T)
+    assert torch.isfinite(x).all()
+    q, k, v = x.cuda().split([2, 2, 2], 1)
+    p = _problem(cc, [4, 2], 2, 2, d, dtype)
+    cc.cc_append_kv8(p, cache.view(cc), k, v, i32([5, 3]), capacity=cache.cap, rotate=False)
+    torch.cuda.synchronize()
+    after, h = cache.read(), f64(x)
+    for b, n, at, m in ((0, 5, 0, 4), (1, 3, 4, 2)):
+        for hh in range(2):
+            for t, off in (("k", 2), ("v", 4)):
+                c, s = cache.plane(0, b, hh, t)
+                s[0] = 254
+                O8.append(c, s, n, h[at:at + m, off + hh], 16, cache.cap)
+                gc, gs = cache.plane(0, b, hh, t, src=after)
+                assert gs[0] == s[0] == 254
+                assert np.all(c[n:n + m] & 0x7f)     # all of them above 2^-9 of the scale
+                np.testing.assert_array_equal(gc, c)
