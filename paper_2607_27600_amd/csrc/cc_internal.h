@@ -317,7 +317,7 @@ struct Kv8View {
 constexpr uint32_t kScaleLow = 27;
 
 // Exponent byte of the smallest power of two s with m <= 448 s (448 = 1.75 * 2^8), from the bits of
-// m >= 0 (finite).
+// m >= 0 (finite, or with an exponent up to 262).
 __device__ __forceinline__ uint32_t e8m0_of(uint32_t m_bits) {
   const int e = int(m_bits >> 23) - 8 + ((m_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
   return e < int(kScaleLow) ? kScaleLow : uint32_t(e);

@@ -68,8 +68,10 @@ __device__ __forceinline__ void move_ids(const Args& a, const CompactList& L) {
   }
 }
 
-// Largest magnitude of 16 codes times their scale, as fp32 bits.  Codes without their sign rise with
-// the magnitudes, two to a 32-bit word by packed 16-bit maxima; 0x7f is NaN and does not count.
+// Largest magnitude of 16 codes times their scale, in the bits of an fp32 number whose exponent goes on past
+// 255 (2^127 times 448 has 262; those of numbers rise with them as whole numbers; 0: nothing above 2^-127, far
+// below the smallest scale).  Codes without their sign rise with the magnitudes, two to a 32-bit word by packed
+// 16-bit maxima; 0x7f is NaN and does not count.
 __device__ __forceinline__ uint32_t top_of(const uint4& w, uint32_t sc) {
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};
@@ -89,10 +91,15 @@ __device__ __forceinline__ uint32_t top_of(const uint4& w, uint32_t sc) {
     }
   }
   const auto f = __builtin_amdgcn_cvt_pk_f32_fp8(int(c), false);
-  return __float_as_uint(f[0] * e8m0_scale(sc));
+  const int bits = int(__float_as_uint(f[0]) >> 9);   // (of a code: 9 trailing bits are zeros)
+  const int e = int(min(sc, 254u)) - 127;
+  return c == 0 ? 0u : uint32_t(max(bits + (e << 14), 0)) << 9;
 }
 
-__device__ __forceinline__ uint4 rescale(const uint4& w, float f) {
+// Codes in the scale 2^(from - 127), in the scale 2^(to - 127).
+__device__ __forceinline__ uint4 rescale(const uint4& w, uint32_t from, uint32_t to) {
+  // A scale more than 2^18 larger than the block's belongs to zeros and NaN alone; one 2^19 smaller leaves zeros.
+  const float f = __uint_as_float(uint32_t(min(max(127 + int(min(from, 254u)) - int(to), 27), 227)) << 23);
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};
   uint32_t y[4];
 #pragma unroll
@@ -199,9 +206,7 @@ __global__ __launch_bounds__(NT) void compact8_kernel(Args a) {
       if (j < k) {
         const uint32_t e = e8m0_of(top[r >> shift]);
         uint4 w = now.w[u];
-        // (a scale more than 2^18 larger than the block's belongs to zeros and NaN alone; up to 2^220 it may be,
-        // past fp32, and infinity is no scale)
-        if (e != now.sc[u]) w = rescale(w, fminf(e8m0_scale(now.sc[u]) * e8m0_inverse(e), 0x1p100f));
+        if (e != now.sc[u]) w = rescale(w, now.sc[u], e);
         const int slot = dv.paged ? j & dv.codes.page_mask : j;
         *reinterpret_cast<uint4*>(db + int64_t(dpage[u]) * dv.codes.page_stride + int64_t(slot) * dv.codes.tok_stride) = w;
         if (col == 0 && (r & ((1 << shift) - 1)) == 0) ds[int64_t(dpage[u]) * dv.s_page + (slot >> shift)] = uint8_t(e);

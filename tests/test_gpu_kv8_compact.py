@@ -191,3 +191,34 @@ def test_pages_of_another_size(page, page2):
                 gc, gs = dst.plane(0, b, h, t, src=after, n=len(kl))
                 np.testing.assert_array_equal(gc, codes)
                 np.testing.assert_array_equal(gs, sc)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_largest_scales(d, in_place):
+    """Scales from 2^119 to 2^127 (byte 255 reads as 254), whose elements pass fp32: kept where they are the
+    block's largest, rounded again where others are."""
+    from paper_2607_27600_amd import cc
+    r = np.random.default_rng(24)
+    n = 176
+    c = Cache8([n], 1, d, block=16, seed=25)
+    codes, sc = c.plane(0, 0, 0, "k", n=n)
+    codes = (r.integers(0, 127, codes.shape) | (r.integers(0, 2, codes.shape) << 7)).astype(np.uint8)
+    codes[1, 3], codes[40, 4], codes[100] = 0x7f, 0xff, 0
+    sc[:] = [246, 247, 248, 250, 252, 253, 254, 255, 253, 27, 249]
+    c.put(0, 0, 0, "k", codes, sc)
+    for t in ("k", "ks"):
+        c.t[t].copy_(torch.from_numpy(c.host[t]))
+    # a destination block of each kind: of one source scale, of several, with and without those past fp32
+    kl = np.concatenate([np.arange(0, 30, 2), np.arange(31, 60, 3), np.arange(64, 176, 5)]).astype(np.int32)
+    p = cc.problem(dtype="bf16", cu_seqlens=[0, n], n_heads_q=1, n_heads_kv=1, head_dim=d, hidden=64, vocab=1)
+    dst = c if in_place else Cache8([n], 1, d, block=16, seed=26)
+    cc.cc_compact_kv8(p, c.view(cc), torch.from_numpy(kl).cuda(), [len(kl)], 0, out=None if in_place else dst.view(cc))
+    torch.cuda.synchronize()
+    want, ws = O8.compact(codes, np.minimum(sc, 254), kl, 16)
+    gc, gs = dst.plane(0, 0, 0, "k", src=dst.read(), n=len(kl))
+    assert ws.max() == 254 and ws.min() < 250
+    np.testing.assert_array_equal(gs, ws)
+    nan = (want & 0x7f) == 0x7f
+    np.testing.assert_array_equal((gc & 0x7f) == 0x7f, nan)
+    np.testing.assert_array_equal(gc[~nan], want[~nan])
