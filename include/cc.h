@@ -465,8 +465,10 @@ cc_status cc_attention_kv8_workspace(const cc_problem* p, int32_t mask, int32_t 
  * negative ones are 0), sizes the launch and the workspace.  The pages of a sequence's entries
  * have valid ids; tok_stride is below 2^28.  Entries past kv_lens[b] are not read, and one that
  * a query may not attend to does not reach it, whatever it holds; a NaN code in one that it
- * attends to gives NaN.  Sums, maxima and outputs are kept in fp32 until the last rounding; the
- * probabilities enter the second product in bf16. */
+ * attends to gives NaN.  Elements are taken in bf16 (exactly, from 2^-126 to below 2^128; those of
+ * 2^128 and more, which scales above 2^119 can have, are infinite and make what they reach infinite or NaN).
+ * Sums, maxima and outputs are kept in fp32 until the last rounding; the probabilities enter
+ * the second product in bf16. */
 cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv, int32_t layer,
                            int32_t mask, const int32_t* kv_lens, int32_t max_kv_len, void* o,
                            void* workspace, size_t workspace_bytes, void* stream);

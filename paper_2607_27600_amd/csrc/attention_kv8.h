@@ -23,6 +23,17 @@ constexpr int KV8_LIST = 64;     // sequences of a launch listed by value
 constexpr int MANY_ROWS = 128;   // rows of a block of the kernel for many
 constexpr int MANY_KEYS = 64;    // entries of its tiles
 
+// Codes that are not finite in bf16: NaN (0x7f), and under scales from 2^120 on those from 2^128 / scale, whose
+// codes are (262 - x) * 8 and above for the scale's byte x.  `wide_of(x)` in every byte, added to four codes
+// without their signs, raises bit 7 of those that are not.
+__device__ __forceinline__ uint32_t wide_of(uint32_t scale_byte) {
+  return uint32_t(max(1, 8 * int(min(scale_byte, 254u)) - 1968)) * 0x01010101u;
+}
+// Bytes 0x80 where a byte of x is such a code.
+__device__ __forceinline__ uint32_t wide_bytes(uint32_t x, uint32_t wide) { return ((x & 0x7f7f7f7fu) + wide) & 0x80808080u; }
+// Bytes 0xff at bytes 0x80.
+__device__ __forceinline__ uint32_t whole_bytes(uint32_t m) { return (m >> 7) * 0xffu; }
+
 // One class of sequences (few or many rows) of a call.
 struct Kv8Args {
   const u16* q;

@@ -11,16 +11,17 @@
 // (maximum, sum, output) are joined by a third kernel, in the pieces' order.
 //
 // Numbers.  E4M3 has 4 significant bits and the scales are powers of two, so entries become bf16
-// exactly (one conversion instruction for two codes, scale included); products accumulate in
-// fp32; a row's maximum and sum are fp32, the reference maximum moving only when it is passed by 2^8
+// exactly wherever it reaches, from 2^-126 to below 2^128 (one conversion instruction for two codes, scale
+// included; scales of 2^-100 to 2^119 stay inside, from 2^120 on the largest elements are infinite); products
+// accumulate in fp32; a row's maximum and sum are fp32, the reference maximum moving only when it is passed by 2^8
 // (numerator and sum share it).  The probabilities are rounded to bf16 for the second product (each by
 // up to 2^-8 of itself, independently: what the output's own rounding costs), the sum takes them unrounded.
 //
 // Masked entries.  Scores are replaced, not added to, so what a masked key holds is lost.  A masked
-// value meets a probability of 0, and 0 * NaN would reach the output: values past the sequence are
-// zeroed as they are read, and in tiles that some row sees in part, NaN codes are zeroed too and
-// counted by a second product of indicators, by the rows that may see them (the kernel for many marks
-// them instead).
+// value meets a probability of 0, and 0 times NaN or infinity would reach the output: values past the
+// sequence are zeroed as they are read, and in tiles that some row sees in part, NaN codes and infinite
+// elements are zeroed too and counted by a second product of indicators, by the rows that may see them, whose
+// outputs become NaN (the kernel for many marks them instead).
 #include <algorithm>
 
 #include "attention_kv8.h"
@@ -53,11 +54,6 @@ __device__ __forceinline__ bf16x8 widen44(uint32_t lo, uint32_t hi, float slo, f
   const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(hi), shi, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-
-// Bytes 0x80 where a byte of x is a NaN code (0x7f or 0xff).
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-// Bytes 0xff there.
-__device__ __forceinline__ uint32_t nan_mask(uint32_t x) { return (nan_bytes(x) >> 7) * 0xffu; }
 
 // 4 x 4 bytes transposed: word i of the result holds byte i of w[0..3].
 __device__ __forceinline__ void transpose4(const uint32_t (&w)[4], uint32_t (&t)[4]) {
@@ -455,6 +451,7 @@ __global__ __launch_bounds__(FEW_NT, 2) void attn_few(Kv8Args a) {
         bool nans = false;
         uint32_t hit[NR];
         if (masked) {
+          const uint32_t wide[2] = {wide_of(s0 >> 8), wide_of(s1 >> 8)};
 #pragma unroll
           for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -473,12 +470,12 @@ __global__ __launch_bounds__(FEW_NT, 2) void attn_few(Kv8Args a) {
 #pragma unroll
               for (int i = 0; i < NDB / 4; ++i) {
                 if (!in) st.v[4 * t + e][i] = 0;
-                nans |= nan_bytes(st.v[4 * t + e][i]) != 0;
+                nans |= wide_bytes(st.v[4 * t + e][i], wide[t]) != 0;
               }
             }
           nans = __any(nans);
           if (nans) {
-            // which outputs of this lane a NaN value reaches: a product of indicators
+            // which outputs of this lane such a value reaches: a product of indicators
 #pragma unroll
             for (int n = 0; n < NR; ++n) hit[n] = 0;
             bf16x8 see[NR];
@@ -494,8 +491,8 @@ __global__ __launch_bounds__(FEW_NT, 2) void attn_few(Kv8Args a) {
               uint32_t wa[4], wb[4], ta[4], tb[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                wa[e] = nan_mask(st.v[e][i]);
-                wb[e] = nan_mask(st.v[4 + e][i]);
+                wa[e] = whole_bytes(wide_bytes(st.v[e][i], wide[0]));
+                wb[e] = whole_bytes(wide_bytes(st.v[4 + e][i], wide[1]));
                 st.v[e][i] &= ~wa[e];
                 st.v[4 + e][i] &= ~wb[e];
               }

@@ -19,9 +19,9 @@
 // 32 heads on 8 in 166 us (830 TFLOP/s), against 144 us of cc_attention_cc on bf16 entries, which has 29
 // vector instructions where this has 39 and 8 scalar ones where this has 24.
 //
-// A NaN value in a tile that some rows see in part becomes the least bf16 number, 2^-133: nothing beside
-// fp32 sums, and told from every other value by its last bit (E4M3 values end in zeros).  A tile that
-// holds one sends its rows through a loop over its codes, which sets NaN where a row sees it.
+// A NaN or infinite value in a tile that some rows see in part becomes the least bf16 number, 2^-133:
+// nothing beside fp32 sums, and told from every other value by its last bit (E4M3 values end in zeros).  A
+// tile that holds one sends its rows through a loop over its codes, which sets NaN where a row sees it.
 #include <type_traits>
 
 #include "attention_kv8.h"
@@ -74,7 +74,7 @@ __device__ __forceinline__ const char* uniform_ptr(const char* p) {
   return reinterpret_cast<const char*>((uint64_t(hi) << 32) | lo);
 }
 
-// Sixteen codes times the scale, in bf16: exact.
+// Sixteen codes times the scale, in bf16.
 __device__ __forceinline__ void widen16(const uint4& w, float scale, uint4& lo, uint4& hi) {
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};
   uint32_t y[8];
@@ -238,15 +238,16 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
     };
     auto put = [&](u16* dst, int i, const uint4& z, int t, const At& at, auto values) {
       constexpr bool V = decltype(values)::value;
-      const float f = e8m0_scale((at.sc[i] >> (V ? 8 : 0)) & 255u);
+      const uint32_t byte = (at.sc[i] >> (V ? 8 : 0)) & 255u;
+      const float f = e8m0_scale(byte);
       uint4 y[2];
       if (V && is_masked(t)) {
         uint32_t w[4] = {z.x, z.y, z.z, z.w}, n[4];
         const bool out = t * BN + lrow + i * RSTEP >= len;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          n[k] = out ? 0 : ((w[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // 0x80 at a NaN code
-          w[k] = out ? 0 : w[k] & ~((n[k] >> 7) * 0xffu);
+          n[k] = out ? 0 : wide_bytes(w[k], wide_of(byte));
+          w[k] = out ? 0 : w[k] & ~whole_bytes(n[k]);
         }
         widen16(make_uint4(w[0], w[1], w[2], w[3]), f, y[0], y[1]);
         auto tag = [](uint32_t& lo, uint32_t& hi, uint32_t m) {
@@ -347,7 +348,7 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
     if (tb + 2 < te) __syncthreads();   // every wave has read K(tb) before its buffer is refilled
     float mx = row_max(sa);
 
-    // NaN into the outputs of rows that see a NaN value in tile t.
+    // NaN into the outputs of rows that see a NaN or infinite value in tile t.
     auto poison = [&](int t) {
 #pragma unroll 1
       for (int key = max(t * BN, lo); key < min(t * BN + BN, past); ++key) {
@@ -355,14 +356,15 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
         const int pg = a.k.paged ? table[gg >> (a.k.codes.page_shift - 4)] : 0;
         const int slot = a.k.paged ? key & a.k.codes.page_mask : key;
         const char* v = vplane + int64_t(pg) * a.k.codes.page_stride + int64_t(slot) * a.k.codes.tok_stride + 4 * hi;
+        const uint32_t wide = wide_of(vscale[int64_t(pg) * a.k.s_page + (slot >> a.k.block_shift)]);
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(v + db * 32 + q * 8);
+            const uint32_t n = wide_bytes(*reinterpret_cast<const uint32_t*>(v + db * 32 + q * 8), wide);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (((w >> (8 * e)) & 0x7fu) == 0x7fu) acc[db][q * 4 + e] = __uint_as_float(0x7fc00000u);
+              if ((n >> (8 * e)) & 0x80u) acc[db][q * 4 + e] = __uint_as_float(0x7fc00000u);
           }
       }
     };

@@ -356,3 +356,40 @@ def test_drafts_in_a_graph(new, hq, hkv, d):
         g.replay()
         torch.cuda.synchronize()
         assert_attention_close(f64(o), _oracle(cache, q, new, [n] * len(new), hq, hkv, "causal"), str(n))
+
+
+@pytest.mark.parametrize("byte,code", [(247, 0x78), (250, 0x7e), (254, 0xc0), (255, 0x40)])
+@pytest.mark.parametrize("new,n", [([4], 100), ([40], 200), ([150], 150)])
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("mask", ["causal", "counter"])
+def test_values_past_bf16_reach_only_rows_that_see_them(new, n, d, mask, byte, code):
+    """Elements of 2^128 and more, which are infinite in bf16 (the first is what appending 3.4e38 writes): a row
+    that may not see one is as if it held zero, a row that sees it is not finite there."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, m = 4, 2, new[0]
+    print(f"[attn8 wide] {new} {n} {d} {mask} {byte}", flush=True)
+    cache = Cache8([n], hkv, d, page=16, block=16, seed=81, fill=0x7f, room=64)
+    tv, tk, dims = n - 2, n - 1 - m // 2, [5, d - 1]
+    want = None
+    for held in (False, True):   # (the 64-bit result of rows that do not see them: they hold zeros)
+        for c, t, which in ((0, tv, "v"), (1, tk, "k")):
+            codes, sc = cache.plane(0, 0, c, which, n=n)
+            sc[t // 16] = byte
+            codes[t // 16 * 16:t // 16 * 16 + 16] = 0    # (others of the block: zeros)
+            if held:
+                codes[t, dims] = code
+            cache.put(0, 0, c, which, codes, sc)
+        if not held:
+            q = _q(new, hq, d, 82)
+            want = _oracle(cache, q, new, [n], hq, hkv, mask)
+    for t in ("k", "v", "ks", "vs"):
+        cache.t[t].copy_(torch.from_numpy(cache.host[t]))
+    o = f64(_run(cc, cache, q, new, [n], hq, hkv, mask))
+    at = np.arange(m) + n - m
+    sees = (lambda t: at >= t) if mask == "causal" else (lambda t: at < t)
+    assert sees(tv).any() and not sees(tv).all()
+    hit = np.zeros(want.shape, bool)
+    hit[np.ix_(sees(tv), [0, 1], dims)] = True
+    assert not np.isfinite(o[hit]).any()
+    hit[np.ix_(sees(tk), [2, 3])] = True       # (a logit past fp32 on one side or the other: nothing is asked)
+    assert_attention_close(np.where(hit, 0, o), np.where(hit, 0, want))
