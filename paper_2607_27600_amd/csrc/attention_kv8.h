@@ -45,6 +45,7 @@ struct Kv8Args {
   float c2;                      // scale * log2(e)
   int R;                         // most rows of a sequence of the class
   int piece, splits;             // many rows: entries of a piece, pieces of the longest sequence
+  int nth0;                      // many rows: first row block, in the order of a sequence, of a launch
   int direct, parts;             // few rows: a workgroup for each (sequence, head); else workgroups to share it all
   // Results to be joined (null: none), outputs and (maximum, sum): many rows
   // [splits][n_list][Hkv][R], few rows [parts + n_list * Hkv][R].

@@ -22,6 +22,7 @@
 // A NaN or infinite value in a tile that some rows see in part becomes the least bf16 number, 2^-133:
 // nothing beside fp32 sums, and told from every other value by its last bit (E4M3 values end in zeros).  A
 // tile that holds one sends its rows through a loop over its codes, which sets NaN where a row sees it.
+#include <algorithm>
 #include <type_traits>
 
 #include "attention_kv8.h"
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
   x /= a.splits;
   const int kvh = x % a.hkv;
   x /= a.hkv;
-  const int j = x % a.n_list, nth = x / a.n_list;
+  const int j = x % a.n_list, nth = a.nth0 + x / a.n_list;
   const int b = a.listed ? a.list[j] : j;
   const int q0 = a.cu[b], m = a.cu[b + 1] - q0;
   const int rows = m * a.g;
@@ -544,14 +545,24 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
 
 }  // namespace
 
-hipError_t launch_attn_many(const Kv8Args& a, hipStream_t s) {
-  const int64_t grid = int64_t((a.R + MANY_ROWS - 1) / MANY_ROWS) * a.n_list * a.hkv * a.splits;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  if (a.head_dim == 128)
-    hipLaunchKernelGGL(attn_many<128>, dim3(unsigned(grid)), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL(attn_many<64>, dim3(unsigned(grid)), dim3(256), 0, s, a);
-  return hipGetLastError();
+hipError_t launch_attn_many(const Kv8Args& args, hipStream_t s) {
+  // A workgroup for each row block of the longest sequence, sequence, head and piece.  A long sequence among many
+  // short ones makes more of these than one launch may have: row blocks are shared out over launches.
+  const int blocks = int((int64_t(args.R) + MANY_ROWS - 1) / MANY_ROWS);
+  const int64_t each = int64_t(args.n_list) * args.hkv * args.splits;
+  if (each > MOST_GROUPS) return hipErrorInvalidValue;   // (refused by the planner)
+  const int most = int(MOST_GROUPS / each);
+  Kv8Args a = args;
+  for (a.nth0 = 0; a.nth0 < blocks; a.nth0 += most) {
+    const dim3 grid(unsigned(each * std::min(most, blocks - a.nth0)));
+    if (a.head_dim == 128)
+      hipLaunchKernelGGL(attn_many<128>, grid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL(attn_many<64>, grid, dim3(256), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace cc

@@ -1156,6 +1156,16 @@ Kv8Class kv8_class(const cc_problem* p, int max_len, bool few) {
   return c;
 }
 
+// Both classes of a call, few rows first.
+cc_status kv8_plan(const cc_problem* p, int max_len, Kv8Class (&c)[2]) {
+  for (int i = 0; i < 2; ++i) {
+    c[i] = kv8_class(p, max_len, i == 0);
+    // what every launch of a class has a workgroup for
+    if (int64_t(c[i].n_list) * p->n_heads_kv * c[i].splits > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+  }
+  return CC_OK;
+}
+
 cc_status check_attention8(const cc_problem* p, int32_t mask, int32_t max_len) {
   CC_TRY(check_problem(p));
   if (mask != CC_MASK_CAUSAL && mask != CC_MASK_COUNTER_CAUSAL) return CC_ERR_ARG;
@@ -1172,7 +1182,9 @@ extern "C" {
 cc_status cc_attention_kv8_workspace(const cc_problem* p, int32_t mask, int32_t max_kv_len, size_t* bytes) {
   if (!bytes) return CC_ERR_ARG;
   CC_TRY(check_attention8(p, mask, max_kv_len));
-  *bytes = kv8_class(p, max_kv_len, true).total + kv8_class(p, max_kv_len, false).total;
+  Kv8Class classes[2];
+  CC_TRY(kv8_plan(p, max_kv_len, classes));
+  *bytes = classes[0].total + classes[1].total;
   return CC_OK;
 }
 
@@ -1185,7 +1197,8 @@ cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv,
   if (kv->codes.tok_stride >= int64_t(1) << 28) return CC_ERR_UNSUPPORTED;   // 16 entries by 32-bit offsets
   const int N = n_tokens(p);
   if (N > 0 && (!q || !o || !kv_lens || !aligned16(q) || !aligned16(o))) return CC_ERR_ARG;
-  const Kv8Class classes[2] = {kv8_class(p, max_kv_len, true), kv8_class(p, max_kv_len, false)};
+  Kv8Class classes[2];
+  CC_TRY(kv8_plan(p, max_kv_len, classes));
   CC_TRY(check_ws(ws, ws_bytes, classes[0].total + classes[1].total));
   if (N == 0) return CC_OK;
   size_t off = 0;
@@ -1211,6 +1224,7 @@ cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv,
     a.R = c.R;
     a.piece = c.piece;
     a.splits = c.splits;
+    a.nth0 = 0;
     a.direct = c.direct;
     a.parts = c.parts;
     a.part = c.total ? reinterpret_cast<float*>(at(ws, off)) : nullptr;

@@ -302,6 +302,9 @@ hipError_t launch_enter(const void* embed, const int32_t* ids, const int32_t* po
 hipError_t launch_residual_rmsnorm(const float* part, int S, float* h, const void* gamma, void* y,
                                    int N, int D, float eps, hipStream_t s);
 
+// A launch has fewer than 2^32 threads: the most workgroups of 256.
+constexpr int64_t MOST_GROUPS = (int64_t(1) << 24) - 1;
+
 // ------------------------------------------------------------------ cache in 8 bits
 // One tensor (keys or values) of a cache in 8 bits: E4M3 codes (strides in bytes) and the scales'
 // exponent bytes.

@@ -6,7 +6,7 @@ import torch
 
 from oracle import kv8_oracle as O8
 from tests.gpu_util import assert_attention_close, f64
-from tests.kv8_util import Cache8, cu_of, i32
+from tests.kv8_util import Cache8, cu_of, i32, quantize
 
 pytestmark = pytest.mark.gpu
 
@@ -393,3 +393,36 @@ def test_values_past_bf16_reach_only_rows_that_see_them(new, n, d, mask, byte, c
     assert not np.isfinite(o[hit]).any()
     hit[np.ix_(sees(tk), [2, 3])] = True       # (a logit past fp32 on one side or the other: nothing is asked)
     assert_attention_close(np.where(hit, 0, o), np.where(hit, 0, want))
+
+
+def test_more_row_blocks_than_one_launch_has():
+    """A long chunk beside hundreds of short ones, 64 heads: (blocks of the longest) * sequences * heads passes
+    2^24 workgroups; the long one's last block comes with a second launch."""
+    from paper_2607_27600_amd import cc
+    n_seqs, h, d, n, short = 600, 64, 64, 64, 33
+    long = 436 * 128 + 77
+    assert 437 * n_seqs * h >= 1 << 24 > 436 * n_seqs * h
+    new = [short] * n_seqs
+    new[7] = long
+    r = np.random.default_rng(91)
+    # one plane a head, which all sequences share
+    codes, scales = zip(*(quantize(r.normal(0, 1, (n, d)), 16) for _ in range(2 * h)))
+    t = lambda x: torch.from_numpy(np.stack(x)).cuda()
+    k, v, ks, vs = t(codes[:h]), t(codes[h:]), t(scales[:h]), t(scales[h:])
+    kv = cc.kv8_contiguous(k, v, ks, vs, n_layers=1, layer_stride=0, head_stride=n * d, tok_stride=d, scale_block=16,
+                           scale_layer_stride=0, scale_head_stride=n // 16)
+    q = torch.randn(sum(new), h, d, generator=torch.Generator("cuda").manual_seed(92), device="cuda").to(torch.bfloat16)
+    o = torch.full_like(q, 7.0)
+    cc.cc_attention_kv8(_problem(cc, new, h, h, d), q, kv, 0, i32([n] * n_seqs), n, o, mask="counter")
+    torch.cuda.synchronize()
+    cu = cu_of(new)
+    val = lambda c, s, i: O8.values(c[i], s[i], 16)
+    for b, i0, i1 in ((0, 0, short), (7, 0, 130), (7, 200 * 128, 200 * 128 + 8), (7, 436 * 128 - 3, long), (8, 0, short),
+                      (n_seqs - 1, 0, short)):
+        for c in (0, 31, 63):
+            qq = f64(q[cu[b]:cu[b + 1], c])
+            kk, vv = val(codes[:h], scales[:h], c), val(codes[h:], scales[h:], c)
+            # (rows of a sequence stand at its cache's end: those asked for, as the last of a shorter one)
+            want = O8.attention(qq[i0:], kk, vv, "counter")[: i1 - i0]
+            assert_attention_close(f64(o[cu[b] + i0:cu[b] + i1, c])[:, None], want[:, None], f"{b} {i0} {c}")
+    assert not (o == 7.0).all(-1).any()     # every row has been written

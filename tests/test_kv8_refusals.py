@@ -444,3 +444,17 @@ def test_logprobs_without_ids_have_no_logprob(monkeypatch):
         cc.cc_lmhead_logprobs("bf16", u, w, 5, torch.zeros(3, dtype=torch.int32), 2, cc.logprobs_out(3, 2, "cpu", ids=False))
     r = cc.cc_lmhead_logprobs("bf16", u, w, 5, torch.zeros(3, dtype=torch.int32), 2, out)
     assert r is out and calls[-1][9].value == out.logprob.data_ptr()
+
+
+def test_attention_refuses_more_sequences_than_a_launch_has_workgroups():
+    """2^24 workgroups of 256 threads and more are not to be had: said before anything is queued."""
+    f, q, n = cc._lib.cc_attention_kv8, cc._lib.cc_attention_kv8_workspace, ctypes.c_size_t()
+    kv = _kv8(paged=False)
+    for rows in (1, 33):    # both kernels
+        for seqs, ok in ((1 << 18, False), ((1 << 18) - 1, True)):
+            p = _problem(range(0, rows * seqs + 1, rows), n_heads_q=64, n_heads_kv=64, head_dim=64)
+            for longest in (100, 100000):
+                st = q(_ref(p), 0, longest, _ref(n))
+                assert st == (cc.CC_OK if ok else cc.CC_ERR_UNSUPPORTED)
+                if not ok:
+                    assert f(_ref(p), P, _ref(kv), 0, 0, P, longest, P, P, 1 << 50, None) == cc.CC_ERR_UNSUPPORTED
