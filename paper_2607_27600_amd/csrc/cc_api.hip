@@ -1069,6 +1069,7 @@ cc_status cc_compact_kv8(const cc_problem* p, const cc_kv8* kv, const int32_t* k
   }
   const int hkv = p->n_heads_kv, per = per_head ? hkv : 1;
   if (per > COMPACT_INLINE) return CC_ERR_UNSUPPORTED;   // the lists of a sequence travel with one launch
+  if (int64_t(hkv) * kv->codes.n_layers >= 1 << 20) return CC_ERR_UNSUPPORTED;   // as do its planes
   int64_t off = 0;
   for (int64_t i = 0; i < int64_t(p->n_seqs) * per; ++i) {
     const int b = int(i / per);

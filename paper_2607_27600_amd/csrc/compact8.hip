@@ -29,7 +29,7 @@ struct Args {
   Kv8View src[2], dst[2];
   const int32_t* keep;
   int n_layers, n_heads, per_head;
-  int chunks;                  // workgroups of a plane (in place: 1)
+  int chunks, chunk0;          // workgroups of a plane (in place: 1), and the first of the launch
   int id_blocks;
   int32_t* ids[2];
   const int32_t* cu;
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(NT) void compact8_kernel(Args a) {
   int i = blockIdx.x - a.id_blocks;
   int c = 0;
   if constexpr (!INPLACE) {
-    c = i % a.chunks;
+    c = a.chunk0 + i % a.chunks;
     i /= a.chunks;
   }
   const int which = i & 1;
@@ -226,7 +226,12 @@ template <int HD>
 hipError_t launch_dim(const Compact8Launch& l, hipStream_t s) {
   constexpr int NT = 256, NT_IN = 1024, CHUNK = NT / (HD / 16) * U;
   const int per = l.per_head ? l.n_heads : 1;
-  const int per_launch = LISTS / per;   // sequences
+  // Sequences of a launch: their lists by value, a workgroup for each plane.  A launch has fewer than 2^32 threads,
+  // so long lists out of place take several, each a range of their chunks.
+  const int64_t planes = 2 * int64_t(l.n_heads) * l.n_layers;
+  const int64_t most = (l.in_place ? MOST_GROUPS * 256 / NT_IN : MOST_GROUPS) - LISTS;   // (workgroups for ids aside)
+  if (planes > most) return hipErrorInvalidValue;   // (refused by the caller)
+  const int per_launch = int(std::min<int64_t>(LISTS / per, most / planes));
   int64_t off = 0;
   for (int lo = 0; lo < l.n_seqs; lo += per_launch) {
     Args a;
@@ -248,8 +253,8 @@ hipError_t launch_dim(const Compact8Launch& l, hipStream_t s) {
       for (int h = 0; h < per; ++h) off += k_h[b * per + h];
     }
     std::sort(order, order + n, [&](int x, int y) { return longest[x] != longest[y] ? longest[x] > longest[y] : x < y; });
-    const int most = longest[order[0]];
-    if (most == 0) continue;
+    const int longest_list = longest[order[0]];
+    if (longest_list == 0) continue;
     for (int i = 0; i < n; ++i) {
       int64_t at = first[order[i]];
       for (int h = 0; h < per; ++h) {
@@ -263,15 +268,19 @@ hipError_t launch_dim(const Compact8Launch& l, hipStream_t s) {
     a.per_head = l.per_head;
     a.cu = l.cu_d;
     a.id_blocks = l.ids[0] || l.ids[1] ? n : 0;
-    a.chunks = l.in_place ? 1 : (most + CHUNK - 1) / CHUNK;
-    const int64_t grid = a.id_blocks + int64_t(n) * l.n_heads * l.n_layers * 2 * a.chunks;
-    if (grid > INT32_MAX) return hipErrorInvalidValue;
-    if (l.in_place)
-      hipLaunchKernelGGL((compact8_kernel<HD, true, NT_IN>), dim3(unsigned(grid)), dim3(NT_IN), 0, s, a);
-    else
-      hipLaunchKernelGGL((compact8_kernel<HD, false, NT>), dim3(unsigned(grid)), dim3(NT), 0, s, a);
-    const hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
+    const int chunks = l.in_place ? 1 : (longest_list + CHUNK - 1) / CHUNK;
+    const int step = int(std::min<int64_t>(chunks, most / (n * planes)));
+    for (a.chunk0 = 0; a.chunk0 < chunks; a.chunk0 += step) {
+      a.chunks = std::min(step, chunks - a.chunk0);
+      const dim3 grid(unsigned(a.id_blocks + n * planes * a.chunks));
+      if (l.in_place)
+        hipLaunchKernelGGL((compact8_kernel<HD, true, NT_IN>), grid, dim3(NT_IN), 0, s, a);
+      else
+        hipLaunchKernelGGL((compact8_kernel<HD, false, NT>), grid, dim3(NT), 0, s, a);
+      const hipError_t err = hipGetLastError();
+      if (err != hipSuccess) return err;
+      a.id_blocks = 0;
+    }
   }
   return hipSuccess;
 }

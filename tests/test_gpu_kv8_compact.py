@@ -222,3 +222,55 @@ def test_the_largest_scales(d, in_place):
     nan = (want & 0x7f) == 0x7f
     np.testing.assert_array_equal((gc & 0x7f) == 0x7f, nan)
     np.testing.assert_array_equal(gc[~nan], want[~nan])
+
+
+def test_more_chunks_than_one_launch_has():
+    """Out of place, 64 lists of 32 layers and 64 heads, one of them so long that the chunks of all pass 2^24
+    workgroups: the longest list's last chunks come with a second launch.  Ids move once."""
+    from paper_2607_27600_amd import cc
+    layers, h, d, page, n = 32, 64, 64, 16, 16640
+    assert 64 * layers * h * 2 * (n // 256) >= 1 << 24 > 64 * layers * h * 2 * (n // 256 - 2)
+    free, _ = torch.cuda.mem_get_info()
+    if free < (12 << 30):
+        pytest.skip("needs 12 GiB of device memory")
+    lens = [n] + [40] * 63
+    per = n // page
+    pages = per + 63 * 3
+    table = torch.zeros(64, per, dtype=torch.int32)
+    table[0] = torch.arange(per)
+    table[1:, :3] = per + torch.arange(63 * 3).view(63, 3)
+    g = torch.Generator("cuda").manual_seed(27)
+    row = page * d
+    # one layer of codes for all; 448 in every row, so that kept blocks of kept blocks' scales are bit copies
+    src = torch.randint(0, 127, (pages, h, page, d), generator=g, device="cuda", dtype=torch.uint8)
+    src[..., 0] = 0x7e
+    ssc = torch.randint(100, 150, (pages, h), generator=g, device="cuda", dtype=torch.uint8)
+    dst = torch.zeros(layers, pages, h, page, d, dtype=torch.uint8, device="cuda")
+    dst_v, dsc = torch.zeros_like(dst), torch.zeros(layers, pages, h, dtype=torch.uint8, device="cuda")
+    dsc_v = torch.zeros_like(dsc)
+    kw = dict(n_layers=layers, page_stride=h * row, head_stride=row, tok_stride=d, page_size=page, scale_block=16,
+              scale_page_stride=h, scale_head_stride=1)
+    bt = table.cuda()
+    kv = cc.kv8_paged(src, src, ssc, ssc, bt, layer_stride=0, scale_layer_stride=0, **kw)
+    out = cc.kv8_paged(dst, dst_v, dsc, dsc_v, bt, layer_stride=pages * h * row, scale_layer_stride=pages * h, **kw)
+    p = cc.problem(dtype="bf16", cu_seqlens=cu_of(lens), n_heads_q=h, n_heads_kv=h, head_dim=d, hidden=64, vocab=1)
+    keep = [n] + [9] * 63
+    lists = torch.cat([torch.arange(n)] + [31 + torch.arange(9)] * 63).to(torch.int32).cuda()
+    ids = torch.arange(sum(lens), dtype=torch.int32, device="cuda")
+    cc.cc_compact_kv8(p, kv, lists, keep, 0, token_ids=ids, out=out)
+    torch.cuda.synchronize()
+    for got, gs in ((dst, dsc), (dst_v, dsc_v)):
+        for l in range(layers):
+            assert torch.equal(got[l, :per], src[:per]) and torch.equal(gs[l, :per], ssc[:per]), l
+    # the short lists: entries 31 to 39 of each, from its second and third pages
+    p1, p2 = per + 1, per + 2
+    x = torch.cat([src[p1::3, :, 15:], src[p2::3, :, :8]], 2)
+    top = torch.maximum(ssc[p1::3], ssc[p2::3])
+    got = dst_v[layers - 1, per::3]
+    assert torch.equal(dsc_v[layers - 1, per::3], top)
+    same = torch.cat([ssc[p1::3, :, None] == top[:, :, None], (ssc[p2::3] == top)[:, :, None].expand(-1, -1, 8)], 2)
+    assert torch.equal(got[:, :, :9][same], x[same])
+    assert torch.count_nonzero(got[:, :, 9:]) == 0
+    cu = cu_of(lens)
+    assert torch.equal(ids[cu[5]:cu[5] + 9].cpu(), cu[5] + 31 + torch.arange(9, dtype=torch.int32))
+    assert torch.equal(ids[:n].cpu(), torch.arange(n, dtype=torch.int32))

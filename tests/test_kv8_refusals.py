@@ -458,3 +458,10 @@ def test_attention_refuses_more_sequences_than_a_launch_has_workgroups():
                 assert st == (cc.CC_OK if ok else cc.CC_ERR_UNSUPPORTED)
                 if not ok:
                     assert f(_ref(p), P, _ref(kv), 0, 0, P, longest, P, P, 1 << 50, None) == cc.CC_ERR_UNSUPPORTED
+
+
+def test_compaction_refuses_more_planes_than_a_launch_has_workgroups():
+    f, p = cc._lib.cc_compact_kv8, _problem(n_heads_q=64, n_heads_kv=64)
+    k = (ctypes.c_int32 * 2)(1, 1)
+    for out in (None, _kv8(n_layers=1 << 14)):
+        assert f(_ref(p), _ref(_kv8(n_layers=1 << 14)), P, k, 0, None, None, out and _ref(out), None) == cc.CC_ERR_UNSUPPORTED
