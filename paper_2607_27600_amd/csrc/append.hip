@@ -17,6 +17,7 @@
 // 3166 ragged tokens into bf16 pages: 78 MB in 15.8 us, 4.9 TB/s, what a large copy reaches) and by the
 // round trips to lengths, then rows, for single tokens (eight: 4.9 us); a row is read 16 elements a lane
 // (e .. e + 7 and their partners), 16 bytes a load.
+#include <algorithm>
 #include <cmath>
 
 #include "cc_internal.h"
@@ -36,7 +37,7 @@ struct AppendArgs {
   void* q_out;
   const int32_t *cached, *pos, *cu;
   Kv8View kc, vc;
-  int n_seqs, M, layer, n_layers, hq, hkv, capacity, rotate;
+  int n_seqs, M, layer, hq, hkv, capacity, rotate;
   int shift;                 // log2 of the tokens of a key/value unit (a scale block)
   int each;                  // new tokens of every sequence, or -1: they differ
   int splits, heads;         // head ranges of a unit, heads of a range
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs<HD> a) {
 template <class T, int HD, bool F8>
 hipError_t launch_typed(const AppendLaunch& l, hipStream_t s) {
   AppendArgs<HD> a;
-  a.k = l.k;
+  a.k = l.k;   // (bases and first layer below)
   a.v = l.v;
   a.q = l.q;
   a.q_out = l.q_out;
@@ -317,8 +318,6 @@ hipError_t launch_typed(const AppendLaunch& l, hipStream_t s) {
   a.vc = l.vc;
   a.n_seqs = l.n_seqs;
   a.M = l.cu_h[l.n_seqs];
-  a.layer = l.layer;
-  a.n_layers = l.n_layers;
   a.hq = l.n_heads_q;
   a.hkv = l.n_heads_kv;
   a.capacity = l.capacity;
@@ -338,7 +337,7 @@ hipError_t launch_typed(const AppendLaunch& l, hipStream_t s) {
   a.heads = (a.hkv + a.splits - 1) / a.splits;
   a.splits = (a.hkv + a.heads - 1) / a.heads;
   const int64_t kv = 2 * blocks * a.splits, q = l.q.base ? (a.M + QT - 1) / QT : 0;
-  if ((kv + q) * l.n_layers > INT32_MAX) return hipErrorInvalidValue;
+  if (kv + q > MOST_GROUPS) return hipErrorInvalidValue;   // (refused by the caller)
   a.units_kv = int(kv);
   a.units_q = int(q);
   a.units = int(kv + q);
@@ -348,8 +347,17 @@ hipError_t launch_typed(const AppendLaunch& l, hipStream_t s) {
   }
   const int most = a.each >= 0 ? std::min(B, a.each) : B;
   const size_t lds = l.rotate ? size_t(std::max(most, QT)) * (HD / 2) * sizeof(float2) : 0;
-  hipLaunchKernelGGL((append_kernel<T, HD, F8>), dim3(unsigned(a.units * l.n_layers)), dim3(NT), lds, s, a);
-  return hipGetLastError();
+  // layers past one launch's workgroups go into further launches
+  const int step = int(MOST_GROUPS / a.units);
+  for (int lo = 0; lo < l.n_layers; lo += step) {
+    a.layer = l.layer + lo;
+    a.k.base = static_cast<const T*>(l.k.base) + lo * l.k.layer_stride;
+    a.v.base = static_cast<const T*>(l.v.base) + lo * l.v.layer_stride;
+    hipLaunchKernelGGL((append_kernel<T, HD, F8>), dim3(unsigned(a.units * std::min(step, l.n_layers - lo))), dim3(NT), lds, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <class T>

@@ -992,7 +992,10 @@ cc_status plan_append(const cc_problem* p, const cc_append* a, const cc_kv* kv, 
   const int64_t room = kv->layout == CC_KV_PAGED ? int64_t(kv->max_pages) * kv->page_size : INT32_MAX;
   if (a->capacity == 0 && kv->layout != CC_KV_PAGED) return CC_ERR_ARG;
   l.capacity = int(std::min<int64_t>({a->capacity ? a->capacity : room, room, INT32_MAX - 128}));
-  if (n_tokens(p) > 0) {
+  // one layer's workgroups: units of 16 tokens or more in ranges of up to 64 heads, of four tokens for queries
+  const int64_t M = n_tokens(p), ranges = (p->n_heads_kv + 63) / 64;
+  if (2 * (M / 16 + 2 * int64_t(p->n_seqs)) * ranges + M / 4 + 640 > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+  if (M > 0) {
     CC_TRY(check_rows(p, a->k));
     CC_TRY(check_rows(p, a->v));
     if (!a->cached) return CC_ERR_ARG;

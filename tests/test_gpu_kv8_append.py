@@ -293,3 +293,25 @@ def test_append_to_a_block_of_the_largest_scale(d, dtype):
                 assert gs[0] == s[0] == 254
                 assert np.all(c[n:n + m] & 0x7f)     # all of them above 2^-9 of the scale
                 np.testing.assert_array_equal(gc, c)
+
+
+def test_more_layers_than_one_launch_has_workgroups_for():
+    """One token each of 4096 sequences into 2100 layers: past 2^24 workgroups, the last layers come with a
+    second launch."""
+    from paper_2607_27600_amd import cc
+    n, layers, d = 4096, 2100, 64
+    assert 2 * n * layers >= 1 << 24
+    free, _ = torch.cuda.mem_get_info()
+    if free < (12 << 30):
+        pytest.skip("needs 12 GiB of device memory")
+    g = torch.Generator("cuda").manual_seed(63)
+    x = torch.randint(0, 30000, (2, layers, n, 1, d), generator=g, device="cuda", dtype=torch.int16).view(torch.bfloat16)
+    # a cache of two entries a sequence: the second is written
+    pools = [torch.zeros(layers, n, 2, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    kv = cc.kv_contiguous(*pools, n_layers=layers, layer_stride=n * 2 * d, seq_stride=2 * d, head_stride=0, tok_stride=d)
+    p = _problem(cc, [1] * n, 1, 1, d)
+    cc.cc_append_kv(p, kv, x[0], x[1], i32([1] * n), capacity=2, n_layers=layers, rotate=False)
+    torch.cuda.synchronize()
+    for pool, y in zip(pools, x):
+        assert torch.equal(pool[:, :, 1].view(torch.int16), y[:, :, 0].view(torch.int16))
+        assert torch.count_nonzero(pool[:, :, 0].view(torch.int16)) == 0

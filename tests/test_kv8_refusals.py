@@ -465,3 +465,11 @@ def test_compaction_refuses_more_planes_than_a_launch_has_workgroups():
     k = (ctypes.c_int32 * 2)(1, 1)
     for out in (None, _kv8(n_layers=1 << 14)):
         assert f(_ref(p), _ref(_kv8(n_layers=1 << 14)), P, k, 0, None, None, out and _ref(out), None) == cc.CC_ERR_UNSUPPORTED
+
+
+def test_append_refuses_more_tokens_than_a_launch_has_workgroups():
+    for cu in ((0, 1 << 26), range((1 << 22) + 1)):
+        for paged in (False, True):
+            p, kw = _problem(cu), dict(max_pages=1 << 23) if paged else {}
+            assert cc._lib.cc_append_kv8(_ref(p), _ref(_append(capacity=100)), _ref(_kv8(paged, **kw)), None) == cc.CC_ERR_UNSUPPORTED
+            assert cc._lib.cc_append_kv(_ref(p), _ref(_append(capacity=100)), _ref(_kv(paged, **kw)), None) == cc.CC_ERR_UNSUPPORTED
