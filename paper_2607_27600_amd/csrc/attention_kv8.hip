@@ -670,7 +670,7 @@ struct Joined {
 constexpr int JOIN_ALONE = 32;
 constexpr int JOIN_ONE = 1024;
 template <int HD, bool FEW>
-__global__ __launch_bounds__(256) void attn_join(Kv8Args a, int one) {
+__global__ __launch_bounds__(256) void attn_join(Kv8Args a, int one, int64_t group0) {
   constexpr int LPR = HD / 4, NG = 256 / LPR;
   __shared__ float4 po[256];
   __shared__ float2 pm[256];
@@ -679,7 +679,7 @@ __global__ __launch_bounds__(256) void attn_join(Kv8Args a, int one) {
   const int tid = threadIdx.x;
   const int gi = tid / LPR, lane = tid % LPR;
   const int64_t all = int64_t(a.n_list) * a.hkv * a.R;
-  const int64_t row_in = one ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * NG + gi;
+  const int64_t row_in = one ? int64_t(blockIdx.x) : (group0 + blockIdx.x) * NG + gi;
   const int d = lane * 4;
   const int r = int(row_in % a.R), jh = int(min(row_in / a.R, int64_t(a.n_list) * a.hkv - 1));
   const int kvh = jh % a.hkv, j = jh / a.hkv;
@@ -805,13 +805,17 @@ hipError_t launch_dim(const Kv8Args& a, bool few, hipStream_t s) {
   const int64_t rows = int64_t(a.n_list) * a.hkv * a.R;
   constexpr int NG = 256 / (HD / 4);
   const int one = rows <= JOIN_ONE;
-  const int64_t grid = one ? rows : (rows + NG - 1) / NG;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  if (few)
-    hipLaunchKernelGGL((attn_join<HD, true>), dim3(unsigned(grid)), dim3(256), 0, s, a, one);
-  else
-    hipLaunchKernelGGL((attn_join<HD, false>), dim3(unsigned(grid)), dim3(256), 0, s, a, one);
-  return hipGetLastError();
+  const int64_t groups = one ? rows : (rows + NG - 1) / NG;
+  for (int64_t group0 = 0; group0 < groups; group0 += MOST_GROUPS) {   // (more than a launch may have: several)
+    const dim3 grid(unsigned(std::min(MOST_GROUPS, groups - group0)));
+    if (few)
+      hipLaunchKernelGGL((attn_join<HD, true>), grid, dim3(256), 0, s, a, one, group0);
+    else
+      hipLaunchKernelGGL((attn_join<HD, false>), grid, dim3(256), 0, s, a, one, group0);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

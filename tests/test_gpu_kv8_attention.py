@@ -426,3 +426,37 @@ def test_more_row_blocks_than_one_launch_has():
             want = O8.attention(qq[i0:], kk, vv, "counter")[: i1 - i0]
             assert_attention_close(f64(o[cu[b] + i0:cu[b] + i1, c])[:, None], want[:, None], f"{b} {i0} {c}")
     assert not (o == 7.0).all(-1).any()     # every row has been written
+
+
+def test_more_rows_to_join_than_one_launch_has():
+    """Few rows of 130 sequences and 2^16 heads, 32 at the most: past 2^24 workgroups of the join, whose second
+    launch has the last sequences; of the last one, heads 877 and 3364 are cut between two workgroups' shares."""
+    from paper_2607_27600_amd import cc
+    n_seqs, h, d, n = 130, 1 << 16, 64, 2400
+    assert n_seqs * h * 32 // 16 >= 1 << 24 > (n_seqs - 3) * h * 32 // 16
+    new, lens = [1] * n_seqs, [3] * n_seqs
+    new[11], lens[11], lens[-1] = 32, 60, n
+    p = _problem(cc, new, h, h, d)
+    size = cc.cc_attention_kv8_workspace(p, "causal", n)
+    free, _ = torch.cuda.mem_get_info()
+    if free < size + (8 << 30):
+        pytest.skip(f"needs {(size >> 30) + 8} GiB of device memory")
+    r = np.random.default_rng(93)
+    # one plane, which all sequences and heads share
+    codes, scales = zip(*(quantize(r.normal(0, 1, (n, d)), 16) for _ in range(2)))
+    t = lambda x: torch.from_numpy(x).cuda()
+    kv = cc.kv8_contiguous(t(codes[0]), t(codes[1]), t(scales[0]), t(scales[1]), n_layers=1, layer_stride=0, head_stride=0,
+                           tok_stride=d, scale_block=16, scale_layer_stride=0, scale_head_stride=0)
+    q = torch.randn(sum(new), h, d, generator=torch.Generator("cuda").manual_seed(94), device="cuda").to(torch.bfloat16)
+    o = torch.full_like(q, 7.0)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    cc.cc_attention_kv8(p, q, kv, 0, i32(lens), n, o, workspace=ws)
+    torch.cuda.synchronize()
+    del ws
+    cu = cu_of(new)
+    for b in (0, 11, n_seqs - 3, n_seqs - 2, n_seqs - 1):
+        kk, vv = (O8.values(codes[i][:lens[b]], scales[i], 16) for i in (0, 1))
+        for c in (0, 877, 3364, h - 1):
+            want = O8.attention(f64(q[cu[b]:cu[b + 1], c]), kk, vv, "causal")
+            assert_attention_close(f64(o[cu[b]:cu[b + 1], c])[:, None], want[:, None], f"{b} {c}")
+    assert not (o == 7.0).all(-1).any()
