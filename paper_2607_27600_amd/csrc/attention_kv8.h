@@ -48,11 +48,15 @@ struct Kv8Args {
   int nth0;                      // many rows: first row block, in the order of a sequence, of a launch
   int direct, parts;             // few rows: a workgroup for each (sequence, head); else workgroups to share it all
   // Results to be joined (null: none), outputs and (maximum, sum): many rows
-  // [splits][n_list][Hkv][R], few rows [parts + n_list * Hkv][R].
+  // [splits][Hkv][all], few rows [parts + n_list * Hkv][R].
   float* part;
   float2* part_ml;
   int n_list, listed;            // sequences walked: list[0..n_list), or (listed = 0) all
   int32_t list[KV8_LIST];
+  // many rows: rows of the sequences walked one after another, and where each one's start (not listed: all
+  // sequences', at their queries times g)
+  int32_t all;
+  int32_t first[KV8_LIST];
 };
 hipError_t launch_attention_kv8(const Kv8Args& a, bool few, hipStream_t s);
 hipError_t launch_attn_many(const Kv8Args& a, hipStream_t s);

@@ -678,11 +678,36 @@ __global__ __launch_bounds__(256) void attn_join(Kv8Args a, int one, int64_t gro
   __shared__ int64_t sslot[NG];
   const int tid = threadIdx.x;
   const int gi = tid / LPR, lane = tid % LPR;
-  const int64_t all = int64_t(a.n_list) * a.hkv * a.R;
+  // few rows: R of each (sequence, head); many: the rows there are, head by head
+  const int64_t all = FEW ? int64_t(a.n_list) * a.hkv * a.R : int64_t(a.hkv) * a.all;
   const int64_t row_in = one ? int64_t(blockIdx.x) : (group0 + blockIdx.x) * NG + gi;
   const int d = lane * 4;
-  const int r = int(row_in % a.R), jh = int(min(row_in / a.R, int64_t(a.n_list) * a.hkv - 1));
-  const int kvh = jh % a.hkv, j = jh / a.hkv;
+  int r, j, kvh, jh = 0;
+  if constexpr (FEW) {
+    r = int(row_in % a.R);
+    jh = int(min(row_in / a.R, int64_t(a.n_list) * a.hkv - 1));
+    kvh = jh % a.hkv;
+    j = jh / a.hkv;
+  } else {
+    const int64_t x = min(row_in, all - 1);
+    kvh = int(x / a.all);
+    r = int(x - int64_t(kvh) * a.all);
+    j = 0;
+    if (a.listed) {
+      for (int i = 1; i < a.n_list; ++i) j += a.first[i] <= r;
+      r -= a.first[j];
+    } else {   // the last sequence that starts at or before the row's query
+      const int query = r / a.g;
+      int n = a.n_list;
+      while (n > 1) {
+        const int half = n >> 1;
+        const bool up = a.cu[j + half] <= query;
+        j = up ? j + half : j;
+        n = up ? n - half : half;
+      }
+      r -= a.cu[j] * a.g;
+    }
+  }
   const Seq s = seq_of(a, j);
   const int rows = s.m * a.g;
   bool on = row_in < all && r < rows && (rows <= FEW_ROWS) == FEW;
@@ -802,9 +827,9 @@ hipError_t launch_dim(const Kv8Args& a, bool few, hipStream_t s) {
   else
     e = launch_attn_many(a, s);
   if (e != hipSuccess || !a.part) return e;
-  const int64_t rows = int64_t(a.n_list) * a.hkv * a.R;
   constexpr int NG = 256 / (HD / 4);
-  const int one = rows <= JOIN_ONE;
+  const int one = int64_t(a.n_list) * a.hkv * a.R <= JOIN_ONE;
+  const int64_t rows = few ? int64_t(a.n_list) * a.hkv * a.R : int64_t(a.hkv) * a.all;
   const int64_t groups = one ? rows : (rows + NG - 1) / NG;
   for (int64_t group0 = 0; group0 < groups; group0 += MOST_GROUPS) {   // (more than a launch may have: several)
     const dim3 grid(unsigned(std::min(MOST_GROUPS, groups - group0)));

@@ -508,7 +508,7 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
   const float l_all = l_run + __shfl_xor(l_run, 32);
   if (a.splits > 1) {
     if (valid) {
-      const int64_t prow = (int64_t(split) * a.n_list * a.hkv + int64_t(j) * a.hkv + kvh) * a.R + row;
+      const int64_t prow = (int64_t(split) * a.hkv + kvh) * a.all + (a.listed ? a.first[j] : q0 * a.g) + row;
       float* po = a.part + prow * HD + 4 * hi;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)

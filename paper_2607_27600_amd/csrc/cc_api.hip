@@ -1111,7 +1111,8 @@ namespace {
 struct Kv8Class {
   int n = 0;               // sequences of the class
   int n_list = 0, listed = 0;
-  int32_t list[KV8_LIST];
+  int32_t list[KV8_LIST], first[KV8_LIST];   // first: rows of the class before the sequence's
+  int64_t all = 0;         // rows walked
   int R = 0, piece = 0, splits = 1, direct = 0, parts = 0;
   size_t part = 0, total = 0;   // workspace: (maximum, sum) pairs behind the outputs
 };
@@ -1125,14 +1126,19 @@ Kv8Class kv8_class(const cc_problem* p, int max_len, bool few) {
   for (int b = 0; b < p->n_seqs; ++b) {
     const int64_t rows = int64_t(p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) * g;
     if (rows == 0 || (rows <= FEW_ROWS) != few) continue;
-    if (c.n < KV8_LIST) c.list[c.n] = b;
+    if (c.n < KV8_LIST) {
+      c.list[c.n] = b;
+      c.first[c.n] = int32_t(c.all);
+    }
     ++c.n;
+    c.all += rows;
     c.R = int(std::max<int64_t>(c.R, rows));
     blocks += few ? 1 : (rows + MANY_ROWS - 1) / MANY_ROWS;
   }
   if (c.n == 0) return c;
   c.listed = c.n <= KV8_LIST;
   c.n_list = c.listed ? c.n : p->n_seqs;
+  if (!c.listed) c.all = int64_t(n_tokens(p)) * g;
   const int64_t items = blocks * p->n_heads_kv;   // workgroups without a cut
   size_t rows = 0;                                // partial results
   if (few) {
@@ -1151,7 +1157,7 @@ Kv8Class kv8_class(const cc_problem* p, int max_len, bool few) {
     c.piece = int(((int64_t(max_len) + want - 1) / want + MANY_KEYS - 1) / MANY_KEYS * MANY_KEYS);
     c.piece = std::max(c.piece, MANY_KEYS);
     c.splits = std::max(1, int((int64_t(max_len) + c.piece - 1) / c.piece));
-    if (c.splits > 1) rows = size_t(c.splits) * c.n_list * p->n_heads_kv * c.R;
+    if (c.splits > 1) rows = size_t(c.splits) * p->n_heads_kv * c.all;
   }
   if (rows) {
     c.part = align_up(rows * p->head_dim * sizeof(float));
@@ -1236,6 +1242,8 @@ cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv,
     a.n_list = c.n_list;
     a.listed = c.listed;
     std::copy_n(c.list, c.listed ? c.n : 0, a.list);
+    a.all = int32_t(c.all);
+    std::copy_n(c.first, c.listed ? c.n : 0, a.first);
     CC_HIP(launch_attention_kv8(a, i == 0, static_cast<hipStream_t>(stream)));
     off += c.total;
   }

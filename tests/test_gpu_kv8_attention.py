@@ -460,3 +460,26 @@ def test_more_rows_to_join_than_one_launch_has():
             want = O8.attention(f64(q[cu[b]:cu[b + 1], c]), kk, vv, "causal")
             assert_attention_close(f64(o[cu[b]:cu[b + 1], c])[:, None], want[:, None], f"{b} {c}")
     assert not (o == 7.0).all(-1).any()
+
+
+@pytest.mark.parametrize("mask", ["causal", "counter"])
+@pytest.mark.parametrize("new,hq,hkv,d", [([20, 0, 700, 1, 33, 17, 300], 4, 2, 128), ([40] * 20 + [1] * 40 + [3000] + [0, 17] * 50, 2, 1, 64)],
+                         ids=["listed", "all"])
+def test_ragged_chunks_in_pieces(new, hq, hkv, d, mask):
+    """Pieces of sequences of different numbers of rows, beside sequences of few rows and none, listed and
+    walked as a whole; the workspace holds no more than asked for."""
+    from paper_2607_27600_amd import cc
+    r = np.random.default_rng(95)
+    lens = [m + int(x) for m, x in zip(new, r.integers(0, 2500, len(new)))]
+    lens[2] = max(lens[2], 2900)
+    cache = Cache8(lens, hkv, d, page=64, block=32, seed=96, fill=0x7f)
+    q = _q(new, hq, d, 97)
+    p = _problem(cc, new, hq, hkv, d)
+    size = cc.cc_attention_kv8_workspace(p, mask, max(lens))
+    assert size > sum(new) * hq * d * 4       # pieces
+    ws = torch.full((size + 4096,), 0x7f, dtype=torch.uint8, device="cuda")
+    o = torch.full_like(q, 7.0)
+    cc.cc_attention_kv8(p, q, cache.view(cc), 0, i32(lens), max(lens), o, mask=mask, workspace=ws[:size])
+    torch.cuda.synchronize()
+    assert (ws[size:] == 0x7f).all()
+    assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, mask))

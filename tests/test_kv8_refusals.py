@@ -473,3 +473,21 @@ def test_append_refuses_more_tokens_than_a_launch_has_workgroups():
             p, kw = _problem(cu), dict(max_pages=1 << 23) if paged else {}
             assert cc._lib.cc_append_kv8(_ref(p), _ref(_append(capacity=100)), _ref(_kv8(paged, **kw)), None) == cc.CC_ERR_UNSUPPORTED
             assert cc._lib.cc_append_kv(_ref(p), _ref(_append(capacity=100)), _ref(_kv(paged, **kw)), None) == cc.CC_ERR_UNSUPPORTED
+
+
+def test_workspace_of_ragged_chunks_goes_by_the_rows_there_are():
+    """Pieces of a chunk beside many short ones: partial results of the rows that exist, not of as many for each
+    sequence as the longest has."""
+    import itertools
+    n = ctypes.c_size_t()
+    for new in ([5] * 99 + [1500], [1] * 5000 + [5] * 65 + [2000], [0] * 40 + [7, 3000, 9], [1] * 3000 + [900]):
+        p = _problem([0, *itertools.accumulate(new)], n_heads_q=8, n_heads_kv=1, head_dim=128)
+        assert cc._lib.cc_attention_kv8_workspace(_ref(p), 0, 5000, _ref(n)) == cc.CC_OK
+        # a row of 128 floats, a maximum and a sum, in each of at most 20 pieces of 256; the shares of few rows
+        # ((512 + sequences) * 32 rows) beside them
+        rows = 8 * (sum(new) if sum(x > 4 for x in new) > 64 else sum(x for x in new if x > 4))
+        few = (512 + len(new)) * 32
+        assert 0 < n.value <= (20 * rows + few) * 520 + 1024
+    p = _problem([0, *itertools.accumulate([5] * 99 + [1500])], n_heads_q=8, n_heads_kv=1, head_dim=128)
+    assert cc._lib.cc_attention_kv8_workspace(_ref(p), 0, 5000, _ref(n)) == cc.CC_OK
+    assert n.value <= 2 * 15960 * 520 + 1024      # two pieces
