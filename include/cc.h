@@ -405,7 +405,7 @@ typedef struct cc_append {
   cc_rows q;                   /* base NULL: none; [M][Hq][head_dim], n_layers = 1 only */
   void* q_out;                 /* with q: [M][Hq][head_dim] packed, in p->dtype; may be q
                                   itself where q is packed like that */
-  const int32_t* cached;       /* device [n_seqs] */
+  const int32_t* cached;       /* device [n_seqs]; negative ones are 0 */
   const int32_t* pos_ids;      /* device [M] original positions, NULL -> cached[b] + i */
   int64_t capacity;            /* entries that a sequence's place in the cache holds.  Paged:
                                   0 selects max_pages * page_size, which is also the limit */
@@ -449,8 +449,9 @@ cc_status cc_compact_kv8(const cc_problem* p, const cc_kv8* kv, const int32_t* k
 /* Which entries a query attends to.  With n_b = kv_lens[b] entries in the cache and m_b
  * queries in the call, query i of a sequence stands at entry n_b - m_b + i (the queries are
  * the last entries).  CAUSAL: entries up to and including its own.  COUNTER_CAUSAL: those
- * after its own (p->diag STRICT) or from its own on (INCLUSIVE).  A query with no entry to
- * attend to (one that stands before the first, too) has a zero output. */
+ * after its own (p->diag STRICT) or from its own on (INCLUSIVE).  With more queries than entries
+ * the first stand before entry 0: they attend to none (CAUSAL) or to all (COUNTER_CAUSAL).  A
+ * query with no entry to attend to has a zero output. */
 typedef enum cc_mask { CC_MASK_CAUSAL = 0, CC_MASK_COUNTER_CAUSAL = 1 } cc_mask;
 
 /* Workspace for cc_attention_kv8 (partial results of rows whose entries are shared out). */

@@ -144,7 +144,7 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs<HD> a) {
           } else {
             b = tok / a.each;
           }
-          pos = a.cached[b] + tok - a.cu[b];
+          pos = max(a.cached[b], 0) + tok - a.cu[b];
         }
         table[x] = turn(pos, a.freq[x % (HD / 2)]);
       }

@@ -315,3 +315,21 @@ def test_more_layers_than_one_launch_has_workgroups_for():
     for pool, y in zip(pools, x):
         assert torch.equal(pool[:, :, 1].view(torch.int16), y[:, :, 0].view(torch.int16))
         assert torch.count_nonzero(pool[:, :, 0].view(torch.int16)) == 0
+
+
+@pytest.mark.parametrize("new", [[2, 2], [3, 1]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_negative_lengths_are_zero(new, d):
+    """Keys and queries of a sequence stand at the same positions."""
+    from paper_2607_27600_amd import cc
+    x = _inputs(sum(new), 4, 2, d, "bf16", 64)[0].cuda()
+    q, k, v = x.split([4, 2, 2], 1)
+    p, out = _problem(cc, new, 4, 2, d), []
+    for cached in ([0, 5], [-7, 5]):
+        cache = Cache8([0, 5], 2, d, block=16, room=32, seed=65)
+        qo = cc.cc_append_kv8(p, cache.view(cc), k, v, i32(cached), capacity=cache.cap, q=q)
+        torch.cuda.synchronize()
+        out.append((f64(qo), cache.read()))
+    np.testing.assert_array_equal(out[0][0], out[1][0])
+    for t in out[0][1]:
+        np.testing.assert_array_equal(out[0][1][t], out[1][1][t])
