@@ -202,3 +202,144 @@ def test_two_graphs_share_a_workspace():
         for o, x in zip(outs, (want[0], want[1], want[1])):
             for t in ("logprob", "entropy", "top_ids", "top_logprob"):
                 assert torch.equal(getattr(o, t), getattr(x, t)), t
+
+
+# ---- batches whose candidates go by a running bound: more than 64 rows and at least two rounds of tiles.  Which
+# words are candidates there depends on the order of workgroups; the results may not.
+
+def _bounded(cc, n, V, D, top):
+    """Whether a call keeps a bound: its workspace has 32 slots and a bound a row behind the rest."""
+    up = lambda x: -(-x // 256) * 256
+    rows, tiles = min(n, 2048), -(-V // 256)
+    rest = up(tiles * rows * 16) + up(2 * tiles * rows) + up(2 * tiles * rows * top * 8) + up(rows * 4)
+    size = cc.cc_lmhead_logprobs_workspace("bf16", n, V, D, top)
+    assert size in (rest, rest + up(rows * 128) + up(rows * 4))
+    return size > rest
+
+
+@pytest.mark.parametrize("n,D,V,top,packed", [(300, 64, 70000, 1, False), (300, 64, 70001, 5, True), (257, 128, 70000, 32, False),
+                                              (600, 192, 50001, 20, True), (100, 64, 131073, 3, False)])
+def test_rows_with_a_running_bound(n, D, V, top, packed):
+    from paper_2607_27600_amd import cc
+    assert _bounded(cc, n, V, D, top)
+    print(f"[logprobs bounded] {n} {D} {V} {top} packed={packed}", flush=True)
+    u, w, ids = _grid(n, D, V, n + V)
+    _check(_call(cc, u, w, ids, top, packed), u, w, ids, top)
+
+
+def test_a_running_bound_starts_anew_with_every_slab():
+    """Rows of a second, shorter slab with logits far below the first's: a bound left over would drop them all."""
+    from paper_2607_27600_amd import cc
+    n, D, V, top = 2100, 64, 16385, 5
+    assert _bounded(cc, n, V, D, top)
+    u, w, ids = _grid(n, D, V, 17)
+    w[:, 0] = 1
+    u[:, 0] = 15
+    u[2048:, 0] = -15
+    _check(_call(cc, u, w, ids, top), u, w, ids, top)
+
+
+@pytest.mark.parametrize("order", ["equal", "falling", "rising", "few"])
+def test_ties_and_orders_with_a_running_bound(order):
+    """All logits equal, rising or falling with the id (every tile passes the bound, or none), a handful of values."""
+    from paper_2607_27600_amd import cc
+    V, D, n, top = 70000, 64, 300, 32
+    assert _bounded(cc, n, V, D, top)
+    w = torch.zeros(V, D)
+    v = torch.arange(V)
+    if order in ("falling", "rising"):      # z = +-v / 1024, in three exact terms; |z| under 69
+        s = -1.0 if order == "falling" else 1.0
+        w[:, 0], w[:, 1], w[:, 2] = s * (v // 4096).float() * 4, s * (v // 64 % 64).float() / 16, s * (v % 64).float() / 1024
+    elif order == "few":
+        w[:, 0] = (v % 7 == 3).float() - (v % 5 == 0).float()
+    u = torch.zeros(n, D)
+    u[:, :3] = 1
+    u[1::2] *= -1
+    u, w = u.to(torch.bfloat16), w.to(torch.bfloat16)
+    ids = torch.arange(n, dtype=torch.int32) * 200
+    ids[2:] = ids[:2].repeat(n // 2)[:n - 2]
+    r = _call(cc, u, w, ids, top)
+    want = O.logprobs(f64(u[:2]), f64(w), ids[:2].numpy(), top)     # all rows are one of two
+    for i in (0, 1):
+        np.testing.assert_array_equal(r.top_ids[i::2].cpu().numpy(), np.tile(want["top_ids"][i], (n // 2, 1)))
+        for t, tol in (("logprob", TOL), ("entropy", TOL_H), ("top_logprob", TOL)):
+            got = f64(getattr(r, t)[i::2])
+            np.testing.assert_allclose(got, np.broadcast_to(want[t][i], got.shape), rtol=0, atol=tol)
+
+
+def test_nan_infinities_and_padding_with_a_running_bound():
+    """Rows of NaN, rows of which five words are numbers and the others NaN or -inf, and ids of no word, among
+    plain rows of a bounded call."""
+    from paper_2607_27600_amd import cc
+    n, D, V, top = 300, 64, 70000, 7
+    assert _bounded(cc, n, V, D, top)
+    u, w, ids = _grid(n, D, V, 18)
+    w[:, 0] = 0
+    w[:, 1] = 0
+    u[:, 0] = u[:, 1] = 0
+    clean = _call(cc, u, w, ids, top)
+    _check(clean, u, w, ids, top)
+    u2, ids2 = u.clone(), ids.clone()
+    u2[9, 5] = u2[299, 1] = float("nan")
+    ids2[[3, 150]] = torch.tensor([-1, V], dtype=torch.int32)
+    r = _call(cc, u2, w, ids2, top)
+    rows = np.setdiff1d(np.arange(n), [9, 299])
+    for t in ("logprob", "entropy", "top_ids", "top_logprob"):
+        x, y = getattr(r, t), getattr(clean, t)
+        keep = np.setdiff1d(rows, [3, 150]) if t == "logprob" else rows
+        assert torch.equal(x[keep], y[keep]), t
+        if t != "top_ids":
+            assert torch.isnan(x[[9, 299]]).all()
+    assert torch.isnan(r.logprob[[3, 150]]).all()
+    assert r.top_ids[[9, 299]].cpu().tolist() == [list(range(top))] * 2
+    # -inf in w: rows of u0 = 1 have -inf in all words but five, rows of u0 = 0 NaN (0 times infinity)
+    u3, w3 = torch.zeros(n, D), torch.zeros(V, D)
+    w3[:, 1] = (torch.arange(V) % 64).float() / 16
+    five = [3, 1000, 33333, 69998, 69999]
+    w3[:, 0] = -float("inf")
+    w3[five, 0] = 0
+    u3[:, 1] = 1
+    u3[::2, 0] = 1
+    ids3 = torch.full((n,), 1000, dtype=torch.int32)
+    r = _call(cc, u3.to(torch.bfloat16), w3.to(torch.bfloat16), ids3, top)
+    z = np.array([x % 64 / 16 for x in five])
+    lse = np.log(np.exp(z).sum())
+    order = np.argsort(-z, kind="stable")
+    want_ids = [five[i] for i in order] + [0, 1]
+    assert (r.top_ids.cpu() == torch.tensor(want_ids, dtype=torch.int32)).all()
+    np.testing.assert_allclose(f64(r.top_logprob[::2, :5]), np.tile(z[order] - lse, (n // 2, 1)), rtol=0, atol=TOL)
+    assert torch.isneginf(r.top_logprob[::2, 5:]).all() and torch.isnan(r.top_logprob[1::2]).all()
+    np.testing.assert_allclose(f64(r.logprob[::2]), z[1] - lse, rtol=0, atol=TOL)
+    np.testing.assert_allclose(f64(r.entropy[::2]), -(np.exp(z - lse) * (z - lse)).sum(), rtol=0, atol=TOL_H)
+
+
+def test_bounded_calls_repeat_bit_for_bit_in_graphs_that_share_a_workspace():
+    """Two captured calls of one workspace, replayed in turn with an eager call between, whatever it holds."""
+    from paper_2607_27600_amd import cc
+    n, D, V, top = 300, 256, 70000, 8
+    assert _bounded(cc, n, V, D, top)
+    sets = [tuple(x.cuda() for x in _grid(n, D, V, s)) for s in (19, 20)]
+    want = [cc.cc_lmhead_logprobs("bf16", u, w, V, ids, top) for u, w, ids in sets]
+    for (u, w, ids), r in zip(sets, want):
+        _check(r, u, w, ids.cpu(), top)
+    ws = torch.empty(cc.cc_lmhead_logprobs_workspace("bf16", n, V, D, top), dtype=torch.uint8, device="cuda")
+    outs = [cc.logprobs_out(n, top) for _ in range(3)]
+    torch.cuda.synchronize()
+    graphs = []
+    for (u, w, ids), out in zip(sets, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            cc.cc_lmhead_logprobs("bf16", u, w, V, ids, top, out, workspace=ws)
+        graphs.append(g)
+    for i in range(5):
+        for o in outs:
+            for t in (o.logprob, o.entropy, o.top_ids, o.top_logprob):
+                t.zero_()
+        ws.fill_(i * 51)
+        graphs[0].replay()
+        cc.cc_lmhead_logprobs("bf16", *sets[1][:2], V, sets[1][2], top, outs[2], workspace=ws)
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for o, x in zip(outs, (want[0], want[1], want[1])):
+            for t in ("logprob", "entropy", "top_ids", "top_logprob"):
+                assert torch.equal(getattr(o, t), getattr(x, t)), t
