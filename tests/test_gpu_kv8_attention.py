@@ -483,3 +483,146 @@ def test_ragged_chunks_in_pieces(new, hq, hkv, d, mask):
     torch.cuda.synchronize()
     assert (ws[size:] == 0x7f).all()
     assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, mask))
+
+
+# ---- equal shares: the kernel for few rows where there is much work.  A copy of its rule, to see that a case
+# gets there and what its shares cut.
+
+def _shares(new, lens, g, hkv, longest):
+    """(mode, what the shares cut) of the few-row sequences of a call."""
+    few = [0 < m * g <= 32 for m in new]
+    n = sum(few)
+    n_list = n if n <= 64 else len(new)
+    if longest <= (2048 if n * hkv >= 128 else 1024):
+        return "direct", set()
+    units = [max(1, -(-min(max(x, 0), longest) // 128)) if f else 0 for x, f in zip(lens, few)]
+    total, items, parts = sum(units) * hkv, n_list * hkv, 512
+    if items < parts and -(-total // (parts - items)) <= 8:
+        return "pieces", set()
+    starts, at = [], 0                       # of every (sequence, head) along the line, two units ahead of its entries
+    for u in units:
+        for _ in range(hkv if u else 0):
+            starts.append((at, u))
+            at += u + 2
+    parts = min(parts, at)
+    cuts = [at * w // parts for w in range(parts + 1)]
+    seen, i = set(), 0
+    for w in range(1, parts):
+        while starts[i][0] + starts[i][1] + 2 <= cuts[w]:
+            i += 1
+        off = cuts[w] - starts[i][0]
+        seen.add("between" if off == 0 else "ahead of the entries" if off <= 2 else "entries")
+    whole = np.searchsorted([s for s, _ in starts], cuts, side="right")
+    if max(np.diff(whole)) >= 3:
+        seen.add("several items in a share")
+    if max(u for _, u in starts) >= 3 * at / parts:
+        seen.add("an item in several shares")
+    return "shares", seen
+
+
+class _Windows:
+    """One plane of n entries; sequence b's head h has the entries from 16 (b * step + h) on, in a contiguous cache or in
+    pages of 16."""
+
+    def __init__(self, cc, n, d, n_seqs, hkv, step, paged, seed):
+        r = np.random.default_rng(seed)
+        self.step = step
+        n = -(-n // 16) * 16
+        self.c, self.s, t = {}, {}, {}
+        for w in "kv":
+            self.c[w], self.s[w] = quantize(r.normal(0, 1, (n, d)) * np.exp2(r.integers(-2, 3, (n, 1))), 16)
+            t[w], t[w + "s"] = torch.from_numpy(self.c[w]).cuda(), torch.from_numpy(self.s[w]).cuda()
+        self.values = {w: O8.values(self.c[w], self.s[w], 16) for w in "kv"}
+        if paged:
+            pages = n // 16
+            table = torch.arange(n_seqs)[:, None] * step + torch.arange(pages)[None]
+            self.kv = cc.kv8_paged(t["k"], t["v"], t["ks"], t["vs"], table.clamp(max=pages - 1).to(torch.int32).cuda(), n_layers=1,
+                                   layer_stride=0, page_stride=16 * d, head_stride=16 * d, tok_stride=d, page_size=16,
+                                   scale_block=16, scale_layer_stride=0, scale_page_stride=1, scale_head_stride=1)
+        else:
+            self.kv = cc.kv8_contiguous(t["k"], t["v"], t["ks"], t["vs"], n_layers=1, layer_stride=0, seq_stride=16 * step * d,
+                                        head_stride=16 * d, tok_stride=d, scale_block=16, scale_layer_stride=0,
+                                        scale_seq_stride=step, scale_head_stride=1)
+
+    def oracle(self, q, new, lens, hq, hkv, mask):
+        g, out, at, qh = hq // hkv, [], 0, f64(q)
+        for b, m in enumerate(new):
+            o = np.zeros((m, hq, q.shape[2]))
+            for h in range(hq if m else 0):
+                i = 16 * (b * self.step + h // g)
+                o[:, h] = O8.attention(qh[at:at + m, h], self.values["k"][i:i + lens[b]], self.values["v"][i:i + lens[b]], mask)
+            out.append(o)
+            at += m
+        return np.concatenate(out)
+
+
+ALL_CUTS = {"ahead of the entries", "entries", "several items in a share"}
+SHARED = [
+    # sequences, heads of a group, KV heads, head_dim, most new tokens, longest, paged, what is cut at least
+    (300, 4, 2, 128, 4, 6000, True, ALL_CUTS),                            # walked as a whole, five sequences a lane; one row block
+    (300, 4, 2, 64, 8, 6000, False, ALL_CUTS),                            # two row blocks
+    (60, 2, 16, 128, 16, 3000, False, ALL_CUTS),                          # listed
+    (40, 1, 20, 64, 3, 2500, True, ALL_CUTS),
+    (1, 2, 16, 128, 2, 37000, False, {"entries", "an item in several shares"}),
+    (3, 8, 8, 64, 4, 40000, True, {"entries", "an item in several shares"}),
+    (700, 2, 1, 64, 1, 9000, False, ALL_CUTS),                            # most of them short, a few in several shares
+]
+
+
+@pytest.mark.parametrize("mask", ["causal", "counter"])
+@pytest.mark.parametrize("case", SHARED, ids=[str(i) for i in range(len(SHARED))])
+def test_equal_shares(case, mask):
+    """Shares that begin and end inside an item, ahead of its entries or between items, and hold several."""
+    from paper_2607_27600_amd import cc
+    n, g, hkv, d, most, longest, paged, cut = case
+    r = np.random.default_rng(n + d)
+    new = [int(x) for x in r.integers(0 if n > 3 else 1, most + 1, n)]
+    lens = [m + int(x) for m, x in zip(new, r.integers(0, 300 if n > 3 else longest, n))]
+    for b in r.permutation(n)[:max(1, n // 8)]:
+        new[b] = max(new[b], 1)
+        lens[b] = int(r.integers(longest // 3, longest))
+    if n > 100:
+        new[5], lens[5], lens[6] = 40, 500, 0             # one of many rows, and one without entries
+    lens[-1], new[-1] = longest, most
+    mode, seen = _shares(new, lens, g, hkv, longest)
+    assert mode == "shares" and cut <= seen, (mode, seen)
+    print(f"[attn8 shares] {case} {mask} {seen}", flush=True)
+    win = _Windows(cc, longest + 16 * (n + hkv) + 16, d, n, hkv, 1, paged, n)
+    q = _q(new, g * hkv, d, n + 1)
+    p = _problem(cc, new, g * hkv, hkv, d)
+    for plan in (longest, longest + 900):
+        if paged and plan > longest:
+            continue                   # (a plan past the block table's rows is refused)
+        o = torch.full_like(q, 7.0)
+        cc.cc_attention_kv8(p, q, win.kv, 0, i32(lens), plan, o, mask=mask)
+        torch.cuda.synchronize()
+        assert_attention_close(f64(o), win.oracle(q, new, lens, g * hkv, hkv, mask), f"{plan}")
+
+
+def test_pieces_and_shares_under_one_plan_in_a_graph():
+    """Device lengths that take a captured call from pieces to equal shares and back."""
+    from paper_2607_27600_amd import cc
+    n, g, hkv, d, longest = 50, 2, 8, 64, 9000
+    new = [1 + b % 3 for b in range(n)]
+    r = np.random.default_rng(98)
+    win = _Windows(cc, longest + 16 * (n + hkv) + 16, d, n, hkv, 1, True, 99)
+    q, lens = _q(new, g * hkv, d, 100), i32([3] * n)
+    p = _problem(cc, new, g * hkv, hkv, d)
+    o = torch.empty_like(q)
+    ws = torch.empty(max(1, cc.cc_attention_kv8_workspace(p, "causal", longest)), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cc.cc_attention_kv8(p, q, win.kv, 0, lens, longest, o, workspace=ws)
+    modes = []
+    for most in (20, longest, 600, 0, 4000, 150):
+        now = [int(x) for x in r.integers(0, most + 1, n)]
+        now[17] = most
+        modes.append(_shares(new, now, g, hkv, longest)[0])
+        lens.copy_(i32(now))
+        o.fill_(9.0)
+        ws.fill_(0x7f)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert_attention_close(f64(o), win.oracle(q, new, now, g * hkv, hkv, "causal"), str(most))
+    assert {"pieces", "shares"} <= set(modes), modes
