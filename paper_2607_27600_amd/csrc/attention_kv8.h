@@ -43,6 +43,7 @@ struct Kv8Args {
   int layer, mask, inclusive, max_len;
   int hq, hkv, g, head_dim;
   float c2;                      // scale * log2(e)
+  float room;                    // how far a logit may pass a row's reference maximum: 2^8 in probability
   int R;                         // most rows of a sequence of the class
   int piece, splits;             // many rows: entries of a piece, pieces of the longest sequence
   int nth0;                      // many rows: first row block, in the order of a sequence, of a launch

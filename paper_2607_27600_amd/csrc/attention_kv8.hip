@@ -29,7 +29,6 @@
 namespace cc {
 namespace {
 
-constexpr float kRescale = 8.f;   // log2 headroom before the reference maximum moves
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -519,12 +518,12 @@ __global__ __launch_bounds__(FEW_NT, 2) void attn_few(Kv8Args a) {
           float t = fmaxf(fmaxf(fmaxf(z[n][0][0], z[n][0][1]), fmaxf(z[n][0][2], z[n][0][3])),
                           fmaxf(fmaxf(z[n][1][0], z[n][1][1]), fmaxf(z[n][1][2], z[n][1][3])));
           mx[n] = quad_max(t);
-          moved |= mx[n] > m_run[n] + kRescale / a.c2;
+          moved |= mx[n] > m_run[n] + a.room;
         }
         if (__any(moved)) {
 #pragma unroll
           for (int n = 0; n < NR; ++n) {
-            const bool up = mx[n] > m_run[n] + kRescale / a.c2;
+            const bool up = mx[n] > m_run[n] + a.room;
             const float corr = up ? fast_exp2((m_run[n] - mx[n]) * a.c2) : 1.f;   // 0 from -inf
             if (up) m_run[n] = mx[n];
             l_run[n] *= corr;

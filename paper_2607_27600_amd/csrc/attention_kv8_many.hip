@@ -33,7 +33,6 @@ namespace {
 constexpr int BN = MANY_KEYS;
 constexpr int ROWS_W = 32;
 constexpr int NWAVES = 4;
-constexpr float kRescale = 8.f;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short v4i16 __attribute__((ext_vector_type(4)));
@@ -395,7 +394,7 @@ __global__ __launch_bounds__(256, 2) void attn_many(Kv8Args a) {
           for (int e = 0; e < 16; ++e) sc[mb][e] = seen(t, mb, e) ? sc[mb][e] : -INFINITY;
         mx = row_max(sc);
       }
-      const bool up = mx > m_run + kRescale / a.c2;
+      const bool up = mx > m_run + a.room;
       const float corr = up ? fast_exp2((m_run - mx) * a.c2) : 1.f;
       m_run = up ? mx : m_run;
       const float mc = (m_run == -INFINITY ? 0.f : m_run) * a.c2;

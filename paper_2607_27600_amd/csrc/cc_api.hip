@@ -2,6 +2,7 @@
 // and kernel launches for the refresh-scoring pass.  Host code only; every kernel lives
 // in its own translation unit behind the launchers declared in cc_internal.h.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <mutex>
@@ -1231,6 +1232,7 @@ cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv,
     a.g = p->n_heads_q / p->n_heads_kv;
     a.head_dim = p->head_dim;
     a.c2 = softmax_scale(p) * kLog2e;
+    a.room = std::min(8.f / a.c2, FLT_MAX);   // (finite: a first logit passes -inf by more)
     a.R = c.R;
     a.piece = c.piece;
     a.splits = c.splits;

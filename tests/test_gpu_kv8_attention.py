@@ -626,3 +626,16 @@ def test_pieces_and_shares_under_one_plan_in_a_graph():
         torch.cuda.synchronize()
         assert_attention_close(f64(o), win.oracle(q, new, now, g * hkv, hkv, "causal"), str(most))
     assert {"pieces", "shares"} <= set(modes), modes
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.2, 0.01, 1e-20, 1e-38, 1e-40])
+@pytest.mark.parametrize("new,lens,hq,hkv,d", [([1, 3], [200, 77], 8, 2, 128), ([2], [3000], 4, 1, 64), ([70, 40], [300, 90], 4, 2, 128),
+                                               ([90], [2500], 2, 1, 64)])
+def test_a_scale_of_the_callers(new, lens, hq, hkv, d, scale):
+    """softmax_scale, few and many rows, whole and in pieces: from peaked rows to ones whose logits vanish."""
+    from paper_2607_27600_amd import cc
+    cache = Cache8(lens, hkv, d, page=16, block=16, seed=101, fill=0x7f, std=0.5)
+    q = _q(new, hq, d, 102)
+    for mask in ("causal", "counter"):
+        o = _run(cc, cache, q, new, lens, hq, hkv, mask, softmax_scale=scale)
+        assert_attention_close(f64(o), _oracle(cache, q, new, lens, hq, hkv, mask, scale=scale), f"{scale} {mask}")
