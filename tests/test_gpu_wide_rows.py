@@ -57,3 +57,21 @@ def test_lmhead(form):
     assert ((lse.double() - ref).abs() <= bound).all()
     want = (ref - z[torch.arange(N, device="cuda"), ids.long()]).clamp(min=0)
     assert ((s.double() - want).abs()[:-1] <= 2 * bound[:-1]).all() and torch.isinf(s[-1])
+
+
+@pytest.mark.parametrize("form", ["row", "packed"])
+def test_logprobs(form):
+    from paper_2607_27600_amd import cc
+    K, top = 1 << 23, 7
+    print(f"[wide] logprobs {form} K={K}", flush=True)
+    x, w, z = _sparse(K, torch.bfloat16, 1, -1, 4)
+    ids = torch.randint(0, ROWS, (N,), device="cuda", dtype=torch.int32)
+    r = cc.cc_lmhead_logprobs("bf16", x, cc.cc_pack_lmhead(w) if form == "packed" else w, ROWS, ids, top, packed=form == "packed")
+    lp = torch.log_softmax(z, 1)
+    # as above: exact logits, then exponentials and a logarithm; an entropy weighs terms of up to 20 nats
+    bound = (2.0 ** -21 * (torch.logsumexp(z, 1).abs() + z.abs().amax(1)) + 4e-6)[:, None]
+    order = torch.sort(z, dim=1, descending=True, stable=True).indices[:, :top]      # ties: the lower word first
+    assert torch.equal(r.top_ids.long(), order)
+    assert ((r.top_logprob.double() - lp.gather(1, order)).abs() <= 2 * bound).all()
+    assert ((r.logprob.double()[:, None] - lp.gather(1, ids.long()[:, None])).abs() <= 2 * bound).all()
+    assert ((r.entropy.double() + (lp.exp() * lp).sum(1)).abs() <= 20 * bound[:, 0]).all()
