@@ -65,3 +65,9 @@ def test_traffic_is_reported_only_for_the_sources_it_was_taken_on(tmp_path, monk
         assert bench.lmhead_traffic("C5") is None, name
         (csrc / name).write_bytes(text)
     assert bench.lmhead_traffic("C5") == 7.0
+
+
+def test_the_recorded_traffic_belongs_to_the_sources_as_they_are():
+    """Whoever changes them takes the counters again, or the benchmark's line loses its traffic."""
+    import bench
+    assert bench.lmhead_traffic("C5") > 1e11 and bench.lmhead_traffic("C2") > 5e9
