@@ -1154,7 +1154,9 @@ Kv8Class kv8_class(const cc_problem* p, int max_len, bool few) {
     // at 8000 entries 110 us, half as many pieces 142, twice 125; rounded up, 600 queries at 30000 500 us for
     // 365 and 24 sequences of 64 at 3000 157 for 130, 18 ragged ones 90 for 100), of 256 entries at the least
     // (128 queries of 8 heads on one at 4000 21 us, of 512 27, of 128 24).
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2 * kCus / items, (int64_t(max_len) + 255) / 256));
+    // And no more than leave a launch a row block (MOST_GROUPS).
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({2 * kCus / items, (int64_t(max_len) + 255) / 256,
+                                                                 MOST_GROUPS / (int64_t(c.n_list) * p->n_heads_kv)}));
     c.piece = int(((int64_t(max_len) + want - 1) / want + MANY_KEYS - 1) / MANY_KEYS * MANY_KEYS);
     c.piece = std::max(c.piece, MANY_KEYS);
     c.splits = std::max(1, int((int64_t(max_len) + c.piece - 1) / c.piece));

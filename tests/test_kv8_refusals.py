@@ -491,3 +491,12 @@ def test_workspace_of_ragged_chunks_goes_by_the_rows_there_are():
     p = _problem([0, *itertools.accumulate([5] * 99 + [1500])], n_heads_q=8, n_heads_kv=1, head_dim=128)
     assert cc._lib.cc_attention_kv8_workspace(_ref(p), 0, 5000, _ref(n)) == cc.CC_OK
     assert n.value <= 2 * 15960 * 520 + 1024      # two pieces
+
+
+def test_attention_takes_a_few_chunks_among_millions_of_single_queries():
+    """The pieces of the chunks are fewer, rather than the call refused."""
+    import itertools
+    n = ctypes.c_size_t()
+    p = _problem([0, *itertools.accumulate([1] * 3_000_000 + [40] * 65)], n_heads_q=1, n_heads_kv=1, head_dim=64)
+    for longest in (100, 100000):
+        assert cc._lib.cc_attention_kv8_workspace(_ref(p), 0, longest, _ref(n)) == cc.CC_OK
