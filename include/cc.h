@@ -420,7 +420,8 @@ typedef struct cc_append {
  * rotation in fp32, one rounding to the cache's type); rotates q into q_out alike.  Tokens
  * at or past the capacity, and those whose page id is negative, are not written.  `cached`
  * is read on the device, so a captured call follows lengths that advance between replays.
- * No other entry is touched.  Sequences must not share pages that are written. */
+ * No other entry is touched.  Sequences must not share pages that are written.  Some 40 million
+ * tokens, or 4 million sequences, are the most of a call. */
 cc_status cc_append_kv(const cc_problem* p, const cc_append* a, const cc_kv* kv, void* stream);
 
 /* The same into a cache in 8 bits (p->dtype: the type of k, v and q; fp32 values are
@@ -439,7 +440,8 @@ cc_status cc_append_kv8(const cc_problem* p, const cc_append* a, const cc_kv8* k
  * elements below 2^-6 of the new scale; NaN codes stay).  keep_idx, k_h, per_head,
  * token_ids and pos_ids as in cc_compact_kv; `out` NULL compacts in place, else a cache of
  * the same layout, layers and scale_block that does not overlap kv.  Codes past entry k_b
- * and scales past its block are left untouched.  Needs no workspace. */
+ * and scales past its block are left untouched.  n_layers * n_heads_kv is below 2^20, and with
+ * per_head n_heads_kv at most 64.  Needs no workspace. */
 cc_status cc_compact_kv8(const cc_problem* p, const cc_kv8* kv, const int32_t* keep_idx,
                          const int32_t* k_h, int32_t per_head, int32_t* token_ids,
                          int32_t* pos_ids, const cc_kv8* out, void* stream);
@@ -469,7 +471,7 @@ cc_status cc_attention_kv8_workspace(const cc_problem* p, int32_t mask, int32_t 
  * attends to gives NaN.  Elements are taken in bf16 (exactly, from 2^-126 to below 2^128; those of
  * 2^128 and more, which scales above 2^119 can have, are infinite and make what they reach infinite or NaN).
  * Sums, maxima and outputs are kept in fp32 until the last rounding; the probabilities enter
- * the second product in bf16. */
+ * the second product in bf16.  n_seqs * n_heads_kv is below 2^24. */
 cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv, int32_t layer,
                            int32_t mask, const int32_t* kv_lens, int32_t max_kv_len, void* o,
                            void* workspace, size_t workspace_bytes, void* stream);

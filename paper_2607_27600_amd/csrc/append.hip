@@ -13,10 +13,10 @@
 // so a block whose scale grows with a later token keeps its entries exactly, but for codes that
 // fall below the normal range, and products with scales are exact wherever they are taken.
 //
-// Bound by memory for chunks of a prompt (8192 tokens, 32 heads on 8, into 8 bits: 185 MB in 44 us, 4.2 TB/s;
-// 3166 ragged tokens into bf16 pages: 78 MB in 15.8 us, 4.9 TB/s, what a large copy reaches) and by the
-// round trips to lengths, then rows, for single tokens (eight: 4.9 us); a row is read 16 elements a lane
-// (e .. e + 7 and their partners), 16 bytes a load.
+// Bound by memory for chunks of a prompt (8192 tokens, 32 heads on 8, into 8 bits: 185 MB in 42 us, 4.4 TB/s, and in 33
+// where the last-level cache still holds the cache's pages; 3166 ragged tokens into bf16 pages: 78 MB in 15.0 us,
+// 5.2 TB/s; a large copy reaches 4.9) and by the round trips to lengths, then rows, for single tokens (eight:
+// 6 us); a row is read 16 elements a lane (e .. e + 7 and their partners), 16 bytes a load.
 #include <algorithm>
 #include <cmath>
 

@@ -15,9 +15,11 @@
 // reads.  Two K and two V buffers, one barrier a tile.  Matrix work of one tile is interleaved with the
 // exponentials of the tile before.
 //
-// Bound by the issue of a wave's instructions, matrix ones and exponentials first: 4096 entries scored by
-// 32 heads on 8 in 166 us (830 TFLOP/s), against 144 us of cc_attention_cc on bf16 entries, which has 29
-// vector instructions where this has 39 and 8 scalar ones where this has 24.
+// Bound by the issue of a wave's instructions: 4096 entries scored by 32 heads on 8 in 165 us (830 TFLOP/s),
+// against 144 us of cc_attention_cc on bf16 entries.  Counted, a matrix instruction comes with 7.9 vector, 5.6
+// scalar and 2.0 LDS ones, there with 5.8, 1.8 and 1.5, and the matrix cores are busy 33% of the time, there 52%.
+// (Tests of the last tiles and of the mask between the matrix instructions also cut a step into short basic
+// blocks, where that kernel's are half a step long.)
 //
 // A NaN or infinite value in a tile that some rows see in part becomes the least bf16 number, 2^-133:
 // nothing beside fp32 sums, and told from every other value by its last bit (E4M3 values end in zeros).  A

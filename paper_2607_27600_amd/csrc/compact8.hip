@@ -6,7 +6,7 @@
 // entry whose source has the block's scale is a bit copy.
 //
 // A workgroup moves chunks of rows, whole blocks: rows in registers, 16 codes a lane; a block's largest
-// magnitude by an LDS maximum of fp32 bits (order-free); one barrier; the codes.
+// magnitude by an LDS maximum of whole numbers (order-free); one barrier; the codes.
 //   Out of place a chunk of 128 rows (head_dim 64: 256) is a workgroup of 256 threads.  Bound by memory: of
 //   four sequences a quarter kept, 8 paged layers, 115 MB in 40 to 49 us (2.9 to 2.3 TB/s; rows of 128 bytes
 //   from anywhere: 94% kept reach 4.2, and a mere copy of the codes takes as long).
