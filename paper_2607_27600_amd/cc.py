@@ -254,8 +254,21 @@ def packed(p: Problem, on: bool = True) -> Problem:
     return Problem(s, p.cu_h, p.cu_d, p.device)
 
 
+class _View:
+    """Where the tensors of a cache view lie: as a tensor says it (None: it holds none)."""
+
+    def __post_init__(self):
+        where = {t.get_device() for t in self.keep}
+        self._device = where.pop() if len(where) == 1 else "different" if where else None
+
+    def get_device(self) -> Optional[int]:
+        if self._device == "different":
+            raise ValueError("tensors on different devices")
+        return self._device
+
+
 @dataclass
-class KV:
+class KV(_View):
     """A cc_kv view plus the tensors it points at."""
     struct: c_kv
     keep: list = field(default_factory=list)
@@ -554,7 +567,7 @@ def cc_compact_rows(p: Problem, rows: torch.Tensor, keep_idx: torch.Tensor, k: S
 # ---------------------------------------------------------------- cache in 8 bits
 
 @dataclass
-class KV8:
+class KV8(_View):
     """A cc_kv8 view (E4M3 codes, E8M0 scales) plus the tensors it points at."""
     struct: c_kv8
     keep: list = field(default_factory=list)
@@ -619,18 +632,17 @@ def _empty(shape, dtype: torch.dtype, device, stream=None) -> torch.Tensor:
 
 
 def _on_gpu(*tensors) -> None:
-    """Kernels run on the current device: tensors elsewhere would be read there by address."""
-    here = None
-    for t in tensors:
-        if t is not None:
-            d = t.get_device()   # negative: not on a GPU
-            if d != here:
-                if d < 0:
-                    raise ValueError(f"tensors must be on the GPU, got one on {t.device}")
-                if here is not None:
-                    raise ValueError("tensors on different devices")
-                here = d
-    if here is not None and here != torch._C._cuda_getDevice():
+    """Kernels run on the current device: tensors (and cache views) elsewhere would be read there by address."""
+    found = {t.get_device() for t in tensors if t is not None}   # negative: not on a GPU
+    found.discard(None)
+    if not found:
+        return
+    if min(found) < 0:
+        raise ValueError("tensors must be on the GPU")
+    if len(found) > 1:
+        raise ValueError("tensors on different devices")
+    here = found.pop()
+    if here != torch._C._cuda_getDevice():
         raise ValueError(f"tensors are on cuda:{here}, the current device is cuda:{torch._C._cuda_getDevice()}")
 
 
@@ -638,13 +650,6 @@ def _codes(kv) -> Optional[torch.Tensor]:
     """The keys of a cache view, which say where it lies."""
     codes = kv.keep[0] if kv.keep else None
     return codes.keep[0] if isinstance(codes, KV) else codes
-
-
-def _parts(kv) -> tuple:
-    """Every tensor of a cache view: keys, values, block table, scales."""
-    if kv is None:
-        return ()
-    return tuple(x for t in kv.keep for x in (t.keep if isinstance(t, KV) else (t,)))
 
 
 def _int32(t: Optional[torch.Tensor], n: int, what: str) -> None:
@@ -659,9 +664,10 @@ def _append(fn, p: Problem, kv, k, v, cached, capacity, layer, n_layers, pos_ids
     dtype = _DTYPES[s.dtype]
     _int32(cached, n_seqs, "cached")
     _int32(pos_ids, M, "pos_ids")
-    codes = _codes(kv)   # (8-bit views are of bytes already)
-    if isinstance(kv, KV) and codes is not None and any(t.dtype != dtype for t in kv.keep[:2]):
-        raise ValueError(f"the cache holds {codes.dtype}, the problem {dtype}")
+    if isinstance(kv, KV) and kv.keep:   # (8-bit views are of bytes already)
+        for t in kv.keep[:2]:
+            if t.dtype != dtype:
+                raise ValueError(f"the cache holds {t.dtype}, the problem {dtype}")
     a = c_append()
     # one layer may come without its dimension
     want = (n_layers, M, hkv, d) if n_layers != 1 or k.dim() == 4 else (M, hkv, d)
@@ -675,7 +681,7 @@ def _append(fn, p: Problem, kv, k, v, cached, capacity, layer, n_layers, pos_ids
         elif q_out.dtype != dtype or q_out.numel() != M * hq * d or not q_out.is_contiguous():
             raise ValueError("q_out must be contiguous rows of q's type and size")
         a.q_out = q_out.data_ptr()
-    _on_gpu(k, v, q, q_out, cached, pos_ids, p.cu_d, *_parts(kv))
+    _on_gpu(k, v, q, q_out, cached, pos_ids, p.cu_d, kv)
     a.cached = cached.data_ptr()
     if pos_ids is not None:
         a.pos_ids = pos_ids.data_ptr()
@@ -715,7 +721,7 @@ def cc_compact_kv8(p: Problem, kv: KV8, keep_idx: torch.Tensor, k: Sequence[int]
     for what, t in (("token_ids", token_ids), ("pos_ids", pos_ids)):
         if t is not None and (t.dtype != torch.int32 or t.numel() < N or not t.is_contiguous()):
             raise ValueError(f"{what} must be at least {N} contiguous int32 values")
-    _on_gpu(keep_idx, token_ids, pos_ids, p.cu_d, *_parts(kv), *_parts(out))
+    _on_gpu(keep_idx, token_ids, pos_ids, p.cu_d, kv, out)
     _check(_lib.cc_compact_kv8(ctypes.byref(p.struct), ctypes.byref(kv.struct), _ptr(keep_idx), kk, per_head,
                                _ptr(token_ids), _ptr(pos_ids),
                                ctypes.byref(out.struct) if out is not None else None, _stream(stream)),
@@ -744,7 +750,7 @@ def cc_attention_kv8(p: Problem, q: torch.Tensor, kv: KV8, layer: int, kv_lens: 
         o = _empty(q.shape, q.dtype, q.device, stream)
     elif o.dtype != q.dtype or o.numel() != q.numel() or not o.is_contiguous():
         raise ValueError("o must be contiguous and of q's type and size")
-    _on_gpu(q, o, kv_lens, workspace, p.cu_d, *_parts(kv))
+    _on_gpu(q, o, kv_lens, workspace, p.cu_d, kv)
     if workspace is None:
         workspace = _empty(max(1, cc_attention_kv8_workspace(p, mask, max_kv_len)), torch.uint8, q.device, stream)
     _check(_lib.cc_attention_kv8(ctypes.byref(s), _ptr(q), ctypes.byref(kv.struct), layer, _MASKS[mask],

@@ -388,40 +388,69 @@ def test_compaction_refuses_ids_of_another_type_or_too_few(monkeypatch, which):
             cc.cc_compact_kv8(p, kv, keep, [1, 1], 0, **{which: torch.zeros(n, dtype=torch.int32)})
 
 
+class _T:
+    """A tensor somewhere, as far as the binding looks at one before the library does."""
+
+    def __init__(self, device, dtype, shape=(1, 2)):
+        self.d, self.dtype, self.shape, self.device = device, dtype, shape, f"cuda:{device}"
+
+    def get_device(self):
+        return self.d
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def data_ptr(self):
+        return P
+
+    def numel(self):
+        return self.shape[0] * self.shape[1]
+
+    def is_contiguous(self):
+        return True
+
+    def to(self, dtype):
+        return self
+
+    def contiguous(self):
+        return self
+
+
 @pytest.mark.parametrize("paged", [False, True])
-def test_every_tensor_of_a_cache_and_a_problem_is_looked_at(monkeypatch, paged):
-    """Values, scales, the block table and the problem's lengths count as much as the keys."""
-    seen = []
-    monkeypatch.setattr(cc, "_on_gpu", lambda *t: seen.append([id(x) for x in t if x is not None]))
+@pytest.mark.parametrize("odd", range(6))
+def test_every_tensor_of_a_cache_and_a_problem_is_looked_at(monkeypatch, paged, odd):
+    """Values, scales, the block table and the problem's lengths elsewhere count as much as the keys."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     monkeypatch.setattr(cc, "_stream", lambda s=None: None)
-    z = lambda *s, t=torch.uint8: torch.zeros(*s, dtype=t)
-    # (the library refuses layer 1 of one and a scale block of 8: nothing is launched)
+    T = lambda i, dtype: _T(int(i == odd), dtype)
     kw = dict(n_layers=1, layer_stride=4096, head_stride=2048, tok_stride=64)
-    kw8 = dict(scale_block=8, scale_layer_stride=4, scale_head_stride=2)
+    kw8 = dict(scale_block=8, scale_layer_stride=4, scale_head_stride=2)   # (a scale block that the library refuses)
 
     def cache(eight):
-        pools = [z(2, 32, 64, t=torch.uint8 if eight else torch.bfloat16) for _ in range(2)]
-        scales = [z(2, 2) for _ in range(2)] if eight else []
-        table = [z(1, 2, t=torch.int32)] if paged else []
-        if eight:
-            kv = (cc.kv8_paged(*pools, *scales, *table, page_stride=4096, page_size=32, scale_page_stride=4, **kw, **kw8) if paged
-                  else cc.kv8_contiguous(*pools, *scales, **kw, **kw8))
-        else:
-            kv = cc.kv_paged(*pools, *table, page_stride=4096, page_size=32, **kw) if paged else cc.kv_contiguous(*pools, **kw)
-        return kv, pools + scales + table
+        pools = [T(i, torch.uint8 if eight else torch.bfloat16) for i in (0, 1)]
+        table = [T(2, torch.int32)] if paged else []
+        scales = [T(i, torch.uint8) for i in (3, 4)]
+        if not eight:
+            return cc.kv_paged(*pools, *table, page_stride=4096, page_size=32, **kw) if paged else cc.kv_contiguous(*pools, **kw)
+        if paged:
+            return cc.kv8_paged(*pools, *scales, *table, page_stride=4096, page_size=32, scale_page_stride=4, **kw, **kw8)
+        return cc.kv8_contiguous(*pools, *scales, **kw, **kw8)
 
-    p = cc.problem(dtype="bf16", cu_seqlens=[0, 2], n_heads_q=4, n_heads_kv=2, head_dim=64, hidden=64, vocab=1, rope_theta=1e4,
-                   device="cpu")
-    k, lens = z(2, 2, 64, t=torch.bfloat16), z(1, t=torch.int32)
-    (a, ta), (b, tb), (c, tc) = cache(False), cache(True), cache(True)
-    for call, parts in ((lambda: cc.cc_append_kv(p, a, k, k, lens, capacity=32, layer=1), ta),
-                        (lambda: cc.cc_append_kv8(p, b, k, k, lens, capacity=32), tb),
-                        (lambda: cc.cc_compact_kv8(p, b, lens, [1], 0, out=c), tb + tc),
-                        (lambda: cc.cc_attention_kv8(p, z(2, 4, 64, t=torch.bfloat16), b, 0, lens, 10, workspace=z(1 << 16)), tb)):
-        with pytest.raises(cc.CCError):
+    p = cc.Problem(_problem((0, 2), n_heads_q=4, head_dim=64), None, T(5, torch.int32), None)
+    here = lambda dtype, *shape: _T(0, dtype, shape)
+    lens = here(torch.int32, 1, 1)
+    k = torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    k.get_device = lambda: 0
+    q = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    q.get_device = lambda: 0
+    away = odd in ({0, 1, 2, 5} if paged else {0, 1, 5})
+    away8 = odd in ({0, 1, 2, 3, 4, 5} if paged else {0, 1, 3, 4, 5})
+    for call, is_away in ((lambda: cc.cc_append_kv(p, cache(False), k, k, lens, capacity=32, layer=1), away),
+                          (lambda: cc.cc_append_kv8(p, cache(True), k, k, lens, capacity=32), away8),
+                          (lambda: cc.cc_compact_kv8(p, cache(True), lens, [1], 0, out=cache(True)), away8),
+                          (lambda: cc.cc_attention_kv8(p, q, cache(True), 0, lens, 10, q, workspace=here(torch.uint8, 1, 1 << 16)), away8)):
+        with pytest.raises(ValueError if is_away else cc.CCError, match="different devices" if is_away else None):
             call()
-        missing = {id(x) for x in parts + [p.cu_d]} - set(seen[-1])
-        assert not missing
 
 
 def test_logprobs_without_ids_have_no_logprob(monkeypatch):
