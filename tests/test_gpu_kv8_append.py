@@ -295,7 +295,7 @@ def test_append_to_a_block_of_the_largest_scale(d, dtype):
                 np.testing.assert_array_equal(gc, c)
 
 
-def test_more_layers_than_one_launch_has_workgroups_for():
+def test_more_layers_than_one_launch_has_workgroups_for(memory_given_back):
     """One token each of 4096 sequences into 2100 layers: past 2^24 workgroups, the last layers come with a
     second launch."""
     from paper_2607_27600_amd import cc

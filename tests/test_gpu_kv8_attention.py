@@ -395,7 +395,7 @@ def test_values_past_bf16_reach_only_rows_that_see_them(new, n, d, mask, byte, c
     assert_attention_close(np.where(hit, 0, o), np.where(hit, 0, want))
 
 
-def test_more_row_blocks_than_one_launch_has():
+def test_more_row_blocks_than_one_launch_has(memory_given_back):
     """A long chunk beside hundreds of short ones, 64 heads: (blocks of the longest) * sequences * heads passes
     2^24 workgroups; the long one's last block comes with a second launch."""
     from paper_2607_27600_amd import cc
@@ -428,7 +428,7 @@ def test_more_row_blocks_than_one_launch_has():
     assert not (o == 7.0).all(-1).any()     # every row has been written
 
 
-def test_more_rows_to_join_than_one_launch_has():
+def test_more_rows_to_join_than_one_launch_has(memory_given_back):
     """Few rows of 130 sequences and 2^16 heads, 32 at the most: past 2^24 workgroups of the join, whose second
     launch has the last sequences; of the last one, heads 877 and 3364 are cut between two workgroups' shares."""
     from paper_2607_27600_amd import cc

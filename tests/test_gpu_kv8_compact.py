@@ -224,7 +224,7 @@ def test_the_largest_scales(d, in_place):
     np.testing.assert_array_equal(gc[~nan], want[~nan])
 
 
-def test_more_chunks_than_one_launch_has():
+def test_more_chunks_than_one_launch_has(memory_given_back):
     """Out of place, 64 lists of 32 layers and 64 heads, one of them so long that the chunks of all pass 2^24
     workgroups: the longest list's last chunks come with a second launch.  Ids move once."""
     from paper_2607_27600_amd import cc
