@@ -470,8 +470,9 @@ cc_status cc_attention_kv8_workspace(const cc_problem* p, int32_t mask, int32_t 
  * a query may not attend to does not reach it, whatever it holds; a NaN code in one that it
  * attends to gives NaN.  Elements are taken in bf16 (exactly, from 2^-126 to below 2^128; those of
  * 2^128 and more, which scales above 2^119 can have, are infinite and make what they reach infinite or NaN).
- * Sums, maxima and outputs are kept in fp32 until the last rounding; the probabilities enter
- * the second product in bf16.  n_seqs * n_heads_kv is below 2^24. */
+ * Sums, maxima and outputs are kept in fp32 until the last rounding (weighted sums before the
+ * division, of weights up to 2^8: values that take these past fp32 give infinities); the
+ * probabilities enter the second product in bf16.  n_seqs * n_heads_kv is below 2^24. */
 cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv, int32_t layer,
                            int32_t mask, const int32_t* kv_lens, int32_t max_kv_len, void* o,
                            void* workspace, size_t workspace_bytes, void* stream);

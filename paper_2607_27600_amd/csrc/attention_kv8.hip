@@ -29,7 +29,6 @@
 namespace cc {
 namespace {
 
-
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
