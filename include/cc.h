@@ -477,6 +477,88 @@ cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv,
                            int32_t mask, const int32_t* kv_lens, int32_t max_kv_len, void* o,
                            void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------ attention over a bf16 cache */
+
+/* Workspace for cc_attention_kv. */
+cc_status cc_attention_kv_workspace(const cc_problem* p, int32_t max_kv_len, size_t* bytes);
+
+/* Causal attention over layer `layer` of a cache in bf16, the inference cycle's own: whole prompts, chunks,
+ * single tokens.  o[i][h][:] = sum_j softmax_j(scale * q[i][h] . k[j][c]) v[j][c], c = h / g.  The problem's
+ * cu_seqlens count the QUERIES of each sequence, packed one sequence after another; with n_b = kv_lens[b] entries
+ * in the cache and m_b queries in the call, query i of a sequence stands at entry n_b - m_b + i (the queries are
+ * the last entries) and attends to the entries up to and including its own.  With more queries than entries
+ * the first stand before entry 0.  A query with no entry to attend to has a zero output.  q, o: [N][Hq][head_dim]
+ * bf16, packed, not overlapping.  lse (nullable): float [N][Hq], log sum_j exp(scale * q . k[j]), -inf without an
+ * entry.  kv_lens: device [n_seqs] entries in the cache (the queries' own among them), read on the device, so a
+ * captured call follows lengths that advance between replays; max_kv_len: host, at least every kv_lens[b] (longer
+ * ones are cut there, negative ones are 0), sizes the launch and the workspace.  The pages of a sequence's entries
+ * have valid ids; tok_stride is below 2^27.  Entries past kv_lens[b] do not reach an output, and one that a query
+ * may not attend to does not reach it, whatever it holds (NaN and infinities included).  Sums, maxima and outputs are
+ * kept in fp32 until the last rounding; the probabilities enter the second product in bf16.  p->diag is not looked at. */
+cc_status cc_attention_kv(const cc_problem* p, const void* q, const cc_kv* kv, int32_t layer,
+                          const int32_t* kv_lens, int32_t max_kv_len, void* o, float* lse, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Prefixes that runs of sequences share: the entries of sequences first_seq[i] .. first_seq[i+1]-1 are those of
+ * prefix i followed by their own.  The prefixes lie in a cache view of their own, in which prefix i is "sequence" i
+ * (a paged cache may hold both: two views with a block table each). */
+typedef struct cc_prefix {
+  cc_kv kv;                    /* of the problem's type */
+  int32_t n_prefixes;          /* >= 1 */
+  int32_t max_len;             /* at least every lens[i] (longer ones are cut there, negative ones are 0) */
+  const int32_t* first_seq_h;  /* host [n_prefixes+1], 0 first, non-decreasing, n_seqs last */
+  const int32_t* first_seq_d;  /* the same values in device memory */
+  const int32_t* lens;         /* device [n_prefixes] entries, read on the device */
+} cc_prefix;
+
+/* Workspace for cc_attention_prefix (the prefix's pointers are unused but for first_seq_h). */
+cc_status cc_attention_prefix_workspace(const cc_problem* p, const cc_prefix* prefix, int32_t max_kv_len,
+                                        size_t* bytes);
+
+/* cc_attention_kv of sequences behind shared prefixes: a query attends to all of its prefix and to its
+ * sequence's own entries up to its own; kv, kv_lens and max_kv_len are the own entries'.  A prefix is read for the
+ * queries of its whole run together.  Layer `layer` of both caches. */
+cc_status cc_attention_prefix(const cc_problem* p, const void* q, const cc_prefix* prefix, const cc_kv* kv,
+                              int32_t layer, const int32_t* kv_lens, int32_t max_kv_len, void* o, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------ eviction by attention weight */
+
+/* Accumulated attention weights: float, of entry t of sequence b for KV head h at
+ * base + b*seq_stride + h*head_stride + t (strides in elements). */
+typedef struct cc_weights {
+  float* base;
+  int64_t seq_stride, head_stride;
+} cc_weights;
+
+/* Workspace for cc_attention_weights. */
+cc_status cc_attention_weights_workspace(const cc_problem* p, int32_t max_kv_len, size_t* bytes);
+
+/* What the entries of a cache layer receive of the queries' attention, added to what they have had:
+ *   out[b][c][t] = prev[b][c][t] + sum_{i, h in group c} exp(scale * q[i][h] . k[t][c] - lse[i][h]),  t < kv_lens[b],
+ * over the queries i that attend to entry t; q, kv_lens and max_kv_len as in cc_attention_kv, lse [N][Hq] what
+ * it (or cc_attention_prefix: weights of the own entries) returned for the same queries.  prev (nullable: zeros) may
+ * be out.  Entries at or past prev_lens[b] (device, nullable: none) have had nothing: prev is not read there, so that
+ * entries appended since need no clearing.  Entries past kv_lens[b] are left as they are.  fp32 throughout; only
+ * the keys of the cache are read.  One order of summation: the same call repeats bit for bit. */
+cc_status cc_attention_weights(const cc_problem* p, const void* q, const cc_kv* kv, int32_t layer,
+                               const int32_t* kv_lens, int32_t max_kv_len, const float* lse, const cc_weights* prev,
+                               const int32_t* prev_lens, const cc_weights* out, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* Scores for cc_select_keep from accumulated weights; the problem's cu_seqlens count the entries of each sequence,
+ * n_b.  The first p->n_frozen and the last n_recent entries of a sequence score +inf.
+ *   per_head = 0: scores[cu[b] + t] = sum_h w[b][h][t] (fp32, in the order of the heads);
+ *   per_head = 1: scores[cu[b]*Hkv + h*n_b + t] = w[b][h][t], a segment for each (sequence, KV head). */
+cc_status cc_weight_scores(const cc_problem* p, const cc_weights* w, int32_t n_recent, int32_t per_head, float* scores,
+                           void* stream);
+
+/* The weights of the kept entries, moved to the front: out[b][h][j] = w[b][h][keep[j]], j < k, with keep_idx, k_h and
+ * per_head as in cc_compact_kv.  out NULL compacts in place, else it does not overlap w.  What lies at and past k is left
+ * untouched.  A bit copy.  Needs no workspace. */
+cc_status cc_compact_weights(const cc_problem* p, const cc_weights* w, const int32_t* keep_idx, const int32_t* k_h,
+                             int32_t per_head, const cc_weights* out, void* stream);
+
 /* ------------------------------------------------------------------ log-probabilities */
 
 /* Most alternatives per row of cc_lmhead_logprobs. */

@@ -38,7 +38,9 @@ EXPORTED = [
     "cc_lmhead_fp8_workspace", "cc_lmhead_score_fp8", "cc_pack_lmhead_bytes", "cc_pack_lmhead",
     "cc_lmhead_score_packed", "cc_lmhead_score_noalloc", "cc_append_kv", "cc_append_kv8",
     "cc_compact_kv8", "cc_attention_kv8_workspace", "cc_attention_kv8",
-    "cc_lmhead_logprobs_workspace", "cc_lmhead_logprobs",
+    "cc_lmhead_logprobs_workspace", "cc_lmhead_logprobs", "cc_attention_kv_workspace", "cc_attention_kv",
+    "cc_attention_prefix_workspace", "cc_attention_prefix", "cc_attention_weights_workspace",
+    "cc_attention_weights", "cc_weight_scores", "cc_compact_weights",
 ]
 
 _c_void_p = ctypes.c_void_p
@@ -90,6 +92,15 @@ class c_append(ctypes.Structure):
     _fields_ = [("k", c_rows), ("v", c_rows), ("q", c_rows), ("q_out", _c_void_p),
                 ("cached", _c_void_p), ("pos_ids", _c_void_p), ("capacity", _i64),
                 ("layer", _i32), ("n_layers", _i32), ("rotate", _i32)]
+
+
+class c_prefix(ctypes.Structure):
+    _fields_ = [("kv", c_kv), ("n_prefixes", _i32), ("max_len", _i32),
+                ("first_seq_h", ctypes.POINTER(_i32)), ("first_seq_d", _c_void_p), ("lens", _c_void_p)]
+
+
+class c_weights(ctypes.Structure):
+    _fields_ = [("base", _c_void_p), ("seq_stride", _i64), ("head_stride", _i64)]
 
 
 def _load():
@@ -149,6 +160,19 @@ def _load():
         "cc_lmhead_logprobs": (st, [_i32, _c_void_p, _c_void_p, _i32, _i32, _i32, _i32, _c_void_p,
                                     _i32, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
                                     ctypes.c_size_t, _c_void_p]),
+        "cc_attention_kv_workspace": (st, [P(c_problem), _i32, sz]),
+        "cc_attention_kv": (st, [P(c_problem), _c_void_p, P(c_kv), _i32, _c_void_p, _i32, _c_void_p,
+                                 _c_void_p, _c_void_p, ctypes.c_size_t, _c_void_p]),
+        "cc_attention_prefix_workspace": (st, [P(c_problem), P(c_prefix), _i32, sz]),
+        "cc_attention_prefix": (st, [P(c_problem), _c_void_p, P(c_prefix), P(c_kv), _i32, _c_void_p, _i32,
+                                     _c_void_p, _c_void_p, _c_void_p, ctypes.c_size_t, _c_void_p]),
+        "cc_attention_weights_workspace": (st, [P(c_problem), _i32, sz]),
+        "cc_attention_weights": (st, [P(c_problem), _c_void_p, P(c_kv), _i32, _c_void_p, _i32, _c_void_p,
+                                      P(c_weights), _c_void_p, P(c_weights), _c_void_p, ctypes.c_size_t,
+                                      _c_void_p]),
+        "cc_weight_scores": (st, [P(c_problem), P(c_weights), _i32, _i32, _c_void_p, _c_void_p]),
+        "cc_compact_weights": (st, [P(c_problem), P(c_weights), _c_void_p, P(_i32), _i32, P(c_weights),
+                                    _c_void_p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -757,6 +781,194 @@ def cc_attention_kv8(p: Problem, q: torch.Tensor, kv: KV8, layer: int, kv_lens: 
                                  _ptr(kv_lens), max_kv_len, _ptr(o), _ptr(workspace), workspace.numel(),
                                  _stream(stream)), "cc_attention_kv8")
     return o
+
+# ---------------------------------------------------------------- attention over a bf16 cache
+
+def cc_attention_kv_workspace(p: Problem, max_kv_len: int) -> int:
+    return _query(_lib.cc_attention_kv_workspace, ctypes.byref(p.struct), max_kv_len)
+
+
+def _queries(p: Problem, q: torch.Tensor, kv: KV, kv_lens: torch.Tensor) -> None:
+    s = p.struct
+    _int32(kv_lens, s.n_seqs, "kv_lens")
+    if (q.dtype != torch.bfloat16 or q.numel() != s.cu_seqlens_h[s.n_seqs] * s.n_heads_q * s.head_dim
+            or not q.is_contiguous()):
+        raise ValueError("q must be contiguous bf16 rows [N][Hq][head_dim]")
+    _bf16_cache(kv)
+
+
+def _bf16_cache(kv: KV) -> None:
+    for t in kv.keep[:2]:
+        if t.dtype != torch.bfloat16:
+            raise ValueError(f"the cache holds {t.dtype}, expected bf16")
+
+
+def _lse(p: Problem, lse: Optional[torch.Tensor]) -> None:
+    n = p.struct.cu_seqlens_h[p.struct.n_seqs] * p.struct.n_heads_q
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != n or not lse.is_contiguous()):
+        raise ValueError(f"lse must be {n} contiguous float32 values [N][Hq]")
+
+
+def cc_attention_kv(p: Problem, q: torch.Tensor, kv: KV, layer: int, kv_lens: torch.Tensor, max_kv_len: int,
+                    o: Optional[torch.Tensor] = None, *, lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Causal attention of the queries q [N][Hq][d] (p.cu_seqlens count them) over a bf16 cache that holds
+    kv_lens[b] entries of each sequence, the queries' own last; lse [N][Hq]: filled where given."""
+    return _attention_kv(p, q, None, kv, layer, kv_lens, max_kv_len, o, lse, workspace, stream)
+
+
+def _attention_kv(p, q, pre, kv, layer, kv_lens, max_kv_len, o, lse, workspace, stream):
+    s = p.struct
+    _queries(p, q, kv, kv_lens)
+    _lse(p, lse)
+    if o is None:
+        o = _empty(q.shape, q.dtype, q.device, stream)
+    elif o.dtype != q.dtype or o.numel() != q.numel() or not o.is_contiguous():
+        raise ValueError("o must be contiguous and of q's type and size")
+    _on_gpu(q, o, lse, kv_lens, workspace, p.cu_d, kv, pre)
+    if workspace is None:
+        need = cc_attention_kv_workspace(p, max_kv_len) if pre is None else cc_attention_prefix_workspace(p, pre, max_kv_len)
+        workspace = _empty(max(1, need), torch.uint8, q.device, stream)
+    out = (_ptr(o), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream))
+    if pre is None:
+        _check(_lib.cc_attention_kv(ctypes.byref(s), _ptr(q), ctypes.byref(kv.struct), layer, _ptr(kv_lens), max_kv_len,
+                                    *out), "cc_attention_kv")
+    else:
+        _check(_lib.cc_attention_prefix(ctypes.byref(s), _ptr(q), ctypes.byref(pre.struct), ctypes.byref(kv.struct), layer,
+                                        _ptr(kv_lens), max_kv_len, *out), "cc_attention_prefix")
+    return o
+
+
+@dataclass
+class Prefix(_View):
+    """A cc_prefix plus the tensors it points at (first_h on the host)."""
+    struct: c_prefix
+    keep: list = field(default_factory=list)
+    first_h: Optional[torch.Tensor] = None
+
+
+def prefix(kv: KV, first_seq: Sequence[int], lens: torch.Tensor, max_len: int,
+           first_device: Optional[torch.Tensor] = None) -> Prefix:
+    """Prefixes that runs of sequences share: "sequence" i of the view kv, of lens[i] entries (device, int32), is
+    before the sequences first_seq[i] .. first_seq[i + 1] - 1.  first_device: the int32 values of first_seq already
+    on the device (the default copies them there and waits for the copy)."""
+    n = len(first_seq) - 1
+    if n < 1:
+        raise ValueError("first_seq holds where each prefix's sequences start, and where the last one's end")
+    _int32(lens, n, "lens")
+    _bf16_cache(kv)
+    first_h = torch.as_tensor(list(first_seq), dtype=torch.int32).contiguous()
+    if first_device is None:
+        first_d = first_h.to(lens.device)
+    elif (first_device.dtype != torch.int32 or first_device.shape != first_h.shape or not first_device.is_contiguous()):
+        raise ValueError("first_device must hold the values of first_seq as contiguous int32")
+    else:
+        first_d = first_device
+    s = c_prefix()
+    s.kv, s.n_prefixes, s.max_len = kv.struct, n, max_len
+    s.first_seq_h = ctypes.cast(first_h.data_ptr(), ctypes.POINTER(_i32))
+    s.first_seq_d, s.lens = first_d.data_ptr(), lens.data_ptr()
+    return Prefix(s, [kv, lens, first_d], first_h)
+
+
+def cc_attention_prefix_workspace(p: Problem, prefix: Prefix, max_kv_len: int) -> int:
+    return _query(_lib.cc_attention_prefix_workspace, ctypes.byref(p.struct), ctypes.byref(prefix.struct), max_kv_len)
+
+
+def cc_attention_prefix(p: Problem, q: torch.Tensor, prefix: Prefix, kv: KV, layer: int, kv_lens: torch.Tensor,
+                        max_kv_len: int, o: Optional[torch.Tensor] = None, *, lse: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """cc_attention_kv of sequences behind shared prefixes; kv, kv_lens and max_kv_len are their own entries'."""
+    return _attention_kv(p, q, prefix, kv, layer, kv_lens, max_kv_len, o, lse, workspace, stream)
+
+
+# ---------------------------------------------------------------- eviction by attention weight
+
+def _weights(p: Problem, w: torch.Tensor, what: str, longest: int) -> c_weights:
+    """The view of weights w [n_seqs][Hkv][entries], entries contiguous."""
+    s = p.struct
+    if w.dtype != torch.float32:
+        raise ValueError(f"{what} is {w.dtype}, expected float32")
+    if w.dim() != 3 or w.shape[0] != s.n_seqs or w.shape[1] != s.n_heads_kv or w.shape[2] < longest:
+        raise ValueError(f"{what} has shape {tuple(w.shape)}, expected {(s.n_seqs, s.n_heads_kv)} and at least {longest} entries")
+    if w.shape[2] > 1 and w.stride(2) != 1:
+        raise ValueError(f"entries of {what} must be contiguous")
+    return c_weights(w.data_ptr(), w.stride(0) if s.n_seqs > 1 else 0, w.stride(1) if s.n_heads_kv > 1 else 0)
+
+
+def _own_places(w: torch.Tensor, what: str) -> None:
+    """Rows that are written may not overlap."""
+    at = sorted((st, n) for st, n in zip(w.stride(), w.shape) if n > 1)
+    for (st, n), (up, _) in zip(at, at[1:]):
+        if up < st * n:
+            raise ValueError(f"{what} overlaps itself (strides {w.stride()})")
+
+
+def cc_attention_weights_workspace(p: Problem, max_kv_len: int) -> int:
+    return _query(_lib.cc_attention_weights_workspace, ctypes.byref(p.struct), max_kv_len)
+
+
+def cc_attention_weights(p: Problem, q: torch.Tensor, kv: KV, layer: int, kv_lens: torch.Tensor, max_kv_len: int,
+                         lse: torch.Tensor, out: torch.Tensor, *, prev: Optional[torch.Tensor] = None,
+                         prev_lens: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+    """What each entry receives of the attention of q [N][Hq][d] (lse [N][Hq] as cc_attention_kv filled it), added to
+    prev where that is given (of the first prev_lens[b] entries; all without): out [n_seqs][Hkv][entries], which may
+    be prev."""
+    s = p.struct
+    _queries(p, q, kv, kv_lens)
+    _lse(p, lse)
+    _int32(prev_lens, s.n_seqs, "prev_lens")
+    if prev is None and prev_lens is not None:
+        raise ValueError("prev_lens without prev")
+    to = _weights(p, out, "out", max_kv_len)
+    _own_places(out, "out")
+    had = _weights(p, prev, "prev", 0 if prev_lens is not None else max_kv_len) if prev is not None else None
+    _on_gpu(q, lse, out, prev, prev_lens, kv_lens, workspace, p.cu_d, kv)
+    if workspace is None:
+        workspace = _empty(max(1, cc_attention_weights_workspace(p, max_kv_len)), torch.uint8, q.device, stream)
+    _check(_lib.cc_attention_weights(ctypes.byref(s), _ptr(q), ctypes.byref(kv.struct), layer, _ptr(kv_lens), max_kv_len,
+                                     _ptr(lse), ctypes.byref(had) if had is not None else None, _ptr(prev_lens),
+                                     ctypes.byref(to), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                     _stream(stream)), "cc_attention_weights")
+    return out
+
+
+def cc_weight_scores(p: Problem, w: torch.Tensor, n_recent: int, per_head: int, scores: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """Scores for cc_select_keep from weights w [n_seqs][Hkv][entries] (p.cu_seqlens count the entries): one segment for
+    each sequence, or with per_head for each of its KV heads; the first p.n_frozen and the last n_recent are +inf."""
+    s = p.struct
+    cu = s.cu_seqlens_h[:s.n_seqs + 1]
+    view = _weights(p, w, "w", max(b - a for a, b in zip(cu, cu[1:])))
+    n = cu[-1] * (s.n_heads_kv if per_head else 1)
+    if scores is None:
+        scores = _empty((n,), torch.float32, w.device, stream)
+    elif scores.dtype != torch.float32 or scores.numel() < n or not scores.is_contiguous():
+        raise ValueError(f"scores must be at least {n} contiguous float32 values")
+    _on_gpu(w, scores, p.cu_d)
+    _check(_lib.cc_weight_scores(ctypes.byref(s), ctypes.byref(view), n_recent, int(per_head), _ptr(scores),
+                                 _stream(stream)), "cc_weight_scores")
+    return scores
+
+
+def cc_compact_weights(p: Problem, w: torch.Tensor, keep_idx: torch.Tensor, k: Sequence[int], per_head: int,
+                       out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The weights of the kept entries, moved to the front of w [n_seqs][Hkv][entries] (or of out)."""
+    s = p.struct
+    kk, n = _host_array(k, np.int32, _i32)
+    if n != s.n_seqs * (s.n_heads_kv if per_head else 1):
+        raise ValueError(f"{n} budgets for {s.n_seqs} sequences")
+    if keep_idx is not None and (keep_idx.dtype != torch.int32 or keep_idx.numel() < sum(k) or not keep_idx.is_contiguous()):
+        raise ValueError(f"keep_idx must be {sum(k)} contiguous int32 values")
+    cu = s.cu_seqlens_h[:s.n_seqs + 1]
+    src = _weights(p, w, "w", max(b - a for a, b in zip(cu, cu[1:])))
+    dst = _weights(p, out, "out", max(k, default=0)) if out is not None else None
+    _own_places(w if out is None else out, "w" if out is None else "out")
+    _on_gpu(w, keep_idx, out, p.cu_d)
+    _check(_lib.cc_compact_weights(ctypes.byref(s), ctypes.byref(src), _ptr(keep_idx), kk, int(per_head),
+                                   ctypes.byref(dst) if dst is not None else None, _stream(stream)), "cc_compact_weights")
+
 
 # ---------------------------------------------------------------- log-probabilities
 

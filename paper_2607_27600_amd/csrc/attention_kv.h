@@ -1,0 +1,125 @@
+// What the kernels of the attention over a bf16 cache share with each other and with the planner.
+#pragma once
+
+#include "cc_internal.h"
+
+namespace cc {
+
+// One tensor pair of a cache: keys and values alike but for their base, strides in bytes.
+struct KvPair {
+  KvView at;                   // of the keys
+  const void* v;
+  int32_t paged;
+};
+
+// Attention of the queries of n_seqs sequences to the entries of a prefix (n_prefixes = 0: none) and to
+// their own entries up to their own.
+struct KvAttnArgs {
+  const u16* q;
+  u16* o;
+  float* lse;                  // or null
+  KvPair own, pre;
+  const int32_t *cu, *lens;    // queries and own entries of the sequences
+  const int32_t *pre_first, *pre_lens;   // sequences [pre_first[i], pre_first[i + 1]) are behind prefix i
+  int n_seqs, n_prefixes;
+  int layer, max_len, pre_max;
+  int hq, hkv, g, head_dim;
+  int N;                       // queries in all
+  float scale, c2;             // c2 = scale * log2(e)
+  float room;                  // how far a logit may pass a row's reference maximum: 2^8 in probability
+};
+hipError_t launch_attention_kv(const KvAttnArgs& a, hipStream_t s);
+
+// What entries receive of the queries' attention, added to what they have.
+struct KvWeightsArgs {
+  const u16* q;
+  const float* lse;            // [N][Hq]
+  KvPair own;
+  const int32_t *cu, *lens;
+  const int32_t* prev_lens;    // or null: every entry has some
+  const float* prev;           // or null: none has
+  float* w;
+  int64_t w_seq, w_head, prev_seq, prev_head;
+  int n_seqs, layer, max_len, hq, hkv, g, head_dim, most;   // most: most queries of a sequence
+  float c2;
+};
+hipError_t launch_attention_weights(const KvWeightsArgs& a, hipStream_t s);
+
+struct WeightScoresArgs {
+  const float* w;
+  int64_t w_seq, w_head;
+  float* scores;
+  const int32_t* cu;
+  int n_seqs, hkv, per_head, recent, frozen, longest;
+};
+hipError_t launch_weight_scores(const WeightScoresArgs& a, hipStream_t s);
+
+struct CompactWeightsArgs {
+  float *w, *out;              // out = w: in place
+  int64_t w_seq, w_head, out_seq, out_head;
+  const int32_t* keep;
+  const int32_t* k_h;          // host
+  int n_seqs, hkv, per_head;
+};
+hipError_t launch_compact_weights(const CompactWeightsArgs& a, hipStream_t s);
+
+// ---- shared by the attention kernels
+
+// A wave-uniform pointer in scalar registers.
+__device__ __forceinline__ const char* uniform_ptr(const char* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(u));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(u >> 32));
+  return reinterpret_cast<const char*>((uint64_t(hi) << 32) | lo);
+}
+
+// Bits 15 and 31 where the low and the high bf16 of a word are NaN or infinite.
+__device__ __forceinline__ uint32_t wide_halves(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+// 0xffff at bits 15 and 31.
+__device__ __forceinline__ uint32_t whole_halves(uint32_t m) { return (m >> 15) * 0xffffu; }
+
+// The log-sum-exp of a row from its reference logit and its sum of 2^((z - ref) c2).
+__device__ __forceinline__ float row_lse(float ref, float sum, float scale) {
+  return sum == 0.f ? -INFINITY : fmaf(ref, scale, __logf(sum));
+}
+
+// The last b with start(b) <= x among 0 .. n - 1, start rising from start(0) <= x.
+template <class F>
+__device__ __forceinline__ int last_at(int n, F start, int64_t x) {
+  int b = 0;
+  while (n > 1) {
+    const int half = n >> 1;
+    const bool up = start(b + half) <= x;
+    b = up ? b + half : b;
+    n = up ? n - half : half;
+  }
+  return b;
+}
+
+// A plane: one (sequence, layer, KV head).  16-entry groups lie in one page.
+struct KvPlane {
+  const char *k, *v;
+  const int32_t* table;
+  uint32_t ts;                 // bytes between entries
+  int paged, page_shift, page_mask;
+  int64_t page_stride;
+  __device__ __forceinline__ int page(int group) const { return paged ? table[group >> (page_shift - 4)] : 0; }
+  __device__ __forceinline__ int64_t offset(int page, int entry) const {
+    return int64_t(page) * page_stride + int64_t(paged ? entry & page_mask : entry) * ts;
+  }
+};
+__device__ __forceinline__ KvPlane kv_plane(const KvPair& p, int b, int layer, int h) {
+  const int64_t c = int64_t(layer) * p.at.layer_stride + int64_t(h) * p.at.head_stride + (p.paged ? 0 : int64_t(b) * p.at.seq_stride);
+  KvPlane x;
+  x.k = static_cast<const char*>(p.at.base) + c;
+  x.v = static_cast<const char*>(p.v) + c;
+  x.table = p.at.block_table + (p.paged ? int64_t(b) * p.at.max_pages : 0);
+  x.ts = uint32_t(p.at.tok_stride);
+  x.paged = p.paged;
+  x.page_shift = p.at.page_shift;
+  x.page_mask = p.at.page_mask;
+  x.page_stride = p.at.page_stride;
+  return x;
+}
+
+}  // namespace cc

@@ -8,6 +8,7 @@
 #include <mutex>
 #include <vector>
 
+#include "attention_kv.h"
 #include "attention_kv8.h"
 #include "cc_internal.h"
 
@@ -1251,6 +1252,215 @@ cc_status cc_attention_kv8(const cc_problem* p, const void* q, const cc_kv8* kv,
     CC_HIP(launch_attention_kv8(a, i == 0, static_cast<hipStream_t>(stream)));
     off += c.total;
   }
+  return CC_OK;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ attention over a bf16 cache
+
+namespace {
+
+cc_status check_attention_kv(const cc_problem* p, int32_t max_len) {
+  CC_TRY(check_problem(p));
+  if (max_len < 0 || max_len > INT32_MAX - 4096) return CC_ERR_SHAPE;
+  if (p->dtype != CC_BF16) return CC_ERR_UNSUPPORTED;
+  if (int64_t(n_tokens(p)) * (p->n_heads_q / p->n_heads_kv) > INT32_MAX - 4096) return CC_ERR_UNSUPPORTED;
+  // what a launch has workgroups for, at the least
+  if (int64_t(p->n_seqs) * p->n_heads_kv > MOST_GROUPS / 2) return CC_ERR_UNSUPPORTED;
+  return CC_OK;
+}
+
+cc_status check_view16(const cc_problem* p, const cc_kv* kv, int32_t layer, int32_t max_len) {
+  CC_TRY(check_kv(p, kv, 1, 0, max_len));
+  if (layer < 0 || layer >= kv->n_layers) return CC_ERR_ARG;
+  if (kv->tok_stride >= int64_t(1) << 27) return CC_ERR_UNSUPPORTED;   // 16 entries by 32-bit offsets
+  return CC_OK;
+}
+
+cc_status check_prefix(const cc_problem* p, const cc_prefix* x) {
+  if (!x || x->n_prefixes < 1 || !x->first_seq_h) return CC_ERR_ARG;
+  if (x->max_len < 0 || x->max_len > INT32_MAX - 4096) return CC_ERR_SHAPE;
+  if (x->first_seq_h[0] != 0 || x->first_seq_h[x->n_prefixes] != p->n_seqs) return CC_ERR_SHAPE;
+  for (int i = 0; i < x->n_prefixes; ++i)
+    if (x->first_seq_h[i + 1] < x->first_seq_h[i]) return CC_ERR_SHAPE;
+  if (int64_t(x->n_prefixes) * p->n_heads_kv > MOST_GROUPS / 2) return CC_ERR_UNSUPPORTED;
+  return CC_OK;
+}
+
+KvPair make_pair(const cc_kv* kv) { return KvPair{make_view(kv, kv->k, 2), kv->v, kv->layout == CC_KV_PAGED}; }
+
+// Both attentions.
+cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* prefix, const cc_kv* kv, int32_t layer,
+                           const int32_t* kv_lens, int32_t max_kv_len, void* o, float* lse, void* ws, size_t ws_bytes,
+                           void* stream) {
+  CC_TRY(check_view16(p, kv, layer, max_kv_len));
+  if (prefix) CC_TRY(check_view16(p, &prefix->kv, layer, prefix->max_len));
+  const int N = n_tokens(p);
+  if (N > 0 && (!q || !o || !kv_lens || !aligned16(q) || !aligned16(o))) return CC_ERR_ARG;
+  if (N > 0 && prefix && (!prefix->first_seq_d || !prefix->lens)) return CC_ERR_ARG;
+  CC_TRY(check_ws(ws, ws_bytes, 0));
+  if (N == 0) return CC_OK;
+  KvAttnArgs a{};
+  a.q = static_cast<const u16*>(q);
+  a.o = static_cast<u16*>(o);
+  a.lse = lse;
+  a.own = make_pair(kv);
+  a.cu = p->cu_seqlens_d;
+  a.lens = kv_lens;
+  if (prefix) {
+    a.pre = make_pair(&prefix->kv);
+    a.pre_first = prefix->first_seq_d;
+    a.pre_lens = prefix->lens;
+    a.n_prefixes = prefix->n_prefixes;
+    a.pre_max = prefix->max_len;
+  }
+  a.n_seqs = p->n_seqs;
+  a.layer = layer;
+  a.max_len = max_kv_len;
+  a.hq = p->n_heads_q;
+  a.hkv = p->n_heads_kv;
+  a.g = p->n_heads_q / p->n_heads_kv;
+  a.head_dim = p->head_dim;
+  a.N = N;
+  a.scale = softmax_scale(p);
+  a.c2 = a.scale * kLog2e;
+  a.room = std::min(8.f / a.c2, FLT_MAX);   // (finite: a first logit passes -inf by more)
+  CC_HIP(launch_attention_kv(a, static_cast<hipStream_t>(stream)));
+  return CC_OK;
+}
+
+// written: each (sequence, KV head) needs a place of its own.
+cc_status check_weights(const cc_problem* p, const cc_weights* w, bool written) {
+  if (!w || !w->base) return CC_ERR_ARG;
+  if (w->seq_stride < 0 || w->head_stride < 0) return CC_ERR_SHAPE;
+  if (written && ((w->seq_stride == 0 && p->n_seqs > 1) || (w->head_stride == 0 && p->n_heads_kv > 1))) return CC_ERR_SHAPE;
+  return CC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cc_status cc_attention_kv_workspace(const cc_problem* p, int32_t max_kv_len, size_t* bytes) {
+  if (!bytes) return CC_ERR_ARG;
+  CC_TRY(check_attention_kv(p, max_kv_len));
+  *bytes = 0;
+  return CC_OK;
+}
+
+cc_status cc_attention_kv(const cc_problem* p, const void* q, const cc_kv* kv, int32_t layer, const int32_t* kv_lens,
+                          int32_t max_kv_len, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  CC_TRY(check_attention_kv(p, max_kv_len));
+  return run_attention_kv(p, q, nullptr, kv, layer, kv_lens, max_kv_len, o, lse, ws, ws_bytes, stream);
+}
+
+cc_status cc_attention_prefix_workspace(const cc_problem* p, const cc_prefix* prefix, int32_t max_kv_len,
+                                        size_t* bytes) {
+  if (!bytes) return CC_ERR_ARG;
+  CC_TRY(check_attention_kv(p, max_kv_len));
+  CC_TRY(check_prefix(p, prefix));
+  *bytes = 0;
+  return CC_OK;
+}
+
+cc_status cc_attention_prefix(const cc_problem* p, const void* q, const cc_prefix* prefix, const cc_kv* kv, int32_t layer,
+                              const int32_t* kv_lens, int32_t max_kv_len, void* o, float* lse, void* ws, size_t ws_bytes,
+                              void* stream) {
+  CC_TRY(check_attention_kv(p, max_kv_len));
+  CC_TRY(check_prefix(p, prefix));
+  return run_attention_kv(p, q, prefix, kv, layer, kv_lens, max_kv_len, o, lse, ws, ws_bytes, stream);
+}
+
+cc_status cc_attention_weights_workspace(const cc_problem* p, int32_t max_kv_len, size_t* bytes) {
+  if (!bytes) return CC_ERR_ARG;
+  CC_TRY(check_attention_kv(p, max_kv_len));
+  *bytes = 0;
+  return CC_OK;
+}
+
+cc_status cc_attention_weights(const cc_problem* p, const void* q, const cc_kv* kv, int32_t layer, const int32_t* kv_lens,
+                               int32_t max_kv_len, const float* lse, const cc_weights* prev, const int32_t* prev_lens,
+                               const cc_weights* out, void* ws, size_t ws_bytes, void* stream) {
+  CC_TRY(check_attention_kv(p, max_kv_len));
+  CC_TRY(check_view16(p, kv, layer, max_kv_len));
+  CC_TRY(check_weights(p, out, true));
+  if (prev) CC_TRY(check_weights(p, prev, false));
+  if (prev && prev->base == out->base && (prev->seq_stride != out->seq_stride || prev->head_stride != out->head_stride))
+    return CC_ERR_ARG;
+  if (!prev && prev_lens) return CC_ERR_ARG;
+  const int N = n_tokens(p);
+  if (!kv_lens || (N > 0 && (!q || !lse || !aligned16(q)))) return CC_ERR_ARG;
+  CC_TRY(check_ws(ws, ws_bytes, 0));
+  if (max_kv_len == 0) return CC_OK;
+  KvWeightsArgs a{};
+  a.q = static_cast<const u16*>(q);
+  a.lse = lse;
+  a.own = make_pair(kv);
+  a.cu = p->cu_seqlens_d;
+  a.lens = kv_lens;
+  a.prev_lens = prev_lens;
+  if (prev) {
+    a.prev = prev->base;
+    a.prev_seq = prev->seq_stride;
+    a.prev_head = prev->head_stride;
+  }
+  a.w = out->base;
+  a.w_seq = out->seq_stride;
+  a.w_head = out->head_stride;
+  a.n_seqs = p->n_seqs;
+  a.layer = layer;
+  a.max_len = max_kv_len;
+  a.hq = p->n_heads_q;
+  a.hkv = p->n_heads_kv;
+  a.g = p->n_heads_q / p->n_heads_kv;
+  a.head_dim = p->head_dim;
+  a.most = max_len(p);
+  a.c2 = softmax_scale(p) * kLog2e;
+  CC_HIP(launch_attention_weights(a, static_cast<hipStream_t>(stream)));
+  return CC_OK;
+}
+
+cc_status cc_weight_scores(const cc_problem* p, const cc_weights* w, int32_t n_recent, int32_t per_head, float* scores,
+                           void* stream) {
+  CC_TRY(check_problem(p));
+  if (per_head != 0 && per_head != 1) return CC_ERR_ARG;
+  if (n_recent < 0) return CC_ERR_ARG;
+  CC_TRY(check_weights(p, w, false));
+  if (n_tokens(p) == 0) return CC_OK;
+  if (!scores) return CC_ERR_ARG;
+  const int longest = max_len(p);
+  if ((int64_t(longest) + 255) / 256 * (per_head ? p->n_heads_kv : 1) * p->n_seqs > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+  const WeightScoresArgs a{w->base, w->seq_stride, w->head_stride, scores, p->cu_seqlens_d, p->n_seqs, p->n_heads_kv,
+                           per_head, n_recent, p->n_frozen, longest};
+  CC_HIP(launch_weight_scores(a, static_cast<hipStream_t>(stream)));
+  return CC_OK;
+}
+
+cc_status cc_compact_weights(const cc_problem* p, const cc_weights* w, const int32_t* keep_idx, const int32_t* k_h,
+                             int32_t per_head, const cc_weights* out, void* stream) {
+  CC_TRY(check_problem(p));
+  if (per_head != 0 && per_head != 1) return CC_ERR_ARG;
+  if (!k_h) return CC_ERR_ARG;
+  CC_TRY(check_weights(p, w, !out));
+  if (out) {
+    CC_TRY(check_weights(p, out, true));
+    if (out->base == w->base) return CC_ERR_ARG;
+  }
+  const int per = per_head ? p->n_heads_kv : 1;
+  if (int64_t(p->n_heads_kv) >= 1 << 20 || int64_t(p->n_seqs) * p->n_heads_kv > INT32_MAX) return CC_ERR_UNSUPPORTED;
+  int64_t all = 0;
+  for (int64_t i = 0; i < int64_t(p->n_seqs) * per; ++i) {
+    const int b = int(i / per);
+    if (k_h[i] < 0 || k_h[i] > p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) return CC_ERR_SHAPE;
+    all += k_h[i];
+  }
+  if (all == 0) return CC_OK;
+  if (!keep_idx) return CC_ERR_ARG;
+  const cc_weights* to = out ? out : w;
+  const CompactWeightsArgs a{w->base, to->base, w->seq_stride, w->head_stride, to->seq_stride, to->head_stride,
+                             keep_idx, k_h, p->n_seqs, p->n_heads_kv, per_head};
+  CC_HIP(launch_compact_weights(a, static_cast<hipStream_t>(stream)));
   return CC_OK;
 }
 

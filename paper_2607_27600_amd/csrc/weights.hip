@@ -1,0 +1,205 @@
+// Accumulated attention weight: what each cached entry receives of the attention of a call's queries,
+//   w[b][c][t] = prev[b][c][t] + sum_{i, h in group c} exp(scale * q[i][h] . k[t][c] - lse[i][h])
+// over the queries i that stand at or after entry t, the scores that select by it, and its compaction.
+//
+// A wave holds 16 KB entries of a (sequence, KV head) as the A operands of 16x16x32 MFMA and takes the rows
+// (query, head of the group) that see them 16 at a time.  A lane then holds four entries of one row, so the sum
+// over rows stays in its registers until the end, where 16 lanes are added up: no atomics, one order.
+// Products and sums are fp32.
+#include <algorithm>
+
+#include "attention_kv.h"
+
+namespace cc {
+namespace {
+
+constexpr int NT = 256, NW = NT / 64;
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+template <int HD, int KB>
+__global__ __launch_bounds__(NT, 2) void attn_weights(KvWeightsArgs a) {
+  constexpr int NKS = HD / 32;
+  const int tid = threadIdx.x, lane = tid & 63, grp = lane >> 4, r16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const unsigned blocks = unsigned(a.max_len + NW * KB * 16 - 1) / (NW * KB * 16);
+  const int kvh = int(blockIdx.x % unsigned(a.hkv));
+  const unsigned y = blockIdx.x / unsigned(a.hkv);
+  const int b = int(y / blocks), t0 = (int(y % blocks) * NW + wave) * KB * 16;
+  const int len = min(max(a.lens[b], 0), a.max_len);
+  if (t0 >= len) return;
+  const int q0 = a.cu[b], mq = a.cu[b + 1] - q0, rows = mq * a.g, shift = len - mq;
+  const KvPlane P = kv_plane(a.own, b, a.layer, kvh);
+
+  float sum[KB][4];
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[k][e] = 0.f;
+  const int from = min(max(0, t0 - shift), mq) * a.g;   // the first row that sees an entry
+  if (from < rows) {
+    bf16x8 kf[KB][NKS];
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+      const int gg = min((t0 >> 4) + k, (len - 1) >> 4);
+      const int t = min(16 * gg + r16, len - 1);
+      const char* p = P.k + P.offset(P.page(gg), 16 * gg) + int64_t(t & 15) * P.ts + 16 * grp;
+#pragma unroll
+      for (int s = 0; s < NKS; ++s) kf[k][s] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 64 * s));
+    }
+    const int seen = min(max(0, t0 + KB * 16 - 1 - shift), mq) * a.g;   // rows from here on see all of the wave's entries
+    int i = (from + r16) / a.g, h = (from + r16) % a.g;
+    const int di = 16 / a.g, dh = 16 % a.g;
+    for (int r0 = from; r0 < rows; r0 += 16) {
+      const bool in = r0 + r16 < rows;
+      const int64_t at = int64_t(q0 + (in ? i : mq - 1)) * a.hq + kvh * a.g + (in ? h : 0);
+      const float lse = a.lse[at] * kLog2e;
+      const u16* q = a.q + at * HD + 8 * grp;
+      f32x4 z[KB];
+#pragma unroll
+      for (int k = 0; k < KB; ++k) z[k] = f32x4{};
+#pragma unroll
+      for (int s = 0; s < NKS; ++s) {
+        const bf16x8 qf = as_bf16x8(*reinterpret_cast<const uint4*>(q + 32 * s));
+#pragma unroll
+        for (int k = 0; k < KB; ++k) z[k] = mfma16(kf[k][s], qf, z[k]);
+      }
+      if (r0 < seen || r0 + 16 > rows) {
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (in && t0 + 16 * k + 4 * grp + e <= shift + i) sum[k][e] += fast_exp2(fmaf(z[k][e], a.c2, -lse));
+      } else {
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[k][e] += fast_exp2(fmaf(z[k][e], a.c2, -lse));
+      }
+      i += di;
+      h += dh;
+      if (h >= a.g) {
+        h -= a.g;
+        ++i;
+      }
+    }
+  }
+  const int had = a.prev ? (a.prev_lens ? a.prev_lens[b] : len) : 0;
+  float* w = a.w + int64_t(b) * a.w_seq + int64_t(kvh) * a.w_head;
+  const float* prev = a.prev + int64_t(b) * a.prev_seq + int64_t(kvh) * a.prev_head;
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float x = sum[k][e];
+#pragma unroll
+      for (int off = 1; off < 16; off <<= 1) x += __shfl_xor(x, off);
+      const int t = t0 + 16 * k + 4 * grp + e;
+      if (r16 == 0 && t < len) w[t] = t < had ? prev[t] + x : x;
+    }
+}
+
+__global__ __launch_bounds__(NT) void weight_scores(WeightScoresArgs a, int blocks) {
+  const int planes = a.per_head ? a.hkv : 1;
+  const int h = int(blockIdx.x % unsigned(planes));
+  const unsigned y = blockIdx.x / unsigned(planes);
+  const int b = int(y / unsigned(blocks)), t = int(y % unsigned(blocks)) * NT + int(threadIdx.x);
+  const int q0 = a.cu[b], n = a.cu[b + 1] - q0;
+  if (t >= n) return;
+  const float* w = a.w + int64_t(b) * a.w_seq + t;
+  float x = INFINITY;
+  if (t >= a.frozen && t < n - a.recent) {
+    x = w[int64_t(h) * a.w_head];
+    if (!a.per_head)
+      for (int k = 1; k < a.hkv; ++k) x += w[int64_t(k) * a.w_head];
+  }
+  a.scores[(a.per_head ? int64_t(q0) * a.hkv + int64_t(h) * n : int64_t(q0)) + t] = x;
+}
+
+// Keep lists of a launch.
+struct WeightLists {
+  static constexpr int MOST = 64;
+  int64_t off[MOST];
+  int32_t k[MOST];
+};
+constexpr int MOVE_NT = 1024, PER = 4;
+// A workgroup a plane (in place) or a chunk of one: chunks of 4096 entries.  In place, lists rise, so keep[j] >= j: what
+// a chunk writes lies before every later chunk's sources.
+__global__ __launch_bounds__(MOVE_NT) void move_weights(CompactWeightsArgs a, WeightLists lists, int first, int chunks, int in_place) {
+  const int plane = int(blockIdx.x / unsigned(chunks)), chunk = int(blockIdx.x % unsigned(chunks));
+  const int l = a.per_head ? plane : plane / a.hkv;
+  const int b = (a.per_head ? (first + plane) / a.hkv : first + l), h = (a.per_head ? first + plane : plane) % a.hkv;
+  const int n = lists.k[l];
+  const int32_t* keep = a.keep + lists.off[l];
+  const float* src = a.w + int64_t(b) * a.w_seq + int64_t(h) * a.w_head;
+  float* dst = a.out + int64_t(b) * a.out_seq + int64_t(h) * a.out_head;
+  for (int64_t c0 = int64_t(chunk) * MOVE_NT * PER; c0 < n; c0 += int64_t(chunks) * MOVE_NT * PER) {
+    float x[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int64_t j = c0 + i * MOVE_NT + int(threadIdx.x);
+      x[i] = j < n ? src[keep[j]] : 0.f;
+    }
+    if (in_place) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int64_t j = c0 + i * MOVE_NT + int(threadIdx.x);
+      if (j < n) dst[j] = x[i];
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attention_weights(const KvWeightsArgs& a, hipStream_t s) {
+  constexpr int KB = 2;
+  const int64_t blocks = (int64_t(a.max_len) + NW * KB * 16 - 1) / (NW * KB * 16) * a.hkv * a.n_seqs;
+  if (blocks > MOST_GROUPS) return hipErrorInvalidValue;
+  if (a.head_dim == 128)
+    hipLaunchKernelGGL((attn_weights<128, KB>), dim3(unsigned(blocks)), dim3(NT), 0, s, a);
+  else
+    hipLaunchKernelGGL((attn_weights<64, KB>), dim3(unsigned(blocks)), dim3(NT), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_weight_scores(const WeightScoresArgs& a, hipStream_t s) {
+  const int blocks = (a.longest + NT - 1) / NT;
+  const int64_t grid = int64_t(blocks) * (a.per_head ? a.hkv : 1) * a.n_seqs;
+  if (grid > MOST_GROUPS) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(weight_scores, dim3(unsigned(grid)), dim3(NT), 0, s, a, blocks);
+  return hipGetLastError();
+}
+
+hipError_t launch_compact_weights(const CompactWeightsArgs& a, hipStream_t s) {
+  const bool in_place = a.out == a.w;
+  const int64_t n = int64_t(a.n_seqs) * (a.per_head ? a.hkv : 1);
+  int64_t off = 0;
+  int longest = 0;
+  for (int64_t i = 0; i < n; ++i) longest = std::max(longest, a.k_h[i]);
+  // the lists of a launch, of fewer than 2^32 threads
+  const int64_t each = (a.per_head ? 1 : a.hkv) * (in_place ? 1 : (int64_t(longest) + MOVE_NT * PER - 1) / (MOVE_NT * PER));
+  if (each > MOST_GROUPS / 4) return hipErrorInvalidValue;
+  const int64_t step = std::min<int64_t>(WeightLists::MOST, MOST_GROUPS / 4 / std::max<int64_t>(1, each));
+  for (int64_t first = 0; first < n; first += step) {
+    const int here = int(std::min<int64_t>(step, n - first));
+    WeightLists lists;
+    int most = 0;
+    for (int i = 0; i < here; ++i) {
+      lists.off[i] = off;
+      lists.k[i] = a.k_h[first + i];
+      off += lists.k[i];
+      most = std::max(most, lists.k[i]);
+    }
+    if (most == 0) continue;
+    const int chunks = in_place ? 1 : int((int64_t(most) + MOVE_NT * PER - 1) / (MOVE_NT * PER));
+    const int64_t grid = int64_t(here) * (a.per_head ? 1 : a.hkv) * chunks;
+    hipLaunchKernelGGL(move_weights, dim3(unsigned(grid)), dim3(MOVE_NT), 0, s, a, lists, int(first), chunks, int(in_place));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace cc

@@ -1,0 +1,240 @@
+"""Attention over a bf16 cache, alone and behind shared prefixes, against fp64: prompts, chunks, drafts and single
+tokens, ragged batches, every layout, rows that see nothing, NaN and infinities where a row may not look."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv16_oracle as O
+from tests.gpu_util import assert_attention_close, f64
+from tests.kv16_util import Cache16, cu_of, i32, logit_error, problem, queries
+
+pytestmark = pytest.mark.gpu
+
+
+def _oracle(cache, q, new, lens, hq, hkv, layer=0, scale=None, pre=None, first=None, pre_lens=None):
+    """(o [N][Hq][d], lse [N][Hq], error bound of lse [N][Hq])"""
+    g, qh, d = hq // hkv, f64(q), cache.d
+    o, lse, tol = np.zeros(qh.shape), np.full(qh.shape[:2], -np.inf), np.zeros(qh.shape[:2])
+    cu = cu_of(new)
+    for b, m in enumerate(new):
+        rows = slice(cu[b], cu[b + 1])
+        for c in range(hkv if m else 0):
+            k, v = (cache.values(layer, b, c, t, lens[b]) for t in "kv")
+            kp = vp = None
+            if pre is not None:
+                i = sum(1 for x in first[1:] if x <= b)
+                kp, vp = (pre.values(layer, i, c, t, pre_lens[i]) for t in "kv")
+            ks = k if kp is None else np.concatenate([kp, k])
+            for h in range(c * g, (c + 1) * g):
+                o[rows, h], lse[rows, h] = O.attention(qh[rows, h], k, v, kp, vp, scale)
+                tol[rows, h] = logit_error(qh[rows, h], np.nan_to_num(ks, posinf=0, neginf=0),
+                                           d ** -0.5 if scale is None else scale)
+    return o, lse, tol
+
+
+def _same(o, lse, want, what=""):
+    ro, rl, tol = want
+    assert_attention_close(f64(o), ro, what)
+    got = f64(lse)
+    np.testing.assert_array_equal(np.isneginf(got), np.isneginf(rl), err_msg=what)
+    fin = np.isfinite(rl)
+    # (and the last rounding of a number of that size, the log's and the sum's)
+    err = np.abs(got[fin] - rl[fin])
+    bad = err > tol[fin] + 2.0 ** -22 * (1 + np.abs(rl[fin]))
+    assert not bad.any(), f"{what}: lse off by {err[bad].max()}"
+
+
+def _run(cc, cache, q, new, lens, hq, hkv, layer=0, longest=None, pre=None, first=None, pre_lens=None, pre_longest=None, **kw):
+    p = problem(cc, new, hq, hkv, cache.d, **kw)
+    o = torch.full_like(q, 7.0)
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    longest = max(lens) if longest is None else longest
+    if pre is None:
+        cc.cc_attention_kv(p, q, cache.view(cc), layer, i32(lens), longest, o, lse=lse)
+    else:
+        x = cc.prefix(pre.view(cc), first, i32(pre_lens), max(pre_lens) if pre_longest is None else pre_longest)
+        cc.cc_attention_prefix(p, q, x, cache.view(cc), layer, i32(lens), longest, o, lse=lse)
+    torch.cuda.synchronize()
+    return o, lse
+
+
+CASES = [
+    # new, lens, hq, hkv, d, page
+    ([1], [1], 4, 2, 128, 0),
+    ([1], [17], 8, 1, 128, 0),
+    ([1, 1, 1, 1], [1, 64, 65, 333], 28, 4, 128, 16),
+    ([1, 1], [1500, 40], 32, 8, 128, 64),
+    ([1, 3, 0, 8], [100, 3, 9, 257], 16, 4, 64, 16),
+    ([5], [700], 20, 2, 128, 32),
+    ([7], [130], 12, 4, 64, 128),
+    ([20, 2], [20, 300], 8, 2, 128, 16),
+    ([64], [1000], 4, 4, 128, 64),
+    ([130, 33], [130, 500], 14, 2, 128, 16),
+    ([200], [321], 8, 8, 64, 0),
+    ([257], [257], 4, 2, 64, 32),
+    ([300, 1, 0, 77, 640], [300, 1, 5, 77, 640], 4, 1, 128, 16),   # whole prompts, packed
+    ([1000], [1000], 2, 1, 128, 0),
+    ([63, 64, 65, 127, 128, 129], [63, 64, 65, 127, 128, 129], 2, 2, 64, 64),
+    ([1], [50], 64, 1, 128, 16),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
+def test_attention(case):
+    from paper_2607_27600_amd import cc
+    new, lens, hq, hkv, d, page = case
+    print(f"[attn16] {case}", flush=True)
+    cache = Cache16(lens, hkv, d, layers=2, page=page, seed=21)
+    q = queries(new, hq, d, 22)
+    _same(*_run(cc, cache, q, new, lens, hq, hkv, layer=1), _oracle(cache, q, new, lens, hq, hkv, layer=1), str(case))
+
+
+PREFIXES = [
+    # prefix lens, first, new, lens, hq, hkv, d, page
+    ([1], [0, 1], [1], [1], 4, 2, 128, 0),
+    ([100], [0, 3], [1, 1, 1], [1, 5, 30], 8, 2, 128, 16),
+    ([333, 17], [0, 2, 5], [1, 4, 0, 2, 1], [70, 4, 3, 9, 1], 4, 1, 64, 16),
+    ([0, 65, 4], [0, 1, 1, 3], [2, 1, 3], [2, 0, 200], 4, 2, 128, 32),      # an empty prefix, one without sequences, no own entries
+    ([700], [0, 4], [40, 33, 1, 60], [40, 300, 1, 60], 14, 2, 128, 64),
+    ([150, 90], [0, 1, 2], [200, 130], [200, 130], 2, 2, 64, 0),
+    ([1300], [0, 20], [1] * 20, [i * 7 % 90 + 1 for i in range(20)], 28, 4, 128, 16),
+]
+
+
+@pytest.mark.parametrize("case", PREFIXES, ids=[str(i) for i in range(len(PREFIXES))])
+def test_shared_prefix(case):
+    from paper_2607_27600_amd import cc
+    pl, first, new, lens, hq, hkv, d, page = case
+    print(f"[prefix] {case}", flush=True)
+    cache = Cache16(lens, hkv, d, layers=2, page=page, seed=31)
+    pre = Cache16(pl, hkv, d, layers=2, page=16 if page else 0, seed=32)
+    q = queries(new, hq, d, 33)
+    kw = dict(layer=1, pre=pre, first=first, pre_lens=pl)
+    _same(*_run(cc, cache, q, new, lens, hq, hkv, **kw), _oracle(cache, q, new, lens, hq, hkv, **kw), str(case))
+
+
+def test_prefix_equals_one_cache():
+    """What a sequence sees behind a prefix is what it sees of one cache that holds both."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d, new, lens, n = 8, 2, 128, [3, 1], [50, 9], 100
+    one = Cache16([n + x for x in lens], hkv, d, page=16, seed=41)
+    pre, own = Cache16([n], hkv, d, page=16, seed=42), Cache16(lens, hkv, d, page=16, seed=43)
+    for b, m in enumerate(lens):
+        for w in "kv":
+            for t in range(n + m):
+                src = (pre, 0, t) if t < n else (own, b, t - n)
+                pg, sl = src[0]._where(src[1], np.asarray([src[2]]))
+                to, at = one._where(b, np.asarray([t]))
+                one.t[w][0, int(to[0]), :, int(at[0]), :d] = src[0].t[w][0, int(pg[0]), :, int(sl[0]), :d]
+    q = queries(new, hq, d, 44)
+    want = _oracle(one, q, new, [n + x for x in lens], hq, hkv)
+    _same(*_run(cc, own, q, new, lens, hq, hkv, pre=pre, first=[0, 2], pre_lens=[n]), want)
+    _same(*_run(cc, one, q, new, [n + x for x in lens], hq, hkv), want)
+
+
+@pytest.mark.parametrize("new,d", [([3, 5, 2], 128), ([100, 5, 70], 128), ([100, 90, 2], 64)])
+def test_rows_that_see_nothing(new, d):
+    """More queries than entries: those that stand before the first see nothing, or their prefix alone."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, lens = 4, 2, [2, 0, 1]
+    cache = Cache16(lens, hkv, d, page=16, seed=25)
+    q = queries(new, hq, d, 26)
+    o, lse = _run(cc, cache, q, new, lens, hq, hkv, longest=16)
+    want = _oracle(cache, q, new, lens, hq, hkv)
+    _same(o, lse, want)
+    empty = np.isneginf(want[1])
+    assert empty.any() and np.all(f64(o)[empty] == 0)
+    pre = Cache16([0, 40], hkv, d, page=16, seed=27)
+    kw = dict(pre=pre, first=[0, 1, 3], pre_lens=[0, 40])
+    _same(*_run(cc, cache, q, new, lens, hq, hkv, longest=16, **kw), _oracle(cache, q, new, lens, hq, hkv, **kw))
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("new,n", [([4], 100), ([40], 200), ([150], 150), ([33], 33)])
+@pytest.mark.parametrize("d", [128, 64])
+def test_what_is_not_finite_reaches_only_rows_that_see_it(new, n, d, value):
+    from paper_2607_27600_amd import cc
+    hq, hkv, m = 4, 2, new[0]
+    print(f"[attn16 nan] {new} {n} {d} {value}", flush=True)
+    cache = Cache16([n], hkv, d, page=16, seed=27)
+    # a value in one dim, and a NaN key, in entries that only some of the queries see; a value in the last entry
+    tv, tk = n - 2, n - 1 - m // 2
+    q = queries(new, hq, d, 28)
+    clean = _oracle(cache, q, new, [n], hq, hkv)
+    cache.put(0, 0, 0, "v", tv, 5, value)
+    cache.put(0, 0, 0, "v", n - 1, d - 1, -value)
+    cache.put(0, 0, 1, "k", tk, 9, float("nan"))
+    o, lse = _run(cc, cache, q, new, [n], hq, hkv)
+    o, lse = f64(o), f64(lse)
+    at = np.arange(m) + n - m
+    hit = np.zeros(o.shape, bool)
+    hit[np.ix_(at >= tv, [0, 1], [5])] = True
+    hit[np.ix_(at >= n - 1, [0, 1], [d - 1])] = True
+    if not np.isnan(value):
+        assert np.all(o[np.ix_(at >= tv, [0, 1], [5])] == value) and np.all(o[np.ix_(at >= n - 1, [0, 1], [d - 1])] == -value)
+    hit[np.ix_(at >= tk, [2, 3])] = True
+    np.testing.assert_array_equal(~np.isfinite(o), hit)
+    np.testing.assert_array_equal(np.isnan(lse), np.broadcast_to((at >= tk)[:, None] & (np.arange(hq) >= 2), lse.shape))
+    assert_attention_close(np.where(hit, 0, o), np.where(hit, 0, clean[0]))
+
+
+def test_lengths_on_the_device_in_a_graph():
+    """A captured call follows its lengths, the prefix's too; lengths beyond the plan are cut to it, negative ones empty."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d, new = 8, 2, 128, [1, 1, 40]
+    cache = Cache16([600, 300, 77], hkv, d, page=16, seed=32, room=600)
+    pre = Cache16([500], hkv, d, page=16, seed=33, room=16)
+    q = queries(new, hq, d, 34)
+    p = problem(cc, new, hq, hkv, d)
+    kv, lens, plens = cache.view(cc), i32([1, 1, 40]), i32([1])
+    x = cc.prefix(pre.view(cc), [0, 3], plens, 500)
+    need = max(cc.cc_attention_kv_workspace(p, 600), cc.cc_attention_prefix_workspace(p, x, 600))
+    ws = torch.empty(max(1, need), dtype=torch.uint8, device="cuda")
+    o, o2 = torch.empty_like(q), torch.empty_like(q)
+    lse, lse2 = torch.empty(42, hq, device="cuda"), torch.empty(42, hq, device="cuda")
+
+    def calls():
+        cc.cc_attention_kv(p, q, kv, 0, lens, 600, o, lse=lse, workspace=ws)
+        cc.cc_attention_prefix(p, q, x, kv, 0, lens, 600, o2, lse=lse2, workspace=ws)
+    calls()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls()
+    for now, pn in (([600, 300, 77], 500), ([1, 17, 40], 0), ([599, 0, 3], 10**6), ([10**6, -5, 77], -3)):
+        lens.copy_(i32(now))
+        plens.fill_(pn)
+        for t in (o, o2, lse, lse2):
+            t.fill_(3.0)
+        ws.fill_(0x7f)
+        g.replay()
+        torch.cuda.synchronize()
+        real, pr = [min(max(x, 0), 600) for x in now], [min(max(pn, 0), 500)]
+        _same(o, lse, _oracle(cache, q, new, real, hq, hkv), str(now))
+        _same(o2, lse2, _oracle(cache, q, new, real, hq, hkv, pre=pre, first=[0, 3], pre_lens=pr), f"{now} {pn}")
+
+
+def test_many_sequences():
+    """More sequences, and more prefixes, than any list by value holds."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d = 4, 2, 64
+    r = np.random.default_rng(34)
+    new = [int(x) for x in r.choice([0, 1, 1, 2, 40], 150)]
+    lens = [m + int(x) for m, x in zip(new, r.integers(0, 60, 150))]
+    cache = Cache16(lens, hkv, d, page=16, seed=35)
+    q = queries(new, hq, d, 36)
+    _same(*_run(cc, cache, q, new, lens, hq, hkv), _oracle(cache, q, new, lens, hq, hkv))
+    pl = [int(x) for x in r.integers(0, 50, 70)]
+    first = [0, *sorted(int(x) for x in r.integers(0, 151, 69)), 150]
+    pre = Cache16(pl, hkv, d, page=16, seed=37)
+    kw = dict(pre=pre, first=first, pre_lens=pl)
+    _same(*_run(cc, cache, q, new, lens, hq, hkv, **kw), _oracle(cache, q, new, lens, hq, hkv, **kw))
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.01, 1e-20, 1e-38])
+@pytest.mark.parametrize("new,lens,hq,hkv,d", [([1, 3], [200, 77], 8, 2, 128), ([70, 40], [300, 90], 4, 2, 64)])
+def test_a_scale_of_the_callers(new, lens, hq, hkv, d, scale):
+    from paper_2607_27600_amd import cc
+    cache = Cache16(lens, hkv, d, page=16, seed=101)
+    q = queries(new, hq, d, 102)
+    _same(*_run(cc, cache, q, new, lens, hq, hkv, softmax_scale=scale), _oracle(cache, q, new, lens, hq, hkv, scale=scale))
