@@ -12,6 +12,11 @@ struct KvPair {
   int32_t paged;
 };
 
+// Rows (queries times heads of a group) up to which a sequence counts as few.
+constexpr int KV_FEW_ROWS = 32;
+constexpr int KV_ROWS = 128;   // rows of a block of the kernel for many
+constexpr int KV_KEYS = 64;    // entries of its tiles
+
 // Attention of the queries of n_seqs sequences to the entries of a prefix (n_prefixes = 0: none) and to
 // their own entries up to their own.
 struct KvAttnArgs {
@@ -27,8 +32,17 @@ struct KvAttnArgs {
   int N;                       // queries in all
   float scale, c2;             // c2 = scale * log2(e)
   float room;                  // how far a logit may pass a row's reference maximum: 2^8 in probability
+  // Many rows.  Row blocks of the sequences of many rows: listed by value, longest first, or (items.n_seqs = 0)
+  // sequence b has those from cu[b] g / KV_ROWS + b on, more than its rows need.
+  AttnMany items;
+  int blocks;
+  int piece, splits;           // entries of a piece (a multiple of KV_KEYS), pieces of the longest sequence
+  // Results to be joined (null: none), outputs and (maximum, sum): [splits][Hkv][N g]
+  float* part;
+  float2* part_ml;
 };
-hipError_t launch_attention_kv(const KvAttnArgs& a, hipStream_t s);
+hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s);
+hipError_t launch_attn_kv_many(const KvAttnArgs& a, hipStream_t s);
 
 // What entries receive of the queries' attention, added to what they have.
 struct KvWeightsArgs {

@@ -244,7 +244,7 @@ __global__ __launch_bounds__(NT, 2) void attn_rows(KvAttnArgs a) {
   const int b = last_at(a.n_seqs, first_block, x);
   const int q0 = a.cu[b], mq = a.cu[b + 1] - q0, rows = mq * a.g;
   const int row0 = int(x - first_block(b)) * ROWS;
-  if (row0 >= rows) return;
+  if (row0 >= rows || (!a.n_prefixes && rows > KV_FEW_ROWS)) return;
   const int len = min(max(a.lens[b], 0), a.max_len), shift = len - mq;
   const int row = min(row0 + r16, rows - 1), i = row / a.g;
   R st;
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(NT, 2) void attn_rows(KvAttnArgs a) {
 
 }  // namespace
 
-hipError_t launch_attention_kv(const KvAttnArgs& a, hipStream_t s) {
+hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s) {
   const int64_t blocks = (int64_t(a.N) * a.g / 16 + a.n_seqs) * a.hkv;
   if (blocks > MOST_GROUPS) return hipErrorInvalidValue;
   if (a.head_dim == 128)

@@ -1288,6 +1288,51 @@ cc_status check_prefix(const cc_problem* p, const cc_prefix* x) {
   return CC_OK;
 }
 
+// How a call's sequences of many rows are cut.  Sizes only, so that the workspace query and the call agree.
+struct KvPlan {
+  bool few = false;            // there are sequences of few rows
+  AttnMany items;              // of many rows, up to ATTN_INLINE; else all are walked
+  int64_t blocks = 0;
+  int piece = KV_KEYS, splits = 1;
+  size_t part = 0, total = 0;  // workspace: (maximum, sum) pairs behind the outputs
+};
+
+cc_status kv_plan(const cc_problem* p, int max_len, KvPlan& c) {
+  const int g = p->n_heads_q / p->n_heads_kv;
+  int many = 0;
+  c.items.nkv = p->n_heads_kv;
+  for (int b = 0; b < p->n_seqs; ++b) {
+    const int seq0 = p->cu_seqlens_h[b], m = p->cu_seqlens_h[b + 1] - seq0;
+    const int64_t rows = int64_t(m) * g;
+    if (rows == 0) continue;
+    if (rows <= KV_FEW_ROWS) {
+      c.few = true;
+      continue;
+    }
+    const int nb = int((rows + KV_ROWS - 1) / KV_ROWS);
+    if (many < ATTN_INLINE) c.items.seqs[many] = AttnSeq{b, seq0, m, nb};
+    ++many;
+    c.blocks += nb;
+  }
+  c.items.n_seqs = many <= ATTN_INLINE ? many : 0;
+  std::stable_sort(c.items.seqs, c.items.seqs + c.items.n_seqs, [](const AttnSeq& x, const AttnSeq& y) { return x.blocks > y.blocks; });
+  if (many == 0) return CC_OK;
+  const int64_t items = c.blocks * p->n_heads_kv;
+  if (!c.items.n_seqs) c.blocks = int64_t(n_tokens(p)) * g / KV_ROWS + p->n_seqs;
+  if (c.blocks * p->n_heads_kv > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+  // As many pieces as leave no more than two workgroups a CU, what is resident, of 256 entries at the least.
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>({2 * kCus / items, (int64_t(max_len) + 255) / 256,
+                                                               MOST_GROUPS / (c.blocks * p->n_heads_kv)}));
+  c.piece = std::max(KV_KEYS, int(((int64_t(max_len) + want - 1) / want + KV_KEYS - 1) / KV_KEYS * KV_KEYS));
+  c.splits = std::max(1, int((int64_t(max_len) + c.piece - 1) / c.piece));
+  if (c.splits > 1) {
+    const size_t rows = size_t(c.splits) * p->n_heads_q * n_tokens(p);
+    c.part = align_up(rows * p->head_dim * sizeof(float));
+    c.total = c.part + align_up(rows * sizeof(float2));
+  }
+  return CC_OK;
+}
+
 KvPair make_pair(const cc_kv* kv) { return KvPair{make_view(kv, kv->k, 2), kv->v, kv->layout == CC_KV_PAGED}; }
 
 // Both attentions.
@@ -1299,7 +1344,9 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
   const int N = n_tokens(p);
   if (N > 0 && (!q || !o || !kv_lens || !aligned16(q) || !aligned16(o))) return CC_ERR_ARG;
   if (N > 0 && prefix && (!prefix->first_seq_d || !prefix->lens)) return CC_ERR_ARG;
-  CC_TRY(check_ws(ws, ws_bytes, 0));
+  KvPlan c;
+  if (!prefix) CC_TRY(kv_plan(p, max_kv_len, c));
+  CC_TRY(check_ws(ws, ws_bytes, c.total));
   if (N == 0) return CC_OK;
   KvAttnArgs a{};
   a.q = static_cast<const u16*>(q);
@@ -1326,7 +1373,14 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
   a.scale = softmax_scale(p);
   a.c2 = a.scale * kLog2e;
   a.room = std::min(8.f / a.c2, FLT_MAX);   // (finite: a first logit passes -inf by more)
-  CC_HIP(launch_attention_kv(a, static_cast<hipStream_t>(stream)));
+  a.items = c.items;
+  a.blocks = int(c.blocks);
+  a.piece = c.piece;
+  a.splits = c.splits;
+  a.part = c.total ? reinterpret_cast<float*>(ws) : nullptr;
+  a.part_ml = c.total ? reinterpret_cast<float2*>(at(ws, c.part)) : nullptr;
+  if (prefix || c.few) CC_HIP(launch_attn_rows(a, static_cast<hipStream_t>(stream)));
+  if (c.blocks) CC_HIP(launch_attn_kv_many(a, static_cast<hipStream_t>(stream)));
   return CC_OK;
 }
 
@@ -1345,7 +1399,9 @@ extern "C" {
 cc_status cc_attention_kv_workspace(const cc_problem* p, int32_t max_kv_len, size_t* bytes) {
   if (!bytes) return CC_ERR_ARG;
   CC_TRY(check_attention_kv(p, max_kv_len));
-  *bytes = 0;
+  KvPlan c;
+  CC_TRY(kv_plan(p, max_kv_len, c));
+  *bytes = c.total;
   return CC_OK;
 }
 

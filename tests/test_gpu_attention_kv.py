@@ -238,3 +238,30 @@ def test_a_scale_of_the_callers(new, lens, hq, hkv, d, scale):
     cache = Cache16(lens, hkv, d, page=16, seed=101)
     q = queries(new, hq, d, 102)
     _same(*_run(cc, cache, q, new, lens, hq, hkv, softmax_scale=scale), _oracle(cache, q, new, lens, hq, hkv, scale=scale))
+
+
+@pytest.mark.parametrize("new,lens,hq,hkv,d,page", [([1], [9000], 4, 1, 128, 16), ([1, 1], [5001, 37], 4, 2, 64, 64),
+                                                    ([70], [4100], 2, 1, 128, 16), ([300, 1], [3000, 2500], 2, 2, 64, 0),
+                                                    ([40, 200, 0, 90], [40, 2000, 7, 90], 4, 1, 128, 32),
+                                                    ([700], [700], 2, 1, 128, 128), ([33] * 20, [33 + 90 * i for i in range(20)], 2, 1, 64, 16)])
+def test_pieces(new, lens, hq, hkv, d, page):
+    """Long caches of few heads are cut into pieces and joined; the plan may reach beyond the longest.  The workspace holds
+    no more than asked for, and the same call repeats bit for bit."""
+    from paper_2607_27600_amd import cc
+    print(f"[attn16 pieces] {new} {lens} {hq} {hkv} {d} {page}", flush=True)
+    cache = Cache16(lens, hkv, d, page=page, seed=23, room=5000)
+    q = queries(new, hq, d, 24)
+    want = _oracle(cache, q, new, lens, hq, hkv)
+    p, kv = problem(cc, new, hq, hkv, d), cache.view(cc)
+    for longest in (max(lens), max(lens) + 4321):
+        size = cc.cc_attention_kv_workspace(p, longest)
+        ws = torch.full((size + 4096,), 0x7f, dtype=torch.uint8, device="cuda")
+        got = []
+        for _ in range(2):
+            o, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+            cc.cc_attention_kv(p, q, kv, 0, i32(lens), longest, o, lse=lse, workspace=ws[:size])
+            torch.cuda.synchronize()
+            _same(o, lse, want, str(longest))
+            got.append((o, lse))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        assert (ws[size:] == 0x7f).all()
