@@ -1,7 +1,7 @@
 // What the kernels of the attention over a bf16 cache share with each other and with the planner.
 #pragma once
 
-#include "cc_internal.h"
+#include "attention_shares.h"
 
 namespace cc {
 
@@ -12,13 +12,11 @@ struct KvPair {
   int32_t paged;
 };
 
-// Rows (queries times heads of a group) up to which a sequence counts as few.
-constexpr int KV_FEW_ROWS = 32;
 constexpr int KV_ROWS = 128;   // rows of a block of the kernel for many
 constexpr int KV_KEYS = 64;    // entries of its tiles
+constexpr int KV_LIST = 64;    // sequences of few rows of a launch listed by value
 
-// Attention of the queries of n_seqs sequences to the entries of a prefix (n_prefixes = 0: none) and to
-// their own entries up to their own.
+// Attention of the queries of n_seqs sequences to the entries of a prefix and to their own entries up to their own.
 struct KvAttnArgs {
   const u16* q;
   u16* o;
@@ -26,12 +24,18 @@ struct KvAttnArgs {
   KvPair own, pre;
   const int32_t *cu, *lens;    // queries and own entries of the sequences
   const int32_t *pre_first, *pre_lens;   // sequences [pre_first[i], pre_first[i + 1]) are behind prefix i
-  int n_seqs, n_prefixes;
+  int n_seqs, n_prefixes;      // (0: no prefixes)
   int layer, max_len, pre_max;
   int hq, hkv, g, head_dim;
   int N;                       // queries in all
   float scale, c2;             // c2 = scale * log2(e)
   float room;                  // how far a logit may pass a row's reference maximum: 2^8 in probability
+  // Few rows: sequences list[0 .. n_list), or (listed = 0) all, those of more than `most` rows left out.
+  int n_list, listed, R, most; // R: most rows of one
+  int direct, parts;           // workgroups that share out the work (attention_shares.h; direct = 0)
+  int32_t list[KV_LIST];
+  float* fpart;                // [parts + n_list * Hkv][R] outputs and (maximum, sum) to be joined
+  float2* fpart_ml;
   // Many rows.  Row blocks of the sequences of many rows: listed by value, longest first, or (items.n_seqs = 0)
   // sequence b has those from cu[b] g / KV_ROWS + b on, more than its rows need.
   AttnMany items;
@@ -40,8 +44,16 @@ struct KvAttnArgs {
   // Results to be joined (null: none), outputs and (maximum, sum): [splits][Hkv][N g]
   float* part;
   float2* part_ml;
+  // What a pass over the prefixes has left (null: none), laid out like part, pieces of ppiece entries.  In that pass
+  // the prefixes stand for sequences (own, lens and n_seqs are theirs) and `shared` is set.
+  const float* ppart;
+  const float2* ppart_ml;
+  int ppiece, shared;
 };
+// 16 rows a workgroup, whole; with n_prefixes and no ppart the prefix's entries too.
 hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s);
+// Few rows, work shared out.
+hipError_t launch_attn_few(const KvAttnArgs& a, hipStream_t s);
 hipError_t launch_attn_kv_many(const KvAttnArgs& a, hipStream_t s);
 
 // What entries receive of the queries' attention, added to what they have.
@@ -79,14 +91,6 @@ hipError_t launch_compact_weights(const CompactWeightsArgs& a, hipStream_t s);
 
 // ---- shared by the attention kernels
 
-// A wave-uniform pointer in scalar registers.
-__device__ __forceinline__ const char* uniform_ptr(const char* p) {
-  const uint64_t u = reinterpret_cast<uint64_t>(p);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(u));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(u >> 32));
-  return reinterpret_cast<const char*>((uint64_t(hi) << 32) | lo);
-}
-
 // Bits 15 and 31 where the low and the high bf16 of a word are NaN or infinite.
 __device__ __forceinline__ uint32_t wide_halves(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 // 0xffff at bits 15 and 31.
@@ -94,8 +98,10 @@ __device__ __forceinline__ uint32_t whole_halves(uint32_t m) { return (m >> 15) 
 
 // The log-sum-exp of a row from its reference logit and its sum of 2^((z - ref) c2).
 __device__ __forceinline__ float row_lse(float ref, float sum, float scale) {
-  return sum == 0.f ? -INFINITY : fmaf(ref, scale, __logf(sum));
+  return __float_as_uint(sum) == 0u ? -INFINITY : fmaf(ref, scale, __logf(sum));
 }
+// Its outputs' factor: an empty row has sum 0 and outputs 0, a NaN sum stays NaN.
+__device__ __forceinline__ float row_inverse(float sum) { return __float_as_uint(sum) == 0u ? 0.f : 1.f / sum; }
 
 // The last b with start(b) <= x among 0 .. n - 1, start rising from start(0) <= x.
 template <class F>
@@ -134,6 +140,45 @@ __device__ __forceinline__ KvPlane kv_plane(const KvPair& p, int b, int layer, i
   x.page_mask = p.at.page_mask;
   x.page_stride = p.at.page_stride;
   return x;
+}
+
+// What the pass over the prefixes has of a row, V outputs from d on, folded into (M, L, o): its pieces in their order, as
+// many at a time as fit V * AT registers.
+template <int HD, int V, int AT>
+__device__ __forceinline__ void fold_prefix(const KvAttnArgs& a, int b, int kvh, int64_t query_row, const int (&d)[V / 4], float& M,
+                                            float& L, float4 (&o)[V / 4]) {
+  const int j = last_at(a.n_prefixes, [&](int i) { return int64_t(a.pre_first[i]); }, b);
+  const int n = max(1, (min(max(a.pre_lens[j], 0), a.pre_max) + a.ppiece - 1) / a.ppiece);
+  const int64_t all = int64_t(a.N) * a.g, row = int64_t(kvh) * all + query_row;
+  for (int i0 = 0; i0 < n; i0 += AT) {
+    float2 p[AT];
+    float4 y[AT][V / 4];
+#pragma unroll
+    for (int q = 0; q < AT; ++q) {
+      const int64_t at = row + min(i0 + q, n - 1) * all * a.hkv;
+      p[q] = a.ppart_ml[at];
+#pragma unroll
+      for (int v = 0; v < V / 4; ++v) y[q][v] = *reinterpret_cast<const float4*>(a.ppart + at * HD + d[v]);
+    }
+    float t = M;
+#pragma unroll
+    for (int q = 0; q < AT; ++q)
+      if (i0 + q < n) t = fmaxf(t, p[q].x);
+    const float ref = t == -INFINITY ? 0.f : t, c = fast_exp2((M - ref) * a.c2);
+    M = t;
+    L *= c;
+#pragma unroll
+    for (int v = 0; v < V / 4; ++v) o[v] = make_float4(o[v].x * c, o[v].y * c, o[v].z * c, o[v].w * c);
+#pragma unroll
+    for (int q = 0; q < AT; ++q) {
+      if (i0 + q >= n) continue;
+      const float f = fast_exp2((p[q].x - ref) * a.c2);
+      L += p[q].y * f;
+#pragma unroll
+      for (int v = 0; v < V / 4; ++v)
+        o[v] = make_float4(o[v].x + y[q][v].x * f, o[v].y + y[q][v].y * f, o[v].z + y[q][v].z * f, o[v].w + y[q][v].w * f);
+    }
+  }
 }
 
 }  // namespace cc

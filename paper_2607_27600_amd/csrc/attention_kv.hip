@@ -19,30 +19,12 @@
 // value meets a probability of 0, and 0 times NaN or infinity would reach the output: values past the
 // sequence are zeroed as they are read, and in steps that some row sees in part, NaN and infinite elements are
 // zeroed too and added by the rows that see them.
+#include <algorithm>
+
 #include "attention_kv.h"
 
 namespace cc {
 namespace {
-
-constexpr int NT = 256, NW = NT / 64;
-
-__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-
-// Maximum and sum over the four lanes l % 16 + 16 k.
-__device__ __forceinline__ float quad_max(float x) {
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float quad_sum(float x) {
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 
 // NR blocks of 16 rows, in a wave: queries, running maximum and sum, outputs.
 template <int HD, int NR>
@@ -226,60 +208,28 @@ struct Rows {
   }
 };
 
-// One workgroup for 16 rows of a (sequence, KV head): its waves share out the entries, the prefix's and the
-// sequence's, and their results meet in LDS.
-template <int HD>
-__global__ __launch_bounds__(NT, 2) void attn_rows(KvAttnArgs a) {
-  constexpr int ROWS = 16, LPR = HD / 8;
-  using R = Rows<HD, 1>;
-  constexpr int NDB = R::NDB;
-  __shared__ float lds[NW * ROWS * HD];
-  __shared__ float2 ml[NW * ROWS];
+// The waves' results of rows [row0, rows) of a (sequence, KV head) meet in LDS, [NW][ROWS][HD] outputs and [NW][ROWS] (max, sum);
+// done(r, d, M, L, o) gets the eight outputs of row row0 + r from d on.
+template <int HD, int NR, int NW, class F>
+__device__ __forceinline__ void meet(const KvAttnArgs& a, const Rows<HD, NR>& st, float* lds, float2* ml, int rows, F done) {
+  constexpr int ROWS = 16 * NR, LPR = HD / 8, NDB = HD / 16;
   const int tid = threadIdx.x, lane = tid & 63, grp = lane >> 4, r16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kvh = int(blockIdx.x % unsigned(a.hkv));
-  const int64_t x = blockIdx.x / unsigned(a.hkv);
-  // sequence b has the blocks from cu[b] g / 16 + b on, more than its rows need
-  auto first_block = [&](int b) { return int64_t(a.cu[b]) * a.g / ROWS + b; };
-  const int b = last_at(a.n_seqs, first_block, x);
-  const int q0 = a.cu[b], mq = a.cu[b + 1] - q0, rows = mq * a.g;
-  const int row0 = int(x - first_block(b)) * ROWS;
-  if (row0 >= rows || (!a.n_prefixes && rows > KV_FEW_ROWS)) return;
-  const int len = min(max(a.lens[b], 0), a.max_len), shift = len - mq;
-  const int row = min(row0 + r16, rows - 1), i = row / a.g;
-  R st;
-  {
-    const u16* q = a.q + (int64_t(q0 + i) * a.hq + kvh * a.g + row % a.g) * HD + 8 * grp;
 #pragma unroll
-    for (int k = 0; k < R::NKS; ++k) st.qf[0][k] = as_bf16x8(*reinterpret_cast<const uint4*>(q + 32 * k));
+  for (int n = 0; n < NR; ++n) {
+    const float l = quad_sum(st.l[n]);
+    const int row = wave * ROWS + n * 16 + r16;
+    if (grp == 0) ml[row] = make_float2(st.m[n], l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float* o = lds + row * HD + NDB * (4 * grp + e);
+#pragma unroll
+      for (int d = 0; d < NDB; d += 4)
+        *reinterpret_cast<float4*>(o + d) = make_float4(st.acc[n][d][e], st.acc[n][d + 1][e], st.acc[n][d + 2][e], st.acc[n][d + 3][e]);
+    }
   }
-  st.clear();
-  auto part = [&](int groups, int& gb, int& ge) {   // this wave's, in whole steps of two
-    const int per = ((groups + NW - 1) / NW + 1) & ~1;
-    gb = wave * per;
-    ge = min(groups, gb + per);
-  };
-  int gb, ge;
-  if (a.n_prefixes) {
-    const int j = last_at(a.n_prefixes, [&](int i) { return int64_t(a.pre_first[i]); }, b);
-    const int n = min(max(a.pre_lens[j], 0), a.pre_max);
-    const int past[1] = {n};
-    part((n + 15) >> 4, gb, ge);
-    st.run(a, kv_plane(a.pre, j, a.layer, kvh), gb, ge, n, past, n);
-  }
-  const int past[1] = {max(0, shift + i + 1)};
-  const int most = max(0, shift + (min(row0 + ROWS, rows) - 1) / a.g + 1);   // what the last row sees
-  part((most + 15) >> 4, gb, ge);
-  st.run(a, kv_plane(a.own, b, a.layer, kvh), gb, ge, len, past, max(0, shift + row0 / a.g + 1));
-
-  const float l = quad_sum(st.l[0]);
-  if (grp == 0) ml[wave * ROWS + r16] = make_float2(st.m[0], l);
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-#pragma unroll
-    for (int d = 0; d < NDB; ++d) lds[(wave * ROWS + r16) * HD + NDB * (4 * grp + e) + d] = st.acc[0][d][e];
   __syncthreads();
-  for (int r = tid / LPR; r < min(ROWS, rows - row0); r += NT / LPR) {
+  for (int r = tid / LPR; r < rows; r += NW * 64 / LPR) {
     const int d = (tid % LPR) * 8;
     float M = -INFINITY;
 #pragma unroll
@@ -291,27 +241,263 @@ __global__ __launch_bounds__(NT, 2) void attn_rows(KvAttnArgs a) {
       const float2 p = ml[w * ROWS + r];
       const float f = fast_exp2((p.x - ref) * a.c2);
       L += p.y * f;
+      const float* src = lds + (w * ROWS + r) * HD + d;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] += lds[(w * ROWS + r) * HD + d + e] * f;
+      for (int e = 0; e < 8; ++e) o[e] += src[e] * f;
     }
-    // an empty row has L = 0 and outputs 0; a NaN sum stays NaN
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    const int64_t out = int64_t(q0 + (row0 + r) / a.g) * a.hq + kvh * a.g + (row0 + r) % a.g;
-    *reinterpret_cast<uint4*>(a.o + out * HD + d) = make_uint4(pack_bf2(o[0] * inv, o[1] * inv), pack_bf2(o[2] * inv, o[3] * inv),
-                                                               pack_bf2(o[4] * inv, o[5] * inv), pack_bf2(o[6] * inv, o[7] * inv));
-    if (a.lse && d == 0) a.lse[out] = row_lse(ref, L, a.scale);
+    float4 x[2] = {make_float4(o[0], o[1], o[2], o[3]), make_float4(o[4], o[5], o[6], o[7])};
+    done(r, d, M, L, x);
   }
+}
+
+// The final result of row r of sequence b, eight outputs from d on.
+template <int HD>
+__device__ __forceinline__ void finish(const KvAttnArgs& a, int b, int q0, int kvh, int r, int d, float M, float L, float4 (&o)[2]) {
+  if (a.ppart) {
+    const int ds[2] = {d, d + 4};
+    fold_prefix<HD, 8, 8>(a, b, kvh, int64_t(q0) * a.g + r, ds, M, L, o);
+  }
+  const float inv = row_inverse(L);
+  const int64_t out = int64_t(q0 + r / a.g) * a.hq + kvh * a.g + r % a.g;
+  *reinterpret_cast<uint4*>(a.o + out * HD + d) =
+      make_uint4(pack_bf2(o[0].x * inv, o[0].y * inv), pack_bf2(o[0].z * inv, o[0].w * inv), pack_bf2(o[1].x * inv, o[1].y * inv),
+                 pack_bf2(o[1].z * inv, o[1].w * inv));
+  if (a.lse && d == 0) a.lse[out] = row_lse(M, L, a.scale);
+}
+
+// Rows' queries; row block n has rows row0 + 16 n ...
+template <int HD, int NR>
+__device__ __forceinline__ void load_queries(const KvAttnArgs& a, Rows<HD, NR>& st, int q0, int kvh, int row0, int rows, int (&i)[NR]) {
+  const int lane = threadIdx.x & 63, grp = lane >> 4, r16 = lane & 15;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int row = min(row0 + 16 * n + r16, rows - 1);
+    i[n] = row / a.g;
+    const u16* q = a.q + (int64_t(q0 + i[n]) * a.hq + kvh * a.g + row % a.g) * HD + 8 * grp;
+#pragma unroll
+    for (int k = 0; k < HD / 32; ++k) st.qf[n][k] = as_bf16x8(*reinterpret_cast<const uint4*>(q + 32 * k));
+  }
+}
+
+// ------------------------------------------------------------------ whole rows
+
+// One workgroup for 16 rows of a (sequence, KV head): its waves share out the entries, the prefix's and the sequence's.
+// Eight waves, so that a wave's chain of loads is short.
+constexpr int ROWS_NT = 512;
+template <int HD>
+__global__ __launch_bounds__(ROWS_NT, 2) void attn_rows(KvAttnArgs a) {
+  constexpr int ROWS = 16, NW = ROWS_NT / 64;
+  __shared__ float lds[NW * ROWS * HD];
+  __shared__ float2 ml[NW * ROWS];
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int kvh = int(blockIdx.x % unsigned(a.hkv));
+  const int64_t x = blockIdx.x / unsigned(a.hkv);
+  int b, row0;
+  if (a.listed) {
+    const int each = (a.R + ROWS - 1) / ROWS;
+    b = a.list[int(x) / each];
+    row0 = int(x) % each * ROWS;
+  } else {
+    // sequence b has the blocks from cu[b] g / 16 + b on, more than its rows need
+    auto first_block = [&](int b) { return int64_t(a.cu[b]) * a.g / ROWS + b; };
+    b = last_at(a.n_seqs, first_block, x);
+    row0 = int(x - first_block(b)) * ROWS;
+  }
+  const int q0 = a.cu[b], mq = a.cu[b + 1] - q0, rows = mq * a.g;
+  if (row0 >= rows || rows > a.most) return;
+  const int len = min(max(a.lens[b], 0), a.max_len), shift = len - mq;
+  Rows<HD, 1> st;
+  int i[1];
+  load_queries(a, st, q0, kvh, row0, rows, i);
+  st.clear();
+  auto part = [&](int groups, int& gb, int& ge) {   // this wave's, in whole steps of two
+    const int per = ((groups + NW - 1) / NW + 1) & ~1;
+    gb = wave * per;
+    ge = min(groups, gb + per);
+  };
+  int gb, ge;
+  if (a.n_prefixes && !a.ppart) {
+    const int j = last_at(a.n_prefixes, [&](int i) { return int64_t(a.pre_first[i]); }, b);
+    const int n = min(max(a.pre_lens[j], 0), a.pre_max);
+    const int past[1] = {n};
+    part((n + 15) >> 4, gb, ge);
+    st.run(a, kv_plane(a.pre, j, a.layer, kvh), gb, ge, n, past, n);
+  }
+  const int past[1] = {max(0, shift + i[0] + 1)};
+  const int most = max(0, shift + (min(row0 + ROWS, rows) - 1) / a.g + 1);   // what the last row sees
+  part((most + 15) >> 4, gb, ge);
+  st.run(a, kv_plane(a.own, b, a.layer, kvh), gb, ge, len, past, max(0, shift + row0 / a.g + 1));
+  meet<HD, 1, NW>(a, st, lds, ml, min(ROWS, rows - row0),
+                  [&](int r, int d, float M, float L, float4(&o)[2]) { finish<HD>(a, b, q0, kvh, row0 + r, d, M, L, o); });
+}
+
+// ------------------------------------------------------------------ few rows, work shared out
+
+constexpr int FEW_NT = 256;
+template <int HD, int NR>
+__global__ __launch_bounds__(FEW_NT, 2) void attn_few(KvAttnArgs a) {
+  constexpr int NW = FEW_NT / 64, ROWS = 16 * NR;
+  extern __shared__ float lds[];        // [NW][ROWS][HD] outputs, then [NW][ROWS] (max, sum)
+  float2* ml = reinterpret_cast<float2*>(lds + NW * ROWS * HD);
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const Shares sh = shares_of(a);
+  if (int(blockIdx.x) >= sh.parts) return;
+  int64_t x = sh.begin(blockIdx.x);
+  const int64_t x1 = sh.begin(blockIdx.x + 1);
+  while (x < x1) {
+    const Item it = item_at(a, sh, x);
+    const int j = it.j, kvh = it.kvh;
+    const Seq s = seq_of(a, j);
+    const int rows = s.m * a.g;
+    const int past_unit = it.unit + int(min(int64_t(it.units - it.unit), x1 - x));   // of the item's units
+    x += past_unit - it.unit;
+    const int u0 = max(0, it.unit - sh.head), u1 = past_unit - sh.head;   // those with entries
+    const bool whole = u0 == 0 && past_unit == it.units;
+    if (u1 <= u0) continue;
+    const int unit = sh.q * UNIT;
+    const int c0 = u0 * unit, c1 = int(min(int64_t(s.len), int64_t(u1) * unit));
+    Rows<HD, NR> st;
+    int i[NR], past[NR];
+    load_queries(a, st, s.q0, kvh, 0, rows, i);
+    st.clear();
+#pragma unroll
+    for (int n = 0; n < NR; ++n) past[n] = max(0, s.shift + i[n] + 1);
+    // this wave's 16-entry groups: the piece's, in NW runs of whole steps of two
+    const int g0 = c0 >> 4, g1 = (c1 + 15) >> 4;
+    const int per = ((g1 - g0 + NW - 1) / NW + 1) & ~1;
+    const int gb = g0 + wave * per, ge = min(g1, gb + per);
+    st.run(a, kv_plane(a.own, s.b, a.layer, kvh), gb, ge, s.len, past, max(0, s.shift + 1));
+    meet<HD, NR, NW>(a, st, lds, ml, rows, [&](int r, int d, float M, float L, float4(&o)[2]) {
+      if (whole) return finish<HD>(a, s.b, s.q0, kvh, r, d, M, L, o);
+      const int64_t row = (int64_t(blockIdx.x) + int64_t(j) * a.hkv + kvh) * a.R + r;
+      float* po = a.fpart + row * HD + d;
+      *reinterpret_cast<float4*>(po) = o[0];
+      *reinterpret_cast<float4*>(po + 4) = o[1];
+      if (d == 0) a.fpart_ml[row] = make_float2(M, L);
+    });
+    __syncthreads();   // the LDS results have been read
+  }
+}
+
+// Joins the pieces of rows that are cut between shares.  A workgroup has NG groups of HD / 8 lanes.  With `one`, for up
+// to JOIN_ONE rows in all, they share out one row's pieces; else a row each.
+constexpr int JOIN_ONE = 1024;
+template <int HD>
+__global__ __launch_bounds__(256) void attn_few_join(KvAttnArgs a, int one, int64_t group0) {
+  constexpr int LPR = HD / 8, NG = 256 / LPR;
+  __shared__ float4 po[2][256];
+  __shared__ float2 pm[256];
+  const int tid = threadIdx.x, gi = tid / LPR, lane = tid % LPR, d = lane * 8;
+  const int64_t all = int64_t(a.n_list) * a.hkv * a.R;
+  const int64_t row_in = one ? int64_t(blockIdx.x) : (group0 + blockIdx.x) * NG + gi;
+  const int r = int(row_in % a.R), jh = int(min(row_in / a.R, int64_t(a.n_list) * a.hkv - 1));
+  const int kvh = jh % a.hkv, j = jh / a.hkv;
+  const Seq s = seq_of(a, j);
+  const int rows = s.m * a.g;
+  bool on = row_in < all && r < rows && rows <= FEW_ROWS;
+  // the rows of a wave lie in one (sequence, head), or the search runs for each in turn
+  const Shares sh = shares_of(a);
+  int64_t start = 0;
+  int units = 0;
+  for (uint64_t left = __ballot(true); left;) {
+    const int jn = __builtin_amdgcn_readlane(j, __builtin_ctzll(left));
+    int64_t st;
+    int un;
+    item_of(a, sh, jn, st, un);
+    if (j == jn) {
+      start = st;
+      units = un;
+    }
+    left &= ~__ballot(j == jn);
+  }
+  const int64_t x = start + int64_t(kvh) * units;
+  const int wa = sh.part_of(x + sh.head), wb = sh.part_of(x + max(units, 1) - 1);
+  const int n = wb - wa + 1;
+  on = on && n > 1;   // a whole one is final
+  const int64_t slot = (int64_t(wa) + jh) * a.R + r;   // piece i at slot + i R
+  Joined g[2] = {{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)}, {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)}};
+  if (on) {
+    const int first = one ? gi : 0, by = one ? NG : 1;
+    for (int i0 = first; i0 < n; i0 += 4 * by) {   // four in flight
+      float2 p[4];
+      float4 y[2][4];
+      bool in[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t at = slot + int64_t(min(i0 + q * by, n - 1)) * a.R;
+        in[q] = i0 + q * by < n;
+        p[q] = a.fpart_ml[at];
+        y[0][q] = *reinterpret_cast<const float4*>(a.fpart + at * HD + d);
+        y[1][q] = *reinterpret_cast<const float4*>(a.fpart + at * HD + d + 4);
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) g[k].add(p, [&](int q) { return y[k][q]; }, in, a.c2);
+    }
+  }
+  if (one) {   // (alike in the whole workgroup)
+    if (!on) return;
+    po[0][tid] = g[0].o;
+    po[1][tid] = g[1].o;
+    pm[tid] = make_float2(g[0].M, g[0].L);
+    __syncthreads();
+    if (gi) return;
+    float2 p[NG];
+    bool in[NG];
+#pragma unroll
+    for (int q = 0; q < NG; ++q) {
+      p[q] = pm[lane + q * LPR];
+      in[q] = true;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      g[k] = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+      g[k].add(p, [&](int q) { return po[k][lane + q * LPR]; }, in, a.c2);
+    }
+  }
+  if (!on) return;
+  float4 o[2] = {g[0].o, g[1].o};
+  finish<HD>(a, s.b, s.q0, kvh, r, d, g[0].M, g[0].L, o);
+}
+
+template <int HD, int NR>
+hipError_t few_rows(const KvAttnArgs& a, hipStream_t s) {
+  constexpr int NW = FEW_NT / 64;
+  constexpr size_t lds = size_t(NW) * 16 * NR * (HD * 4 + 8);
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_few<HD, NR>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((attn_few<HD, NR>), dim3(unsigned(a.parts)), dim3(FEW_NT), lds, s, a);
+  return hipGetLastError();
+}
+
+template <int HD>
+hipError_t few_dim(const KvAttnArgs& a, hipStream_t s) {
+  hipError_t e = a.R <= 16 ? few_rows<HD, 1>(a, s) : few_rows<HD, 2>(a, s);
+  if (e != hipSuccess) return e;
+  constexpr int NG = 256 / (HD / 8);
+  const int64_t rows = int64_t(a.n_list) * a.hkv * a.R;
+  const int one = rows <= JOIN_ONE;
+  const int64_t groups = one ? rows : (rows + NG - 1) / NG;
+  for (int64_t g0 = 0; g0 < groups; g0 += MOST_GROUPS) {   // (more than a launch may have: several)
+    hipLaunchKernelGGL((attn_few_join<HD>), dim3(unsigned(std::min(MOST_GROUPS, groups - g0))), dim3(256), 0, s, a, one, g0);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
 
+hipError_t launch_attn_few(const KvAttnArgs& a, hipStream_t s) { return a.head_dim == 128 ? few_dim<128>(a, s) : few_dim<64>(a, s); }
+
 hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s) {
-  const int64_t blocks = (int64_t(a.N) * a.g / 16 + a.n_seqs) * a.hkv;
-  if (blocks > MOST_GROUPS) return hipErrorInvalidValue;
+  const int64_t blocks = (a.listed ? int64_t(a.n_list) * ((a.R + 15) / 16) : int64_t(a.N) * a.g / 16 + a.n_seqs) * a.hkv;
+  if (blocks > MOST_GROUPS / 2) return hipErrorInvalidValue;   // (refused by the planner)
   if (a.head_dim == 128)
-    hipLaunchKernelGGL(attn_rows<128>, dim3(unsigned(blocks)), dim3(NT), 0, s, a);
+    hipLaunchKernelGGL(attn_rows<128>, dim3(unsigned(blocks)), dim3(ROWS_NT), 0, s, a);
   else
-    hipLaunchKernelGGL(attn_rows<64>, dim3(unsigned(blocks)), dim3(NT), 0, s, a);
+    hipLaunchKernelGGL(attn_rows<64>, dim3(unsigned(blocks)), dim3(ROWS_NT), 0, s, a);
   return hipGetLastError();
 }
 

@@ -1,14 +1,10 @@
 // What the kernels of the attention over a cache in 8 bits share with each other and with the planner.
 #pragma once
 
-#include "cc_internal.h"
+#include "attention_shares.h"
 
 namespace cc {
 
-// Rows (queries times heads of a group) up to which a sequence counts as few: up to two row blocks of 16.  Two
-// blocks against the kernel for many, 32 rows, 8000 entries, 8 KV heads of 128: 23.2 us and 24.7, sixteen such
-// sequences 83 and 116; four blocks, 64 rows: 41.5 and (68 rows) 31.6, sixteen 328 and 122.
-constexpr int FEW_ROWS = 32;
 // Few rows: the longest cache of which each (sequence, head) is one workgroup's, with nothing to join.  A
 // CU's own loads, some 40 GB/s, are the bound there, so it grows with the workgroups there are, up to where a
 // batch of one long sequence among short ones would wait for it.  One token each, heads of 128, that

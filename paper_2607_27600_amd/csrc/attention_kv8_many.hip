@@ -68,14 +68,6 @@ __device__ __forceinline__ void dma16(const char* sbase, uint32_t voff, uint32_t
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(p)));
 }
-// A wave-uniform pointer in scalar registers.
-__device__ __forceinline__ const char* uniform_ptr(const char* p) {
-  const uint64_t u = reinterpret_cast<uint64_t>(p);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(u));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(u >> 32));
-  return reinterpret_cast<const char*>((uint64_t(hi) << 32) | lo);
-}
-
 // Sixteen codes times the scale, in bf16.
 __device__ __forceinline__ void widen16(const uint4& w, float scale, uint4& lo, uint4& hi) {
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};

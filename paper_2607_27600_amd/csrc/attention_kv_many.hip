@@ -102,24 +102,25 @@ __global__ __launch_bounds__(256, 2) void attn_many(KvAttnArgs a) {
   } else {
     kvh = int(x % unsigned(a.hkv));
     const int at = a.blocks - 1 - int(x / unsigned(a.hkv));
-    auto first_block = [&](int b) { return int64_t(a.cu[b]) * a.g / KV_ROWS + b; };
+    auto start = [&](int b) { return a.cu[a.shared ? a.pre_first[b] : b]; };
+    auto first_block = [&](int b) { return int64_t(start(b)) * a.g / KV_ROWS + b; };
     b = last_at(a.n_seqs, first_block, at);
     rb = int(at - first_block(b));
-    q0 = a.cu[b];
-    m = a.cu[b + 1] - q0;
+    q0 = start(b);
+    m = start(b + 1) - q0;
   }
   const int rows = m * a.g, row0 = rb * KV_ROWS;
-  if (rows <= KV_FEW_ROWS || row0 >= rows) return;
+  if ((rows <= FEW_ROWS && !a.shared) || row0 >= rows) return;
   const int len = min(max(a.lens[b], 0), a.max_len), shift = len - m;   // shift: entry of query 0
   const int i_lo = row0 / a.g, i_hi = (min(row0 + KV_ROWS, rows) - 1) / a.g;   // the block's queries
   const int c0 = split * a.piece, c1 = min(len, c0 + a.piece);
-  const int see = min(c1, max(0, shift + i_hi + 1));     // entries [c0, see) are seen by some row
-  const int full = min(c1, max(0, shift + i_lo + 1));    // those before it by every row
+  const int see = a.shared ? c1 : min(c1, max(0, shift + i_hi + 1));     // entries [c0, see) are seen by some row
+  const int full = a.shared ? c1 : min(c1, max(0, shift + i_lo + 1));    // those before it by every row
   if (split > 0 && c0 >= see) return;
   const int row = row0 + wave * ROWS_W + col;
   const bool valid = row < rows;
   const int i_row = (valid ? row : rows - 1) / a.g;
-  const int past = max(0, shift + i_row + 1);            // what the row sees ends here
+  const int past = a.shared ? len : max(0, shift + i_row + 1);           // what the row sees ends here
 
   bf16x8 qf[NKS];
   {
@@ -384,7 +385,7 @@ __global__ __launch_bounds__(256, 2) void attn_many(KvAttnArgs a) {
     }
   }
 
-  const float l_all = l_run + __shfl_xor(l_run, 32);
+  float l_all = l_run + __shfl_xor(l_run, 32);
   if (a.part) {
     if (valid) {
       const int64_t prow = (int64_t(split) * a.hkv + kvh) * (int64_t(a.N) * a.g) + int64_t(q0) * a.g + row;
@@ -399,7 +400,24 @@ __global__ __launch_bounds__(256, 2) void attn_many(KvAttnArgs a) {
     }
     return;
   }
-  const float inv = l_all == 0.f ? 0.f : 1.f / l_all;   // an empty row gives 0, a NaN sum NaN
+  if (a.ppart && valid) {
+    int d[4 * NDB];
+    float4 o[4 * NDB];
+#pragma unroll
+    for (int q = 0; q < 4 * NDB; ++q) {
+      d[q] = (q >> 2) * 32 + (q & 3) * 8 + 4 * hi;
+      o[q] = make_float4(acc[q >> 2][(q & 3) * 4], acc[q >> 2][(q & 3) * 4 + 1], acc[q >> 2][(q & 3) * 4 + 2], acc[q >> 2][(q & 3) * 4 + 3]);
+    }
+    fold_prefix<HD, 16 * NDB, 1>(a, b, kvh, int64_t(q0) * a.g + row, d, m_run, l_all, o);
+#pragma unroll
+    for (int q = 0; q < 4 * NDB; ++q) {
+      acc[q >> 2][(q & 3) * 4] = o[q].x;
+      acc[q >> 2][(q & 3) * 4 + 1] = o[q].y;
+      acc[q >> 2][(q & 3) * 4 + 2] = o[q].z;
+      acc[q >> 2][(q & 3) * 4 + 3] = o[q].w;
+    }
+  }
+  const float inv = row_inverse(l_all);
   if (a.lse && valid && hi == 0)
     a.lse[int64_t(q0 + row / a.g) * a.hq + kvh * a.g + row % a.g] = row_lse(m_run, l_all, a.scale);
   // The outputs go out through LDS as whole rows (the K buffers are free), 16 bytes a lane.
@@ -423,7 +441,7 @@ __global__ __launch_bounds__(256, 2) void attn_many(KvAttnArgs a) {
   }
 }
 
-// out = sum_s o_s 2^((m_s - M) c2) / sum_s l_s 2^((m_s - M) c2), M = max m_s, over a row's pieces in their order.
+// Joins a row's pieces, in their order, and what the pass over the prefixes has of it.
 template <int HD>
 __global__ __launch_bounds__(256) void attn_join(KvAttnArgs a, int64_t group0) {
   constexpr int LPR = HD / 4, NG = 256 / LPR;
@@ -435,43 +453,36 @@ __global__ __launch_bounds__(256) void attn_join(KvAttnArgs a, int64_t group0) {
   const int query = int(r / a.g);
   const int b = last_at(a.n_seqs, [&](int i) { return int64_t(a.cu[i]); }, query);
   const int q0 = a.cu[b], m = a.cu[b + 1] - q0, rows = m * a.g;
-  if (rows <= KV_FEW_ROWS) return;
+  if (rows <= FEW_ROWS) return;
   const int len = min(max(a.lens[b], 0), a.max_len);
   // the pieces that the row's block has
   const int block = int(r - int64_t(q0) * a.g) / KV_ROWS;
   const int see = min(len, max(0, len - m + (min((block + 1) * KV_ROWS, rows) - 1) / a.g + 1));
   const int n = max(1, (see + a.piece - 1) / a.piece);
-  float M = -INFINITY, L = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  Joined j{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
   for (int i0 = 0; i0 < n; i0 += 4) {   // four in flight
     float2 p[4];
     float4 y[4];
+    bool in[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int64_t at = x + min(i0 + q, n - 1) * all * a.hkv;
+      in[q] = i0 + q < n;
       p[q] = a.part_ml[at];
       y[q] = *reinterpret_cast<const float4*>(a.part + at * HD + d);
     }
-    float t = M;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (i0 + q < n) t = fmaxf(t, p[q].x);
-    const float ref = t == -INFINITY ? 0.f : t, c = fast_exp2((M - ref) * a.c2);
-    M = t;
-    L *= c;
-    o = make_float4(o.x * c, o.y * c, o.z * c, o.w * c);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (i0 + q >= n) continue;
-      const float f = fast_exp2((p[q].x - ref) * a.c2);
-      L += p[q].y * f;
-      o = make_float4(o.x + y[q].x * f, o.y + y[q].y * f, o.z + y[q].z * f, o.w + y[q].w * f);
-    }
+    j.add(p, [&](int q) { return y[q]; }, in, a.c2);
   }
-  const float inv = L == 0.f ? 0.f : 1.f / L;
+  if (a.ppart) {
+    const int ds[1] = {d};
+    float4 o[1] = {j.o};
+    fold_prefix<HD, 4, 8>(a, b, kvh, r, ds, j.M, j.L, o);
+    j.o = o[0];
+  }
+  const float inv = row_inverse(j.L);
   const int64_t at = int64_t(query) * a.hq + kvh * a.g + r % a.g;
-  *reinterpret_cast<uint2*>(a.o + at * HD + d) = make_uint2(pack_bf2(o.x * inv, o.y * inv), pack_bf2(o.z * inv, o.w * inv));
-  if (a.lse && d == 0) a.lse[at] = row_lse(M, L, a.scale);
+  *reinterpret_cast<uint2*>(a.o + at * HD + d) = make_uint2(pack_bf2(j.o.x * inv, j.o.y * inv), pack_bf2(j.o.z * inv, j.o.w * inv));
+  if (a.lse && d == 0) a.lse[at] = row_lse(j.M, j.L, a.scale);
 }
 
 template <int HD>
@@ -482,7 +493,7 @@ hipError_t launch_dim(const KvAttnArgs& a, hipStream_t s) {
   else
     hipLaunchKernelGGL((attn_many<HD, false>), grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.part) return e;
+  if (e != hipSuccess || !a.part || a.shared) return e;
   constexpr int NG = 256 / (HD / 4);
   const int64_t groups = (int64_t(a.N) * a.g * a.hkv + NG - 1) / NG;
   for (int64_t g0 = 0; g0 < groups; g0 += MOST_GROUPS) {

@@ -1288,48 +1288,98 @@ cc_status check_prefix(const cc_problem* p, const cc_prefix* x) {
   return CC_OK;
 }
 
-// How a call's sequences of many rows are cut.  Sizes only, so that the workspace query and the call agree.
-struct KvPlan {
-  bool few = false;            // there are sequences of few rows
-  AttnMany items;              // of many rows, up to ATTN_INLINE; else all are walked
+// Row blocks of the kernel for many and how their entries are cut.
+struct KvMany {
+  AttnMany items;              // up to ATTN_INLINE sequences; else all are walked
+  int n = 0;
   int64_t blocks = 0;
   int piece = KV_KEYS, splits = 1;
   size_t part = 0, total = 0;  // workspace: (maximum, sum) pairs behind the outputs
+  void add(int seq, int seq0, int m, int g) {
+    const int nb = int((int64_t(m) * g + KV_ROWS - 1) / KV_ROWS);
+    if (n < ATTN_INLINE) items.seqs[n] = AttnSeq{seq, seq0, m, nb};
+    ++n;
+    blocks += nb;
+  }
+  // walked: sequences there are; groups: workgroups to make by cutting; always: results are joined even if whole
+  cc_status cut(const cc_problem* p, int walked, int max_len, int groups, bool always) {
+    items.nkv = p->n_heads_kv;
+    items.n_seqs = n <= ATTN_INLINE ? n : 0;
+    std::stable_sort(items.seqs, items.seqs + items.n_seqs, [](const AttnSeq& x, const AttnSeq& y) { return x.blocks > y.blocks; });
+    if (n == 0) return CC_OK;
+    const int64_t each = blocks * p->n_heads_kv;
+    if (!items.n_seqs) blocks = int64_t(n_tokens(p)) * (p->n_heads_q / p->n_heads_kv) / KV_ROWS + walked;
+    if (blocks * p->n_heads_kv > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+    // pieces of 256 entries at the least
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({groups / each, (int64_t(max_len) + 255) / 256,
+                                                                 MOST_GROUPS / (blocks * p->n_heads_kv)}));
+    piece = std::max(KV_KEYS, int(((int64_t(max_len) + want - 1) / want + KV_KEYS - 1) / KV_KEYS * KV_KEYS));
+    splits = std::max(1, int((int64_t(max_len) + piece - 1) / piece));
+    if (splits > 1 || always) {
+      const size_t rows = size_t(splits) * p->n_heads_q * n_tokens(p);
+      part = align_up(rows * p->head_dim * sizeof(float));
+      total = part + align_up(rows * sizeof(float2));
+    }
+    return CC_OK;
+  }
 };
 
-cc_status kv_plan(const cc_problem* p, int max_len, KvPlan& c) {
-  const int g = p->n_heads_q / p->n_heads_kv;
-  int many = 0;
-  c.items.nkv = p->n_heads_kv;
+// How a call's sequences are taken.  Sizes only, so that the workspace query and the call agree.
+struct KvPlan {
+  bool rows = false;           // all by 16 rows a workgroup
+  bool inside = false;         // which takes the prefix's entries too
+  int n_few = 0, n_list = 0, listed = 0, R = 0, parts = 0;
+  bool direct = false;         // few rows: by 16 rows a workgroup
+  int32_t list[KV_LIST];
+  size_t fpart = 0, ftotal = 0;
+  KvMany many, prefix;
+  size_t total() const { return prefix.total + ftotal + many.total; }
+};
+
+// What a workgroup for each 16 rows of a (sequence, KV head) is for: short calls, with nothing to join.
+constexpr int KV_SHORT = 1024;
+
+cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& c) {
+  const int g = p->n_heads_q / p->n_heads_kv, hkv = p->n_heads_kv;
+  const int longest = int(std::min<int64_t>(INT32_MAX, int64_t(max_len) + (x ? x->max_len : 0)));
+  int64_t blocks16 = 0;
+  for (int b = 0; b < p->n_seqs; ++b) blocks16 += (int64_t(p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) * g + 15) / 16;
+  c.rows = longest <= KV_SHORT && blocks16 * hkv <= 512;
+  c.inside = x && c.rows;
   for (int b = 0; b < p->n_seqs; ++b) {
     const int seq0 = p->cu_seqlens_h[b], m = p->cu_seqlens_h[b + 1] - seq0;
     const int64_t rows = int64_t(m) * g;
     if (rows == 0) continue;
-    if (rows <= KV_FEW_ROWS) {
-      c.few = true;
-      continue;
+    if (rows <= FEW_ROWS || c.rows) {
+      if (c.n_few < KV_LIST) c.list[c.n_few] = b;
+      ++c.n_few;
+      c.R = int(std::max<int64_t>(c.R, rows));
+    } else {
+      c.many.add(b, seq0, m, g);
     }
-    const int nb = int((rows + KV_ROWS - 1) / KV_ROWS);
-    if (many < ATTN_INLINE) c.items.seqs[many] = AttnSeq{b, seq0, m, nb};
-    ++many;
-    c.blocks += nb;
   }
-  c.items.n_seqs = many <= ATTN_INLINE ? many : 0;
-  std::stable_sort(c.items.seqs, c.items.seqs + c.items.n_seqs, [](const AttnSeq& x, const AttnSeq& y) { return x.blocks > y.blocks; });
-  if (many == 0) return CC_OK;
-  const int64_t items = c.blocks * p->n_heads_kv;
-  if (!c.items.n_seqs) c.blocks = int64_t(n_tokens(p)) * g / KV_ROWS + p->n_seqs;
-  if (c.blocks * p->n_heads_kv > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
-  // As many pieces as leave no more than two workgroups a CU, what is resident, of 256 entries at the least.
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>({2 * kCus / items, (int64_t(max_len) + 255) / 256,
-                                                               MOST_GROUPS / (c.blocks * p->n_heads_kv)}));
-  c.piece = std::max(KV_KEYS, int(((int64_t(max_len) + want - 1) / want + KV_KEYS - 1) / KV_KEYS * KV_KEYS));
-  c.splits = std::max(1, int((int64_t(max_len) + c.piece - 1) / c.piece));
-  if (c.splits > 1) {
-    const size_t rows = size_t(c.splits) * p->n_heads_q * n_tokens(p);
-    c.part = align_up(rows * p->head_dim * sizeof(float));
-    c.total = c.part + align_up(rows * sizeof(float2));
+  const int64_t walked = int64_t(n_tokens(p)) * g / 16 + p->n_seqs;
+  c.direct = c.rows || max_len <= kv8_direct(int64_t(c.n_few) * hkv);
+  // (listed sequences have the blocks of the longest)
+  c.listed = c.n_few <= KV_LIST && (!c.direct || int64_t(c.n_few) * ((c.R + 15) / 16) <= walked);
+  c.n_list = c.listed ? c.n_few : p->n_seqs;
+  c.parts = 2 * kCus;
+  if (c.n_few && !c.direct) {
+    const size_t rows = (size_t(c.parts) + size_t(c.n_list) * hkv) * c.R;
+    c.fpart = align_up(rows * p->head_dim * sizeof(float));
+    c.ftotal = c.fpart + align_up(rows * sizeof(float2));
   }
+  CC_TRY(c.many.cut(p, p->n_seqs, max_len, 2 * kCus, false));
+  if (x && !c.inside) {
+    for (int i = 0; i < x->n_prefixes; ++i) {
+      const int q0 = p->cu_seqlens_h[x->first_seq_h[i]], m = p->cu_seqlens_h[x->first_seq_h[i + 1]] - q0;
+      if (m) c.prefix.add(i, q0, m, g);
+    }
+    CC_TRY(c.prefix.cut(p, x->n_prefixes, x->max_len, kCus, true));
+  }
+  // (a launch by 16 rows a workgroup of 512)
+  const int64_t by16 = (c.listed ? int64_t(c.n_list) * ((c.R + 15) / 16) : walked) * hkv;
+  if (c.n_few && c.direct && by16 > MOST_GROUPS / 2) return CC_ERR_UNSUPPORTED;
   return CC_OK;
 }
 
@@ -1345,8 +1395,8 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
   if (N > 0 && (!q || !o || !kv_lens || !aligned16(q) || !aligned16(o))) return CC_ERR_ARG;
   if (N > 0 && prefix && (!prefix->first_seq_d || !prefix->lens)) return CC_ERR_ARG;
   KvPlan c;
-  if (!prefix) CC_TRY(kv_plan(p, max_kv_len, c));
-  CC_TRY(check_ws(ws, ws_bytes, c.total));
+  CC_TRY(kv_plan(p, prefix, max_kv_len, c));
+  CC_TRY(check_ws(ws, ws_bytes, c.total()));
   if (N == 0) return CC_OK;
   KvAttnArgs a{};
   a.q = static_cast<const u16*>(q);
@@ -1373,14 +1423,46 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
   a.scale = softmax_scale(p);
   a.c2 = a.scale * kLog2e;
   a.room = std::min(8.f / a.c2, FLT_MAX);   // (finite: a first logit passes -inf by more)
-  a.items = c.items;
-  a.blocks = int(c.blocks);
-  a.piece = c.piece;
-  a.splits = c.splits;
-  a.part = c.total ? reinterpret_cast<float*>(ws) : nullptr;
-  a.part_ml = c.total ? reinterpret_cast<float2*>(at(ws, c.part)) : nullptr;
-  if (prefix || c.few) CC_HIP(launch_attn_rows(a, static_cast<hipStream_t>(stream)));
-  if (c.blocks) CC_HIP(launch_attn_kv_many(a, static_cast<hipStream_t>(stream)));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  size_t off = 0;
+  auto many = [&](const KvMany& m) {
+    a.items = m.items;
+    a.blocks = int(m.blocks);
+    a.piece = m.piece;
+    a.splits = m.splits;
+    a.part = m.total ? reinterpret_cast<float*>(at(ws, off)) : nullptr;
+    a.part_ml = m.total ? reinterpret_cast<float2*>(at(ws, off + m.part)) : nullptr;
+    off += m.total;
+    return launch_attn_kv_many(a, st);
+  };
+  if (c.prefix.n) {
+    const KvAttnArgs own = a;
+    a.own = a.pre;
+    a.lens = a.pre_lens;
+    a.max_len = a.pre_max;
+    a.n_seqs = a.n_prefixes;
+    a.shared = 1;
+    CC_HIP(many(c.prefix));
+    const float* part = a.part;
+    const float2* part_ml = a.part_ml;
+    a = own;
+    a.ppart = part;
+    a.ppart_ml = part_ml;
+    a.ppiece = c.prefix.piece;
+  }
+  if (c.n_few) {
+    a.n_list = c.n_list;
+    a.listed = c.listed;
+    a.R = c.R;
+    a.most = c.rows ? INT32_MAX : FEW_ROWS;
+    a.parts = c.parts;
+    std::copy_n(c.list, c.listed ? c.n_few : 0, a.list);
+    a.fpart = c.ftotal ? reinterpret_cast<float*>(at(ws, off)) : nullptr;
+    a.fpart_ml = c.ftotal ? reinterpret_cast<float2*>(at(ws, off + c.fpart)) : nullptr;
+    off += c.ftotal;
+    CC_HIP(c.direct ? launch_attn_rows(a, st) : launch_attn_few(a, st));
+  }
+  if (c.many.n) CC_HIP(many(c.many));
   return CC_OK;
 }
 
@@ -1400,8 +1482,8 @@ cc_status cc_attention_kv_workspace(const cc_problem* p, int32_t max_kv_len, siz
   if (!bytes) return CC_ERR_ARG;
   CC_TRY(check_attention_kv(p, max_kv_len));
   KvPlan c;
-  CC_TRY(kv_plan(p, max_kv_len, c));
-  *bytes = c.total;
+  CC_TRY(kv_plan(p, nullptr, max_kv_len, c));
+  *bytes = c.total();
   return CC_OK;
 }
 
@@ -1416,7 +1498,9 @@ cc_status cc_attention_prefix_workspace(const cc_problem* p, const cc_prefix* pr
   if (!bytes) return CC_ERR_ARG;
   CC_TRY(check_attention_kv(p, max_kv_len));
   CC_TRY(check_prefix(p, prefix));
-  *bytes = 0;
+  KvPlan c;
+  CC_TRY(kv_plan(p, prefix, max_kv_len, c));
+  *bytes = c.total();
   return CC_OK;
 }
 
