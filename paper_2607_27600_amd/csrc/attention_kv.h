@@ -91,6 +91,14 @@ hipError_t launch_compact_weights(const CompactWeightsArgs& a, hipStream_t s);
 
 // ---- shared by the attention kernels
 
+// T at a wave-uniform base and a lane's offset: in the global address space, so that the base stays in scalar registers
+// (as generic loads, each with a 64-bit address a lane, the kernel for few rows spilled 45 registers).
+template <class T>
+__device__ __forceinline__ T load_at(const char* base, uint32_t off) {
+  typedef __attribute__((address_space(1))) const char* gptr;
+  return *(__attribute__((address_space(1))) const T*)((gptr)(base) + off);
+}
+
 // Bits 15 and 31 where the low and the high bf16 of a word are NaN or infinite.
 __device__ __forceinline__ uint32_t wide_halves(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 // 0xffff at bits 15 and 31.

@@ -20,11 +20,14 @@
 // sequence are zeroed as they are read, and in steps that some row sees in part, NaN and infinite elements are
 // zeroed too and added by the rows that see them.
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_kv.h"
 
 namespace cc {
 namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // NR blocks of 16 rows, in a wave: queries, running maximum and sum, outputs.
 template <int HD, int NR>
@@ -35,9 +38,13 @@ struct Rows {
   bf16x8 qf[NR][NKS];
   float m[NR], l[NR];
   f32x4 acc[NR][NDB];
-  struct Step {                         // two groups of 16 entries
-    uint4 k[2][NKS];
-    uint32_t v[8][VW];
+  typedef uint32_t Words __attribute__((ext_vector_type(VW)));
+  // a step: two groups of 16 entries
+  struct Keys {
+    u32x4 k[2][NKS];
+  };
+  struct Values {
+    Words v[8];
   };
 
   __device__ __forceinline__ void clear() {
@@ -54,43 +61,45 @@ struct Rows {
   // past[n], and every row those before full.
   __device__ __forceinline__ void run(const KvAttnArgs& a, const KvPlane& P, int gb, int ge, int len, const int (&past)[NR],
                                       int full) {
-    const int lane = threadIdx.x & 63, grp = lane >> 4, r16 = lane & 15;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));   // what follows from it is made anew for each item, not kept over a loop of them
+    const int grp = lane >> 4, r16 = lane & 15;
     const int last = len - 1;
     const uint32_t ts = P.ts;
+    // Steps before group `mid` are seen by every row.  (Past the wave's own groups counts as masked: the last group
+    // stands there a second time.)
+    const int stop = min(ge << 4, len);
+    const int mid = gb + max(0, min(full, stop) - (gb << 4)) / 32 * 2;
     // Pages of 64 groups at a time, a lane each.
     for (int sb = gb; sb < ge; sb += 64) {
       const int se = min(ge, sb + 64);
       const int page = P.page(min(sb + lane, se - 1));
       auto base = [&](int gg) { return P.offset(__builtin_amdgcn_readlane(page, gg - sb), gg << 4); };
-      auto load = [&](int gr, Step& st) {   // groups gr and gr + 1 (past the end: the last one again)
+      // of groups gr and gr + 1 (past the end: the last one again; past a group's last entry: that one again)
+      auto load_keys = [&](int gr, Keys& st) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const int gg = min(gr + t, se - 1);
-          const int64_t off = base(gg);
-          const char* kp = uniform_ptr(P.k + off);
-          const char* vp = uniform_ptr(P.v + off);
-          const int have = last - (gg << 4);   // the group's last entry; past it: that one again
-          const uint32_t ko = uint32_t(min(r16, have)) * ts + 16 * grp;
+          const char* kp = uniform_ptr(P.k + base(gg));
+          const uint32_t ko = uint32_t(min(r16, last - (gg << 4))) * ts + 16 * grp;
 #pragma unroll
-          for (int k = 0; k < NKS; ++k) st.k[t][k] = *reinterpret_cast<const uint4*>(kp + ko + 64 * k);
+          for (int k = 0; k < NKS; ++k) st.k[t][k] = load_at<u32x4>(kp, ko + 64 * k);
+        }
+      };
+      auto load_values = [&](int gr, Values& st) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int gg = min(gr + t, se - 1);
+          const char* vp = uniform_ptr(P.v + base(gg));
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const char* x = vp + uint32_t(min(4 * grp + e, have)) * ts + 2 * NDB * r16;
-            if constexpr (VW == 4) {
-              const uint4 w = *reinterpret_cast<const uint4*>(x);
-              st.v[4 * t + e][0] = w.x;
-              st.v[4 * t + e][1] = w.y;
-              st.v[4 * t + e][VW - 2] = w.z;
-              st.v[4 * t + e][VW - 1] = w.w;
-            } else {
-              const uint2 w = *reinterpret_cast<const uint2*>(x);
-              st.v[4 * t + e][0] = w.x;
-              st.v[4 * t + e][1] = w.y;
-            }
+            const uint32_t vo = uint32_t(min(4 * grp + e, last - (gg << 4))) * ts + 2 * NDB * r16;
+            st.v[4 * t + e] = load_at<Words>(vp, vo);
           }
         }
       };
-      auto compute = [&](int gr, Step& st) {
+      // The probabilities of a step, as far as the running maximum goes.
+      auto scores = [&](int gr, const Keys& st, bf16x8(&pf)[NR], auto masked) {
         f32x4 z[NR][2];
 #pragma unroll
         for (int n = 0; n < NR; ++n) z[n][0] = z[n][1] = f32x4{};
@@ -99,13 +108,9 @@ struct Rows {
 #pragma unroll
           for (int k = 0; k < NKS; ++k)
 #pragma unroll
-            for (int n = 0; n < NR; ++n) z[n][t] = mfma16(as_bf16x8(st.k[t][k]), qf[n][k], z[n][t]);
+            for (int n = 0; n < NR; ++n) z[n][t] = mfma16(__builtin_bit_cast(bf16x8, st.k[t][k]), qf[n][k], z[n][t]);
         const int e0 = gr << 4;
-        // past the wave's own groups counts as masked: the last group stands there a second time
-        const int stop = min(ge << 4, len);
-        const bool masked = e0 + 32 > min(full, stop);
-        bool wide = false;
-        if (masked) {
+        if constexpr (decltype(masked)::value) {
 #pragma unroll
           for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -113,24 +118,6 @@ struct Rows {
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 if (e0 + 16 * t + 4 * grp + e >= min(past[n], stop)) z[n][t][e] = -INFINITY;
-          uint32_t bits = 0;
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-              for (int i = 0; i < VW; ++i) {
-                uint32_t& w = st.v[4 * t + e][i];
-                if (e0 + 16 * t + 4 * grp + e >= stop) w = 0;   // values that the sequence does not have
-                bits |= wide_halves(w);
-              }
-          wide = __any(bits != 0);
-          if (wide) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-#pragma unroll
-              for (int i = 0; i < VW; ++i) st.v[e][i] &= ~whole_halves(wide_halves(st.v[e][i]));
-          }
         }
         float mx[NR];
         bool moved = false;
@@ -151,7 +138,6 @@ struct Rows {
             for (int d = 0; d < NDB; ++d) acc[n][d] *= corr;
           }
         }
-        bf16x8 pf[NR];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
           const float mc = m[n] == -INFINITY ? 0.f : m[n] * a.c2;
@@ -163,6 +149,29 @@ struct Rows {
             pf[n][e] = (__bf16)p;
           }
           l[n] += sum;
+        }
+      };
+      auto values = [&](int gr, Values& st, const bf16x8(&pf)[NR], auto masked) {
+        const int e0 = gr << 4;
+        bool wide = false;
+        if constexpr (decltype(masked)::value) {
+          uint32_t bits = 0;
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int i = 0; i < VW; ++i) {
+                if (e0 + 16 * t + 4 * grp + e >= stop) st.v[4 * t + e][i] = 0;   // values that the sequence does not have
+                bits |= wide_halves(st.v[4 * t + e][i]);
+              }
+          wide = __any(bits != 0);
+          if (wide) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+              for (int i = 0; i < VW; ++i) st.v[e][i] &= ~whole_halves(wide_halves(st.v[e][i]));
+          }
         }
 #pragma unroll
         for (int i = 0; i < VW; ++i)
@@ -185,7 +194,7 @@ struct Rows {
 #pragma unroll
               for (int d = 0; d < NDB; ++d) {
                 const float x = bf2f(reinterpret_cast<const u16*>(v)[NDB * e + d]);
-                if (!(fabsf(x) < INFINITY)) {
+                if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) {
 #pragma unroll
                   for (int n = 0; n < NR; ++n)
                     if (key < past[n]) acc[n][d][e] += x;
@@ -194,15 +203,36 @@ struct Rows {
           }
         }
       };
-      Step st[2];
-      load(sb, st[0]);
-      for (int gr = sb; gr < se; gr += 4) {
-        if (gr + 2 < se) load(gr + 2, st[1]);
-        compute(gr, st[0]);
-        if (gr + 2 < se) {
-          if (gr + 4 < se) load(gr + 4, st[0]);
-          compute(gr + 2, st[1]);
+      // In flight: the keys of the next step during a step's first product, its values during the second (the fences
+      // keep loads from being hoisted, which takes twice the registers).
+      Keys k[2];
+      Values v[2];
+      bf16x8 pf[NR];
+      auto step = [&](int gr, int to, Keys& k0, Keys& k1, Values& v0, Values& v1) {
+        const bool more = gr + 2 < to;
+        if (more) load_keys(gr + 2, k1);
+        scores(gr, k0, pf, std::false_type{});
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) load_values(gr + 2, v1);
+        __builtin_amdgcn_sched_barrier(0);
+        values(gr, v0, pf, std::false_type{});
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      const int sm = min(se, mid);
+      if (sb < sm) {
+        load_keys(sb, k[0]);
+        load_values(sb, v[0]);
+        for (int gr = sb; gr < sm; gr += 4) {
+          step(gr, sm, k[0], k[1], v[0], v[1]);
+          if (gr + 2 < sm) step(gr + 2, sm, k[1], k[0], v[1], v[0]);
         }
+      }
+#pragma unroll 1
+      for (int gr = max(sb, mid); gr < se; gr += 2) {   // the last ones
+        load_keys(gr, k[0]);
+        load_values(gr, v[0]);
+        scores(gr, k[0], pf, std::true_type{});
+        values(gr, v[0], pf, std::true_type{});
       }
     }
   }
@@ -213,7 +243,9 @@ struct Rows {
 template <int HD, int NR, int NW, class F>
 __device__ __forceinline__ void meet(const KvAttnArgs& a, const Rows<HD, NR>& st, float* lds, float2* ml, int rows, F done) {
   constexpr int ROWS = 16 * NR, LPR = HD / 8, NDB = HD / 16;
-  const int tid = threadIdx.x, lane = tid & 63, grp = lane >> 4, r16 = lane & 15;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, grp = lane >> 4, r16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
@@ -268,7 +300,9 @@ __device__ __forceinline__ void finish(const KvAttnArgs& a, int b, int q0, int k
 // Rows' queries; row block n has rows row0 + 16 n ...
 template <int HD, int NR>
 __device__ __forceinline__ void load_queries(const KvAttnArgs& a, Rows<HD, NR>& st, int q0, int kvh, int row0, int rows, int (&i)[NR]) {
-  const int lane = threadIdx.x & 63, grp = lane >> 4, r16 = lane & 15;
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  const int grp = lane >> 4, r16 = lane & 15;
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     const int row = min(row0 + 16 * n + r16, rows - 1);
