@@ -44,11 +44,14 @@ struct KvAttnArgs {
   // Results to be joined (null: none), outputs and (maximum, sum): [splits][Hkv][N g]
   float* part;
   float2* part_ml;
-  // What a pass over the prefixes has left (null: none), laid out like part, pieces of ppiece entries.  In that pass
-  // the prefixes stand for sequences (own, lens and n_seqs are theirs) and `shared` is set.
-  const float* ppart;
-  const float2* ppart_ml;
-  int ppiece, shared;
+  // The pass over the prefixes (shared = 1): they stand for sequences, and own, lens and n_seqs are theirs.  Its pieces
+  // are sized on the device, by the prefixes' lengths, for `slots` workgroups at the least: a workgroup, and KV_ROWS rows
+  // of ppart, for each.  Where prefix i's begin and how many each of its (row block, KV head) has is in pre_at[i].  For the
+  // passes over the sequences' own entries ppart and pre_at are what it has left (null: none).
+  float* ppart;
+  float2* ppart_ml;
+  int2* pre_at;
+  int slots, shared;
 };
 // 16 rows a workgroup, whole; with n_prefixes and no ppart the prefix's entries too.
 hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s);
@@ -150,43 +153,19 @@ __device__ __forceinline__ KvPlane kv_plane(const KvPair& p, int b, int layer, i
   return x;
 }
 
-// What the pass over the prefixes has of a row, V outputs from d on, folded into (M, L, o): its pieces in their order, as
-// many at a time as fit V * AT registers.
-template <int HD, int V, int AT>
-__device__ __forceinline__ void fold_prefix(const KvAttnArgs& a, int b, int kvh, int64_t query_row, const int (&d)[V / 4], float& M,
-                                            float& L, float4 (&o)[V / 4]) {
-  const int j = last_at(a.n_prefixes, [&](int i) { return int64_t(a.pre_first[i]); }, b);
-  const int n = max(1, (min(max(a.pre_lens[j], 0), a.pre_max) + a.ppiece - 1) / a.ppiece);
-  const int64_t all = int64_t(a.N) * a.g, row = int64_t(kvh) * all + query_row;
-  for (int i0 = 0; i0 < n; i0 += AT) {
-    float2 p[AT];
-    float4 y[AT][V / 4];
-#pragma unroll
-    for (int q = 0; q < AT; ++q) {
-      const int64_t at = row + min(i0 + q, n - 1) * all * a.hkv;
-      p[q] = a.ppart_ml[at];
-#pragma unroll
-      for (int v = 0; v < V / 4; ++v) y[q][v] = *reinterpret_cast<const float4*>(a.ppart + at * HD + d[v]);
-    }
-    float t = M;
-#pragma unroll
-    for (int q = 0; q < AT; ++q)
-      if (i0 + q < n) t = fmaxf(t, p[q].x);
-    const float ref = t == -INFINITY ? 0.f : t, c = fast_exp2((M - ref) * a.c2);
-    M = t;
-    L *= c;
-#pragma unroll
-    for (int v = 0; v < V / 4; ++v) o[v] = make_float4(o[v].x * c, o[v].y * c, o[v].z * c, o[v].w * c);
-#pragma unroll
-    for (int q = 0; q < AT; ++q) {
-      if (i0 + q >= n) continue;
-      const float f = fast_exp2((p[q].x - ref) * a.c2);
-      L += p[q].y * f;
-#pragma unroll
-      for (int v = 0; v < V / 4; ++v)
-        o[v] = make_float4(o[v].x + y[q][v].x * f, o[v].y + y[q][v].y * f, o[v].z + y[q][v].z * f, o[v].w + y[q][v].w * f);
-    }
-  }
+// Where the pass over the prefixes has left row `row` of run j's queries, for KV head kvh: rows first, first + KV_ROWS, ... of
+// ppart, n of them.
+struct PrefixRow {
+  int64_t first;
+  int n;
+};
+__device__ __forceinline__ PrefixRow prefix_row(const KvAttnArgs& a, int j, int kvh, int64_t row) {
+  const int2 at = a.pre_at[j];
+  const int64_t item = row / KV_ROWS * a.hkv + kvh;
+  return PrefixRow{(at.x + item * at.y) * KV_ROWS + row % KV_ROWS, at.y};
+}
+__device__ __forceinline__ int prefix_of(const KvAttnArgs& a, int b) {
+  return last_at(a.n_prefixes, [&](int i) { return int64_t(a.pre_first[i]); }, b);
 }
 
 }  // namespace cc

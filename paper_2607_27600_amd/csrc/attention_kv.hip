@@ -57,6 +57,32 @@ struct Rows {
     }
   }
 
+  // The share of wave w of NW of what the pass over the prefixes has left of row block n's rows, p of them (one a lane).
+  template <int NW>
+  __device__ __forceinline__ void absorb(const KvAttnArgs& a, int w, const PrefixRow (&p)[NR]) {
+    const int grp = (threadIdx.x & 63) >> 4;
+    for (int s = w; s < p[0].n; s += NW)   // (rows of one run: alike in all)
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const int64_t row = p[n].first + int64_t(s) * KV_ROWS;
+        const float2 ml = a.ppart_ml[row];
+        const float* x = a.ppart + row * HD + NDB * 4 * grp;
+        f32x4 y[4][NDB / 4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int d = 0; d < NDB / 4; ++d) y[e][d] = *reinterpret_cast<const f32x4*>(x + NDB * e + 4 * d);
+        const float top = fmaxf(m[n], ml.x), ref = top == -INFINITY ? 0.f : top;
+        const float c = fast_exp2((m[n] - ref) * a.c2), f = fast_exp2((ml.x - ref) * a.c2);
+        m[n] = top;
+        l[n] = l[n] * c + (grp == 0 ? ml.y * f : 0.f);   // (the sum over the lanes of a row comes later)
+#pragma unroll
+        for (int d = 0; d < NDB; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[n][d][e] = acc[n][d][e] * c + y[e][d >> 2][d & 3] * f;
+      }
+  }
+
   // 16-entry groups [gb, ge) of a plane of len entries, of which row block n's rows (one a lane) see those before
   // past[n], and every row those before full.
   __device__ __forceinline__ void run(const KvAttnArgs& a, const KvPlane& P, int gb, int ge, int len, const int (&past)[NR],
@@ -282,13 +308,9 @@ __device__ __forceinline__ void meet(const KvAttnArgs& a, const Rows<HD, NR>& st
   }
 }
 
-// The final result of row r of sequence b, eight outputs from d on.
+// The final result of row r of the sequence of query q0, eight outputs from d on.
 template <int HD>
-__device__ __forceinline__ void finish(const KvAttnArgs& a, int b, int q0, int kvh, int r, int d, float M, float L, float4 (&o)[2]) {
-  if (a.ppart) {
-    const int ds[2] = {d, d + 4};
-    fold_prefix<HD, 8, 8>(a, b, kvh, int64_t(q0) * a.g + r, ds, M, L, o);
-  }
+__device__ __forceinline__ void finish(const KvAttnArgs& a, int q0, int kvh, int r, int d, float M, float L, const float4 (&o)[2]) {
   const float inv = row_inverse(L);
   const int64_t out = int64_t(q0 + r / a.g) * a.hq + kvh * a.g + r % a.g;
   *reinterpret_cast<uint4*>(a.o + out * HD + d) =
@@ -350,8 +372,12 @@ __global__ __launch_bounds__(ROWS_NT, 2) void attn_rows(KvAttnArgs a) {
     ge = min(groups, gb + per);
   };
   int gb, ge;
-  if (a.n_prefixes && !a.ppart) {
-    const int j = last_at(a.n_prefixes, [&](int i) { return int64_t(a.pre_first[i]); }, b);
+  if (a.ppart) {
+    const int j = prefix_of(a, b);
+    const PrefixRow p[1] = {prefix_row(a, j, kvh, int64_t(q0 - a.cu[a.pre_first[j]]) * a.g + min(row0 + int(threadIdx.x & 15), rows - 1))};
+    st.template absorb<NW>(a, wave, p);
+  } else if (a.n_prefixes) {
+    const int j = prefix_of(a, b);
     const int n = min(max(a.pre_lens[j], 0), a.pre_max);
     const int past[1] = {n};
     part((n + 15) >> 4, gb, ge);
@@ -362,7 +388,7 @@ __global__ __launch_bounds__(ROWS_NT, 2) void attn_rows(KvAttnArgs a) {
   part((most + 15) >> 4, gb, ge);
   st.run(a, kv_plane(a.own, b, a.layer, kvh), gb, ge, len, past, max(0, shift + row0 / a.g + 1));
   meet<HD, 1, NW>(a, st, lds, ml, min(ROWS, rows - row0),
-                  [&](int r, int d, float M, float L, float4(&o)[2]) { finish<HD>(a, b, q0, kvh, row0 + r, d, M, L, o); });
+                  [&](int r, int d, float M, float L, float4(&o)[2]) { finish<HD>(a, q0, kvh, row0 + r, d, M, L, o); });
 }
 
 // ------------------------------------------------------------------ few rows, work shared out
@@ -394,6 +420,14 @@ __global__ __launch_bounds__(FEW_NT, 2) void attn_few(KvAttnArgs a) {
     int i[NR], past[NR];
     load_queries(a, st, s.q0, kvh, 0, rows, i);
     st.clear();
+    if (a.ppart && u0 == 0) {   // an item's first entries go with its prefix
+      const int jp = prefix_of(a, s.b);
+      const int64_t first = int64_t(s.q0 - a.cu[a.pre_first[jp]]) * a.g;
+      PrefixRow p[NR];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) p[n] = prefix_row(a, jp, kvh, first + min(16 * n + int(threadIdx.x & 15), rows - 1));
+      st.template absorb<NW>(a, wave, p);
+    }
 #pragma unroll
     for (int n = 0; n < NR; ++n) past[n] = max(0, s.shift + i[n] + 1);
     // this wave's 16-entry groups: the piece's, in NW runs of whole steps of two
@@ -402,7 +436,7 @@ __global__ __launch_bounds__(FEW_NT, 2) void attn_few(KvAttnArgs a) {
     const int gb = g0 + wave * per, ge = min(g1, gb + per);
     st.run(a, kv_plane(a.own, s.b, a.layer, kvh), gb, ge, s.len, past, max(0, s.shift + 1));
     meet<HD, NR, NW>(a, st, lds, ml, rows, [&](int r, int d, float M, float L, float4(&o)[2]) {
-      if (whole) return finish<HD>(a, s.b, s.q0, kvh, r, d, M, L, o);
+      if (whole) return finish<HD>(a, s.q0, kvh, r, d, M, L, o);
       const int64_t row = (int64_t(blockIdx.x) + int64_t(j) * a.hkv + kvh) * a.R + r;
       float* po = a.fpart + row * HD + d;
       *reinterpret_cast<float4*>(po) = o[0];
@@ -490,7 +524,7 @@ __global__ __launch_bounds__(256) void attn_few_join(KvAttnArgs a, int one, int6
   }
   if (!on) return;
   float4 o[2] = {g[0].o, g[1].o};
-  finish<HD>(a, s.b, s.q0, kvh, r, d, g[0].M, g[0].L, o);
+  finish<HD>(a, s.q0, kvh, r, d, g[0].M, g[0].L, o);
 }
 
 template <int HD, int NR>

@@ -73,6 +73,70 @@ __device__ __forceinline__ void page_numbers(const int32_t* p0, const int32_t* p
                : "=&s"(o0), "=&s"(o1), "=&s"(o2), "=&s"(o3) : "s"(p0), "s"(p1), "s"(p2), "s"(p3) : "memory");
 }
 
+// The pieces of the pass over the prefixes, a workgroup each, prefix by prefix, of each its row blocks, KV heads and pieces in
+// order.  All are of as many tiles (TILES at the least) as make no more than `slots` of them, or whole where there are
+// more (row block, KV head)s than that.  Lengths are known on the device alone, so every workgroup works it out, and the
+// first leaves where each prefix's begin.
+struct Piece {
+  int j, q0, m, len, item, nth, tiles;   // item: row block * Hkv + KV head; j < 0: none
+};
+constexpr int TILES = 4;
+__device__ __forceinline__ Piece piece_of(const KvAttnArgs& a, int64_t x) {
+  const int lane = threadIdx.x & 63;
+  const int64_t items = int64_t(a.blocks) * a.hkv;   // at least those there are
+  struct Run {
+    int q0, m, len, tiles;
+    int64_t items;
+  };
+  auto run = [&](int i) {   // a lane's
+    Run r{0, 0, 0, 0, 0};
+    if (i < a.n_seqs) {
+      r.q0 = a.cu[a.pre_first[i]];
+      r.m = a.cu[a.pre_first[i + 1]] - r.q0;
+      r.len = min(max(a.lens[i], 0), a.max_len);
+      r.tiles = (r.len + BN - 1) / BN;
+      r.items = (int64_t(r.m) * a.g + KV_ROWS - 1) / KV_ROWS * a.hkv;
+    }
+    return r;
+  };
+  int tiles = INT32_MAX / BN;
+  if (items < a.slots) {   // (fewer than 2^31 tiles, then)
+    int64_t all = 0;
+    for (int i = 0; i < a.n_seqs; i += 64) {
+      const Run r = run(i + lane);
+      // lanes' sums of fewer than 512 items of fewer than 2^26 tiles, taken apart at bit 16
+      const int64_t mine = r.items * r.tiles;
+      all += (int64_t(__builtin_amdgcn_readlane(wave_scan(int(mine >> 16)), 63)) << 16) +
+             __builtin_amdgcn_readlane(wave_scan(int(mine & 0xffff)), 63);
+    }
+    tiles = int(min(int64_t(tiles), max(int64_t(TILES), (all + a.slots - items - 1) / (a.slots - items))));
+  }
+  Piece p{-1, 0, 0, 0, 0, 0, tiles};
+  int64_t start = 0;
+  for (int i = 0; i < a.n_seqs; i += 64) {
+    const Run r = run(i + lane);
+    const int n = max(1, (r.tiles + p.tiles - 1) / p.tiles);
+    const int mine = int(r.items) * n;
+    const int sum = wave_scan(mine);
+    if (x == 0 && threadIdx.x < 64 && i + lane < a.n_seqs) a.pre_at[i + lane] = make_int2(int(start) + sum - mine, n);
+    const uint64_t past = __ballot(start + sum > x);
+    if (past && p.j < 0) {
+      const int l = __builtin_ctzll(past);
+      const int at = int(x - start) - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(mine, l));
+      const int each = __builtin_amdgcn_readlane(n, l);
+      p.j = i + l;
+      p.q0 = __builtin_amdgcn_readlane(r.q0, l);
+      p.m = __builtin_amdgcn_readlane(r.m, l);
+      p.len = __builtin_amdgcn_readlane(r.len, l);
+      p.item = at / each;
+      p.nth = at % each;
+      if (x) return p;
+    }
+    start += __builtin_amdgcn_readlane(sum, 63);
+  }
+  return p;
+}
+
 template <int HD, bool PAGED>
 __global__ __launch_bounds__(256, 2) void attn_many(KvAttnArgs a) {
   using SH = Shape<HD>;
@@ -86,34 +150,49 @@ __global__ __launch_bounds__(256, 2) void attn_many(KvAttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hi = lane >> 5, col = lane & 31;
 
-  // Heaviest blocks first: the last rows of the longest sequences.
+  int b, kvh, rb, q0, m, len, split, piece;
   unsigned x = blockIdx.x;
-  const int split = int(x % unsigned(a.splits));
-  x /= unsigned(a.splits);
-  int b, kvh, rb, q0, m;
-  if (a.items.n_seqs) {
-    const AttnItem w = a.items.item(int(x));
-    b = w.seq;
-    kvh = w.kvh;
-    q0 = w.seq0;
-    m = w.n;
-    // (the list's items begin with the first blocks)
-    rb = int((int64_t(m) * a.g + KV_ROWS - 1) / KV_ROWS) - 1 - w.rb;
+  if (a.shared) {
+    const Piece p = piece_of(a, x);
+    if (p.j < 0) return;
+    b = p.j;
+    q0 = p.q0;
+    m = p.m;
+    len = p.len;
+    split = p.nth;
+    rb = p.item / a.hkv;
+    kvh = p.item % a.hkv;
+    piece = p.tiles * BN;
   } else {
-    kvh = int(x % unsigned(a.hkv));
-    const int at = a.blocks - 1 - int(x / unsigned(a.hkv));
-    auto start = [&](int b) { return a.cu[a.shared ? a.pre_first[b] : b]; };
-    auto first_block = [&](int b) { return int64_t(start(b)) * a.g / KV_ROWS + b; };
-    b = last_at(a.n_seqs, first_block, at);
-    rb = int(at - first_block(b));
-    q0 = start(b);
-    m = start(b + 1) - q0;
+    // Heaviest blocks first: the last rows of the longest sequences.
+    split = int(x % unsigned(a.splits));
+    piece = a.piece;
+    x /= unsigned(a.splits);
+    if (a.items.n_seqs) {
+      const AttnItem w = a.items.item(int(x));
+      b = w.seq;
+      kvh = w.kvh;
+      q0 = w.seq0;
+      m = w.n;
+      // (the list's items begin with the first blocks)
+      rb = int((int64_t(m) * a.g + KV_ROWS - 1) / KV_ROWS) - 1 - w.rb;
+    } else {
+      kvh = int(x % unsigned(a.hkv));
+      const int at = a.blocks - 1 - int(x / unsigned(a.hkv));
+      auto first_block = [&](int b) { return int64_t(a.cu[b]) * a.g / KV_ROWS + b; };
+      b = last_at(a.n_seqs, first_block, at);
+      rb = int(at - first_block(b));
+      q0 = a.cu[b];
+      m = a.cu[b + 1] - q0;
+    }
+    if (m * a.g <= FEW_ROWS) return;
+    len = min(max(a.lens[b], 0), a.max_len);
   }
   const int rows = m * a.g, row0 = rb * KV_ROWS;
-  if ((rows <= FEW_ROWS && !a.shared) || row0 >= rows) return;
-  const int len = min(max(a.lens[b], 0), a.max_len), shift = len - m;   // shift: entry of query 0
+  if (row0 >= rows) return;
+  const int shift = len - m;                                                   // entry of query 0
   const int i_lo = row0 / a.g, i_hi = (min(row0 + KV_ROWS, rows) - 1) / a.g;   // the block's queries
-  const int c0 = split * a.piece, c1 = min(len, c0 + a.piece);
+  const int c0 = split * piece, c1 = int(min(int64_t(len), int64_t(c0) + piece));
   const int see = a.shared ? c1 : min(c1, max(0, shift + i_hi + 1));     // entries [c0, see) are seen by some row
   const int full = a.shared ? c1 : min(c1, max(0, shift + i_lo + 1));    // those before it by every row
   if (split > 0 && c0 >= see) return;
@@ -386,36 +465,40 @@ __global__ __launch_bounds__(256, 2) void attn_many(KvAttnArgs a) {
   }
 
   float l_all = l_run + __shfl_xor(l_run, 32);
-  if (a.part) {
+  if (a.ppart && !a.shared && split == 0 && valid) {   // a row's first entries go with its prefix
+    const int j = prefix_of(a, b);
+    const PrefixRow p = prefix_row(a, j, kvh, int64_t(q0 - a.cu[a.pre_first[j]]) * a.g + row);
+    for (int s = 0; s < p.n; ++s) {
+      const int64_t at = p.first + int64_t(s) * KV_ROWS;
+      const float2 ml = a.ppart_ml[at];
+      const float top = fmaxf(m_run, ml.x), ref = top == -INFINITY ? 0.f : top;
+      const float c = fast_exp2((m_run - ref) * a.c2), f = fast_exp2((ml.x - ref) * a.c2);
+      m_run = top;
+      l_all = l_all * c + ml.y * f;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 y = *reinterpret_cast<const f32x4*>(a.ppart + at * HD + db * 32 + q * 8 + 4 * hi);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[db][q * 4 + e] = acc[db][q * 4 + e] * c + y[e] * f;
+        }
+    }
+  }
+  if (a.part || a.shared) {
     if (valid) {
-      const int64_t prow = (int64_t(split) * a.hkv + kvh) * (int64_t(a.N) * a.g) + int64_t(q0) * a.g + row;
-      float* po = a.part + prow * HD + 4 * hi;
+      const int64_t prow = a.shared ? int64_t(blockIdx.x) * KV_ROWS + wave * ROWS_W + col
+                                    : (int64_t(split) * a.hkv + kvh) * (int64_t(a.N) * a.g) + int64_t(q0) * a.g + row;
+      float* po = (a.shared ? a.ppart : a.part) + prow * HD + 4 * hi;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           *reinterpret_cast<float4*>(po + db * 32 + q * 8) =
               make_float4(acc[db][q * 4], acc[db][q * 4 + 1], acc[db][q * 4 + 2], acc[db][q * 4 + 3]);
-      if (hi == 0) a.part_ml[prow] = make_float2(m_run, l_all);
+      if (hi == 0) (a.shared ? a.ppart_ml : a.part_ml)[prow] = make_float2(m_run, l_all);
     }
     return;
-  }
-  if (a.ppart && valid) {
-    int d[4 * NDB];
-    float4 o[4 * NDB];
-#pragma unroll
-    for (int q = 0; q < 4 * NDB; ++q) {
-      d[q] = (q >> 2) * 32 + (q & 3) * 8 + 4 * hi;
-      o[q] = make_float4(acc[q >> 2][(q & 3) * 4], acc[q >> 2][(q & 3) * 4 + 1], acc[q >> 2][(q & 3) * 4 + 2], acc[q >> 2][(q & 3) * 4 + 3]);
-    }
-    fold_prefix<HD, 16 * NDB, 1>(a, b, kvh, int64_t(q0) * a.g + row, d, m_run, l_all, o);
-#pragma unroll
-    for (int q = 0; q < 4 * NDB; ++q) {
-      acc[q >> 2][(q & 3) * 4] = o[q].x;
-      acc[q >> 2][(q & 3) * 4 + 1] = o[q].y;
-      acc[q >> 2][(q & 3) * 4 + 2] = o[q].z;
-      acc[q >> 2][(q & 3) * 4 + 3] = o[q].w;
-    }
   }
   const float inv = row_inverse(l_all);
   if (a.lse && valid && hi == 0)
@@ -441,7 +524,7 @@ __global__ __launch_bounds__(256, 2) void attn_many(KvAttnArgs a) {
   }
 }
 
-// Joins a row's pieces, in their order, and what the pass over the prefixes has of it.
+// Joins a row's pieces, in their order.
 template <int HD>
 __global__ __launch_bounds__(256) void attn_join(KvAttnArgs a, int64_t group0) {
   constexpr int LPR = HD / 4, NG = 256 / LPR;
@@ -473,12 +556,6 @@ __global__ __launch_bounds__(256) void attn_join(KvAttnArgs a, int64_t group0) {
     }
     j.add(p, [&](int q) { return y[q]; }, in, a.c2);
   }
-  if (a.ppart) {
-    const int ds[1] = {d};
-    float4 o[1] = {j.o};
-    fold_prefix<HD, 4, 8>(a, b, kvh, r, ds, j.M, j.L, o);
-    j.o = o[0];
-  }
   const float inv = row_inverse(j.L);
   const int64_t at = int64_t(query) * a.hq + kvh * a.g + r % a.g;
   *reinterpret_cast<uint2*>(a.o + at * HD + d) = make_uint2(pack_bf2(j.o.x * inv, j.o.y * inv), pack_bf2(j.o.z * inv, j.o.w * inv));
@@ -487,7 +564,8 @@ __global__ __launch_bounds__(256) void attn_join(KvAttnArgs a, int64_t group0) {
 
 template <int HD>
 hipError_t launch_dim(const KvAttnArgs& a, hipStream_t s) {
-  const dim3 grid(unsigned(int64_t(a.blocks) * a.hkv * a.splits));
+  const int64_t each = int64_t(a.blocks) * a.hkv;
+  const dim3 grid(unsigned(a.shared ? std::max<int64_t>(a.slots, each) : each * a.splits));
   if (a.own.paged)
     hipLaunchKernelGGL((attn_many<HD, true>), grid, dim3(256), 0, s, a);
   else

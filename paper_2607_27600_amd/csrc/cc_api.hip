@@ -1301,8 +1301,8 @@ struct KvMany {
     ++n;
     blocks += nb;
   }
-  // walked: sequences there are; groups: workgroups to make by cutting; always: results are joined even if whole
-  cc_status cut(const cc_problem* p, int walked, int max_len, int groups, bool always) {
+  // walked: sequences there are
+  cc_status cut(const cc_problem* p, int walked, int max_len) {
     items.nkv = p->n_heads_kv;
     items.n_seqs = n <= ATTN_INLINE ? n : 0;
     std::stable_sort(items.seqs, items.seqs + items.n_seqs, [](const AttnSeq& x, const AttnSeq& y) { return x.blocks > y.blocks; });
@@ -1310,12 +1310,12 @@ struct KvMany {
     const int64_t each = blocks * p->n_heads_kv;
     if (!items.n_seqs) blocks = int64_t(n_tokens(p)) * (p->n_heads_q / p->n_heads_kv) / KV_ROWS + walked;
     if (blocks * p->n_heads_kv > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
-    // pieces of 256 entries at the least
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({groups / each, (int64_t(max_len) + 255) / 256,
+    // As many pieces as leave no more than two workgroups a CU, what is resident, of 256 entries at the least.
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({2 * kCus / each, (int64_t(max_len) + 255) / 256,
                                                                  MOST_GROUPS / (blocks * p->n_heads_kv)}));
     piece = std::max(KV_KEYS, int(((int64_t(max_len) + want - 1) / want + KV_KEYS - 1) / KV_KEYS * KV_KEYS));
     splits = std::max(1, int((int64_t(max_len) + piece - 1) / piece));
-    if (splits > 1 || always) {
+    if (splits > 1) {
       const size_t rows = size_t(splits) * p->n_heads_q * n_tokens(p);
       part = align_up(rows * p->head_dim * sizeof(float));
       total = part + align_up(rows * sizeof(float2));
@@ -1332,12 +1332,16 @@ struct KvPlan {
   bool direct = false;         // few rows: by 16 rows a workgroup
   int32_t list[KV_LIST];
   size_t fpart = 0, ftotal = 0;
-  KvMany many, prefix;
-  size_t total() const { return prefix.total + ftotal + many.total; }
+  KvMany many;
+  int64_t pre_blocks = 0;      // row blocks of the pass over the prefixes (0: none)
+  size_t pre_at = 0, ppart = 0, ptotal = 0;   // its workspace: where its pieces are, outputs, (maximum, sum) pairs
+  size_t total() const { return ptotal + ftotal + many.total; }
 };
 
 // What a workgroup for each 16 rows of a (sequence, KV head) is for: short calls, with nothing to join.
 constexpr int KV_SHORT = 1024;
+// Workgroups that the pass over the prefixes is cut into: two a CU.
+constexpr int KV_SLOTS = 2 * kCus;
 
 cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& c) {
   const int g = p->n_heads_q / p->n_heads_kv, hkv = p->n_heads_kv;
@@ -1369,13 +1373,17 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
     c.fpart = align_up(rows * p->head_dim * sizeof(float));
     c.ftotal = c.fpart + align_up(rows * sizeof(float2));
   }
-  CC_TRY(c.many.cut(p, p->n_seqs, max_len, 2 * kCus, false));
+  CC_TRY(c.many.cut(p, p->n_seqs, max_len));
   if (x && !c.inside) {
     for (int i = 0; i < x->n_prefixes; ++i) {
-      const int q0 = p->cu_seqlens_h[x->first_seq_h[i]], m = p->cu_seqlens_h[x->first_seq_h[i + 1]] - q0;
-      if (m) c.prefix.add(i, q0, m, g);
+      const int64_t m = p->cu_seqlens_h[x->first_seq_h[i + 1]] - p->cu_seqlens_h[x->first_seq_h[i]];
+      c.pre_blocks += (m * g + KV_ROWS - 1) / KV_ROWS;
     }
-    CC_TRY(c.prefix.cut(p, x->n_prefixes, x->max_len, kCus, true));
+    const int64_t groups = std::max<int64_t>(KV_SLOTS, c.pre_blocks * hkv);
+    if (groups > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+    c.pre_at = align_up(size_t(x->n_prefixes) * sizeof(int2));
+    c.ppart = c.pre_at + align_up(size_t(groups) * KV_ROWS * p->head_dim * sizeof(float));
+    c.ptotal = c.ppart + align_up(size_t(groups) * KV_ROWS * sizeof(float2));
   }
   // (a launch by 16 rows a workgroup of 512)
   const int64_t by16 = (c.listed ? int64_t(c.n_list) * ((c.R + 15) / 16) : walked) * hkv;
@@ -1435,20 +1443,20 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
     off += m.total;
     return launch_attn_kv_many(a, st);
   };
-  if (c.prefix.n) {
-    const KvAttnArgs own = a;
-    a.own = a.pre;
-    a.lens = a.pre_lens;
-    a.max_len = a.pre_max;
-    a.n_seqs = a.n_prefixes;
-    a.shared = 1;
-    CC_HIP(many(c.prefix));
-    const float* part = a.part;
-    const float2* part_ml = a.part_ml;
-    a = own;
-    a.ppart = part;
-    a.ppart_ml = part_ml;
-    a.ppiece = c.prefix.piece;
+  if (c.pre_blocks) {
+    a.pre_at = reinterpret_cast<int2*>(at(ws, 0));
+    a.ppart = reinterpret_cast<float*>(at(ws, c.pre_at));
+    a.ppart_ml = reinterpret_cast<float2*>(at(ws, c.ppart));
+    off = c.ptotal;
+    KvAttnArgs pass = a;
+    pass.own = a.pre;
+    pass.lens = a.pre_lens;
+    pass.max_len = a.pre_max;
+    pass.n_seqs = a.n_prefixes;
+    pass.blocks = int(c.pre_blocks);
+    pass.slots = KV_SLOTS;
+    pass.shared = 1;
+    CC_HIP(launch_attn_kv_many(pass, st));
   }
   if (c.n_few) {
     a.n_list = c.n_list;

@@ -265,3 +265,58 @@ def test_pieces(new, lens, hq, hkv, d, page):
             got.append((o, lse))
         assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
         assert (ws[size:] == 0x7f).all()
+
+
+LONG_PREFIXES = [
+    # prefix lens, first, new, lens, hq, hkv, d, page: cut into pieces on the device, two and more row blocks, few and many rows behind
+    ([5000], [0, 40], [1] * 40, [1 + 13 * i % 200 for i in range(40)], 8, 2, 128, 16),
+    ([3000, 700, 0, 1500], [0, 9, 9, 12, 30], [6, 0, 1] * 10, [6 + 29 * i % 300 for i in range(30)], 16, 4, 64, 64),
+    ([2500, 40], [0, 3, 6], [40, 200, 1, 90, 2, 64], [40, 900, 2500, 90, 3, 64], 4, 1, 128, 32),
+    ([1200], [0, 2], [1, 1], [9000, 12], 4, 1, 128, 16),             # own entries that are cut too
+    ([1100] * 70, list(range(71)), [1] * 70, [1 + i % 9 for i in range(70)], 2, 1, 64, 0),
+    ([2000], [0, 1], [700], [700], 32, 8, 64, 16),
+    ([1500], [0, 3], [700, 900, 1000], [700, 900, 1000], 16, 16, 64, 128),   # more (row block, head)s than workgroups at a time
+]
+
+
+@pytest.mark.parametrize("case", LONG_PREFIXES, ids=[str(i) for i in range(len(LONG_PREFIXES))])
+def test_long_shared_prefix(case):
+    from paper_2607_27600_amd import cc
+    pl, first, new, lens, hq, hkv, d, page = case
+    print(f"[prefix long] {case}", flush=True)
+    cache = Cache16(lens, hkv, d, page=page, seed=61, room=400)
+    pre = Cache16(pl, hkv, d, page=64 if page else 0, seed=62, room=700)
+    q = queries(new, hq, d, 63)
+    p, kv = problem(cc, new, hq, hkv, d), cache.view(cc)
+    want = _oracle(cache, q, new, lens, hq, hkv, pre=pre, first=first, pre_lens=pl)
+    for more in (0, 333):
+        x = cc.prefix(pre.view(cc), first, i32(pl), max(pl) + more)
+        size = cc.cc_attention_prefix_workspace(p, x, max(lens) + more)
+        ws = torch.full((size + 4096,), 0x7f, dtype=torch.uint8, device="cuda")
+        got = []
+        for _ in range(2):
+            o, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+            cc.cc_attention_prefix(p, q, x, kv, 0, i32(lens), max(lens) + more, o, lse=lse, workspace=ws[:size])
+            torch.cuda.synchronize()
+            _same(o, lse, want, str(more))
+            got.append((o, lse))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        assert (ws[size:] == 0x7f).all()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("n", [300, 3000])
+def test_what_is_not_finite_in_a_prefix(n, value):
+    """It reaches the rows of its run, and no others; what lies past a prefix reaches none."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d, new, lens = 4, 2, 128, [1, 40, 2, 3], [7, 40, 2, 30]
+    cache, pre = Cache16(lens, hkv, d, page=16, seed=64), Cache16([n, n - 9], hkv, d, page=16, seed=65)
+    q = queries(new, hq, d, 66)
+    kw = dict(pre=pre, first=[0, 2, 4], pre_lens=[n, n - 9])
+    clean = _oracle(cache, q, new, lens, hq, hkv, **kw)[0]
+    pre.put(0, 1, 1, "v", n - 11, 17, value)
+    o = f64(_run(cc, cache, q, new, lens, hq, hkv, **kw)[0])
+    hit = np.zeros(o.shape, bool)
+    hit[41:, 2:, 17] = True
+    np.testing.assert_array_equal(~np.isfinite(o), hit)
+    assert_attention_close(np.where(hit, 0, o), np.where(hit, 0, clean))
