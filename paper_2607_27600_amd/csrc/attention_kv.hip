@@ -337,12 +337,10 @@ __device__ __forceinline__ void load_queries(const KvAttnArgs& a, Rows<HD, NR>& 
 
 // ------------------------------------------------------------------ whole rows
 
-// One workgroup for 16 rows of a (sequence, KV head): its waves share out the entries, the prefix's and the sequence's.
-// Eight waves, so that a wave's chain of loads is short.
-constexpr int ROWS_NT = 512;
-template <int HD>
-__global__ __launch_bounds__(ROWS_NT, 2) void attn_rows(KvAttnArgs a) {
-  constexpr int ROWS = 16, NW = ROWS_NT / 64;
+// One workgroup for 16 rows of a (sequence, KV head): its NW waves share out the entries, the prefix's and the sequence's.
+template <int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_rows(KvAttnArgs a) {
+  constexpr int ROWS = 16;
   __shared__ float lds[NW * ROWS * HD];
   __shared__ float2 ml[NW * ROWS];
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
@@ -562,10 +560,13 @@ hipError_t launch_attn_few(const KvAttnArgs& a, hipStream_t s) { return a.head_d
 hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s) {
   const int64_t blocks = (a.listed ? int64_t(a.n_list) * ((a.R + 15) / 16) : int64_t(a.N) * a.g / 16 + a.n_seqs) * a.hkv;
   if (blocks > MOST_GROUPS / 2) return hipErrorInvalidValue;   // (refused by the planner)
+  // Eight waves where there is a CU for every workgroup, so that a wave's chain of loads is short.
+  const bool wide = blocks <= 256;
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(blocks)), dim3(wide ? 512 : 256), 0, s, a); };
   if (a.head_dim == 128)
-    hipLaunchKernelGGL(attn_rows<128>, dim3(unsigned(blocks)), dim3(ROWS_NT), 0, s, a);
+    wide ? launch(attn_rows<128, 8>) : launch(attn_rows<128, 4>);
   else
-    hipLaunchKernelGGL(attn_rows<64>, dim3(unsigned(blocks)), dim3(ROWS_NT), 0, s, a);
+    wide ? launch(attn_rows<64, 8>) : launch(attn_rows<64, 4>);
   return hipGetLastError();
 }
 

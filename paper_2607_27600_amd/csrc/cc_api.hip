@@ -1310,9 +1310,11 @@ struct KvMany {
     const int64_t each = blocks * p->n_heads_kv;
     if (!items.n_seqs) blocks = int64_t(n_tokens(p)) * (p->n_heads_q / p->n_heads_kv) / KV_ROWS + walked;
     if (blocks * p->n_heads_kv > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
-    // As many pieces as leave no more than two workgroups a CU, what is resident, of 256 entries at the least.
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({2 * kCus / each, (int64_t(max_len) + 255) / 256,
-                                                                 MOST_GROUPS / (blocks * p->n_heads_kv)}));
+    // As many pieces as leave no more than two workgroups a CU, what is resident, of 256 entries at the least; but only
+    // where they take some 12 tiles off a workgroup's chain, what the join costs.
+    int64_t want = std::max<int64_t>(1, std::min<int64_t>({2 * kCus / each, (int64_t(max_len) + 255) / 256,
+                                                           MOST_GROUPS / (blocks * p->n_heads_kv)}));
+    if ((int64_t(max_len) - max_len / want) / KV_KEYS <= 12) want = 1;
     piece = std::max(KV_KEYS, int(((int64_t(max_len) + want - 1) / want + KV_KEYS - 1) / KV_KEYS * KV_KEYS));
     splits = std::max(1, int((int64_t(max_len) + piece - 1) / piece));
     if (splits > 1) {
@@ -1348,7 +1350,7 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
   const int longest = int(std::min<int64_t>(INT32_MAX, int64_t(max_len) + (x ? x->max_len : 0)));
   int64_t blocks16 = 0;
   for (int b = 0; b < p->n_seqs; ++b) blocks16 += (int64_t(p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) * g + 15) / 16;
-  c.rows = longest <= KV_SHORT && blocks16 * hkv <= 512;
+  c.rows = longest <= KV_SHORT && blocks16 * hkv <= 640;
   c.inside = x && c.rows;
   for (int b = 0; b < p->n_seqs; ++b) {
     const int seq0 = p->cu_seqlens_h[b], m = p->cu_seqlens_h[b + 1] - seq0;
