@@ -69,10 +69,20 @@ struct KvWeightsArgs {
   const float* prev;           // or null: none has
   float* w;
   int64_t w_seq, w_head, prev_seq, prev_head;
-  int n_seqs, layer, max_len, hq, hkv, g, head_dim, most;   // most: most queries of a sequence
+  int n_seqs, layer, max_len, hq, hkv, g, head_dim;
   float c2;
+  // Sequences of more than W_FEW_ROWS rows: list[0 .. n_list), or (listed = 0) all there are.
+  int n_list, listed;
+  int32_t list[KV_LIST];
+  int chunk, chunks;           // rows of a chunk (a multiple of W_ROWS), chunks of the longest sequence
+  float* part;                 // sums of chunks to be added up (null: one chunk): [chunks][n_list][Hkv][max_len]
 };
-hipError_t launch_attention_weights(const KvWeightsArgs& a, hipStream_t s);
+// Rows up to which a sequence's are read by each wave for itself; beyond, in tiles that a workgroup shares.
+constexpr int W_FEW_ROWS = 64;
+constexpr int W_KEYS = 256;    // entries of a workgroup
+constexpr int W_ROWS = 64;     // rows of a tile
+hipError_t launch_weights_few(const KvWeightsArgs& a, hipStream_t s);
+hipError_t launch_weights_many(const KvWeightsArgs& a, hipStream_t s);
 
 struct WeightScoresArgs {
   const float* w;

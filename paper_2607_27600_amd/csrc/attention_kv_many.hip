@@ -81,6 +81,9 @@ struct Piece {
   int j, q0, m, len, item, nth, tiles;   // item: row block * Hkv + KV head; j < 0: none
 };
 constexpr int TILES = 4;
+// Up to that many tiles a workgroup, half as many workgroups: 40 sequences behind 16000 entries, 4 heads of 7 rows, 49.9 us in
+// place of 51.4; 64 behind 5000, 8 heads of 4, 28.3 in place of 32.2; but 24 of six tokens behind 30001 and 6000 104 for 90.
+constexpr int CHAIN = 16;
 __device__ __forceinline__ Piece piece_of(const KvAttnArgs& a, int64_t x) {
   const int lane = threadIdx.x & 63;
   const int64_t items = int64_t(a.blocks) * a.hkv;   // at least those there are
@@ -109,7 +112,10 @@ __device__ __forceinline__ Piece piece_of(const KvAttnArgs& a, int64_t x) {
       all += (int64_t(__builtin_amdgcn_readlane(wave_scan(int(mine >> 16)), 63)) << 16) +
              __builtin_amdgcn_readlane(wave_scan(int(mine & 0xffff)), 63);
     }
-    tiles = int(min(int64_t(tiles), max(int64_t(TILES), (all + a.slots - items - 1) / (a.slots - items))));
+    auto per = [&](int64_t groups) { return max(int64_t(TILES), (all + groups - 1) / groups); };
+    // (one workgroup a CU, with half the results to pass on, while that is a chain of few tiles)
+    const int half = a.slots / 2;
+    tiles = int(min(int64_t(tiles), items < half && per(half - items) <= CHAIN ? per(half - items) : per(a.slots - items)));
   }
   Piece p{-1, 0, 0, 0, 0, 0, tiles};
   int64_t start = 0;

@@ -1476,6 +1476,47 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
   return CC_OK;
 }
 
+// How a call's sequences of many rows are cut.
+struct WeightsPlan {
+  bool few = false;            // there are sequences of few rows, or without any
+  int n = 0, n_list = 0, listed = 0, chunk = W_ROWS, chunks = 1;
+  int32_t list[KV_LIST];
+  size_t total = 0;
+};
+
+cc_status weights_plan(const cc_problem* p, int max_len, WeightsPlan& c) {
+  const int g = p->n_heads_q / p->n_heads_kv, hkv = p->n_heads_kv;
+  int64_t most = 0, tiles = 0;
+  const int64_t blocks = (int64_t(max_len) + W_KEYS - 1) / W_KEYS;
+  for (int b = 0; b < p->n_seqs; ++b) {
+    const int64_t rows = int64_t(p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) * g;
+    if (rows <= W_FEW_ROWS) {
+      c.few = true;
+      continue;
+    }
+    if (c.n < KV_LIST) c.list[c.n] = b;
+    ++c.n;
+    most = std::max(most, rows);
+    tiles += (rows + W_ROWS - 1) / W_ROWS * blocks * hkv;
+  }
+  const int64_t few = (int64_t(max_len) + 127) / 128 * hkv * p->n_seqs;
+  if (c.few && few > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+  if (c.n == 0) return CC_OK;
+  c.listed = c.n <= KV_LIST;
+  c.n_list = c.listed ? c.n : p->n_seqs;
+  const int64_t planes = int64_t(c.n_list) * hkv;
+  if (blocks * planes > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+  // Chunks of an eighth of what each of three workgroups a CU would have if all were seen by all, of eight tiles at the
+  // least; as many as a launch and 2^28 bytes of sums have room for.
+  int64_t each = std::max<int64_t>(8, tiles / (8 * 3 * kCus));
+  const int64_t room = std::max<int64_t>(1, std::min(MOST_GROUPS / (blocks * planes), (int64_t(1) << 26) / (planes * std::max(max_len, 1))));
+  each = std::max(each, ((most + W_ROWS - 1) / W_ROWS + room - 1) / room);
+  c.chunk = int(std::min<int64_t>(each * W_ROWS, INT32_MAX / W_ROWS * W_ROWS));
+  c.chunks = int((most + c.chunk - 1) / c.chunk);
+  if (c.chunks > 1) c.total = align_up(size_t(c.chunks) * planes * max_len * sizeof(float));
+  return CC_OK;
+}
+
 // written: each (sequence, KV head) needs a place of its own.
 cc_status check_weights(const cc_problem* p, const cc_weights* w, bool written) {
   if (!w || !w->base) return CC_ERR_ARG;
@@ -1525,7 +1566,9 @@ cc_status cc_attention_prefix(const cc_problem* p, const void* q, const cc_prefi
 cc_status cc_attention_weights_workspace(const cc_problem* p, int32_t max_kv_len, size_t* bytes) {
   if (!bytes) return CC_ERR_ARG;
   CC_TRY(check_attention_kv(p, max_kv_len));
-  *bytes = 0;
+  WeightsPlan c;
+  CC_TRY(weights_plan(p, max_kv_len, c));
+  *bytes = c.total;
   return CC_OK;
 }
 
@@ -1541,7 +1584,9 @@ cc_status cc_attention_weights(const cc_problem* p, const void* q, const cc_kv* 
   if (!prev && prev_lens) return CC_ERR_ARG;
   const int N = n_tokens(p);
   if (!kv_lens || (N > 0 && (!q || !lse || !aligned16(q)))) return CC_ERR_ARG;
-  CC_TRY(check_ws(ws, ws_bytes, 0));
+  WeightsPlan c;
+  CC_TRY(weights_plan(p, max_kv_len, c));
+  CC_TRY(check_ws(ws, ws_bytes, c.total));
   if (max_kv_len == 0) return CC_OK;
   KvWeightsArgs a{};
   a.q = static_cast<const u16*>(q);
@@ -1565,9 +1610,16 @@ cc_status cc_attention_weights(const cc_problem* p, const void* q, const cc_kv* 
   a.hkv = p->n_heads_kv;
   a.g = p->n_heads_q / p->n_heads_kv;
   a.head_dim = p->head_dim;
-  a.most = max_len(p);
   a.c2 = softmax_scale(p) * kLog2e;
-  CC_HIP(launch_attention_weights(a, static_cast<hipStream_t>(stream)));
+  a.n_list = c.n_list;
+  a.listed = c.listed;
+  std::copy_n(c.list, c.listed ? c.n : 0, a.list);
+  a.chunk = c.chunk;
+  a.chunks = c.chunks;
+  a.part = c.total ? static_cast<float*>(ws) : nullptr;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (c.few) CC_HIP(launch_weights_few(a, st));
+  if (c.n) CC_HIP(launch_weights_many(a, st));
   return CC_OK;
 }
 

@@ -5,7 +5,8 @@
 // A wave holds 16 KB entries of a (sequence, KV head) as the A operands of 16x16x32 MFMA and takes the rows
 // (query, head of the group) that see them 16 at a time.  A lane then holds four entries of one row, so the sum
 // over rows stays in its registers until the end, where 16 lanes are added up: no atomics, one order.
-// Products and sums are fp32.
+// Products and sums are fp32.  Sequences of few rows (single tokens, drafts) are bound by the bytes of their keys, those of
+// many by the matrix instructions and exponentials of every (row, entry) pair.
 #include <algorithm>
 
 #include "attention_kv.h"
@@ -15,12 +16,29 @@ namespace {
 
 constexpr int NT = 256, NW = NT / 64;
 
-__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+// Over the 16 lanes of an entry.
+__device__ __forceinline__ float row_sum(float x) {
+#pragma unroll
+  for (int off = 1; off < 16; off <<= 1) x += __shfl_xor(x, off);
+  return x;
 }
 
+// The weights of a (sequence, KV head): what came of a call, added to what entries had.
+struct Total {
+  float* w;
+  const float* prev;
+  int had;
+  __device__ __forceinline__ Total(const KvWeightsArgs& a, int b, int kvh, int len)
+      : w(a.w + int64_t(b) * a.w_seq + int64_t(kvh) * a.w_head),
+        prev(a.prev + int64_t(b) * a.prev_seq + int64_t(kvh) * a.prev_head),
+        had(a.prev ? (a.prev_lens ? a.prev_lens[b] : len) : 0) {}
+  __device__ __forceinline__ void put(int t, float x) const { w[t] = t < had ? prev[t] + x : x; }
+};
+
+// ------------------------------------------------------------------ few rows
+
 template <int HD, int KB>
-__global__ __launch_bounds__(NT, 2) void attn_weights(KvWeightsArgs a) {
+__global__ __launch_bounds__(NT, 2) void weights_few(KvWeightsArgs a) {
   constexpr int NKS = HD / 32;
   const int tid = threadIdx.x, lane = tid & 63, grp = lane >> 4, r16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -31,6 +49,7 @@ __global__ __launch_bounds__(NT, 2) void attn_weights(KvWeightsArgs a) {
   const int len = min(max(a.lens[b], 0), a.max_len);
   if (t0 >= len) return;
   const int q0 = a.cu[b], mq = a.cu[b + 1] - q0, rows = mq * a.g, shift = len - mq;
+  if (rows > W_FEW_ROWS) return;
   const KvPlane P = kv_plane(a.own, b, a.layer, kvh);
 
   float sum[KB][4];
@@ -86,19 +105,186 @@ __global__ __launch_bounds__(NT, 2) void attn_weights(KvWeightsArgs a) {
       }
     }
   }
-  const int had = a.prev ? (a.prev_lens ? a.prev_lens[b] : len) : 0;
-  float* w = a.w + int64_t(b) * a.w_seq + int64_t(kvh) * a.w_head;
-  const float* prev = a.prev + int64_t(b) * a.prev_seq + int64_t(kvh) * a.prev_head;
+  const Total to(a, b, kvh, len);
 #pragma unroll
   for (int k = 0; k < KB; ++k)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      float x = sum[k][e];
-#pragma unroll
-      for (int off = 1; off < 16; off <<= 1) x += __shfl_xor(x, off);
+      const float x = row_sum(sum[k][e]);
       const int t = t0 + 16 * k + 4 * grp + e;
-      if (r16 == 0 && t < len) w[t] = t < had ? prev[t] + x : x;
+      if (r16 == 0 && t < len) to.put(t, x);
     }
+}
+
+// ------------------------------------------------------------------ many rows
+
+// 16 bytes a lane from a lane's address into LDS at lds + 16 * lane, by the wave; waited for by the caller.
+__device__ __forceinline__ void dma16(const char* vaddr, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(vaddr), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(p)));
+}
+
+// One workgroup for W_KEYS entries of a (sequence, KV head) and a chunk of the rows: 64 entries a wave, which stay in its
+// registers, and tiles of W_ROWS rows that go from memory straight into LDS, two buffers, one barrier a tile.
+template <int HD>
+__global__ __launch_bounds__(NT, 2) void weights_many(KvWeightsArgs a) {
+  constexpr int KB = 4, NKS = HD / 32, CPR = HD / 8, ROWB = HD * 2;
+  constexpr int RPW = 64 / CPR, NI = W_ROWS / (NW * RPW);   // rows of a wave's load, loads of a wave and tile
+  __shared__ __attribute__((aligned(1024))) u16 tile[2][W_ROWS * HD];
+  auto swz = [](int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; };
+  const int tid = threadIdx.x, lane = tid & 63, grp = lane >> 4, r16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const unsigned blocks = unsigned(a.max_len + W_KEYS - 1) / W_KEYS;
+  unsigned x = blockIdx.x;
+  const int kvh = int(x % unsigned(a.hkv));
+  x /= unsigned(a.hkv);
+  const int chunk = int(x % unsigned(a.chunks));
+  x /= unsigned(a.chunks);
+  const int j = int(x / blocks), b = a.listed ? a.list[j] : j, first = int(x % blocks) * W_KEYS;
+  const int len = min(max(a.lens[b], 0), a.max_len);
+  const int q0 = a.cu[b], mq = a.cu[b + 1] - q0, rows = mq * a.g, shift = len - mq;
+  if (rows <= W_FEW_ROWS || first >= len) return;
+  const int from = min(max(0, first - shift), mq) * a.g;          // the first row that sees an entry
+  const int r_lo = max(from, chunk * a.chunk) / W_ROWS * W_ROWS;  // this chunk's: whole tiles of the sequence
+  const int r_hi = int(min(int64_t(rows), int64_t(chunk + 1) * a.chunk));
+  // (a chunk that sees nothing is not added up; the only one writes what there was)
+  if (r_lo >= r_hi && a.part) return;
+  const int t0 = first + wave * KB * 16;
+  const KvPlane P = kv_plane(a.own, b, a.layer, kvh);
+
+  float sum[KB][4];
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[k][e] = 0.f;
+  if (r_lo < r_hi) {
+    bf16x8 kf[KB][NKS];
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+      const int t = min(t0 + 16 * k + r16, len - 1), gg = t >> 4;
+      const char* p = P.k + P.offset(P.page(gg), 16 * gg) + int64_t(t & 15) * P.ts + 16 * grp;
+#pragma unroll
+      for (int s = 0; s < NKS; ++s) kf[k][s] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 64 * s));
+    }
+    // rows that this wave's entries are seen by begin here, and those that see all of them
+    const int mine = min(max(0, t0 - shift), mq) * a.g, all = min(max(0, t0 + KB * 16 - 1 - shift), mq) * a.g;
+    const int di = W_ROWS / a.g, dh = W_ROWS % a.g;
+    struct Row {   // of the sequence, a tile apart
+      int i, h;
+    };
+    auto row_at = [&](int r) { return Row{r / a.g, r % a.g}; };
+    auto next = [&](Row& r) {
+      r.i += di;
+      r.h += dh;
+      if (r.h >= a.g) {
+        r.h -= a.g;
+        ++r.i;
+      }
+    };
+    auto index = [&](const Row& r) { return int64_t(q0 + min(r.i, mq - 1)) * a.hq + kvh * a.g + r.h; };
+    Row ld[NI], ls[W_ROWS / 16];   // rows of the lane's loads, and of its log-sum-exps
+    int ch[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = (i * NW + wave) * RPW + lane / CPR;
+      ld[i] = row_at(r_lo + r);
+      ch[i] = ((lane % CPR) ^ swz(r)) * 16;
+    }
+#pragma unroll
+    for (int n = 0; n < W_ROWS / 16; ++n) ls[n] = row_at(r_lo + 16 * n + r16);
+    float lse[W_ROWS / 16], lse_n[W_ROWS / 16];
+    auto load = [&](int buf) {   // the next tile
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        dma16(reinterpret_cast<const char*>(a.q) + index(ld[i]) * ROWB + ch[i], lds_addr(tile[buf] + (i * NW + wave) * RPW * HD));
+        next(ld[i]);
+      }
+    };
+    load(0);
+#pragma unroll
+    for (int n = 0; n < W_ROWS / 16; ++n) lse_n[n] = a.lse[index(ls[n])];
+    int buf = 0;
+    for (int r0 = r_lo; r0 < r_hi; r0 += W_ROWS, buf ^= 1) {
+      int at[W_ROWS / 16];
+      __builtin_amdgcn_s_waitcnt(0);   // this wave's part of the tile has landed
+      __syncthreads();                 // everyone's, and everyone is done with the other buffer
+      const bool more = r0 + W_ROWS < r_hi;
+      if (more) load(buf ^ 1);
+#pragma unroll
+      for (int n = 0; n < W_ROWS / 16; ++n) {
+        at[n] = ls[n].i;
+        lse[n] = lse_n[n];
+        next(ls[n]);
+        if (more) lse_n[n] = a.lse[index(ls[n])];
+      }
+      if (r0 + W_ROWS <= mine) continue;
+      const bool masked = r0 < all || r0 + W_ROWS > r_hi;
+#pragma unroll
+      for (int n = 0; n < W_ROWS / 16; ++n) {
+        f32x4 z[KB];
+#pragma unroll
+        for (int k = 0; k < KB; ++k) z[k] = f32x4{};
+#pragma unroll
+        for (int s = 0; s < NKS; ++s) {
+          const int r = 16 * n + r16;
+          const bf16x8 qf = as_bf16x8(*reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(tile[buf]) + r * ROWB +
+                                                                      (((4 * s + grp) ^ swz(r)) * 16)));
+#pragma unroll
+          for (int k = 0; k < KB; ++k) z[k] = mfma16(kf[k][s], qf, z[k]);
+        }
+        const float l2 = lse[n] * kLog2e;
+        if (masked) {
+          const bool in = r0 + 16 * n + r16 < r_hi;
+#pragma unroll
+          for (int k = 0; k < KB; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (in && t0 + 16 * k + 4 * grp + e <= shift + at[n]) sum[k][e] += fast_exp2(fmaf(z[k][e], a.c2, -l2));
+        } else {
+#pragma unroll
+          for (int k = 0; k < KB; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[k][e] += fast_exp2(fmaf(z[k][e], a.c2, -l2));
+        }
+      }
+    }
+  }
+  const Total to(a, b, kvh, len);
+  float* part = a.part ? a.part + ((int64_t(chunk) * a.n_list + j) * a.hkv + kvh) * a.max_len : nullptr;
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float y = row_sum(sum[k][e]);
+      const int t = t0 + 16 * k + 4 * grp + e;
+      if (r16 == 0 && t < len) {
+        if (part)
+          part[t] = y;
+        else
+          to.put(t, y);
+      }
+    }
+}
+
+// Adds up the chunks of an entry, in their order.
+__global__ __launch_bounds__(NT) void add_chunks(KvWeightsArgs a, int blocks) {
+  unsigned x = blockIdx.x;
+  const int t = int(x % unsigned(blocks)) * NT + int(threadIdx.x);
+  x /= unsigned(blocks);
+  const int kvh = int(x % unsigned(a.hkv)), j = int(x / unsigned(a.hkv)), b = a.listed ? a.list[j] : j;
+  const int len = min(max(a.lens[b], 0), a.max_len);
+  const int mq = a.cu[b + 1] - a.cu[b], rows = mq * a.g, shift = len - mq;
+  if (rows <= W_FEW_ROWS || t >= len) return;
+  // what its workgroup's entries are seen by
+  const int from = min(max(0, t / W_KEYS * W_KEYS - shift), mq) * a.g;
+  const float* part = a.part + (int64_t(j) * a.hkv + kvh) * a.max_len + t;
+  const int64_t step = int64_t(a.n_list) * a.hkv * a.max_len;
+  float y = 0.f;
+  if (from < rows)
+    for (int c = from / a.chunk; c <= (rows - 1) / a.chunk; ++c) y += part[c * step];
+  Total(a, b, kvh, len).put(t, y);
 }
 
 __global__ __launch_bounds__(NT) void weight_scores(WeightScoresArgs a, int blocks) {
@@ -153,14 +339,29 @@ __global__ __launch_bounds__(MOVE_NT) void move_weights(CompactWeightsArgs a, We
 
 }  // namespace
 
-hipError_t launch_attention_weights(const KvWeightsArgs& a, hipStream_t s) {
+hipError_t launch_weights_few(const KvWeightsArgs& a, hipStream_t s) {
   constexpr int KB = 2;
   const int64_t blocks = (int64_t(a.max_len) + NW * KB * 16 - 1) / (NW * KB * 16) * a.hkv * a.n_seqs;
-  if (blocks > MOST_GROUPS) return hipErrorInvalidValue;
+  if (blocks > MOST_GROUPS) return hipErrorInvalidValue;   // (refused by the planner)
   if (a.head_dim == 128)
-    hipLaunchKernelGGL((attn_weights<128, KB>), dim3(unsigned(blocks)), dim3(NT), 0, s, a);
+    hipLaunchKernelGGL((weights_few<128, KB>), dim3(unsigned(blocks)), dim3(NT), 0, s, a);
   else
-    hipLaunchKernelGGL((attn_weights<64, KB>), dim3(unsigned(blocks)), dim3(NT), 0, s, a);
+    hipLaunchKernelGGL((weights_few<64, KB>), dim3(unsigned(blocks)), dim3(NT), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_weights_many(const KvWeightsArgs& a, hipStream_t s) {
+  const int64_t planes = int64_t(a.n_list) * a.hkv;
+  const int64_t grid = (int64_t(a.max_len) + W_KEYS - 1) / W_KEYS * a.chunks * planes;
+  if (grid > MOST_GROUPS) return hipErrorInvalidValue;     // (refused by the planner)
+  if (a.head_dim == 128)
+    hipLaunchKernelGGL(weights_many<128>, dim3(unsigned(grid)), dim3(NT), 0, s, a);
+  else
+    hipLaunchKernelGGL(weights_many<64>, dim3(unsigned(grid)), dim3(NT), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.part) return e;
+  const int blocks = (a.max_len + NT - 1) / NT;
+  hipLaunchKernelGGL(add_chunks, dim3(unsigned(blocks * planes)), dim3(NT), 0, s, a, blocks);
   return hipGetLastError();
 }
 

@@ -216,3 +216,34 @@ def test_the_cycle_of_eviction(per_head):
                 at = kept[b * hkv + c] if per_head else kept[b]
                 host[b][c] = {name: x[at] for name, x in host[b][c].items()}
         n = J
+
+
+@pytest.mark.parametrize("new,lens,hq,hkv,d,page", [([3000], [3000], 28, 4, 128, 16), ([1, 2100, 64, 700], [5, 2500, 9000, 700], 4, 1, 64, 32),
+                                                    ([500] * 3, [500, 6000, 501], 8, 1, 128, 0), ([100] * 70, [100 + i for i in range(70)], 4, 2, 64, 16),
+                                                    ([17], [30], 8, 2, 128, 16), ([300], [100], 8, 2, 64, 16), ([40, 65, 1], [900, 900, 900], 256, 2, 64, 64)])
+def test_weights_in_chunks(new, lens, hq, hkv, d, page):
+    """Many rows: tiles that a workgroup shares, chunks that are added up, beside sequences of few; the workspace holds no
+    more than asked for, and the same call repeats bit for bit."""
+    from paper_2607_27600_amd import cc
+    print(f"[weights chunks] {new} {lens} {hq} {hkv} {d}", flush=True)
+    cache = Cache16(lens, hkv, d, page=page, seed=71, room=300)
+    q = queries(new, hq, d, 72)
+    lse, want, tol = _oracle(cache, q, new, lens, hq, hkv)
+    p, n = problem(cc, new, hq, hkv, d), max(lens)
+    prev = torch.rand(len(new), hkv, n, generator=torch.Generator().manual_seed(73)).cuda() * 4
+    for longest in (n, n + 300):
+        size = cc.cc_attention_weights_workspace(p, longest)
+        ws = torch.full((size + 4096,), 0x7f, dtype=torch.uint8, device="cuda")
+        got = []
+        for _ in range(2):
+            out = torch.full((len(new), hkv, longest), 7.0, device="cuda")
+            cc.cc_attention_weights(p, q, cache.view(cc), 0, i32(lens), longest, torch.from_numpy(lse).cuda(), out, prev=prev,
+                                    prev_lens=i32(lens), workspace=ws[:size])
+            torch.cuda.synchronize()
+            got.append(out)
+        assert torch.equal(*got) and (ws[size:] == 0x7f).all()
+        for b, m in enumerate(lens):
+            ref = f64(prev)[b, :, :m] + want[b, :, :m]
+            err = np.abs(f64(got[0])[b, :, :m] - ref)
+            assert np.all(err <= tol[b, :, :m] + 2.0 ** -24 * np.abs(ref)), (longest, b, err.max())
+            assert (got[0][b, :, m:] == 7).all()
