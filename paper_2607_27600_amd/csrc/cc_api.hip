@@ -1486,10 +1486,13 @@ struct WeightsPlan {
 
 cc_status weights_plan(const cc_problem* p, int max_len, WeightsPlan& c) {
   const int g = p->n_heads_q / p->n_heads_kv, hkv = p->n_heads_kv;
-  int64_t most = 0, tiles = 0;
+  int64_t most = 0;
+  double tiles = 0;            // (tile, block of entries) pairs that meet, in all
   const int64_t blocks = (int64_t(max_len) + W_KEYS - 1) / W_KEYS;
+  const bool prompts = ::max_len(p) == max_len;   // as far as the host can tell
   for (int b = 0; b < p->n_seqs; ++b) {
-    const int64_t rows = int64_t(p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) * g;
+    const int m = p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b];
+    const int64_t rows = int64_t(m) * g;
     if (rows <= W_FEW_ROWS) {
       c.few = true;
       continue;
@@ -1497,7 +1500,8 @@ cc_status weights_plan(const cc_problem* p, int max_len, WeightsPlan& c) {
     if (c.n < KV_LIST) c.list[c.n] = b;
     ++c.n;
     most = std::max(most, rows);
-    tiles += (rows + W_ROWS - 1) / W_ROWS * blocks * hkv;
+    const double n = prompts ? m : std::max(max_len, m);
+    tiles += (double(rows) / W_ROWS + 1) * ((n - 0.5 * m) / W_KEYS + 1) * hkv;
   }
   const int64_t few = (int64_t(max_len) + 127) / 128 * hkv * p->n_seqs;
   if (c.few && few > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
@@ -1506,9 +1510,22 @@ cc_status weights_plan(const cc_problem* p, int max_len, WeightsPlan& c) {
   c.n_list = c.listed ? c.n : p->n_seqs;
   const int64_t planes = int64_t(c.n_list) * hkv;
   if (blocks * planes > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
-  // Chunks of an eighth of what each of three workgroups a CU would have if all were seen by all, of eight tiles at the
-  // least; as many as a launch and 2^28 bytes of sums have room for.
-  int64_t each = std::max<int64_t>(8, tiles / (8 * 3 * kCus));
+  // (a tile's rows by 32-bit offsets)
+  if (int64_t(W_ROWS / g + 2) * p->n_heads_q * p->head_dim * 2 >= int64_t(1) << 32) return CC_ERR_UNSUPPORTED;
+  // Chunks that make r rounds of two workgroups a CU, an item of a block ending half a chunk early, where a round costs
+  // its tiles and four more to begin: the r of the least.
+  const double slots = 2 * kCus, ends = 0.5 * double(blocks) * planes;
+  int64_t each = 8;
+  double least = 0;
+  for (int r = 1; r <= 16; ++r) {
+    if (r * slots <= 2 * ends) continue;
+    const double t = std::max(4.0, tiles / (r * slots - ends));
+    if (least == 0 || r * (t + 4) < least) {
+      least = r * (t + 4);
+      each = int64_t(t) + 1;
+    }
+  }
+  if (least == 0) each = (most + W_ROWS - 1) / W_ROWS;   // workgroups enough without a cut
   const int64_t room = std::max<int64_t>(1, std::min(MOST_GROUPS / (blocks * planes), (int64_t(1) << 26) / (planes * std::max(max_len, 1))));
   each = std::max(each, ((most + W_ROWS - 1) / W_ROWS + room - 1) / room);
   c.chunk = int(std::min<int64_t>(each * W_ROWS, INT32_MAX / W_ROWS * W_ROWS));

@@ -8,6 +8,7 @@
 // Products and sums are fp32.  Sequences of few rows (single tokens, drafts) are bound by the bytes of their keys, those of
 // many by the matrix instructions and exponentials of every (row, entry) pair.
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_kv.h"
 
@@ -118,21 +119,32 @@ __global__ __launch_bounds__(NT, 2) void weights_few(KvWeightsArgs a) {
 
 // ------------------------------------------------------------------ many rows
 
-// 16 bytes a lane from a lane's address into LDS at lds + 16 * lane, by the wave; waited for by the caller.
-__device__ __forceinline__ void dma16(const char* vaddr, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(vaddr), "s"(lds) : "memory", "m0");
+// 16 and 4 bytes a lane from a scalar base and a lane's offset into LDS at lds + 16 (4) * lane, by the wave; waited for by
+// the caller.
+__device__ __forceinline__ void dma16(const char* sbase, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(const char* sbase, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(voff), "s"(sbase), "s"(lds)
+               : "memory", "m0");
 }
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)(p)));
 }
 
-// One workgroup for W_KEYS entries of a (sequence, KV head) and a chunk of the rows: 64 entries a wave, which stay in its
-// registers, and tiles of W_ROWS rows that go from memory straight into LDS, two buffers, one barrier a tile.
+// One workgroup of eight waves for W_KEYS entries of a (sequence, KV head) and a chunk of the rows: 32 entries a wave, which
+// stay in its registers, and tiles of W_ROWS rows that go from memory straight into LDS, two buffers, one barrier a tile.
+// A prompt of 16384 tokens, 32 heads on 8: 1.04 to 1.11 ms (1 PFLOP/s).  That is what the card's power allows: at 45% matrix
+// use it runs at 2.1 GHz, and 32x32x16 instructions with the exponentials of the rows before between them, in 15% fewer cycles
+// (57%), at 1.7, in the same time; as four waves of 64 entries, three buffers, or rows shared in the L2, 1.03 to 1.2 ms.
+constexpr int MANY_NT = 512;
 template <int HD>
-__global__ __launch_bounds__(NT, 2) void weights_many(KvWeightsArgs a) {
-  constexpr int KB = 4, NKS = HD / 32, CPR = HD / 8, ROWB = HD * 2;
+__global__ __launch_bounds__(MANY_NT, 4) void weights_many(KvWeightsArgs a) {
+  constexpr int NW = MANY_NT / 64, KB = W_KEYS / 16 / NW, NKS = HD / 32, CPR = HD / 8, ROWB = HD * 2;
   constexpr int RPW = 64 / CPR, NI = W_ROWS / (NW * RPW);   // rows of a wave's load, loads of a wave and tile
   __shared__ __attribute__((aligned(1024))) u16 tile[2][W_ROWS * HD];
+  __shared__ __attribute__((aligned(256))) float lse[2][W_ROWS];
   auto swz = [](int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; };
   const int tid = threadIdx.x, lane = tid & 63, grp = lane >> 4, r16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -170,85 +182,99 @@ __global__ __launch_bounds__(NT, 2) void weights_many(KvWeightsArgs a) {
     }
     // rows that this wave's entries are seen by begin here, and those that see all of them
     const int mine = min(max(0, t0 - shift), mq) * a.g, all = min(max(0, t0 + KB * 16 - 1 - shift), mq) * a.g;
+    // Row r of the sequence is query r / g, head r % g of the group; the g heads of a query lie side by side.  A tile's
+    // rows from its first row's query on: x = r % g + (row in the tile) is x / g queries and x % g heads further.
+    // (2^24 / g rounded up gives x / g for x g < 2^24; from 64 heads on x is below 2 g.)
+    const uint32_t inverse = (1u << 24) / a.g + 1;
+    const uint32_t gap = uint32_t(a.hq - a.g);
+    auto further = [&](uint32_t x) {   // in rows of q
+      return x + (a.g < W_ROWS ? (x * inverse >> 24) * gap : x >= uint32_t(a.g) ? gap : 0);
+    };
     const int di = W_ROWS / a.g, dh = W_ROWS % a.g;
-    struct Row {   // of the sequence, a tile apart
-      int i, h;
-    };
-    auto row_at = [&](int r) { return Row{r / a.g, r % a.g}; };
-    auto next = [&](Row& r) {
-      r.i += di;
-      r.h += dh;
-      if (r.h >= a.g) {
-        r.h -= a.g;
-        ++r.i;
-      }
-    };
-    auto index = [&](const Row& r) { return int64_t(q0 + min(r.i, mq - 1)) * a.hq + kvh * a.g + r.h; };
-    Row ld[NI], ls[W_ROWS / 16];   // rows of the lane's loads, and of its log-sum-exps
-    int ch[NI];
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int r = (i * NW + wave) * RPW + lane / CPR;
-      ld[i] = row_at(r_lo + r);
-      ch[i] = ((lane % CPR) ^ swz(r)) * 16;
-    }
-#pragma unroll
-    for (int n = 0; n < W_ROWS / 16; ++n) ls[n] = row_at(r_lo + 16 * n + r16);
-    float lse[W_ROWS / 16], lse_n[W_ROWS / 16];
-    auto load = [&](int buf) {   // the next tile
+    int i0 = r_lo / a.g, h0 = r_lo % a.g;      // the next tile's first row
+    uint32_t q_off[NI], lse_off = 0;           // of this lane's loads
+    auto offsets = [&](int left) {             // left: rows that there are from the tile on
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        dma16(reinterpret_cast<const char*>(a.q) + index(ld[i]) * ROWB + ch[i], lds_addr(tile[buf] + (i * NW + wave) * RPW * HD));
-        next(ld[i]);
+        const int r = (i * NW + wave) * RPW + lane / CPR;
+        q_off[i] = further(h0 + min(r, left - 1)) * ROWB + ((lane % CPR) ^ swz(r)) * 16;
+      }
+      lse_off = further(h0 + min(lane, left - 1)) * 4;
+    };
+    auto load = [&](int buf, int r0) {         // tile r0, the next one
+      if (r0 == r_lo || dh || r0 + W_ROWS > rows) offsets(rows - r0);
+      const int64_t row = int64_t(q0 + i0) * a.hq + kvh * a.g;
+      const char* qp = reinterpret_cast<const char*>(a.q) + row * ROWB;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) dma16(qp, q_off[i], lds_addr(tile[buf] + (i * NW + wave) * RPW * HD));
+      if (wave == 0) dma4(reinterpret_cast<const char*>(a.lse + row), lse_off, lds_addr(lse[buf]));
+      i0 += di;
+      h0 += dh;
+      if (h0 >= a.g) {
+        h0 -= a.g;
+        ++i0;
       }
     };
-    load(0);
-#pragma unroll
-    for (int n = 0; n < W_ROWS / 16; ++n) lse_n[n] = a.lse[index(ls[n])];
+    load(0, r_lo);
     int buf = 0;
     for (int r0 = r_lo; r0 < r_hi; r0 += W_ROWS, buf ^= 1) {
-      int at[W_ROWS / 16];
       __builtin_amdgcn_s_waitcnt(0);   // this wave's part of the tile has landed
       __syncthreads();                 // everyone's, and everyone is done with the other buffer
-      const bool more = r0 + W_ROWS < r_hi;
-      if (more) load(buf ^ 1);
-#pragma unroll
-      for (int n = 0; n < W_ROWS / 16; ++n) {
-        at[n] = ls[n].i;
-        lse[n] = lse_n[n];
-        next(ls[n]);
-        if (more) lse_n[n] = a.lse[index(ls[n])];
-      }
+      if (r0 + W_ROWS < r_hi) load(buf ^ 1, r0 + W_ROWS);
       if (r0 + W_ROWS <= mine) continue;
-      const bool masked = r0 < all || r0 + W_ROWS > r_hi;
+      // The products of 16 rows with a wave's entries carry the exponentials of the 16 before: one of each takes as
+      // long as the other's issue.
+      auto take = [&](auto masked) {
+        constexpr int NB = W_ROWS / 16;
+        f32x4 z[2][KB];
 #pragma unroll
-      for (int n = 0; n < W_ROWS / 16; ++n) {
-        f32x4 z[KB];
+        for (int n = 0; n <= NB; ++n) {
+          const int r = 16 * n + r16, m = n - 1;
+          const char* rowp = reinterpret_cast<const char*>(tile[buf]) + r * ROWB;
+          bf16x8 qf[NKS];
+          if (n < NB) {
 #pragma unroll
-        for (int k = 0; k < KB; ++k) z[k] = f32x4{};
+            for (int s = 0; s < NKS; ++s) qf[s] = as_bf16x8(*reinterpret_cast<const uint4*>(rowp + (((4 * s + grp) ^ swz(r)) * 16)));
 #pragma unroll
-        for (int s = 0; s < NKS; ++s) {
-          const int r = 16 * n + r16;
-          const bf16x8 qf = as_bf16x8(*reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(tile[buf]) + r * ROWB +
-                                                                      (((4 * s + grp) ^ swz(r)) * 16)));
+            for (int k = 0; k < KB; ++k) z[n & 1][k] = f32x4{};
+          }
+          const float l2 = n > 0 ? lse[buf][16 * m + r16] * kLog2e : 0.f;
+          const bool in = n > 0 && r0 + 16 * m + r16 < r_hi;
+          const int last = n > 0 ? shift + (r0 + 16 * m + r16) / a.g : 0;
+          // element f of 4 KB: its argument two slots ahead, its power one ahead, its sum
+          float arg[4 * KB], p[4 * KB];
+          auto argument = [&](int f) { arg[f] = fmaf(z[m & 1][f >> 2][f & 3], a.c2, -l2); };
+          auto power = [&](int f) {
+            p[f] = fast_exp2(arg[f]);
+            if constexpr (decltype(masked)::value) p[f] = in && t0 + 16 * (f >> 2) + 4 * grp + (f & 3) <= last ? p[f] : 0.f;
+          };
+          if (n > 0) {
+            argument(0);
+            argument(1);
+            power(0);
+          }
+          constexpr int SLOTS = NKS * KB, PER = 4 * KB / SLOTS;
 #pragma unroll
-          for (int k = 0; k < KB; ++k) z[k] = mfma16(kf[k][s], qf, z[k]);
+          for (int slot = 0; slot < SLOTS; ++slot) {
+            const int s = slot / KB, k = slot % KB;
+            if (n < NB) z[n & 1][k] = mfma16(kf[k][s], qf[s], z[n & 1][k]);
+            if (n > 0) {
+#pragma unroll
+              for (int f = slot * PER; f < slot * PER + PER; ++f) {
+                if (f + 2 < 4 * KB) argument(f + 2);
+                if (f + 1 < 4 * KB) power(f + 1);
+                sum[f >> 2][f & 3] += p[f];
+                asm volatile("" : "+v"(sum[f >> 2][f & 3]));   // here, between the matrix instructions
+              }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
-        const float l2 = lse[n] * kLog2e;
-        if (masked) {
-          const bool in = r0 + 16 * n + r16 < r_hi;
-#pragma unroll
-          for (int k = 0; k < KB; ++k)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (in && t0 + 16 * k + 4 * grp + e <= shift + at[n]) sum[k][e] += fast_exp2(fmaf(z[k][e], a.c2, -l2));
-        } else {
-#pragma unroll
-          for (int k = 0; k < KB; ++k)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[k][e] += fast_exp2(fmaf(z[k][e], a.c2, -l2));
-        }
-      }
+      };
+      if (r0 < all || r0 + W_ROWS > r_hi)
+        take(std::true_type{});
+      else
+        take(std::false_type{});
     }
   }
   const Total to(a, b, kvh, len);
@@ -355,9 +381,9 @@ hipError_t launch_weights_many(const KvWeightsArgs& a, hipStream_t s) {
   const int64_t grid = (int64_t(a.max_len) + W_KEYS - 1) / W_KEYS * a.chunks * planes;
   if (grid > MOST_GROUPS) return hipErrorInvalidValue;     // (refused by the planner)
   if (a.head_dim == 128)
-    hipLaunchKernelGGL(weights_many<128>, dim3(unsigned(grid)), dim3(NT), 0, s, a);
+    hipLaunchKernelGGL(weights_many<128>, dim3(unsigned(grid)), dim3(MANY_NT), 0, s, a);
   else
-    hipLaunchKernelGGL(weights_many<64>, dim3(unsigned(grid)), dim3(NT), 0, s, a);
+    hipLaunchKernelGGL(weights_many<64>, dim3(unsigned(grid)), dim3(MANY_NT), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part) return e;
   const int blocks = (a.max_len + NT - 1) / NT;
