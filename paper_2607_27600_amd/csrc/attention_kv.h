@@ -34,6 +34,11 @@ struct KvAttnArgs {
   int n_list, listed, R, most; // R: most rows of one
   int direct, parts;           // workgroups that share out the work (attention_shares.h; direct = 0)
   int32_t list[KV_LIST];
+  // 16 rows a workgroup: entries of a piece (0: rows whole), pieces of the longest sequence, and where their outputs and
+  // (maximum, sum) go, to be joined with the prefixes': [rsplits][N][Hq].
+  int rpiece, rsplits;
+  float* rpart;
+  float2* rpart_ml;
   float* fpart;                // [parts + n_list * Hkv][R] outputs and (maximum, sum) to be joined
   float2* fpart_ml;
   // Many rows.  Row blocks of the sequences of many rows: listed by value, longest first, or (items.n_seqs = 0)
@@ -53,7 +58,7 @@ struct KvAttnArgs {
   int2* pre_at;
   int slots, shared;
 };
-// 16 rows a workgroup, whole; with n_prefixes and no ppart the prefix's entries too.
+// 16 rows a workgroup, whole or (rpiece) in pieces that are joined; with n_prefixes and no ppart the prefix's entries too.
 hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s);
 // Few rows, work shared out.
 hipError_t launch_attn_few(const KvAttnArgs& a, hipStream_t s);

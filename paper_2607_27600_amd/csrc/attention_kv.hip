@@ -85,6 +85,7 @@ struct Rows {
 
   // 16-entry groups [gb, ge) of a plane of len entries, of which row block n's rows (one a lane) see those before
   // past[n], and every row those before full.
+  template <bool LONG>
   __device__ __forceinline__ void run(const KvAttnArgs& a, const KvPlane& P, int gb, int ge, int len, const int (&past)[NR],
                                       int full) {
     int lane = threadIdx.x & 63;
@@ -230,27 +231,36 @@ struct Rows {
         }
       };
       // In flight: the keys of the next step during a step's first product, its values during the second (the fences
-      // keep loads from being hoisted, which takes twice the registers).
+      // keep loads from being hoisted, which takes twice the registers).  In long runs the last step asks for itself again:
+      // loads under a condition are waited for as if they might not be there, which costs drafts of 8 tokens (8000
+      // entries, 16 sequences, 32 heads on 8) 37 of 165 us; in short ones asking again costs more (500 entries, 8 heads, one
+      // token: 10.7 us for 9.0).
       Keys k[2];
       Values v[2];
       bf16x8 pf[NR];
-      auto step = [&](int gr, int to, Keys& k0, Keys& k1, Values& v0, Values& v1) {
-        const bool more = gr + 2 < to;
-        if (more) load_keys(gr + 2, k1);
+      const int sm = min(se, mid), end = sm - 2;
+      auto step = [&](int gr, Keys& k0, Keys& k1, Values& v0, Values& v1) {
+        const int next = min(gr + 2, end);
+        const bool more = LONG || gr + 2 < sm;
+        if (more) load_keys(next, k1);
         scores(gr, k0, pf, std::false_type{});
         __builtin_amdgcn_sched_barrier(0);
-        if (more) load_values(gr + 2, v1);
+        if (more) load_values(next, v1);
         __builtin_amdgcn_sched_barrier(0);
         values(gr, v0, pf, std::false_type{});
         __builtin_amdgcn_sched_barrier(0);
       };
-      const int sm = min(se, mid);
       if (sb < sm) {
         load_keys(sb, k[0]);
         load_values(sb, v[0]);
-        for (int gr = sb; gr < sm; gr += 4) {
-          step(gr, sm, k[0], k[1], v[0], v[1]);
-          if (gr + 2 < sm) step(gr + 2, sm, k[1], k[0], v[1], v[0]);
+        int gr = sb;
+        for (; gr + 2 < sm; gr += 4) {
+          step(gr, k[0], k[1], v[0], v[1]);
+          step(gr + 2, k[1], k[0], v[1], v[0]);
+        }
+        if (gr < sm) {   // (its loads are the last ones asked for)
+          scores(gr, k[0], pf, std::false_type{});
+          values(gr, v[0], pf, std::false_type{});
         }
       }
 #pragma unroll 1
@@ -337,7 +347,12 @@ __device__ __forceinline__ void load_queries(const KvAttnArgs& a, Rows<HD, NR>& 
 
 // ------------------------------------------------------------------ whole rows
 
-// One workgroup for 16 rows of a (sequence, KV head): its NW waves share out the entries, the prefix's and the sequence's.
+// What the last of the 16 rows from row0 on sees of its mq queries' len entries.
+__device__ __forceinline__ int rows_see(const KvAttnArgs& a, int mq, int len, int row0) {
+  return max(0, len - mq + (min(row0 + 16, mq * a.g) - 1) / a.g + 1);
+}
+
+// One workgroup for 16 rows of a (sequence, KV head), or a piece of their entries: its NW waves share out the entries, the prefix's and the sequence's.
 template <int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_rows(KvAttnArgs a) {
   constexpr int ROWS = 16;
@@ -345,7 +360,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows(KvAttnArgs a) {
   __shared__ float2 ml[NW * ROWS];
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   const int kvh = int(blockIdx.x % unsigned(a.hkv));
-  const int64_t x = blockIdx.x / unsigned(a.hkv);
+  int64_t x = blockIdx.x / unsigned(a.hkv);
+  int split = 0;
+  if (a.rpiece) {
+    split = int(x % a.rsplits);
+    x /= a.rsplits;
+  }
   int b, row0;
   if (a.listed) {
     const int each = (a.R + ROWS - 1) / ROWS;
@@ -360,33 +380,94 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows(KvAttnArgs a) {
   const int q0 = a.cu[b], mq = a.cu[b + 1] - q0, rows = mq * a.g;
   if (row0 >= rows || rows > a.most) return;
   const int len = min(max(a.lens[b], 0), a.max_len), shift = len - mq;
+  const int most = rows_see(a, mq, len, row0);
+  if (split > 0 && split * a.rpiece >= most) return;
   Rows<HD, 1> st;
   int i[1];
   load_queries(a, st, q0, kvh, row0, rows, i);
   st.clear();
-  auto part = [&](int groups, int& gb, int& ge) {   // this wave's, in whole steps of two
-    const int per = ((groups + NW - 1) / NW + 1) & ~1;
-    gb = wave * per;
-    ge = min(groups, gb + per);
+  auto part = [&](int g0, int g1, int& gb, int& ge) {   // this wave's, in whole steps of two
+    const int per = ((g1 - g0 + NW - 1) / NW + 1) & ~1;
+    gb = g0 + wave * per;
+    ge = min(g1, gb + per);
   };
   int gb, ge;
-  if (a.ppart) {
+  if (a.ppart && !a.rpiece) {
     const int j = prefix_of(a, b);
     const PrefixRow p[1] = {prefix_row(a, j, kvh, int64_t(q0 - a.cu[a.pre_first[j]]) * a.g + min(row0 + int(threadIdx.x & 15), rows - 1))};
     st.template absorb<NW>(a, wave, p);
-  } else if (a.n_prefixes) {
+  } else if (a.n_prefixes && !a.ppart) {
     const int j = prefix_of(a, b);
     const int n = min(max(a.pre_lens[j], 0), a.pre_max);
     const int past[1] = {n};
-    part((n + 15) >> 4, gb, ge);
-    st.run(a, kv_plane(a.pre, j, a.layer, kvh), gb, ge, n, past, n);
+    part(0, (n + 15) >> 4, gb, ge);
+    st.template run<false>(a, kv_plane(a.pre, j, a.layer, kvh), gb, ge, n, past, n);
   }
   const int past[1] = {max(0, shift + i[0] + 1)};
-  const int most = max(0, shift + (min(row0 + ROWS, rows) - 1) / a.g + 1);   // what the last row sees
-  part((most + 15) >> 4, gb, ge);
-  st.run(a, kv_plane(a.own, b, a.layer, kvh), gb, ge, len, past, max(0, shift + row0 / a.g + 1));
-  meet<HD, 1, NW>(a, st, lds, ml, min(ROWS, rows - row0),
-                  [&](int r, int d, float M, float L, float4(&o)[2]) { finish<HD>(a, q0, kvh, row0 + r, d, M, L, o); });
+  part(split * a.rpiece >> 4, (a.rpiece ? min(most, (split + 1) * a.rpiece) + 15 : most + 15) >> 4, gb, ge);
+  st.template run<false>(a, kv_plane(a.own, b, a.layer, kvh), gb, ge, len, past, max(0, shift + row0 / a.g + 1));
+  meet<HD, 1, NW>(a, st, lds, ml, min(ROWS, rows - row0), [&](int r, int d, float M, float L, float4(&o)[2]) {
+    if (!a.rpiece) return finish<HD>(a, q0, kvh, row0 + r, d, M, L, o);
+    const int64_t at = (int64_t(split) * a.N + q0 + (row0 + r) / a.g) * a.hq + kvh * a.g + (row0 + r) % a.g;
+    float* po = a.rpart + at * HD + d;
+    *reinterpret_cast<float4*>(po) = o[0];
+    *reinterpret_cast<float4*>(po + 4) = o[1];
+    if (d == 0) a.rpart_ml[at] = make_float2(M, L);
+  });
+}
+
+// Joins what the pass over the prefixes has of a row with its own pieces: a wave a row, whose groups of HD / 8 lanes share out
+// the pieces, the prefix's first, four in flight each.
+template <int HD>
+__global__ __launch_bounds__(256) void attn_rows_join(KvAttnArgs a, int64_t group0) {
+  constexpr int LPR = HD / 8, NG = 64 / LPR;
+  const int lane = threadIdx.x & 63, gi = lane / LPR, d = (lane % LPR) * 8;
+  const int64_t out = (group0 + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  if (out >= int64_t(a.N) * a.hq) return;
+  const int query = int(out / a.hq), h = int(out % a.hq), kvh = h / a.g;
+  const int b = last_at(a.n_seqs, [&](int i) { return int64_t(a.cu[i]); }, query);
+  const int q0 = a.cu[b], mq = a.cu[b + 1] - q0;
+  const int64_t rows = int64_t(mq) * a.g;
+  if (rows > a.most) return;
+  const int row = (query - q0) * a.g + h % a.g;
+  const int own = max(1, (rows_see(a, mq, min(max(a.lens[b], 0), a.max_len), row & ~15) + a.rpiece - 1) / a.rpiece);
+  const int j = prefix_of(a, b);
+  const PrefixRow p = prefix_row(a, j, kvh, int64_t(q0 - a.cu[a.pre_first[j]]) * a.g + row);
+  const int n = p.n + own;
+  Joined g[2] = {{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)}, {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)}};
+  for (int i0 = gi; i0 < n; i0 += 4 * NG) {
+    float2 ml[4];
+    float4 y[2][4];
+    bool in[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int i = min(i0 + q * NG, n - 1);
+      const bool pre = i < p.n;
+      const int64_t at = pre ? p.first + int64_t(i) * KV_ROWS : int64_t(i - p.n) * a.N * a.hq + out;
+      const float* x = (pre ? a.ppart : a.rpart) + at * HD + d;
+      in[q] = i0 + q * NG < n;
+      ml[q] = (pre ? a.ppart_ml : a.rpart_ml)[at];
+      y[0][q] = *reinterpret_cast<const float4*>(x);
+      y[1][q] = *reinterpret_cast<const float4*>(x + 4);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) g[k].add(ml, [&](int q) { return y[k][q]; }, in, a.c2);
+  }
+  // the groups' results, pairs first
+#pragma unroll
+  for (int off = LPR; off < 64; off <<= 1) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float2 ml[1] = {make_float2(__shfl_xor(g[k].M, off), __shfl_xor(g[k].L, off))};
+      const float4 o = make_float4(__shfl_xor(g[k].o.x, off), __shfl_xor(g[k].o.y, off), __shfl_xor(g[k].o.z, off),
+                                   __shfl_xor(g[k].o.w, off));
+      const bool in[1] = {true};
+      g[k].add(ml, [&](int) { return o; }, in, a.c2);
+    }
+  }
+  if (gi) return;
+  const float4 o[2] = {g[0].o, g[1].o};
+  finish<HD>(a, q0, kvh, row, d, g[0].M, g[0].L, o);
 }
 
 // ------------------------------------------------------------------ few rows, work shared out
@@ -432,7 +513,7 @@ __global__ __launch_bounds__(FEW_NT, 2) void attn_few(KvAttnArgs a) {
     const int g0 = c0 >> 4, g1 = (c1 + 15) >> 4;
     const int per = ((g1 - g0 + NW - 1) / NW + 1) & ~1;
     const int gb = g0 + wave * per, ge = min(g1, gb + per);
-    st.run(a, kv_plane(a.own, s.b, a.layer, kvh), gb, ge, s.len, past, max(0, s.shift + 1));
+    st.template run<true>(a, kv_plane(a.own, s.b, a.layer, kvh), gb, ge, s.len, past, max(0, s.shift + 1));
     meet<HD, NR, NW>(a, st, lds, ml, rows, [&](int r, int d, float M, float L, float4(&o)[2]) {
       if (whole) return finish<HD>(a, s.q0, kvh, r, d, M, L, o);
       const int64_t row = (int64_t(blockIdx.x) + int64_t(j) * a.hkv + kvh) * a.R + r;
@@ -558,7 +639,8 @@ hipError_t few_dim(const KvAttnArgs& a, hipStream_t s) {
 hipError_t launch_attn_few(const KvAttnArgs& a, hipStream_t s) { return a.head_dim == 128 ? few_dim<128>(a, s) : few_dim<64>(a, s); }
 
 hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s) {
-  const int64_t blocks = (a.listed ? int64_t(a.n_list) * ((a.R + 15) / 16) : int64_t(a.N) * a.g / 16 + a.n_seqs) * a.hkv;
+  const int64_t blocks = (a.listed ? int64_t(a.n_list) * ((a.R + 15) / 16) : int64_t(a.N) * a.g / 16 + a.n_seqs) * a.hkv *
+                         (a.rpiece ? a.rsplits : 1);
   if (blocks > MOST_GROUPS / 2) return hipErrorInvalidValue;   // (refused by the planner)
   // Eight waves where there is a CU for every workgroup, so that a wave's chain of loads is short.
   const bool wide = blocks <= 256;
@@ -567,7 +649,18 @@ hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s) {
     wide ? launch(attn_rows<128, 8>) : launch(attn_rows<128, 4>);
   else
     wide ? launch(attn_rows<64, 8>) : launch(attn_rows<64, 4>);
-  return hipGetLastError();
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.rpiece) return e;
+  const int64_t groups = (int64_t(a.N) * a.hq + 3) / 4;
+  for (int64_t g0 = 0; g0 < groups; g0 += MOST_GROUPS) {
+    const dim3 grid(unsigned(std::min(MOST_GROUPS, groups - g0)));
+    if (a.head_dim == 128)
+      hipLaunchKernelGGL(attn_rows_join<128>, grid, dim3(256), 0, s, a, g0);
+    else
+      hipLaunchKernelGGL(attn_rows_join<64>, grid, dim3(256), 0, s, a, g0);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace cc

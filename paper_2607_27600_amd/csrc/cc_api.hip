@@ -1333,6 +1333,7 @@ struct KvPlan {
   int n_few = 0, n_list = 0, listed = 0, R = 0, parts = 0;
   bool direct = false;         // few rows: by 16 rows a workgroup
   int32_t list[KV_LIST];
+  int rpiece = 0, rsplits = 1; // behind prefixes: entries of a piece of those (0: whole)
   size_t fpart = 0, ftotal = 0;
   KvMany many;
   int64_t pre_blocks = 0;      // row blocks of the pass over the prefixes (0: none)
@@ -1342,6 +1343,7 @@ struct KvPlan {
 
 // What a workgroup for each 16 rows of a (sequence, KV head) is for: short calls, with nothing to join.
 constexpr int KV_SHORT = 1024;
+constexpr int KV_OWN = 512;
 // Workgroups that the pass over the prefixes is cut into: two a CU.
 constexpr int KV_SLOTS = 2 * kCus;
 
@@ -1370,7 +1372,15 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
   c.listed = c.n_few <= KV_LIST && (!c.direct || int64_t(c.n_few) * ((c.R + 15) / 16) <= walked);
   c.n_list = c.listed ? c.n_few : p->n_seqs;
   c.parts = 2 * kCus;
-  if (c.n_few && !c.direct) {
+  // Behind prefixes results are joined anyhow, and a CU takes some 60 GB/s: pieces of what a CU takes in 4 us.
+  if (x && !c.inside && c.n_few && max_len > KV_OWN) {
+    c.direct = true;
+    c.rpiece = KV_OWN;
+    c.rsplits = int((int64_t(max_len) + KV_OWN - 1) / KV_OWN);
+    const size_t rows = size_t(c.rsplits) * p->n_heads_q * n_tokens(p);
+    c.fpart = align_up(rows * p->head_dim * sizeof(float));
+    c.ftotal = c.fpart + align_up(rows * sizeof(float2));
+  } else if (c.n_few && !c.direct) {
     const size_t rows = (size_t(c.parts) + size_t(c.n_list) * hkv) * c.R;
     c.fpart = align_up(rows * p->head_dim * sizeof(float));
     c.ftotal = c.fpart + align_up(rows * sizeof(float2));
@@ -1388,7 +1398,7 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
     c.ptotal = c.ppart + align_up(size_t(groups) * KV_ROWS * sizeof(float2));
   }
   // (a launch by 16 rows a workgroup of 512)
-  const int64_t by16 = (c.listed ? int64_t(c.n_list) * ((c.R + 15) / 16) : walked) * hkv;
+  const int64_t by16 = (c.listed ? int64_t(c.n_list) * ((c.R + 15) / 16) : walked) * hkv * c.rsplits;
   if (c.n_few && c.direct && by16 > MOST_GROUPS / 2) return CC_ERR_UNSUPPORTED;
   return CC_OK;
 }
@@ -1467,8 +1477,10 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
     a.most = c.rows ? INT32_MAX : FEW_ROWS;
     a.parts = c.parts;
     std::copy_n(c.list, c.listed ? c.n_few : 0, a.list);
-    a.fpart = c.ftotal ? reinterpret_cast<float*>(at(ws, off)) : nullptr;
-    a.fpart_ml = c.ftotal ? reinterpret_cast<float2*>(at(ws, off + c.fpart)) : nullptr;
+    a.rpiece = c.rpiece;
+    a.rsplits = c.rsplits;
+    (c.rpiece ? a.rpart : a.fpart) = c.ftotal ? reinterpret_cast<float*>(at(ws, off)) : nullptr;
+    (c.rpiece ? a.rpart_ml : a.fpart_ml) = c.ftotal ? reinterpret_cast<float2*>(at(ws, off + c.fpart)) : nullptr;
     off += c.ftotal;
     CC_HIP(c.direct ? launch_attn_rows(a, st) : launch_attn_few(a, st));
   }
