@@ -17,7 +17,8 @@ ARCH = "gfx950"
 
 SOURCES = ["attention.hip", "attention_f32.hip", "lmhead.hip", "gemm_f32.hip", "projections.hip", "select.hip", "compact.hip", "fullpass.hip",
            "append.hip", "compact8.hip", "attention_kv8.hip", "attention_kv8_many.hip",
-           "attention_kv.hip", "attention_kv_many.hip", "weights.hip", "logprobs.hip", "cc_api.hip"]
+           "attention_kv.hip", "attention_kv_many.hip", "attention_kv_prefix.hip",
+           "weights.hip", "logprobs.hip", "cc_api.hip"]
 
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}",

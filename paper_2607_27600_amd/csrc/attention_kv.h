@@ -49,17 +49,24 @@ struct KvAttnArgs {
   // Results to be joined (null: none), outputs and (maximum, sum): [splits][Hkv][N g]
   float* part;
   float2* part_ml;
-  // The pass over the prefixes (shared = 1): they stand for sequences, and own, lens and n_seqs are theirs.  Its pieces
+  // The pass over the prefixes: they stand for sequences, and own, lens and n_seqs are theirs.  Its pieces
   // are sized on the device, by the prefixes' lengths, for `slots` workgroups at the least: a workgroup, and KV_ROWS rows
   // of ppart, for each.  Where prefix i's begin and how many each of its (row block, KV head) has is in pre_at[i].  For the
   // passes over the sequences' own entries ppart and pre_at are what it has left (null: none).
   float* ppart;
   float2* ppart_ml;
   int2* pre_at;
-  int slots, shared;
+  int slots;
 };
-// 16 rows a workgroup, whole or (rpiece) in pieces that are joined; with n_prefixes and no ppart the prefix's entries too.
+// 16 rows a workgroup; with n_prefixes the prefix's entries too.
 hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s);
+// Workgroups of that, or of the pieces of it.
+inline int64_t rows_groups(const KvAttnArgs& a) {
+  return (a.listed ? int64_t(a.n_list) * ((a.R + 15) / 16) : int64_t(a.N) * a.g / 16 + a.n_seqs) * a.hkv *
+         (a.rpiece ? a.rsplits : 1);
+}
+// The pass over the prefixes, and with `few` the sequences of few rows, done.
+hipError_t launch_attn_prefix(const KvAttnArgs& pass, const KvAttnArgs& own, bool few, hipStream_t s);
 // Few rows, work shared out.
 hipError_t launch_attn_few(const KvAttnArgs& a, hipStream_t s);
 hipError_t launch_attn_kv_many(const KvAttnArgs& a, hipStream_t s);

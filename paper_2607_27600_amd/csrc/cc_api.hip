@@ -1372,11 +1372,11 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
   c.listed = c.n_few <= KV_LIST && (!c.direct || int64_t(c.n_few) * ((c.R + 15) / 16) <= walked);
   c.n_list = c.listed ? c.n_few : p->n_seqs;
   c.parts = 2 * kCus;
-  // Behind prefixes results are joined anyhow, and a CU takes some 60 GB/s: pieces of what a CU takes in 4 us.
-  if (x && !c.inside && c.n_few && max_len > KV_OWN) {
+  // Behind prefixes results are joined anyhow, and a CU takes some 60 GB/s: pieces of what it takes in a few us.
+  if (x && !c.inside && c.n_few) {
     c.direct = true;
-    c.rpiece = KV_OWN;
-    c.rsplits = int((int64_t(max_len) + KV_OWN - 1) / KV_OWN);
+    c.rpiece = std::max(KV_OWN, int((int64_t(max_len) + 32 * 16 - 1) / (32 * 16) * 16));
+    c.rsplits = std::max(1, int((int64_t(max_len) + c.rpiece - 1) / c.rpiece));
     const size_t rows = size_t(c.rsplits) * p->n_heads_q * n_tokens(p);
     c.fpart = align_up(rows * p->head_dim * sizeof(float));
     c.ftotal = c.fpart + align_up(rows * sizeof(float2));
@@ -1392,7 +1392,7 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
       c.pre_blocks += (m * g + KV_ROWS - 1) / KV_ROWS;
     }
     const int64_t groups = std::max<int64_t>(KV_SLOTS, c.pre_blocks * hkv);
-    if (groups > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+    if (groups > MOST_GROUPS / 2) return CC_ERR_UNSUPPORTED;
     c.pre_at = align_up(size_t(x->n_prefixes) * sizeof(int2));
     c.ppart = c.pre_at + align_up(size_t(groups) * KV_ROWS * p->head_dim * sizeof(float));
     c.ptotal = c.ppart + align_up(size_t(groups) * KV_ROWS * sizeof(float2));
@@ -1460,15 +1460,6 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
     a.ppart = reinterpret_cast<float*>(at(ws, c.pre_at));
     a.ppart_ml = reinterpret_cast<float2*>(at(ws, c.ppart));
     off = c.ptotal;
-    KvAttnArgs pass = a;
-    pass.own = a.pre;
-    pass.lens = a.pre_lens;
-    pass.max_len = a.pre_max;
-    pass.n_seqs = a.n_prefixes;
-    pass.blocks = int(c.pre_blocks);
-    pass.slots = KV_SLOTS;
-    pass.shared = 1;
-    CC_HIP(launch_attn_kv_many(pass, st));
   }
   if (c.n_few) {
     a.n_list = c.n_list;
@@ -1482,6 +1473,17 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
     (c.rpiece ? a.rpart : a.fpart) = c.ftotal ? reinterpret_cast<float*>(at(ws, off)) : nullptr;
     (c.rpiece ? a.rpart_ml : a.fpart_ml) = c.ftotal ? reinterpret_cast<float2*>(at(ws, off + c.fpart)) : nullptr;
     off += c.ftotal;
+  }
+  if (c.pre_blocks) {
+    KvAttnArgs pass = a;
+    pass.own = a.pre;
+    pass.lens = a.pre_lens;
+    pass.max_len = a.pre_max;
+    pass.n_seqs = a.n_prefixes;
+    pass.blocks = int(c.pre_blocks);
+    pass.slots = KV_SLOTS;
+    CC_HIP(launch_attn_prefix(pass, a, c.n_few > 0, st));
+  } else if (c.n_few) {
     CC_HIP(c.direct ? launch_attn_rows(a, st) : launch_attn_few(a, st));
   }
   if (c.many.n) CC_HIP(many(c.many));
