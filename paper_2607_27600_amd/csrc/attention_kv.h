@@ -41,6 +41,7 @@ struct KvAttnArgs {
   float2* rpart_ml;
   float* fpart;                // [parts + n_list * Hkv][R] outputs and (maximum, sum) to be joined
   float2* fpart_ml;
+  int2* fpart_at;              // [n_list * Hkv] first and last workgroup that has some of a (sequence, head)'s entries
   // Many rows.  Row blocks of the sequences of many rows: listed by value, longest first, or (items.n_seqs = 0)
   // sequence b has those from cu[b] g / KV_ROWS + b on, more than its rows need.
   AttnMany items;

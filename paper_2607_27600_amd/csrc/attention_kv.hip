@@ -39,6 +39,11 @@ __global__ __launch_bounds__(FEW_NT, 2) void attn_few(KvAttnArgs a) {
     const int u0 = max(0, it.unit - sh.head), u1 = past_unit - sh.head;   // those with entries
     const bool whole = u0 == 0 && past_unit == it.units;
     if (u1 <= u0) continue;
+    if (threadIdx.x == 0) {
+      int2* at = a.fpart_at + int64_t(j) * a.hkv + kvh;
+      if (u0 == 0) at->x = int(blockIdx.x);
+      if (past_unit == it.units) at->y = int(blockIdx.x);
+    }
     const int unit = sh.q * UNIT;
     const int c0 = u0 * unit, c1 = int(min(int64_t(s.len), int64_t(u1) * unit));
     Rows<HD, NR> st;
@@ -80,24 +85,8 @@ __global__ __launch_bounds__(256) void attn_few_join(KvAttnArgs a, int one, int6
   const Seq s = seq_of(a, j);
   const int rows = s.m * a.g;
   bool on = row_in < all && r < rows && rows <= FEW_ROWS;
-  // the rows of a wave lie in one (sequence, head), or the search runs for each in turn
-  const Shares sh = shares_of(a);
-  int64_t start = 0;
-  int units = 0;
-  for (uint64_t left = __ballot(true); left;) {
-    const int jn = __builtin_amdgcn_readlane(j, __builtin_ctzll(left));
-    int64_t st;
-    int un;
-    item_of(a, sh, jn, st, un);
-    if (j == jn) {
-      start = st;
-      units = un;
-    }
-    left &= ~__ballot(j == jn);
-  }
-  const int64_t x = start + int64_t(kvh) * units;
-  const int wa = sh.part_of(x + sh.head), wb = sh.part_of(x + max(units, 1) - 1);
-  const int n = wb - wa + 1;
+  const int2 parts = on ? a.fpart_at[jh] : make_int2(0, 0);
+  const int wa = parts.x, n = parts.y - wa + 1;
   on = on && n > 1;   // a whole one is final
   const int64_t slot = (int64_t(wa) + jh) * a.R + r;   // piece i at slot + i R
   Joined g[2] = {{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)}, {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)}};

@@ -1334,7 +1334,7 @@ struct KvPlan {
   bool direct = false;         // few rows: by 16 rows a workgroup
   int32_t list[KV_LIST];
   int rpiece = 0, rsplits = 1; // behind prefixes: entries of a piece of those (0: whole)
-  size_t fpart = 0, ftotal = 0;
+  size_t fpart = 0, fat = 0, ftotal = 0;
   KvMany many;
   int64_t pre_blocks = 0;      // row blocks of the pass over the prefixes (0: none)
   size_t pre_at = 0, ppart = 0, ptotal = 0;   // its workspace: where its pieces are, outputs, (maximum, sum) pairs
@@ -1383,7 +1383,8 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
   } else if (c.n_few && !c.direct) {
     const size_t rows = (size_t(c.parts) + size_t(c.n_list) * hkv) * c.R;
     c.fpart = align_up(rows * p->head_dim * sizeof(float));
-    c.ftotal = c.fpart + align_up(rows * sizeof(float2));
+    c.fat = c.fpart + align_up(rows * sizeof(float2));
+    c.ftotal = c.fat + align_up(size_t(c.n_list) * hkv * sizeof(int2));
   }
   CC_TRY(c.many.cut(p, p->n_seqs, max_len));
   if (x && !c.inside) {
@@ -1472,6 +1473,7 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
     a.rsplits = c.rsplits;
     (c.rpiece ? a.rpart : a.fpart) = c.ftotal ? reinterpret_cast<float*>(at(ws, off)) : nullptr;
     (c.rpiece ? a.rpart_ml : a.fpart_ml) = c.ftotal ? reinterpret_cast<float2*>(at(ws, off + c.fpart)) : nullptr;
+    a.fpart_at = c.fat ? reinterpret_cast<int2*>(at(ws, off + c.fat)) : nullptr;
     off += c.ftotal;
   }
   if (c.pre_blocks) {
