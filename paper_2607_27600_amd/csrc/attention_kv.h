@@ -15,9 +15,14 @@ struct KvPair {
 constexpr int KV_ROWS = 128;   // rows of a block of the kernel for many
 constexpr int KV_KEYS = 64;    // entries of its tiles
 constexpr int KV_LIST = 64;    // sequences of few rows of a launch listed by value
+// Few rows: the longest cache of which each (sequence, head) is one workgroup's, with nothing to join.  A CU alone takes
+// some 60 GB/s, with four waves half.  That against shares: 16 sequences of 2000, 8 heads, 25 us and 35; 64 of 2000 96 and 103,
+// but 40 and 26 where eight have 1900 entries and the others 20.
+inline int kv_direct(int64_t items) { return items >= 128 && items <= 256 ? 2048 : 1024; }
 
 // Attention of the queries of n_seqs sequences to the entries of a prefix and to their own entries up to their own.
 struct KvAttnArgs {
+  static constexpr int LEAST = 1;   // (of entries of 16 bits; with two, one sequence of 2048 entries and 8 heads 12.9 us for 11.1)
   const u16* q;
   u16* o;
   float* lse;                  // or null

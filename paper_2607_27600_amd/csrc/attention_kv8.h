@@ -32,6 +32,7 @@ __device__ __forceinline__ uint32_t whole_bytes(uint32_t m) { return (m >> 7) * 
 
 // One class of sequences (few or many rows) of a call.
 struct Kv8Args {
+  static constexpr int LEAST = 2;
   const u16* q;
   u16* o;
   Kv8View k, v;                  // alike but for base and scale

@@ -1,6 +1,6 @@
 // What the attentions over a cache share, in 8 bits and in bf16: how the work of the kernels for few rows is shared out
 // among workgroups, and how results are joined.  A: the arguments of a launch, with the sequences walked (list, listed,
-// n_list), their queries and entries (cu, lens, max_len) and heads (hkv, g), and direct and parts.
+// n_list), their queries and entries (cu, lens, max_len) and heads (hkv, g), and direct and parts; LEAST: units of a piece.
 #pragma once
 
 #include "cc_internal.h"
@@ -134,7 +134,7 @@ __device__ __forceinline__ Shares shares_of(const A& a) {
   s.total = units_in_all(a, raw);
   const int items = a.n_list * a.hkv;
   if (items < a.parts) {
-    const int64_t q = max(int64_t(2), (s.total + a.parts - items - 1) / (a.parts - items));
+    const int64_t q = max(int64_t(A::LEAST), (s.total + a.parts - items - 1) / (a.parts - items));
     if (q <= LITTLE) {   // at most total / q + items <= parts pieces
       s.q = int(q);
       s.mine = s.per == 1 ? s.of(raw) : sum(n);

@@ -1367,7 +1367,7 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
     }
   }
   const int64_t walked = int64_t(n_tokens(p)) * g / 16 + p->n_seqs;
-  c.direct = c.rows || max_len <= kv8_direct(int64_t(c.n_few) * hkv);
+  c.direct = c.rows || max_len <= kv_direct(int64_t(c.n_few) * hkv);
   // (listed sequences have the blocks of the longest)
   c.listed = c.n_few <= KV_LIST && (!c.direct || int64_t(c.n_few) * ((c.R + 15) / 16) <= walked);
   c.n_list = c.listed ? c.n_few : p->n_seqs;
