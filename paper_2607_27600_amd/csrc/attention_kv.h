@@ -17,8 +17,8 @@ constexpr int KV_KEYS = 64;    // entries of its tiles
 constexpr int KV_LIST = 64;    // sequences of few rows of a launch listed by value
 // Few rows: the longest cache of which each (sequence, head) is one workgroup's, with nothing to join.  A CU alone takes
 // some 60 GB/s, with four waves half.  That against shares: 16 sequences of 2000, 8 heads, 25 us and 35; 64 of 2000 96 and 103,
-// but 40 and 26 where eight have 1900 entries and the others 20.
-inline int kv_direct(int64_t items) { return items >= 128 && items <= 256 ? 2048 : 1024; }
+// but 40 and 26 where eight have 1900 entries and the others 20; one of 500, 8 heads, 8.8 and 10.9, of 1000 13.2 and 11.0.
+inline int kv_direct(int64_t items) { return items < 128 ? 600 : items <= 256 ? 2048 : 1024; }
 
 // Attention of the queries of n_seqs sequences to the entries of a prefix and to their own entries up to their own.
 struct KvAttnArgs {

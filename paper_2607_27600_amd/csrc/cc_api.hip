@@ -1341,8 +1341,12 @@ struct KvPlan {
   size_t total() const { return ptotal + ftotal + many.total; }
 };
 
-// What a workgroup for each 16 rows of a (sequence, KV head) is for: short calls, with nothing to join.
+// Prompts, chunks and sequences behind a prefix: up to that many entries, and that many workgroups of 16 rows, each has its
+// own, with nothing to join and no tiles of 128 rows to fill.  That against those: a prompt of 300 tokens, 32 heads on 8 (600
+// workgroups), 11.4 us and 12.5, of 400 15.9 and 14.1; 64 tokens at the end of 964 13.3 and 23.9; one of 1000, 4 heads, 9.6 and
+// 18.2; eight sequences of one token behind 900 entries 13.0 and 13.9.
 constexpr int KV_SHORT = 1024;
+constexpr int KV_SHORT_GROUPS = 640;
 constexpr int KV_OWN = 512;
 // Workgroups that the pass over the prefixes is cut into: two a CU.
 constexpr int KV_SLOTS = 2 * kCus;
@@ -1351,8 +1355,13 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
   const int g = p->n_heads_q / p->n_heads_kv, hkv = p->n_heads_kv;
   const int longest = int(std::min<int64_t>(INT32_MAX, int64_t(max_len) + (x ? x->max_len : 0)));
   int64_t blocks16 = 0;
-  for (int b = 0; b < p->n_seqs; ++b) blocks16 += (int64_t(p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) * g + 15) / 16;
-  c.rows = longest <= KV_SHORT && blocks16 * hkv <= 640;
+  bool many = false;
+  for (int b = 0; b < p->n_seqs; ++b) {
+    const int64_t rows = int64_t(p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) * g;
+    blocks16 += (rows + 15) / 16;
+    many |= rows > FEW_ROWS;
+  }
+  c.rows = (many || x) && longest <= KV_SHORT && blocks16 * hkv <= KV_SHORT_GROUPS;
   c.inside = x && c.rows;
   for (int b = 0; b < p->n_seqs; ++b) {
     const int seq0 = p->cu_seqlens_h[b], m = p->cu_seqlens_h[b + 1] - seq0;
