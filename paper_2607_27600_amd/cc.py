@@ -9,6 +9,7 @@ module raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass, field
 from typing import Optional, Sequence
@@ -238,6 +239,11 @@ class Problem:
     @property
     def n_tokens(self) -> int:
         return int(self.cu_h[-1])
+
+    @functools.cached_property
+    def longest(self) -> int:
+        """The most of a sequence."""
+        return int((self.cu_h[1:] - self.cu_h[:-1]).max()) if len(self.cu_h) > 1 else 0
 
 
 def problem(*, dtype: str, cu_seqlens: Sequence[int], n_heads_q: int, n_heads_kv: int,
@@ -798,9 +804,12 @@ def _queries(p: Problem, q: torch.Tensor, kv: KV, kv_lens: torch.Tensor) -> None
 
 
 def _bf16_cache(kv: KV) -> None:
+    if getattr(kv, "_bf16", False):   # (a view's tensors stay what they are)
+        return
     for t in kv.keep[:2]:
         if t.dtype != torch.bfloat16:
             raise ValueError(f"the cache holds {t.dtype}, expected bf16")
+    kv._bf16 = True
 
 
 def _lse(p: Problem, lse: Optional[torch.Tensor]) -> None:
@@ -884,24 +893,22 @@ def cc_attention_prefix(p: Problem, q: torch.Tensor, prefix: Prefix, kv: KV, lay
 
 # ---------------------------------------------------------------- eviction by attention weight
 
-def _weights(p: Problem, w: torch.Tensor, what: str, longest: int) -> c_weights:
-    """The view of weights w [n_seqs][Hkv][entries], entries contiguous."""
+def _weights(p: Problem, w: torch.Tensor, what: str, longest: int, written: bool = False) -> c_weights:
+    """The view of weights w [n_seqs][Hkv][entries], entries contiguous; where they are written rows may not overlap."""
     s = p.struct
     if w.dtype != torch.float32:
         raise ValueError(f"{what} is {w.dtype}, expected float32")
-    if w.dim() != 3 or w.shape[0] != s.n_seqs or w.shape[1] != s.n_heads_kv or w.shape[2] < longest:
-        raise ValueError(f"{what} has shape {tuple(w.shape)}, expected {(s.n_seqs, s.n_heads_kv)} and at least {longest} entries")
-    if w.shape[2] > 1 and w.stride(2) != 1:
-        raise ValueError(f"entries of {what} must be contiguous")
-    return c_weights(w.data_ptr(), w.stride(0) if s.n_seqs > 1 else 0, w.stride(1) if s.n_heads_kv > 1 else 0)
-
-
-def _own_places(w: torch.Tensor, what: str) -> None:
-    """Rows that are written may not overlap."""
-    at = sorted((st, n) for st, n in zip(w.stride(), w.shape) if n > 1)
-    for (st, n), (up, _) in zip(at, at[1:]):
-        if up < st * n:
+    shape = w.shape
+    if len(shape) != 3 or shape[0] != s.n_seqs or shape[1] != s.n_heads_kv or shape[2] < longest:
+        raise ValueError(f"{what} has shape {tuple(shape)}, expected {(s.n_seqs, s.n_heads_kv)} and at least {longest} entries")
+    seq, head, entry = w.stride()
+    if not w.is_contiguous():
+        if shape[2] > 1 and entry != 1:
+            raise ValueError(f"entries of {what} must be contiguous")
+        at = sorted((st, n) for st, n in zip((seq, head, entry), shape) if n > 1)
+        if written and any(up < st * n for (st, n), (up, _) in zip(at, at[1:])):
             raise ValueError(f"{what} overlaps itself (strides {w.stride()})")
+    return c_weights(w.data_ptr(), seq if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
 
 
 def cc_attention_weights_workspace(p: Problem, max_kv_len: int) -> int:
@@ -921,8 +928,7 @@ def cc_attention_weights(p: Problem, q: torch.Tensor, kv: KV, layer: int, kv_len
     _int32(prev_lens, s.n_seqs, "prev_lens")
     if prev is None and prev_lens is not None:
         raise ValueError("prev_lens without prev")
-    to = _weights(p, out, "out", max_kv_len)
-    _own_places(out, "out")
+    to = _weights(p, out, "out", max_kv_len, True)
     had = _weights(p, prev, "prev", 0 if prev_lens is not None else max_kv_len) if prev is not None else None
     _on_gpu(q, lse, out, prev, prev_lens, kv_lens, workspace, p.cu_d, kv)
     if workspace is None:
@@ -939,9 +945,8 @@ def cc_weight_scores(p: Problem, w: torch.Tensor, n_recent: int, per_head: int, 
     """Scores for cc_select_keep from weights w [n_seqs][Hkv][entries] (p.cu_seqlens count the entries): one segment for
     each sequence, or with per_head for each of its KV heads; the first p.n_frozen and the last n_recent are +inf."""
     s = p.struct
-    cu = s.cu_seqlens_h[:s.n_seqs + 1]
-    view = _weights(p, w, "w", max(b - a for a, b in zip(cu, cu[1:])))
-    n = cu[-1] * (s.n_heads_kv if per_head else 1)
+    view = _weights(p, w, "w", p.longest)
+    n = s.cu_seqlens_h[s.n_seqs] * (s.n_heads_kv if per_head else 1)
     if scores is None:
         scores = _empty((n,), torch.float32, w.device, stream)
     elif scores.dtype != torch.float32 or scores.numel() < n or not scores.is_contiguous():
@@ -961,10 +966,8 @@ def cc_compact_weights(p: Problem, w: torch.Tensor, keep_idx: torch.Tensor, k: S
         raise ValueError(f"{n} budgets for {s.n_seqs} sequences")
     if keep_idx is not None and (keep_idx.dtype != torch.int32 or keep_idx.numel() < sum(k) or not keep_idx.is_contiguous()):
         raise ValueError(f"keep_idx must be {sum(k)} contiguous int32 values")
-    cu = s.cu_seqlens_h[:s.n_seqs + 1]
-    src = _weights(p, w, "w", max(b - a for a, b in zip(cu, cu[1:])))
-    dst = _weights(p, out, "out", max(k, default=0)) if out is not None else None
-    _own_places(w if out is None else out, "w" if out is None else "out")
+    src = _weights(p, w, "w", p.longest, out is None)
+    dst = _weights(p, out, "out", max(k, default=0), True) if out is not None else None
     _on_gpu(w, keep_idx, out, p.cu_d)
     _check(_lib.cc_compact_weights(ctypes.byref(s), ctypes.byref(src), _ptr(keep_idx), kk, int(per_head),
                                    ctypes.byref(dst) if dst is not None else None, _stream(stream)), "cc_compact_weights")
