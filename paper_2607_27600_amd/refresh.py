@@ -15,8 +15,13 @@ libcc.  Entries keep the absolute positions they were appended with.
 
 The cache holds bf16, or 8 bits (cache="e4m3": E4M3 codes with a power-of-two scale for each
 block of entries and head, half the bytes): the same cycle on cc_append_kv8, cc_attention_kv8
-and cc_compact_kv8.  An 8-bit cache scores the given-query fast variants, and `attend` runs
-the inference cycle's own attention over it.
+and cc_compact_kv8.  An 8-bit cache scores the given-query fast variants.  `attend` runs the
+inference cycle's own attention over either (cc_attention_kv, cc_attention_kv8).
+
+With policy="weight" a bf16 cache keeps the entries that received most of the attention instead
+of the most surprising ones: every `attend` adds what its queries gave (cc_attention_weights;
+layers and heads summed), and a refresh keeps the J entries of the largest sums, the last
+n_recent among them.
 """
 from __future__ import annotations
 
@@ -58,8 +63,11 @@ class RefreshLoop:
     """One sequence's cache under counter-causal memory management."""
 
     def __init__(self, model: Model, J: int, h: int, device="cuda",
-                 capacity: Optional[int] = None, cache: str = "bf16", scale_block: int = 16):
-        """cache: "bf16" or "e4m3" (scale_block entries a scale: a power of two from 16 to 128)."""
+                 capacity: Optional[int] = None, cache: str = "bf16", scale_block: int = 16,
+                 policy: str = "surprise", n_recent: int = 0):
+        """cache: "bf16" or "e4m3" (scale_block entries a scale: a power of two from 16 to 128).
+        policy: "surprise" (the counter-causal score) or "weight" (accumulated attention, bf16 caches;
+        the last n_recent entries stay)."""
         if model.mode not in ("last_layer", "last_layer_fused", "last_layer_h"):
             raise ValueError("mode must be last_layer, last_layer_fused or last_layer_h")
         if J < 1 or h < 1:
@@ -70,8 +78,14 @@ class RefreshLoop:
             raise ValueError("an 8-bit cache scores given queries (last_layer or last_layer_fused)")
         if cache == "e4m3" and scale_block not in (16, 32, 64, 128):
             raise ValueError("scale_block must be 16, 32, 64 or 128")
+        if policy not in ("surprise", "weight"):
+            raise ValueError("policy must be surprise or weight")
+        if policy == "weight" and cache != "bf16":
+            raise ValueError("attention weights are accumulated over bf16 caches")
+        if n_recent < 0 or (n_recent and policy != "weight"):
+            raise ValueError("n_recent counts entries that policy weight keeps")
         self.m, self.J, self.h = model, J, h
-        self.cache = cache
+        self.cache, self.policy, self.n_recent = cache, policy, n_recent
         self.device = torch.device(device)
         cap = capacity if capacity is not None else J + h   # chunked mode needs J + h
         self.cap = cap
@@ -95,6 +109,8 @@ class RefreshLoop:
         else:
             self.kv = cc.kv_contiguous(self.k, self.v, n_layers=L, layer_stride=hkv * cap * d,
                                        head_stride=cap * d, tok_stride=d)
+        if policy == "weight":
+            self.w = torch.zeros((1, hkv, cap), dtype=torch.float32, device=self.device)
         self.refreshes = 0
 
     # ---------------------------------------------------------------- inference side
@@ -118,6 +134,8 @@ class RefreshLoop:
         self.ids[sl].copy_(ids)
         self.pos[sl].copy_(pos)
         self.rows[sl].copy_(rows)
+        if self.policy == "weight":
+            self.w[:, :, sl].zero_()
         self.n += m
 
     # ---------------------------------------------------------------- refresh cycle
@@ -138,14 +156,21 @@ class RefreshLoop:
 
     def attend(self, layer: int, q: torch.Tensor) -> torch.Tensor:
         """Causal attention of the last m entries' queries q [m][Hq][head_dim] (rotated) over cache
-        layer `layer` (8-bit caches): the inference cycle's attention after its append."""
-        if self.cache != "e4m3":
-            raise ValueError("attend runs on 8-bit caches")
+        layer `layer`: the inference cycle's attention after its append.  With policy "weight" the
+        entries' sums take what the queries gave them."""
         m = int(q.shape[0])
         if m > self.n:
             raise ValueError(f"{m} queries for {self.n} entries")
         lens = torch.full((1,), self.n, dtype=torch.int32, device=self.device)
-        return cc.cc_attention_kv8(self._queued_problem(m), q, self.kv, layer, lens, self.n)
+        p = self._queued_problem(m)
+        if self.cache == "e4m3":
+            return cc.cc_attention_kv8(p, q, self.kv, layer, lens, self.n)
+        if self.policy != "weight":
+            return cc.cc_attention_kv(p, q, self.kv, layer, lens, self.n)
+        lse = torch.empty((m, self.m.n_heads_q), dtype=torch.float32, device=self.device)
+        o = cc.cc_attention_kv(p, q, self.kv, layer, lens, self.n, lse=lse)
+        cc.cc_attention_weights(p, q, self.kv, layer, lens, self.n, lse, self.w, prev=self.w)
+        return o
 
     def _scores8(self) -> torch.Tensor:
         """scores() on an 8-bit cache, step by step: attention, W_o, LM head."""
@@ -172,7 +197,10 @@ class RefreshLoop:
                          w_lm_packed=m.w_lm_packed)
 
     def scores(self) -> torch.Tensor:
-        """Counter-causal surprise of every cached entry (the last one is +inf)."""
+        """What a refresh keeps the highest of: the counter-causal surprise of every cached entry (the last one is
+        +inf), or its accumulated attention weight (the last n_recent are)."""
+        if self.policy == "weight":
+            return cc.cc_weight_scores(self._queued_problem(), self.w, self.n_recent, 0)
         if self.cache == "e4m3":
             return self._scores8()
         s = torch.empty(self.n, dtype=torch.float32, device=self.device)
@@ -193,6 +221,8 @@ class RefreshLoop:
         compact = cc.cc_compact_kv8 if self.cache == "e4m3" else cc.cc_compact_kv
         compact(p, self.kv, keep, [self.J], 0, token_ids=self.ids, pos_ids=self.pos)
         cc.cc_compact_rows(p, self.rows, keep, [self.J], 0)
+        if self.policy == "weight":
+            cc.cc_compact_weights(p, self.w, keep, [self.J], 0)
         self.n = self.J
         self.refreshes += 1
         return keep
