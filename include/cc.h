@@ -540,7 +540,8 @@ cc_status cc_attention_weights_workspace(const cc_problem* p, int32_t max_kv_len
  * it (or cc_attention_prefix: weights of the own entries) returned for the same queries.  prev (nullable: zeros) may
  * be out.  Entries at or past prev_lens[b] (device, nullable: none) have had nothing: prev is not read there, so that
  * entries appended since need no clearing.  Entries past kv_lens[b] are left as they are.  fp32 throughout; only
- * the keys of the cache are read.  One order of summation: the same call repeats bit for bit. */
+ * the keys of the cache are read.  One order of summation: the same call repeats bit for bit.  max_kv_len * n_heads_kv
+ * is up to 2^30 (some more are taken, others CC_ERR_UNSUPPORTED).  out overlaps nothing else but a prev that is the same. */
 cc_status cc_attention_weights(const cc_problem* p, const void* q, const cc_kv* kv, int32_t layer,
                                const int32_t* kv_lens, int32_t max_kv_len, const float* lse, const cc_weights* prev,
                                const int32_t* prev_lens, const cc_weights* out, void* workspace,

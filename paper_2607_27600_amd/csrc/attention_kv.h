@@ -92,6 +92,7 @@ struct KvWeightsArgs {
   // Sequences of more than W_FEW_ROWS rows: list[0 .. n_list), or (listed = 0) all there are.
   int n_list, listed;
   int32_t list[KV_LIST];
+  int seq0;                    // first sequence (of the list) of a launch
   int chunk, chunks;           // rows of a chunk (a multiple of W_ROWS), chunks of the longest sequence
   float* part;                 // sums of chunks to be added up (null: one chunk): [chunks][n_list][Hkv][max_len]
 };
@@ -108,6 +109,7 @@ struct WeightScoresArgs {
   float* scores;
   const int32_t* cu;
   int n_seqs, hkv, per_head, recent, frozen, longest;
+  int seq0;                    // first sequence of a launch
 };
 hipError_t launch_weight_scores(const WeightScoresArgs& a, hipStream_t s);
 

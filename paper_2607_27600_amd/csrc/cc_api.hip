@@ -1528,13 +1528,12 @@ cc_status weights_plan(const cc_problem* p, int max_len, WeightsPlan& c) {
     const double n = prompts ? m : std::max(max_len, m);
     tiles += (double(rows) / W_ROWS + 1) * ((n - 0.5 * m) / W_KEYS + 1) * hkv;
   }
-  const int64_t few = (int64_t(max_len) + 127) / 128 * hkv * p->n_seqs;
-  if (c.few && few > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
-  if (c.n == 0) return CC_OK;
+  // A sequence's workgroups are a launch's at most (sequences are shared out over launches).
+  if ((int64_t(max_len) + W_KEYS - 1) / W_KEYS * 2 * hkv > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+  if (c.n == 0 || max_len == 0) return CC_OK;
   c.listed = c.n <= KV_LIST;
   c.n_list = c.listed ? c.n : p->n_seqs;
   const int64_t planes = int64_t(c.n_list) * hkv;
-  if (blocks * planes > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
   // (a tile's rows by 32-bit offsets)
   if (int64_t(W_ROWS / g + 2) * p->n_heads_q * p->head_dim * 2 >= int64_t(1) << 32) return CC_ERR_UNSUPPORTED;
   // Chunks that make r rounds of two workgroups a CU, an item of a block ending half a chunk early, where a round costs
@@ -1551,7 +1550,7 @@ cc_status weights_plan(const cc_problem* p, int max_len, WeightsPlan& c) {
     }
   }
   if (least == 0) each = (most + W_ROWS - 1) / W_ROWS;   // workgroups enough without a cut
-  const int64_t room = std::max<int64_t>(1, std::min(MOST_GROUPS / (blocks * planes), (int64_t(1) << 26) / (planes * std::max(max_len, 1))));
+  const int64_t room = std::max<int64_t>(1, std::min(MOST_GROUPS / (2 * blocks * hkv), (int64_t(1) << 26) / (planes * std::max(max_len, 1))));
   each = std::max(each, ((most + W_ROWS - 1) / W_ROWS + room - 1) / room);
   c.chunk = int(std::min<int64_t>(each * W_ROWS, INT32_MAX / W_ROWS * W_ROWS));
   c.chunks = int((most + c.chunk - 1) / c.chunk);
@@ -1674,9 +1673,9 @@ cc_status cc_weight_scores(const cc_problem* p, const cc_weights* w, int32_t n_r
   if (n_tokens(p) == 0) return CC_OK;
   if (!scores) return CC_ERR_ARG;
   const int longest = max_len(p);
-  if ((int64_t(longest) + 255) / 256 * (per_head ? p->n_heads_kv : 1) * p->n_seqs > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
+  if ((int64_t(longest) + 255) / 256 * (per_head ? p->n_heads_kv : 1) > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
   const WeightScoresArgs a{w->base, w->seq_stride, w->head_stride, scores, p->cu_seqlens_d, p->n_seqs, p->n_heads_kv,
-                           per_head, n_recent, p->n_frozen, longest};
+                           per_head, n_recent, p->n_frozen, longest, 0};
   CC_HIP(launch_weight_scores(a, static_cast<hipStream_t>(stream)));
   return CC_OK;
 }

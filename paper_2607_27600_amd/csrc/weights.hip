@@ -46,7 +46,7 @@ __global__ __launch_bounds__(NT, 2) void weights_few(KvWeightsArgs a) {
   const unsigned blocks = unsigned(a.max_len + NW * KB * 16 - 1) / (NW * KB * 16);
   const int kvh = int(blockIdx.x % unsigned(a.hkv));
   const unsigned y = blockIdx.x / unsigned(a.hkv);
-  const int b = int(y / blocks), t0 = (int(y % blocks) * NW + wave) * KB * 16;
+  const int b = a.seq0 + int(y / blocks), t0 = (int(y % blocks) * NW + wave) * KB * 16;
   const int len = min(max(a.lens[b], 0), a.max_len);
   if (t0 >= len) return;
   const int q0 = a.cu[b], mq = a.cu[b + 1] - q0, rows = mq * a.g, shift = len - mq;
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(MANY_NT, 4) void weights_many(KvWeightsArgs a) {
   x /= unsigned(a.hkv);
   const int chunk = int(x % unsigned(a.chunks));
   x /= unsigned(a.chunks);
-  const int j = int(x / blocks), b = a.listed ? a.list[j] : j, first = int(x % blocks) * W_KEYS;
+  const int j = a.seq0 + int(x / blocks), b = a.listed ? a.list[j] : j, first = int(x % blocks) * W_KEYS;
   const int len = min(max(a.lens[b], 0), a.max_len);
   const int q0 = a.cu[b], mq = a.cu[b + 1] - q0, rows = mq * a.g, shift = len - mq;
   if (rows <= W_FEW_ROWS || first >= len) return;
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(NT) void add_chunks(KvWeightsArgs a, int blocks) {
   unsigned x = blockIdx.x;
   const int t = int(x % unsigned(blocks)) * NT + int(threadIdx.x);
   x /= unsigned(blocks);
-  const int kvh = int(x % unsigned(a.hkv)), j = int(x / unsigned(a.hkv)), b = a.listed ? a.list[j] : j;
+  const int kvh = int(x % unsigned(a.hkv)), j = a.seq0 + int(x / unsigned(a.hkv)), b = a.listed ? a.list[j] : j;
   const int len = min(max(a.lens[b], 0), a.max_len);
   const int mq = a.cu[b + 1] - a.cu[b], rows = mq * a.g, shift = len - mq;
   if (rows <= W_FEW_ROWS || t >= len) return;
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(NT) void weight_scores(WeightScoresArgs a, int bloc
   const int planes = a.per_head ? a.hkv : 1;
   const int h = int(blockIdx.x % unsigned(planes));
   const unsigned y = blockIdx.x / unsigned(planes);
-  const int b = int(y / unsigned(blocks)), t = int(y % unsigned(blocks)) * NT + int(threadIdx.x);
+  const int b = a.seq0 + int(y / unsigned(blocks)), t = int(y % unsigned(blocks)) * NT + int(threadIdx.x);
   const int q0 = a.cu[b], n = a.cu[b + 1] - q0;
   if (t >= n) return;
   const float* w = a.w + int64_t(b) * a.w_seq + t;
@@ -363,52 +363,63 @@ __global__ __launch_bounds__(MOVE_NT) void move_weights(CompactWeightsArgs a, We
   }
 }
 
+// f(arguments, workgroups) for as many sequences at a time as a launch has workgroups for, `each` of them a sequence (the
+// planner refuses more of these than a launch's).
+template <class A, class F>
+hipError_t by_sequences(A a, int n, int64_t each, F f) {
+  if (each > MOST_GROUPS) return hipErrorInvalidValue;
+  const int64_t step = MOST_GROUPS / std::max<int64_t>(1, each);
+  for (int64_t s = 0; s < n; s += step) {
+    a.seq0 = int(s);
+    f(a, unsigned(std::min(step, n - s) * each));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 }  // namespace
 
 hipError_t launch_weights_few(const KvWeightsArgs& a, hipStream_t s) {
   constexpr int KB = 2;
-  const int64_t blocks = (int64_t(a.max_len) + NW * KB * 16 - 1) / (NW * KB * 16) * a.hkv * a.n_seqs;
-  if (blocks > MOST_GROUPS) return hipErrorInvalidValue;   // (refused by the planner)
-  if (a.head_dim == 128)
-    hipLaunchKernelGGL((weights_few<128, KB>), dim3(unsigned(blocks)), dim3(NT), 0, s, a);
-  else
-    hipLaunchKernelGGL((weights_few<64, KB>), dim3(unsigned(blocks)), dim3(NT), 0, s, a);
-  return hipGetLastError();
+  const int64_t each = (int64_t(a.max_len) + NW * KB * 16 - 1) / (NW * KB * 16) * a.hkv;
+  return by_sequences(a, a.n_seqs, each, [&](const KvWeightsArgs& x, unsigned grid) {
+    if (a.head_dim == 128)
+      hipLaunchKernelGGL((weights_few<128, KB>), dim3(grid), dim3(NT), 0, s, x);
+    else
+      hipLaunchKernelGGL((weights_few<64, KB>), dim3(grid), dim3(NT), 0, s, x);
+  });
 }
 
 hipError_t launch_weights_many(const KvWeightsArgs& a, hipStream_t s) {
-  const int64_t planes = int64_t(a.n_list) * a.hkv;
-  const int64_t grid = (int64_t(a.max_len) + W_KEYS - 1) / W_KEYS * a.chunks * planes;
-  if (grid > MOST_GROUPS) return hipErrorInvalidValue;     // (refused by the planner)
-  if (a.head_dim == 128)
-    hipLaunchKernelGGL(weights_many<128>, dim3(unsigned(grid)), dim3(MANY_NT), 0, s, a);
-  else
-    hipLaunchKernelGGL(weights_many<64>, dim3(unsigned(grid)), dim3(MANY_NT), 0, s, a);
-  const hipError_t e = hipGetLastError();
+  const int64_t each = (int64_t(a.max_len) + W_KEYS - 1) / W_KEYS * a.chunks * a.hkv;
+  const hipError_t e = by_sequences(a, a.n_list, 2 * each, [&](const KvWeightsArgs& x, unsigned grid) {   // (of 512)
+    if (a.head_dim == 128)
+      hipLaunchKernelGGL(weights_many<128>, dim3(grid / 2), dim3(MANY_NT), 0, s, x);
+    else
+      hipLaunchKernelGGL(weights_many<64>, dim3(grid / 2), dim3(MANY_NT), 0, s, x);
+  });
   if (e != hipSuccess || !a.part) return e;
   const int blocks = (a.max_len + NT - 1) / NT;
-  hipLaunchKernelGGL(add_chunks, dim3(unsigned(blocks * planes)), dim3(NT), 0, s, a, blocks);
-  return hipGetLastError();
+  return by_sequences(a, a.n_list, int64_t(blocks) * a.hkv, [&](const KvWeightsArgs& x, unsigned grid) {
+    hipLaunchKernelGGL(add_chunks, dim3(grid), dim3(NT), 0, s, x, blocks);
+  });
 }
 
 hipError_t launch_weight_scores(const WeightScoresArgs& a, hipStream_t s) {
   const int blocks = (a.longest + NT - 1) / NT;
-  const int64_t grid = int64_t(blocks) * (a.per_head ? a.hkv : 1) * a.n_seqs;
-  if (grid > MOST_GROUPS) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(weight_scores, dim3(unsigned(grid)), dim3(NT), 0, s, a, blocks);
-  return hipGetLastError();
+  return by_sequences(a, a.n_seqs, int64_t(blocks) * (a.per_head ? a.hkv : 1), [&](const WeightScoresArgs& x, unsigned grid) {
+    hipLaunchKernelGGL(weight_scores, dim3(grid), dim3(NT), 0, s, x, blocks);
+  });
 }
 
 hipError_t launch_compact_weights(const CompactWeightsArgs& a, hipStream_t s) {
   const bool in_place = a.out == a.w;
   const int64_t n = int64_t(a.n_seqs) * (a.per_head ? a.hkv : 1);
   int64_t off = 0;
-  int longest = 0;
-  for (int64_t i = 0; i < n; ++i) longest = std::max(longest, a.k_h[i]);
-  // the lists of a launch, of fewer than 2^32 threads
-  const int64_t each = (a.per_head ? 1 : a.hkv) * (in_place ? 1 : (int64_t(longest) + MOVE_NT * PER - 1) / (MOVE_NT * PER));
-  if (each > MOST_GROUPS / 4) return hipErrorInvalidValue;
-  const int64_t step = std::min<int64_t>(WeightLists::MOST, MOST_GROUPS / 4 / std::max<int64_t>(1, each));
+  // the lists of a launch, of fewer than 2^32 threads; planes that leave each a workgroup at the least
+  const int64_t planes = a.per_head ? 1 : a.hkv;
+  if (planes > MOST_GROUPS / 4) return hipErrorInvalidValue;   // (refused at the entry)
+  const int64_t step = std::min<int64_t>(WeightLists::MOST, MOST_GROUPS / 4 / planes);
   for (int64_t first = 0; first < n; first += step) {
     const int here = int(std::min<int64_t>(step, n - first));
     WeightLists lists;
@@ -420,8 +431,9 @@ hipError_t launch_compact_weights(const CompactWeightsArgs& a, hipStream_t s) {
       most = std::max(most, lists.k[i]);
     }
     if (most == 0) continue;
-    const int chunks = in_place ? 1 : int((int64_t(most) + MOVE_NT * PER - 1) / (MOVE_NT * PER));
-    const int64_t grid = int64_t(here) * (a.per_head ? 1 : a.hkv) * chunks;
+    const int64_t cut = (int64_t(most) + MOVE_NT * PER - 1) / (MOVE_NT * PER), room = MOST_GROUPS / 4 / (here * planes);
+    const int chunks = in_place ? 1 : int(std::min(cut, room));
+    const int64_t grid = here * planes * chunks;
     hipLaunchKernelGGL(move_weights, dim3(unsigned(grid)), dim3(MOVE_NT), 0, s, a, lists, int(first), chunks, int(in_place));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -231,7 +231,7 @@ def test_many_sequences():
     _same(*_run(cc, cache, q, new, lens, hq, hkv, **kw), _oracle(cache, q, new, lens, hq, hkv, **kw))
 
 
-@pytest.mark.parametrize("scale", [1.0, 0.01, 1e-20, 1e-38])
+@pytest.mark.parametrize("scale", [1.0, 0.01, 1e-20, 1e-38, 1e-40])
 @pytest.mark.parametrize("new,lens,hq,hkv,d", [([1, 3], [200, 77], 8, 2, 128), ([70, 40], [300, 90], 4, 2, 64)])
 def test_a_scale_of_the_callers(new, lens, hq, hkv, d, scale):
     from paper_2607_27600_amd import cc
@@ -320,3 +320,147 @@ def test_what_is_not_finite_in_a_prefix(n, value):
     hit[41:, 2:, 17] = True
     np.testing.assert_array_equal(~np.isfinite(o), hit)
     assert_attention_close(np.where(hit, 0, o), np.where(hit, 0, clean))
+
+
+def test_a_plan_for_no_entries():
+    """max_kv_len 0: every length is cut to it, every output is zero and no page is looked up; the prefix alone is seen."""
+    from paper_2607_27600_amd import cc
+    new, hq, hkv, d = [1, 40, 2, 300], 4, 2, 128
+    cache = Cache16([9, 40, 2, 300], hkv, d, page=16, seed=61)
+    cache.bt.fill_(-(1 << 30))
+    q = queries(new, hq, d, 62)
+    o, lse = _run(cc, cache, q, new, [9, 40, 2, 300], hq, hkv, longest=0)
+    assert torch.count_nonzero(o) == 0 and torch.isneginf(lse).all()
+    for n in (50, 3000):
+        pre = Cache16([n], hkv, d, page=16, seed=63)
+        kw = dict(pre=pre, first=[0, 4], pre_lens=[n])
+        o, lse = _run(cc, cache, q, new, [9, 40, 2, 300], hq, hkv, longest=0, **kw)
+        empty = Cache16([0] * 4, hkv, d, page=16, seed=64)
+        _same(o, lse, _oracle(empty, q, new, [0] * 4, hq, hkv, **kw))
+    pre.bt.fill_(-(1 << 30))
+    o, lse = _run(cc, cache, q, new, [9, 40, 2, 300], hq, hkv, longest=0, pre_longest=0, **kw)
+    assert torch.count_nonzero(o) == 0 and torch.isneginf(lse).all()
+
+
+@pytest.mark.parametrize("new", [[1], [40], [150], [1, 3, 200]])
+@pytest.mark.parametrize("prefix", [0, 60, 2000])
+def test_a_query_that_is_not_finite(new, prefix):
+    """It spoils its own outputs and no other row's."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d = 4, 2, 128
+    lens = [m + 30 for m in new]
+    cache = Cache16(lens, hkv, d, page=16, seed=67)
+    q = queries(new, hq, d, 68)
+    kw = dict(pre=Cache16([prefix], hkv, d, page=16, seed=69), first=[0, len(new)], pre_lens=[prefix]) if prefix else {}
+    want, lse, tol = _oracle(cache, q, new, lens, hq, hkv, **kw)
+    q[sum(new) // 2, 1, 7] = float("nan")
+    o, got = _run(cc, cache, q, new, lens, hq, hkv, **kw)
+    hit = np.zeros(lse.shape, bool)
+    hit[sum(new) // 2, 1] = True
+    np.testing.assert_array_equal(np.isnan(f64(got)), hit)
+    np.testing.assert_array_equal(np.isnan(f64(o)), np.broadcast_to(hit[..., None], want.shape))
+    assert_attention_close(np.where(hit[..., None], 0, f64(o)), np.where(hit[..., None], 0, want))
+
+
+@pytest.mark.parametrize("new,hq,hkv,d", [([8] * 3, 16, 4, 128), ([8, 5], 16, 4, 64), ([1] * 40, 8, 8, 128)])
+def test_few_rows_in_a_graph(new, hq, hkv, d):
+    """Shares of the work of one and two row blocks, captured and replayed as the lengths change, from pieces to shares."""
+    from paper_2607_27600_amd import cc
+    cache = Cache16([3000] * len(new), hkv, d, page=16, seed=71)
+    q, kv, lens = queries(new, hq, d, 72), cache.view(cc), i32([2000] * len(new))
+    p = problem(cc, new, hq, hkv, d)
+    o, lse = torch.empty_like(q), torch.empty(sum(new), hq, device="cuda")
+    ws = torch.empty(max(1, cc.cc_attention_kv_workspace(p, 3000)), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cc.cc_attention_kv(p, q, kv, 0, lens, 3000, o, lse=lse, workspace=ws)
+    r = np.random.default_rng(73)
+    for most in (3000, 45, 700, 2999):
+        now = [int(x) for x in r.integers(min(most, 8), most + 1, len(new))]
+        lens.copy_(i32(now))
+        o.fill_(9.0)
+        ws.fill_(0x7f)
+        g.replay()
+        torch.cuda.synchronize()
+        _same(o, lse, _oracle(cache, q, new, now, hq, hkv), str(most))
+
+
+@pytest.mark.parametrize("n,most,hkv", [(150, 5000, 2), (700, 3000, 1), (70, 4000, 3)])
+def test_shares_of_many_sequences(n, most, hkv):
+    """Work shared out over more sequences than a wave has lanes and than are listed; rows whose entries lie in one share,
+    in a few and in many."""
+    from paper_2607_27600_amd import cc
+    d, hq = 64, 2 * hkv
+    r = np.random.default_rng(n)
+    new = [int(x) for x in r.choice([0, 1, 1, 3], n)]
+    lens = [m + int(x) for m, x in zip(new, r.integers(0, 30, n))]
+    lens[n // 3], lens[n - 1], new[n // 3], new[n - 1] = most, most - 1, 1, 2
+    new[5], lens[5] = 40, 500            # one of many rows
+    cache = Cache16(lens, hkv, d, page=16 if n == 150 else 0, seed=n + 1, fill=0.0)
+    q = queries(new, hq, d, n + 2)
+    want = _oracle(cache, q, new, lens, hq, hkv)
+    _same(*_run(cc, cache, q, new, lens, hq, hkv), want)
+
+
+def test_two_calls_at_once():
+    """Two streams, each with its own workspace and outputs; nothing is shared."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d, new, lens = 8, 2, 128, [1, 40, 3], [3000, 900, 2500]
+    cache, pre = Cache16(lens, hkv, d, page=16, seed=75), Cache16([2000], hkv, d, page=16, seed=76)
+    qs = [queries(new, hq, d, s) for s in (77, 78)]
+    p, kv, x, ld = problem(cc, new, hq, hkv, d), cache.view(cc), cc.prefix(pre.view(cc), [0, 3], i32([2000]), 2000), i32(lens)
+    want = [(cc.cc_attention_kv(p, q, kv, 0, ld, 3000), cc.cc_attention_prefix(p, q, x, kv, 0, ld, 3000)) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    got = []
+    for _ in range(5):
+        for q, s in zip(qs, streams):
+            got.append((cc.cc_attention_kv(p, q, kv, 0, ld, 3000, stream=s), cc.cc_attention_prefix(p, q, x, kv, 0, ld, 3000, stream=s)))
+    torch.cuda.synchronize()
+    for i, pair in enumerate(got):
+        for a, b in zip(pair, want[i % 2]):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_offsets_past_32_bits(new, memory_given_back):
+    """Entries 64 KiB apart, the ones that count beyond 4 GiB of their plane."""
+    from paper_2607_27600_amd import cc
+    n, d, hq, tok = 70000, 64, 4, 1 << 15
+    free, _ = torch.cuda.mem_get_info()
+    if free < (14 << 30):
+        pytest.skip("needs 14 GiB of device memory")
+    pools = {t: torch.zeros(n * tok, dtype=torch.bfloat16, device="cuda") for t in "kv"}
+    rows = {t: x.view(n, tok)[:, :d] for t, x in pools.items()}
+    g = torch.Generator().manual_seed(79)
+    head, tail = 48, 500
+    for t in "kv":
+        rows[t][:head] = torch.randn(head, d, generator=g).to(torch.bfloat16).cuda()
+        rows[t][n - tail:] = torch.randn(tail, d, generator=g).to(torch.bfloat16).cuda()
+    rows["k"][head:n - tail] = -300.0            # (so far from the queries that they weigh nothing)
+    q = torch.randn(new, hq, d, generator=g).abs().to(torch.bfloat16).cuda()
+    kv = cc.kv_contiguous(pools["k"], pools["v"], n_layers=1, layer_stride=0, head_stride=0, tok_stride=tok)
+    p, lens = problem(cc, [new], hq, 1, d), i32([n])
+    lse = torch.empty(new, hq, device="cuda")
+    o = cc.cc_attention_kv(p, q, kv, 0, lens, n, lse=lse)
+    w = cc.cc_attention_weights(p, q, kv, 0, lens, n, lse, torch.full((1, 1, n), 7.0, device="cuda"))
+    torch.cuda.synchronize()
+    ends = np.r_[0:head, n - tail:n]
+    k, v, qh = (f64(rows[t][torch.from_numpy(ends).cuda()]) for t in "kv"), None, f64(q)
+    k, v = k
+    ref, sums = np.zeros((new, hq, d)), np.zeros(len(ends))
+    for h in range(hq):
+        ref[:, h], r = O.attention(qh[:, h], k, v)
+        sums += O.weights(qh[:, h], k, r)
+    assert_attention_close(f64(o), ref)
+    got = f64(w)[0, 0]
+    np.testing.assert_allclose(got[ends], sums, rtol=2.0 ** -12, atol=1e-9)
+    assert np.all(got[head:n - tail] == 0)
+    # as a prefix
+    x = cc.prefix(kv, [0, 1], lens, n)
+    one = cc.kv_contiguous(pools["k"], pools["v"], n_layers=1, layer_stride=0, head_stride=0, tok_stride=tok)
+    o = cc.cc_attention_prefix(p, q, x, one, 0, i32([0]), 0)
+    torch.cuda.synchronize()
+    full = np.stack([O.attention(qh[:, h], np.zeros((0, d)), np.zeros((0, d)), k, v)[0] for h in range(hq)], 1)
+    assert_attention_close(f64(o), full)

@@ -247,3 +247,85 @@ def test_weights_in_chunks(new, lens, hq, hkv, d, page):
             err = np.abs(f64(got[0])[b, :, :m] - ref)
             assert np.all(err <= tol[b, :, :m] + 2.0 ** -24 * np.abs(ref)), (longest, b, err.max())
             assert (got[0][b, :, m:] == 7).all()
+
+
+@pytest.mark.parametrize("new,most", [([1, 4], 300), ([70, 1], 900), ([400], 1500)])
+def test_a_cycle_in_two_graphs(new, most):
+    """Attention and its weights in place, captured twice with one workspace and replayed in turn as the lengths advance."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d = 8, 2, 64
+    cache = Cache16([most] * len(new), hkv, d, page=16, seed=81)
+    q, kv, p = queries(new, hq, d, 82), cache.view(cc), problem(cc, new, hq, hkv, d)
+    ws = torch.empty(max(1, cc.cc_attention_kv_workspace(p, most), cc.cc_attention_weights_workspace(p, most)),
+                     dtype=torch.uint8, device="cuda")
+    lens, had = i32(new), i32([0] * len(new))
+    lse, w = torch.empty(sum(new), hq, device="cuda"), torch.full((len(new), hkv, most), float("nan"), device="cuda")
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            cc.cc_attention_kv(p, q, kv, 0, lens, most, lse=lse, workspace=ws)
+            cc.cc_attention_weights(p, q, kv, 0, lens, most, lse, w, prev=w, prev_lens=had, workspace=ws)
+        graphs.append(g)
+    want, tol, had_h = np.zeros(w.shape), np.zeros(w.shape), [0] * len(new)
+    for step in range(4):
+        now = [min(most, m * (step + 1) + 37 * step) for m in new]
+        lens.copy_(i32(now))
+        had.copy_(i32(had_h))
+        ws.fill_(0x7f)
+        graphs[step % 2].replay()
+        torch.cuda.synchronize()
+        _, x, t = _oracle(cache, q, new, now, hq, hkv)
+        longest = x.shape[2]
+        want[:, :, :longest] += x
+        # (the kernel's own lse is off by the logits' error and its sum's, what the bound counts once already)
+        tol[:, :, :longest] += 2 * t + 2.0 ** -22 * want[:, :, :longest]
+        got = f64(w)
+        for b, n in enumerate(now):
+            assert np.all(np.abs(got[b, :, :n] - want[b, :, :n]) <= tol[b, :, :n]), (step, b)
+            assert np.isnan(got[b, :, n:]).all()
+        had_h = now
+
+
+def test_a_query_that_is_not_finite_reaches_the_entries_it_sees():
+    from paper_2607_27600_amd import cc
+    hq, hkv, d = 4, 2, 64
+    for new, n, bad in (([3], 50, 1), ([200], 700, 100)):
+        cache, q = Cache16([n], hkv, d, page=16, seed=83), queries(new, hq, d, 84)
+        lse, want, tol = _oracle(cache, q, new, [n], hq, hkv)
+        q[bad, 3, 5] = float("nan")          # of the second KV head's group
+        w = torch.full((1, hkv, n), 7.0, device="cuda")
+        cc.cc_attention_weights(problem(cc, new, hq, hkv, d), q, cache.view(cc), 0, i32([n]), n, torch.from_numpy(lse).cuda(), w)
+        torch.cuda.synchronize()
+        hit = np.zeros((hkv, n), bool)
+        hit[1, :n - new[0] + bad + 1] = True
+        np.testing.assert_array_equal(np.isnan(f64(w)[0]), hit)
+        assert np.all(np.abs(f64(w)[0] - want[0])[~hit] <= tol[0][~hit])
+
+
+def test_weights_in_other_layouts():
+    """Heads outermost, sequences spread, one earlier weight for all heads; the gaps stay as they are."""
+    from paper_2607_27600_amd import cc
+    new, lens, hq, hkv, d = [2, 90], [40, 300], 4, 2, 128
+    cache, q = Cache16(lens, hkv, d, page=16, seed=85), queries(new, hq, d, 86)
+    lse, want, tol = _oracle(cache, q, new, lens, hq, hkv)
+    room = torch.full((hkv, 3, 333), 7.0, device="cuda")
+    w = room[:, :2, :300].permute(1, 0, 2)
+    prev = torch.rand(2, 1, 300, generator=torch.Generator().manual_seed(87)).cuda().expand(2, hkv, 300)
+    cc.cc_attention_weights(problem(cc, new, hq, hkv, d), q, cache.view(cc), 0, i32(lens), 300, torch.from_numpy(lse).cuda(), w,
+                            prev=prev)
+    torch.cuda.synchronize()
+    got = f64(room)
+    for b, n in enumerate(lens):
+        ref = want[b, :, :n] + f64(prev)[b, :, :n]
+        assert np.all(np.abs(got[:, b, :n] - ref) <= tol[b, :, :n] + 2.0 ** -24 * np.abs(ref))
+        assert (got[:, b, n:] == 7).all()
+    assert (got[:, 2] == 7).all()
+    # and compacted out of them
+    keep = [0, 7, 39, 5, 299]
+    out = torch.full((2, hkv, 8), 3.0, device="cuda")
+    cc.cc_compact_weights(problem(cc, lens, hkv, hkv, d), w, i32(keep), [3, 2], 0, out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0, :, :3], w[0][:, keep[:3]]) and torch.equal(out[1, :, :2], w[1][:, keep[3:]])
+    assert (out[0, :, 3:] == 3).all() and (out[1, :, 2:] == 3).all()

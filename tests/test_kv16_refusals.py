@@ -143,6 +143,21 @@ def test_workspaces():
             assert _attention(p=p, kv=long, longest=1 << 20, ws=P + 16, size=n.value, pre=pre) == cc.CC_ERR_ARG
 
 
+@pytest.mark.parametrize("cu", [(0, 0, 0), (0, 1, 2), (0, 40, 700), (0, 5000, 5001)])
+@pytest.mark.parametrize("longest", [0, 1, 1 << 24, 2 ** 31 - 4097])
+def test_workspaces_of_the_shortest_and_longest_plans(cu, longest):
+    """(A division by the number of blocks would end the process.)"""
+    n = ctypes.c_size_t(0)
+    p, kv = _problem(cu=cu), _kv(paged=False)
+    for call in (lambda: cc._lib.cc_attention_kv_workspace(_ref(p), longest, ctypes.byref(n)),
+                 lambda: cc._lib.cc_attention_prefix_workspace(_ref(p), _ref(_prefix(kv=kv, max_len=longest)), longest, ctypes.byref(n)),
+                 lambda: cc._lib.cc_attention_weights_workspace(_ref(p), longest, ctypes.byref(n))):
+        n.value = 0
+        st = call()
+        assert st == cc.CC_OK or (longest > 1 << 24 and st == cc.CC_ERR_UNSUPPORTED)
+        assert n.value < 1 << 36
+
+
 def test_no_queries_need_nothing():
     assert _attention(p=_problem(cu=(0, 0, 0)), q=None, o=None, lens=None, lse=None, ws=None, size=0) == cc.CC_OK
 
