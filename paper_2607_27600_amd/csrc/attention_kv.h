@@ -48,9 +48,9 @@ struct KvAttnArgs {
   float2* fpart_ml;
   int2* fpart_at;              // [n_list * Hkv] first and last workgroup that has some of a (sequence, head)'s entries
   // Many rows.  Row blocks of the sequences of many rows: listed by value, longest first, or (items.n_seqs = 0)
-  // sequence b has those from cu[b] g / KV_ROWS + b on, more than its rows need.
+  // sequence b has those from cu[b] g / KV_ROWS + b on, more than its rows need.  Those of up to `few` rows are left out.
   AttnMany items;
-  int blocks;
+  int blocks, few;
   int piece, splits;           // entries of a piece (a multiple of KV_KEYS), pieces of the longest sequence
   // Results to be joined (null: none), outputs and (maximum, sum): [splits][Hkv][N g]
   float* part;

@@ -190,7 +190,7 @@ __device__ __forceinline__ void group(const KvAttnArgs& a, unsigned x, u16* kb0,
       q0 = a.cu[b];
       m = a.cu[b + 1] - q0;
     }
-    if (m * a.g <= FEW_ROWS) return;
+    if (m * a.g <= a.few) return;
     len = min(max(a.lens[b], 0), a.max_len);
   }
   const int rows = m * a.g, row0 = rb * KV_ROWS;

@@ -29,12 +29,12 @@ __global__ __launch_bounds__(256) void attn_join(KvAttnArgs a, int64_t group0) {
   const int query = int(r / a.g);
   const int b = last_at(a.n_seqs, [&](int i) { return int64_t(a.cu[i]); }, query);
   const int q0 = a.cu[b], m = a.cu[b + 1] - q0, rows = m * a.g;
-  if (rows <= FEW_ROWS) return;
+  if (rows <= a.few) return;
   const int len = min(max(a.lens[b], 0), a.max_len);
   // the pieces that the row's block has
   const int block = int(r - int64_t(q0) * a.g) / KV_ROWS;
   const int see = min(len, max(0, len - m + (min((block + 1) * KV_ROWS, rows) - 1) / a.g + 1));
-  const int n = max(1, (see + a.piece - 1) / a.piece);
+  const int n = max(see - 1, 0) / a.piece + 1;
   Joined j{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
   for (int i0 = 0; i0 < n; i0 += 4) {   // four in flight
     float2 p[4];

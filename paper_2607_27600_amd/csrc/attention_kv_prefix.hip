@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256) void attn_rows_join(KvAttnArgs a, int64_t grou
   const int64_t rows = int64_t(mq) * a.g;
   if (rows > a.most) return;
   const int row = (query - q0) * a.g + h % a.g;
-  const int own = max(1, (rows_see(a, mq, min(max(a.lens[b], 0), a.max_len), row & ~15) + a.rpiece - 1) / a.rpiece);
+  const int own = max(rows_see(a, mq, min(max(a.lens[b], 0), a.max_len), row & ~15) - 1, 0) / a.rpiece + 1;
   const int j = prefix_of(a, b);
   const PrefixRow p = prefix_row(a, j, kvh, int64_t(q0 - a.cu[a.pre_first[j]]) * a.g + row);
   const int n = p.n + own;

@@ -1330,6 +1330,7 @@ struct KvMany {
 struct KvPlan {
   bool rows = false;           // all by 16 rows a workgroup
   bool inside = false;         // which takes the prefix's entries too
+  bool along = false;          // few rows: with the others
   int n_few = 0, n_list = 0, listed = 0, R = 0, parts = 0;
   bool direct = false;         // few rows: by 16 rows a workgroup
   int32_t list[KV_LIST];
@@ -1355,19 +1356,24 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
   const int g = p->n_heads_q / p->n_heads_kv, hkv = p->n_heads_kv;
   const int longest = int(std::min<int64_t>(INT32_MAX, int64_t(max_len) + (x ? x->max_len : 0)));
   int64_t blocks16 = 0;
-  bool many = false;
+  int64_t few = 0, many = 0;   // sequences of few rows, blocks of the others
   for (int b = 0; b < p->n_seqs; ++b) {
     const int64_t rows = int64_t(p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) * g;
     blocks16 += (rows + 15) / 16;
-    many |= rows > FEW_ROWS;
+    if (rows > FEW_ROWS)
+      many += (rows + KV_ROWS - 1) / KV_ROWS;
+    else
+      few += rows > 0;
   }
   c.rows = (many || x) && longest <= KV_SHORT && blocks16 * hkv <= KV_SHORT_GROUPS;
+  // A few short prompts beside long ones go along as blocks of 128 rows.
+  c.along = !x && !c.rows && few * 4 <= many && max_len <= ::max_len(p);
   c.inside = x && c.rows;
   for (int b = 0; b < p->n_seqs; ++b) {
     const int seq0 = p->cu_seqlens_h[b], m = p->cu_seqlens_h[b + 1] - seq0;
     const int64_t rows = int64_t(m) * g;
     if (rows == 0) continue;
-    if (rows <= FEW_ROWS || c.rows) {
+    if ((rows <= FEW_ROWS && !c.along) || c.rows) {
       if (c.n_few < KV_LIST) c.list[c.n_few] = b;
       ++c.n_few;
       c.R = int(std::max<int64_t>(c.R, rows));
@@ -1458,6 +1464,7 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
   auto many = [&](const KvMany& m) {
     a.items = m.items;
     a.blocks = int(m.blocks);
+    a.few = c.along ? 0 : FEW_ROWS;
     a.piece = m.piece;
     a.splits = m.splits;
     a.part = m.total ? reinterpret_cast<float*>(at(ws, off)) : nullptr;

@@ -464,3 +464,19 @@ def test_offsets_past_32_bits(new, memory_given_back):
     torch.cuda.synchronize()
     full = np.stack([O.attention(qh[:, h], np.zeros((0, d)), np.zeros((0, d)), k, v)[0] for h in range(hq)], 1)
     assert_attention_close(f64(o), full)
+
+
+@pytest.mark.parametrize("new,lens,hq,hkv,d,page", [
+    ([1500, 1, 3, 700, 0], [1500, 1, 3, 700, 40], 28, 4, 128, 16),
+    ([1, 1200, 2], [1199, 1200, 2], 4, 1, 64, 0),                       # a token behind as many entries as a prompt has
+    ([300] + [40, 1] * 24 + [1100], [300] + [40, 1] * 24 + [1100], 8, 2, 64, 16),   # more than a launch lists
+    ([1100] + [1] * 40, [1100] + list(range(1, 41)), 8, 2, 128, 32),    # more short ones than go along
+])
+@pytest.mark.parametrize("more", [0, 300])
+def test_short_prompts_beside_long_ones(new, lens, hq, hkv, d, page, more):
+    """Sequences of few rows in a call of prompts, which go along with them where no cache is longer than a prompt."""
+    from paper_2607_27600_amd import cc
+    cache = Cache16(lens, hkv, d, page=page, seed=91, room=more)
+    q = queries(new, hq, d, 92)
+    want = _oracle(cache, q, new, lens, hq, hkv)
+    _same(*_run(cc, cache, q, new, lens, hq, hkv, longest=max(lens) + more), want)
