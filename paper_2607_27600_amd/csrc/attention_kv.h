@@ -50,7 +50,7 @@ struct KvAttnArgs {
   // Many rows.  Row blocks of the sequences of many rows: listed by value, longest first, or (items.n_seqs = 0)
   // sequence b has those from cu[b] g / KV_ROWS + b on, more than its rows need.  Those of up to `few` rows are left out.
   AttnMany items;
-  int blocks, few;
+  int blocks, few, ends;       // ends: row blocks * Hkv of listed sequences of few rows
   int piece, splits;           // entries of a piece (a multiple of KV_KEYS), pieces of the longest sequence
   // Results to be joined (null: none), outputs and (maximum, sum): [splits][Hkv][N g]
   float* part;

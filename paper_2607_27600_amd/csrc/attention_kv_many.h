@@ -169,12 +169,13 @@ __device__ __forceinline__ void group(const KvAttnArgs& a, unsigned x, u16* kb0,
     kvh = p.item % a.hkv;
     piece = p.tiles * BN;
   } else {
-    // Heaviest blocks first: the last rows of the longest sequences.
+    // Heaviest blocks first: the last rows of the longest sequences, but before them those of sequences of few rows, whose
+    // caches may be as long as any (the last ones of the list).
     split = int(x % unsigned(a.splits));
     piece = a.piece;
     x /= unsigned(a.splits);
     if (a.items.n_seqs) {
-      const AttnItem w = a.items.item(int(x));
+      const AttnItem w = a.items.item(int(x) < a.ends ? a.blocks * a.hkv - a.ends + int(x) : int(x) - a.ends);
       b = w.seq;
       kvh = w.kvh;
       q0 = w.seq0;
