@@ -9,6 +9,9 @@ namespace {
 
 // ------------------------------------------------------------------ whole rows
 
+// A workgroup's waves share out the entries of 16 rows and meet in LDS: one launch, nothing to join.  Bound by the chain of loads:
+// a prompt of 200 tokens, 32 heads on 8, 8.1 us (400 workgroups); four tokens behind 900 entries each 13.4, 32 workgroups, each
+// of 460 KB at some 60 GB/s.
 template <int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_rows(KvAttnArgs a) {
   __shared__ float lds[NW * 16 * HD];
@@ -18,6 +21,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_rows(KvAttnArgs a) {
 
 // ------------------------------------------------------------------ few rows, work shared out
 
+// Single tokens and drafts over long caches: every workgroup takes an equal share of all (sequence, head)s' entries, two workgroups
+// a CU.  Bound by the bytes of the cache: 48 ragged sequences of up to 15987 entries, 28 heads on 4, 94 us (5.2 TB/s) and 6 for
+// the join; one of 2048, 32 heads on 8, is a chain of loads, 8 us and 4.
 constexpr int FEW_NT = 256;
 template <int HD, int NR>
 __global__ __launch_bounds__(FEW_NT, 2) void attn_few(KvAttnArgs a) {

@@ -1,6 +1,10 @@
 // The pass over the prefixes that runs of sequences share, and with it, in the same launch, over the own entries of the
-// sequences of few rows, in pieces of rpiece; a second launch joins the two.  (One after the other, for 40 sequences behind
-// 16000 entries, 24 and 25 us, either with half of the card's slots empty.)
+// sequences of few rows, in pieces of rpiece; a second launch joins the two.  A prefix is read for 128 rows of its run at a time,
+// whatever their sequences, so what the run's sequences would each read is read some once.
+//
+// 40 sequences of one token behind 16000 entries, 28 heads on 4: 32 us and 7 for the join (one after the other the two passes take 24
+// and 25, either with half of the card's slots empty); 24 of six tokens behind 30001 and 6000, 32 heads on 8, 80 and 10.  Bound by
+// what comes beside the tiles: their load before the first, and outputs in fp32 that go out to be joined (14 and 37 MB).
 #include <algorithm>
 
 #include "attention_kv_many.h"

@@ -2,7 +2,8 @@
 // the query's prefix and its sequence's own up to the query's, c = h / g, and the log-sum-exp of each row.
 //
 // A row is one (query, query head of the group) pair, so the g heads that share a KV head share every entry
-// that is read.  A wave streams entries from memory into MFMA operands, no LDS in the loop.
+// that is read.  A wave streams entries from memory into MFMA operands, no LDS in the loop: few rows are bound by the bytes of
+// their entries, which pass once, and a step's 16 KB in registers are what a wave keeps in flight.
 //
 // S^T = K Q^T on 16x16x32 MFMA, entries as its rows, so that a lane holds four entries of one row of
 // queries in each 16-entry group, and the two groups of a step are the eight k-slots of its P operand:

@@ -49,6 +49,8 @@ struct Total {
 
 // ------------------------------------------------------------------ few rows
 
+// Each wave for 32 entries, whose rows it reads for itself.  Bound by the bytes of the keys: 64 sequences of 4000 entries, 28 heads
+// on 4, 45 us (5.8 TB/s); eight ragged ones of up to 12001 10 us, a chain of four loads.
 template <int HD, int KB>
 __global__ __launch_bounds__(NT, 2) void weights_few(KvWeightsArgs a) {
   constexpr int NKS = HD / 32;
@@ -333,6 +335,7 @@ __global__ __launch_bounds__(NT) void add_chunks(KvWeightsArgs a, int blocks) {
   Total(a, b, kvh, len).put(t, y);
 }
 
+// A score a thread: 768 entries, 4 heads, 2.4 us, the launch and one chain of loads.
 __global__ __launch_bounds__(NT) void weight_scores(WeightScoresArgs a, int blocks) {
   const int planes = a.per_head ? a.hkv : 1;
   const int h = int(blockIdx.x % unsigned(planes));
@@ -358,7 +361,8 @@ struct WeightLists {
 };
 constexpr int MOVE_NT = 1024, PER = 4;
 // A workgroup a plane (in place) or a chunk of one: chunks of 4096 entries.  In place, lists rise, so keep[j] >= j: what
-// a chunk writes lies before every later chunk's sources.
+// a chunk writes lies before every later chunk's sources.  4 bytes an entry kept beside the 512 of its keys and values: 512 of 768,
+// 4 heads, 2.8 us, the launch and two dependent loads.
 __global__ __launch_bounds__(MOVE_NT) void move_weights(CompactWeightsArgs a, WeightLists lists, int first, int chunks, int in_place) {
   const int plane = int(blockIdx.x / unsigned(chunks)), chunk = int(blockIdx.x % unsigned(chunks));
   const int l = a.per_head ? plane : plane / a.hkv;
