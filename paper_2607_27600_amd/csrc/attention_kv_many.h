@@ -175,6 +175,7 @@ __device__ __forceinline__ void group(const KvAttnArgs& a, unsigned x, u16* kb0,
   } else {
     // Heaviest blocks first: the last rows of the longest sequences, but before them those of sequences of few rows, whose
     // caches may be as long as any (the last ones of the list).
+    if (gridDim.x <= 512 && x >= 256) x = gridDim.x + 255 - x;
     split = int(x % unsigned(a.splits));
     piece = a.piece;
     x /= unsigned(a.splits);
