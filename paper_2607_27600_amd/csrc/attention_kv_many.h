@@ -11,7 +11,8 @@
 //
 // Bound by the clock that the card's power allows: a prompt of 16384, 32 heads on 8, 1.87 to 2.09 ms by box (1.05 to 1.18 PFLOP/s,
 // matrix cores busy in 66% of the cycles).  Short prompts are bound by what a block takes to begin and end beside its tiles,
-// some 8 us: eight of 1024, 28 heads on 4, 93 us (0.65 PFLOP/s); prompts of 97 to 4001 tokens together 204 to 222 (0.9).
+// some 8 us: eight of 1024, 28 heads on 4, 93 us (0.65 PFLOP/s); prompts of 97 to 4001 tokens together 204 to 222 (0.9).  Loads
+// are not what a tile waits for: a barrier between the products, so that each has half a step more to land, took 0 to 10% longer.
 //
 // Where few workgroups come of it, the entries are cut into pieces, whose results a launch of its own joins.
 //
@@ -175,6 +176,8 @@ __device__ __forceinline__ void group(const KvAttnArgs& a, unsigned x, u16* kb0,
   } else {
     // Heaviest blocks first: the last rows of the longest sequences, but before them those of sequences of few rows, whose
     // caches may be as long as any (the last ones of the list).
+    // Where all are resident at once, two a CU, the second ones begin with the lightest (a prompt of 2048, 32 heads on 8, 47.4 us
+    // for 49.9).
     if (gridDim.x <= 512 && x >= 256) x = gridDim.x + 255 - x;
     split = int(x % unsigned(a.splits));
     piece = a.piece;
