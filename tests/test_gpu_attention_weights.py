@@ -329,3 +329,27 @@ def test_weights_in_other_layouts():
     torch.cuda.synchronize()
     assert torch.equal(out[0, :, :3], w[0][:, keep[:3]]) and torch.equal(out[1, :, :2], w[1][:, keep[3:]])
     assert (out[0, :, 3:] == 3).all() and (out[1, :, 2:] == 3).all()
+
+
+@pytest.mark.parametrize("new,lens,hq,hkv,d,page", [
+    ([300, 1, 7, 900, 0], [300, 1, 7, 900, 40], 8, 2, 128, 16),
+    ([1200, 2, 70], [1200, 1199, 2], 4, 1, 64, 0),                  # two tokens behind as many entries as a prompt has
+    ([600] + [40, 1] * 40, [600] + [40, 1] * 40, 8, 4, 64, 16),     # more than a launch lists
+    ([600] + [1] * 3, [600, 5, 1, 600], 8, 2, 128, 32),             # more short ones than go along
+])
+def test_weights_of_short_prompts_beside_long_ones(new, lens, hq, hkv, d, page):
+    from paper_2607_27600_amd import cc
+    cache, q = Cache16(lens, hkv, d, page=page, seed=93), queries(new, hq, d, 94)
+    lse, want, tol = _oracle(cache, q, new, lens, hq, hkv)
+    n = max(lens)
+    had = [max(0, a - m) for a, m in zip(lens, new)]
+    prev = torch.rand(len(new), hkv, n, generator=torch.Generator().manual_seed(95)).cuda()
+    out = torch.full((len(new), hkv, n), 7.0, device="cuda")
+    cc.cc_attention_weights(problem(cc, new, hq, hkv, d), q, cache.view(cc), 0, i32(lens), n, torch.from_numpy(lse).cuda(), out,
+                            prev=prev, prev_lens=i32(had))
+    torch.cuda.synchronize()
+    for b, m in enumerate(lens):
+        ref = want[b, :, :m].copy()
+        ref[:, :had[b]] += f64(prev)[b, :, :had[b]]
+        assert np.all(np.abs(f64(out)[b, :, :m] - ref) <= tol[b, :, :m] + 2.0 ** -24 * np.abs(ref)), b
+        assert (out[b, :, m:] == 7).all()
