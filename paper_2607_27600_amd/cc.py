@@ -801,6 +801,12 @@ def _queries(p: Problem, q: torch.Tensor, kv: KV, kv_lens: torch.Tensor) -> None
             or not q.is_contiguous()):
         raise ValueError("q must be contiguous bf16 rows [N][Hq][head_dim]")
     _bf16_cache(kv)
+    _rows_of_pages(kv, s.n_seqs)
+
+
+def _rows_of_pages(kv: KV, n: int) -> None:
+    if len(kv.keep) > 2 and kv.keep[2].shape[0] < n:
+        raise ValueError(f"the block table has {kv.keep[2].shape[0]} rows, expected {n}")
 
 
 def _bf16_cache(kv: KV) -> None:
@@ -866,6 +872,7 @@ def prefix(kv: KV, first_seq: Sequence[int], lens: torch.Tensor, max_len: int,
         raise ValueError("first_seq holds where each prefix's sequences start, and where the last one's end")
     _int32(lens, n, "lens")
     _bf16_cache(kv)
+    _rows_of_pages(kv, n)
     first_h = torch.as_tensor(list(first_seq), dtype=torch.int32).contiguous()
     if first_device is None:
         first_d = first_h.to(lens.device)

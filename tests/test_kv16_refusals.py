@@ -300,6 +300,20 @@ def test_binding_weights():
             cc.cc_compact_weights(pe, **{"w": w, "keep_idx": keep, "k": [2, 2], "per_head": 0, **bad})
 
 
+def test_binding_block_tables():
+    """A table with fewer rows than sequences, or prefixes, would be read past its end."""
+    p, q, kv, lens = _host()
+    pool, lse, w = torch.zeros(4, 16, 2, 64, dtype=torch.bfloat16), torch.zeros(3, 4), torch.zeros(2, 2, 8)
+    paged = cc.kv_paged(pool, pool, torch.zeros(1, 1, dtype=torch.int32), n_layers=1, layer_stride=0, page_stride=2048, head_stride=64,
+                        tok_stride=128, page_size=16)
+    x = cc.prefix(paged, [0, 2], lens[:1], 8)
+    for call in (lambda: cc.cc_attention_kv(p, q, paged, 0, lens, 8), lambda: cc.prefix(paged, [0, 1, 2], lens, 8),
+                 lambda: cc.cc_attention_prefix(p, q, x, paged, 0, lens, 8),
+                 lambda: cc.cc_attention_weights(p, q, paged, 0, lens, 8, lse, w)):
+        with pytest.raises(ValueError, match="block table has 1 rows"):
+            call()
+
+
 def test_struct_layouts_match_header(tmp_path):
     import os
     import subprocess
