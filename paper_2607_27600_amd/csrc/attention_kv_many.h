@@ -9,7 +9,7 @@
 // first product carry the exponentials of the tile before, those of the second the packing of P, the row sums and
 // the next maximum.
 //
-// Bound by the clock that the card's power allows: a prompt of 16384, 32 heads on 8, 1.87 to 2.09 ms by box (1.05 to 1.18 PFLOP/s,
+// Bound by the clock that the card's power allows: a prompt of 16384, 32 heads on 8, 1.87 to 2.09 ms by card (1.05 to 1.18 PFLOP/s,
 // matrix cores busy in 66% of the cycles).  Short prompts are bound by what a block takes to begin and end beside its tiles,
 // some 8 us: eight of 1024, 28 heads on 4, 93 us (0.65 PFLOP/s); prompts of 97 to 4001 tokens together 204 to 222 (0.9).  Loads
 // are not what a tile waits for: a barrier between the products, so that each has half a step more to land, took 0 to 10% longer.

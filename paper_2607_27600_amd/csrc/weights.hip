@@ -50,7 +50,9 @@ struct Total {
 // ------------------------------------------------------------------ few rows
 
 // Each wave for 32 entries, whose rows it reads for itself.  Bound by the bytes of the keys: 64 sequences of 4000 entries, 28 heads
-// on 4, 45 us (5.8 TB/s); eight ragged ones of up to 12001 10 us, a chain of four loads.
+// on 4, 45 us (5.8 TB/s); eight ragged ones of up to 12001 10 us, a chain of four loads.  With 16 entries a wave (more
+// workgroups, rows read twice as often) 51 and 9.7, with 64 51 and 10.6; drafts of 8 tokens, 3000 entries, 8 sequences 15.3, 20.5 and
+// 13.8.
 template <int HD, int KB>
 __global__ __launch_bounds__(NT, 2) void weights_few(KvWeightsArgs a) {
   constexpr int NKS = HD / 32;
