@@ -89,6 +89,7 @@ struct KvWeightsArgs {
   int64_t w_seq, w_head, prev_seq, prev_head;
   int n_seqs, layer, max_len, hq, hkv, g, head_dim;
   float c2;
+  int R;                       // most rows of a sequence of few
   // Sequences of more than W_FEW_ROWS rows: list[0 .. n_list), or (listed = 0) all there are.
   int n_list, listed;
   int32_t list[KV_LIST];

@@ -1517,6 +1517,7 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
 // How a call's sequences of many rows are cut.
 struct WeightsPlan {
   bool few = false;            // there are sequences of few rows, or without any
+  int R = 0;                   // most rows of one
   int n = 0, n_list = 0, listed = 0, chunk = W_ROWS, chunks = 1;
   int32_t list[KV_LIST];
   size_t total = 0;
@@ -1533,6 +1534,7 @@ cc_status weights_plan(const cc_problem* p, int max_len, WeightsPlan& c) {
     const int64_t rows = int64_t(m) * g;
     if (rows <= W_FEW_ROWS) {
       c.few = true;
+      c.R = std::max(c.R, int(rows));
       continue;
     }
     if (c.n < KV_LIST) c.list[c.n] = b;
@@ -1668,6 +1670,7 @@ cc_status cc_attention_weights(const cc_problem* p, const void* q, const cc_kv* 
   a.n_list = c.n_list;
   a.listed = c.listed;
   std::copy_n(c.list, c.listed ? c.n : 0, a.list);
+  a.R = c.R;
   a.chunk = c.chunk;
   a.chunks = c.chunks;
   a.part = c.total ? static_cast<float*>(ws) : nullptr;

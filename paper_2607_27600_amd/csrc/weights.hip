@@ -49,10 +49,9 @@ struct Total {
 
 // ------------------------------------------------------------------ few rows
 
-// Each wave for 32 entries, whose rows it reads for itself.  Bound by the bytes of the keys: 64 sequences of 4000 entries, 28 heads
+// Each wave for 32 or 64 entries, whose rows it reads for itself.  Bound by the bytes of the keys: 64 sequences of 4000 entries, 28 heads
 // on 4, 45 us (5.8 TB/s); eight ragged ones of up to 12001 10 us, a chain of four loads.  With 16 entries a wave (more
-// workgroups, rows read twice as often) 51 and 9.7, with 64 51 and 10.6; drafts of 8 tokens, 3000 entries, 8 sequences 15.3, 20.5 and
-// 13.8.
+// workgroups, rows read twice as often) 51 and 9.7, with 64 51 and 10.6.
 template <int HD, int KB>
 __global__ __launch_bounds__(NT, 2) void weights_few(KvWeightsArgs a) {
   constexpr int NKS = HD / 32;
@@ -406,14 +405,21 @@ hipError_t by_sequences(A a, int n, int64_t each, F f) {
 }  // namespace
 
 hipError_t launch_weights_few(const KvWeightsArgs& a, hipStream_t s) {
-  constexpr int KB = 2;
-  const int64_t each = (int64_t(a.max_len) + NW * KB * 16 - 1) / (NW * KB * 16) * a.hkv;
-  return by_sequences(a, a.n_seqs, each, [&](const KvWeightsArgs& x, unsigned grid) {
-    if (a.head_dim == 128)
-      hipLaunchKernelGGL((weights_few<128, KB>), dim3(grid), dim3(NT), 0, s, x);
-    else
-      hipLaunchKernelGGL((weights_few<64, KB>), dim3(grid), dim3(NT), 0, s, x);
-  });
+  auto launch = [&](auto blocks16, auto kernel) {
+    constexpr int SPAN = NW * decltype(blocks16)::value * 16;
+    return by_sequences(a, a.n_seqs, (int64_t(a.max_len) + SPAN - 1) / SPAN * a.hkv, [&](const KvWeightsArgs& x, unsigned grid) {
+      hipLaunchKernelGGL(kernel, dim3(grid), dim3(NT), 0, s, x);
+    });
+  };
+  // Rows of drafts are as many bytes as the entries: 64 of those a wave, so that rows are read half as often, where that
+  // leaves workgroups enough (8 sequences of 8 tokens behind 3000 entries, 32 heads on 8, 13.9 us and 15.4, of 16 16.6 and 20.8; but
+  // one of 8 behind 1000 6.6 and 5.1, and 16 of 3 behind 4000, 28 heads on 4, 19.7 and 18.6).
+  const bool wide = a.R >= 32 && (int64_t(a.max_len) + 255) / 256 * a.hkv * a.n_seqs >= 512;
+  using I2 = std::integral_constant<int, 2>;
+  using I4 = std::integral_constant<int, 4>;
+  if (a.head_dim == 128)
+    return wide ? launch(I4{}, weights_few<128, 4>) : launch(I2{}, weights_few<128, 2>);
+  return wide ? launch(I4{}, weights_few<64, 4>) : launch(I2{}, weights_few<64, 2>);
 }
 
 hipError_t launch_weights_many(const KvWeightsArgs& a, hipStream_t s) {

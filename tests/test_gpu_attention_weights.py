@@ -353,3 +353,24 @@ def test_weights_of_short_prompts_beside_long_ones(new, lens, hq, hkv, d, page):
         ref[:, :had[b]] += f64(prev)[b, :, :had[b]]
         assert np.all(np.abs(f64(out)[b, :, :m] - ref) <= tol[b, :, :m] + 2.0 ** -24 * np.abs(ref)), b
         assert (out[b, :, m:] == 7).all()
+
+
+@pytest.mark.parametrize("new,lens,hq,hkv,d,page", [
+    ([8] * 8, [3000, 17, 64, 65, 1, 2999, 500, 8], 32, 8, 128, 16),       # 64 entries a wave
+    ([32, 1, 0, 5] * 4, [2000, 63, 1999, 4] * 4, 16, 8, 64, 0),
+    ([32], [1000], 2, 1, 64, 16),                                        # 32
+])
+def test_weights_of_drafts(new, lens, hq, hkv, d, page):
+    from paper_2607_27600_amd import cc
+    cache, q = Cache16(lens, hkv, d, page=page, seed=96), queries(new, hq, d, 97)
+    lse, want, tol = _oracle(cache, q, new, lens, hq, hkv)
+    n = max(lens)
+    prev = torch.rand(len(new), hkv, n, generator=torch.Generator().manual_seed(98)).cuda()
+    out = torch.full((len(new), hkv, n), 7.0, device="cuda")
+    cc.cc_attention_weights(problem(cc, new, hq, hkv, d), q, cache.view(cc), 0, i32(lens), n, torch.from_numpy(lse).cuda(), out,
+                            prev=prev)
+    torch.cuda.synchronize()
+    for b, m in enumerate(lens):
+        ref = want[b, :, :m] + f64(prev)[b, :, :m]
+        assert np.all(np.abs(f64(out)[b, :, :m] - ref) <= tol[b, :, :m] + 2.0 ** -24 * np.abs(ref)), b
+        assert (out[b, :, m:] == 7).all()
