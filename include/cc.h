@@ -549,6 +549,7 @@ cc_status cc_attention_weights(const cc_problem* p, const void* q, const cc_kv* 
 
 /* Scores for cc_select_keep from accumulated weights; the problem's cu_seqlens count the entries of each sequence,
  * n_b.  The first p->n_frozen and the last n_recent entries of a sequence score +inf.
+ * (With more of these than the budget, cc_select_keep keeps the first ones of them: equal scores go to the lower index.)
  *   per_head = 0: scores[cu[b] + t] = sum_h w[b][h][t] (fp32, in the order of the heads);
  *   per_head = 1: scores[cu[b]*Hkv + h*n_b + t] = w[b][h][t], a segment for each (sequence, KV head). */
 cc_status cc_weight_scores(const cc_problem* p, const cc_weights* w, int32_t n_recent, int32_t per_head, float* scores,

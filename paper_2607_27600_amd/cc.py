@@ -950,7 +950,8 @@ def cc_attention_weights(p: Problem, q: torch.Tensor, kv: KV, layer: int, kv_len
 def cc_weight_scores(p: Problem, w: torch.Tensor, n_recent: int, per_head: int, scores: Optional[torch.Tensor] = None,
                      stream=None) -> torch.Tensor:
     """Scores for cc_select_keep from weights w [n_seqs][Hkv][entries] (p.cu_seqlens count the entries): one segment for
-    each sequence, or with per_head for each of its KV heads; the first p.n_frozen and the last n_recent are +inf."""
+    each sequence, or with per_head for each of its KV heads; the first p.n_frozen and the last n_recent are +inf (more of these than a budget: the first
+    ones of them are kept)."""
     s = p.struct
     view = _weights(p, w, "w", p.longest)
     n = s.cu_seqlens_h[s.n_seqs] * (s.n_heads_kv if per_head else 1)

@@ -67,7 +67,7 @@ class RefreshLoop:
                  policy: str = "surprise", n_recent: int = 0):
         """cache: "bf16" or "e4m3" (scale_block entries a scale: a power of two from 16 to 128).
         policy: "surprise" (the counter-causal score) or "weight" (accumulated attention, bf16 caches;
-        the last n_recent entries stay)."""
+        the last n_recent entries, J at the most, stay)."""
         if model.mode not in ("last_layer", "last_layer_fused", "last_layer_h"):
             raise ValueError("mode must be last_layer, last_layer_fused or last_layer_h")
         if J < 1 or h < 1:
@@ -84,6 +84,8 @@ class RefreshLoop:
             raise ValueError("attention weights are accumulated over bf16 caches")
         if n_recent < 0 or (n_recent and policy != "weight"):
             raise ValueError("n_recent counts entries that policy weight keeps")
+        if n_recent > J:   # (they score alike, and of those the oldest would stay)
+            raise ValueError(f"n_recent is {n_recent}, a refresh keeps {J} entries")
         self.m, self.J, self.h = model, J, h
         self.cache, self.policy, self.n_recent = cache, policy, n_recent
         self.device = torch.device(device)
