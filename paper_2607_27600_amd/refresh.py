@@ -7,8 +7,8 @@ needs: queries for the given-query fast variant, the activations entering the la
 layer for the exact fast variant).  `refresh` runs one memory-refresh cycle: the
 counter-causal score of every cached entry, selection of the J highest (kept in their
 original order), and compaction of keys, values, ids, positions and rows.  `run_stream`
-drives a prompt and a decode phase, refreshing every h tokens (chunked mode) or once at
-the end of the prompt (prefill-end mode).
+drives a prompt and a decode phase by surprise, refreshing every h tokens (chunked mode) or
+once at the end of the prompt (prefill-end mode).
 
 Everything here is orchestration on the caller's stream; every step of the pass runs in
 libcc.  Entries keep the absolute positions they were appended with.
@@ -238,7 +238,10 @@ def run_stream(loop: RefreshLoop, entry: Callable, T_prompt: int, T_total: int,
     reaches a multiple of h: the prompt is appended in batches up to each refresh point,
     the decode phase one token at a time.  Prefill-end mode appends the whole prompt,
     refreshes once, then decodes without refreshing (the cache must hold the prompt and
-    the decoded tokens)."""
+    the decoded tokens).  It has no queries to attend with, so it drives no loop of policy
+    "weight": that is append, attend in every layer, and refresh."""
+    if loop.policy == "weight":   # (all weights would be 0, and a refresh keep the first entries)
+        raise ValueError("run_stream does not attend, which policy weight selects by")
     h = loop.h
     t = 0
     while t < T_prompt:

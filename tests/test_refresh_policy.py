@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2607_27600_amd.refresh import Model, RefreshLoop
+from paper_2607_27600_amd.refresh import Model, RefreshLoop, run_stream
 
 
 def _model():
@@ -16,3 +16,12 @@ def test_more_recent_entries_than_are_kept(J, recent):
     with pytest.raises(ValueError, match="n_recent"):
         RefreshLoop(_model(), J, 4, device="cpu", policy="weight", n_recent=recent)
     assert RefreshLoop(_model(), J, 4, device="cpu", policy="weight", n_recent=J).n_recent == J
+
+
+def test_a_stream_without_queries():
+    """Without attention every weight is 0, and a refresh would keep the first entries whatever came."""
+    loop, calls = RefreshLoop(_model(), 4, 4, device="cpu", policy="weight"), []
+    for chunked in (True, False):
+        with pytest.raises(ValueError, match="policy weight"):
+            run_stream(loop, lambda t0, t1: calls.append((t0, t1)), 3, 5, chunked=chunked)
+    assert not calls and loop.n == 0
