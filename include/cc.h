@@ -529,6 +529,7 @@ cc_status cc_attention_prefix(const cc_problem* p, const void* q, const cc_prefi
 typedef struct cc_weights {
   float* base;
   int64_t seq_stride, head_stride;
+  int64_t entries;             /* that there are of each; 0: at least as many as the call reaches */
 } cc_weights;
 
 /* Workspace for cc_attention_weights. */
@@ -538,8 +539,8 @@ cc_status cc_attention_weights_workspace(const cc_problem* p, int32_t max_kv_len
  *   out[b][c][t] = prev[b][c][t] + sum_{i, h in group c} exp(scale * q[i][h] . k[t][c] - lse[i][h]),  t < kv_lens[b],
  * over the queries i that attend to entry t; q, kv_lens and max_kv_len as in cc_attention_kv, lse [N][Hq] what
  * it (or cc_attention_prefix: weights of the own entries) returned for the same queries.  prev (nullable: zeros) may
- * be out.  Entries at or past prev_lens[b] (device, nullable: none) have had nothing: prev is not read there, so that
- * entries appended since need no clearing.  Entries past kv_lens[b] are left as they are.  fp32 throughout; only
+ * be out.  Entries at or past prev_lens[b] (device, nullable: none) or past prev's own have had nothing: prev is not read
+ * there, so that entries appended since need no clearing.  Entries past kv_lens[b] are left as they are.  fp32 throughout; only
  * the keys of the cache are read.  One order of summation: the same call repeats bit for bit.  max_kv_len * n_heads_kv
  * is up to 2^30 (some more are taken, others CC_ERR_UNSUPPORTED).  out overlaps nothing else but a prev that is the same. */
 cc_status cc_attention_weights(const cc_problem* p, const void* q, const cc_kv* kv, int32_t layer,

@@ -101,7 +101,7 @@ class c_prefix(ctypes.Structure):
 
 
 class c_weights(ctypes.Structure):
-    _fields_ = [("base", _c_void_p), ("seq_stride", _i64), ("head_stride", _i64)]
+    _fields_ = [("base", _c_void_p), ("seq_stride", _i64), ("head_stride", _i64), ("entries", _i64)]
 
 
 def _load():
@@ -915,7 +915,7 @@ def _weights(p: Problem, w: torch.Tensor, what: str, longest: int, written: bool
         at = sorted((st, n) for st, n in zip((seq, head, entry), shape) if n > 1)
         if written and any(up < st * n for (st, n), (up, _) in zip(at, at[1:])):
             raise ValueError(f"{what} overlaps itself (strides {w.stride()})")
-    return c_weights(w.data_ptr(), seq if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
+    return c_weights(w.data_ptr(), seq if shape[0] > 1 else 0, head if shape[1] > 1 else 0, shape[2])
 
 
 def cc_attention_weights_workspace(p: Problem, max_kv_len: int) -> int:
@@ -927,8 +927,8 @@ def cc_attention_weights(p: Problem, q: torch.Tensor, kv: KV, layer: int, kv_len
                          prev_lens: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                          stream=None) -> torch.Tensor:
     """What each entry receives of the attention of q [N][Hq][d] (lse [N][Hq] as cc_attention_kv filled it), added to
-    prev where that is given (of the first prev_lens[b] entries; all without): out [n_seqs][Hkv][entries], which may
-    be prev."""
+    prev where that is given (of the first prev_lens[b] entries, as far as prev goes; all without): out
+    [n_seqs][Hkv][entries], which may be prev."""
     s = p.struct
     _queries(p, q, kv, kv_lens)
     _lse(p, lse)

@@ -85,6 +85,7 @@ struct KvWeightsArgs {
   const int32_t *cu, *lens;
   const int32_t* prev_lens;    // or null: every entry has some
   const float* prev;           // or null: none has
+  int prev_n;                  // entries that prev holds of a (sequence, KV head)
   float* w;
   int64_t w_seq, w_head, prev_seq, prev_head;
   int n_seqs, layer, max_len, hq, hkv, g, head_dim;

@@ -1573,10 +1573,11 @@ cc_status weights_plan(const cc_problem* p, int max_len, WeightsPlan& c) {
   return CC_OK;
 }
 
-// written: each (sequence, KV head) needs a place of its own.
-cc_status check_weights(const cc_problem* p, const cc_weights* w, bool written) {
+// written: each (sequence, KV head) needs a place of its own.  longest: entries of each that are reached.
+cc_status check_weights(const cc_problem* p, const cc_weights* w, bool written, int longest) {
   if (!w || !w->base) return CC_ERR_ARG;
   if (w->seq_stride < 0 || w->head_stride < 0) return CC_ERR_SHAPE;
+  if (w->entries != 0 && w->entries < longest) return CC_ERR_SHAPE;
   if (written && ((w->seq_stride == 0 && p->n_seqs > 1) || (w->head_stride == 0 && p->n_heads_kv > 1))) return CC_ERR_SHAPE;
   return CC_OK;
 }
@@ -1633,8 +1634,8 @@ cc_status cc_attention_weights(const cc_problem* p, const void* q, const cc_kv* 
                                const cc_weights* out, void* ws, size_t ws_bytes, void* stream) {
   CC_TRY(check_attention_kv(p, max_kv_len));
   CC_TRY(check_view16(p, kv, layer, max_kv_len));
-  CC_TRY(check_weights(p, out, true));
-  if (prev) CC_TRY(check_weights(p, prev, false));
+  CC_TRY(check_weights(p, out, true, max_kv_len));
+  if (prev) CC_TRY(check_weights(p, prev, false, prev_lens ? 0 : max_kv_len));
   if (prev && prev->base == out->base && (prev->seq_stride != out->seq_stride || prev->head_stride != out->head_stride))
     return CC_ERR_ARG;
   if (!prev && prev_lens) return CC_ERR_ARG;
@@ -1653,6 +1654,7 @@ cc_status cc_attention_weights(const cc_problem* p, const void* q, const cc_kv* 
   a.prev_lens = prev_lens;
   if (prev) {
     a.prev = prev->base;
+    a.prev_n = prev->entries ? int(std::min<int64_t>(prev->entries, INT32_MAX)) : INT32_MAX;
     a.prev_seq = prev->seq_stride;
     a.prev_head = prev->head_stride;
   }
@@ -1685,10 +1687,10 @@ cc_status cc_weight_scores(const cc_problem* p, const cc_weights* w, int32_t n_r
   CC_TRY(check_problem(p));
   if (per_head != 0 && per_head != 1) return CC_ERR_ARG;
   if (n_recent < 0) return CC_ERR_ARG;
-  CC_TRY(check_weights(p, w, false));
+  const int longest = max_len(p);
+  CC_TRY(check_weights(p, w, false, longest));
   if (n_tokens(p) == 0) return CC_OK;
   if (!scores) return CC_ERR_ARG;
-  const int longest = max_len(p);
   if ((int64_t(longest) + 255) / 256 * (per_head ? p->n_heads_kv : 1) > MOST_GROUPS) return CC_ERR_UNSUPPORTED;
   const WeightScoresArgs a{w->base, w->seq_stride, w->head_stride, scores, p->cu_seqlens_d, p->n_seqs, p->n_heads_kv,
                            per_head, n_recent, p->n_frozen, longest, 0};
@@ -1701,9 +1703,9 @@ cc_status cc_compact_weights(const cc_problem* p, const cc_weights* w, const int
   CC_TRY(check_problem(p));
   if (per_head != 0 && per_head != 1) return CC_ERR_ARG;
   if (!k_h) return CC_ERR_ARG;
-  CC_TRY(check_weights(p, w, !out));
+  CC_TRY(check_weights(p, w, !out, max_len(p)));
   if (out) {
-    CC_TRY(check_weights(p, out, true));
+    CC_TRY(check_weights(p, out, true, 0));
     if (out->base == w->base) return CC_ERR_ARG;
   }
   const int per = per_head ? p->n_heads_kv : 1;
@@ -1712,6 +1714,7 @@ cc_status cc_compact_weights(const cc_problem* p, const cc_weights* w, const int
   for (int64_t i = 0; i < int64_t(p->n_seqs) * per; ++i) {
     const int b = int(i / per);
     if (k_h[i] < 0 || k_h[i] > p->cu_seqlens_h[b + 1] - p->cu_seqlens_h[b]) return CC_ERR_SHAPE;
+    if (out && out->entries != 0 && k_h[i] > out->entries) return CC_ERR_SHAPE;
     all += k_h[i];
   }
   if (all == 0) return CC_OK;

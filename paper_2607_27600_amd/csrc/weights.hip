@@ -43,7 +43,7 @@ struct Total {
   __device__ __forceinline__ Total(const KvWeightsArgs& a, int b, int kvh, int len)
       : w(a.w + int64_t(b) * a.w_seq + int64_t(kvh) * a.w_head),
         prev(a.prev + int64_t(b) * a.prev_seq + int64_t(kvh) * a.prev_head),
-        had(a.prev ? (a.prev_lens ? a.prev_lens[b] : len) : 0) {}
+        had(a.prev ? min(a.prev_lens ? a.prev_lens[b] : len, a.prev_n) : 0) {}
   __device__ __forceinline__ void put(int t, float x) const { w[t] = t < had ? prev[t] + x : x; }
 };
 

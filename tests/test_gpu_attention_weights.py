@@ -374,3 +374,26 @@ def test_weights_of_drafts(new, lens, hq, hkv, d, page):
         ref = want[b, :, :m] + f64(prev)[b, :, :m]
         assert np.all(np.abs(f64(out)[b, :, :m] - ref) <= tol[b, :, :m] + 2.0 ** -24 * np.abs(ref)), b
         assert (out[b, :, m:] == 7).all()
+
+
+@pytest.mark.parametrize("new,lens,hq,hkv,d,wide", [([1, 3], [900, 40], 8, 2, 128, 500), ([8] * 8, [3000, 17, 64, 65, 1, 2999, 500, 8], 32, 8, 128, 65),
+                                                    ([90, 200], [900, 300], 8, 2, 64, 301), ([700], [700], 4, 1, 128, 1)])
+def test_earlier_weights_end_where_their_tensor_does(new, lens, hq, hkv, d, wide):
+    """Lengths on the device past the tensor of the earlier weights: entries beyond have had nothing."""
+    from paper_2607_27600_amd import cc
+    cache, q = Cache16(lens, hkv, d, page=16, seed=99), queries(new, hq, d, 100)
+    lse, want, tol = _oracle(cache, q, new, lens, hq, hkv)
+    n = max(lens)
+    room = torch.full((len(new), hkv, n + 8), float("nan"), device="cuda")      # (what lies past the earlier weights)
+    room[:, :, :wide] = torch.rand(len(new), hkv, wide, generator=torch.Generator().manual_seed(101)).cuda()
+    prev = room[:, :, :wide]
+    out = torch.full((len(new), hkv, n), 7.0, device="cuda")
+    cc.cc_attention_weights(problem(cc, new, hq, hkv, d), q, cache.view(cc), 0, i32(lens), n, torch.from_numpy(lse).cuda(), out,
+                            prev=prev, prev_lens=i32([10 ** 6] * len(new)))
+    torch.cuda.synchronize()
+    for b, m in enumerate(lens):
+        ref = want[b, :, :m].copy()
+        k = min(m, wide)
+        ref[:, :k] += f64(prev)[b, :, :k]
+        assert np.all(np.abs(f64(out)[b, :, :m] - ref) <= tol[b, :, :m] + 2.0 ** -24 * np.abs(ref)), b
+        assert (out[b, :, m:] == 7).all()

@@ -330,3 +330,20 @@ def test_struct_layouts_match_header(tmp_path):
     for c in classes.values():
         want += [ctypes.sizeof(c), *(getattr(c, f[0]).offset for f in c._fields_)]
     assert got == want
+
+
+def test_entries_of_weights():
+    """Weights that say how many entries they hold are held against what a call reaches; earlier ones with lengths of
+    their own are read as far as they go."""
+    assert _weights(out=_w(entries=199)) == cc.CC_ERR_SHAPE
+    assert _weights(out=_w(entries=-1)) == cc.CC_ERR_SHAPE
+    assert _weights(prev=_w(base=2 * P, entries=199)) == cc.CC_ERR_SHAPE
+    assert _weights(prev=_w(base=2 * P, entries=-1), prev_lens=P) == cc.CC_ERR_SHAPE
+    assert _weights(out=_w(entries=200), prev=_w(base=2 * P, entries=3), prev_lens=P, lse=None) == cc.CC_ERR_ARG     # (as far as lse)
+    assert _scores(w=_w(entries=4)) == cc.CC_ERR_SHAPE
+    assert _compact(w=_w(entries=4)) == cc.CC_ERR_SHAPE
+    assert _compact(out=_w(base=2 * P, entries=1)) == cc.CC_ERR_SHAPE
+    assert _compact(w=_w(entries=5), out=_w(base=2 * P, entries=1), k=(0, 0)) == cc.CC_OK
+    p, _, _, _ = _host()
+    for w in (torch.zeros(2, 2, 8), torch.zeros(2, 2, 16)[:, :, :5], torch.zeros(2, 9, 2).transpose(1, 2)[:, :, :1]):
+        assert cc._weights(p, w, "w", 1).entries == w.shape[2]
