@@ -38,9 +38,16 @@ struct KvAttnArgs {
   // Few rows: sequences list[0 .. n_list), or (listed = 0) all, those of more than `most` rows left out.
   int n_list, listed, R, most; // R: most rows of one
   int direct, parts;           // workgroups that share out the work (attention_shares.h; direct = 0)
-  int32_t list[KV_LIST];
-  // 16 rows a workgroup: entries of a piece (0: rows whole), pieces of the longest sequence, and where their outputs and
-  // (maximum, sum) go, to be joined with the prefixes': [rsplits][N][Hq].
+  union {
+    int32_t list[KV_LIST];
+    int32_t few_at[KV_LIST];   // in the arguments of the pass over the prefixes and of the joins
+  };
+  // Rows of a KV head that sequences of few rows have, in all and before the first sequence of each of KV_LIST groups of
+  // few_per sequences (few_at; few_before).  Results to be joined lie by them, so that they take no place for the other
+  // sequences' rows.
+  int few_rows, few_per, mixed;   // mixed: there are others
+  // 16 rows a workgroup, behind prefixes (0: rows whole): entries of a piece, pieces of the longest sequence, and where their outputs and
+  // (maximum, sum) go, to be joined with the prefixes': [rsplits][few_rows * Hkv], a sequence's [Hkv][rows] together.
   int rpiece, rsplits;
   float* rpart;
   float2* rpart_ml;
@@ -66,12 +73,12 @@ struct KvAttnArgs {
 };
 // 16 rows a workgroup; with n_prefixes the prefix's entries too.
 hipError_t launch_attn_rows(const KvAttnArgs& a, hipStream_t s);
-// Workgroups of that, or of the pieces of it.
+// Workgroups of that, or of the pieces of own entries that go along with the pass over the prefixes.
 inline int64_t rows_groups(const KvAttnArgs& a) {
   return (a.listed ? int64_t(a.n_list) * ((a.R + 15) / 16) : int64_t(a.N) * a.g / 16 + a.n_seqs) * a.hkv *
          (a.rpiece ? a.rsplits : 1);
 }
-// The pass over the prefixes, and with `few` the sequences of few rows, done.
+// The pass over the prefixes (few_at in its arguments), and with `few` the sequences of few rows, done.
 hipError_t launch_attn_prefix(const KvAttnArgs& pass, const KvAttnArgs& own, bool few, hipStream_t s);
 // Few rows, work shared out.
 hipError_t launch_attn_few(const KvAttnArgs& a, hipStream_t s);
@@ -196,6 +203,41 @@ __device__ __forceinline__ PrefixRow prefix_row(const KvAttnArgs& a, int j, int 
   const int2 at = a.pre_at[j];
   const int64_t item = row / KV_ROWS * a.hkv + kvh;
   return PrefixRow{(at.x + item * at.y) * KV_ROWS + row % KV_ROWS, at.y};
+}
+
+// The rows of a KV head that a sequence has if it is one of few rows.
+__device__ __forceinline__ int few_rows_of(const KvAttnArgs& a, int b) {
+  const int64_t rows = int64_t(a.cu[b + 1] - a.cu[b]) * a.g;
+  return rows > FEW_ROWS ? 0 : int(rows);
+}
+// Those of the sequences before b, whose queries begin at q0; alike in a wave.  (Without others it is known: 300 tokens behind
+// a prefix of 16000, 28 heads on 4, 185 us, counted 190.)
+__device__ __forceinline__ int few_before(const KvAttnArgs& a, const int32_t* few_at, int b, int q0) {
+  if (!a.mixed) return q0 * a.g;
+  const int k = b / a.few_per, lane = threadIdx.x & 63;
+  int n = few_at[k];
+  for (int i = k * a.few_per; i < b; i += 64)
+    n += __builtin_amdgcn_readlane(wave_scan(i + lane < b ? few_rows_of(a, i + lane) : 0), 63);
+  return n;
+}
+// The sequence whose rows of that order row f is among, and its first.
+__device__ __forceinline__ int few_at_row(const KvAttnArgs& a, int f, int& first) {
+  const int lane = threadIdx.x & 63;
+  // (groups past the last sequence begin at few_rows, so a row lies in the last group that begins no later)
+  const int k = __builtin_popcountll(__ballot(a.few_at[lane] <= f)) - 1;
+  first = a.few_at[k];
+  int b = k * a.few_per;
+  if (a.few_per == 1) return b;
+  for (;; b += 64) {
+    const int rows = b + lane < a.n_seqs ? few_rows_of(a, b + lane) : 0, sum = wave_scan(rows);
+    const uint64_t past = __ballot(first + sum > f);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      first += __builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(rows, l);
+      return b + l;
+    }
+    first += __builtin_amdgcn_readlane(sum, 63);
+  }
 }
 __device__ __forceinline__ int prefix_of(const KvAttnArgs& a, int b) {
   return last_at(a.n_prefixes, [&](int i) { return int64_t(a.pre_first[i]); }, b);

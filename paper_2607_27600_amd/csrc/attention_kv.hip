@@ -16,7 +16,7 @@ template <int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_rows(KvAttnArgs a) {
   __shared__ float lds[NW * 16 * HD];
   __shared__ float2 ml[NW * 16];
-  rows_group<HD, NW>(a, blockIdx.x, lds, ml);
+  rows_group<HD, NW, false>(a, blockIdx.x, lds, ml);
 }
 
 // ------------------------------------------------------------------ few rows, work shared out

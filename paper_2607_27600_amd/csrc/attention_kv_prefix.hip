@@ -20,7 +20,8 @@ __global__ __launch_bounds__(256, 2) void attn_prefix(KvAttnArgs pass, KvAttnArg
   if (blockIdx.x < groups)
     many::group<HD, PAGED, true>(pass, blockIdx.x, lds, lds + TILE, lds + 2 * TILE, lds + 3 * TILE);
   else
-    rows_group<HD, 4>(own, blockIdx.x - groups, reinterpret_cast<float*>(lds), reinterpret_cast<float2*>(lds + 2 * TILE));
+    rows_group<HD, 4, true>(own, blockIdx.x - groups, reinterpret_cast<float*>(lds), reinterpret_cast<float2*>(lds + 2 * TILE),
+                                pass.few_at);
 }
 
 // Joins what the pass over the prefixes has of a row with its own pieces: a wave a row, whose groups of HD / 8 lanes share out
@@ -29,14 +30,13 @@ template <int HD>
 __global__ __launch_bounds__(256) void attn_rows_join(KvAttnArgs a, int64_t group0) {
   constexpr int LPR = HD / 8, NG = 64 / LPR;
   const int lane = threadIdx.x & 63, gi = lane / LPR, d = (lane % LPR) * 8;
-  const int64_t out = (group0 + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-  if (out >= int64_t(a.N) * a.hq) return;
-  const int query = int(out / a.hq), h = int(out % a.hq), kvh = h / a.g;
-  const int b = last_at(a.n_seqs, [&](int i) { return int64_t(a.cu[i]); }, query);
-  const int q0 = a.cu[b], mq = a.cu[b + 1] - q0;
-  const int64_t rows = int64_t(mq) * a.g;
-  if (rows > a.most) return;
-  const int row = (query - q0) * a.g + h % a.g;
+  const int64_t x = (group0 + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int64_t all = int64_t(a.few_rows) * a.hkv;
+  if (x >= all) return;
+  int first;
+  const int b = few_at_row(a, int(x / a.hkv), first);
+  const int q0 = a.cu[b], mq = a.cu[b + 1] - q0, rows = mq * a.g;
+  const int at_b = int(x - int64_t(first) * a.hkv), kvh = at_b / rows, row = at_b % rows;
   const int own = max(rows_see(a, mq, min(max(a.lens[b], 0), a.max_len), row & ~15) - 1, 0) / a.rpiece + 1;
   const int j = prefix_of(a, b);
   const PrefixRow p = prefix_row(a, j, kvh, int64_t(q0 - a.cu[a.pre_first[j]]) * a.g + row);
@@ -50,12 +50,12 @@ __global__ __launch_bounds__(256) void attn_rows_join(KvAttnArgs a, int64_t grou
     for (int q = 0; q < 4; ++q) {
       const int i = min(i0 + q * NG, n - 1);
       const bool pre = i < p.n;
-      const int64_t at = pre ? p.first + int64_t(i) * KV_ROWS : int64_t(i - p.n) * a.N * a.hq + out;
-      const float* x = (pre ? a.ppart : a.rpart) + at * HD + d;
+      const int64_t at = pre ? p.first + int64_t(i) * KV_ROWS : int64_t(i - p.n) * all + x;
+      const float* from = (pre ? a.ppart : a.rpart) + at * HD + d;
       in[q] = i0 + q * NG < n;
       ml[q] = (pre ? a.ppart_ml : a.rpart_ml)[at];
-      y[0][q] = *reinterpret_cast<const float4*>(x);
-      y[1][q] = *reinterpret_cast<const float4*>(x + 4);
+      y[0][q] = *reinterpret_cast<const float4*>(from);
+      y[1][q] = *reinterpret_cast<const float4*>(from + 4);
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) g[k].add(ml, [&](int q) { return y[k][q]; }, in, a.c2);
@@ -91,13 +91,15 @@ hipError_t launch_attn_prefix(const KvAttnArgs& pass, const KvAttnArgs& own, boo
     pass.own.paged ? launch(attn_prefix<64, true>) : launch(attn_prefix<64, false>);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !few) return e;
-  const int64_t waves = (int64_t(own.N) * own.hq + 3) / 4;
+  KvAttnArgs join = own;
+  std::copy_n(pass.few_at, KV_LIST, join.few_at);
+  const int64_t waves = (int64_t(own.few_rows) * own.hkv + 3) / 4;
   for (int64_t g0 = 0; g0 < waves; g0 += MOST_GROUPS) {
     const dim3 grid(unsigned(std::min(MOST_GROUPS, waves - g0)));
     if (own.head_dim == 128)
-      hipLaunchKernelGGL(attn_rows_join<128>, grid, dim3(256), 0, s, own, g0);
+      hipLaunchKernelGGL(attn_rows_join<128>, grid, dim3(256), 0, s, join, g0);
     else
-      hipLaunchKernelGGL(attn_rows_join<64>, grid, dim3(256), 0, s, own, g0);
+      hipLaunchKernelGGL(attn_rows_join<64>, grid, dim3(256), 0, s, join, g0);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   return hipSuccess;

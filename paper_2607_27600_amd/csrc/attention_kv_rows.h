@@ -328,16 +328,17 @@ __device__ __forceinline__ int rows_see(const KvAttnArgs& a, int mq, int len, in
   return max(0, len - mq + (min(row0 + 16, mq * a.g) - 1) / a.g + 1);
 }
 
-// One workgroup for 16 rows of a (sequence, KV head), or a piece of their entries: its NW waves share out the entries, the prefix's and the sequence's.
-// lds: [NW][16][HD] outputs, ml: [NW][16] (max, sum).
-template <int HD, int NW>
-__device__ __forceinline__ void rows_group(const KvAttnArgs& a, unsigned group, float* lds, float2* ml) {
+// One workgroup for 16 rows of a (sequence, KV head): its NW waves share out the entries, the prefix's and the sequence's, or
+// (PIECES) a piece of the sequence's, to be joined.  lds: [NW][16][HD] outputs, ml: [NW][16] (max, sum).
+template <int HD, int NW, bool PIECES>
+__device__ __forceinline__ void rows_group(const KvAttnArgs& a, unsigned group, float* lds, float2* ml,
+                                           const int32_t* few_at = nullptr) {
   constexpr int ROWS = 16;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   const int kvh = int(group % unsigned(a.hkv));
   int64_t x = group / unsigned(a.hkv);
   int split = 0;
-  if (a.rpiece) {
+  if constexpr (PIECES) {
     split = int(x % a.rsplits);
     x /= a.rsplits;
   }
@@ -356,7 +357,7 @@ __device__ __forceinline__ void rows_group(const KvAttnArgs& a, unsigned group, 
   if (row0 >= rows || rows > a.most) return;
   const int len = min(max(a.lens[b], 0), a.max_len), shift = len - mq;
   const int most = rows_see(a, mq, len, row0);
-  if (split > 0 && split * a.rpiece >= most) return;
+  if (PIECES && split > 0 && split * a.rpiece >= most) return;
   Rows<HD, 1> st;
   int i[1];
   load_queries(a, st, q0, kvh, row0, rows, i);
@@ -367,7 +368,7 @@ __device__ __forceinline__ void rows_group(const KvAttnArgs& a, unsigned group, 
     ge = min(g1, gb + per);
   };
   int gb, ge;
-  if (a.n_prefixes && !a.rpiece) {
+  if (!PIECES && a.n_prefixes) {
     const int j = prefix_of(a, b);
     const int n = min(max(a.pre_lens[j], 0), a.pre_max);
     const int past[1] = {n};
@@ -375,11 +376,13 @@ __device__ __forceinline__ void rows_group(const KvAttnArgs& a, unsigned group, 
     st.template run<false>(a, kv_plane(a.pre, j, a.layer, kvh), gb, ge, n, past, n);
   }
   const int past[1] = {max(0, shift + i[0] + 1)};
-  part(split * a.rpiece >> 4, (a.rpiece ? min(most, (split + 1) * a.rpiece) + 15 : most + 15) >> 4, gb, ge);
+  part(PIECES ? split * a.rpiece >> 4 : 0, (PIECES ? min(most, (split + 1) * a.rpiece) + 15 : most + 15) >> 4, gb, ge);
   st.template run<false>(a, kv_plane(a.own, b, a.layer, kvh), gb, ge, len, past, max(0, shift + row0 / a.g + 1));
+  const int64_t place =
+      PIECES ? (int64_t(split) * a.few_rows + few_before(a, few_at, b, q0)) * a.hkv + int64_t(kvh) * rows + row0 : 0;
   meet<HD, 1, NW>(a, st, lds, ml, min(ROWS, rows - row0), [&](int r, int d, float M, float L, float4(&o)[2]) {
-    if (!a.rpiece) return finish<HD>(a, q0, kvh, row0 + r, d, M, L, o);
-    const int64_t at = (int64_t(split) * a.N + q0 + (row0 + r) / a.g) * a.hq + kvh * a.g + (row0 + r) % a.g;
+    if constexpr (!PIECES) return finish<HD>(a, q0, kvh, row0 + r, d, M, L, o);
+    const int64_t at = place + r;
     float* po = a.rpart + at * HD + d;
     *reinterpret_cast<float4*>(po) = o[0];
     *reinterpret_cast<float4*>(po + 4) = o[1];

@@ -1335,6 +1335,8 @@ struct KvPlan {
   int n_few = 0, n_list = 0, listed = 0, R = 0, parts = 0;
   bool direct = false;         // few rows: by 16 rows a workgroup
   int32_t list[KV_LIST];
+  int few_rows = 0, few_per = 1;   // of a KV head, and where groups of few_per sequences begin among them
+  int32_t few_at[KV_LIST];
   int rpiece = 0, rsplits = 1; // behind prefixes: entries of a piece of those (0: whole)
   size_t fpart = 0, fat = 0, ftotal = 0;
   KvMany many;
@@ -1374,18 +1376,22 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
   c.along = !x && !c.rows && few <= 8 * many && max_len <= ::max_len(p);
   c.ends = int(few * hkv);
   c.inside = x && c.rows;
+  c.few_per = (p->n_seqs + KV_LIST - 1) / KV_LIST;
   for (int b = 0; b < p->n_seqs; ++b) {
+    if (b % c.few_per == 0) c.few_at[b / c.few_per] = c.few_rows;
     const int seq0 = p->cu_seqlens_h[b], m = p->cu_seqlens_h[b + 1] - seq0;
     const int64_t rows = int64_t(m) * g;
     if (rows == 0) continue;
     if ((rows <= FEW_ROWS && !c.along) || c.rows) {
       if (c.n_few < KV_LIST) c.list[c.n_few] = b;
       ++c.n_few;
+      c.few_rows += int(rows);
       c.R = int(std::max<int64_t>(c.R, rows));
     } else {
       c.many.add(b, seq0, m, g);
     }
   }
+  std::fill(c.few_at + (p->n_seqs + c.few_per - 1) / c.few_per, c.few_at + KV_LIST, c.few_rows);
   const int64_t walked = int64_t(n_tokens(p)) * g / 16 + p->n_seqs;
   c.direct = c.rows || max_len <= kv_direct(int64_t(c.n_few) * hkv);
   // (listed sequences have the blocks of the longest)
@@ -1397,7 +1403,7 @@ cc_status kv_plan(const cc_problem* p, const cc_prefix* x, int max_len, KvPlan& 
     c.direct = true;
     c.rpiece = std::max(KV_OWN, int((int64_t(max_len) + 32 * 16 - 1) / (32 * 16) * 16));
     c.rsplits = std::max(1, int((int64_t(max_len) + c.rpiece - 1) / c.rpiece));
-    const size_t rows = size_t(c.rsplits) * p->n_heads_q * n_tokens(p);
+    const size_t rows = size_t(c.rsplits) * c.few_rows * hkv;
     c.fpart = align_up(rows * p->head_dim * sizeof(float));
     c.ftotal = c.fpart + align_up(rows * sizeof(float2));
   } else if (c.n_few && !c.direct) {
@@ -1491,6 +1497,9 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
     a.most = c.rows ? INT32_MAX : FEW_ROWS;
     a.parts = c.parts;
     std::copy_n(c.list, c.listed ? c.n_few : 0, a.list);
+    a.few_rows = c.few_rows;
+    a.few_per = c.few_per;
+    a.mixed = c.few_rows != N * a.g;
     a.rpiece = c.rpiece;
     a.rsplits = c.rsplits;
     (c.rpiece ? a.rpart : a.fpart) = c.ftotal ? reinterpret_cast<float*>(at(ws, off)) : nullptr;
@@ -1506,6 +1515,7 @@ cc_status run_attention_kv(const cc_problem* p, const void* q, const cc_prefix* 
     pass.n_seqs = a.n_prefixes;
     pass.blocks = int(c.pre_blocks);
     pass.slots = KV_SLOTS;
+    std::copy_n(c.few_at, KV_LIST, pass.few_at);
     CC_HIP(launch_attn_prefix(pass, a, c.n_few > 0, st));
   } else if (c.n_few) {
     CC_HIP(c.direct ? launch_attn_rows(a, st) : launch_attn_few(a, st));

@@ -480,3 +480,32 @@ def test_short_prompts_beside_long_ones(new, lens, hq, hkv, d, page, more):
     q = queries(new, hq, d, 92)
     want = _oracle(cache, q, new, lens, hq, hkv)
     _same(*_run(cc, cache, q, new, lens, hq, hkv, longest=max(lens) + more), want)
+
+
+MIXED_PREFIXES = [
+    # prefix lens, first, new, lens, hq, hkv, d, page: few rows in pieces, among others, more sequences than a wave has lanes
+    ([700, 1500], [0, 60, 150], [1, 40, 0, 2, 1] * 30, [1 + 41 * i % 1400 for i in range(150)], 4, 2, 64, 16),
+    ([2000], [0, 90], [0] * 30 + [300] + [1, 3] * 29 + [0], [5] * 30 + [300] + [3 + 57 * i % 2100 for i in range(58)] + [9], 8, 2, 128, 64),
+    ([1100], [0, 5], [1, 0, 500, 4, 1], [1900, 7, 500, 40, 1100], 28, 4, 128, 0),
+    ([1200, 0], [0, 200, 300], [0] * 130 + [2] * 100 + [33] * 5 + [0] * 65, [1 + 11 * i % 900 for i in range(300)], 4, 1, 64, 16),
+]
+
+
+@pytest.mark.parametrize("case", MIXED_PREFIXES, ids=[str(i) for i in range(len(MIXED_PREFIXES))])
+def test_few_rows_beside_many_behind_a_prefix(case):
+    """The workspace holds no more than asked for, whose results to be joined are those of the few rows alone."""
+    from paper_2607_27600_amd import cc
+    pl, first, new, lens, hq, hkv, d, page = case
+    print(f"[prefix mixed] {case[:2]} {hq} {hkv} {d} {page}", flush=True)
+    cache = Cache16(lens, hkv, d, page=page, seed=103)
+    pre = Cache16(pl, hkv, d, page=16 if page else 0, seed=104)
+    q = queries(new, hq, d, 105)
+    p, kv, x = problem(cc, new, hq, hkv, d), cache.view(cc), cc.prefix(pre.view(cc), first, i32(pl), max(pl))
+    want = _oracle(cache, q, new, lens, hq, hkv, pre=pre, first=first, pre_lens=pl)
+    size = cc.cc_attention_prefix_workspace(p, x, max(lens))
+    ws = torch.full((size + 4096,), 0x7f, dtype=torch.uint8, device="cuda")
+    o, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    cc.cc_attention_prefix(p, q, x, kv, 0, i32(lens), max(lens), o, lse=lse, workspace=ws[:size])
+    torch.cuda.synchronize()
+    _same(o, lse, want)
+    assert (ws[size:] == 0x7f).all()

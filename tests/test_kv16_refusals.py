@@ -347,3 +347,20 @@ def test_entries_of_weights():
     p, _, _, _ = _host()
     for w in (torch.zeros(2, 2, 8), torch.zeros(2, 2, 16)[:, :, :5], torch.zeros(2, 9, 2).transpose(1, 2)[:, :, :1]):
         assert cc._weights(p, w, "w", 1).entries == w.shape[2]
+
+
+def _bytes_behind(new, prefix, longest, hq, hkv):
+    n, p = ctypes.c_size_t(0), _problem(cu=[sum(new[:i]) for i in range(len(new) + 1)], n_heads_q=hq, n_heads_kv=hkv)
+    x = _prefix(first=(0, len(new)), max_len=prefix)
+    assert cc._lib.cc_attention_prefix_workspace(_ref(p), _ref(x), longest, ctypes.byref(n)) == cc.CC_OK
+    return n.value
+
+
+@pytest.mark.parametrize("few,many,longest,hq,hkv", [([1], [8000], 16384, 32, 8), ([1] * 40, [8192], 16384, 28, 4),
+                                                     ([1] * 40, [16000], 32768, 32, 8), ([6] * 24, [40] * 3, 8000, 32, 8),
+                                                     ([1] * 200, [3000, 100], 16384, 28, 4)])
+def test_workspace_of_tokens_beside_prompts_behind_a_prefix(few, many, longest, hq, hkv):
+    """What one call of both needs is no more than two calls need (results to be joined are those of the rows that have pieces)."""
+    alone = _bytes_behind(few, 16000, longest, hq, hkv) + _bytes_behind(many, 16000, longest, hq, hkv)
+    for new in (few + many, many + few, few[:1] + many + few[1:]):
+        assert _bytes_behind(new, 16000, longest, hq, hkv) <= alone + 4096
