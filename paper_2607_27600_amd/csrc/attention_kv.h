@@ -40,7 +40,7 @@ struct KvAttnArgs {
   int direct, parts;           // workgroups that share out the work (attention_shares.h; direct = 0)
   union {
     int32_t list[KV_LIST];
-    int32_t few_at[KV_LIST];   // in the arguments of the pass over the prefixes and of the joins
+    int32_t few_at[KV_LIST];   // in the arguments of the pass over the prefixes, of the joins and of many rows
   };
   // Rows of a KV head that sequences of few rows have, in all and before the first sequence of each of KV_LIST groups of
   // few_per sequences (few_at; few_before).  Results to be joined lie by them, so that they take no place for the other
@@ -59,7 +59,9 @@ struct KvAttnArgs {
   AttnMany items;
   int blocks, few, ends;       // ends: row blocks * Hkv of listed sequences of few rows
   int piece, splits;           // entries of a piece (a multiple of KV_KEYS), pieces of the longest sequence
-  // Results to be joined (null: none), outputs and (maximum, sum): [splits][Hkv][N g]
+  // Results to be joined (null: none), outputs and (maximum, sum): [Hkv][places][splits], of the rows from row0 on, or with
+  // `skip` of all but those of sequences of few
+  int row0, places, skip;
   float* part;
   float2* part_ml;
   // The pass over the prefixes: they stand for sequences, and own, lens and n_seqs are theirs.  Its pieces

@@ -500,9 +500,10 @@ __device__ __forceinline__ void group(const KvAttnArgs& a, unsigned x, u16* kb0,
     }
   }
   if (a.part || SHARED) {
+    const int before = SHARED ? 0 : a.skip ? few_before(a, a.few_at, b, q0) : a.row0;
     if (valid) {
       const int64_t prow = SHARED ? int64_t(nth) * KV_ROWS + wave * ROWS_W + col
-                                    : (int64_t(split) * a.hkv + kvh) * (int64_t(a.N) * a.g) + int64_t(q0) * a.g + row;
+                                  : (int64_t(kvh) * a.places + q0 * a.g - before + row) * a.splits + split;
       float* po = (SHARED ? a.ppart : a.part) + prow * HD + 4 * hi;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)

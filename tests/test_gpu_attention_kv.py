@@ -509,3 +509,26 @@ def test_few_rows_beside_many_behind_a_prefix(case):
     torch.cuda.synchronize()
     _same(o, lse, want)
     assert (ws[size:] == 0x7f).all()
+
+
+@pytest.mark.parametrize("new,most,hq,hkv,d,page", [([1] * 20 + [40] + [1, 0, 2] * 10, 5000, 4, 1, 128, 16),
+                                                    ([2] * 100 + [70] + [1, 0] * 30, 4000, 8, 2, 64, 64),        # more than a wave has lanes
+                                                    ([0] * 70 + [1] * 90 + [33, 300] + [3] * 140, 6000, 4, 1, 64, 0),
+                                                    ([1, 40] * 18 + [1] * 300, 3000, 2, 1, 128, 32)])            # more than a launch lists
+def test_pieces_beside_few_rows(new, most, hq, hkv, d, page):
+    """Chunks in pieces among single tokens and drafts: the workspace holds no more than asked for, whose results to be joined
+    are those of the chunks alone."""
+    from paper_2607_27600_amd import cc
+    lens = [most - 3 * i if m * hq // hkv > 32 else m + 7 * i % 60 for i, m in enumerate(new)]
+    print(f"[attn16 mixed] {len(new)} {most} {hq} {hkv} {d} {page}", flush=True)
+    cache = Cache16(lens, hkv, d, page=page, seed=106, fill=0.0)
+    q = queries(new, hq, d, 107)
+    p = problem(cc, new, hq, hkv, d)
+    most = max(lens)
+    size = cc.cc_attention_kv_workspace(p, most)
+    ws = torch.full((size + 4096,), 0x7f, dtype=torch.uint8, device="cuda")
+    o, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    cc.cc_attention_kv(p, q, cache.view(cc), 0, i32(lens), most, o, lse=lse, workspace=ws[:size])
+    torch.cuda.synchronize()
+    _same(o, lse, _oracle(cache, q, new, lens, hq, hkv))
+    assert (ws[size:] == 0x7f).all()

@@ -364,3 +364,20 @@ def test_workspace_of_tokens_beside_prompts_behind_a_prefix(few, many, longest, 
     alone = _bytes_behind(few, 16000, longest, hq, hkv) + _bytes_behind(many, 16000, longest, hq, hkv)
     for new in (few + many, many + few, few[:1] + many + few[1:]):
         assert _bytes_behind(new, 16000, longest, hq, hkv) <= alone + 4096
+
+
+def _bytes_of(new, longest, hq, hkv):
+    n, p = ctypes.c_size_t(0), _problem(cu=[sum(new[:i]) for i in range(len(new) + 1)], n_heads_q=hq, n_heads_kv=hkv)
+    assert cc._lib.cc_attention_kv_workspace(_ref(p), longest, ctypes.byref(n)) == cc.CC_OK
+    return n.value
+
+
+@pytest.mark.parametrize("few,many,longest,hq,hkv", [([1] * 1000, [16], 16384, 32, 8), ([1] * 128, [16], 16384, 28, 4),
+                                                     ([2] * 300, [40, 33], 5000, 8, 2), ([1, 0] * 4000, [9] * 30, 60000, 4, 1)])
+def test_workspace_of_tokens_beside_a_chunk(few, many, longest, hq, hkv):
+    """What one call of both needs is no more than two calls need (results to be joined are those of the rows that are cut), but
+    for what the few rows' shares need of every sequence: outputs, (maximum, sum) and a pair of whole numbers."""
+    alone = _bytes_of(few, longest, hq, hkv) + _bytes_of(many, longest, hq, hkv)
+    alone += len(many) * hkv * (max(few) * hq // hkv * (4 * 128 + 8) + 8)
+    for new in (few + many, many + few, few[:7] + many + few[7:]):
+        assert _bytes_of(new, longest, hq, hkv) <= alone + 4096
