@@ -532,3 +532,32 @@ def test_pieces_beside_few_rows(new, most, hq, hkv, d, page):
     torch.cuda.synchronize()
     _same(o, lse, _oracle(cache, q, new, lens, hq, hkv))
     assert (ws[size:] == 0x7f).all()
+
+
+@pytest.mark.parametrize("new,most,hq,hkv,d", [([16] + [1] * 50 + [16], 4000, 28, 4, 128), ([0, 40] + [1] * 200 + [40, 9, 2], 3000, 4, 1, 64),
+                                               ([1] * 70 + [33, 2] * 2 + [3, 0, 1] * 60 + [50] + [1] * 5, 3000, 8, 2, 128)])
+@pytest.mark.parametrize("prefix", [0, 1500])
+def test_chunks_in_pieces_on_either_side_of_tokens(new, most, hq, hkv, d, prefix):
+    """More rows of single tokens between the first and the last chunk than the chunks have: places for the chunks' alone."""
+    from paper_2607_27600_amd import cc
+    g = hq // hkv
+    lens = [most - 5 * (i % 40) if m * g > 32 else m + 7 * i % 60 for i, m in enumerate(new)]
+    print(f"[attn16 scattered] {len(new)} {most} {hq} {hkv} {d} {prefix}", flush=True)
+    cache, q, p = Cache16(lens, hkv, d, page=16, seed=108, fill=0.0), queries(new, hq, d, 109), problem(cc, new, hq, hkv, d)
+    most, kw = max(lens), {}
+    o, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    if prefix:
+        pre = Cache16([prefix], hkv, d, page=16, seed=110)
+        kw = dict(pre=pre, first=[0, len(new)], pre_lens=[prefix])
+        x = cc.prefix(pre.view(cc), [0, len(new)], i32([prefix]), prefix)
+        size = cc.cc_attention_prefix_workspace(p, x, most)
+    else:
+        size = cc.cc_attention_kv_workspace(p, most)
+    ws = torch.full((size + 4096,), 0x7f, dtype=torch.uint8, device="cuda")
+    if prefix:
+        cc.cc_attention_prefix(p, q, x, cache.view(cc), 0, i32(lens), most, o, lse=lse, workspace=ws[:size])
+    else:
+        cc.cc_attention_kv(p, q, cache.view(cc), 0, i32(lens), most, o, lse=lse, workspace=ws[:size])
+    torch.cuda.synchronize()
+    _same(o, lse, _oracle(cache, q, new, lens, hq, hkv, **kw))
+    assert (ws[size:] == 0x7f).all()
