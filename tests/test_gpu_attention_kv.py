@@ -561,3 +561,28 @@ def test_chunks_in_pieces_on_either_side_of_tokens(new, most, hq, hkv, d, prefix
     torch.cuda.synchronize()
     _same(o, lse, _oracle(cache, q, new, lens, hq, hkv, **kw))
     assert (ws[size:] == 0x7f).all()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("new,n,prefix", [([4], 900, 0), ([150], 700, 0), ([40], 5000, 0), ([1, 200, 3], 300, 1500), ([2, 70], 90, 2000)])
+@pytest.mark.parametrize("d", [128, 64])
+def test_a_key_that_is_not_finite_and_seen_by_all(new, n, prefix, d, value):
+    """NaN logits spoil their rows, infinite ones those that they draw; what they repel sees the other entries."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, lens = 4, 2, [n] * len(new)
+    cache, q = Cache16(lens, hkv, d, page=16, seed=111), queries(new, hq, d, 112)
+    kw = dict(pre=Cache16([prefix], hkv, d, page=16, seed=113), first=[0, len(new)], pre_lens=[prefix]) if prefix else {}
+    clean, clean_lse, tol = _oracle(cache, q, new, lens, hq, hkv, **kw)
+    where = kw["pre"] if prefix else cache
+    for b in range(len(where.lens)):
+        where.put(0, b, 1, "k", 37, 5, value)
+    o, lse = (f64(x) for x in _run(cc, cache, q, new, lens, hq, hkv, **kw))
+    # the entry's logit, of the second KV head's rows: NaN, drawn (+inf) or repelled (-inf)
+    z = f64(q)[:, 2:, 5] * value
+    spoilt = np.zeros(lse.shape, bool)
+    spoilt[:, 2:] = ~np.isneginf(z)
+    np.testing.assert_array_equal(np.isnan(lse), spoilt)
+    np.testing.assert_array_equal(np.isnan(o), np.broadcast_to(spoilt[..., None], o.shape))
+    want, rl, _ = _oracle(cache, q, new, lens, hq, hkv, **kw)
+    assert_attention_close(np.where(spoilt[..., None], 0, o), np.where(spoilt[..., None], 0, want))
+    assert np.all(np.abs(lse - rl)[~spoilt] <= (tol + 2.0 ** -22 * (1 + np.abs(clean_lse)))[~spoilt])
