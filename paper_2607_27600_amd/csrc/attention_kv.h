@@ -37,7 +37,8 @@ struct KvAttnArgs {
   float room;                  // how far a logit may pass a row's reference maximum: 2^8 in probability
   // Few rows: sequences list[0 .. n_list), or (listed = 0) all, those of more than `most` rows left out.
   int n_list, listed, R, most; // R: most rows of one
-  int direct, parts;           // workgroups that share out the work (attention_shares.h; direct = 0)
+  static constexpr int direct = 0;   // (short caches have a launch of their own)
+  int parts;                   // workgroups that share out the work (attention_shares.h)
   union {
     int32_t list[KV_LIST];
     int32_t few_at[KV_LIST];   // in the arguments of the pass over the prefixes, of the joins and of many rows
