@@ -586,3 +586,32 @@ def test_a_key_that_is_not_finite_and_seen_by_all(new, n, prefix, d, value):
     want, rl, _ = _oracle(cache, q, new, lens, hq, hkv, **kw)
     assert_attention_close(np.where(spoilt[..., None], 0, o), np.where(spoilt[..., None], 0, want))
     assert np.all(np.abs(lse - rl)[~spoilt] <= (tol + 2.0 ** -22 * (1 + np.abs(clean_lse)))[~spoilt])
+
+
+@pytest.mark.parametrize("prefix", [0, 1100])
+def test_thousands_of_sequences(prefix):
+    """More sequences than 64 groups of 64: tokens and drafts among sequences without queries, between chunks that are planned
+    in pieces."""
+    from paper_2607_27600_amd import cc
+    hq, hkv, d, n = 4, 1, 64, 5000
+    r = np.random.default_rng(114)
+    new = [int(x) for x in r.choice([0, 0, 0, 1, 2], n)]
+    for b in (3, 64, 4097, 4990):
+        new[b] = 33 + b % 7
+    lens = [m + int(x) for m, x in zip(new, r.integers(0, 25, n))]
+    cache, q, p = Cache16(lens, hkv, d, seed=115, fill=0.0), queries(new, hq, d, 116), problem(cc, new, hq, hkv, d)
+    kw = dict(pre=Cache16([prefix], hkv, d, page=16, seed=117), first=[0, n], pre_lens=[prefix]) if prefix else {}
+    longest = 5000                       # (a contiguous cache may be planned for more than its sequences have)
+    size = cc.cc_attention_kv_workspace(p, longest)
+    if prefix:
+        x = cc.prefix(kw["pre"].view(cc), [0, n], i32([prefix]), prefix)
+        size = cc.cc_attention_prefix_workspace(p, x, longest)
+    ws = torch.full((size + 4096,), 0x7f, dtype=torch.uint8, device="cuda")
+    o, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    if prefix:
+        cc.cc_attention_prefix(p, q, x, cache.view(cc), 0, i32(lens), longest, o, lse=lse, workspace=ws[:size])
+    else:
+        cc.cc_attention_kv(p, q, cache.view(cc), 0, i32(lens), longest, o, lse=lse, workspace=ws[:size])
+    torch.cuda.synchronize()
+    _same(o, lse, _oracle(cache, q, new, lens, hq, hkv, **kw))
+    assert (ws[size:] == 0x7f).all()
