@@ -195,6 +195,8 @@ __device__ __forceinline__ void group(const KvAttnArgs& a, unsigned x, u16* kb0,
       // (the list's items begin with the first blocks)
       rb = int((int64_t(m) * a.g + KV_ROWS - 1) / KV_ROWS) - 1 - w.rb;
     } else {
+      // More sequences than are listed: by number, the last rows of the last one first, and a block without rows for each (16
+      // prompts of 40 to 2500, 28 heads on 4, 303 us for a floor of 170; 32, which are walked, 447 for 245).
       kvh = int(x % unsigned(a.hkv));
       const int at = a.blocks - 1 - int(x / unsigned(a.hkv));
       auto first_block = [&](int b) { return int64_t(a.cu[b]) * a.g / KV_ROWS + b; };

@@ -1324,8 +1324,8 @@ struct KvMany {
     splits = std::max(1, int((int64_t(max_len) + piece - 1) / piece));
     if (splits > 1) {
       // From the first row to the last; where more of these than not are of sequences of few, those are left out: to find a
-      // row costs more then (128 tokens between two chunks of 16 behind 16000 entries, 32 heads on 8, 107.2 us and 104.8, but
-      // 17 MB in place of 85).
+      // row takes some 2 us more then (128 tokens between two chunks of 16 behind 16000 entries, 32 heads on 8, 107.2 us and
+      // 104.8, but 17 MB in place of 85).
       skip = places > 2 * rows;
       if (skip) {
         row0 = 0;
